@@ -334,6 +334,148 @@ const char* accordion_stage_name(int32_t stage);
  * Errors: ACC_EINVAL, ACC_EHIP (message via accordion_last_error(NULL)). */
 int32_t accordion_probe_copy(float* dst_dev, const float* src_dev, int64_t n, void* hip_stream);
 
+/* --- operators of a language model's training step around the compression path -----------------
+ * Forward and backward pass of three layers of a recurrent language model, whose gradients the
+ * path compresses, and the AdamW step that consumes its averaged gradient.  They need no context.
+ *
+ * Conventions, besides those at the top of this file:
+ *  - Activations and their gradients are fp32 or bf16 (ACC_FLOAT, ACC_BF16); parameters' gradients,
+ *    statistics and states are fp32.  All arithmetic, sums and states are fp32; what is stored as
+ *    bf16 is rounded once, to nearest even.
+ *  - DEVICE pointers need the alignment of their element type only; rows may start anywhere and lie
+ *    apart by a stride (in elements, at least the row's length unless there is one row at most);
+ *    a row's own elements are contiguous.  Buffers that are written must not overlap any other buffer.
+ *  - Every call enqueues its kernels on hip_stream (NULL = the default stream) and returns without
+ *    waiting.  It allocates nothing and keeps nothing: a call that needs memory takes a workspace of
+ *    at least ..._workspace_bytes() bytes (256-byte aligned), whose contents mean nothing before and
+ *    after.  Work on one workspace must be ordered.  Every call may be captured into a HIP graph (what
+ *    the host passes by value, step and learning rate among it, is frozen into the graph).
+ *  - The order of every sum is fixed: the same call gives the same bits.
+ *  - Empty inputs (no tokens, rows, steps or sequences) are valid.
+ *  - Nothing is launched when an argument is refused.  Errors: ACC_EINVAL, ACC_ENOSPACE (workspace),
+ *    ACC_EHIP; accordion_operator_error() describes the last failure of the calling thread. */
+enum { ACC_FLOAT = 0, ACC_BF16 = 1 };
+
+const char* accordion_operator_error(void);
+
+/* Embedding lookup with scaling.
+ *   forward:   out[t, :] = scale * table[id_t, :]
+ *   backward:  grad_table[v, :] = scale * sum over { t : id_t = v } of grad_out[t, :]   (ascending t)
+ * An id outside [0, vocab) gives a row of zeros and takes no part in the gradient (padding).
+ * grad_table is dense fp32, as the compressors take it: rows without a token become zeros, or, with
+ * accumulate, stay as they are and the sums are added (a table shared with the decoder). */
+typedef struct acc_embedding {
+  int64_t vocab, dim, tokens;    /* vocab in [1, 2^31 - 2], dim in [1, 2^24], tokens in [0, 2^28] */
+  int64_t table_stride;          /* rows of table / grad_table */
+  int64_t out_stride;            /* rows of out / grad_out */
+  int32_t index_bits;            /* 32 or 64: int32 or int64 ids */
+  int32_t table_type, out_type;  /* ACC_FLOAT / ACC_BF16; backward: grad_table is fp32 whatever table_type says */
+  int32_t accumulate;            /* backward: 0 or 1 */
+  float   scale;                 /* finite */
+} acc_embedding;
+int32_t accordion_embedding_forward(const acc_embedding* cfg, const void* ids_dev, const void* table_dev,
+                                    void* out_dev, void* hip_stream);
+int32_t accordion_embedding_workspace_bytes(const acc_embedding* cfg, size_t* out_bytes);   /* backward */
+int32_t accordion_embedding_backward(const acc_embedding* cfg, const void* ids_dev, const void* grad_out_dev,
+                                     float* grad_table_dev, void* workspace_dev, size_t workspace_bytes,
+                                     void* hip_stream);
+
+/* Layer norm over rows.
+ *   forward:   mean = sum x / dim, rstd = 1 / sqrt(sum (x - mean)^2 / dim + eps),
+ *              y = (x - mean) rstd weight + bias
+ *   backward:  xh = (x - mean) rstd, g = grad_y weight,
+ *              grad_x = rstd (g - sum g / dim - xh sum(g xh) / dim),
+ *              grad_weight = sum over rows of grad_y xh,  grad_bias = sum over rows of grad_y
+ * bias_dev and grad_bias_dev may be NULL, and so may mean_dev and rstd_dev of the forward pass (both).
+ * accumulate: grad_weight and grad_bias are added to. */
+typedef struct acc_layernorm {
+  int64_t rows;                  /* [0, 2^31) */
+  int64_t dim;                   /* [1, 2^24] */
+  int64_t x_stride, y_stride;    /* rows of x / y (backward: grad_y) */
+  int64_t grad_x_stride;         /* backward */
+  int32_t type;                  /* of x, y and their gradients */
+  int32_t accumulate;            /* backward: 0 or 1 */
+  float   eps;                   /* finite, >= 0 */
+} acc_layernorm;
+int32_t accordion_layernorm_forward(const acc_layernorm* cfg, const void* x_dev, const float* weight_dev,
+                                    const float* bias_dev, void* y_dev, float* mean_dev, float* rstd_dev,
+                                    void* hip_stream);
+int32_t accordion_layernorm_workspace_bytes(const acc_layernorm* cfg, size_t* out_bytes);   /* backward */
+int32_t accordion_layernorm_backward(const acc_layernorm* cfg, const void* grad_y_dev, const void* x_dev,
+                                     const float* weight_dev, const float* mean_dev, const float* rstd_dev,
+                                     void* grad_x_dev, float* grad_weight_dev, float* grad_bias_dev,
+                                     void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* Gated linear recurrence, element by element of the channels.
+ *   forward:   a_t = 1 / (1 + exp(-gate_t)), z_t = 1 / (1 + exp(gate_t)),
+ *              h_t = a_t h_{t-1} + z_t input_t,   out_t = h_t,   h_last = the last h
+ *   backward:  G_t = grad_out_t + a_{t+1} G_{t+1}  (the last one with grad_last),
+ *              grad_input_t = z_t G_t,  grad_gate_t = G_t (h_{t-1} - input_t) a_t z_t,
+ *              grad_h0 = a_0 G_0
+ * z is not computed as a difference from one; gates of +-infinity keep the state / take the input alone.
+ * h0_dev (NULL: zeros), h_last_dev, grad_last_dev (NULL: zeros) and grad_h0_dev are batch x channels,
+ * contiguous fp32; h_last_dev and grad_h0_dev may be NULL.  lengths_dev (int32 per sequence, NULL:
+ * all steps): steps from a sequence's length on write zeros and leave the state as it is; their
+ * gradients are zeros; what their inputs hold plays no role.  A length below 0 counts as 0, one above
+ * steps as steps.  steps = 1 is the serving form: one token, the state in h0 and h_last (which may be
+ * the same buffer then, and for any number of steps). */
+typedef struct acc_recurrence {
+  int64_t batch;                 /* [0, 65535] */
+  int64_t steps;                 /* [0, 2^31) */
+  int64_t channels;              /* [1, 2^24] */
+  /* elements between sequences and between steps */
+  int64_t gate_batch, gate_step, input_batch, input_step, out_batch, out_step;
+  /* the same of the gradients (backward) */
+  int64_t grad_gate_batch, grad_gate_step, grad_input_batch, grad_input_step, grad_out_batch, grad_out_step;
+  int32_t type;                  /* of gate, input, out and their gradients */
+} acc_recurrence;
+int32_t accordion_recurrence_workspace_bytes(const acc_recurrence* cfg, size_t* out_bytes);
+int32_t accordion_recurrence_forward(const acc_recurrence* cfg, const void* gate_dev, const void* input_dev,
+                                     const float* h0_dev, const int32_t* lengths_dev, void* out_dev,
+                                     float* h_last_dev, void* workspace_dev, size_t workspace_bytes,
+                                     void* hip_stream);
+int32_t accordion_recurrence_backward(const acc_recurrence* cfg, const void* gate_dev, const void* input_dev,
+                                      const void* out_dev, const float* h0_dev, const int32_t* lengths_dev,
+                                      const void* grad_out_dev, const float* grad_last_dev, void* grad_gate_dev,
+                                      void* grad_input_dev, float* grad_h0_dev, void* workspace_dev,
+                                      size_t workspace_bytes, void* hip_stream);
+
+/* One AdamW step over many tensors (for example the layers of a flat buffer and their averaged
+ * gradients from accordion_decompress).  For every element, in fp32, every product and sum rounded on
+ * its own, in this order; scalars on the right of ':' are computed in fp64 and rounded once:
+ *     g = grad * *grad_scale_dev                        (only if grad_scale_dev is given)
+ *     m = beta1 m + c1 g                                 : c1 = 1 - beta1
+ *     v = beta2 v + (c2 g) g                             : c2 = 1 - beta2
+ *     w = w keep - (rate m) / (sqrt(v) up + eps)         : keep = 1 - lr weight_decay,
+ *                                                          rate = lr / (1 - beta1^step), up = 1 / sqrt(1 - beta2^step)
+ * step counts from 1.  copies (NULL: none; an entry may be NULL): w also as bf16.
+ * State, accordion_adamw_state_elements() elements in all, the tensors one after the other:
+ *   state_bits 32: m and v as fp32; m_scale and v_scale are NULL.
+ *   state_bits 8:  every tensor starts on a multiple of ACC_ADAMW_BLOCK elements.  A block of
+ *     ACC_ADAMW_BLOCK elements of a tensor holds x, for m, and sqrt(v), for v, as 8-bit floating-point
+ *     codes (e4m3, largest 448, to nearest even) of x (448 / max|x|), and max|x| / 448 as its fp32 scale; a
+ *     block whose max|x| is below 2^-100 is held as zeros.  A positive sqrt(v) of any other block keeps a code of at least
+ *     the smallest positive one, so that no update is divided by eps alone because of the rounding.
+ *     The step itself uses the values before they are rounded to codes.  An infinity or NaN in a
+ *     block's moments makes the whole block's moments NaN.
+ * A state of zeros is the state before the first step. */
+#define ACC_ADAMW_BLOCK 256
+typedef struct acc_adamw {
+  int32_t n_tensors;             /* [0, 2^20] */
+  int32_t weight_type;           /* ACC_FLOAT, or ACC_BF16: weights that are kept in bf16 alone */
+  int32_t grad_type;
+  int32_t state_bits;            /* 8 or 32 */
+  const int64_t* sizes_host;     /* elements per tensor, >= 0 */
+  const float* weight_decay_host;/* per tensor, finite and >= 0; NULL: none */
+  double lr, beta1, beta2, eps;  /* finite; lr >= 0, betas in [0, 1), eps >= 0 */
+  int64_t step;                  /* >= 1 */
+} acc_adamw;
+int32_t accordion_adamw_state_elements(const acc_adamw* cfg, int64_t* out_elements);
+int32_t accordion_adamw_step(const acc_adamw* cfg, void* const* weights_host_array,
+                             const void* const* grads_host_array, void* const* copies_host_array, void* m_dev,
+                             void* v_dev, float* m_scale_dev, float* v_scale_dev, const float* grad_scale_dev,
+                             void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

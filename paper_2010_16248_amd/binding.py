@@ -39,6 +39,33 @@ class acc_config(C.Structure):
                 ("detector", C.c_int32)]
 
 
+class acc_embedding(C.Structure):
+    _fields_ = [("vocab", C.c_int64), ("dim", C.c_int64), ("tokens", C.c_int64), ("table_stride", C.c_int64),
+                ("out_stride", C.c_int64), ("index_bits", C.c_int32), ("table_type", C.c_int32),
+                ("out_type", C.c_int32), ("accumulate", C.c_int32), ("scale", C.c_float)]
+
+
+class acc_layernorm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("dim", C.c_int64), ("x_stride", C.c_int64), ("y_stride", C.c_int64),
+                ("grad_x_stride", C.c_int64), ("type", C.c_int32), ("accumulate", C.c_int32), ("eps", C.c_float)]
+
+
+class acc_recurrence(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("steps", C.c_int64), ("channels", C.c_int64),
+                ("gate_batch", C.c_int64), ("gate_step", C.c_int64), ("input_batch", C.c_int64),
+                ("input_step", C.c_int64), ("out_batch", C.c_int64), ("out_step", C.c_int64),
+                ("grad_gate_batch", C.c_int64), ("grad_gate_step", C.c_int64), ("grad_input_batch", C.c_int64),
+                ("grad_input_step", C.c_int64), ("grad_out_batch", C.c_int64), ("grad_out_step", C.c_int64),
+                ("type", C.c_int32)]
+
+
+class acc_adamw(C.Structure):
+    _fields_ = [("n_tensors", C.c_int32), ("weight_type", C.c_int32), ("grad_type", C.c_int32),
+                ("state_bits", C.c_int32), ("sizes_host", C.POINTER(C.c_int64)),
+                ("weight_decay_host", C.POINTER(C.c_float)), ("lr", C.c_double), ("beta1", C.c_double),
+                ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int64)]
+
+
 class AccordionError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{_STATUS.get(status, status)}: {message}")
@@ -56,6 +83,10 @@ EXPORTS = [
     "accordion_payload_words", "accordion_state_bytes", "accordion_get_state", "accordion_set_state",
     "accordion_set_profiling", "accordion_get_profile", "accordion_stage_name",
     "accordion_probe_copy", "accordion_topk_stats", "accordion_topk_short_lists", "accordion_flush",
+    "accordion_operator_error", "accordion_embedding_forward", "accordion_embedding_workspace_bytes",
+    "accordion_embedding_backward", "accordion_layernorm_forward", "accordion_layernorm_workspace_bytes",
+    "accordion_layernorm_backward", "accordion_recurrence_workspace_bytes", "accordion_recurrence_forward",
+    "accordion_recurrence_backward", "accordion_adamw_state_elements", "accordion_adamw_step",
 ]
 ACC_N_STAGES = 48     # upper bound of the stage numbers; accordion_stage_name is NULL beyond the last
 
@@ -107,6 +138,17 @@ def load_library() -> C.CDLL:
         "accordion_probe_copy": [vp, vp, i64, vp],
         "accordion_topk_stats": [vp, C.POINTER(i64), C.POINTER(i64)],
         "accordion_topk_short_lists": [vp, C.POINTER(i64)],
+        "accordion_embedding_forward": [C.POINTER(acc_embedding), vp, vp, vp, vp],
+        "accordion_embedding_workspace_bytes": [C.POINTER(acc_embedding), C.POINTER(C.c_size_t)],
+        "accordion_embedding_backward": [C.POINTER(acc_embedding), vp, vp, vp, vp, C.c_size_t, vp],
+        "accordion_layernorm_forward": [C.POINTER(acc_layernorm), vp, vp, vp, vp, vp, vp, vp],
+        "accordion_layernorm_workspace_bytes": [C.POINTER(acc_layernorm), C.POINTER(C.c_size_t)],
+        "accordion_layernorm_backward": [C.POINTER(acc_layernorm)] + [vp] * 9 + [C.c_size_t, vp],
+        "accordion_recurrence_workspace_bytes": [C.POINTER(acc_recurrence), C.POINTER(C.c_size_t)],
+        "accordion_recurrence_forward": [C.POINTER(acc_recurrence)] + [vp] * 7 + [C.c_size_t, vp],
+        "accordion_recurrence_backward": [C.POINTER(acc_recurrence)] + [vp] * 11 + [C.c_size_t, vp],
+        "accordion_adamw_state_elements": [C.POINTER(acc_adamw), C.POINTER(i64)],
+        "accordion_adamw_step": [C.POINTER(acc_adamw), C.POINTER(vp), C.POINTER(vp), C.POINTER(vp)] + [vp] * 6,
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -114,6 +156,8 @@ def load_library() -> C.CDLL:
         fn.restype = i32
     lib.accordion_last_error.argtypes = [vp]
     lib.accordion_last_error.restype = C.c_char_p
+    lib.accordion_operator_error.argtypes = []
+    lib.accordion_operator_error.restype = C.c_char_p
     lib.accordion_stage_name.argtypes = [i32]
     lib.accordion_stage_name.restype = C.c_char_p
     _lib = lib
@@ -186,6 +230,271 @@ def probe_copy(dst, src) -> None:
     stream = torch.cuda.current_stream().cuda_stream
     _check(lib, None, lib.accordion_probe_copy(C.c_void_p(dst.data_ptr()), C.c_void_p(src.data_ptr()),
                                                src.numel(), C.c_void_p(stream)))
+
+
+# ---- operators of a language model's training step (no context) ----------------------------------
+# Tensors are torch tensors on one GPU; the work goes to torch's current stream of that GPU.  What the
+# C ABI cannot see (shapes, element types, devices, strides inside a row) is checked here and raises
+# ValueError; what it refuses raises AccordionError.  A workspace is taken from torch's allocator for the
+# call unless one is given (uint8, 256-byte aligned, of at least the bytes that the C ABI asks for).
+
+ACC_FLOAT, ACC_BF16 = 0, 1
+ACC_ADAMW_BLOCK = 256
+
+
+def _operator_check(lib, rc: int) -> None:
+    if rc != ACC_OK:
+        raise AccordionError(rc, lib.accordion_operator_error().decode())
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _type_of(t, name: str) -> int:
+    import torch
+    if t.dtype == torch.float32:
+        return ACC_FLOAT
+    _need(t.dtype == torch.bfloat16, f"{name} must be float32 or bfloat16, not {t.dtype}")
+    return ACC_BF16
+
+
+def _rows_of(t, name: str) -> Tuple[int, int, int]:
+    """(rows, elements per row, elements between rows) of a tensor whose last dimension is a row."""
+    _need(t.dim() >= 1, f"{name} needs a dimension")
+    dim = t.shape[-1]
+    if t.is_contiguous():
+        return (t.numel() // dim if dim else 0), dim, dim
+    _need(t.dim() == 2 and (t.stride(1) == 1 or dim <= 1), f"{name}: rows must be contiguous, and lie in one or two dimensions")
+    return t.shape[0], dim, t.stride(0)
+
+
+def _plain(t, name: str, shape: Tuple[int, ...], dtype) -> Optional[int]:
+    """Pointer of an optional contiguous tensor of this shape and type."""
+    if t is None:
+        return None
+    _need(t.dtype == dtype and tuple(t.shape) == shape and t.is_contiguous(), f"{name} must be contiguous, {dtype}, of shape {shape}")
+    return t.data_ptr()
+
+
+class _Launch:
+    """The current stream of the tensors' GPU, with that GPU current."""
+
+    def __init__(self, *tensors):
+        import torch
+        device = tensors[0].device
+        for t in tensors:
+            if t is not None and (not t.is_cuda or t.device != device):
+                raise ValueError("all tensors must be on one GPU")
+        self.torch, self.device, self.guard = torch, device, None
+
+    def __enter__(self) -> int:
+        if self.torch.cuda.current_device() != self.device.index:
+            self.guard = self.torch.cuda.device(self.device)
+            self.guard.__enter__()
+        return self.torch.cuda.current_stream().cuda_stream
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+    def workspace(self, lib, fn, cfg, given):
+        """(pointer, bytes) of the call's workspace; keeps the tensor it took until the call is enqueued."""
+        n = C.c_size_t(0)
+        _operator_check(lib, fn(C.byref(cfg), C.byref(n)))
+        if given is None:
+            if n.value == 0:
+                return None, 0
+            given = self.taken = self.torch.empty(n.value, dtype=self.torch.uint8, device=self.device)
+        _need(given.device == self.device and given.is_contiguous(), "workspace must be contiguous and on the tensors' GPU")
+        return given.data_ptr(), given.numel() * given.element_size()
+
+
+def _embedding(ids, table, out, scale: float, accumulate: bool) -> acc_embedding:
+    import torch
+    _need(ids.dtype in (torch.int32, torch.int64) and ids.is_contiguous(), "ids must be contiguous int32 or int64")
+    vocab, dim, table_stride = _rows_of(table, "table")
+    tokens, width, out_stride = _rows_of(out, "out")
+    _need(table.dim() == 2 and width == dim and tokens == ids.numel(), "ids, table and out do not fit together")
+    return acc_embedding(vocab, dim, tokens, table_stride, out_stride, 32 if ids.dtype == torch.int32 else 64,
+                         _type_of(table, "table"), _type_of(out, "out"), int(accumulate), scale)
+
+
+def embedding_forward(ids, table, out, scale: float = 1.0) -> None:
+    """out[t, :] = scale * table[ids[t], :]; ids outside the table give zeros."""
+    lib = load_library()
+    cfg = _embedding(ids, table, out, scale, False)
+    with _Launch(ids, table, out) as stream:
+        _operator_check(lib, lib.accordion_embedding_forward(C.byref(cfg), ids.data_ptr(), table.data_ptr(), out.data_ptr(), stream))
+
+
+def embedding_backward(ids, grad_out, grad_table, scale: float = 1.0, accumulate: bool = False, workspace=None) -> None:
+    """grad_table[v, :] (+)= scale * sum of grad_out[t, :] over the t with ids[t] == v; grad_table is float32."""
+    import torch
+    lib = load_library()
+    _need(grad_table.dtype == torch.float32, "grad_table must be float32")
+    cfg = _embedding(ids, grad_table, grad_out, scale, accumulate)
+    launch = _Launch(ids, grad_out, grad_table)
+    with launch as stream:
+        ws, n = launch.workspace(lib, lib.accordion_embedding_workspace_bytes, cfg, workspace)
+        _operator_check(lib, lib.accordion_embedding_backward(C.byref(cfg), ids.data_ptr(), grad_out.data_ptr(),
+                                                              grad_table.data_ptr(), ws, n, stream))
+
+
+def layernorm_forward(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-5) -> None:
+    """y = (x - mean) rstd weight + bias over the last dimension; bias may be None; mean and rstd are written if given."""
+    import torch
+    lib = load_library()
+    rows, dim, x_stride = _rows_of(x, "x")
+    y_rows, y_dim, y_stride = _rows_of(y, "y")
+    _need((y_rows, y_dim, y.dtype) == (rows, dim, x.dtype), "x and y do not fit together")
+    f = torch.float32
+    w, b = _plain(weight, "weight", (dim,), f), _plain(bias, "bias", (dim,), f)
+    m, r = _plain(mean, "mean", (rows,), f), _plain(rstd, "rstd", (rows,), f)
+    cfg = acc_layernorm(rows, dim, x_stride, y_stride, 0, _type_of(x, "x"), 0, eps)
+    with _Launch(x, weight, bias, y, mean, rstd) as stream:
+        _operator_check(lib, lib.accordion_layernorm_forward(C.byref(cfg), x.data_ptr(), w, b, y.data_ptr(), m, r, stream))
+
+
+def layernorm_backward(grad_y, x, weight, mean, rstd, grad_x, grad_weight, grad_bias=None, accumulate: bool = False,
+                       workspace=None) -> None:
+    """Gradients of layernorm_forward; grad_bias may be None; accumulate adds to grad_weight and grad_bias."""
+    import torch
+    lib = load_library()
+    rows, dim, x_stride = _rows_of(x, "x")
+    g_rows, g_dim, g_stride = _rows_of(grad_y, "grad_y")
+    d_rows, d_dim, d_stride = _rows_of(grad_x, "grad_x")
+    _need((g_rows, g_dim, grad_y.dtype) == (rows, dim, x.dtype) and (d_rows, d_dim, grad_x.dtype) == (rows, dim, x.dtype),
+          "x, grad_y and grad_x do not fit together")
+    f = torch.float32
+    w, m, r = _plain(weight, "weight", (dim,), f), _plain(mean, "mean", (rows,), f), _plain(rstd, "rstd", (rows,), f)
+    dw, db = _plain(grad_weight, "grad_weight", (dim,), f), _plain(grad_bias, "grad_bias", (dim,), f)
+    cfg = acc_layernorm(rows, dim, x_stride, g_stride, d_stride, _type_of(x, "x"), int(accumulate), 0.0)
+    launch = _Launch(x, grad_y, weight, mean, rstd, grad_x, grad_weight, grad_bias)
+    with launch as stream:
+        ws, n = launch.workspace(lib, lib.accordion_layernorm_workspace_bytes, cfg, workspace)
+        _operator_check(lib, lib.accordion_layernorm_backward(C.byref(cfg), grad_y.data_ptr(), x.data_ptr(), w, m, r,
+                                                              grad_x.data_ptr(), dw, db, ws, n, stream))
+
+
+def _steps_of(t, name: str, like) -> Tuple[int, int]:
+    """(elements between sequences, between steps) of a batch x steps x channels tensor."""
+    _need(t.dim() == 3 and t.shape == like.shape and t.dtype == like.dtype, f"{name} must have gate's shape and type")
+    _need(t.stride(2) == 1 or t.shape[2] <= 1, f"{name}: the channels of a step must be contiguous")
+    return t.stride(0), t.stride(1)
+
+
+def recurrence_forward(gate, input, out, h0=None, h_last=None, lengths=None, workspace=None) -> None:
+    """h_t = sigmoid(gate_t) h_{t-1} + sigmoid(-gate_t) input_t along dimension 1 of batch x steps x channels tensors;
+    out gets every h, h_last (batch x channels, float32) the last one.  steps = 1 with h0 and h_last: one token."""
+    import torch
+    lib = load_library()
+    _need(gate.dim() == 3, "gate must be batch x steps x channels")
+    batch, steps, channels = gate.shape
+    cfg = acc_recurrence(batch, steps, channels, *_steps_of(gate, "gate", gate), *_steps_of(input, "input", gate),
+                         *_steps_of(out, "out", gate), 0, 0, 0, 0, 0, 0, _type_of(gate, "gate"))
+    ends = (batch, channels)
+    first, last = _plain(h0, "h0", ends, torch.float32), _plain(h_last, "h_last", ends, torch.float32)
+    n_steps = _plain(lengths, "lengths", (batch,), torch.int32)
+    launch = _Launch(gate, input, out, h0, h_last, lengths)
+    with launch as stream:
+        ws, n = launch.workspace(lib, lib.accordion_recurrence_workspace_bytes, cfg, workspace)
+        _operator_check(lib, lib.accordion_recurrence_forward(C.byref(cfg), gate.data_ptr(), input.data_ptr(), first, n_steps,
+                                                              out.data_ptr(), last, ws, n, stream))
+
+
+def recurrence_backward(gate, input, out, grad_out, grad_gate, grad_input, h0=None, grad_last=None, grad_h0=None,
+                        lengths=None, workspace=None) -> None:
+    """Gradients of recurrence_forward; out is what it wrote, grad_last the gradient of h_last (None: zeros)."""
+    import torch
+    lib = load_library()
+    _need(gate.dim() == 3, "gate must be batch x steps x channels")
+    batch, steps, channels = gate.shape
+    cfg = acc_recurrence(batch, steps, channels, *_steps_of(gate, "gate", gate), *_steps_of(input, "input", gate),
+                         *_steps_of(out, "out", gate), *_steps_of(grad_gate, "grad_gate", gate),
+                         *_steps_of(grad_input, "grad_input", gate), *_steps_of(grad_out, "grad_out", gate),
+                         _type_of(gate, "gate"))
+    ends, f = (batch, channels), torch.float32
+    first, last, dh0 = _plain(h0, "h0", ends, f), _plain(grad_last, "grad_last", ends, f), _plain(grad_h0, "grad_h0", ends, f)
+    n_steps = _plain(lengths, "lengths", (batch,), torch.int32)
+    launch = _Launch(gate, input, out, grad_out, grad_gate, grad_input, h0, grad_last, grad_h0, lengths)
+    with launch as stream:
+        ws, n = launch.workspace(lib, lib.accordion_recurrence_workspace_bytes, cfg, workspace)
+        _operator_check(lib, lib.accordion_recurrence_backward(
+            C.byref(cfg), gate.data_ptr(), input.data_ptr(), out.data_ptr(), first, n_steps, grad_out.data_ptr(), last,
+            grad_gate.data_ptr(), grad_input.data_ptr(), dh0, ws, n, stream))
+
+
+def adamw_state_elements(sizes: Sequence[int], state_bits: int = 32) -> int:
+    """Elements of each moment of adamw_step for tensors of these sizes; host arithmetic only."""
+    lib = load_library()
+    arr = (C.c_int64 * max(1, len(sizes)))(*sizes)
+    cfg = acc_adamw(n_tensors=len(sizes), state_bits=state_bits, sizes_host=arr)
+    out = C.c_int64(0)
+    _operator_check(lib, lib.accordion_adamw_state_elements(C.byref(cfg), C.byref(out)))
+    return out.value
+
+
+def adamw_state(sizes: Sequence[int], state_bits: int = 32, device: str = "cuda:0"):
+    """(m, v, m_scale, v_scale) before the first step: float32 moments and no scales, or with 8 bits e4m3 codes (of
+    sqrt(v) in v's place) and a float32 scale for each block of ACC_ADAMW_BLOCK elements."""
+    import torch
+    n = adamw_state_elements(sizes, state_bits)
+    if state_bits == 32:
+        return tuple(torch.zeros(n, device=device) for _ in range(2)) + (None, None)
+    return (*(torch.zeros(n, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2)),
+            *(torch.zeros(n // ACC_ADAMW_BLOCK, device=device) for _ in range(2)))
+
+
+def adamw_step(weights: Sequence, grads: Sequence, state, lr: float, step: int, weight_decay=0.0,
+               betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8, copies: Optional[Sequence] = None,
+               grad_scale=None) -> None:
+    """One AdamW step over all tensors (contiguous; all weights of one type, all gradients of one type).  state: as
+    adamw_state made it for their sizes; weight_decay: one number or one per tensor; copies: bfloat16 tensors that get the
+    new weights too; grad_scale: a float32 element on the GPU that multiplies every gradient."""
+    import torch
+    lib = load_library()
+    count = len(weights)
+    _need(len(grads) == count and (copies is None or len(copies) == count), "weights, grads and copies must be of one length")
+    if count == 0:
+        return
+    m, v, m_scale, v_scale = state
+    bits = 32 if m_scale is None else 8
+    sizes = (C.c_int64 * count)()
+    ptrs = [(C.c_void_p * count)() for _ in range(3)]
+    w_type, g_type, device = weights[0].dtype, grads[0].dtype, weights[0].device
+    elements = 0
+    for i in range(count):
+        w, g = weights[i], grads[i]
+        n = w.numel()
+        _need(w.dtype == w_type and g.dtype == g_type and g.numel() == n, "weights and grads do not fit together")
+        _need(w.is_contiguous() and g.is_contiguous(), "weights and grads must be contiguous")
+        _need(w.device == device and g.device == device, "all tensors must be on one GPU")
+        sizes[i], ptrs[0][i], ptrs[1][i] = n, w.data_ptr(), g.data_ptr()
+        elements += n if bits == 32 else -(-n // ACC_ADAMW_BLOCK) * ACC_ADAMW_BLOCK
+        if copies is not None and copies[i] is not None:
+            c = copies[i]
+            _need(c.dtype == torch.bfloat16 and c.numel() == n and c.is_contiguous() and c.device == device,
+                  "a copy must be bfloat16, contiguous, of its tensor's size, on its GPU")
+            ptrs[2][i] = c.data_ptr()
+    held = torch.float32 if bits == 32 else torch.float8_e4m3fn
+    mp, vp = _plain(m, "m", (elements,), held), _plain(v, "v", (elements,), held)
+    blocks = (elements // ACC_ADAMW_BLOCK,)
+    ms, vs = _plain(m_scale, "m_scale", blocks, torch.float32), _plain(v_scale, "v_scale", blocks, torch.float32)
+    _need(grad_scale is None or (grad_scale.dtype == torch.float32 and grad_scale.numel() == 1), "grad_scale must be one float32 element")
+    decay = None
+    if not isinstance(weight_decay, (int, float)):
+        _need(len(weight_decay) == count, "one weight decay per tensor")
+        decay = (C.c_float * count)(*weight_decay)
+    elif weight_decay != 0.0:
+        decay = (C.c_float * count)(*([weight_decay] * count))
+    cfg = acc_adamw(count, _type_of(weights[0], "weights"), _type_of(grads[0], "grads"), bits, sizes, decay, lr, betas[0], betas[1],
+                    eps, step)
+    with _Launch(weights[0], m, v, m_scale, v_scale, grad_scale) as stream:
+        _operator_check(lib, lib.accordion_adamw_step(
+            C.byref(cfg), ptrs[0], ptrs[1], ptrs[2] if copies is not None else None, mp, vp, ms, vs,
+            grad_scale.data_ptr() if grad_scale is not None else None, stream))
 
 
 class Accordion:

@@ -7,7 +7,7 @@ import subprocess
 import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRC = os.path.join(HERE, "csrc", "accordion.hip")
+SRC = [os.path.join(HERE, "csrc", "accordion.hip"), os.path.join(HERE, "csrc", "operators", "operators.hip")]
 LIB = os.path.join(HERE, "libaccordion.so")
 
 FLAGS = [
@@ -27,7 +27,7 @@ def hipcc() -> str:
 
 
 def build(verbose: bool = True) -> str:
-    cmd = [hipcc()] + FLAGS + ["-o", LIB, SRC]
+    cmd = [hipcc()] + FLAGS + ["-o", LIB] + SRC
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)

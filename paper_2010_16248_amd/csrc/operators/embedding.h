@@ -1,0 +1,295 @@
+// Embedding lookup with scaling, and the table's gradient by sorted tokens.
+#pragma once
+#include "op_common.h"
+
+namespace accop {
+
+// ---- forward: out[t, :] = scale * table[id_t, :] ------------------------------------------------------
+// A copy of rows, bound by memory (a few thousand rows: by the launch).  A group of 2^lanes_log2 lanes takes a
+// row, four requests per lane under way; grid.y splits rows of more columns.
+constexpr int kLookupLoads = 4;
+
+template <typename I, typename T, typename O, int N>
+__global__ __launch_bounds__(256) void embedding_lookup_kernel(const I* __restrict__ ids, const T* __restrict__ table,
+                                                               O* __restrict__ out, int64_t tokens, int64_t vocab,
+                                                               int64_t dim, int64_t table_stride, int64_t out_stride,
+                                                               float scale, int lanes_log2) {
+  const int lanes = 1 << lanes_log2;
+  const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> lanes_log2;
+  if (t >= tokens) return;
+  const int64_t id = (int64_t)ids[t];
+  const bool known = id >= 0 && id < vocab;
+  const T* row = table + (known ? id : 0) * table_stride;
+  O* to = out + t * out_stride;
+  const int64_t c0 = (int64_t)blockIdx.y * kLookupLoads * lanes * N + (int64_t)(threadIdx.x & (lanes - 1)) * N;
+  const int64_t pitch = (int64_t)lanes * N;
+  Pack<T, N> v[kLookupLoads];
+#pragma unroll
+  for (int i = 0; i < kLookupLoads; ++i) v[i] = load_some<N>(row + c0 + i * pitch, known ? dim - (c0 + i * pitch) : 0);
+#pragma unroll
+  for (int i = 0; i < kLookupLoads; ++i) {
+    const int64_t left = dim - (c0 + i * pitch);
+    if (left > 0) store_some<O, N>(to + c0 + i * pitch, widen<T, N>(v[i]) * scale, left);
+  }
+}
+
+// ---- backward: order the tokens by id, ties by position ------------------------------------------------
+// key = id, or vocab for an id outside the table (sorts behind all others and is left out).
+template <typename I>
+__device__ __forceinline__ uint32_t key_of_id(I id, uint32_t vocab) {
+  const int64_t v = (int64_t)id;
+  return v >= 0 && v < (int64_t)vocab ? (uint32_t)v : vocab;
+}
+
+// The zeros of the rows that no token asks for, in the launch that starts the sort: the sort waits for latencies
+// and leaves the memory idle.  (Rows with tokens are written again later.)
+__device__ __forceinline__ void clear_rows(float* __restrict__ table, int64_t vocab, int64_t dim, int64_t stride,
+                                           int64_t block, int64_t blocks) {
+  const F32<4> zero = {0.f, 0.f, 0.f, 0.f};
+  if (stride == dim) {
+    const int64_t n = vocab * dim;
+    for (int64_t i = (block * blockDim.x + threadIdx.x) * 4; i < n; i += blocks * blockDim.x * 4)
+      store_some<float, 4>(table + i, zero, n - i);
+  } else {
+    for (int64_t r = block; r < vocab; r += blocks)
+      for (int64_t i = (int64_t)threadIdx.x * 4; i < dim; i += (int64_t)blockDim.x * 4)
+        store_some<float, 4>(table + r * stride + i, zero, dim - i);
+  }
+}
+
+// Few tokens: a token's place is the number of tokens that come before it, counted against all others.
+// A workgroup places 64 tokens (one per lane); its waves share the tokens to compare with.
+constexpr int kRankThreads = 1024;
+template <typename I>
+__global__ __launch_bounds__(kRankThreads) void embedding_rank_kernel(const I* __restrict__ ids, int n, uint32_t vocab,
+                                                                     uint32_t* __restrict__ skey, uint32_t* __restrict__ spos,
+                                                                     int rank_blocks, float* __restrict__ table, int64_t rows,
+                                                                     int64_t dim, int64_t stride) {
+  if ((int)blockIdx.x >= rank_blocks) {
+    clear_rows(table, rows, dim, stride, (int64_t)blockIdx.x - rank_blocks, (int64_t)gridDim.x - rank_blocks);
+    return;
+  }
+  __shared__ uint32_t part[kRankThreads];
+  constexpr int waves = kRankThreads / kWave;
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int first = blockIdx.x * kWave, i = first + l;
+  const uint32_t mine = i < n ? key_of_id(ids[i], vocab) : 0u;
+  const int share = (n + waves - 1) / waves;
+  const int lo = w * share, hi = min(n, lo + share);
+  uint32_t before = 0;
+  // in front of the workgroup's own tokens an equal key counts, behind them it does not
+  for (int j = lo; j < min(hi, first); ++j) before += key_of_id(ids[j], vocab) <= mine;
+  for (int j = max(lo, first); j < min(hi, first + kWave); ++j) {
+    const uint32_t k = key_of_id(ids[j], vocab);
+    before += k < mine || (k == mine && j < i);
+  }
+  for (int j = max(lo, first + kWave); j < hi; ++j) before += key_of_id(ids[j], vocab) < mine;
+  part[threadIdx.x] = before;
+  __syncthreads();
+  if (w == 0 && i < n) {
+    uint32_t place = 0;
+    for (int k = 0; k < waves; ++k) place += part[k * kWave + l];
+    skey[place] = mine;
+    spos[place] = (uint32_t)i;
+  }
+}
+
+// Many tokens: stable counting passes over digits of up to 10 key bits, lowest first.  A workgroup takes a tile of
+// consecutive tokens, 4096 (kSortItems per thread) at a time.
+constexpr int kSortThreads = 1024, kSortItems = 4, kSortStep = kSortThreads * kSortItems, kSortTiles = 128;
+constexpr int kSortDigitBits = 10, kSortDigits = 1 << kSortDigitBits;
+
+// Where a pass finds its keys: in the ids (first pass: the position is the place) or in the last pass's order.
+template <typename I, bool FIRST>
+__device__ __forceinline__ uint32_t sort_key(const I* ids, const uint32_t* key, int64_t i, uint32_t vocab) {
+  if (FIRST) return key_of_id(ids[i], vocab);
+  return key[i];
+}
+
+template <typename I, bool FIRST>
+__global__ __launch_bounds__(kSortThreads) void embedding_count_kernel(const I* __restrict__ ids, const uint32_t* __restrict__ key,
+                                                                      int64_t n, uint32_t vocab, int64_t tile, int shift, int digits,
+                                                                      uint32_t* __restrict__ counts, int tiles,
+                                                                      float* __restrict__ table, int64_t rows, int64_t dim,
+                                                                      int64_t stride) {
+  if ((int)blockIdx.x >= tiles) {
+    clear_rows(table, rows, dim, stride, (int64_t)blockIdx.x - tiles, (int64_t)gridDim.x - tiles);
+    return;
+  }
+  __shared__ uint32_t count[kSortDigits];
+  for (int d = threadIdx.x; d < digits; d += kSortThreads) count[d] = 0;
+  __syncthreads();
+  const int64_t lo = blockIdx.x * tile, hi = min(n, lo + tile);
+  for (int64_t i = lo + threadIdx.x; i < hi; i += kSortThreads)
+    atomicAdd(&count[(sort_key<I, FIRST>(ids, key, i, vocab) >> shift) & (digits - 1)], 1u);
+  __syncthreads();
+  for (int d = threadIdx.x; d < digits; d += kSortThreads) counts[(int64_t)blockIdx.x * digits + d] = count[d];
+}
+
+template <typename I, bool FIRST>
+__global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(const I* __restrict__ ids, const uint32_t* __restrict__ key,
+                                                                      const uint32_t* __restrict__ pos, int64_t n, uint32_t vocab,
+                                                                      int64_t tile, int shift, int digit_bits,
+                                                                      const uint32_t* __restrict__ counts, int tiles,
+                                                                      uint32_t* __restrict__ key_out, uint32_t* __restrict__ pos_out) {
+  constexpr int waves = kSortThreads / kWave;
+  __shared__ uint32_t base[kSortDigits];               // where the tile's next token of a digit goes
+  __shared__ uint16_t seen[waves][kSortDigits];        // tokens of a digit in a wave, then in the waves before it
+  __shared__ uint32_t sums[waves];
+  const int digits = 1 << digit_bits;
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6, d = threadIdx.x;
+  // all tiles' tokens of smaller digits, and of this digit those of the tiles in front (kSortDigits == kSortThreads)
+  uint32_t all = 0, front = 0;
+  if (d < digits)
+    for (int t = 0; t < tiles; ++t) {
+      const uint32_t c = counts[(int64_t)t * digits + d];
+      if (t < (int)blockIdx.x) front += c;
+      all += c;
+    }
+  uint32_t incl = all;
+  for (int s = 1; s < kWave; s <<= 1) {
+    const uint32_t o = __shfl_up(incl, s, kWave);
+    if (l >= s) incl += o;
+  }
+  if (l == 63) sums[w] = incl;
+  __syncthreads();
+  uint32_t smaller = incl - all;
+  for (int k = 0; k < w; ++k) smaller += sums[k];
+  base[d] = smaller + front;
+  const int64_t lo = blockIdx.x * tile, hi = min(n, lo + tile);
+  for (int64_t step = lo; step < hi; step += kSortStep) {
+    for (int k = threadIdx.x; k < waves * kSortDigits; k += kSortThreads) (&seen[0][0])[k] = 0;
+    __syncthreads();
+    uint32_t k[kSortItems], p[kSortItems], rank[kSortItems];
+#pragma unroll
+    for (int r = 0; r < kSortItems; ++r) {
+      const int64_t i = step + w * (kWave * kSortItems) + r * kWave + l;
+      k[r] = p[r] = 0;
+      if (i < hi) {
+        k[r] = sort_key<I, FIRST>(ids, key, i, vocab);
+        p[r] = FIRST ? (uint32_t)i : pos[i];
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < kSortItems; ++r) {
+      const int64_t i = step + w * (kWave * kSortItems) + r * kWave + l;
+      const bool in = i < hi;
+      const uint32_t dig = (k[r] >> shift) & (digits - 1);
+      uint64_t same = __ballot(in);
+      for (int b = 0; b < digit_bits; ++b) {
+        const uint64_t ones = __ballot((dig >> b) & 1);
+        same &= (dig >> b) & 1 ? ones : ~ones;
+      }
+      const uint32_t below = __popcll(same & ((1ull << l) - 1));
+      const uint32_t had = in ? seen[w][dig] : 0;
+      rank[r] = had + below;
+      // the wave's lanes read and write its counts in turn
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      if (in && below == 0) seen[w][dig] = (uint16_t)(had + __popcll(same));
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    // tokens of a digit: waves in front of each wave; the tile's base moves on once all have read it
+    uint32_t run = 0;
+    if (d < digits)
+      for (int k2 = 0; k2 < waves; ++k2) {
+        const uint32_t c = seen[k2][d];
+        seen[k2][d] = (uint16_t)run;
+        run += c;
+      }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kSortItems; ++r) {
+      const int64_t i = step + w * (kWave * kSortItems) + r * kWave + l;
+      if (i < hi) {
+        const uint32_t dig = (k[r] >> shift) & (digits - 1);
+        const uint32_t to = base[dig] + seen[w][dig] + rank[r];
+        key_out[to] = k[r];
+        pos_out[to] = p[r];
+      }
+    }
+    __syncthreads();
+    if (d < digits) base[d] += run;
+    __syncthreads();
+  }
+}
+
+// ---- backward: sums over runs of equal ids ---------------------------------------------------------------
+// A workgroup takes a chunk of consecutive places of the order and up to 256 N columns.  A run of equal ids
+// inside the chunk is summed and written to its row; of a run that crosses the chunk's ends the part inside
+// is left in the workspace: parts[2 c] for a run that began in an earlier chunk, parts[2 c + 1] for one that
+// begins here and goes on.
+constexpr int kSumAhead = 8;   // rows under way
+
+template <typename T, int N>
+__global__ __launch_bounds__(256) void embedding_sum_kernel(const uint32_t* __restrict__ skey, const uint32_t* __restrict__ spos,
+                                                            int64_t n, int chunk, uint32_t vocab, const T* __restrict__ grad,
+                                                            int64_t grad_stride, float* __restrict__ table, int64_t table_stride,
+                                                            int64_t dim, float scale, int accumulate, float* __restrict__ parts) {
+  const int64_t lo = (int64_t)blockIdx.x * chunk, hi = min(n, lo + chunk);
+  const int64_t c = ((int64_t)blockIdx.y * 256 + threadIdx.x) * N, left = dim - c;
+  const uint32_t front = lo > 0 ? skey[lo - 1] : 0xffffffffu, behind = hi < n ? skey[hi] : 0xffffffffu;
+  F32<N> acc = {};
+  uint32_t run = skey[lo];
+  bool opened = run != front;    // the run began in this chunk
+  auto close = [&](uint32_t row, bool ends) {
+    if (row >= vocab || left <= 0) return;
+    if (!opened) {
+      store_some<float, N>(parts + (2 * (int64_t)blockIdx.x) * dim + c, acc, left);
+    } else if (!ends) {
+      store_some<float, N>(parts + (2 * (int64_t)blockIdx.x + 1) * dim + c, acc, left);
+    } else {
+      float* to = table + (int64_t)row * table_stride + c;
+      F32<N> v = acc * scale;
+      if (accumulate) v = widen<float, N>(load_some<N>(to, left)) + v;
+      store_some<float, N>(to, v, left);
+    }
+  };
+  for (int64_t i0 = lo; i0 < hi; i0 += kSumAhead) {
+    Pack<T, N> v[kSumAhead];
+    uint32_t key[kSumAhead];
+#pragma unroll
+    for (int j = 0; j < kSumAhead; ++j) {
+      const int64_t i = min(i0 + j, hi - 1);
+      key[j] = skey[i];
+      v[j] = load_some<N>(grad + (int64_t)spos[i] * grad_stride + c, key[j] < vocab ? left : 0);
+    }
+#pragma unroll
+    for (int j = 0; j < kSumAhead; ++j) {
+      if (i0 + j >= hi) break;
+      if (key[j] != run) {
+        close(run, true);
+        run = key[j];
+        opened = true;
+        acc = F32<N>{};
+      }
+      acc += widen<T, N>(v[j]);
+    }
+  }
+  close(run, run != behind);
+}
+
+// The runs that cross chunks: the workgroup of the chunk where one begins adds its parts in order.
+template <int N>
+__global__ __launch_bounds__(256) void embedding_join_kernel(const uint32_t* __restrict__ skey, int64_t n, int chunk, int64_t chunks,
+                                                             uint32_t vocab, const float* __restrict__ parts,
+                                                             float* __restrict__ table, int64_t table_stride, int64_t dim, float scale,
+                                                             int accumulate) {
+  const int64_t b = blockIdx.x, lo = b * chunk, hi = lo + chunk;
+  if (hi >= n) return;
+  const uint32_t row = skey[hi];
+  if (row >= vocab || skey[hi - 1] != row || (lo > 0 && skey[lo] == row && skey[lo - 1] == row)) return;
+  const int64_t c = ((int64_t)blockIdx.y * 256 + threadIdx.x) * N, left = dim - c;
+  if (left <= 0) return;
+  F32<N> acc = widen<float, N>(load_some<N>(parts + (2 * b + 1) * dim + c, left));
+  for (int64_t k = b + 1; k < chunks && skey[k * chunk] == row; ++k)
+    acc += widen<float, N>(load_some<N>(parts + 2 * k * dim + c, left));
+  float* to = table + (int64_t)row * table_stride + c;
+  F32<N> v = acc * scale;
+  if (accumulate) v = widen<float, N>(load_some<N>(to, left)) + v;
+  store_some<float, N>(to, v, left);
+}
+
+}  // namespace accop
