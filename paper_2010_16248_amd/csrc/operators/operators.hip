@@ -334,20 +334,69 @@ RecurrenceShape shape_of(const acc_recurrence& c) {
           c.grad_gate_batch, c.grad_gate_step, c.grad_input_batch, c.grad_input_step, c.grad_out_batch, c.grad_out_step};
 }
 
-template <typename T>
-void walk_forward(const acc_recurrence& c, const void* gate, const void* input, const float* h0, const int32_t* lengths, void* out,
-                  float* h_last, void* stream) {
-  constexpr int N = sizeof(T) == 2 ? 2 : 1;
-  LAUNCH((recurrence_forward_walk_kernel<T, N>), dim3((unsigned)up(c.channels, 256 * N), (unsigned)c.batch), dim3(256), stream,
-         shape_of(c), static_cast<const T*>(gate), static_cast<const T*>(input), h0, lengths, static_cast<T*>(out), h_last);
+// Up to kWalkSteps steps a lane walks them.  More: chunks, whose number of waves follows the steps.
+constexpr int64_t kWalkSteps = 16;
+constexpr int64_t kMostChunks = int64_t(1) << 22;   // see kRowsPerLaunch
+
+struct RecurrencePlan {
+  bool walk;
+  int lane = 1;                            // channels per lane
+  int wave_steps = 0, waves = 0, chunks = 0;
+  int64_t channel_blocks = 0, chains = 0, slots = 0;
+  int64_t bytes = 0;                       // workspace: the counter, then three words per slot
+};
+
+RecurrencePlan plan_recurrence(const acc_recurrence& c) {
+  RecurrencePlan p;
+  p.lane = c.type == ACC_BF16 && c.channels % 2 == 0 ? 2 : 1;
+  p.walk = c.steps <= kWalkSteps;
+  if (p.walk) return p;
+  p.wave_steps = p.lane == 2 ? 8 : 16;
+  p.waves = (int)std::min<int64_t>(kChunkWaves, up(c.steps, p.wave_steps));
+  p.chunks = (int)up(c.steps, p.waves * p.wave_steps);
+  p.channel_blocks = up(c.channels, kWave * p.lane);
+  p.chains = p.channel_blocks * c.batch;
+  if (p.chunks > 1) {
+    p.slots = p.chains * p.chunks * kWave * p.lane;
+    p.bytes = 256 + round256(24 * p.slots);
+  }
+  return p;
 }
 
-template <typename T>
-void walk_backward(const acc_recurrence& c, const void* gate, const void* input, const void* out, const float* h0,
-                   const int32_t* lengths, const void* dout, const float* dlast, void* dgate, void* dinput, float* dh0, void* stream) {
-  constexpr int N = sizeof(T) == 2 ? 2 : 1;
-  LAUNCH((recurrence_backward_walk_kernel<T, N>), dim3((unsigned)up(c.channels, 256 * N), (unsigned)c.batch), dim3(256), stream,
-         shape_of(c), static_cast<const T*>(gate), static_cast<const T*>(input), static_cast<const T*>(out), h0, lengths,
+ChunkSlots chunk_slots(const RecurrencePlan& p, void* workspace, void* stream) {
+  uint32_t* counter = static_cast<uint32_t*>(workspace);
+  unsigned long long* words = reinterpret_cast<unsigned long long*>(static_cast<char*>(workspace) + 256);
+  const ChunkSlots s = {words, words + p.slots, words + 2 * p.slots, counter, p.chains, p.channel_blocks, p.chunks};
+  if (p.chunks > 1) LAUNCH(recurrence_clear_kernel, dim3((unsigned)up(3 * p.slots, 256)), dim3(256), stream, words, 3 * p.slots, counter);
+  return s;
+}
+
+template <typename T, int N, int S>
+void run_forward(const acc_recurrence& c, const RecurrencePlan& p, const void* gate, const void* input, const float* h0,
+                 const int32_t* lengths, void* out, float* h_last, void* ws, void* stream) {
+  if (p.walk) {
+    LAUNCH((recurrence_forward_walk_kernel<T, N>), dim3((unsigned)up(c.channels, 256 * N), (unsigned)c.batch), dim3(256), stream,
+           shape_of(c), static_cast<const T*>(gate), static_cast<const T*>(input), h0, lengths, static_cast<T*>(out), h_last);
+    return;
+  }
+  const ChunkSlots slots = chunk_slots(p, ws, stream);
+  LAUNCH((recurrence_forward_chunk_kernel<T, N, S>), dim3((unsigned)(p.chains * p.chunks)), dim3(kWave * p.waves), stream, shape_of(c),
+         slots, static_cast<const T*>(gate), static_cast<const T*>(input), h0, lengths, static_cast<T*>(out), h_last);
+}
+
+template <typename T, int N, int S>
+void run_backward(const acc_recurrence& c, const RecurrencePlan& p, const void* gate, const void* input, const void* out,
+                  const float* h0, const int32_t* lengths, const void* dout, const float* dlast, void* dgate, void* dinput, float* dh0,
+                  void* ws, void* stream) {
+  if (p.walk) {
+    LAUNCH((recurrence_backward_walk_kernel<T, N>), dim3((unsigned)up(c.channels, 256 * N), (unsigned)c.batch), dim3(256), stream,
+           shape_of(c), static_cast<const T*>(gate), static_cast<const T*>(input), static_cast<const T*>(out), h0, lengths,
+           static_cast<const T*>(dout), dlast, static_cast<T*>(dgate), static_cast<T*>(dinput), dh0);
+    return;
+  }
+  const ChunkSlots slots = chunk_slots(p, ws, stream);
+  LAUNCH((recurrence_backward_chunk_kernel<T, N, S>), dim3((unsigned)(p.chains * p.chunks)), dim3(kWave * p.waves), stream, shape_of(c),
+         slots, static_cast<const T*>(gate), static_cast<const T*>(input), static_cast<const T*>(out), h0, lengths,
          static_cast<const T*>(dout), dlast, static_cast<T*>(dgate), static_cast<T*>(dinput), dh0);
 }
 
@@ -492,7 +541,9 @@ int32_t accordion_layernorm_backward(const acc_layernorm* c, const void* grad_y_
 int32_t accordion_recurrence_workspace_bytes(const acc_recurrence* c, size_t* out_bytes) {
   REQUIRE(out_bytes, "out_bytes is NULL");
   if (const int32_t rc = check_recurrence(c, false)) return rc;
-  *out_bytes = 0;
+  const RecurrencePlan p = plan_recurrence(*c);
+  REQUIRE(p.chains * p.chunks <= kMostChunks, "too many steps");
+  *out_bytes = (size_t)p.bytes;
   return ACC_OK;
 }
 
@@ -506,13 +557,16 @@ int32_t accordion_recurrence_forward(const acc_recurrence* c, const void* gate_d
   REQUIRE(!off_type(gate_dev, e) && !off_type(input_dev, e) && !off_type(out_dev, e) && !off_type(h0_dev, 4) &&
               !off_type(lengths_dev, 4) && !off_type(h_last_dev, 4),
           "a pointer is not aligned to its element type");
-  const Span s[6] = {steps_span(out_dev, *c, c->out_batch, c->out_step), rows_span(h_last_dev, c->batch, c->channels, c->channels, 4),
+  const RecurrencePlan p = plan_recurrence(*c);
+  REQUIRE(p.chains * p.chunks <= kMostChunks, "too many steps");
+  if (const int32_t rc = check_workspace(workspace_dev, workspace_bytes, p.bytes)) return rc;
+  const Span s[7] = {{static_cast<const char*>(workspace_dev), p.bytes}, steps_span(out_dev, *c, c->out_batch, c->out_step), rows_span(h_last_dev, c->batch, c->channels, c->channels, 4),
                      steps_span(gate_dev, *c, c->gate_batch, c->gate_step), steps_span(input_dev, *c, c->input_batch, c->input_step),
                      {reinterpret_cast<const char*>(lengths_dev), lengths_dev ? 4 * c->batch : 0},
                      rows_span(h0_dev == h_last_dev ? nullptr : h0_dev, c->batch, c->channels, c->channels, 4)};
-  REQUIRE(!any_overlap(s, 2, 6), "a buffer that is written overlaps another one");
-  if (c->type == ACC_BF16) walk_forward<bf16>(*c, gate_dev, input_dev, h0_dev, lengths_dev, out_dev, h_last_dev, hip_stream);
-  else walk_forward<float>(*c, gate_dev, input_dev, h0_dev, lengths_dev, out_dev, h_last_dev, hip_stream);
+  REQUIRE(!any_overlap(s, 3, 7), "a buffer that is written overlaps another one");
+  const auto run = c->type == ACC_FLOAT ? run_forward<float, 1, 16> : p.lane == 2 ? run_forward<bf16, 2, 8> : run_forward<bf16, 1, 16>;
+  run(*c, p, gate_dev, input_dev, h0_dev, lengths_dev, out_dev, h_last_dev, workspace_dev, hip_stream);
   return launched();
 }
 
@@ -528,7 +582,11 @@ int32_t accordion_recurrence_backward(const acc_recurrence* c, const void* gate_
               !off_type(grad_gate_dev, e) && !off_type(grad_input_dev, e) && !off_type(h0_dev, 4) && !off_type(lengths_dev, 4) &&
               !off_type(grad_last_dev, 4) && !off_type(grad_h0_dev, 4),
           "a pointer is not aligned to its element type");
-  const Span s[10] = {steps_span(grad_gate_dev, *c, c->grad_gate_batch, c->grad_gate_step),
+  const RecurrencePlan p = plan_recurrence(*c);
+  REQUIRE(p.chains * p.chunks <= kMostChunks, "too many steps");
+  if (const int32_t rc = check_workspace(workspace_dev, workspace_bytes, p.bytes)) return rc;
+  const Span s[11] = {{static_cast<const char*>(workspace_dev), p.bytes},
+                      steps_span(grad_gate_dev, *c, c->grad_gate_batch, c->grad_gate_step),
                       steps_span(grad_input_dev, *c, c->grad_input_batch, c->grad_input_step),
                       rows_span(grad_h0_dev, c->batch, c->channels, c->channels, 4),
                       steps_span(gate_dev, *c, c->gate_batch, c->gate_step),
@@ -538,13 +596,10 @@ int32_t accordion_recurrence_backward(const acc_recurrence* c, const void* gate_
                       rows_span(h0_dev, c->batch, c->channels, c->channels, 4),
                       rows_span(grad_last_dev, c->batch, c->channels, c->channels, 4),
                       {reinterpret_cast<const char*>(lengths_dev), lengths_dev ? 4 * c->batch : 0}};
-  REQUIRE(!any_overlap(s, 3, 10), "a buffer that is written overlaps another one");
-  if (c->type == ACC_BF16)
-    walk_backward<bf16>(*c, gate_dev, input_dev, out_dev, h0_dev, lengths_dev, grad_out_dev, grad_last_dev, grad_gate_dev,
-                        grad_input_dev, grad_h0_dev, hip_stream);
-  else
-    walk_backward<float>(*c, gate_dev, input_dev, out_dev, h0_dev, lengths_dev, grad_out_dev, grad_last_dev, grad_gate_dev,
-                         grad_input_dev, grad_h0_dev, hip_stream);
+  REQUIRE(!any_overlap(s, 4, 11), "a buffer that is written overlaps another one");
+  const auto run = c->type == ACC_FLOAT ? run_backward<float, 1, 16> : p.lane == 2 ? run_backward<bf16, 2, 8> : run_backward<bf16, 1, 16>;
+  run(*c, p, gate_dev, input_dev, out_dev, h0_dev, lengths_dev, grad_out_dev, grad_last_dev, grad_gate_dev, grad_input_dev,
+                              grad_h0_dev, workspace_dev, hip_stream);
   return launched();
 }
 
