@@ -419,7 +419,7 @@ int32_t accordion_layernorm_backward(const acc_layernorm* cfg, const void* grad_
  * gradients are zeros; what their inputs hold plays no role.  A length below 0 counts as 0, one above
  * steps as steps.  steps = 1 is the serving form: one token, the state in h0 and h_last (which may be
  * the same buffer then, and for any number of steps).
- * Sequences x blocks of 64 channels (bf16: 128) x blocks of 256 steps: at most 2^22. */
+ * Sequences x blocks of 64 channels (bf16: 128) x blocks of 64 steps: at most 2^22. */
 typedef struct acc_recurrence {
   int64_t batch;                 /* [0, 65535] */
   int64_t steps;                 /* [0, 2^31) */

@@ -341,24 +341,28 @@ constexpr int64_t kMostChunks = int64_t(1) << 22;   // see kRowsPerLaunch
 struct RecurrencePlan {
   bool walk;
   int lane = 1;                            // channels per lane
-  int wave_steps = 0, waves = 0, chunks = 0;
-  int64_t channel_blocks = 0, chains = 0, slots = 0;
-  int64_t bytes = 0;                       // workspace: the counter, then three words per slot
+  int wave_steps = 0, waves = 0, chunks = 0, groups = 0;
+  int64_t channel_blocks = 0, chains = 0;
+  int64_t slots = 0, group_slots = 0;      // chunks' and groups' words of a kind
+  int64_t words = 0, bytes = 0;            // workspace: the counter, then the words
 };
 
-RecurrencePlan plan_recurrence(const acc_recurrence& c) {
+RecurrencePlan plan_recurrence(const acc_recurrence& c, bool backward) {
   RecurrencePlan p;
   p.lane = c.type == ACC_BF16 && c.channels % 2 == 0 ? 2 : 1;
   p.walk = c.steps <= kWalkSteps;
   if (p.walk) return p;
-  p.wave_steps = p.lane == 2 ? 8 : 16;
+  p.wave_steps = backward && p.lane == 2 ? 8 : 16;
   p.waves = (int)std::min<int64_t>(kChunkWaves, up(c.steps, p.wave_steps));
   p.chunks = (int)up(c.steps, p.waves * p.wave_steps);
   p.channel_blocks = up(c.channels, kWave * p.lane);
   p.chains = p.channel_blocks * c.batch;
   if (p.chunks > 1) {
+    p.groups = (int)up(p.chunks, kChunkGroup);
     p.slots = p.chains * p.chunks * kWave * p.lane;
-    p.bytes = 256 + round256(24 * p.slots);
+    p.group_slots = p.groups > 1 ? p.chains * p.groups * kWave * p.lane : 0;
+    p.words = 2 * p.slots + 3 * p.group_slots;
+    p.bytes = 256 + round256(8 * p.words);
   }
   return p;
 }
@@ -366,8 +370,10 @@ RecurrencePlan plan_recurrence(const acc_recurrence& c) {
 ChunkSlots chunk_slots(const RecurrencePlan& p, void* workspace, void* stream) {
   uint32_t* counter = static_cast<uint32_t*>(workspace);
   unsigned long long* words = reinterpret_cast<unsigned long long*>(static_cast<char*>(workspace) + 256);
-  const ChunkSlots s = {words, words + p.slots, words + 2 * p.slots, counter, p.chains, p.channel_blocks, p.chunks};
-  if (p.chunks > 1) LAUNCH(recurrence_clear_kernel, dim3((unsigned)up(3 * p.slots, 256)), dim3(256), stream, words, 3 * p.slots, counter);
+  unsigned long long* const groups = words + 2 * p.slots;
+  const ChunkSlots s = {words, words + p.slots, groups, groups + p.group_slots, groups + 2 * p.group_slots, counter, p.chains,
+                        p.channel_blocks, p.chunks, p.groups};
+  if (p.chunks > 1) LAUNCH(recurrence_clear_kernel, dim3((unsigned)up(p.words, 256)), dim3(256), stream, words, p.words, counter);
   return s;
 }
 
@@ -541,9 +547,9 @@ int32_t accordion_layernorm_backward(const acc_layernorm* c, const void* grad_y_
 int32_t accordion_recurrence_workspace_bytes(const acc_recurrence* c, size_t* out_bytes) {
   REQUIRE(out_bytes, "out_bytes is NULL");
   if (const int32_t rc = check_recurrence(c, false)) return rc;
-  const RecurrencePlan p = plan_recurrence(*c);
-  REQUIRE(p.chains * p.chunks <= kMostChunks, "too many steps");
-  *out_bytes = (size_t)p.bytes;
+  const RecurrencePlan f = plan_recurrence(*c, false), b = plan_recurrence(*c, true);
+  REQUIRE(std::max(f.chains * f.chunks, b.chains * b.chunks) <= kMostChunks, "too many steps");
+  *out_bytes = (size_t)std::max(f.bytes, b.bytes);
   return ACC_OK;
 }
 
@@ -557,7 +563,7 @@ int32_t accordion_recurrence_forward(const acc_recurrence* c, const void* gate_d
   REQUIRE(!off_type(gate_dev, e) && !off_type(input_dev, e) && !off_type(out_dev, e) && !off_type(h0_dev, 4) &&
               !off_type(lengths_dev, 4) && !off_type(h_last_dev, 4),
           "a pointer is not aligned to its element type");
-  const RecurrencePlan p = plan_recurrence(*c);
+  const RecurrencePlan p = plan_recurrence(*c, false);
   REQUIRE(p.chains * p.chunks <= kMostChunks, "too many steps");
   if (const int32_t rc = check_workspace(workspace_dev, workspace_bytes, p.bytes)) return rc;
   const Span s[7] = {{static_cast<const char*>(workspace_dev), p.bytes}, steps_span(out_dev, *c, c->out_batch, c->out_step), rows_span(h_last_dev, c->batch, c->channels, c->channels, 4),
@@ -565,7 +571,7 @@ int32_t accordion_recurrence_forward(const acc_recurrence* c, const void* gate_d
                      {reinterpret_cast<const char*>(lengths_dev), lengths_dev ? 4 * c->batch : 0},
                      rows_span(h0_dev == h_last_dev ? nullptr : h0_dev, c->batch, c->channels, c->channels, 4)};
   REQUIRE(!any_overlap(s, 3, 7), "a buffer that is written overlaps another one");
-  const auto run = c->type == ACC_FLOAT ? run_forward<float, 1, 16> : p.lane == 2 ? run_forward<bf16, 2, 8> : run_forward<bf16, 1, 16>;
+  const auto run = c->type == ACC_FLOAT ? run_forward<float, 1, 16> : p.lane == 2 ? run_forward<bf16, 2, 16> : run_forward<bf16, 1, 16>;
   run(*c, p, gate_dev, input_dev, h0_dev, lengths_dev, out_dev, h_last_dev, workspace_dev, hip_stream);
   return launched();
 }
@@ -582,7 +588,7 @@ int32_t accordion_recurrence_backward(const acc_recurrence* c, const void* gate_
               !off_type(grad_gate_dev, e) && !off_type(grad_input_dev, e) && !off_type(h0_dev, 4) && !off_type(lengths_dev, 4) &&
               !off_type(grad_last_dev, 4) && !off_type(grad_h0_dev, 4),
           "a pointer is not aligned to its element type");
-  const RecurrencePlan p = plan_recurrence(*c);
+  const RecurrencePlan p = plan_recurrence(*c, true);
   REQUIRE(p.chains * p.chunks <= kMostChunks, "too many steps");
   if (const int32_t rc = check_workspace(workspace_dev, workspace_bytes, p.bytes)) return rc;
   const Span s[11] = {{static_cast<const char*>(workspace_dev), p.bytes},

@@ -130,34 +130,37 @@ __global__ __launch_bounds__(256) void recurrence_backward_walk_kernel(Recurrenc
 
 // ---- a workgroup per chunk of steps ---------------------------------------------------------------------------
 // The step maps of a chunk compose to one map h -> A h + H.  A wave takes S consecutive steps of 64 N channels and keeps
-// their maps in registers, a workgroup as many waves as it has; so the inputs are read once.  Where a sequence has several
-// chunks, a chunk leaves its map in the workspace, takes the state at its start from the chunks before it (look_back) and
-// leaves the state at its end.  Whatever it finds there, the state it starts with is the fold of the maps in front of it,
-// from the first one on, map after map: the bits do not depend on who was faster.
+// their maps in registers, a workgroup has up to kChunkWaves waves; so the inputs are read once.  Where a sequence has
+// several chunks, they meet in the workspace, in groups of kChunkGroup:
+//   a chunk leaves its map there and takes those of the chunks in front of it in its group,
+//   the last one of a group also leaves the group's map, and the state at the group's end once it has its start,
+//   the state at a group's start is the nearest state found in front of it, taken through the groups' maps in between.
+// Whatever a chunk finds, it starts from the same fold of the same maps in the same order: the bits do not depend on who was
+// faster.
 //
 // Maps and the states between waves are fp64: composed maps meet in differences (A h against H) that the steps one by
 // one do not have, and so a wave starts from the state that steps without rounding would have reached.
 //
 // Chunks are handed out by a counter in the order of the steps, so that all chunks a workgroup waits for have
-// been taken by workgroups that run already.  A map is left without waiting for anything; of the chunks without
-// a state at their end the first one always finds the one in front of it: every wait ends.
+// been taken by workgroups that run already.  Chunks' maps wait for nothing, groups' maps for chunks' maps alone, and of the
+// groups without a state at their end the first one finds the one in front of it: every wait ends.
 //
 // A word of the workspace holds a value and the news that it is there at once (all ones: not yet); its accesses are
 // atomic and go past the caches that compute units do not share.
-constexpr int kChunkWaves = 16;       // most waves of a workgroup
-constexpr int kLookBack = 8;          // chunks looked at in one go
+constexpr int kChunkWaves = 8;        // most waves of a workgroup; all of them where there are several chunks
+constexpr int kChunkGroup = 8;        // a wave for every chunk in front of the group's last one
+constexpr int kLookBack = 4;          // groups looked at in one go
 constexpr unsigned long long kNotYet = ~0ull;
 
 template <int N>
 using F64 = double __attribute__((ext_vector_type(N)));
 
 struct ChunkSlots {
-  unsigned long long* map_a;          // per chain, chunk and channel
-  unsigned long long* map_h;
-  unsigned long long* state;          // the state at the chunk's end
-  uint32_t* counter;                  // chunks handed out
-  int64_t chains, channel_blocks;     // (sequence, block of 64 N channels)
-  int chunks;
+  unsigned long long *map_a, *map_h;             // per chain, chunk and channel
+  unsigned long long *group_a, *group_h, *state; // per chain, group and channel: the group's map, the state at its end
+  uint32_t* counter;                             // chunks handed out
+  int64_t chains, channel_blocks;                // (sequence, block of 64 N channels)
+  int chunks, groups;
 };
 
 __global__ __launch_bounds__(256) void recurrence_clear_kernel(unsigned long long* words, int64_t n, uint32_t* counter) {
@@ -174,38 +177,39 @@ __device__ __forceinline__ void leave(unsigned long long* p, double v) {
 __device__ __forceinline__ unsigned long long look(const unsigned long long* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
+__device__ __forceinline__ double value(unsigned long long word) { return __longlong_as_double((long long)word); }
 
-// The state at the start of chunk `chunk` > 0 of one channel per lane.  slot0: the channel's slot in chunk 0, pitch: slots
-// per chunk.
-__device__ __forceinline__ double look_back(const ChunkSlots& s, int64_t slot0, int64_t pitch, int chunk) {
-  const int most = min(chunk, kLookBack);
+// The state at the start of group `group` > 0 of one channel per lane.  slot0: the channel's slot in group 0, pitch: slots per
+// group.
+__device__ __forceinline__ double look_back(const ChunkSlots& s, int64_t slot0, int64_t pitch, int group) {
+  const int most = min(group, kLookBack);
   for (;;) {
     unsigned long long st[kLookBack];
 #pragma unroll
-    for (int q = 0; q < kLookBack; ++q) st[q] = look(s.state + slot0 + (int64_t)(chunk - 1 - min(q, most - 1)) * pitch);
+    for (int q = 0; q < kLookBack; ++q) st[q] = look(s.state + slot0 + (int64_t)(group - 1 - min(q, most - 1)) * pitch);
     int at = -1;
     double h = 0.0;
 #pragma unroll
     for (int q = kLookBack - 1; q >= 0; --q)
       if (q < most && __ballot(st[q] == kNotYet) == 0) {
         at = q;
-        h = __longlong_as_double((long long)st[q]);
+        h = value(st[q]);
       }
     if (at == 0) return h;
     if (at > 0) {
       unsigned long long a[kLookBack - 1], b[kLookBack - 1];
 #pragma unroll
       for (int q = 0; q < kLookBack - 1; ++q) {
-        const int64_t slot = slot0 + (int64_t)(chunk - 1 - min(q, at - 1)) * pitch;
-        a[q] = look(s.map_a + slot);
-        b[q] = look(s.map_h + slot);
+        const int64_t slot = slot0 + (int64_t)(group - 1 - min(q, at - 1)) * pitch;
+        a[q] = look(s.group_a + slot);
+        b[q] = look(s.group_h + slot);
       }
       bool all = true;
 #pragma unroll
       for (int q = kLookBack - 2; q >= 0; --q)
         if (q < at) {
           all = all && a[q] != kNotYet && b[q] != kNotYet;
-          h = fma(__longlong_as_double((long long)a[q]), h, __longlong_as_double((long long)b[q]));
+          h = fma(value(a[q]), h, value(b[q]));
         }
       if (__ballot(!all) == 0) return h;
     }
@@ -216,8 +220,8 @@ __device__ __forceinline__ double look_back(const ChunkSlots& s, int64_t slot0, 
 // Where a workgroup works: which chunk of which chain.
 struct ChunkPlace {
   int chunk;
+  uint32_t chain;
   int64_t b, c, left;                 // sequence, the lane's first channel, channels from there on
-  int64_t slot0;                      // the chain's first slot
 };
 
 template <int N>
@@ -230,21 +234,23 @@ __device__ __forceinline__ ChunkPlace chunk_place(const ChunkSlots& s, const Rec
   }
   ChunkPlace p;
   p.chunk = (int)(ticket / (uint32_t)s.chains);
-  const uint32_t chain = ticket % (uint32_t)s.chains;
-  p.b = chain / (uint32_t)s.channel_blocks;
-  p.c = (int64_t)(chain % (uint32_t)s.channel_blocks) * (kWave * N) + (threadIdx.x & 63) * N;
+  p.chain = ticket % (uint32_t)s.chains;
+  p.b = p.chain / (uint32_t)s.channel_blocks;
+  p.c = (int64_t)(p.chain % (uint32_t)s.channel_blocks) * (kWave * N) + (threadIdx.x & 63) * N;
   p.left = shape.channels - p.c;
-  p.slot0 = (int64_t)chain * s.chunks * (kWave * N);
   return p;
 }
 
-// Maps of a workgroup's waves, per channel of its block.
+// Per channel of the workgroup's block: the maps of its waves, those of the chunks in front of it in its group, the state at its start.
 template <int N>
 struct ChunkFold {
-  double a[kChunkWaves][kWave * N], h[kChunkWaves][kWave * N], start[kWave * N];
+  double a[kChunkWaves][kWave * N], h[kChunkWaves][kWave * N];
+  double before_a[kChunkGroup - 1][kWave * N], before_h[kChunkGroup - 1][kWave * N];
+  double start[kWave * N];
 };
 
-// From the waves' maps to the state at this wave's start.  first: the state at the chain's start (used in chunk 0 only).
+// From the waves' maps to the state at this wave's start.  first: the state at the chain's start (used in its first group only; wave 0
+// has read it before the chunk leaves its map, so the last chunk may write over it).
 template <int N>
 __device__ __forceinline__ F32<N> chunk_state(const ChunkSlots& s, const ChunkPlace& p, const F64<N>& a_mine, const F64<N>& h_mine,
                                               const F32<N>& first, ChunkFold<N>& fold) {
@@ -258,26 +264,66 @@ __device__ __forceinline__ F32<N> chunk_state(const ChunkSlots& s, const ChunkPl
   }
   __syncthreads();
   if (s.chunks > 1) {
+    const int group = p.chunk / kChunkGroup, at = p.chunk % kChunkGroup, ch = w * kWave + l;
+    const int64_t slot0 = (int64_t)p.chain * s.chunks * pitch, group0 = (int64_t)p.chain * s.groups * pitch;
+    const bool ends = at == kChunkGroup - 1 && group + 1 < s.groups;   // other groups build on this chunk
+    double A = 1.0, H = 0.0;
     if (w < N) {                       // a wave for every 64 channels
-      const int ch = w * kWave + l;
-      double A = fold.a[0][ch], H = fold.h[0][ch];
-      for (int k = 1; k < waves; ++k) {
+#pragma unroll 2
+      for (int k = 0; k < waves; ++k) {
         const double ak = fold.a[k][ch];
         A *= ak;
         H = fma(ak, H, fold.h[k][ch]);
       }
-      const int64_t slot = p.slot0 + (int64_t)p.chunk * pitch + ch;
-      const bool last = p.chunk + 1 == s.chunks;
-      double h = fold.start[ch];
-      if (p.chunk > 0) {
-        if (!last) {
-          leave(s.map_a + slot, A);
-          leave(s.map_h + slot, H);
-        }
-        h = look_back(s, p.slot0 + ch, pitch, p.chunk);
-        fold.start[ch] = h;
+      if (at < kChunkGroup - 1 && p.chunk + 1 < s.chunks) {
+        leave(s.map_a + slot0 + (int64_t)p.chunk * pitch + ch, A);
+        leave(s.map_h + slot0 + (int64_t)p.chunk * pitch + ch, H);
       }
-      if (!last) leave(s.state + slot, fma(A, h, H));
+    }
+    if (w < at) {
+      const int64_t slot = slot0 + (int64_t)(p.chunk - at + w) * pitch + l;
+      for (;;) {
+        unsigned long long a[N], b[N];
+        bool all = true;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          a[i] = look(s.map_a + slot + i * kWave);
+          b[i] = look(s.map_h + slot + i * kWave);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          all = all && a[i] != kNotYet && b[i] != kNotYet;
+          fold.before_a[w][l + i * kWave] = value(a[i]);
+          fold.before_h[w][l + i * kWave] = value(b[i]);
+        }
+        if (__ballot(!all) == 0) break;
+        __builtin_amdgcn_s_sleep(1);
+      }
+    }
+    __syncthreads();
+    if (w < N) {
+      const int64_t slot = group0 + (int64_t)group * pitch + ch;
+      if (ends) {
+        double GA = 1.0, GH = 0.0;
+#pragma unroll 2
+        for (int k = 0; k < at; ++k) {
+          GA *= fold.before_a[k][ch];
+          GH = fma(fold.before_a[k][ch], GH, fold.before_h[k][ch]);
+        }
+        A *= GA;
+        H = fma(fold.a[0][ch], GH, fold.h[0][ch]);
+#pragma unroll 2
+        for (int k = 1; k < waves; ++k) H = fma(fold.a[k][ch], H, fold.h[k][ch]);
+        if (group > 0) {
+          leave(s.group_a + slot, A);
+          leave(s.group_h + slot, H);
+        }
+      }
+      double h = group > 0 ? look_back(s, group0 + ch, pitch, group) : fold.start[ch];
+      if (ends) leave(s.state + slot, fma(A, h, H));
+#pragma unroll 2
+      for (int k = 0; k < at; ++k) h = fma(fold.before_a[k][ch], h, fold.before_h[k][ch]);
+      fold.start[ch] = h;
     }
     __syncthreads();
   }
@@ -285,6 +331,7 @@ __device__ __forceinline__ F32<N> chunk_state(const ChunkSlots& s, const ChunkPl
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     h[i] = fold.start[l * N + i];
+#pragma unroll 2
     for (int k = 0; k < w; ++k) h[i] = fma(fold.a[k][l * N + i], h[i], fold.h[k][l * N + i]);
   }
   return __builtin_convertvector(h, F32<N>);
@@ -301,19 +348,16 @@ __device__ __forceinline__ void load_steps(Pack<T, N> (&v)[S], const T* p, int64
 }
 
 // N divides the channels, so a lane has all of its N channels or none (it then works on the first ones and stores nothing).
-template <typename T, int N, int S>
-__global__ __launch_bounds__(kWave* kChunkWaves) void recurrence_forward_chunk_kernel(
-    RecurrenceShape s, ChunkSlots slots, const T* __restrict__ gate, const T* __restrict__ input, const float* h0,
-    const int32_t* __restrict__ lengths, T* __restrict__ out, float* h_last) {
-  __shared__ ChunkFold<N> fold;
-  __shared__ uint32_t ticket;
-  const ChunkPlace p = chunk_place<N>(slots, s, &ticket);
+// WHOLE: every step of the chunk belongs to the sequence.
+template <typename T, int N, int S, bool WHOLE>
+__device__ __forceinline__ void forward_chunk(const RecurrenceShape& s, const ChunkSlots& slots, const ChunkPlace& p, ChunkFold<N>& fold,
+                                              const T* gate, const T* input, const float* h0, int64_t len, T* out, float* h_last) {
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const bool mine = p.left > 0;
   const int64_t c = mine ? p.c : 0, ends = p.b * s.channels + c;
   const int64_t t0 = ((int64_t)p.chunk * waves + w) * S;
-  const int in = (int)min((int64_t)S, max(steps_of(lengths, p.b, s.steps) - t0, (int64_t)0));   // steps of the sequence
-  const int here = (int)min((int64_t)S, max(s.steps - t0, (int64_t)0));                        // steps of the tensors
+  const int in = WHOLE ? S : (int)min((int64_t)S, max(len - t0, (int64_t)0));          // steps of the sequence
+  const int here = WHOLE ? S : (int)min((int64_t)S, max(s.steps - t0, (int64_t)0));    // steps of the tensors
   F32<N> a[S], b[S], first = {};
   F64<N> A = F64<N>{} + 1.0, H = {};
   if (in > 0) {
@@ -333,7 +377,7 @@ __global__ __launch_bounds__(kWave* kChunkWaves) void recurrence_forward_chunk_k
       }
     }
   }
-  if (h0 && p.chunk == 0) first = widen<float, N>(load<N>(h0 + ends));
+  if (h0 && p.chunk < kChunkGroup) first = widen<float, N>(load<N>(h0 + ends));
   F32<N> h = chunk_state<N>(slots, p, A, H, first, fold);
   if (!mine) return;
   T* o = out + p.b * s.out_b + t0 * s.out_t + c;
@@ -351,22 +395,30 @@ __global__ __launch_bounds__(kWave* kChunkWaves) void recurrence_forward_chunk_k
   if (h_last && p.chunk == slots.chunks - 1 && w == waves - 1) store<float, N>(h_last + ends, h);
 }
 
-// Backward in time: the state is c_t = a_t G_t, the gradient of h_{t-1}; c_t = a_t c_{t+1} + a_t grad_out_t.  Steps are counted from
-// the last one on.
 template <typename T, int N, int S>
-__global__ __launch_bounds__(kWave* kChunkWaves) void recurrence_backward_chunk_kernel(
-    RecurrenceShape s, ChunkSlots slots, const T* __restrict__ gate, const T* __restrict__ input, const T* __restrict__ out,
-    const float* __restrict__ h0, const int32_t* __restrict__ lengths, const T* __restrict__ dout, const float* __restrict__ dlast,
-    T* __restrict__ dgate, T* __restrict__ dinput, float* __restrict__ dh0) {
+__global__ __launch_bounds__(kWave* kChunkWaves, 3) void recurrence_forward_chunk_kernel(
+    RecurrenceShape s, ChunkSlots slots, const T* __restrict__ gate, const T* __restrict__ input, const float* h0,
+    const int32_t* __restrict__ lengths, T* __restrict__ out, float* h_last) {
   __shared__ ChunkFold<N> fold;
   __shared__ uint32_t ticket;
   const ChunkPlace p = chunk_place<N>(slots, s, &ticket);
+  const int64_t len = steps_of(lengths, p.b, s.steps), per = (int64_t)(blockDim.x >> 6) * S;
+  if ((p.chunk + 1) * per <= len) forward_chunk<T, N, S, true>(s, slots, p, fold, gate, input, h0, len, out, h_last);
+  else forward_chunk<T, N, S, false>(s, slots, p, fold, gate, input, h0, len, out, h_last);
+}
+
+// Backward in time: the state is c_t = a_t G_t, the gradient of h_{t-1}; c_t = a_t c_{t+1} + a_t grad_out_t.  Steps are counted from
+// the last one on.  WHOLE: every step of the chunk belongs to the sequence and none is its first.
+template <typename T, int N, int S, bool WHOLE>
+__device__ __forceinline__ void backward_chunk(const RecurrenceShape& s, const ChunkSlots& slots, const ChunkPlace& p, ChunkFold<N>& fold,
+                                               const T* gate, const T* input, const T* out, const float* h0, int64_t len, const T* dout,
+                                               const float* dlast, T* dgate, T* dinput, float* dh0) {
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const bool mine = p.left > 0;
   const int64_t c = mine ? p.c : 0, ends = p.b * s.channels + c;
   const int64_t t0 = s.steps - 1 - ((int64_t)p.chunk * waves + w) * S;                          // the wave's latest step
-  const int here = (int)min((int64_t)S, max(t0 + 1, (int64_t)0));                               // steps of the tensors: j < here
-  const int out_of = (int)min((int64_t)here, max(t0 + 1 - steps_of(lengths, p.b, s.steps), (int64_t)0));   // of the sequence: out_of <= j
+  const int here = WHOLE ? S : (int)min((int64_t)S, max(t0 + 1, (int64_t)0));                   // steps of the tensors: j < here
+  const int out_of = WHOLE ? 0 : (int)min((int64_t)here, max(t0 + 1 - len, (int64_t)0));        // of the sequence: out_of <= j
   F32<N> a[S], z[S], first = {}, state;
   F64<N> A = F64<N>{} + 1.0, H = {};
   Pack<T, N> d[S], x[S], before[S];
@@ -376,6 +428,7 @@ __global__ __launch_bounds__(kWave* kChunkWaves) void recurrence_backward_chunk_
     const T* pf = gate + p.b * s.gate_b + (t0 - out_of) * s.gate_t + c;
     const T* pd = dout + p.b * s.dout_b + (t0 - out_of) * s.dout_t + c;
     const T* px = input + p.b * s.input_b + (t0 - out_of) * s.input_t + c;
+    const T* pb = out + p.b * s.out_b + (WHOLE ? t0 - 1 : max(t0 - out_of - 1, (int64_t)0)) * s.out_t + c;
 #pragma unroll
     for (int j = 0; j < S; ++j) {
       const bool on = j >= out_of && j < here - 1;
@@ -384,13 +437,13 @@ __global__ __launch_bounds__(kWave* kChunkWaves) void recurrence_backward_chunk_
       pf -= on ? s.gate_t : 0;
       pd -= on ? s.dout_t : 0;
     }
-    const T* pb = out + p.b * s.out_b + max(t0 - out_of - 1, (int64_t)0) * s.out_t + c;
 #pragma unroll
     for (int j = 0; j < S; ++j) {
+      const bool on = j >= out_of && j < here - 1;
       x[j] = load<N>(px);
       before[j] = load<N>(pb);
-      px -= j >= out_of && j < here - 1 ? s.input_t : 0;
-      pb -= j >= out_of && j < here - 1 && t0 - j - 1 > 0 ? s.out_t : 0;
+      px -= on ? s.input_t : 0;
+      pb -= on && (WHOLE || t0 - j - 1 > 0) ? s.out_t : 0;
     }
 #pragma unroll
     for (int j = 0; j < S; ++j) {
@@ -406,11 +459,11 @@ __global__ __launch_bounds__(kWave* kChunkWaves) void recurrence_backward_chunk_
       }
     }
   }
-  if (dlast && p.chunk == 0) first = widen<float, N>(load<N>(dlast + ends));
+  if (dlast && p.chunk < kChunkGroup) first = widen<float, N>(load<N>(dlast + ends));
   state = chunk_state<N>(slots, p, A, H, first, fold);
   if (!mine) return;
   F32<N> h_first = {};
-  if (h0 && here > 0 && t0 - here + 1 == 0) h_first = widen<float, N>(load<N>(h0 + ends));
+  if (!WHOLE && h0 && here > 0 && t0 - here + 1 == 0) h_first = widen<float, N>(load<N>(h0 + ends));
   T* og = dgate + p.b * s.dgate_b + t0 * s.dgate_t + c;
   T* ox = dinput + p.b * s.dinput_b + t0 * s.dinput_t + c;
 #pragma unroll
@@ -419,7 +472,7 @@ __global__ __launch_bounds__(kWave* kChunkWaves) void recurrence_backward_chunk_
       F32<N> dg = {}, dx = {};
       if (j >= out_of) {
         const F32<N> total = state + widen<T, N>(d[j]), xx = widen<T, N>(x[j]);
-        const F32<N> h = t0 - j > 0 ? widen<T, N>(before[j]) : h_first;
+        const F32<N> h = WHOLE || t0 - j > 0 ? widen<T, N>(before[j]) : h_first;
         dx = z[j] * total;
         dg = (h - xx) * a[j] * dx;
         state = a[j] * total;
@@ -431,6 +484,22 @@ __global__ __launch_bounds__(kWave* kChunkWaves) void recurrence_backward_chunk_
     ox -= s.dinput_t;
   }
   if (dh0 && p.chunk == slots.chunks - 1 && w == waves - 1) store<float, N>(dh0 + ends, state);
+}
+
+template <typename T, int N, int S>
+__global__ __launch_bounds__(kWave* kChunkWaves, 3) void recurrence_backward_chunk_kernel(
+    RecurrenceShape s, ChunkSlots slots, const T* __restrict__ gate, const T* __restrict__ input, const T* __restrict__ out,
+    const float* __restrict__ h0, const int32_t* __restrict__ lengths, const T* __restrict__ dout, const float* __restrict__ dlast,
+    T* __restrict__ dgate, T* __restrict__ dinput, float* __restrict__ dh0) {
+  __shared__ ChunkFold<N> fold;
+  __shared__ uint32_t ticket;
+  const ChunkPlace p = chunk_place<N>(slots, s, &ticket);
+  const int64_t len = steps_of(lengths, p.b, s.steps), per = (int64_t)(blockDim.x >> 6) * S;
+  const int64_t latest = s.steps - p.chunk * per, earliest = latest - per;     // steps [earliest, latest)
+  if (latest <= len && earliest > 0)
+    backward_chunk<T, N, S, true>(s, slots, p, fold, gate, input, out, h0, len, dout, dlast, dgate, dinput, dh0);
+  else
+    backward_chunk<T, N, S, false>(s, slots, p, fold, gate, input, out, h0, len, dout, dlast, dgate, dinput, dh0);
 }
 
 }  // namespace accop
