@@ -8,6 +8,7 @@ load, every call raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import os
 from typing import List, Optional, Sequence, Tuple
@@ -242,104 +243,107 @@ ACC_FLOAT, ACC_BF16 = 0, 1
 ACC_ADAMW_BLOCK = 256
 
 
-def _operator_check(lib, rc: int) -> None:
-    if rc != ACC_OK:
-        raise AccordionError(rc, lib.accordion_operator_error().decode())
-
-
 def _need(ok: bool, what: str) -> None:
     if not ok:
         raise ValueError(what)
 
 
+_TYPES = None      # torch's types, once it is loaded
+
+
 def _type_of(t, name: str) -> int:
-    import torch
-    if t.dtype == torch.float32:
-        return ACC_FLOAT
-    _need(t.dtype == torch.bfloat16, f"{name} must be float32 or bfloat16, not {t.dtype}")
-    return ACC_BF16
+    global _TYPES
+    if _TYPES is None:
+        import torch
+        _TYPES = {torch.float32: ACC_FLOAT, torch.bfloat16: ACC_BF16}
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        raise ValueError(f"{name} must be float32 or bfloat16, not {t.dtype}")
+    return kind
 
 
 def _rows_of(t, name: str) -> Tuple[int, int, int]:
     """(rows, elements per row, elements between rows) of a tensor whose last dimension is a row."""
-    _need(t.dim() >= 1, f"{name} needs a dimension")
-    dim = t.shape[-1]
-    if t.is_contiguous():
-        return (t.numel() // dim if dim else 0), dim, dim
-    _need(t.dim() == 2 and (t.stride(1) == 1 or dim <= 1), f"{name}: rows must be contiguous, and lie in one or two dimensions")
-    return t.shape[0], dim, t.stride(0)
+    shape = t.shape
+    if len(shape) == 2 and (t.is_contiguous() or t.stride(1) == 1 or shape[1] <= 1):
+        return shape[0], shape[1], t.stride(0)
+    _need(len(shape) >= 1 and t.is_contiguous(), f"{name}: rows must be contiguous, and lie in one or two dimensions")
+    return (t.numel() // shape[-1] if shape[-1] else 0), shape[-1], shape[-1]
 
 
 def _plain(t, name: str, shape: Tuple[int, ...], dtype) -> Optional[int]:
     """Pointer of an optional contiguous tensor of this shape and type."""
     if t is None:
         return None
-    _need(t.dtype == dtype and tuple(t.shape) == shape and t.is_contiguous(), f"{name} must be contiguous, {dtype}, of shape {shape}")
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous, {dtype}, of shape {tuple(shape)}")
     return t.data_ptr()
 
 
-class _Launch:
-    """The current stream of the tensors' GPU, with that GPU current."""
+def _gpu_of(*tensors) -> int:
+    """Index of the GPU that all the tensors are on."""
+    index = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            index = -1
+    if index < 0:
+        raise ValueError("all tensors must be on one GPU")
+    return index
 
-    def __init__(self, *tensors):
+
+def _launch(gpu: int, fn, *args) -> None:
+    """fn(*args, torch's current stream of the GPU), with that GPU current."""
+    import torch
+    if torch.cuda.current_device() != gpu:
+        with torch.cuda.device(gpu):
+            return _launch(gpu, fn, *args)
+    rc = fn(*args, torch._C._cuda_getCurrentRawStream(gpu))
+    if rc != ACC_OK:
+        raise AccordionError(rc, _lib.accordion_operator_error().decode())
+
+
+def _workspace(gpu: int, fn, cfg, given):
+    """(tensor or None, pointer, bytes) of the workspace of a call: as given, or from torch's allocator for the current stream."""
+    n = C.c_size_t(0)
+    rc = fn(C.byref(cfg), C.byref(n))
+    if rc != ACC_OK:
+        raise AccordionError(rc, _lib.accordion_operator_error().decode())
+    if given is None:
+        if n.value == 0:
+            return None, None, 0
         import torch
-        device = tensors[0].device
-        for t in tensors:
-            if t is not None and (not t.is_cuda or t.device != device):
-                raise ValueError("all tensors must be on one GPU")
-        self.torch, self.device, self.guard = torch, device, None
-
-    def __enter__(self) -> int:
-        if self.torch.cuda.current_device() != self.device.index:
-            self.guard = self.torch.cuda.device(self.device)
-            self.guard.__enter__()
-        return self.torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
-
-    def workspace(self, lib, fn, cfg, given):
-        """(pointer, bytes) of the call's workspace; keeps the tensor it took until the call is enqueued."""
-        n = C.c_size_t(0)
-        _operator_check(lib, fn(C.byref(cfg), C.byref(n)))
-        if given is None:
-            if n.value == 0:
-                return None, 0
-            given = self.taken = self.torch.empty(n.value, dtype=self.torch.uint8, device=self.device)
-        _need(given.device == self.device and given.is_contiguous(), "workspace must be contiguous and on the tensors' GPU")
-        return given.data_ptr(), given.numel() * given.element_size()
+        given = torch.empty(n.value, dtype=torch.uint8, device=f"cuda:{gpu}")
+    elif given.get_device() != gpu or not given.is_contiguous():
+        raise ValueError("workspace must be contiguous and on the tensors' GPU")
+    return given, given.data_ptr(), given.numel() * given.element_size()
 
 
 def _embedding(ids, table, out, scale: float, accumulate: bool) -> acc_embedding:
     import torch
-    _need(ids.dtype in (torch.int32, torch.int64) and ids.is_contiguous(), "ids must be contiguous int32 or int64")
+    bits = 64 if ids.dtype == torch.int64 else 32 if ids.dtype == torch.int32 else 0
+    _need(bits and ids.is_contiguous(), "ids must be contiguous int32 or int64")
     vocab, dim, table_stride = _rows_of(table, "table")
     tokens, width, out_stride = _rows_of(out, "out")
     _need(table.dim() == 2 and width == dim and tokens == ids.numel(), "ids, table and out do not fit together")
-    return acc_embedding(vocab, dim, tokens, table_stride, out_stride, 32 if ids.dtype == torch.int32 else 64,
-                         _type_of(table, "table"), _type_of(out, "out"), int(accumulate), scale)
+    return acc_embedding(vocab, dim, tokens, table_stride, out_stride, bits, _type_of(table, "table"), _type_of(out, "out"),
+                         accumulate, scale)
 
 
 def embedding_forward(ids, table, out, scale: float = 1.0) -> None:
     """out[t, :] = scale * table[ids[t], :]; ids outside the table give zeros."""
     lib = load_library()
     cfg = _embedding(ids, table, out, scale, False)
-    with _Launch(ids, table, out) as stream:
-        _operator_check(lib, lib.accordion_embedding_forward(C.byref(cfg), ids.data_ptr(), table.data_ptr(), out.data_ptr(), stream))
+    _launch(_gpu_of(ids, table, out), lib.accordion_embedding_forward, C.byref(cfg), ids.data_ptr(), table.data_ptr(), out.data_ptr())
 
 
 def embedding_backward(ids, grad_out, grad_table, scale: float = 1.0, accumulate: bool = False, workspace=None) -> None:
     """grad_table[v, :] (+)= scale * sum of grad_out[t, :] over the t with ids[t] == v; grad_table is float32."""
-    import torch
     lib = load_library()
-    _need(grad_table.dtype == torch.float32, "grad_table must be float32")
     cfg = _embedding(ids, grad_table, grad_out, scale, accumulate)
-    launch = _Launch(ids, grad_out, grad_table)
-    with launch as stream:
-        ws, n = launch.workspace(lib, lib.accordion_embedding_workspace_bytes, cfg, workspace)
-        _operator_check(lib, lib.accordion_embedding_backward(C.byref(cfg), ids.data_ptr(), grad_out.data_ptr(),
-                                                              grad_table.data_ptr(), ws, n, stream))
+    _need(cfg.table_type == ACC_FLOAT, "grad_table must be float32")
+    gpu = _gpu_of(ids, grad_out, grad_table)
+    held, ws, n = _workspace(gpu, lib.accordion_embedding_workspace_bytes, cfg, workspace)
+    _launch(gpu, lib.accordion_embedding_backward, C.byref(cfg), ids.data_ptr(), grad_out.data_ptr(), grad_table.data_ptr(), ws, n)
 
 
 def layernorm_forward(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-5) -> None:
@@ -348,13 +352,13 @@ def layernorm_forward(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-
     lib = load_library()
     rows, dim, x_stride = _rows_of(x, "x")
     y_rows, y_dim, y_stride = _rows_of(y, "y")
-    _need((y_rows, y_dim, y.dtype) == (rows, dim, x.dtype), "x and y do not fit together")
+    _need(y_rows == rows and y_dim == dim and y.dtype == x.dtype, "x and y do not fit together")
     f = torch.float32
     w, b = _plain(weight, "weight", (dim,), f), _plain(bias, "bias", (dim,), f)
     m, r = _plain(mean, "mean", (rows,), f), _plain(rstd, "rstd", (rows,), f)
     cfg = acc_layernorm(rows, dim, x_stride, y_stride, 0, _type_of(x, "x"), 0, eps)
-    with _Launch(x, weight, bias, y, mean, rstd) as stream:
-        _operator_check(lib, lib.accordion_layernorm_forward(C.byref(cfg), x.data_ptr(), w, b, y.data_ptr(), m, r, stream))
+    _launch(_gpu_of(x, weight, bias, y, mean, rstd), lib.accordion_layernorm_forward, C.byref(cfg), x.data_ptr(), w, b, y.data_ptr(),
+            m, r)
 
 
 def layernorm_backward(grad_y, x, weight, mean, rstd, grad_x, grad_weight, grad_bias=None, accumulate: bool = False,
@@ -365,24 +369,26 @@ def layernorm_backward(grad_y, x, weight, mean, rstd, grad_x, grad_weight, grad_
     rows, dim, x_stride = _rows_of(x, "x")
     g_rows, g_dim, g_stride = _rows_of(grad_y, "grad_y")
     d_rows, d_dim, d_stride = _rows_of(grad_x, "grad_x")
-    _need((g_rows, g_dim, grad_y.dtype) == (rows, dim, x.dtype) and (d_rows, d_dim, grad_x.dtype) == (rows, dim, x.dtype),
+    _need(g_rows == d_rows == rows and g_dim == d_dim == dim and grad_y.dtype == grad_x.dtype == x.dtype,
           "x, grad_y and grad_x do not fit together")
     f = torch.float32
     w, m, r = _plain(weight, "weight", (dim,), f), _plain(mean, "mean", (rows,), f), _plain(rstd, "rstd", (rows,), f)
     dw, db = _plain(grad_weight, "grad_weight", (dim,), f), _plain(grad_bias, "grad_bias", (dim,), f)
-    cfg = acc_layernorm(rows, dim, x_stride, g_stride, d_stride, _type_of(x, "x"), int(accumulate), 0.0)
-    launch = _Launch(x, grad_y, weight, mean, rstd, grad_x, grad_weight, grad_bias)
-    with launch as stream:
-        ws, n = launch.workspace(lib, lib.accordion_layernorm_workspace_bytes, cfg, workspace)
-        _operator_check(lib, lib.accordion_layernorm_backward(C.byref(cfg), grad_y.data_ptr(), x.data_ptr(), w, m, r,
-                                                              grad_x.data_ptr(), dw, db, ws, n, stream))
+    cfg = acc_layernorm(rows, dim, x_stride, g_stride, d_stride, _type_of(x, "x"), accumulate, 0.0)
+    gpu = _gpu_of(x, grad_y, weight, mean, rstd, grad_x, grad_weight, grad_bias)
+    held, ws, n = _workspace(gpu, lib.accordion_layernorm_workspace_bytes, cfg, workspace)
+    _launch(gpu, lib.accordion_layernorm_backward, C.byref(cfg), grad_y.data_ptr(), x.data_ptr(), w, m, r, grad_x.data_ptr(), dw, db,
+            ws, n)
 
 
 def _steps_of(t, name: str, like) -> Tuple[int, int]:
     """(elements between sequences, between steps) of a batch x steps x channels tensor."""
-    _need(t.dim() == 3 and t.shape == like.shape and t.dtype == like.dtype, f"{name} must have gate's shape and type")
-    _need(t.stride(2) == 1 or t.shape[2] <= 1, f"{name}: the channels of a step must be contiguous")
-    return t.stride(0), t.stride(1)
+    if t.shape != like.shape or t.dtype != like.dtype:
+        raise ValueError(f"{name} must have gate's shape and type")
+    batch, step, channel = t.stride()
+    if channel != 1 and t.shape[2] > 1:
+        raise ValueError(f"{name}: the channels of a step must be contiguous")
+    return batch, step
 
 
 def recurrence_forward(gate, input, out, h0=None, h_last=None, lengths=None, workspace=None) -> None:
@@ -394,14 +400,13 @@ def recurrence_forward(gate, input, out, h0=None, h_last=None, lengths=None, wor
     batch, steps, channels = gate.shape
     cfg = acc_recurrence(batch, steps, channels, *_steps_of(gate, "gate", gate), *_steps_of(input, "input", gate),
                          *_steps_of(out, "out", gate), 0, 0, 0, 0, 0, 0, _type_of(gate, "gate"))
-    ends = (batch, channels)
-    first, last = _plain(h0, "h0", ends, torch.float32), _plain(h_last, "h_last", ends, torch.float32)
+    ends, f = (batch, channels), torch.float32
+    first, last = _plain(h0, "h0", ends, f), _plain(h_last, "h_last", ends, f)
     n_steps = _plain(lengths, "lengths", (batch,), torch.int32)
-    launch = _Launch(gate, input, out, h0, h_last, lengths)
-    with launch as stream:
-        ws, n = launch.workspace(lib, lib.accordion_recurrence_workspace_bytes, cfg, workspace)
-        _operator_check(lib, lib.accordion_recurrence_forward(C.byref(cfg), gate.data_ptr(), input.data_ptr(), first, n_steps,
-                                                              out.data_ptr(), last, ws, n, stream))
+    gpu = _gpu_of(gate, input, out, h0, h_last, lengths)
+    held, ws, n = _workspace(gpu, lib.accordion_recurrence_workspace_bytes, cfg, workspace)
+    _launch(gpu, lib.accordion_recurrence_forward, C.byref(cfg), gate.data_ptr(), input.data_ptr(), first, n_steps, out.data_ptr(),
+            last, ws, n)
 
 
 def recurrence_backward(gate, input, out, grad_out, grad_gate, grad_input, h0=None, grad_last=None, grad_h0=None,
@@ -418,21 +423,24 @@ def recurrence_backward(gate, input, out, grad_out, grad_gate, grad_input, h0=No
     ends, f = (batch, channels), torch.float32
     first, last, dh0 = _plain(h0, "h0", ends, f), _plain(grad_last, "grad_last", ends, f), _plain(grad_h0, "grad_h0", ends, f)
     n_steps = _plain(lengths, "lengths", (batch,), torch.int32)
-    launch = _Launch(gate, input, out, grad_out, grad_gate, grad_input, h0, grad_last, grad_h0, lengths)
-    with launch as stream:
-        ws, n = launch.workspace(lib, lib.accordion_recurrence_workspace_bytes, cfg, workspace)
-        _operator_check(lib, lib.accordion_recurrence_backward(
-            C.byref(cfg), gate.data_ptr(), input.data_ptr(), out.data_ptr(), first, n_steps, grad_out.data_ptr(), last,
-            grad_gate.data_ptr(), grad_input.data_ptr(), dh0, ws, n, stream))
+    gpu = _gpu_of(gate, input, out, grad_out, grad_gate, grad_input, h0, grad_last, grad_h0, lengths)
+    held, ws, n = _workspace(gpu, lib.accordion_recurrence_workspace_bytes, cfg, workspace)
+    _launch(gpu, lib.accordion_recurrence_backward, C.byref(cfg), gate.data_ptr(), input.data_ptr(), out.data_ptr(), first, n_steps,
+            grad_out.data_ptr(), last, grad_gate.data_ptr(), grad_input.data_ptr(), dh0, ws, n)
 
 
 def adamw_state_elements(sizes: Sequence[int], state_bits: int = 32) -> int:
     """Elements of each moment of adamw_step for tensors of these sizes; host arithmetic only."""
     lib = load_library()
     arr = (C.c_int64 * max(1, len(sizes)))(*sizes)
-    cfg = acc_adamw(n_tensors=len(sizes), state_bits=state_bits, sizes_host=arr)
+    return _state_elements(lib, acc_adamw(n_tensors=len(sizes), state_bits=state_bits, sizes_host=arr))
+
+
+def _state_elements(lib, cfg: acc_adamw) -> int:
     out = C.c_int64(0)
-    _operator_check(lib, lib.accordion_adamw_state_elements(C.byref(cfg), C.byref(out)))
+    rc = lib.accordion_adamw_state_elements(C.byref(cfg), C.byref(out))
+    if rc != ACC_OK:
+        raise AccordionError(rc, lib.accordion_operator_error().decode())
     return out.value
 
 
@@ -445,6 +453,23 @@ def adamw_state(sizes: Sequence[int], state_bits: int = 32, device: str = "cuda:
         return tuple(torch.zeros(n, device=device) for _ in range(2)) + (None, None)
     return (*(torch.zeros(n, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2)),
             *(torch.zeros(n // ACC_ADAMW_BLOCK, device=device) for _ in range(2)))
+
+
+def _c_array(kind, code: str, values):
+    """A C array of numbers (through array.array: filling a ctypes array item by item takes twice as long)."""
+    held = array.array(code, values)
+    return (kind * len(held)).from_buffer(held)
+
+
+def _tensors_of(tensors: Sequence, name: str):
+    """(sizes, pointers, type, GPU) of contiguous tensors of one type on one GPU."""
+    import torch
+    t = torch.Tensor
+    kinds, gpus = {x.dtype for x in tensors}, set(map(t.get_device, tensors))
+    _need(len(kinds) == 1, f"{name} must be of one type")
+    _need(len(gpus) == 1, "all tensors must be on one GPU")
+    _need(all(map(t.is_contiguous, tensors)), f"{name} must be contiguous")
+    return list(map(t.numel, tensors)), _c_array(C.c_void_p, "Q", map(t.data_ptr, tensors)), kinds.pop(), gpus.pop()
 
 
 def adamw_step(weights: Sequence, grads: Sequence, state, lr: float, step: int, weight_decay=0.0,
@@ -461,40 +486,33 @@ def adamw_step(weights: Sequence, grads: Sequence, state, lr: float, step: int, 
         return
     m, v, m_scale, v_scale = state
     bits = 32 if m_scale is None else 8
-    sizes = (C.c_int64 * count)()
-    ptrs = [(C.c_void_p * count)() for _ in range(3)]
-    w_type, g_type, device = weights[0].dtype, grads[0].dtype, weights[0].device
-    elements = 0
-    for i in range(count):
-        w, g = weights[i], grads[i]
-        n = w.numel()
-        _need(w.dtype == w_type and g.dtype == g_type and g.numel() == n, "weights and grads do not fit together")
-        _need(w.is_contiguous() and g.is_contiguous(), "weights and grads must be contiguous")
-        _need(w.device == device and g.device == device, "all tensors must be on one GPU")
-        sizes[i], ptrs[0][i], ptrs[1][i] = n, w.data_ptr(), g.data_ptr()
-        elements += n if bits == 32 else -(-n // ACC_ADAMW_BLOCK) * ACC_ADAMW_BLOCK
-        if copies is not None and copies[i] is not None:
-            c = copies[i]
-            _need(c.dtype == torch.bfloat16 and c.numel() == n and c.is_contiguous() and c.device == device,
-                  "a copy must be bfloat16, contiguous, of its tensor's size, on its GPU")
-            ptrs[2][i] = c.data_ptr()
+    sizes, w_ptrs, _, gpu = _tensors_of(weights, "weights")
+    g_sizes, g_ptrs, _, g_gpu = _tensors_of(grads, "grads")
+    _need(sizes == g_sizes, "weights and grads do not fit together")
+    _need(gpu == g_gpu, "all tensors must be on one GPU")
+    c_ptrs = None
+    if copies is not None:
+        kept = [c for c in copies if c is not None]
+        if kept:
+            c_sizes, _, c_type, c_gpu = _tensors_of(kept, "copies")
+            _need(c_type == torch.bfloat16 and c_gpu == gpu and c_sizes == [n for n, c in zip(sizes, copies) if c is not None],
+                  "a copy must be bfloat16, of its tensor's size, on its GPU")
+            c_ptrs = _c_array(C.c_void_p, "Q", [0 if c is None else c.data_ptr() for c in copies])
+    cfg = acc_adamw(count, _type_of(weights[0], "weights"), _type_of(grads[0], "grads"), bits, _c_array(C.c_int64, "q", sizes), None, lr,
+                    betas[0], betas[1], eps, step)
+    elements = _state_elements(lib, cfg)
     held = torch.float32 if bits == 32 else torch.float8_e4m3fn
     mp, vp = _plain(m, "m", (elements,), held), _plain(v, "v", (elements,), held)
     blocks = (elements // ACC_ADAMW_BLOCK,)
     ms, vs = _plain(m_scale, "m_scale", blocks, torch.float32), _plain(v_scale, "v_scale", blocks, torch.float32)
     _need(grad_scale is None or (grad_scale.dtype == torch.float32 and grad_scale.numel() == 1), "grad_scale must be one float32 element")
-    decay = None
     if not isinstance(weight_decay, (int, float)):
         _need(len(weight_decay) == count, "one weight decay per tensor")
-        decay = (C.c_float * count)(*weight_decay)
+        cfg.weight_decay_host = _c_array(C.c_float, "f", weight_decay)
     elif weight_decay != 0.0:
-        decay = (C.c_float * count)(*([weight_decay] * count))
-    cfg = acc_adamw(count, _type_of(weights[0], "weights"), _type_of(grads[0], "grads"), bits, sizes, decay, lr, betas[0], betas[1],
-                    eps, step)
-    with _Launch(weights[0], m, v, m_scale, v_scale, grad_scale) as stream:
-        _operator_check(lib, lib.accordion_adamw_step(
-            C.byref(cfg), ptrs[0], ptrs[1], ptrs[2] if copies is not None else None, mp, vp, ms, vs,
-            grad_scale.data_ptr() if grad_scale is not None else None, stream))
+        cfg.weight_decay_host = _c_array(C.c_float, "f", [weight_decay] * count)
+    _launch(_gpu_of(weights[0], m, v, m_scale, v_scale, grad_scale), lib.accordion_adamw_step, C.byref(cfg), w_ptrs, g_ptrs, c_ptrs, mp,
+            vp, ms, vs, grad_scale.data_ptr() if grad_scale is not None else None)
 
 
 class Accordion:

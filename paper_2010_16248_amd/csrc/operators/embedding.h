@@ -43,13 +43,17 @@ __device__ __forceinline__ uint32_t key_of_id(I id, uint32_t vocab) {
 
 // The zeros of the rows that no token asks for, in the launch that starts the sort: the sort waits for latencies
 // and leaves the memory idle.  (Rows with tokens are written again later.)
+constexpr int kClearAhead = 4;
 __device__ __forceinline__ void clear_rows(float* __restrict__ table, int64_t vocab, int64_t dim, int64_t stride,
                                            int64_t block, int64_t blocks) {
   const F32<4> zero = {0.f, 0.f, 0.f, 0.f};
   if (stride == dim) {
-    const int64_t n = vocab * dim;
-    for (int64_t i = (block * blockDim.x + threadIdx.x) * 4; i < n; i += blocks * blockDim.x * 4)
-      store_some<float, 4>(table + i, zero, n - i);
+    const int64_t n = vocab * dim, step = (int64_t)blockDim.x * 4;
+    for (int64_t i = block * step * kClearAhead + threadIdx.x * 4; i < n; i += blocks * step * kClearAhead) {
+#pragma unroll
+      for (int k = 0; k < kClearAhead; ++k)
+        if (i + k * step < n) store_some_stream<float, 4>(table + i + k * step, zero, n - (i + k * step));
+    }
   } else {
     for (int64_t r = block; r < vocab; r += blocks)
       for (int64_t i = (int64_t)threadIdx.x * 4; i < dim; i += (int64_t)blockDim.x * 4)
@@ -57,8 +61,9 @@ __device__ __forceinline__ void clear_rows(float* __restrict__ table, int64_t vo
   }
 }
 
-// Few tokens: a token's place is the number of tokens that come before it, counted against all others.
-// A workgroup places 64 tokens (one per lane); its waves share the tokens to compare with.
+// Few tokens: a token's place is the number of tokens that come before it, counted against all others.  A workgroup
+// holds all keys in LDS and places 64 tokens (one per lane); its waves share the tokens to compare with, four per
+// read: two operations per pair of tokens.
 constexpr int kRankThreads = 1024;
 template <typename I>
 __global__ __launch_bounds__(kRankThreads) void embedding_rank_kernel(const I* __restrict__ ids, int n, uint32_t vocab,
@@ -69,21 +74,35 @@ __global__ __launch_bounds__(kRankThreads) void embedding_rank_kernel(const I* _
     clear_rows(table, rows, dim, stride, (int64_t)blockIdx.x - rank_blocks, (int64_t)gridDim.x - rank_blocks);
     return;
   }
+  extern __shared__ uint32_t keys[];     // n, filled up to whole groups of four with keys above all others
   __shared__ uint32_t part[kRankThreads];
   constexpr int waves = kRankThreads / kWave;
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int groups = (n + 3) >> 2;
+  for (int j = threadIdx.x; j < 4 * groups; j += kRankThreads) keys[j] = j < n ? key_of_id(ids[j], vocab) : 0xffffffffu;
+  __syncthreads();
   const int first = blockIdx.x * kWave, i = first + l;
-  const uint32_t mine = i < n ? key_of_id(ids[i], vocab) : 0u;
-  const int share = (n + waves - 1) / waves;
-  const int lo = w * share, hi = min(n, lo + share);
+  const uint32_t mine = keys[min(i, n - 1)];
+  const uint4* quads = reinterpret_cast<const uint4*>(keys);
+  const int share = (groups + waves - 1) / waves, lo = min(w * share, groups), hi = min(lo + share, groups);
+  // in front of the workgroup's own tokens an equal key counts, behind them it does not (16 groups are the workgroup's own)
+  const int own = first >> 2;
   uint32_t before = 0;
-  // in front of the workgroup's own tokens an equal key counts, behind them it does not
-  for (int j = lo; j < min(hi, first); ++j) before += key_of_id(ids[j], vocab) <= mine;
-  for (int j = max(lo, first); j < min(hi, first + kWave); ++j) {
-    const uint32_t k = key_of_id(ids[j], vocab);
-    before += k < mine || (k == mine && j < i);
+#pragma unroll 4
+  for (int j = lo; j < min(hi, own); ++j) {
+    const uint4 k = quads[j];
+    before += (uint32_t)(k.x <= mine) + (uint32_t)(k.y <= mine) + (uint32_t)(k.z <= mine) + (uint32_t)(k.w <= mine);
   }
-  for (int j = max(lo, first + kWave); j < hi; ++j) before += key_of_id(ids[j], vocab) < mine;
+  for (int j = max(lo, own); j < min(hi, own + kWave / 4); ++j)
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t k = keys[4 * j + q];
+      before += k < mine || (k == mine && 4 * j + q < i);
+    }
+#pragma unroll 4
+  for (int j = max(lo, own + kWave / 4); j < hi; ++j) {
+    const uint4 k = quads[j];
+    before += (uint32_t)(k.x < mine) + (uint32_t)(k.y < mine) + (uint32_t)(k.z < mine) + (uint32_t)(k.w < mine);
+  }
   part[threadIdx.x] = before;
   __syncthreads();
   if (w == 0 && i < n) {
@@ -126,6 +145,8 @@ __global__ __launch_bounds__(kSortThreads) void embedding_count_kernel(const I* 
   for (int d = threadIdx.x; d < digits; d += kSortThreads) counts[(int64_t)blockIdx.x * digits + d] = count[d];
 }
 
+constexpr int kCountAhead = 16;   // tiles' counts under way
+
 template <typename I, bool FIRST>
 __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(const I* __restrict__ ids, const uint32_t* __restrict__ key,
                                                                       const uint32_t* __restrict__ pos, int64_t n, uint32_t vocab,
@@ -141,10 +162,15 @@ __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(const I* 
   // all tiles' tokens of smaller digits, and of this digit those of the tiles in front (kSortDigits == kSortThreads)
   uint32_t all = 0, front = 0;
   if (d < digits)
-    for (int t = 0; t < tiles; ++t) {
-      const uint32_t c = counts[(int64_t)t * digits + d];
-      if (t < (int)blockIdx.x) front += c;
-      all += c;
+    for (int t0 = 0; t0 < tiles; t0 += kCountAhead) {
+      uint32_t c[kCountAhead];
+#pragma unroll
+      for (int k = 0; k < kCountAhead; ++k) c[k] = t0 + k < tiles ? counts[(int64_t)(t0 + k) * digits + d] : 0u;
+#pragma unroll
+      for (int k = 0; k < kCountAhead; ++k) {
+        if (t0 + k < (int)blockIdx.x) front += c[k];
+        all += c[k];
+      }
     }
   uint32_t incl = all;
   for (int s = 1; s < kWave; s <<= 1) {
@@ -217,79 +243,100 @@ __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(const I* 
 }
 
 // ---- backward: sums over runs of equal ids ---------------------------------------------------------------
-// A workgroup takes a chunk of consecutive places of the order and up to 256 N columns.  A run of equal ids
-// inside the chunk is summed and written to its row; of a run that crosses the chunk's ends the part inside
-// is left in the workspace: parts[2 c] for a run that began in an earlier chunk, parts[2 c + 1] for one that
-// begins here and goes on.
-constexpr int kSumAhead = 8;   // rows under way
+// A wave takes a chunk of consecutive places of the order and 64 N columns.  A run of equal ids inside the chunk is
+// summed and written to its row; of a run that crosses the chunk's ends the part inside is left in the workspace:
+// parts[2 c] for a run that began in an earlier chunk, parts[2 c + 1] for one that begins here and goes on.
+constexpr int kSumAhead = 8;     // rows under way
+constexpr int kJoinRows = 16;    // parts under way
 
-template <typename T, int N>
+template <int N>
+__device__ __forceinline__ void to_row(float* to, const F32<N>& sum, const F32<N>& old, float scale, bool accumulate, int64_t left) {
+  F32<N> v = sum * scale;
+  if (accumulate) v = old + v;
+  store_some<float, N>(to, v, left);
+}
+
+// EVEN: N divides the columns.
+template <typename T, int N, bool ACCUMULATE, bool EVEN>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const uint32_t* __restrict__ skey, const uint32_t* __restrict__ spos,
                                                             int64_t n, int chunk, uint32_t vocab, const T* __restrict__ grad,
                                                             int64_t grad_stride, float* __restrict__ table, int64_t table_stride,
-                                                            int64_t dim, float scale, int accumulate, float* __restrict__ parts) {
-  const int64_t lo = (int64_t)blockIdx.x * chunk, hi = min(n, lo + chunk);
-  const int64_t c = ((int64_t)blockIdx.y * 256 + threadIdx.x) * N, left = dim - c;
-  const uint32_t front = lo > 0 ? skey[lo - 1] : 0xffffffffu, behind = hi < n ? skey[hi] : 0xffffffffu;
+                                                            int64_t dim, uint32_t across, float scale, float* __restrict__ parts) {
+  // neighbouring waves take neighbouring columns of one chunk
+  const uint32_t unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t b = unit / across, lo = b * chunk, hi = min(n, lo + chunk);
+  const int64_t c = ((int64_t)(unit % across) * kWave + (threadIdx.x & 63)) * N, left = EVEN ? min(dim - c, (int64_t)N) : dim - c;
+  if (lo >= n || left <= 0) return;
+  bool opened = lo == 0 || skey[lo - 1] != skey[lo];   // the run began in this chunk
   F32<N> acc = {};
-  uint32_t run = skey[lo];
-  bool opened = run != front;    // the run began in this chunk
-  auto close = [&](uint32_t row, bool ends) {
-    if (row >= vocab || left <= 0) return;
-    if (!opened) {
-      store_some<float, N>(parts + (2 * (int64_t)blockIdx.x) * dim + c, acc, left);
-    } else if (!ends) {
-      store_some<float, N>(parts + (2 * (int64_t)blockIdx.x + 1) * dim + c, acc, left);
-    } else {
-      float* to = table + (int64_t)row * table_stride + c;
-      F32<N> v = acc * scale;
-      if (accumulate) v = widen<float, N>(load_some<N>(to, left)) + v;
-      store_some<float, N>(to, v, left);
-    }
-  };
   for (int64_t i0 = lo; i0 < hi; i0 += kSumAhead) {
     Pack<T, N> v[kSumAhead];
-    uint32_t key[kSumAhead];
+    uint32_t key[kSumAhead + 1];
+#pragma unroll
+    for (int j = 0; j <= kSumAhead; ++j) key[j] = i0 + j < n ? skey[i0 + j] : 0xffffffffu;
 #pragma unroll
     for (int j = 0; j < kSumAhead; ++j) {
-      const int64_t i = min(i0 + j, hi - 1);
-      key[j] = skey[i];
-      v[j] = load_some<N>(grad + (int64_t)spos[i] * grad_stride + c, key[j] < vocab ? left : 0);
+      if (i0 + j < hi && key[j] < vocab) {
+        const T* from = grad + (int64_t)spos[i0 + j] * grad_stride + c;
+        v[j] = EVEN ? load<N>(from) : load_some<N>(from, left);
+      }
     }
 #pragma unroll
     for (int j = 0; j < kSumAhead; ++j) {
-      if (i0 + j >= hi) break;
-      if (key[j] != run) {
-        close(run, true);
-        run = key[j];
-        opened = true;
-        acc = F32<N>{};
+      if (i0 + j < hi && key[j] < vocab) {
+        acc += widen<T, N>(v[j]);
+        if (key[j + 1] != key[j]) {                    // the run ends here
+          if (opened) {
+            float* to = table + (int64_t)key[j] * table_stride + c;
+            F32<N> old = {};
+            if (ACCUMULATE) old = widen<float, N>(EVEN ? load<N>(to) : load_some<N>(to, left));
+            to_row<N>(to, acc, old, scale, ACCUMULATE, EVEN ? N : left);
+          } else {
+            store_some<float, N>(parts + 2 * b * dim + c, acc, EVEN ? N : left);
+          }
+          opened = true;
+          acc = F32<N>{};
+        } else if (i0 + j == hi - 1) {                 // ... or in a later chunk
+          store_some<float, N>(parts + (2 * b + (opened ? 1 : 0)) * dim + c, acc, EVEN ? N : left);
+        }
       }
-      acc += widen<T, N>(v[j]);
     }
   }
-  close(run, run != behind);
 }
 
-// The runs that cross chunks: the workgroup of the chunk where one begins adds its parts in order.
+// The runs that cross chunks: the wave of the chunk where one begins adds its parts in order.
 template <int N>
 __global__ __launch_bounds__(256) void embedding_join_kernel(const uint32_t* __restrict__ skey, int64_t n, int chunk, int64_t chunks,
                                                              uint32_t vocab, const float* __restrict__ parts,
                                                              float* __restrict__ table, int64_t table_stride, int64_t dim, float scale,
                                                              int accumulate) {
-  const int64_t b = blockIdx.x, lo = b * chunk, hi = lo + chunk;
+  const int64_t b = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lo = b * chunk, hi = lo + chunk;
   if (hi >= n) return;
   const uint32_t row = skey[hi];
   if (row >= vocab || skey[hi - 1] != row || (lo > 0 && skey[lo] == row && skey[lo - 1] == row)) return;
-  const int64_t c = ((int64_t)blockIdx.y * 256 + threadIdx.x) * N, left = dim - c;
+  // the chunks that begin with the run's id
+  const int l = threadIdx.x & 63;
+  int64_t end = b + 1;
+  for (;;) {
+    const int64_t k = end + l;
+    const uint64_t others = __ballot(k >= chunks || skey[min(k, chunks - 1) * chunk] != row);
+    end += others ? __builtin_ctzll(others) : kWave;
+    if (others) break;
+  }
+  const int64_t c = ((int64_t)blockIdx.y * kWave + l) * N, left = dim - c;
   if (left <= 0) return;
-  F32<N> acc = widen<float, N>(load_some<N>(parts + (2 * b + 1) * dim + c, left));
-  for (int64_t k = b + 1; k < chunks && skey[k * chunk] == row; ++k)
-    acc += widen<float, N>(load_some<N>(parts + 2 * k * dim + c, left));
   float* to = table + (int64_t)row * table_stride + c;
-  F32<N> v = acc * scale;
-  if (accumulate) v = widen<float, N>(load_some<N>(to, left)) + v;
-  store_some<float, N>(to, v, left);
+  F32<N> old = {}, acc = widen<float, N>(load_some<N>(parts + (2 * b + 1) * dim + c, left));
+  if (accumulate) old = widen<float, N>(load_some<N>(to, left));
+  for (int64_t k = b + 1; k < end; k += kJoinRows) {
+    Pack<float, N> v[kJoinRows];
+#pragma unroll
+    for (int j = 0; j < kJoinRows; ++j) v[j] = load_some<N>(parts + 2 * min(k + j, end - 1) * dim + c, left);
+#pragma unroll
+    for (int j = 0; j < kJoinRows; ++j)
+      if (k + j < end) acc += widen<float, N>(v[j]);
+  }
+  to_row<N>(to, acc, old, scale, accumulate != 0, left);
 }
 
 }  // namespace accop

@@ -239,6 +239,7 @@ __global__ __launch_bounds__(256) void layernorm_columns_kernel(const T* __restr
 
 // Adds the workgroups' sums per column, in order: a workgroup takes 64 columns of one of the two gradients, each
 // of its 16 waves a run of consecutive parts.
+constexpr int kJoinAhead = 16;   // parts under way
 __global__ __launch_bounds__(1024) void layernorm_join_kernel(const float* __restrict__ parts, int count, int dim,
                                                               float* __restrict__ grad_weight, float* __restrict__ grad_bias,
                                                               int accumulate) {
@@ -250,7 +251,13 @@ __global__ __launch_bounds__(1024) void layernorm_join_kernel(const float* __res
   const int share = (count + 15) / 16, lo = w * share, hi = min(count, lo + share);
   float s = 0.f;
   if (c < dim)
-    for (int i = lo; i < hi; ++i) s += parts[(2 * (int64_t)i + blockIdx.y) * dim + c];
+    for (int i = lo; i < hi; i += kJoinAhead) {
+      float v[kJoinAhead];
+#pragma unroll
+      for (int k = 0; k < kJoinAhead; ++k) v[k] = i + k < hi ? parts[(2 * (int64_t)(i + k) + blockIdx.y) * dim + c] : 0.f;
+#pragma unroll
+      for (int k = 0; k < kJoinAhead; ++k) s += v[k];
+    }
   fold[w][l] = s;
   __syncthreads();
   if (w == 0 && c < dim) {

@@ -60,6 +60,12 @@ __device__ __forceinline__ void store_some(T* p, const F32<N>& v, int64_t n) {
     if (i < n) p[i] = (T)v[i];
 }
 
+template <typename T, int N>
+__device__ __forceinline__ void store_some_stream(T* p, const F32<N>& v, int64_t n) {
+  if (n >= N) store_stream<T, N>(p, v);
+  else store_some<T, N>(p, v, n);
+}
+
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));

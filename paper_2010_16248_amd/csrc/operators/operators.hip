@@ -82,7 +82,7 @@ int32_t launched() {
 
 // ---- embedding --------------------------------------------------------------------------------------
 
-constexpr int64_t kRankTokens = 8192;   // up to here the order is counted, from here on it is sorted by digits
+constexpr int64_t kRankTokens = 14336;  // up to here the order is counted, from here on it is sorted by digits
 
 int32_t check_embedding(const acc_embedding* e) {
   REQUIRE(e, "config is NULL");
@@ -117,7 +117,10 @@ EmbeddingPlan plan_embedding(const acc_embedding& e) {
     p.tile = up(up(n, kSortTiles), kSortStep) * kSortStep;
     p.tiles = (int)up(n, p.tile);
   }
-  p.chunk = n <= 4096 ? 16 : (n <= 32768 ? 32 : 64);
+  // A wave goes through a chunk's tokens one after the other, and through the parts of a run, of which there may be one per
+  // chunk: chunks of about sqrt(n) / 8 to sqrt(n) / 4.
+  p.chunk = 8;
+  while (p.chunk < 128 && 64LL * p.chunk * p.chunk < n) p.chunk *= 2;
   p.chunks = up(n, p.chunk);
   int64_t at = 0;
   auto take = [&](int64_t bytes) { const int64_t o = at; at += round256(bytes); return o; };
@@ -153,10 +156,20 @@ void lookup_to(const acc_embedding& e, const void* ids, const void* table, void*
 template <typename T>
 void sum_runs(const acc_embedding& e, const EmbeddingPlan& p, const uint32_t* key, const uint32_t* pos, const void* grad,
               float* table, float* parts, void* stream) {
-  constexpr int N = sizeof(T) == 2 ? 8 : 4;
-  LAUNCH((embedding_sum_kernel<T, N>), dim3((unsigned)p.chunks, (unsigned)up(e.dim, 256 * N)), dim3(256), stream, key, pos, e.tokens,
-         p.chunk, (uint32_t)e.vocab, static_cast<const T*>(grad), e.out_stride, table, e.table_stride, e.dim, e.scale, e.accumulate,
-         parts);
+  constexpr int N = 4;
+  const int64_t across = up(e.dim, kWave * N);
+  const dim3 grid((unsigned)up(p.chunks * across, 4));
+#define SUM(ACCUMULATE, EVEN)                                                                                                      \
+  LAUNCH((embedding_sum_kernel<T, N, ACCUMULATE, EVEN>), grid, dim3(256), stream, key, pos, e.tokens, p.chunk, (uint32_t)e.vocab, \
+         static_cast<const T*>(grad), e.out_stride, table, e.table_stride, e.dim, (uint32_t)across, e.scale, parts)
+  if (e.dim % N == 0) {
+    if (e.accumulate) SUM(true, true);
+    else SUM(false, true);
+  } else {
+    if (e.accumulate) SUM(true, false);
+    else SUM(false, false);
+  }
+#undef SUM
 }
 
 template <typename I>
@@ -168,13 +181,14 @@ void embedding_gradient(const acc_embedding& e, const EmbeddingPlan& p, const I*
   float* parts = reinterpret_cast<float*>(ws + p.parts);
   const uint32_t vocab = (uint32_t)e.vocab;
   const int64_t stride = e.vocab == 1 ? e.dim : e.table_stride;
-  const int64_t clear = e.accumulate ? 0 : std::min<int64_t>(up(e.vocab * e.dim, 4 * kRankThreads), 8 * kComputeUnits);
+  const int64_t clear = e.accumulate ? 0 : std::min<int64_t>(up(e.vocab * e.dim, 4 * kClearAhead * kRankThreads), 8 * kComputeUnits);
   int at = 0;
   if (p.rank) {
     const int blocks = (int)up(e.tokens, kWave);
     if (blocks + clear > 0)
-      LAUNCH((embedding_rank_kernel<I>), dim3((unsigned)(blocks + clear)), dim3(kRankThreads), stream, ids, (int)e.tokens, vocab, key[0],
-             pos[0], blocks, table, e.vocab, e.dim, stride);
+      hipLaunchKernelGGL((embedding_rank_kernel<I>), dim3((unsigned)(blocks + clear)), dim3(kRankThreads),
+                         (unsigned)round256(4 * e.tokens), static_cast<hipStream_t>(stream), ids, (int)e.tokens, vocab, key[0], pos[0],
+                         blocks, table, e.vocab, e.dim, stride);
   } else {
     for (int pass = 0; pass < p.passes; ++pass) {
       const int shift = pass * p.digit_bits, digits = 1 << p.digit_bits, to = pass & 1;
@@ -196,7 +210,7 @@ void embedding_gradient(const acc_embedding& e, const EmbeddingPlan& p, const I*
   if (e.out_type == ACC_BF16) sum_runs<bf16>(e, p, key[at], pos[at], grad, table, parts, stream);
   else sum_runs<float>(e, p, key[at], pos[at], grad, table, parts, stream);
   if (p.chunks > 1)
-    LAUNCH((embedding_join_kernel<4>), dim3((unsigned)p.chunks, (unsigned)up(e.dim, 256 * 4)), dim3(256), stream, key[at], e.tokens,
+    LAUNCH((embedding_join_kernel<4>), dim3((unsigned)up(p.chunks, 4), (unsigned)up(e.dim, kWave * 4)), dim3(256), stream, key[at], e.tokens,
            p.chunk, p.chunks, vocab, parts, table, stride, e.dim, e.scale, e.accumulate);
 }
 
