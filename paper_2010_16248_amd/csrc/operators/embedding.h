@@ -41,23 +41,49 @@ __device__ __forceinline__ uint32_t key_of_id(I id, uint32_t vocab) {
   return v >= 0 && v < (int64_t)vocab ? (uint32_t)v : vocab;
 }
 
-// The zeros of the rows that no token asks for, in the launch that starts the sort: the sort waits for latencies
-// and leaves the memory idle.  (Rows with tokens are written again later.)
+// The zeros of the rows that no token asks for.  The launches that order the tokens wait for latencies and leave the
+// memory idle, so each of them also clears a share of the last rows, whatever they will hold (Clear); the rest is cleared in
+// the launch that sums, which knows the rows without tokens.
 constexpr int kClearAhead = 4;
-__device__ __forceinline__ void clear_rows(float* __restrict__ table, int64_t vocab, int64_t dim, int64_t stride,
-                                           int64_t block, int64_t blocks) {
+struct Clear {
+  float* table;
+  int64_t first, rows, dim, stride;   // rows [first, first + rows)
+};
+__device__ __forceinline__ void clear_rows(const Clear& s, int64_t block, int64_t blocks) {
   const F32<4> zero = {0.f, 0.f, 0.f, 0.f};
-  if (stride == dim) {
-    const int64_t n = vocab * dim, step = (int64_t)blockDim.x * 4;
+  float* table = s.table + s.first * s.stride;
+  if (s.stride == s.dim) {
+    const int64_t n = s.rows * s.dim, step = (int64_t)blockDim.x * 4;
     for (int64_t i = block * step * kClearAhead + threadIdx.x * 4; i < n; i += blocks * step * kClearAhead) {
 #pragma unroll
       for (int k = 0; k < kClearAhead; ++k)
         if (i + k * step < n) store_some_stream<float, 4>(table + i + k * step, zero, n - (i + k * step));
     }
   } else {
-    for (int64_t r = block; r < vocab; r += blocks)
-      for (int64_t i = (int64_t)threadIdx.x * 4; i < dim; i += (int64_t)blockDim.x * 4)
-        store_some<float, 4>(table + r * stride + i, zero, dim - i);
+    for (int64_t r = block; r < s.rows; r += blocks)
+      for (int64_t i = (int64_t)threadIdx.x * 4; i < s.dim; i += (int64_t)blockDim.x * 4)
+        store_some<float, 4>(table + r * s.stride + i, zero, s.dim - i);
+  }
+}
+
+// A wave clears those of kGapRows rows from `row` on (below `rows`) that no token asks for.
+constexpr int kGapRows = 4;
+__device__ __forceinline__ void clear_gaps(const Clear& s, int64_t row, int64_t rows, const uint32_t* __restrict__ skey, int64_t n) {
+  const int l = threadIdx.x & 63;
+  // lane l < kGapRows looks for its row in the order: the first place whose key is not below it
+  const uint32_t mine = (uint32_t)min(row + (l & (kGapRows - 1)), rows - 1);
+  int64_t lo = 0, hi = n;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) >> 1;
+    if (skey[mid] < mine) lo = mid + 1; else hi = mid;
+  }
+  const bool empty = l < kGapRows && row + l < rows && (lo == n || skey[lo] != mine);
+  uint64_t gaps = __ballot(empty);
+  const F32<4> zero = {0.f, 0.f, 0.f, 0.f};
+  while (gaps) {
+    float* to = s.table + (row + __builtin_ctzll(gaps)) * s.stride;
+    gaps &= gaps - 1;
+    for (int64_t i = 4 * l; i < s.dim; i += 4 * kWave) store_some_stream<float, 4>(to + i, zero, s.dim - i);
   }
 }
 
@@ -68,10 +94,9 @@ constexpr int kRankThreads = 1024;
 template <typename I>
 __global__ __launch_bounds__(kRankThreads) void embedding_rank_kernel(const I* __restrict__ ids, int n, uint32_t vocab,
                                                                      uint32_t* __restrict__ skey, uint32_t* __restrict__ spos,
-                                                                     int rank_blocks, float* __restrict__ table, int64_t rows,
-                                                                     int64_t dim, int64_t stride) {
+                                                                     int rank_blocks, Clear clear) {
   if ((int)blockIdx.x >= rank_blocks) {
-    clear_rows(table, rows, dim, stride, (int64_t)blockIdx.x - rank_blocks, (int64_t)gridDim.x - rank_blocks);
+    clear_rows(clear, (int64_t)blockIdx.x - rank_blocks, (int64_t)gridDim.x - rank_blocks);
     return;
   }
   extern __shared__ uint32_t keys[];     // n, filled up to whole groups of four with keys above all others
@@ -128,11 +153,9 @@ __device__ __forceinline__ uint32_t sort_key(const I* ids, const uint32_t* key, 
 template <typename I, bool FIRST>
 __global__ __launch_bounds__(kSortThreads) void embedding_count_kernel(const I* __restrict__ ids, const uint32_t* __restrict__ key,
                                                                       int64_t n, uint32_t vocab, int64_t tile, int shift, int digits,
-                                                                      uint32_t* __restrict__ counts, int tiles,
-                                                                      float* __restrict__ table, int64_t rows, int64_t dim,
-                                                                      int64_t stride) {
+                                                                      uint32_t* __restrict__ counts, int tiles, Clear clear) {
   if ((int)blockIdx.x >= tiles) {
-    clear_rows(table, rows, dim, stride, (int64_t)blockIdx.x - tiles, (int64_t)gridDim.x - tiles);
+    clear_rows(clear, (int64_t)blockIdx.x - tiles, (int64_t)gridDim.x - tiles);
     return;
   }
   __shared__ uint32_t count[kSortDigits];
@@ -152,7 +175,12 @@ __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(const I* 
                                                                       const uint32_t* __restrict__ pos, int64_t n, uint32_t vocab,
                                                                       int64_t tile, int shift, int digit_bits,
                                                                       const uint32_t* __restrict__ counts, int tiles,
-                                                                      uint32_t* __restrict__ key_out, uint32_t* __restrict__ pos_out) {
+                                                                      uint32_t* __restrict__ key_out, uint32_t* __restrict__ pos_out,
+                                                                      Clear clear) {
+  if ((int)blockIdx.x >= tiles) {
+    clear_rows(clear, (int64_t)blockIdx.x - tiles, (int64_t)gridDim.x - tiles);
+    return;
+  }
   constexpr int waves = kSortThreads / kWave;
   __shared__ uint32_t base[kSortDigits];               // where the tile's next token of a digit goes
   __shared__ uint16_t seen[waves][kSortDigits];        // tokens of a digit in a wave, then in the waves before it
@@ -256,14 +284,21 @@ __device__ __forceinline__ void to_row(float* to, const F32<N>& sum, const F32<N
   store_some<float, N>(to, v, left);
 }
 
-// EVEN: N divides the columns.
-template <typename T, int N, bool ACCUMULATE, bool EVEN>
+// EVEN: N divides the columns.  STREAM: gradients and rows go past the caches (131072 tokens x 2048 bf16 into 65537 rows: 271 ->
+// 247 us, added to what is there 276 -> 253; 2800 tokens x 672 fp32: 25.7 -> 26.5).
+template <typename T, int N, bool ACCUMULATE, bool EVEN, bool STREAM>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const uint32_t* __restrict__ skey, const uint32_t* __restrict__ spos,
                                                             int64_t n, int chunk, uint32_t vocab, const T* __restrict__ grad,
                                                             int64_t grad_stride, float* __restrict__ table, int64_t table_stride,
-                                                            int64_t dim, uint32_t across, float scale, float* __restrict__ parts) {
-  // neighbouring waves take neighbouring columns of one chunk
+                                                            int64_t dim, uint32_t across, uint32_t units, float scale,
+                                                            float* __restrict__ parts, int64_t gap_rows) {
+  // neighbouring waves take neighbouring columns of one chunk; those beyond the chunks' clear rows [0, gap_rows)
   const uint32_t unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (unit >= units) {
+    const int64_t row = (int64_t)(unit - units) * kGapRows;
+    if (row < gap_rows) clear_gaps(Clear{table, 0, gap_rows, dim, table_stride}, row, gap_rows, skey, n);
+    return;
+  }
   const int64_t b = unit / across, lo = b * chunk, hi = min(n, lo + chunk);
   const int64_t c = ((int64_t)(unit % across) * kWave + (threadIdx.x & 63)) * N, left = EVEN ? min(dim - c, (int64_t)N) : dim - c;
   if (lo >= n || left <= 0) return;
@@ -278,7 +313,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const uint32_t* __re
     for (int j = 0; j < kSumAhead; ++j) {
       if (i0 + j < hi && key[j] < vocab) {
         const T* from = grad + (int64_t)spos[i0 + j] * grad_stride + c;
-        v[j] = EVEN ? load<N>(from) : load_some<N>(from, left);
+        v[j] = STREAM ? load_stream<N>(from) : EVEN ? load<N>(from) : load_some<N>(from, left);
       }
     }
 #pragma unroll
@@ -290,7 +325,8 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const uint32_t* __re
             float* to = table + (int64_t)key[j] * table_stride + c;
             F32<N> old = {};
             if (ACCUMULATE) old = widen<float, N>(EVEN ? load<N>(to) : load_some<N>(to, left));
-            to_row<N>(to, acc, old, scale, ACCUMULATE, EVEN ? N : left);
+            if (STREAM) store_stream<float, N>(to, ACCUMULATE ? old + acc * scale : acc * scale);
+            else to_row<N>(to, acc, old, scale, ACCUMULATE, EVEN ? N : left);
           } else {
             store_some<float, N>(parts + 2 * b * dim + c, acc, EVEN ? N : left);
           }

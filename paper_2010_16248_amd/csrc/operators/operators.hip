@@ -153,21 +153,30 @@ void lookup_to(const acc_embedding& e, const void* ids, const void* table, void*
   e.out_type == ACC_BF16 ? lookup<I, T, bf16>(e, ids, table, out, stream) : lookup<I, T, float>(e, ids, table, out, stream);
 }
 
+constexpr int64_t kSumStream = 128 << 20;   // bytes of gradients that are streamed from here on (they fit no cache)
+// Rows cleared beside the ordering of the tokens: what the memory takes while a launch of it lasts.
+constexpr int64_t kClearRank = 40 << 20, kClearCount = 16 << 20, kClearPlace = 48 << 20;   // bytes
+
 template <typename T>
 void sum_runs(const acc_embedding& e, const EmbeddingPlan& p, const uint32_t* key, const uint32_t* pos, const void* grad,
-              float* table, float* parts, void* stream) {
+              float* table, int64_t stride, float* parts, int64_t gap_rows, void* stream) {
   constexpr int N = 4;
-  const int64_t across = up(e.dim, kWave * N);
-  const dim3 grid((unsigned)up(p.chunks * across, 4));
-#define SUM(ACCUMULATE, EVEN)                                                                                                      \
-  LAUNCH((embedding_sum_kernel<T, N, ACCUMULATE, EVEN>), grid, dim3(256), stream, key, pos, e.tokens, p.chunk, (uint32_t)e.vocab, \
-         static_cast<const T*>(grad), e.out_stride, table, e.table_stride, e.dim, (uint32_t)across, e.scale, parts)
-  if (e.dim % N == 0) {
-    if (e.accumulate) SUM(true, true);
-    else SUM(false, true);
+  const int64_t across = up(e.dim, kWave * N), units = p.chunks * across;
+  const dim3 grid((unsigned)up(units + up(gap_rows, kGapRows), 4));
+  const bool stream_rows = e.tokens * e.dim * (int64_t)sizeof(T) > kSumStream;
+#define SUM(ACCUMULATE, EVEN, STREAM)                                                                                              \
+  LAUNCH((embedding_sum_kernel<T, N, ACCUMULATE, EVEN, STREAM>), grid, dim3(256), stream, key, pos, e.tokens, p.chunk,             \
+         (uint32_t)e.vocab, static_cast<const T*>(grad), e.out_stride, table, stride, e.dim, (uint32_t)across, (uint32_t)units,    \
+         e.scale, parts, gap_rows)
+  if (e.dim % N != 0) {
+    if (e.accumulate) SUM(true, false, false);
+    else SUM(false, false, false);
+  } else if (stream_rows) {
+    if (e.accumulate) SUM(true, true, true);
+    else SUM(false, true, true);
   } else {
-    if (e.accumulate) SUM(true, false);
-    else SUM(false, false);
+    if (e.accumulate) SUM(true, true, false);
+    else SUM(false, true, false);
   }
 #undef SUM
 }
@@ -181,34 +190,44 @@ void embedding_gradient(const acc_embedding& e, const EmbeddingPlan& p, const I*
   float* parts = reinterpret_cast<float*>(ws + p.parts);
   const uint32_t vocab = (uint32_t)e.vocab;
   const int64_t stride = e.vocab == 1 ? e.dim : e.table_stride;
-  const int64_t clear = e.accumulate ? 0 : std::min<int64_t>(up(e.vocab * e.dim, 4 * kClearAhead * kRankThreads), 8 * kComputeUnits);
+  // rows [0, dirty) are still to be cleared; share() takes the last ones of them off, as many as `bytes` hold
+  int64_t dirty = e.accumulate ? 0 : e.vocab;
+  auto share = [&](int64_t bytes) {
+    const int64_t rows = std::min(dirty, std::max<int64_t>(1, bytes / (4 * e.dim)));
+    dirty -= rows;
+    return Clear{table, dirty, rows, e.dim, stride};
+  };
+  auto blocks = [&](const Clear& c) { return std::min<int64_t>(up(c.rows * c.dim, 4 * kClearAhead * 1024), 8 * kComputeUnits); };
   int at = 0;
   if (p.rank) {
-    const int blocks = (int)up(e.tokens, kWave);
-    if (blocks + clear > 0)
-      hipLaunchKernelGGL((embedding_rank_kernel<I>), dim3((unsigned)(blocks + clear)), dim3(kRankThreads),
+    const int rank_blocks = (int)up(e.tokens, kWave);
+    const Clear clear = share(e.tokens > 0 ? kClearRank : INT64_MAX);
+    if (rank_blocks + blocks(clear) > 0)
+      hipLaunchKernelGGL((embedding_rank_kernel<I>), dim3((unsigned)(rank_blocks + blocks(clear))), dim3(kRankThreads),
                          (unsigned)round256(4 * e.tokens), static_cast<hipStream_t>(stream), ids, (int)e.tokens, vocab, key[0], pos[0],
-                         blocks, table, e.vocab, e.dim, stride);
+                         rank_blocks, clear);
   } else {
     for (int pass = 0; pass < p.passes; ++pass) {
       const int shift = pass * p.digit_bits, digits = 1 << p.digit_bits, to = pass & 1;
+      const Clear c = share(kClearCount), d = share(kClearPlace);
+      const dim3 count_grid((unsigned)(p.tiles + blocks(c))), place_grid((unsigned)(p.tiles + blocks(d)));
       if (pass == 0) {
-        LAUNCH((embedding_count_kernel<I, true>), dim3((unsigned)(p.tiles + clear)), dim3(kSortThreads), stream, ids, nullptr, e.tokens,
-               vocab, p.tile, shift, digits, counts, p.tiles, table, e.vocab, e.dim, stride);
-        LAUNCH((embedding_place_kernel<I, true>), dim3((unsigned)p.tiles), dim3(kSortThreads), stream, ids, nullptr, nullptr, e.tokens,
-               vocab, p.tile, shift, p.digit_bits, counts, p.tiles, key[to], pos[to]);
+        LAUNCH((embedding_count_kernel<I, true>), count_grid, dim3(kSortThreads), stream, ids, nullptr, e.tokens, vocab, p.tile, shift,
+               digits, counts, p.tiles, c);
+        LAUNCH((embedding_place_kernel<I, true>), place_grid, dim3(kSortThreads), stream, ids, nullptr, nullptr, e.tokens, vocab, p.tile,
+               shift, p.digit_bits, counts, p.tiles, key[to], pos[to], d);
       } else {
-        LAUNCH((embedding_count_kernel<I, false>), dim3((unsigned)p.tiles), dim3(kSortThreads), stream, ids, key[at], e.tokens, vocab,
-               p.tile, shift, digits, counts, p.tiles, table, e.vocab, e.dim, stride);
-        LAUNCH((embedding_place_kernel<I, false>), dim3((unsigned)p.tiles), dim3(kSortThreads), stream, ids, key[at], pos[at], e.tokens,
-               vocab, p.tile, shift, p.digit_bits, counts, p.tiles, key[to], pos[to]);
+        LAUNCH((embedding_count_kernel<I, false>), count_grid, dim3(kSortThreads), stream, ids, key[at], e.tokens, vocab, p.tile, shift,
+               digits, counts, p.tiles, c);
+        LAUNCH((embedding_place_kernel<I, false>), place_grid, dim3(kSortThreads), stream, ids, key[at], pos[at], e.tokens, vocab, p.tile,
+               shift, p.digit_bits, counts, p.tiles, key[to], pos[to], d);
       }
       at = to;
     }
   }
   if (e.tokens == 0) return;
-  if (e.out_type == ACC_BF16) sum_runs<bf16>(e, p, key[at], pos[at], grad, table, parts, stream);
-  else sum_runs<float>(e, p, key[at], pos[at], grad, table, parts, stream);
+  if (e.out_type == ACC_BF16) sum_runs<bf16>(e, p, key[at], pos[at], grad, table, stride, parts, dirty, stream);
+  else sum_runs<float>(e, p, key[at], pos[at], grad, table, stride, parts, dirty, stream);
   if (p.chunks > 1)
     LAUNCH((embedding_join_kernel<4>), dim3((unsigned)up(p.chunks, 4), (unsigned)up(e.dim, kWave * 4)), dim3(256), stream, key[at], e.tokens,
            p.chunk, p.chunks, vocab, parts, table, stride, e.dim, e.scale, e.accumulate);
