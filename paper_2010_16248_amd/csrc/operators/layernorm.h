@@ -51,14 +51,14 @@ __device__ __forceinline__ float sum_of(const F32<N>& v) {
 // ---- forward ----------------------------------------------------------------------------------------------
 // THREADS lanes hold a row in registers (K requests of N elements each): one read, one write; the deviations are
 // summed from the registers, after the mean.
-template <typename T, int N, int THREADS, int K>
-__global__ __launch_bounds__(256) void layernorm_forward_kernel(const T* __restrict__ x, const float* __restrict__ weight,
+template <typename T, int N, int THREADS, int K, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void layernorm_forward_kernel(const T* __restrict__ x, const float* __restrict__ weight,
                                                                 const float* __restrict__ bias, T* __restrict__ y,
                                                                 float* __restrict__ mean_out, float* __restrict__ rstd_out,
                                                                 int64_t rows, int dim, int64_t x_stride, int64_t y_stride, float eps) {
-  __shared__ float red[8];
-  const int64_t row = (int64_t)blockIdx.x * (256 / THREADS) + threadIdx.x / THREADS;
-  if (row >= rows) return;               // THREADS == 256: the whole workgroup
+  __shared__ float red[2 * BLOCK / kWave];
+  const int64_t row = (int64_t)blockIdx.x * (BLOCK / THREADS) + threadIdx.x / THREADS;
+  if (row >= rows) return;               // THREADS == BLOCK: the whole workgroup
   const int c = (threadIdx.x % THREADS) * N;
   const T* from = x + row * x_stride;
   F32<N> v[K];
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(256) void layernorm_forward_kernel(const T* __restr
     if (at >= dim) continue;
     F32<N> r = v[k] * rstd * widen<float, N>(load_some<N>(weight + at, dim - at));
     if (bias) r += widen<float, N>(load_some<N>(bias + at, dim - at));
-    store_some<T, N>(y + row * y_stride + at, r, dim - at);
+    store_some_stream<T, N>(y + row * y_stride + at, r, dim - at);
   }
 }
 
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(BLOCK) void layernorm_backward_kernel(const T* __re
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int at = c + k * THREADS * N;
-      if (at < dim) store_some<T, N>(dx + row * dx_stride + at, (g[k] - sg - xh[k] * sgx) * rstd, dim - at);
+      if (at < dim) store_some_stream<T, N>(dx + row * dx_stride + at, (g[k] - sg - xh[k] * sgx) * rstd, dim - at);
     }
   }
   float* to = parts + 2 * (int64_t)blockIdx.x * dim;

@@ -255,15 +255,16 @@ void norm_forward(const acc_layernorm& c, const T* x, const float* w, const floa
                   void* stream) {
   constexpr int N = sizeof(T) == 2 ? 8 : 4;
   const int64_t packs = up(c.dim, N);
-#define FORWARD(THREADS, K)                                                                                                       \
-  LAUNCH((layernorm_forward_kernel<T, N, THREADS, K>), dim3((unsigned)up(rows, 256 / THREADS)), dim3(256), stream, x, w, b, y,    \
-         mean, rstd, rows, (int)c.dim, c.x_stride, c.y_stride, c.eps)
-  if (packs <= 64) FORWARD(64, 1);
-  else if (packs <= 128) FORWARD(64, 2);
-  else if (packs <= 256) FORWARD(64, 4);
-  else if (packs <= 512) FORWARD(256, 2);
-  else if (packs <= 1024) FORWARD(256, 4);
-  else if (packs <= 2048) FORWARD(256, 8);
+#define FORWARD(THREADS, K, BLOCK)                                                                                                \
+  LAUNCH((layernorm_forward_kernel<T, N, THREADS, K, BLOCK>), dim3((unsigned)up(rows, BLOCK / THREADS)), dim3(BLOCK), stream, x, w, \
+         b, y, mean, rstd, rows, (int)c.dim, c.x_stride, c.y_stride, c.eps)
+  if (packs <= 64) FORWARD(64, 1, 256);
+  else if (packs <= 128) FORWARD(64, 2, 256);
+  else if (packs <= 256) FORWARD(64, 4, 256);
+  else if (packs <= 512) FORWARD(256, 2, 256);
+  else if (packs <= 1024) FORWARD(256, 4, 256);
+  else if (packs <= 2048) FORWARD(256, 8, 256);
+  else if (packs <= 4096) FORWARD(1024, 4, 1024);
   else
     LAUNCH((layernorm_forward_long_kernel<T, N>), dim3((unsigned)rows), dim3(256), stream, x, w, b, y, mean, rstd, (int)c.dim,
            c.x_stride, c.y_stride, c.eps);
@@ -278,11 +279,13 @@ void norm_forward_rows(const acc_layernorm& c, const void* x, const float* w, co
                     rstd ? rstd + r : nullptr, std::min(kRowsPerLaunch, c.rows - r), stream);
 }
 
-// Parts that the backward pass leaves (two rows of dim each): enough workgroups to fill the chip, no more than rows.
+// Parts that the backward pass leaves (two rows of dim each): enough workgroups to fill the chip, no more than rows.  Two per
+// compute unit where a wave has a row, one where a workgroup has (4096 x 8192 bf16 with two: 58 us, with one 52; 5003 x 1001 fp32
+// 18.4 and 18.7).
 int64_t norm_parts(const acc_layernorm& c) {
   const int64_t packs = up(c.dim, c.type == ACC_BF16 ? 8 : 4);
   const int64_t rows_at_once = packs <= 256 ? 4 : 1;
-  return std::max<int64_t>(1, std::min<int64_t>(up(c.rows, rows_at_once), 2 * kComputeUnits));
+  return std::max<int64_t>(1, std::min<int64_t>(up(c.rows, rows_at_once), (packs <= 256 ? 2 : 1) * kComputeUnits));
 }
 
 template <typename T>
@@ -301,6 +304,7 @@ void norm_backward(const acc_layernorm& c, const void* dy, const void* x, const 
   else if (packs <= 512) BACKWARD(256, 2, 256);
   else if (packs <= 1024) BACKWARD(512, 2, 512);
   else if (packs <= 2048) BACKWARD(1024, 2, 1024);
+  else if (N == 4 && packs <= 4096) BACKWARD(1024, N == 4 ? 4 : 2, 1024);
   else {
     for (int64_t r = 0; r < c.rows; r += kRowsPerLaunch)
       LAUNCH((layernorm_backward_long_kernel<T, N>), dim3((unsigned)std::min(kRowsPerLaunch, c.rows - r)), dim3(256), stream,
