@@ -330,12 +330,10 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const uint32_t* __re
       Pack<T, N> v[kSumAhead];
 #pragma unroll
       for (int j = 0; j < kSumAhead; ++j) {
-        const int at = j0 + j;
-        if (at < here) {
-          const uint32_t key = (uint32_t)__builtin_amdgcn_readlane((int)keys, at);
-          const T* from = grad + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)places, at) * grad_stride + c;
-          if (key < vocab && mine) v[j] = STREAM ? load_stream<N>(from) : EVEN ? load<N>(from) : load_some<N>(from, left);
-        }
+        // places behind the last one load it again, lanes without columns the first ones: no branch between the requests
+        const int at = min(j0 + j, here - 1);
+        const T* from = grad + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)places, at) * grad_stride + (EVEN && !mine ? 0 : c);
+        v[j] = STREAM ? load_stream<N>(from) : EVEN ? load<N>(from) : load_some<N>(from, left);
       }
 #pragma unroll
       for (int j = 0; j < kSumAhead; ++j) {
