@@ -365,7 +365,8 @@ const char* accordion_operator_error(void);
  * grad_table is dense fp32, as the compressors take it: rows without a token become zeros, or, with
  * accumulate, stay as they are and the sums are added (a table shared with the decoder). */
 typedef struct acc_embedding {
-  int64_t vocab, dim, tokens;    /* vocab in [1, 2^31 - 2], dim in [1, 2^24], tokens in [0, 2^28] */
+  int64_t vocab, dim, tokens;    /* vocab in [1, 2^31 - 2], dim in [1, 2^23], tokens in [0, 2^28]; backward:
+                                  * tokens x dim up to about 2^36 */
   int64_t table_stride;          /* rows of table / grad_table */
   int64_t out_stride;            /* rows of out / grad_out */
   int32_t index_bits;            /* 32 or 64: int32 or int64 ids */

@@ -306,12 +306,13 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const uint32_t* __re
                                                             int64_t n, int chunk, uint32_t vocab, const T* __restrict__ grad,
                                                             int64_t grad_stride, float* __restrict__ table, int64_t table_stride,
                                                             int64_t dim, uint32_t across, uint32_t units, float scale,
-                                                            float* __restrict__ parts, int64_t gap_rows) {
+                                                            float* __restrict__ parts, int64_t gap_rows, uint32_t gap_units) {
   // neighbouring waves take neighbouring columns of one chunk; those beyond the chunks' clear rows [0, gap_rows)
   const uint32_t unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (unit >= units) {
-    const int64_t row = (int64_t)(unit - units) * kGapRows;
-    if (row < gap_rows) clear_gaps(Clear{table, 0, gap_rows, dim, table_stride}, row, gap_rows, skey, n);
+    if (unit - units < gap_units)
+      for (int64_t row = (int64_t)(unit - units) * kGapRows; row < gap_rows; row += (int64_t)gap_units * kGapRows)
+        clear_gaps(Clear{table, 0, gap_rows, dim, table_stride}, row, gap_rows, skey, n);
     return;
   }
   const int64_t b = unit / across, lo = b * chunk, hi = min(n, lo + chunk);

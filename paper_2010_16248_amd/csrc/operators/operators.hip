@@ -34,7 +34,7 @@ int32_t fail(int32_t code, const char* msg) {
 constexpr int kComputeUnits = 256;
 constexpr int64_t kMaxStride = int64_t(1) << 40;
 // A launch has fewer than 2^32 work items per axis: rows beyond this many go into further launches.
-constexpr int64_t kRowsPerLaunch = int64_t(1) << 22;
+constexpr int64_t kRowsPerLaunch = int64_t(1) << 21;
 
 inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t round256(int64_t bytes) { return up(bytes, 256) * 256; }
@@ -87,7 +87,7 @@ constexpr int64_t kRankTokens = 14336;  // up to here the order is counted, from
 int32_t check_embedding(const acc_embedding* e) {
   REQUIRE(e, "config is NULL");
   REQUIRE(e->vocab >= 1 && e->vocab <= (int64_t(1) << 31) - 2, "vocab out of range");
-  REQUIRE(e->dim >= 1 && e->dim <= (int64_t(1) << 24), "dim out of range");
+  REQUIRE(e->dim >= 1 && e->dim <= (int64_t(1) << 23), "dim out of range");
   REQUIRE(e->tokens >= 0 && e->tokens <= (int64_t(1) << 28), "tokens out of range");
   REQUIRE(e->index_bits == 32 || e->index_bits == 64, "index_bits must be 32 or 64");
   REQUIRE(is_type(e->table_type) && is_type(e->out_type), "unknown type");
@@ -97,6 +97,9 @@ int32_t check_embedding(const acc_embedding* e) {
   REQUIRE(e->tokens <= 1 || (e->out_stride >= e->dim && e->out_stride <= kMaxStride), "out_stride out of range");
   return ACC_OK;
 }
+
+// Waves that sum: fewer than a launch has (see kRowsPerLaunch).
+constexpr int64_t kMostUnits = int64_t(1) << 25;
 
 struct EmbeddingPlan {
   bool rank;
@@ -162,12 +165,13 @@ void sum_runs(const acc_embedding& e, const EmbeddingPlan& p, const uint32_t* ke
               float* table, int64_t stride, float* parts, int64_t gap_rows, void* stream) {
   constexpr int N = 4;
   const int64_t across = up(e.dim, kWave * N), units = p.chunks * across;
-  const dim3 grid((unsigned)up(units + up(gap_rows, kGapRows), 4));
+  const int64_t gap_units = std::min<int64_t>(up(gap_rows, kGapRows), int64_t(1) << 20);
+  const dim3 grid((unsigned)up(units + gap_units, 4));
   const bool stream_rows = e.tokens * e.dim * (int64_t)sizeof(T) > kSumStream;
 #define SUM(ACCUMULATE, EVEN, STREAM)                                                                                              \
   LAUNCH((embedding_sum_kernel<T, N, ACCUMULATE, EVEN, STREAM>), grid, dim3(256), stream, key, pos, e.tokens, p.chunk,             \
          (uint32_t)e.vocab, static_cast<const T*>(grad), e.out_stride, table, stride, e.dim, (uint32_t)across, (uint32_t)units,    \
-         e.scale, parts, gap_rows)
+         e.scale, parts, gap_rows, (uint32_t)gap_units)
   if (e.dim % N != 0) {
     if (e.accumulate) SUM(true, false, false);
     else SUM(false, false, false);
@@ -373,7 +377,7 @@ RecurrenceShape shape_of(const acc_recurrence& c) {
 
 // Up to kWalkSteps steps a lane walks them.  More: chunks, whose number of waves follows the steps.
 constexpr int64_t kWalkSteps = 16;
-constexpr int64_t kMostChunks = int64_t(1) << 22;   // see kRowsPerLaunch
+constexpr int64_t kMostChunks = int64_t(1) << 22;   // work items per launch: see kRowsPerLaunch
 
 struct RecurrencePlan {
   bool walk;
@@ -485,7 +489,6 @@ int32_t accordion_embedding_forward(const acc_embedding* e, const void* ids_dev,
                      rows_span(table_dev, e->vocab, e->dim, e->table_stride, type_bytes(e->table_type)),
                      {static_cast<const char*>(ids_dev), e->tokens * (e->index_bits / 8)}};
   REQUIRE(!any_overlap(s, 1, 3), "out_dev overlaps another buffer");
-  REQUIRE(up(e->dim, 4 * kLookupLoads * 256) <= 65535, "dim out of range");
   if (e->index_bits == 32)
     e->table_type == ACC_BF16 ? lookup_to<int32_t, bf16>(*e, ids_dev, table_dev, out_dev, hip_stream)
                               : lookup_to<int32_t, float>(*e, ids_dev, table_dev, out_dev, hip_stream);
@@ -498,7 +501,9 @@ int32_t accordion_embedding_forward(const acc_embedding* e, const void* ids_dev,
 int32_t accordion_embedding_workspace_bytes(const acc_embedding* e, size_t* out_bytes) {
   REQUIRE(out_bytes, "out_bytes is NULL");
   if (const int32_t rc = check_embedding(e)) return rc;
-  *out_bytes = (size_t)plan_embedding(*e).bytes;
+  const EmbeddingPlan p = plan_embedding(*e);
+  REQUIRE(p.chunks * up(e->dim, kWave * 4) <= kMostUnits, "tokens x dim out of range");
+  *out_bytes = (size_t)p.bytes;
   return ACC_OK;
 }
 
@@ -513,6 +518,7 @@ int32_t accordion_embedding_backward(const acc_embedding* e, const void* ids_dev
             "a pointer is not aligned to its element type");
   }
   const EmbeddingPlan p = plan_embedding(*e);
+  REQUIRE(p.chunks * up(e->dim, kWave * 4) <= kMostUnits, "tokens x dim out of range");
   if (const int32_t rc = check_workspace(workspace_dev, workspace_bytes, p.bytes)) return rc;
   const Span s[4] = {rows_span(grad_table_dev, e->vocab, e->dim, e->table_stride, 4),
                      {static_cast<const char*>(workspace_dev), p.bytes},

@@ -10,14 +10,15 @@ struct RecurrenceShape {
   int64_t dgate_b, dgate_t, dinput_b, dinput_t, dout_b, dout_t;
 };
 
-// e^-x for x >= 0 (NaN for NaN): 2^t of the rounded product t = -x log2(e), corrected by what the rounding lost.
-// From 104 on the result is below the smallest fp32 number.
+// e^-x for x >= 0 (NaN for NaN): 2^t of the rounded t = -x log2(e), times e^d with d = -x - t ln 2, what the rounding lost
+// (d is below 2^-16, so e^d = 1 + d; ln 2 rounded to fp32 is off by 1.9e-9, times t): within 4 units of 2^-24 up to x = 20, 7 beyond.  From 104 on the result is below the
+// smallest fp32 number.
 __device__ __forceinline__ float exp_neg(float x) {
   x = x > 104.f ? 104.f : x;
   const float t = -1.44269502f * x;
-  const float lost = fmaf(-1.44269502f, x, -t) + -1.92596303e-8f * x;
+  const float d = fmaf(t, -0.693147182f, -x);
   const float e = __builtin_amdgcn_exp2f(t);
-  return fmaf(e, lost * 0.693147182f, e);
+  return fmaf(e, d, e);
 }
 
 // sigmoid(f) and sigmoid(-f).  Neither is a difference from one: a gate near one keeps all digits of 1 - a.
@@ -386,7 +387,7 @@ __device__ __forceinline__ void forward_chunk(const RecurrenceShape& s, const Ch
     if (j < in) {
 #pragma unroll
       for (int i = 0; i < N; ++i) h[i] = fmaf(a[j][i], h[i], b[j][i]);
-      store<T, N>(o, h);
+      store_stream<T, N>(o, h);
     } else if (j < here) {
       store<T, N>(o, F32<N>{});
     }
@@ -477,8 +478,8 @@ __device__ __forceinline__ void backward_chunk(const RecurrenceShape& s, const C
         dg = (h - xx) * a[j] * dx;
         state = a[j] * total;
       }
-      store<T, N>(og, dg);
-      store<T, N>(ox, dx);
+      store_stream<T, N>(og, dg);
+      store_stream<T, N>(ox, dx);
     }
     og -= s.dgate_t;
     ox -= s.dinput_t;

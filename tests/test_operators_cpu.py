@@ -269,3 +269,14 @@ def test_the_binding_refuses_what_the_c_abi_cannot_see():
         B.adamw_step([cpu(6)], [cpu(6)], state, 0.1, 1, grad_scale=cpu(2))
     with pytest.raises(ValueError, match="one GPU"):
         B.adamw_step([cpu(6)], [cpu(6)], state, 0.1, 1)
+
+
+def test_sizes_beyond_a_launch_are_refused(lib):
+    n = C.c_size_t(0)
+    cfg = embedding(tokens=2 ** 28, dim=2 ** 20, out_stride=2 ** 20, table_stride=2 ** 20)
+    refused(lib, lib.accordion_embedding_workspace_bytes(C.byref(cfg), C.byref(n)), "tokens x dim")
+    refused(lib, lib.accordion_embedding_backward(C.byref(cfg), at(0), at(1 << 10), at(2 << 10), at(3 << 10), 1 << 40, None), "tokens x dim")
+    cfg = recurrence(batch=65535, steps=2 ** 20, channels=64, out_batch=2 ** 26, out_step=64, gate_batch=2 ** 26, gate_step=64,
+                     input_batch=2 ** 26, input_step=64)
+    refused(lib, lib.accordion_recurrence_workspace_bytes(C.byref(cfg), C.byref(n)), "too many steps")
+    refused(lib, lib.accordion_recurrence_forward(C.byref(cfg), *[at(i << 12) for i in range(7)], 1 << 40, None), "too many steps")
