@@ -103,7 +103,9 @@ def load_library() -> C.CDLL:
     # The caller's device memory and streams come from PyTorch, which ships its own HIP runtime:
     # that runtime has to be the one already in the process when the library is loaded, or the
     # library binds to a second copy that sees no device.
-    import torch  # noqa: F401
+    import torch
+    _TYPES.update({torch.float32: ACC_FLOAT, torch.bfloat16: ACC_BF16})
+    _INDEX_BITS.update({torch.int32: 32, torch.int64: 64})
     lib = C.CDLL(LIB_PATH)
     vp, i32, i64, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
     sig = {
@@ -248,14 +250,10 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-_TYPES = None      # torch's types, once it is loaded
+_TYPES, _INDEX_BITS = {}, {}      # by torch's types, filled once torch is loaded
 
 
 def _type_of(t, name: str) -> int:
-    global _TYPES
-    if _TYPES is None:
-        import torch
-        _TYPES = {torch.float32: ACC_FLOAT, torch.bfloat16: ACC_BF16}
     kind = _TYPES.get(t.dtype)
     if kind is None:
         raise ValueError(f"{name} must be float32 or bfloat16, not {t.dtype}")
@@ -264,11 +262,15 @@ def _type_of(t, name: str) -> int:
 
 def _rows_of(t, name: str) -> Tuple[int, int, int]:
     """(rows, elements per row, elements between rows) of a tensor whose last dimension is a row."""
-    shape = t.shape
-    if len(shape) == 2 and (t.is_contiguous() or t.stride(1) == 1 or shape[1] <= 1):
-        return shape[0], shape[1], t.stride(0)
-    _need(len(shape) >= 1 and t.is_contiguous(), f"{name}: rows must be contiguous, and lie in one or two dimensions")
-    return (t.numel() // shape[-1] if shape[-1] else 0), shape[-1], shape[-1]
+    if t.dim() == 2:
+        rows, dim = t.shape
+        stride, inner = t.stride()
+        if inner == 1 or dim <= 1:
+            return rows, dim, stride
+    elif t.dim() >= 1 and t.is_contiguous():
+        dim = t.shape[-1]
+        return (t.numel() // dim if dim else 0), dim, dim
+    raise ValueError(f"{name}: rows must be contiguous, and lie in one or two dimensions")
 
 
 def _plain(t, name: str, shape: Tuple[int, ...], dtype) -> Optional[int]:
@@ -285,7 +287,7 @@ def _gpu_of(*tensors) -> int:
     index = tensors[0].get_device()
     for t in tensors:
         if t is not None and t.get_device() != index:
-            index = -1
+            raise ValueError("all tensors must be on one GPU")
     if index < 0:
         raise ValueError("all tensors must be on one GPU")
     return index
@@ -297,6 +299,7 @@ def _launch(gpu: int, fn, *args) -> None:
     if torch.cuda.current_device() != gpu:
         with torch.cuda.device(gpu):
             return _launch(gpu, fn, *args)
+    # (the stream's handle alone: torch.cuda.current_stream makes an object around it, 2.7 us of a call's 7)
     rc = fn(*args, torch._C._cuda_getCurrentRawStream(gpu))
     if rc != ACC_OK:
         raise AccordionError(rc, _lib.accordion_operator_error().decode())
@@ -319,12 +322,13 @@ def _workspace(gpu: int, fn, cfg, given):
 
 
 def _embedding(ids, table, out, scale: float, accumulate: bool) -> acc_embedding:
-    import torch
-    bits = 64 if ids.dtype == torch.int64 else 32 if ids.dtype == torch.int32 else 0
-    _need(bits and ids.is_contiguous(), "ids must be contiguous int32 or int64")
+    bits = _INDEX_BITS.get(ids.dtype)
+    if bits is None or not ids.is_contiguous():
+        raise ValueError("ids must be contiguous int32 or int64")
     vocab, dim, table_stride = _rows_of(table, "table")
     tokens, width, out_stride = _rows_of(out, "out")
-    _need(table.dim() == 2 and width == dim and tokens == ids.numel(), "ids, table and out do not fit together")
+    if width != dim or tokens != ids.numel() or table.dim() != 2:
+        raise ValueError("ids, table and out do not fit together")
     return acc_embedding(vocab, dim, tokens, table_stride, out_stride, bits, _type_of(table, "table"), _type_of(out, "out"),
                          accumulate, scale)
 

@@ -105,7 +105,7 @@ __device__ __forceinline__ void clear_gaps(const Clear& s, int64_t row, int64_t 
 // Few tokens: a token's place is the number of tokens that come before it, counted against all others.  A workgroup
 // holds all keys in LDS and places 64 tokens (one per lane); its waves share the tokens to compare with, four per
 // read: two operations per pair of tokens.
-constexpr int kRankThreads = 1024;
+constexpr int kRankThreads = 1024, kRankAhead = 4;   // ids under way per thread
 template <typename I>
 __global__ __launch_bounds__(kRankThreads) void embedding_rank_kernel(const I* __restrict__ ids, int n, uint32_t vocab,
                                                                      uint32_t* __restrict__ skey, uint32_t* __restrict__ spos,
@@ -119,7 +119,16 @@ __global__ __launch_bounds__(kRankThreads) void embedding_rank_kernel(const I* _
   constexpr int waves = kRankThreads / kWave;
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int groups = (n + 3) >> 2;
-  for (int j = threadIdx.x; j < 4 * groups; j += kRankThreads) keys[j] = j < n ? key_of_id(ids[j], vocab) : 0xffffffffu;
+  for (int j0 = threadIdx.x; j0 < 4 * groups; j0 += kRankAhead * kRankThreads) {
+    I v[kRankAhead];
+#pragma unroll
+    for (int k = 0; k < kRankAhead; ++k) v[k] = ids[min(j0 + k * kRankThreads, n - 1)];
+#pragma unroll
+    for (int k = 0; k < kRankAhead; ++k) {
+      const int j = j0 + k * kRankThreads;
+      if (j < 4 * groups) keys[j] = j < n ? key_of_id(v[k], vocab) : 0xffffffffu;
+    }
+  }
   __syncthreads();
   const int first = blockIdx.x * kWave, i = first + l;
   const uint32_t mine = keys[min(i, n - 1)];
