@@ -79,8 +79,21 @@ __device__ __forceinline__ void clear_rows(const Clear& s, int64_t block, int64_
   }
 }
 
-// A wave clears those of kGapRows rows from `row` on (below `rows`) that no token asks for.
+// A wave clears those of kGapRows rows from `row` on whose bits are set.
 constexpr int kGapRows = 4;
+__device__ __forceinline__ void clear_gap_rows(const Clear& s, int64_t row, uint64_t gaps) {
+  const int l = threadIdx.x & 63;
+  if (gaps == (1ull << kGapRows) - 1 && s.stride == s.dim) {     // one piece
+    clear_span(s.table + row * s.stride, kGapRows * s.dim, l, kWave);
+    return;
+  }
+  while (gaps) {
+    clear_span(s.table + (row + __builtin_ctzll(gaps)) * s.stride, s.dim, l, kWave);
+    gaps &= gaps - 1;
+  }
+}
+
+// A wave clears those of kGapRows rows from `row` on (below `rows`) that no token asks for.
 __device__ __forceinline__ void clear_gaps(const Clear& s, int64_t row, int64_t rows, const uint32_t* __restrict__ skey, int64_t n) {
   const int l = threadIdx.x & 63;
   // lane l < kGapRows looks for its row in the order: the first place whose key is not below it
@@ -92,14 +105,78 @@ __device__ __forceinline__ void clear_gaps(const Clear& s, int64_t row, int64_t 
   }
   const bool empty = l < kGapRows && row + l < rows && (lo == n || skey[lo] != mine);
   uint64_t gaps = __ballot(empty);
-  if (gaps == (1ull << kGapRows) - 1 && s.stride == s.dim) {     // one piece
-    clear_span(s.table + row * s.stride, kGapRows * s.dim, l, kWave);
+  clear_gap_rows(s, row, gaps);
+}
+
+template <int N>
+__device__ __forceinline__ void to_row(float* to, const F32<N>& sum, const F32<N>& old, float scale, bool accumulate, int64_t left) {
+  F32<N> v = sum * scale;
+  if (accumulate) v = old + v;
+  store_some<float, N>(to, v, left);
+}
+
+// A handful of tokens: one launch, nothing is ordered.  The wave of the first token of an id (and 64 N columns) finds the
+// others by comparing all ids, 64 at a time, and adds their rows; other waves clear the rows of which no id is found.
+// us per call at 32768 x 672 fp32, in one launch and in the three of the other way: 20 tokens 16.1 and 19.2, 512 tokens 17.6 and 22.3, added to
+// what is there 7.8 and 15.2; 700 tokens 18.6 and 22.5.  500 tokens of two ids, which two waves add: 21.9 and 13.7, 1000 of them 43 and 18,
+// hence the limit (kFewTokens).  Sixteen rows under way: 512 tokens 19.1.
+constexpr int kFewAhead = 8;
+template <typename I, typename T, int N, bool ACCUMULATE, bool EVEN>
+__global__ __launch_bounds__(256) void embedding_few_kernel(const I* __restrict__ ids, int n, int64_t vocab, const T* __restrict__ grad,
+                                                            int64_t grad_stride, float* __restrict__ table, int64_t table_stride,
+                                                            int64_t dim, uint32_t across, uint32_t units, float scale, uint32_t gap_units) {
+  const int l = threadIdx.x & 63;
+  const uint32_t unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (unit >= units) {
+    if (ACCUMULATE || unit - units >= gap_units) return;
+    for (int64_t row = (int64_t)(unit - units) * kGapRows; row < vocab; row += (int64_t)gap_units * kGapRows) {
+      uint32_t found = 0;
+      for (int j = l; j < n; j += kWave) {
+        const int64_t at = (int64_t)ids[j] - row;
+        if (at >= 0 && at < kGapRows) found |= 1u << at;
+      }
+      uint32_t gaps = 0;
+#pragma unroll
+      for (int r = 0; r < kGapRows; ++r) gaps |= (row + r < vocab && __ballot(found >> r & 1) == 0) ? 1u << r : 0u;
+      clear_gap_rows(Clear{table, 0, vocab, dim, table_stride}, row, gaps);
+    }
     return;
   }
-  while (gaps) {
-    clear_span(s.table + (row + __builtin_ctzll(gaps)) * s.stride, s.dim, l, kWave);
-    gaps &= gaps - 1;
+  const int i = (int)(unit / across);
+  const int64_t id = (int64_t)ids[i];
+  if (id < 0 || id >= vocab) return;
+  for (int j = l; j - l < i; j += kWave)
+    if (__ballot(j < i && (int64_t)ids[j] == id) != 0) return;
+  const int64_t c = ((int64_t)(unit % across) * kWave + l) * N, left = EVEN ? min(dim - c, (int64_t)N) : dim - c;
+  const bool mine = left > 0;
+  const T* from = grad + (EVEN && !mine ? 0 : c);
+  F32<N> acc = {};
+  for (int j0 = i; j0 < n; j0 += kWave) {
+    uint64_t same = __ballot(j0 + l < n && (int64_t)ids[min(j0 + l, n - 1)] == id);
+    while (same) {
+      // up to kFewAhead rows under way; behind the last one it is requested again
+      const int here = min(kFewAhead, (int)__popcll(same));
+      Pack<T, N> v[kFewAhead];
+      int at = 0;
+#pragma unroll
+      for (int k = 0; k < kFewAhead; ++k) {
+        if (same) {
+          at = __builtin_ctzll(same);
+          same &= same - 1;
+        }
+        const T* p = from + (int64_t)(j0 + at) * grad_stride;
+        v[k] = EVEN ? load<N>(p) : load_some<N>(p, left);
+      }
+#pragma unroll
+      for (int k = 0; k < kFewAhead; ++k)
+        if (k < here) acc += widen<T, N>(v[k]);
+    }
   }
+  if (!mine) return;
+  float* to = table + id * table_stride + c;
+  F32<N> old = {};
+  if (ACCUMULATE) old = widen<float, N>(EVEN ? load<N>(to) : load_some<N>(to, left));
+  to_row<N>(to, acc, old, scale, ACCUMULATE, EVEN ? N : left);
 }
 
 // Few tokens: a token's place is the number of tokens that come before it, counted against all others.  A workgroup
@@ -300,13 +377,6 @@ __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(const I* 
 // parts[2 c] for a run that began in an earlier chunk, parts[2 c + 1] for one that begins here and goes on.
 constexpr int kSumAhead = 8;     // rows under way
 constexpr int kJoinRows = 16;    // parts under way
-
-template <int N>
-__device__ __forceinline__ void to_row(float* to, const F32<N>& sum, const F32<N>& old, float scale, bool accumulate, int64_t left) {
-  F32<N> v = sum * scale;
-  if (accumulate) v = old + v;
-  store_some<float, N>(to, v, left);
-}
 
 // EVEN: N divides the columns.  STREAM: gradients and rows go past the caches (131072 tokens x 2048 bf16 into 65537 rows: 271 ->
 // 247 us, added to what is there 276 -> 253; 2800 tokens x 672 fp32: 25.7 -> 26.5).

@@ -82,6 +82,7 @@ int32_t launched() {
 
 // ---- embedding --------------------------------------------------------------------------------------
 
+constexpr int64_t kFewTokens = 512;     // up to here nothing is ordered (embedding_few_kernel)
 constexpr int64_t kRankTokens = 14336;  // up to here the order is counted, from here on it is sorted by digits
 
 int32_t check_embedding(const acc_embedding* e) {
@@ -102,15 +103,20 @@ int32_t check_embedding(const acc_embedding* e) {
 constexpr int64_t kMostUnits = int64_t(1) << 25;
 
 struct EmbeddingPlan {
-  bool rank;
+  bool few, rank;
   int passes = 0, digit_bits = 0, tiles = 0, chunk = 0;
   int64_t tile = 0, chunks = 0;
   int64_t key[2], pos[2], counts, parts, bytes;   // offsets in the workspace
 };
 
 EmbeddingPlan plan_embedding(const acc_embedding& e) {
-  EmbeddingPlan p;
+  EmbeddingPlan p{};
   const int64_t n = e.tokens;
+  p.few = n <= kFewTokens;
+  if (p.few) {
+    p.chunks = n;                      // a token takes the place of a chunk
+    return p;
+  }
   p.rank = n <= kRankTokens;
   if (!p.rank) {
     int bits = 1;
@@ -132,7 +138,7 @@ EmbeddingPlan plan_embedding(const acc_embedding& e) {
   p.key[1] = p.rank ? 0 : take(4 * n);
   p.pos[1] = p.rank ? 0 : take(4 * n);
   p.counts = p.rank ? 0 : take(4 * (int64_t)p.tiles << p.digit_bits);
-  p.parts = take(n > 0 ? 8 * p.chunks * e.dim : 0);
+  p.parts = take(8 * p.chunks * e.dim);
   p.bytes = at;
   return p;
 }
@@ -185,6 +191,26 @@ void sum_runs(const acc_embedding& e, const EmbeddingPlan& p, const uint32_t* ke
 #undef SUM
 }
 
+template <typename I, typename T>
+void sum_few(const acc_embedding& e, const I* ids, const void* grad, float* table, int64_t stride, void* stream) {
+  constexpr int N = 4;
+  const int64_t across = up(e.dim, kWave * N), units = e.tokens * across;
+  const int64_t gap_units = e.accumulate ? 0 : std::min<int64_t>(up(e.vocab, kGapRows), int64_t(1) << 20);
+  if (units + gap_units == 0) return;
+#define FEW(ACCUMULATE, EVEN)                                                                                                     \
+  LAUNCH((embedding_few_kernel<I, T, N, ACCUMULATE, EVEN>), dim3((unsigned)up(units + gap_units, 4)), dim3(256), stream, ids,     \
+         (int)e.tokens, e.vocab, static_cast<const T*>(grad), e.out_stride, table, stride, e.dim, (uint32_t)across,               \
+         (uint32_t)units, e.scale, (uint32_t)gap_units)
+  if (e.dim % N == 0) {
+    if (e.accumulate) FEW(true, true);
+    else FEW(false, true);
+  } else {
+    if (e.accumulate) FEW(true, false);
+    else FEW(false, false);
+  }
+#undef FEW
+}
+
 template <typename I>
 void embedding_gradient(const acc_embedding& e, const EmbeddingPlan& p, const I* ids, const void* grad, float* table, char* ws,
                         void* stream) {
@@ -194,6 +220,11 @@ void embedding_gradient(const acc_embedding& e, const EmbeddingPlan& p, const I*
   float* parts = reinterpret_cast<float*>(ws + p.parts);
   const uint32_t vocab = (uint32_t)e.vocab;
   const int64_t stride = e.vocab == 1 ? e.dim : e.table_stride;
+  if (p.few) {
+    if (e.out_type == ACC_BF16) sum_few<I, bf16>(e, ids, grad, table, stride, stream);
+    else sum_few<I, float>(e, ids, grad, table, stride, stream);
+    return;
+  }
   // rows [0, dirty) are still to be cleared; share() takes the last ones of them off, as many as `bytes` hold
   int64_t dirty = e.accumulate ? 0 : e.vocab;
   auto share = [&](int64_t bytes) {
@@ -205,7 +236,7 @@ void embedding_gradient(const acc_embedding& e, const EmbeddingPlan& p, const I*
   int at = 0;
   if (p.rank) {
     const int rank_blocks = (int)up(e.tokens, kWave);
-    const Clear clear = share(e.tokens > 0 ? kClearRank : INT64_MAX);
+    const Clear clear = share(kClearRank);
     if (rank_blocks + blocks(clear) > 0)
       hipLaunchKernelGGL((embedding_rank_kernel<I>), dim3((unsigned)(rank_blocks + blocks(clear))), dim3(kRankThreads),
                          (unsigned)round256(4 * e.tokens), static_cast<hipStream_t>(stream), ids, (int)e.tokens, vocab, key[0], pos[0],
@@ -229,12 +260,10 @@ void embedding_gradient(const acc_embedding& e, const EmbeddingPlan& p, const I*
       at = to;
     }
   }
-  if (e.tokens == 0) return;
   if (e.out_type == ACC_BF16) sum_runs<bf16>(e, p, key[at], pos[at], grad, table, stride, parts, dirty, stream);
   else sum_runs<float>(e, p, key[at], pos[at], grad, table, stride, parts, dirty, stream);
-  if (p.chunks > 1)
-    LAUNCH((embedding_join_kernel<4>), dim3((unsigned)up(p.chunks, 4), (unsigned)up(e.dim, kWave * 4)), dim3(256), stream, key[at], e.tokens,
-           p.chunk, p.chunks, vocab, parts, table, stride, e.dim, e.scale, e.accumulate);
+  LAUNCH((embedding_join_kernel<4>), dim3((unsigned)up(p.chunks, 4), (unsigned)up(e.dim, kWave * 4)), dim3(256), stream, key[at], e.tokens,
+         p.chunk, p.chunks, vocab, parts, table, stride, e.dim, e.scale, e.accumulate);
 }
 
 // ---- layer norm -------------------------------------------------------------------------------------

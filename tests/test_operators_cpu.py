@@ -59,6 +59,7 @@ def test_embedding_pointers(lib):
         refused(lib, fwd(C.byref(cfg), *ptrs, None), "aligned")
         refused(lib, bwd(C.byref(cfg), *ptrs, at(3), 1 << 40, None), "aligned")
     refused(lib, fwd(C.byref(cfg), at(0), at(1), C.c_void_p(at(1).value + 32), None), "overlaps")
+    cfg = embedding(tokens=600)          # enough for a workspace
     assert lib.accordion_embedding_workspace_bytes(C.byref(cfg), C.byref(n)) == B.ACC_OK and n.value > 0
     refused(lib, bwd(C.byref(cfg), at(0), at(1), at(2), None, n.value, None), "workspace")
     refused(lib, bwd(C.byref(cfg), at(0), at(1), at(2), C.c_void_p(at(3).value + 128), n.value, None), "aligned")
