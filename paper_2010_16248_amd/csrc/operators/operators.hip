@@ -83,7 +83,7 @@ int32_t launched() {
 // ---- embedding --------------------------------------------------------------------------------------
 
 constexpr int64_t kFewTokens = 512;     // up to here nothing is ordered (embedding_few_kernel)
-constexpr int64_t kRankTokens = 14336;  // up to here the order is counted, from here on it is sorted by digits
+constexpr int64_t kRankTokens = 8192;   // up to here the order is counted, from here on it is sorted by digits
 
 int32_t check_embedding(const acc_embedding* e) {
   REQUIRE(e, "config is NULL");
