@@ -4,10 +4,11 @@
 
 namespace accop {
 
-// Sum over the THREADS lanes that share a row (one wave, or a whole workgroup: then every thread calls this),
+// Sum over the THREADS lanes that share a row (16 lanes, one wave, or a whole workgroup: then every thread calls this),
 // the same value in all of them.
 template <int THREADS>
 __device__ __forceinline__ float row_sum(float v, float* red) {
+  if (THREADS == 16) return row16_sum(v);
   v = wave_sum(v);
   if (THREADS == kWave) return v;
   constexpr int waves = THREADS / kWave;
@@ -21,6 +22,11 @@ __device__ __forceinline__ float row_sum(float v, float* red) {
 }
 template <int THREADS>
 __device__ __forceinline__ void row_sum2(float& a, float& b, float* red) {
+  if (THREADS == 16) {
+    a = row16_sum(a);
+    b = row16_sum(b);
+    return;
+  }
   a = wave_sum(a);
   b = wave_sum(b);
   if (THREADS == kWave) return;

@@ -73,13 +73,18 @@ __device__ __forceinline__ float dpp(float v) {
 __device__ __forceinline__ float lane(float v, int l) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l));
 }
-// Sum over the 64 lanes, the same value in every lane (lane exchanges inside rows of 16, then the four rows).
-// All lanes must be active.
-__device__ __forceinline__ float wave_sum(float v) {
+// Sum over each row of 16 lanes, the same value in all of them.
+__device__ __forceinline__ float row16_sum(float v) {
   v += dpp<0xB1>(v);
   v += dpp<0x4E>(v);
   v += dpp<0x141>(v);
   v += dpp<0x140>(v);
+  return v;
+}
+// Sum over the 64 lanes, the same value in every lane (lane exchanges inside rows of 16, then the four rows).
+// All lanes must be active.
+__device__ __forceinline__ float wave_sum(float v) {
+  v = row16_sum(v);
   return (lane(v, 0) + lane(v, 16)) + (lane(v, 32) + lane(v, 48));
 }
 

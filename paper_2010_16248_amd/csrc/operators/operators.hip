@@ -291,7 +291,9 @@ void norm_forward(const acc_layernorm& c, const T* x, const float* w, const floa
 #define FORWARD(THREADS, K, BLOCK)                                                                                                \
   LAUNCH((layernorm_forward_kernel<T, N, THREADS, K, BLOCK>), dim3((unsigned)up(rows, BLOCK / THREADS)), dim3(BLOCK), stream, x, w, \
          b, y, mean, rstd, rows, (int)c.dim, c.x_stride, c.y_stride, c.eps)
-  if (packs <= 64) FORWARD(64, 1, 256);
+  if (packs <= 16) FORWARD(16, 1, 256);
+  else if (packs <= 32) FORWARD(16, 2, 256);
+  else if (packs <= 64) FORWARD(64, 1, 256);
   else if (packs <= 128) FORWARD(64, 2, 256);
   else if (packs <= 256) FORWARD(64, 4, 256);
   else if (packs <= 512) FORWARD(256, 2, 256);
@@ -317,8 +319,11 @@ void norm_forward_rows(const acc_layernorm& c, const void* x, const float* w, co
 // 18.4 and 18.7).
 int64_t norm_parts(const acc_layernorm& c) {
   const int64_t packs = up(c.dim, c.type == ACC_BF16 ? 8 : 4);
-  const int64_t rows_at_once = packs <= 256 ? 4 : 1;
-  return std::max<int64_t>(1, std::min<int64_t>(up(c.rows, rows_at_once), (packs <= 256 ? 2 : 1) * kComputeUnits));
+  const int64_t at_once = packs <= 32 ? 16 : packs <= 256 ? 4 : 1;      // rows a workgroup has under way
+  const int64_t most = (packs <= 256 ? 2 : 1) * kComputeUnits;
+  // no more than keep the longest wave as short as it is
+  const int64_t turns = std::max<int64_t>(1, up(c.rows, most * at_once));
+  return std::max<int64_t>(1, up(c.rows, turns * at_once));
 }
 
 template <typename T>
@@ -331,7 +336,9 @@ void norm_backward(const acc_layernorm& c, const void* dy, const void* x, const 
   LAUNCH((layernorm_backward_kernel<T, N, THREADS, K, BLOCK>), dim3(count), dim3(BLOCK), stream, static_cast<const T*>(dy),      \
          static_cast<const T*>(x), w, mean, rstd, static_cast<T*>(dx), c.rows, (int)c.dim, c.y_stride, c.x_stride,               \
          c.grad_x_stride, parts)
-  if (packs <= 64) BACKWARD(64, 1, 256);
+  if (packs <= 16) BACKWARD(16, 1, 256);
+  else if (packs <= 32) BACKWARD(16, 2, 256);
+  else if (packs <= 64) BACKWARD(64, 1, 256);
   else if (packs <= 128) BACKWARD(64, 2, 256);
   else if (packs <= 256) BACKWARD(64, 4, 256);
   else if (packs <= 512) BACKWARD(256, 2, 256);
