@@ -143,11 +143,15 @@ EmbeddingPlan plan_embedding(const acc_embedding& e) {
   return p;
 }
 
+constexpr int64_t kLookupMany = 4096;
+
 template <typename I, typename T, typename O>
 void lookup(const acc_embedding& e, const void* ids, const void* table, void* out, void* stream) {
   constexpr int N = sizeof(T) == 2 ? 8 : 4;
   int lanes_log2 = 3;
-  while (lanes_log2 < 8 && ((int64_t)N << lanes_log2) < e.dim) ++lanes_log2;
+  // many tokens: lanes with all their requests under way; few: lanes for all columns
+  const int each = e.tokens >= kLookupMany ? kLookupLoads : 1;
+  while (lanes_log2 < 8 && ((int64_t)(N * each) << lanes_log2) < e.dim) ++lanes_log2;
   const int64_t across = up(e.dim, (int64_t)kLookupLoads * N << lanes_log2);
   for (int64_t t = 0; t < e.tokens; t += kRowsPerLaunch) {
     const int64_t n = std::min(kRowsPerLaunch, e.tokens - t);
