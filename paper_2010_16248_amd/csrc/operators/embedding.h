@@ -448,18 +448,20 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const uint32_t* __re
   }
 }
 
-// The runs that cross chunks: the wave of the chunk where one begins adds its parts in order.
+// The runs that cross chunks: the workgroup of the chunk where one begins adds its parts in order, its first wave those of
+// short runs, all its waves a share each of long ones (a frequent token has thousands of rows).
+constexpr int kJoinWaves = 4;
 template <int N>
-__global__ __launch_bounds__(256) void embedding_join_kernel(const uint32_t* __restrict__ skey, int64_t n, int chunk, int64_t chunks,
-                                                             uint32_t vocab, const float* __restrict__ parts,
-                                                             float* __restrict__ table, int64_t table_stride, int64_t dim, float scale,
-                                                             int accumulate) {
-  const int64_t b = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lo = b * chunk, hi = lo + chunk;
+__global__ __launch_bounds__(kWave* kJoinWaves) void embedding_join_kernel(const uint32_t* __restrict__ skey, int64_t n, int chunk,
+                                                                          int64_t chunks, uint32_t vocab,
+                                                                          const float* __restrict__ parts, float* __restrict__ table,
+                                                                          int64_t table_stride, int64_t dim, float scale, int accumulate) {
+  const int64_t b = blockIdx.x, lo = b * chunk, hi = lo + chunk;
   if (hi >= n) return;
   const uint32_t row = skey[hi];
   if (row >= vocab || skey[hi - 1] != row || (lo > 0 && skey[lo] == row && skey[lo - 1] == row)) return;
   // the chunks that begin with the run's id
-  const int l = threadIdx.x & 63;
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int64_t end = b + 1;
   for (;;) {
     const int64_t k = end + l;
@@ -467,20 +469,35 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(const uint32_t* __r
     end += others ? __builtin_ctzll(others) : kWave;
     if (others) break;
   }
+  const int64_t count = end - b - 1;
+  const bool shared = count > kJoinRows;               // the same for the whole workgroup
+  if (!shared && w > 0) return;
+  const int64_t share = shared ? (count + kJoinWaves - 1) / kJoinWaves : count;
+  const int64_t from = min(b + 1 + w * share, end), to_part = min(from + share, end);
   const int64_t c = ((int64_t)blockIdx.y * kWave + l) * N, left = dim - c;
-  if (left <= 0) return;
   float* to = table + (int64_t)row * table_stride + c;
-  F32<N> old = {}, acc = widen<float, N>(load_some<N>(parts + (2 * b + 1) * dim + c, left));
-  if (accumulate) old = widen<float, N>(load_some<N>(to, left));
-  for (int64_t k = b + 1; k < end; k += kJoinRows) {
+  F32<N> old = {}, acc = {};
+  if (w == 0) {
+    acc = widen<float, N>(load_some<N>(parts + (2 * b + 1) * dim + c, left));
+    if (accumulate) old = widen<float, N>(load_some<N>(to, left));
+  }
+  for (int64_t k = from; k < to_part; k += kJoinRows) {
     Pack<float, N> v[kJoinRows];
 #pragma unroll
-    for (int j = 0; j < kJoinRows; ++j) v[j] = load_some<N>(parts + 2 * min(k + j, end - 1) * dim + c, left);
+    for (int j = 0; j < kJoinRows; ++j) v[j] = load_some<N>(parts + 2 * min(k + j, to_part - 1) * dim + c, left);
 #pragma unroll
     for (int j = 0; j < kJoinRows; ++j)
-      if (k + j < end) acc += widen<float, N>(v[j]);
+      if (k + j < to_part) acc += widen<float, N>(v[j]);
   }
-  to_row<N>(to, acc, old, scale, accumulate != 0, left);
+  if (shared) {
+    __shared__ F32<N> of[kJoinWaves][kWave];
+    of[w][l] = acc;
+    __syncthreads();
+    if (w > 0) return;
+#pragma unroll
+    for (int k = 1; k < kJoinWaves; ++k) acc += of[k][l];
+  }
+  if (left > 0) to_row<N>(to, acc, old, scale, accumulate != 0, left);
 }
 
 }  // namespace accop

@@ -126,10 +126,12 @@ EmbeddingPlan plan_embedding(const acc_embedding& e) {
     p.tile = up(up(n, kSortTiles), kSortStep) * kSortStep;
     p.tiles = (int)up(n, p.tile);
   }
-  // A wave goes through a chunk's tokens one after the other, and through the parts of a run, of which there may be one per
-  // chunk: chunks of about sqrt(n) / 8 to sqrt(n) / 4.
+  // A wave goes through a chunk's tokens one after the other, and a few through the parts of a run, of which there may be one per
+  // chunk: chunks of about sqrt(n) / 12 to sqrt(n) / 6, twice that where waves abound or runs are long (us at the shorter and the longer:
+  // 86738 tokens of 62 columns 59 and 77, 20000 of 672 45 and 46, 131072 of 2048 264 and 249, 128345 of 348 in 425 rows 79 and 68).
+  const int64_t scale = up(e.dim, kWave * 4) >= 8 || n > 32 * e.vocab ? 64 : 128;
   p.chunk = 8;
-  while (p.chunk < 128 && 64LL * p.chunk * p.chunk < n) p.chunk *= 2;
+  while (p.chunk < 128 && scale * p.chunk * p.chunk < n) p.chunk *= 2;
   p.chunks = up(n, p.chunk);
   int64_t at = 0;
   auto take = [&](int64_t bytes) { const int64_t o = at; at += round256(bytes); return o; };
@@ -266,7 +268,7 @@ void embedding_gradient(const acc_embedding& e, const EmbeddingPlan& p, const I*
   }
   if (e.out_type == ACC_BF16) sum_runs<bf16>(e, p, key[at], pos[at], grad, table, stride, parts, dirty, stream);
   else sum_runs<float>(e, p, key[at], pos[at], grad, table, stride, parts, dirty, stream);
-  LAUNCH((embedding_join_kernel<4>), dim3((unsigned)up(p.chunks, 4), (unsigned)up(e.dim, kWave * 4)), dim3(256), stream, key[at], e.tokens,
+  LAUNCH((embedding_join_kernel<4>), dim3((unsigned)p.chunks, (unsigned)up(e.dim, kWave * 4)), dim3(kWave * kJoinWaves), stream, key[at], e.tokens,
          p.chunk, p.chunks, vocab, parts, table, stride, e.dim, e.scale, e.accumulate);
 }
 
@@ -430,7 +432,7 @@ struct RecurrencePlan {
 
 RecurrencePlan plan_recurrence(const acc_recurrence& c, bool backward) {
   RecurrencePlan p;
-  p.lane = c.type == ACC_BF16 && c.channels % 2 == 0 ? 2 : 1;
+  p.lane = c.type == ACC_BF16 && c.channels > 1 ? 2 : 1;
   p.walk = c.steps <= kWalkSteps;
   if (p.walk) return p;
   p.wave_steps = backward && p.lane == 2 ? 8 : 16;
@@ -458,7 +460,7 @@ ChunkSlots chunk_slots(const RecurrencePlan& p, void* workspace, void* stream) {
   return s;
 }
 
-template <typename T, int N, int S>
+template <typename T, int N, int S, bool ODD>
 void run_forward(const acc_recurrence& c, const RecurrencePlan& p, const void* gate, const void* input, const float* h0,
                  const int32_t* lengths, void* out, float* h_last, void* ws, void* stream) {
   if (p.walk) {
@@ -467,11 +469,11 @@ void run_forward(const acc_recurrence& c, const RecurrencePlan& p, const void* g
     return;
   }
   const ChunkSlots slots = chunk_slots(p, ws, stream);
-  LAUNCH((recurrence_forward_chunk_kernel<T, N, S>), dim3((unsigned)(p.chains * p.chunks)), dim3(kWave * p.waves), stream, shape_of(c),
+  LAUNCH((recurrence_forward_chunk_kernel<T, N, S, ODD>), dim3((unsigned)(p.chains * p.chunks)), dim3(kWave * p.waves), stream, shape_of(c),
          slots, static_cast<const T*>(gate), static_cast<const T*>(input), h0, lengths, static_cast<T*>(out), h_last);
 }
 
-template <typename T, int N, int S>
+template <typename T, int N, int S, bool ODD>
 void run_backward(const acc_recurrence& c, const RecurrencePlan& p, const void* gate, const void* input, const void* out,
                   const float* h0, const int32_t* lengths, const void* dout, const float* dlast, void* dgate, void* dinput, float* dh0,
                   void* ws, void* stream) {
@@ -482,7 +484,7 @@ void run_backward(const acc_recurrence& c, const RecurrencePlan& p, const void* 
     return;
   }
   const ChunkSlots slots = chunk_slots(p, ws, stream);
-  LAUNCH((recurrence_backward_chunk_kernel<T, N, S>), dim3((unsigned)(p.chains * p.chunks)), dim3(kWave * p.waves), stream, shape_of(c),
+  LAUNCH((recurrence_backward_chunk_kernel<T, N, S, ODD>), dim3((unsigned)(p.chains * p.chunks)), dim3(kWave * p.waves), stream, shape_of(c),
          slots, static_cast<const T*>(gate), static_cast<const T*>(input), static_cast<const T*>(out), h0, lengths,
          static_cast<const T*>(dout), dlast, static_cast<T*>(dgate), static_cast<T*>(dinput), dh0);
 }
@@ -654,7 +656,10 @@ int32_t accordion_recurrence_forward(const acc_recurrence* c, const void* gate_d
                      {reinterpret_cast<const char*>(lengths_dev), lengths_dev ? 4 * c->batch : 0},
                      rows_span(h0_dev == h_last_dev ? nullptr : h0_dev, c->batch, c->channels, c->channels, 4)};
   REQUIRE(!any_overlap(s, 3, 7), "a buffer that is written overlaps another one");
-  const auto run = c->type == ACC_FLOAT ? run_forward<float, 1, 16> : p.lane == 2 ? run_forward<bf16, 2, 16> : run_forward<bf16, 1, 16>;
+  const auto run = c->type == ACC_FLOAT ? run_forward<float, 1, 16, false>
+                   : p.lane == 1      ? run_forward<bf16, 1, 16, false>
+                   : c->channels % 2  ? run_forward<bf16, 2, 16, true>
+                                      : run_forward<bf16, 2, 16, false>;
   run(*c, p, gate_dev, input_dev, h0_dev, lengths_dev, out_dev, h_last_dev, workspace_dev, hip_stream);
   return launched();
 }
@@ -686,7 +691,10 @@ int32_t accordion_recurrence_backward(const acc_recurrence* c, const void* gate_
                       rows_span(grad_last_dev, c->batch, c->channels, c->channels, 4),
                       {reinterpret_cast<const char*>(lengths_dev), lengths_dev ? 4 * c->batch : 0}};
   REQUIRE(!any_overlap(s, 4, 11), "a buffer that is written overlaps another one");
-  const auto run = c->type == ACC_FLOAT ? run_backward<float, 1, 16> : p.lane == 2 ? run_backward<bf16, 2, 8> : run_backward<bf16, 1, 16>;
+  const auto run = c->type == ACC_FLOAT ? run_backward<float, 1, 16, false>
+                   : p.lane == 1      ? run_backward<bf16, 1, 16, false>
+                   : c->channels % 2  ? run_backward<bf16, 2, 8, true>
+                                      : run_backward<bf16, 2, 8, false>;
   run(*c, p, gate_dev, input_dev, out_dev, h0_dev, lengths_dev, grad_out_dev, grad_last_dev, grad_gate_dev, grad_input_dev,
                               grad_h0_dev, workspace_dev, hip_stream);
   return launched();

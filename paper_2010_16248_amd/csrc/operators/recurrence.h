@@ -348,14 +348,29 @@ __device__ __forceinline__ void load_steps(Pack<T, N> (&v)[S], const T* p, int64
   }
 }
 
-// N divides the channels, so a lane has all of its N channels or none (it then works on the first ones and stores nothing).
+// A lane has all of its N channels or none (it then works on the first ones and stores nothing) -- or, of an odd number of channels
+// (ODD, N = 2), the last one alone: it loads the one in front of it too, takes its own for both and stores one.
+// (bf16, one channel per lane instead: 32 x 757 x 1717 backward 226 us, this way 163.)
+template <typename T, int N, bool ODD>
+__device__ __forceinline__ F32<N> lane_values(const Pack<T, N>& v, bool alone) {
+  F32<N> f = widen<T, N>(v);
+  if (ODD && alone) f[0] = f[N - 1];
+  return f;
+}
+template <typename T, int N, bool ODD, bool STREAM>
+__device__ __forceinline__ void store_lane(T* p, const F32<N>& v, bool alone) {
+  if (ODD && alone) *p = (T)v[0];
+  else if (STREAM) store_stream<T, N>(p, v);
+  else store<T, N>(p, v);
+}
+
 // WHOLE: every step of the chunk belongs to the sequence.
-template <typename T, int N, int S, bool WHOLE>
+template <typename T, int N, int S, bool ODD, bool WHOLE>
 __device__ __forceinline__ void forward_chunk(const RecurrenceShape& s, const ChunkSlots& slots, const ChunkPlace& p, ChunkFold<N>& fold,
                                               const T* gate, const T* input, const float* h0, int64_t len, T* out, float* h_last) {
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-  const bool mine = p.left > 0;
-  const int64_t c = mine ? p.c : 0, ends = p.b * s.channels + c;
+  const bool mine = p.left > 0, alone = ODD && p.left == 1;
+  const int64_t c = mine ? p.c - (alone ? 1 : 0) : 0, ends = p.b * s.channels + c;
   const int64_t t0 = ((int64_t)p.chunk * waves + w) * S;
   const int in = WHOLE ? S : (int)min((int64_t)S, max(len - t0, (int64_t)0));          // steps of the sequence
   const int here = WHOLE ? S : (int)min((int64_t)S, max(s.steps - t0, (int64_t)0));    // steps of the tensors
@@ -367,7 +382,7 @@ __device__ __forceinline__ void forward_chunk(const RecurrenceShape& s, const Ch
     load_steps<T, N, S>(v, input + p.b * s.input_b + t0 * s.input_t + c, s.input_t, in - 1);
 #pragma unroll
     for (int j = 0; j < S; ++j) {
-      const F32<N> ff = widen<T, N>(f[j]), xx = widen<T, N>(v[j]);
+      const F32<N> ff = lane_values<T, N, ODD>(f[j], alone), xx = lane_values<T, N, ODD>(v[j], alone);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const Gates k = gates(ff[i]);
@@ -378,25 +393,25 @@ __device__ __forceinline__ void forward_chunk(const RecurrenceShape& s, const Ch
       }
     }
   }
-  if (h0 && p.chunk < kChunkGroup) first = widen<float, N>(load<N>(h0 + ends));
+  if (h0 && p.chunk < kChunkGroup) first = lane_values<float, N, ODD>(load<N>(h0 + ends), alone);
   F32<N> h = chunk_state<N>(slots, p, A, H, first, fold);
   if (!mine) return;
-  T* o = out + p.b * s.out_b + t0 * s.out_t + c;
+  T* o = out + p.b * s.out_b + t0 * s.out_t + p.c;
 #pragma unroll
   for (int j = 0; j < S; ++j) {
     if (j < in) {
 #pragma unroll
       for (int i = 0; i < N; ++i) h[i] = fmaf(a[j][i], h[i], b[j][i]);
-      store_stream<T, N>(o, h);
+      store_lane<T, N, ODD, true>(o, h, alone);
     } else if (j < here) {
-      store<T, N>(o, F32<N>{});
+      store_lane<T, N, ODD, true>(o, F32<N>{}, alone);
     }
     o += s.out_t;
   }
-  if (h_last && p.chunk == slots.chunks - 1 && w == waves - 1) store<float, N>(h_last + ends, h);
+  if (h_last && p.chunk == slots.chunks - 1 && w == waves - 1) store_lane<float, N, ODD, false>(h_last + p.b * s.channels + p.c, h, alone);
 }
 
-template <typename T, int N, int S>
+template <typename T, int N, int S, bool ODD>
 __global__ __launch_bounds__(kWave* kChunkWaves, 3) void recurrence_forward_chunk_kernel(
     RecurrenceShape s, ChunkSlots slots, const T* __restrict__ gate, const T* __restrict__ input, const float* h0,
     const int32_t* __restrict__ lengths, T* __restrict__ out, float* h_last) {
@@ -404,19 +419,19 @@ __global__ __launch_bounds__(kWave* kChunkWaves, 3) void recurrence_forward_chun
   __shared__ uint32_t ticket;
   const ChunkPlace p = chunk_place<N>(slots, s, &ticket);
   const int64_t len = steps_of(lengths, p.b, s.steps), per = (int64_t)(blockDim.x >> 6) * S;
-  if ((p.chunk + 1) * per <= len) forward_chunk<T, N, S, true>(s, slots, p, fold, gate, input, h0, len, out, h_last);
-  else forward_chunk<T, N, S, false>(s, slots, p, fold, gate, input, h0, len, out, h_last);
+  if ((p.chunk + 1) * per <= len) forward_chunk<T, N, S, ODD, true>(s, slots, p, fold, gate, input, h0, len, out, h_last);
+  else forward_chunk<T, N, S, ODD, false>(s, slots, p, fold, gate, input, h0, len, out, h_last);
 }
 
 // Backward in time: the state is c_t = a_t G_t, the gradient of h_{t-1}; c_t = a_t c_{t+1} + a_t grad_out_t.  Steps are counted from
 // the last one on.  WHOLE: every step of the chunk belongs to the sequence and none is its first.
-template <typename T, int N, int S, bool WHOLE>
+template <typename T, int N, int S, bool ODD, bool WHOLE>
 __device__ __forceinline__ void backward_chunk(const RecurrenceShape& s, const ChunkSlots& slots, const ChunkPlace& p, ChunkFold<N>& fold,
                                                const T* gate, const T* input, const T* out, const float* h0, int64_t len, const T* dout,
                                                const float* dlast, T* dgate, T* dinput, float* dh0) {
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-  const bool mine = p.left > 0;
-  const int64_t c = mine ? p.c : 0, ends = p.b * s.channels + c;
+  const bool mine = p.left > 0, alone = ODD && p.left == 1;
+  const int64_t c = mine ? p.c - (alone ? 1 : 0) : 0, ends = p.b * s.channels + c;
   const int64_t t0 = s.steps - 1 - ((int64_t)p.chunk * waves + w) * S;                          // the wave's latest step
   const int here = WHOLE ? S : (int)min((int64_t)S, max(t0 + 1, (int64_t)0));                   // steps of the tensors: j < here
   const int out_of = WHOLE ? 0 : (int)min((int64_t)here, max(t0 + 1 - len, (int64_t)0));        // of the sequence: out_of <= j
@@ -449,7 +464,7 @@ __device__ __forceinline__ void backward_chunk(const RecurrenceShape& s, const C
 #pragma unroll
     for (int j = 0; j < S; ++j) {
       const bool on = j >= out_of && j < here;
-      const F32<N> ff = widen<T, N>(f[j]), dd = widen<T, N>(d[j]);
+      const F32<N> ff = lane_values<T, N, ODD>(f[j], alone), dd = lane_values<T, N, ODD>(d[j], alone);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const Gates k = gates(ff[i]);
@@ -460,34 +475,34 @@ __device__ __forceinline__ void backward_chunk(const RecurrenceShape& s, const C
       }
     }
   }
-  if (dlast && p.chunk < kChunkGroup) first = widen<float, N>(load<N>(dlast + ends));
+  if (dlast && p.chunk < kChunkGroup) first = lane_values<float, N, ODD>(load<N>(dlast + ends), alone);
   state = chunk_state<N>(slots, p, A, H, first, fold);
   if (!mine) return;
   F32<N> h_first = {};
-  if (!WHOLE && h0 && here > 0 && t0 - here + 1 == 0) h_first = widen<float, N>(load<N>(h0 + ends));
-  T* og = dgate + p.b * s.dgate_b + t0 * s.dgate_t + c;
-  T* ox = dinput + p.b * s.dinput_b + t0 * s.dinput_t + c;
+  if (!WHOLE && h0 && here > 0 && t0 - here + 1 == 0) h_first = lane_values<float, N, ODD>(load<N>(h0 + ends), alone);
+  T* og = dgate + p.b * s.dgate_b + t0 * s.dgate_t + p.c;
+  T* ox = dinput + p.b * s.dinput_b + t0 * s.dinput_t + p.c;
 #pragma unroll
   for (int j = 0; j < S; ++j) {
     if (j < here) {
       F32<N> dg = {}, dx = {};
       if (j >= out_of) {
-        const F32<N> total = state + widen<T, N>(d[j]), xx = widen<T, N>(x[j]);
-        const F32<N> h = WHOLE || t0 - j > 0 ? widen<T, N>(before[j]) : h_first;
+        const F32<N> total = state + lane_values<T, N, ODD>(d[j], alone), xx = lane_values<T, N, ODD>(x[j], alone);
+        const F32<N> h = WHOLE || t0 - j > 0 ? lane_values<T, N, ODD>(before[j], alone) : h_first;
         dx = z[j] * total;
         dg = (h - xx) * a[j] * dx;
         state = a[j] * total;
       }
-      store_stream<T, N>(og, dg);
-      store_stream<T, N>(ox, dx);
+      store_lane<T, N, ODD, true>(og, dg, alone);
+      store_lane<T, N, ODD, true>(ox, dx, alone);
     }
     og -= s.dgate_t;
     ox -= s.dinput_t;
   }
-  if (dh0 && p.chunk == slots.chunks - 1 && w == waves - 1) store<float, N>(dh0 + ends, state);
+  if (dh0 && p.chunk == slots.chunks - 1 && w == waves - 1) store_lane<float, N, ODD, false>(dh0 + p.b * s.channels + p.c, state, alone);
 }
 
-template <typename T, int N, int S>
+template <typename T, int N, int S, bool ODD>
 __global__ __launch_bounds__(kWave* kChunkWaves, 3) void recurrence_backward_chunk_kernel(
     RecurrenceShape s, ChunkSlots slots, const T* __restrict__ gate, const T* __restrict__ input, const T* __restrict__ out,
     const float* __restrict__ h0, const int32_t* __restrict__ lengths, const T* __restrict__ dout, const float* __restrict__ dlast,
@@ -498,9 +513,9 @@ __global__ __launch_bounds__(kWave* kChunkWaves, 3) void recurrence_backward_chu
   const int64_t len = steps_of(lengths, p.b, s.steps), per = (int64_t)(blockDim.x >> 6) * S;
   const int64_t latest = s.steps - p.chunk * per, earliest = latest - per;     // steps [earliest, latest)
   if (latest <= len && earliest > 0)
-    backward_chunk<T, N, S, true>(s, slots, p, fold, gate, input, out, h0, len, dout, dlast, dgate, dinput, dh0);
+    backward_chunk<T, N, S, ODD, true>(s, slots, p, fold, gate, input, out, h0, len, dout, dlast, dgate, dinput, dh0);
   else
-    backward_chunk<T, N, S, false>(s, slots, p, fold, gate, input, out, h0, len, dout, dlast, dgate, dinput, dh0);
+    backward_chunk<T, N, S, ODD, false>(s, slots, p, fold, gate, input, out, h0, len, dout, dlast, dgate, dinput, dh0);
 }
 
 }  // namespace accop
