@@ -412,6 +412,9 @@ int32_t check_recurrence(const acc_recurrence* c, bool backward) {
   return ACC_OK;
 }
 
+// Whether rows start on whole pieces of memory.
+bool whole_rows(const void* p, int64_t step_bytes) { return reinterpret_cast<uintptr_t>(p) % 64 == 0 && step_bytes % 64 == 0; }
+
 RecurrenceShape shape_of(const acc_recurrence& c) {
   return {c.steps, c.channels, c.gate_batch, c.gate_step, c.input_batch, c.input_step, c.out_batch, c.out_step,
           c.grad_gate_batch, c.grad_gate_step, c.grad_input_batch, c.grad_input_step, c.grad_out_batch, c.grad_out_step};
@@ -460,7 +463,7 @@ ChunkSlots chunk_slots(const RecurrencePlan& p, void* workspace, void* stream) {
   return s;
 }
 
-template <typename T, int N, int S, bool ODD>
+template <typename T, int N, int S, bool ODD, bool STREAM>
 void run_forward(const acc_recurrence& c, const RecurrencePlan& p, const void* gate, const void* input, const float* h0,
                  const int32_t* lengths, void* out, float* h_last, void* ws, void* stream) {
   if (p.walk) {
@@ -469,11 +472,11 @@ void run_forward(const acc_recurrence& c, const RecurrencePlan& p, const void* g
     return;
   }
   const ChunkSlots slots = chunk_slots(p, ws, stream);
-  LAUNCH((recurrence_forward_chunk_kernel<T, N, S, ODD>), dim3((unsigned)(p.chains * p.chunks)), dim3(kWave * p.waves), stream, shape_of(c),
+  LAUNCH((recurrence_forward_chunk_kernel<T, N, S, ODD, STREAM>), dim3((unsigned)(p.chains * p.chunks)), dim3(kWave * p.waves), stream, shape_of(c),
          slots, static_cast<const T*>(gate), static_cast<const T*>(input), h0, lengths, static_cast<T*>(out), h_last);
 }
 
-template <typename T, int N, int S, bool ODD>
+template <typename T, int N, int S, bool ODD, bool STREAM>
 void run_backward(const acc_recurrence& c, const RecurrencePlan& p, const void* gate, const void* input, const void* out,
                   const float* h0, const int32_t* lengths, const void* dout, const float* dlast, void* dgate, void* dinput, float* dh0,
                   void* ws, void* stream) {
@@ -484,7 +487,7 @@ void run_backward(const acc_recurrence& c, const RecurrencePlan& p, const void* 
     return;
   }
   const ChunkSlots slots = chunk_slots(p, ws, stream);
-  LAUNCH((recurrence_backward_chunk_kernel<T, N, S, ODD>), dim3((unsigned)(p.chains * p.chunks)), dim3(kWave * p.waves), stream, shape_of(c),
+  LAUNCH((recurrence_backward_chunk_kernel<T, N, S, ODD, STREAM>), dim3((unsigned)(p.chains * p.chunks)), dim3(kWave * p.waves), stream, shape_of(c),
          slots, static_cast<const T*>(gate), static_cast<const T*>(input), static_cast<const T*>(out), h0, lengths,
          static_cast<const T*>(dout), dlast, static_cast<T*>(dgate), static_cast<T*>(dinput), dh0);
 }
@@ -656,10 +659,12 @@ int32_t accordion_recurrence_forward(const acc_recurrence* c, const void* gate_d
                      {reinterpret_cast<const char*>(lengths_dev), lengths_dev ? 4 * c->batch : 0},
                      rows_span(h0_dev == h_last_dev ? nullptr : h0_dev, c->batch, c->channels, c->channels, 4)};
   REQUIRE(!any_overlap(s, 3, 7), "a buffer that is written overlaps another one");
-  const auto run = c->type == ACC_FLOAT ? run_forward<float, 1, 16, false>
-                   : p.lane == 1      ? run_forward<bf16, 1, 16, false>
-                   : c->channels % 2  ? run_forward<bf16, 2, 16, true>
-                                      : run_forward<bf16, 2, 16, false>;
+  const bool whole = whole_rows(out_dev, c->out_step * e);
+  const auto run = c->type == ACC_FLOAT ? (whole ? run_forward<float, 1, 16, false, true> : run_forward<float, 1, 16, false, false>)
+                   : p.lane == 1      ? run_forward<bf16, 1, 16, false, false>
+                   : c->channels % 2  ? run_forward<bf16, 2, 16, true, false>
+                   : whole            ? run_forward<bf16, 2, 16, false, true>
+                                      : run_forward<bf16, 2, 16, false, false>;
   run(*c, p, gate_dev, input_dev, h0_dev, lengths_dev, out_dev, h_last_dev, workspace_dev, hip_stream);
   return launched();
 }
@@ -691,10 +696,12 @@ int32_t accordion_recurrence_backward(const acc_recurrence* c, const void* gate_
                       rows_span(grad_last_dev, c->batch, c->channels, c->channels, 4),
                       {reinterpret_cast<const char*>(lengths_dev), lengths_dev ? 4 * c->batch : 0}};
   REQUIRE(!any_overlap(s, 4, 11), "a buffer that is written overlaps another one");
-  const auto run = c->type == ACC_FLOAT ? run_backward<float, 1, 16, false>
-                   : p.lane == 1      ? run_backward<bf16, 1, 16, false>
-                   : c->channels % 2  ? run_backward<bf16, 2, 8, true>
-                                      : run_backward<bf16, 2, 8, false>;
+  const bool whole = whole_rows(grad_gate_dev, c->grad_gate_step * e) && whole_rows(grad_input_dev, c->grad_input_step * e);
+  const auto run = c->type == ACC_FLOAT ? (whole ? run_backward<float, 1, 16, false, true> : run_backward<float, 1, 16, false, false>)
+                   : p.lane == 1      ? run_backward<bf16, 1, 16, false, false>
+                   : c->channels % 2  ? run_backward<bf16, 2, 8, true, false>
+                   : whole            ? run_backward<bf16, 2, 8, false, true>
+                                      : run_backward<bf16, 2, 8, false, false>;
   run(*c, p, gate_dev, input_dev, out_dev, h0_dev, lengths_dev, grad_out_dev, grad_last_dev, grad_gate_dev, grad_input_dev,
                               grad_h0_dev, workspace_dev, hip_stream);
   return launched();
