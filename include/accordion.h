@@ -455,9 +455,20 @@ int32_t accordion_recurrence_backward(const acc_recurrence* cfg, const void* gat
  *   state_bits 32: m and v as fp32; m_scale and v_scale are NULL.
  *   state_bits 8:  every tensor starts on a multiple of ACC_ADAMW_BLOCK elements.  A block of
  *     ACC_ADAMW_BLOCK elements of a tensor holds x, for m, and sqrt(v), for v, as 8-bit floating-point
- *     codes (e4m3, largest 448, to nearest even) of x (448 / max|x|), and max|x| / 448 as its fp32 scale; a
- *     block whose max|x| is below 2^-100 is held as zeros.  A positive sqrt(v) of any other block keeps a code of at least
- *     the smallest positive one, so that no update is divided by eps alone because of the rounding.
+ *     codes (e4m3, largest 448) of x (448 / max|x|), and max|x| / 448 as its fp32 scale; a
+ *     block whose max|x| is below 2^-100 is held as zeros.  A positive sqrt(v) of any other block keeps
+ *     a code of at least the smallest positive one, so that no update is divided by eps alone because
+ *     of the rounding.
+ *     Codes are rounded to nearest even where beta1 <= 0.9 (m) and beta2 <= 0.95 (sqrt(v)).  Codes to
+ *     nearest do not follow an average that a step moves by less than half their spacing: beyond these
+ *     betas, and everywhere with dither = 1, code values are floor(|y| / q + u) q (at most 448), for
+ *     y = x (448 / max|x|), the spacing q of codes at |y| and
+ *         u = floor(((e k + step 0x9E3779B9) mod 2^32) / 2^12) / 2^20,
+ *     e being the element's place in the state and k 0x6A09E667 for m, 0xBB67AE85 for sqrt(v): what is
+ *     cut off in one step is made up for in others.  A step frozen into a graph freezes u too, and an
+ *     average that moves slowly then stands still.  To nearest, at beta2 = 0.95, sqrt(v) of random
+ *     gradients is held 3 to 6 % too large; gradients that do not vary at all from step to step need
+ *     dither = 1 at any betas.
  *     The step itself uses the values before they are rounded to codes.  An infinity or NaN in a
  *     block's moments makes the whole block's moments NaN.
  * A state of zeros is the state before the first step. */
@@ -471,6 +482,7 @@ typedef struct acc_adamw {
   const float* weight_decay_host;/* per tensor, finite and >= 0; NULL: none */
   double lr, beta1, beta2, eps;  /* finite; lr >= 0, betas in [0, 1), eps >= 0 */
   int64_t step;                  /* >= 1 */
+  int32_t dither;                /* 0 or 1 (8 bits: see above; 32 bits: plays no role) */
 } acc_adamw;
 int32_t accordion_adamw_state_elements(const acc_adamw* cfg, int64_t* out_elements);
 int32_t accordion_adamw_step(const acc_adamw* cfg, void* const* weights_host_array,

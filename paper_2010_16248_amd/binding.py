@@ -64,7 +64,7 @@ class acc_adamw(C.Structure):
     _fields_ = [("n_tensors", C.c_int32), ("weight_type", C.c_int32), ("grad_type", C.c_int32),
                 ("state_bits", C.c_int32), ("sizes_host", C.POINTER(C.c_int64)),
                 ("weight_decay_host", C.POINTER(C.c_float)), ("lr", C.c_double), ("beta1", C.c_double),
-                ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int64)]
+                ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int64), ("dither", C.c_int32)]
 
 
 class AccordionError(RuntimeError):
@@ -478,10 +478,12 @@ def _tensors_of(tensors: Sequence, name: str):
 
 def adamw_step(weights: Sequence, grads: Sequence, state, lr: float, step: int, weight_decay=0.0,
                betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8, copies: Optional[Sequence] = None,
-               grad_scale=None) -> None:
+               grad_scale=None, dither: bool = False) -> None:
     """One AdamW step over all tensors (contiguous; all weights of one type, all gradients of one type).  state: as
     adamw_state made it for their sizes; weight_decay: one number or one per tensor; copies: bfloat16 tensors that get the
-    new weights too; grad_scale: a float32 element on the GPU that multiplies every gradient."""
+    new weights too; grad_scale: a float32 element on the GPU that multiplies every gradient.  8-bit moments are rounded to nearest
+    where betas are at most (0.9, 0.95), and with thresholds that change with the step, so that they follow their averages, beyond;
+    dither: with thresholds everywhere (gradients that hardly vary from step to step)."""
     import torch
     lib = load_library()
     count = len(weights)
@@ -503,7 +505,7 @@ def adamw_step(weights: Sequence, grads: Sequence, state, lr: float, step: int, 
                   "a copy must be bfloat16, of its tensor's size, on its GPU")
             c_ptrs = _c_array(C.c_void_p, "Q", [0 if c is None else c.data_ptr() for c in copies])
     cfg = acc_adamw(count, _type_of(weights[0], "weights"), _type_of(grads[0], "grads"), bits, _c_array(C.c_int64, "q", sizes), None, lr,
-                    betas[0], betas[1], eps, step)
+                    betas[0], betas[1], eps, step, dither)
     elements = _state_elements(lib, cfg)
     held = torch.float32 if bits == 32 else torch.float8_e4m3fn
     mp, vp = _plain(m, "m", (elements,), held), _plain(v, "v", (elements,), held)

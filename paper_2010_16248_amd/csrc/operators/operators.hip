@@ -512,8 +512,9 @@ int64_t state_elements(const acc_adamw& c, int64_t n) { return c.state_bits == 8
 
 template <typename W, typename G>
 void adamw(const AdamArgs& a, int bits, unsigned tiles, void* stream) {
-  if (bits == 8) LAUNCH((adamw_kernel<W, G, true>), dim3(tiles), dim3(256), stream, a);
-  else LAUNCH((adamw_kernel<W, G, false>), dim3(tiles), dim3(256), stream, a);
+  if (bits == 32) LAUNCH((adamw_kernel<W, G, false, false>), dim3(tiles), dim3(256), stream, a);
+  else if (a.dither_m || a.dither_v) LAUNCH((adamw_kernel<W, G, true, true>), dim3(tiles), dim3(256), stream, a);
+  else LAUNCH((adamw_kernel<W, G, true, false>), dim3(tiles), dim3(256), stream, a);
 }
 
 }  // namespace
@@ -723,6 +724,7 @@ int32_t accordion_adamw_step(const acc_adamw* c, void* const* weights_host_array
   REQUIRE(std::isfinite(c->lr) && c->lr >= 0 && std::isfinite(c->eps) && c->eps >= 0, "lr and eps must be finite and not negative");
   REQUIRE(c->beta1 >= 0 && c->beta1 < 1 && c->beta2 >= 0 && c->beta2 < 1, "betas must lie in [0, 1)");
   REQUIRE(c->step >= 1, "step counts from 1");
+  REQUIRE(c->dither == 0 || c->dither == 1, "dither must be 0 or 1");
   int64_t elements = 0;
   for (int32_t i = 0; i < c->n_tensors; ++i) {
     const float wd = c->weight_decay_host ? c->weight_decay_host[i] : 0.f;
@@ -773,6 +775,9 @@ int32_t accordion_adamw_step(const acc_adamw* c, void* const* weights_host_array
   a.rate = (float)(c->lr / (1.0 - std::pow(c->beta1, (double)c->step)));
   a.up = (float)(1.0 / std::sqrt(1.0 - std::pow(c->beta2, (double)c->step)));
   a.eps = (float)c->eps;
+  a.turn = (uint32_t)c->step * kTurn;
+  a.dither_m = bits8 && (c->dither || c->beta1 > kNearestBeta1);
+  a.dither_v = bits8 && (c->dither || c->beta2 > kNearestBeta2);
   int64_t at = 0;
   int64_t tiles = 0;
   a.count = 0;

@@ -281,3 +281,8 @@ def test_sizes_beyond_a_launch_are_refused(lib):
                      input_batch=2 ** 26, input_step=64)
     refused(lib, lib.accordion_recurrence_workspace_bytes(C.byref(cfg), C.byref(n)), "too many steps")
     refused(lib, lib.accordion_recurrence_forward(C.byref(cfg), *[at(i << 12) for i in range(7)], 1 << 40, None), "too many steps")
+
+
+@pytest.mark.parametrize("dither", [-1, 2])
+def test_adamw_thresholds_are_on_or_off(lib, dither):
+    refused(lib, step(lib, adamw(state_bits=8, dither=dither)), "dither")
