@@ -89,7 +89,7 @@ __device__ __forceinline__ float dithered(float y, float u) {
 template <bool ROOT>
 __device__ __forceinline__ uint32_t encode_block(const f4& x, float* scale, bool dither, uint32_t phase, uint32_t step_phase) {
   const float top = __uint_as_float(wave_top(x));
-  const bool held = !(top < kTiny);            // NaN: held, and everything becomes NaN
+  const bool held = !(top < kTiny);            // infinity, NaN: held, with an up of zero or NaN that makes the whole block NaN
   const float up = held ? kTop / top : 0.f;
   f4 y = x * up;
   if (dither)
@@ -98,7 +98,7 @@ __device__ __forceinline__ uint32_t encode_block(const f4& x, float* scale, bool
   if (ROOT)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (held && x[i] > 0.f && y[i] < kLeast) y[i] = kLeast;
+      if (up > 0.f && x[i] > 0.f && y[i] < kLeast) y[i] = kLeast;
   if ((threadIdx.x & 63) == 0) *scale = held ? top * (1.0f / kTop) : 0.f;
   return encode4(y);
 }

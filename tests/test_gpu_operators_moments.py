@@ -144,3 +144,20 @@ def test_infinities_and_nan_pass_the_thresholds():
         bad = torch.zeros(700, dtype=torch.bool, device=DEV)
         bad[256:512] = True
         assert torch.equal(w[0].isnan(), bad)
+
+
+@pytest.mark.parametrize("dither", [False, True])
+def test_a_second_moment_that_overflows_spoils_its_block(dither):
+    """A gradient of 1e25 is finite, and so is m; its square is not.  The block must not go on with infinite sqrt(v), which would hold all
+    of its weights still without a sign."""
+    n = 700
+    w, g, half = [torch.ones(n, device=DEV)], torch.full((n,), 0.5, device=DEV), torch.full((n,), 0.5, device=DEV)
+    g[300] = 1e25
+    state = B.adamw_state([n], 8, DEV)
+    B.adamw_step(w, [g], state, 0.1, 1, dither=dither)
+    m, root = _held(state)
+    bad = torch.zeros(n, dtype=torch.bool, device=DEV)
+    bad[256:512] = True
+    assert m.isfinite().all() and torch.equal(root[:n].isnan(), bad) and root[~root.isnan()].isfinite().all()
+    B.adamw_step(w, [half], state, 0.1, 2, dither=dither)
+    assert torch.equal(w[0].isnan(), bad)
