@@ -161,6 +161,26 @@ constexpr unsigned long long kNotYet = ~0ull;
 template <int N>
 using F64 = double __attribute__((ext_vector_type(N)));
 
+// The product of gates A and B of maps that follow one another.  It must not become zero unless a gate is: an infinite state stays
+// infinite through any number of gates above zero, and meets no 0 x infinity.  (Below 2^-1022 its size plays no other role.)
+constexpr double kLeastGates = 0x1p-1022;
+__device__ __forceinline__ double gates_product(double A, double B) {
+  const double p = A * B;
+  return p == 0.0 && A != 0.0 && B != 0.0 ? kLeastGates : p;
+}
+// The same of a wave's S gates, whose plain product is A.
+template <int N, int S>
+__device__ __forceinline__ void keep_gates(F64<N>& A, const F32<N> (&a)[S]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (__ballot(A[i] == 0.0) == 0) continue;
+    bool shut = false;
+#pragma unroll
+    for (int j = 0; j < S; ++j) shut |= a[j][i] == 0.f;
+    if (A[i] == 0.0 && !shut) A[i] = kLeastGates;
+  }
+}
+
 struct ChunkSlots {
   unsigned long long *map_a, *map_h;             // per chain, chunk and channel
   unsigned long long *group_a, *group_h, *state; // per chain, group and channel: the group's map, the state at its end
@@ -278,7 +298,7 @@ __device__ __forceinline__ F32<N> chunk_state(const ChunkSlots& s, const ChunkPl
 #pragma unroll 2
       for (int k = 0; k < waves; ++k) {
         const double ak = fold.a[k][ch];
-        A *= ak;
+        A = gates_product(A, ak);
         H = fma(ak, H, fold.h[k][ch]);
       }
       if (at < kChunkGroup - 1 && p.chunk + 1 < s.chunks) {
@@ -313,10 +333,10 @@ __device__ __forceinline__ F32<N> chunk_state(const ChunkSlots& s, const ChunkPl
         double GA = 1.0, GH = 0.0;
 #pragma unroll 2
         for (int k = 0; k < at; ++k) {
-          GA *= fold.before_a[k][ch];
+          GA = gates_product(GA, fold.before_a[k][ch]);
           GH = fma(fold.before_a[k][ch], GH, fold.before_h[k][ch]);
         }
-        A *= GA;
+        A = gates_product(A, GA);
         H = fma(fold.a[0][ch], GH, fold.h[0][ch]);
 #pragma unroll 2
         for (int k = 1; k < waves; ++k) H = fma(fold.a[k][ch], H, fold.h[k][ch]);
@@ -398,6 +418,7 @@ __device__ __forceinline__ void forward_chunk(const RecurrenceShape& s, const Ch
         H[i] = fma((double)a[j][i], H[i], (double)b[j][i]);
       }
     }
+    keep_gates<N, S>(A, a);
   }
   if (h0 && p.chunk < kChunkGroup) first = lane_values<float, N, ODD>(load<N>(h0 + ends), alone);
   F32<N> h = chunk_state<N>(slots, p, A, H, first, fold);
@@ -480,6 +501,7 @@ __device__ __forceinline__ void backward_chunk(const RecurrenceShape& s, const C
         H[i] = (double)a[j][i] * (H[i] + (on ? (double)dd[i] : 0.0));
       }
     }
+    keep_gates<N, S>(A, a);
   }
   if (dlast && p.chunk < kChunkGroup) first = lane_values<float, N, ODD>(load<N>(dlast + ends), alone);
   state = chunk_state<N>(slots, p, A, H, first, fold);
