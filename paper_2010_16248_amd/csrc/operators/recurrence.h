@@ -161,25 +161,10 @@ constexpr unsigned long long kNotYet = ~0ull;
 template <int N>
 using F64 = double __attribute__((ext_vector_type(N)));
 
-// The product of gates A and B of maps that follow one another.  It must not become zero unless a gate is: an infinite state stays
-// infinite through any number of gates above zero, and meets no 0 x infinity.  (Below 2^-1022 its size plays no other role.)
+// A product of gates must not become zero unless a gate is: an infinite state stays infinite through any number of gates above zero, and
+// meets no 0 x infinity.  (Below 2^-1022 its size plays no other role.)
 constexpr double kLeastGates = 0x1p-1022;
-__device__ __forceinline__ double gates_product(double A, double B) {
-  const double p = A * B;
-  return p == 0.0 && A != 0.0 && B != 0.0 ? kLeastGates : p;
-}
-// The same of a wave's S gates, whose plain product is A.
-template <int N, int S>
-__device__ __forceinline__ void keep_gates(F64<N>& A, const F32<N> (&a)[S]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    if (__ballot(A[i] == 0.0) == 0) continue;
-    bool shut = false;
-#pragma unroll
-    for (int j = 0; j < S; ++j) shut |= a[j][i] == 0.f;
-    if (A[i] == 0.0 && !shut) A[i] = kLeastGates;
-  }
-}
+__device__ __forceinline__ double keep_gates(double product, bool shut) { return product == 0.0 && !shut ? kLeastGates : product; }
 
 struct ChunkSlots {
   unsigned long long *map_a, *map_h;             // per chain, chunk and channel
@@ -295,12 +280,15 @@ __device__ __forceinline__ F32<N> chunk_state(const ChunkSlots& s, const ChunkPl
     const bool ends = at == kChunkGroup - 1 && group + 1 < s.groups;   // other groups build on this chunk
     double A = 1.0, H = 0.0;
     if (w < N) {                       // a wave for every 64 channels
+      bool shut = false;
 #pragma unroll 2
       for (int k = 0; k < waves; ++k) {
         const double ak = fold.a[k][ch];
-        A = gates_product(A, ak);
+        A *= ak;
+        shut |= ak == 0.0;
         H = fma(ak, H, fold.h[k][ch]);
       }
+      A = keep_gates(A, shut);
       if (at < kChunkGroup - 1 && p.chunk + 1 < s.chunks) {
         leave(s.map_a + slot0 + (int64_t)p.chunk * pitch + ch, A);
         leave(s.map_h + slot0 + (int64_t)p.chunk * pitch + ch, H);
@@ -331,12 +319,14 @@ __device__ __forceinline__ F32<N> chunk_state(const ChunkSlots& s, const ChunkPl
       const int64_t slot = group0 + (int64_t)group * pitch + ch;
       if (ends) {
         double GA = 1.0, GH = 0.0;
+        bool shut = A == 0.0;
 #pragma unroll 2
         for (int k = 0; k < at; ++k) {
-          GA = gates_product(GA, fold.before_a[k][ch]);
+          GA *= fold.before_a[k][ch];
+          shut |= fold.before_a[k][ch] == 0.0;
           GH = fma(fold.before_a[k][ch], GH, fold.before_h[k][ch]);
         }
-        A = gates_product(A, GA);
+        A = keep_gates(A * GA, shut);
         H = fma(fold.a[0][ch], GH, fold.h[0][ch]);
 #pragma unroll 2
         for (int k = 1; k < waves; ++k) H = fma(fold.a[k][ch], H, fold.h[k][ch]);
@@ -400,7 +390,7 @@ __device__ __forceinline__ void forward_chunk(const RecurrenceShape& s, const Ch
   const int64_t t0 = ((int64_t)p.chunk * waves + w) * S;
   const int in = WHOLE ? S : (int)min((int64_t)S, max(len - t0, (int64_t)0));          // steps of the sequence
   const int here = WHOLE ? S : (int)min((int64_t)S, max(s.steps - t0, (int64_t)0));    // steps of the tensors
-  F32<N> a[S], b[S], first = {};
+  F32<N> a[S], b[S], first = {}, least = F32<N>{} + 1.f;
   F64<N> A = F64<N>{} + 1.0, H = {};
   if (in > 0) {
     Pack<T, N> f[S], v[S];
@@ -415,10 +405,12 @@ __device__ __forceinline__ void forward_chunk(const RecurrenceShape& s, const Ch
         a[j][i] = j < in ? k.a : 1.f;
         b[j][i] = j < in ? k.z * xx[i] : 0.f;
         A[i] *= (double)a[j][i];
+        least[i] = fminf(least[i], a[j][i]);
         H[i] = fma((double)a[j][i], H[i], (double)b[j][i]);
       }
     }
-    keep_gates<N, S>(A, a);
+#pragma unroll
+    for (int i = 0; i < N; ++i) A[i] = keep_gates(A[i], least[i] == 0.f);
   }
   if (h0 && p.chunk < kChunkGroup) first = lane_values<float, N, ODD>(load<N>(h0 + ends), alone);
   F32<N> h = chunk_state<N>(slots, p, A, H, first, fold);
@@ -462,7 +454,7 @@ __device__ __forceinline__ void backward_chunk(const RecurrenceShape& s, const C
   const int64_t t0 = s.steps - 1 - ((int64_t)p.chunk * waves + w) * S;                          // the wave's latest step
   const int here = WHOLE ? S : (int)min((int64_t)S, max(t0 + 1, (int64_t)0));                   // steps of the tensors: j < here
   const int out_of = WHOLE ? 0 : (int)min((int64_t)here, max(t0 + 1 - len, (int64_t)0));        // of the sequence: out_of <= j
-  F32<N> a[S], z[S], first = {}, state;
+  F32<N> a[S], z[S], first = {}, least = F32<N>{} + 1.f, state;
   F64<N> A = F64<N>{} + 1.0, H = {};
   Pack<T, N> d[S], x[S], before[S];
   if (out_of < here) {
@@ -498,10 +490,12 @@ __device__ __forceinline__ void backward_chunk(const RecurrenceShape& s, const C
         a[j][i] = on ? k.a : 1.f;
         z[j][i] = k.z;
         A[i] *= (double)a[j][i];
+        least[i] = fminf(least[i], a[j][i]);
         H[i] = (double)a[j][i] * (H[i] + (on ? (double)dd[i] : 0.0));
       }
     }
-    keep_gates<N, S>(A, a);
+#pragma unroll
+    for (int i = 0; i < N; ++i) A[i] = keep_gates(A[i], least[i] == 0.f);
   }
   if (dlast && p.chunk < kChunkGroup) first = lane_values<float, N, ODD>(load<N>(dlast + ends), alone);
   state = chunk_state<N>(slots, p, A, H, first, fold);
