@@ -414,6 +414,7 @@ int32_t accordion_layernorm_backward(const acc_layernorm* cfg, const void* grad_
  *              grad_input_t = z_t G_t,  grad_gate_t = G_t (h_{t-1} - input_t) a_t z_t,
  *              grad_h0 = a_0 G_0
  * z is not computed as a difference from one; gates of +-infinity keep the state / take the input alone.
+ * Both gates keep values below the normal fp32 numbers; from |gate| = 104 on the smaller one is zero.
  * h0_dev (NULL: zeros), h_last_dev, grad_last_dev (NULL: zeros) and grad_h0_dev are batch x channels,
  * contiguous fp32; h_last_dev and grad_h0_dev may be NULL.  lengths_dev (int32 per sequence, NULL:
  * all steps): steps from a sequence's length on write zeros and leave the state as it is; their

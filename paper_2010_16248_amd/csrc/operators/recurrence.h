@@ -10,14 +10,15 @@ struct RecurrenceShape {
   int64_t dgate_b, dgate_t, dinput_b, dinput_t, dout_b, dout_t;
 };
 
-// e^-x for x >= 0 (NaN for NaN): 2^t of the rounded t = -x log2(e), times e^d with d = -x - t ln 2, what the rounding lost
-// (d is below 2^-16, so e^d = 1 + d; ln 2 rounded to fp32 is off by 1.9e-9, times t): within 4 units of 2^-24 up to x = 20, 7 beyond.  From 104 on the result is below the
-// smallest fp32 number.
-__device__ __forceinline__ float exp_neg(float x) {
-  x = x > 104.f ? 104.f : x;
+// e^-x for x >= 0 (NaN for NaN), times 2^32 where `far`: 2^t of the rounded t = -x log2(e), times e^d with d = -x - t ln 2, what the
+// rounding lost (d is below 2^-16, so e^d = 1 + d; ln 2 rounded to fp32 is off by 1.9e-9, times t): within 4 units of 2^-24 up to
+// x = 20, 7 beyond.  The power's instruction gives zero below 2^-126, so the last ones are taken 2^32 times as large.
+__device__ __forceinline__ float exp_neg(float x, bool* far) {
+  x = x > 104.f ? 104.f : x;              // below half the smallest fp32 number from there on
   const float t = -1.44269502f * x;
+  *far = t < -125.f;
   const float d = fmaf(t, -0.693147182f, -x);
-  const float e = __builtin_amdgcn_exp2f(t);
+  const float e = __builtin_amdgcn_exp2f(*far ? t + 32.f : t);
   return fmaf(e, d, e);
 }
 
@@ -26,11 +27,12 @@ struct Gates {
   float a, z;
 };
 __device__ __forceinline__ Gates gates(float f) {
-  const float e = exp_neg(fabsf(f));
-  const float d = 1.f + e;
+  bool far;
+  const float e = exp_neg(fabsf(f), &far);
+  const float d = 1.f + e;                // 1 where far, and so is big
   float big = __builtin_amdgcn_rcpf(d);
   big = fmaf(fmaf(-d, big, 1.f), big, big);
-  const float small = e * big;
+  const float small = e * (far ? 0x1p-32f : big);
   return f >= 0.f ? Gates{big, small} : Gates{small, big};
 }
 

@@ -1,6 +1,7 @@
 """Infinite states, inputs and gradients of the gated recurrence over long sequences: what the formula gives, step after step."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -52,3 +53,35 @@ def test_a_shut_gate_makes_nan_of_infinity(steps):
     gate[:, steps // 2] = -math.inf
     out, last, dh0 = _check(gate, x, h0, dout, dlast)
     assert out[0, :steps // 2, 64].eq(math.inf).all() and out[0, steps // 2:, 64].isnan().all() and dh0[0, 0].isnan()
+
+
+@pytest.mark.parametrize("steps", [9, 40, 300])
+def test_gates_below_the_normal_numbers_count(steps):
+    """sigmoid(-f) for f from 87.4 to 103.9 lies between 1e-38 and the smallest fp32 number: it shows beside large inputs, states and
+    gradients.  One step has such a gate for each channel, all others keep what is there."""
+    print(f"case subnormal gates {steps}", flush=True)
+    f = torch.linspace(80.0, 103.9, 70, device=DEV)
+    for sign in (1.0, -1.0):
+        gate = torch.full((1, steps, 70), math.inf, device=DEV)
+        gate[:, 5] = sign * f
+        x, dout = torch.zeros(1, steps, 70, device=DEV), torch.zeros(1, steps, 70, device=DEV)
+        h0, dlast = torch.zeros(1, 70, device=DEV), torch.full((1, 70), 1e38, device=DEV)
+        (x[:, 5] if sign > 0 else h0).fill_(1e38)
+        out, last = torch.empty_like(x), torch.empty_like(h0)
+        B.recurrence_forward(gate, x, out, h0=h0, h_last=last)
+        # the gate is rounded to a multiple of 2^-149, which acts on 1e38
+        coarse = 2.0 ** -149 * 1e38
+        ref, ref_last, off, last_off = P.recurrence(gate, x, h0)
+        P.assert_within(out, ref, off + coarse * (np.arange(steps) >= 5)[None, :, None], "out")
+        P.assert_within(last, ref_last, last_off + coarse, "last")
+        assert last.min() > 0
+        dgate, dinput, dh0 = torch.empty_like(x), torch.empty_like(x), torch.empty_like(h0)
+        B.recurrence_backward(gate, x, out, dout, dgate, dinput, h0=h0, grad_last=dlast, grad_h0=dh0)
+        ref, off = P.recurrence_gradients(gate, x, out, h0, dout, dlast)
+        P.assert_within(dinput, ref[1], off[1] + coarse, "dinput")
+        P.assert_within(dh0, ref[2], off[2] + coarse, "dh0")
+        assert (dinput[:, 5] if sign > 0 else dh0).min() > 0
+    h0 = torch.full((1, 70), math.inf, device=DEV)
+    gate[:, 5] = -f
+    B.recurrence_forward(gate, torch.zeros_like(x), out, h0=h0)
+    assert out.eq(math.inf).all()
