@@ -353,7 +353,8 @@ int32_t accordion_probe_copy(float* dst_dev, const float* src_dev, int64_t n, vo
  *  - The order of every sum is fixed: the same call gives the same bits.
  *  - Empty inputs (no tokens, rows, steps or sequences) are valid.
  *  - Nothing is launched when an argument is refused.  Errors: ACC_EINVAL, ACC_ENOSPACE (workspace),
- *    ACC_EHIP; accordion_operator_error() describes the last failure of the calling thread. */
+ *    ACC_EHIP (a launch of this call failed: nothing is enqueued behind it); accordion_operator_error()
+ *    describes the last failure of the calling thread. */
 enum { ACC_FLOAT = 0, ACC_BF16 = 1 };
 
 const char* accordion_operator_error(void);

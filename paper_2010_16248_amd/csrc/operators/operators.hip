@@ -8,6 +8,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <tuple>
 
 #include "op_common.h"
 #include "adamw.h"
@@ -73,12 +74,35 @@ int32_t check_workspace(const void* ws, size_t have, int64_t need) {
   return ACC_OK;
 }
 
-int32_t launched() {
-  return hipGetLastError() == hipSuccess ? ACC_OK : fail(ACC_EHIP, "kernel launch failed");
+// A call's launches, in order: after one that fails nothing more is enqueued, and what other calls of this thread left behind as
+// HIP's last error plays no role.
+struct Queue {
+  hipStream_t stream;
+  hipError_t status = hipSuccess;
+  explicit Queue(void* s) : stream(static_cast<hipStream_t>(s)) {}
+};
+
+template <typename... P, typename... A>
+void enqueue(Queue& q, void (*kernel)(P...), dim3 grid, dim3 block, unsigned lds, const A&... args) {
+  static_assert(sizeof...(P) == sizeof...(A), "a kernel's arguments");
+  if (q.status != hipSuccess) return;
+  std::tuple<P...> held{static_cast<P>(args)...};
+  std::apply(
+      [&](P&... each) {
+        void* at[] = {static_cast<void*>(&each)...};
+        q.status = hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, at, lds, q.stream);
+      },
+      held);
 }
 
-#define LAUNCH(kernel, grid, block, stream, ...) \
-  hipLaunchKernelGGL(kernel, grid, block, 0, static_cast<hipStream_t>(stream), __VA_ARGS__)
+int32_t launched(const Queue& q) {
+  if (q.status == hipSuccess) return ACC_OK;
+  (void)hipGetLastError();                 // it is reported here
+  std::snprintf(g_error, sizeof g_error, "kernel launch failed: %s", hipGetErrorString(q.status));
+  return ACC_EHIP;
+}
+
+#define LAUNCH(kernel, grid, block, queue, ...) enqueue(queue, kernel, grid, block, 0, __VA_ARGS__)
 
 // ---- embedding --------------------------------------------------------------------------------------
 
@@ -148,7 +172,7 @@ EmbeddingPlan plan_embedding(const acc_embedding& e) {
 constexpr int64_t kLookupMany = 4096;
 
 template <typename I, typename T, typename O>
-void lookup(const acc_embedding& e, const void* ids, const void* table, void* out, void* stream) {
+void lookup(const acc_embedding& e, const void* ids, const void* table, void* out, Queue& queue) {
   constexpr int N = sizeof(T) == 2 ? 8 : 4;
   int lanes_log2 = 3;
   // many tokens: lanes with all their requests under way; few: lanes for all columns
@@ -157,15 +181,15 @@ void lookup(const acc_embedding& e, const void* ids, const void* table, void* ou
   const int64_t across = up(e.dim, (int64_t)kLookupLoads * N << lanes_log2);
   for (int64_t t = 0; t < e.tokens; t += kRowsPerLaunch) {
     const int64_t n = std::min(kRowsPerLaunch, e.tokens - t);
-    LAUNCH((embedding_lookup_kernel<I, T, O, N>), dim3((unsigned)up(n << lanes_log2, 256), (unsigned)across), dim3(256), stream,
+    LAUNCH((embedding_lookup_kernel<I, T, O, N>), dim3((unsigned)up(n << lanes_log2, 256), (unsigned)across), dim3(256), queue,
            static_cast<const I*>(ids) + t, static_cast<const T*>(table), static_cast<O*>(out) + t * e.out_stride, n, e.vocab, e.dim,
            e.table_stride, e.out_stride, e.scale, lanes_log2);
   }
 }
 
 template <typename I, typename T>
-void lookup_to(const acc_embedding& e, const void* ids, const void* table, void* out, void* stream) {
-  e.out_type == ACC_BF16 ? lookup<I, T, bf16>(e, ids, table, out, stream) : lookup<I, T, float>(e, ids, table, out, stream);
+void lookup_to(const acc_embedding& e, const void* ids, const void* table, void* out, Queue& queue) {
+  e.out_type == ACC_BF16 ? lookup<I, T, bf16>(e, ids, table, out, queue) : lookup<I, T, float>(e, ids, table, out, queue);
 }
 
 constexpr int64_t kSumStream = 128 << 20;   // bytes of gradients that are streamed from here on (they fit no cache)
@@ -174,14 +198,14 @@ constexpr int64_t kClearRank = 40 << 20, kClearCount = 16 << 20, kClearPlace = 4
 
 template <typename T>
 void sum_runs(const acc_embedding& e, const EmbeddingPlan& p, const uint32_t* key, const uint32_t* pos, const void* grad,
-              float* table, int64_t stride, float* parts, int64_t gap_rows, void* stream) {
+              float* table, int64_t stride, float* parts, int64_t gap_rows, Queue& queue) {
   constexpr int N = 4;
   const int64_t across = up(e.dim, kWave * N), units = p.chunks * across;
   const int64_t gap_units = std::min<int64_t>(up(gap_rows, kGapRows), int64_t(1) << 20);
   const dim3 grid((unsigned)up(units + gap_units, 4));
   const bool stream_rows = e.tokens * e.dim * (int64_t)sizeof(T) > kSumStream;
 #define SUM(ACCUMULATE, EVEN, STREAM)                                                                                              \
-  LAUNCH((embedding_sum_kernel<T, N, ACCUMULATE, EVEN, STREAM>), grid, dim3(256), stream, key, pos, e.tokens, p.chunk,             \
+  LAUNCH((embedding_sum_kernel<T, N, ACCUMULATE, EVEN, STREAM>), grid, dim3(256), queue, key, pos, e.tokens, p.chunk,             \
          (uint32_t)e.vocab, static_cast<const T*>(grad), e.out_stride, table, stride, e.dim, (uint32_t)across, (uint32_t)units,    \
          e.scale, parts, gap_rows, (uint32_t)gap_units)
   if (e.dim % N != 0) {
@@ -198,13 +222,13 @@ void sum_runs(const acc_embedding& e, const EmbeddingPlan& p, const uint32_t* ke
 }
 
 template <typename I, typename T>
-void sum_few(const acc_embedding& e, const I* ids, const void* grad, float* table, int64_t stride, void* stream) {
+void sum_few(const acc_embedding& e, const I* ids, const void* grad, float* table, int64_t stride, Queue& queue) {
   constexpr int N = 4;
   const int64_t across = up(e.dim, kWave * N), units = e.tokens * across;
   const int64_t gap_units = e.accumulate ? 0 : std::min<int64_t>(up(e.vocab, kGapRows), int64_t(1) << 20);
   if (units + gap_units == 0) return;
 #define FEW(ACCUMULATE, EVEN)                                                                                                     \
-  LAUNCH((embedding_few_kernel<I, T, N, ACCUMULATE, EVEN>), dim3((unsigned)up(units + gap_units, 4)), dim3(256), stream, ids,     \
+  LAUNCH((embedding_few_kernel<I, T, N, ACCUMULATE, EVEN>), dim3((unsigned)up(units + gap_units, 4)), dim3(256), queue, ids,     \
          (int)e.tokens, e.vocab, static_cast<const T*>(grad), e.out_stride, table, stride, e.dim, (uint32_t)across,               \
          (uint32_t)units, e.scale, (uint32_t)gap_units)
   if (e.dim % N == 0) {
@@ -219,7 +243,7 @@ void sum_few(const acc_embedding& e, const I* ids, const void* grad, float* tabl
 
 template <typename I>
 void embedding_gradient(const acc_embedding& e, const EmbeddingPlan& p, const I* ids, const void* grad, float* table, char* ws,
-                        void* stream) {
+                        Queue& queue) {
   uint32_t* key[2] = {reinterpret_cast<uint32_t*>(ws + p.key[0]), reinterpret_cast<uint32_t*>(ws + p.key[1])};
   uint32_t* pos[2] = {reinterpret_cast<uint32_t*>(ws + p.pos[0]), reinterpret_cast<uint32_t*>(ws + p.pos[1])};
   uint32_t* counts = reinterpret_cast<uint32_t*>(ws + p.counts);
@@ -227,8 +251,8 @@ void embedding_gradient(const acc_embedding& e, const EmbeddingPlan& p, const I*
   const uint32_t vocab = (uint32_t)e.vocab;
   const int64_t stride = e.vocab == 1 ? e.dim : e.table_stride;
   if (p.few) {
-    if (e.out_type == ACC_BF16) sum_few<I, bf16>(e, ids, grad, table, stride, stream);
-    else sum_few<I, float>(e, ids, grad, table, stride, stream);
+    if (e.out_type == ACC_BF16) sum_few<I, bf16>(e, ids, grad, table, stride, queue);
+    else sum_few<I, float>(e, ids, grad, table, stride, queue);
     return;
   }
   // rows [0, dirty) are still to be cleared; share() takes the last ones of them off, as many as `bytes` hold
@@ -244,31 +268,30 @@ void embedding_gradient(const acc_embedding& e, const EmbeddingPlan& p, const I*
     const int rank_blocks = (int)up(e.tokens, kWave);
     const Clear clear = share(kClearRank);
     if (rank_blocks + blocks(clear) > 0)
-      hipLaunchKernelGGL((embedding_rank_kernel<I>), dim3((unsigned)(rank_blocks + blocks(clear))), dim3(kRankThreads),
-                         (unsigned)round256(4 * e.tokens), static_cast<hipStream_t>(stream), ids, (int)e.tokens, vocab, key[0], pos[0],
-                         rank_blocks, clear);
+      enqueue(queue, embedding_rank_kernel<I>, dim3((unsigned)(rank_blocks + blocks(clear))), dim3(kRankThreads),
+              (unsigned)round256(4 * e.tokens), ids, (int)e.tokens, vocab, key[0], pos[0], rank_blocks, clear);
   } else {
     for (int pass = 0; pass < p.passes; ++pass) {
       const int shift = pass * p.digit_bits, digits = 1 << p.digit_bits, to = pass & 1;
       const Clear c = share(kClearCount), d = share(kClearPlace);
       const dim3 count_grid((unsigned)(p.tiles + blocks(c))), place_grid((unsigned)(p.tiles + blocks(d)));
       if (pass == 0) {
-        LAUNCH((embedding_count_kernel<I, true>), count_grid, dim3(kSortThreads), stream, ids, nullptr, e.tokens, vocab, p.tile, shift,
+        LAUNCH((embedding_count_kernel<I, true>), count_grid, dim3(kSortThreads), queue, ids, nullptr, e.tokens, vocab, p.tile, shift,
                digits, counts, p.tiles, c);
-        LAUNCH((embedding_place_kernel<I, true>), place_grid, dim3(kSortThreads), stream, ids, nullptr, nullptr, e.tokens, vocab, p.tile,
+        LAUNCH((embedding_place_kernel<I, true>), place_grid, dim3(kSortThreads), queue, ids, nullptr, nullptr, e.tokens, vocab, p.tile,
                shift, p.digit_bits, counts, p.tiles, key[to], pos[to], d);
       } else {
-        LAUNCH((embedding_count_kernel<I, false>), count_grid, dim3(kSortThreads), stream, ids, key[at], e.tokens, vocab, p.tile, shift,
+        LAUNCH((embedding_count_kernel<I, false>), count_grid, dim3(kSortThreads), queue, ids, key[at], e.tokens, vocab, p.tile, shift,
                digits, counts, p.tiles, c);
-        LAUNCH((embedding_place_kernel<I, false>), place_grid, dim3(kSortThreads), stream, ids, key[at], pos[at], e.tokens, vocab, p.tile,
+        LAUNCH((embedding_place_kernel<I, false>), place_grid, dim3(kSortThreads), queue, ids, key[at], pos[at], e.tokens, vocab, p.tile,
                shift, p.digit_bits, counts, p.tiles, key[to], pos[to], d);
       }
       at = to;
     }
   }
-  if (e.out_type == ACC_BF16) sum_runs<bf16>(e, p, key[at], pos[at], grad, table, stride, parts, dirty, stream);
-  else sum_runs<float>(e, p, key[at], pos[at], grad, table, stride, parts, dirty, stream);
-  LAUNCH((embedding_join_kernel<4>), dim3((unsigned)p.chunks, (unsigned)up(e.dim, kWave * 4)), dim3(kWave * kJoinWaves), stream, key[at], e.tokens,
+  if (e.out_type == ACC_BF16) sum_runs<bf16>(e, p, key[at], pos[at], grad, table, stride, parts, dirty, queue);
+  else sum_runs<float>(e, p, key[at], pos[at], grad, table, stride, parts, dirty, queue);
+  LAUNCH((embedding_join_kernel<4>), dim3((unsigned)p.chunks, (unsigned)up(e.dim, kWave * 4)), dim3(kWave * kJoinWaves), queue, key[at], e.tokens,
          p.chunk, p.chunks, vocab, parts, table, stride, e.dim, e.scale, e.accumulate);
 }
 
@@ -291,11 +314,11 @@ int32_t check_layernorm(const acc_layernorm* c, bool backward) {
 
 template <typename T>
 void norm_forward(const acc_layernorm& c, const T* x, const float* w, const float* b, T* y, float* mean, float* rstd, int64_t rows,
-                  void* stream) {
+                  Queue& queue) {
   constexpr int N = sizeof(T) == 2 ? 8 : 4;
   const int64_t packs = up(c.dim, N);
 #define FORWARD(THREADS, K, BLOCK)                                                                                                \
-  LAUNCH((layernorm_forward_kernel<T, N, THREADS, K, BLOCK>), dim3((unsigned)up(rows, BLOCK / THREADS)), dim3(BLOCK), stream, x, w, \
+  LAUNCH((layernorm_forward_kernel<T, N, THREADS, K, BLOCK>), dim3((unsigned)up(rows, BLOCK / THREADS)), dim3(BLOCK), queue, x, w, \
          b, y, mean, rstd, rows, (int)c.dim, c.x_stride, c.y_stride, c.eps)
   if (packs <= 16) FORWARD(16, 1, 256);
   else if (packs <= 32) FORWARD(16, 2, 256);
@@ -307,17 +330,17 @@ void norm_forward(const acc_layernorm& c, const T* x, const float* w, const floa
   else if (packs <= 2048) FORWARD(256, 8, 256);
   else if (packs <= 4096) FORWARD(1024, 4, 1024);
   else
-    LAUNCH((layernorm_forward_long_kernel<T, N>), dim3((unsigned)rows), dim3(256), stream, x, w, b, y, mean, rstd, (int)c.dim,
+    LAUNCH((layernorm_forward_long_kernel<T, N>), dim3((unsigned)rows), dim3(256), queue, x, w, b, y, mean, rstd, (int)c.dim,
            c.x_stride, c.y_stride, c.eps);
 #undef FORWARD
 }
 
 template <typename T>
 void norm_forward_rows(const acc_layernorm& c, const void* x, const float* w, const float* b, void* y, float* mean, float* rstd,
-                       void* stream) {
+                       Queue& queue) {
   for (int64_t r = 0; r < c.rows; r += kRowsPerLaunch)
     norm_forward<T>(c, static_cast<const T*>(x) + r * c.x_stride, w, b, static_cast<T*>(y) + r * c.y_stride, mean ? mean + r : nullptr,
-                    rstd ? rstd + r : nullptr, std::min(kRowsPerLaunch, c.rows - r), stream);
+                    rstd ? rstd + r : nullptr, std::min(kRowsPerLaunch, c.rows - r), queue);
 }
 
 // Parts that the backward pass leaves (two rows of dim each): enough workgroups to fill the chip, no more than rows.  Two per
@@ -334,12 +357,12 @@ int64_t norm_parts(const acc_layernorm& c) {
 
 template <typename T>
 void norm_backward(const acc_layernorm& c, const void* dy, const void* x, const float* w, const float* mean, const float* rstd,
-                   void* dx, float* dw, float* db, float* parts, void* stream) {
+                   void* dx, float* dw, float* db, float* parts, Queue& queue) {
   constexpr int N = sizeof(T) == 2 ? 8 : 4;
   const int64_t packs = up(c.dim, N);
   const unsigned count = (unsigned)norm_parts(c);
 #define BACKWARD(THREADS, K, BLOCK)                                                                                               \
-  LAUNCH((layernorm_backward_kernel<T, N, THREADS, K, BLOCK>), dim3(count), dim3(BLOCK), stream, static_cast<const T*>(dy),      \
+  LAUNCH((layernorm_backward_kernel<T, N, THREADS, K, BLOCK>), dim3(count), dim3(BLOCK), queue, static_cast<const T*>(dy),      \
          static_cast<const T*>(x), w, mean, rstd, static_cast<T*>(dx), c.rows, (int)c.dim, c.y_stride, c.x_stride,               \
          c.grad_x_stride, parts)
   if (packs <= 16) BACKWARD(16, 1, 256);
@@ -353,14 +376,14 @@ void norm_backward(const acc_layernorm& c, const void* dy, const void* x, const 
   else if (N == 4 && packs <= 4096) BACKWARD(1024, N == 4 ? 4 : 2, 1024);
   else {
     for (int64_t r = 0; r < c.rows; r += kRowsPerLaunch)
-      LAUNCH((layernorm_backward_long_kernel<T, N>), dim3((unsigned)std::min(kRowsPerLaunch, c.rows - r)), dim3(256), stream,
+      LAUNCH((layernorm_backward_long_kernel<T, N>), dim3((unsigned)std::min(kRowsPerLaunch, c.rows - r)), dim3(256), queue,
              static_cast<const T*>(dy) + r * c.y_stride, static_cast<const T*>(x) + r * c.x_stride, w, mean + r, rstd + r,
              static_cast<T*>(dx) + r * c.grad_x_stride, (int)c.dim, c.y_stride, c.x_stride, c.grad_x_stride);
-    LAUNCH((layernorm_columns_kernel<T, N>), dim3(count, (unsigned)up(c.dim, 256 * N)), dim3(256), stream, static_cast<const T*>(dy),
+    LAUNCH((layernorm_columns_kernel<T, N>), dim3(count, (unsigned)up(c.dim, 256 * N)), dim3(256), queue, static_cast<const T*>(dy),
            static_cast<const T*>(x), mean, rstd, c.rows, (int)c.dim, c.y_stride, c.x_stride, parts);
   }
 #undef BACKWARD
-  LAUNCH(layernorm_join_kernel, dim3((unsigned)up(c.dim, kWave), 2), dim3(1024), stream, parts, (int)count, (int)c.dim, dw, db,
+  LAUNCH(layernorm_join_kernel, dim3((unsigned)up(c.dim, kWave), 2), dim3(1024), queue, parts, (int)count, (int)c.dim, dw, db,
          c.accumulate);
 }
 
@@ -453,41 +476,41 @@ RecurrencePlan plan_recurrence(const acc_recurrence& c, bool backward) {
   return p;
 }
 
-ChunkSlots chunk_slots(const RecurrencePlan& p, void* workspace, void* stream) {
+ChunkSlots chunk_slots(const RecurrencePlan& p, void* workspace, Queue& queue) {
   uint32_t* counter = static_cast<uint32_t*>(workspace);
   unsigned long long* words = reinterpret_cast<unsigned long long*>(static_cast<char*>(workspace) + 256);
   unsigned long long* const groups = words + 2 * p.slots;
   const ChunkSlots s = {words, words + p.slots, groups, groups + p.group_slots, groups + 2 * p.group_slots, counter, p.chains,
                         p.channel_blocks, p.chunks, p.groups};
-  if (p.chunks > 1) LAUNCH(recurrence_clear_kernel, dim3((unsigned)up(p.words, 256)), dim3(256), stream, words, p.words, counter);
+  if (p.chunks > 1) LAUNCH(recurrence_clear_kernel, dim3((unsigned)up(p.words, 256)), dim3(256), queue, words, p.words, counter);
   return s;
 }
 
 template <typename T, int N, int S, bool ODD, bool STREAM>
 void run_forward(const acc_recurrence& c, const RecurrencePlan& p, const void* gate, const void* input, const float* h0,
-                 const int32_t* lengths, void* out, float* h_last, void* ws, void* stream) {
+                 const int32_t* lengths, void* out, float* h_last, void* ws, Queue& queue) {
   if (p.walk) {
-    LAUNCH((recurrence_forward_walk_kernel<T, N>), dim3((unsigned)up(c.channels, 256 * N), (unsigned)c.batch), dim3(256), stream,
+    LAUNCH((recurrence_forward_walk_kernel<T, N>), dim3((unsigned)up(c.channels, 256 * N), (unsigned)c.batch), dim3(256), queue,
            shape_of(c), static_cast<const T*>(gate), static_cast<const T*>(input), h0, lengths, static_cast<T*>(out), h_last);
     return;
   }
-  const ChunkSlots slots = chunk_slots(p, ws, stream);
-  LAUNCH((recurrence_forward_chunk_kernel<T, N, S, ODD, STREAM>), dim3((unsigned)(p.chains * p.chunks)), dim3(kWave * p.waves), stream, shape_of(c),
+  const ChunkSlots slots = chunk_slots(p, ws, queue);
+  LAUNCH((recurrence_forward_chunk_kernel<T, N, S, ODD, STREAM>), dim3((unsigned)(p.chains * p.chunks)), dim3(kWave * p.waves), queue, shape_of(c),
          slots, static_cast<const T*>(gate), static_cast<const T*>(input), h0, lengths, static_cast<T*>(out), h_last);
 }
 
 template <typename T, int N, int S, bool ODD, bool STREAM>
 void run_backward(const acc_recurrence& c, const RecurrencePlan& p, const void* gate, const void* input, const void* out,
                   const float* h0, const int32_t* lengths, const void* dout, const float* dlast, void* dgate, void* dinput, float* dh0,
-                  void* ws, void* stream) {
+                  void* ws, Queue& queue) {
   if (p.walk) {
-    LAUNCH((recurrence_backward_walk_kernel<T, N>), dim3((unsigned)up(c.channels, 256 * N), (unsigned)c.batch), dim3(256), stream,
+    LAUNCH((recurrence_backward_walk_kernel<T, N>), dim3((unsigned)up(c.channels, 256 * N), (unsigned)c.batch), dim3(256), queue,
            shape_of(c), static_cast<const T*>(gate), static_cast<const T*>(input), static_cast<const T*>(out), h0, lengths,
            static_cast<const T*>(dout), dlast, static_cast<T*>(dgate), static_cast<T*>(dinput), dh0);
     return;
   }
-  const ChunkSlots slots = chunk_slots(p, ws, stream);
-  LAUNCH((recurrence_backward_chunk_kernel<T, N, S, ODD, STREAM>), dim3((unsigned)(p.chains * p.chunks)), dim3(kWave * p.waves), stream, shape_of(c),
+  const ChunkSlots slots = chunk_slots(p, ws, queue);
+  LAUNCH((recurrence_backward_chunk_kernel<T, N, S, ODD, STREAM>), dim3((unsigned)(p.chains * p.chunks)), dim3(kWave * p.waves), queue, shape_of(c),
          slots, static_cast<const T*>(gate), static_cast<const T*>(input), static_cast<const T*>(out), h0, lengths,
          static_cast<const T*>(dout), dlast, static_cast<T*>(dgate), static_cast<T*>(dinput), dh0);
 }
@@ -511,10 +534,10 @@ constexpr int64_t kAdamPiece = int64_t(1) << 33;
 int64_t state_elements(const acc_adamw& c, int64_t n) { return c.state_bits == 8 ? up(n, kAdamBlock) * kAdamBlock : n; }
 
 template <typename W, typename G>
-void adamw(const AdamArgs& a, int bits, unsigned tiles, void* stream) {
-  if (bits == 32) LAUNCH((adamw_kernel<W, G, false, false>), dim3(tiles), dim3(256), stream, a);
-  else if (a.dither_m || a.dither_v) LAUNCH((adamw_kernel<W, G, true, true>), dim3(tiles), dim3(256), stream, a);
-  else LAUNCH((adamw_kernel<W, G, true, false>), dim3(tiles), dim3(256), stream, a);
+void adamw(const AdamArgs& a, int bits, unsigned tiles, Queue& queue) {
+  if (bits == 32) LAUNCH((adamw_kernel<W, G, false, false>), dim3(tiles), dim3(256), queue, a);
+  else if (a.dither_m || a.dither_v) LAUNCH((adamw_kernel<W, G, true, true>), dim3(tiles), dim3(256), queue, a);
+  else LAUNCH((adamw_kernel<W, G, true, false>), dim3(tiles), dim3(256), queue, a);
 }
 
 }  // namespace
@@ -525,6 +548,7 @@ const char* accordion_operator_error(void) { return g_error; }
 
 int32_t accordion_embedding_forward(const acc_embedding* e, const void* ids_dev, const void* table_dev, void* out_dev,
                                     void* hip_stream) {
+  Queue queue(hip_stream);
   if (const int32_t rc = check_embedding(e)) return rc;
   if (e->tokens == 0) return ACC_OK;
   REQUIRE(ids_dev && table_dev && out_dev, "a pointer is NULL");
@@ -536,12 +560,12 @@ int32_t accordion_embedding_forward(const acc_embedding* e, const void* ids_dev,
                      {static_cast<const char*>(ids_dev), e->tokens * (e->index_bits / 8)}};
   REQUIRE(!any_overlap(s, 1, 3), "out_dev overlaps another buffer");
   if (e->index_bits == 32)
-    e->table_type == ACC_BF16 ? lookup_to<int32_t, bf16>(*e, ids_dev, table_dev, out_dev, hip_stream)
-                              : lookup_to<int32_t, float>(*e, ids_dev, table_dev, out_dev, hip_stream);
+    e->table_type == ACC_BF16 ? lookup_to<int32_t, bf16>(*e, ids_dev, table_dev, out_dev, queue)
+                              : lookup_to<int32_t, float>(*e, ids_dev, table_dev, out_dev, queue);
   else
-    e->table_type == ACC_BF16 ? lookup_to<int64_t, bf16>(*e, ids_dev, table_dev, out_dev, hip_stream)
-                              : lookup_to<int64_t, float>(*e, ids_dev, table_dev, out_dev, hip_stream);
-  return launched();
+    e->table_type == ACC_BF16 ? lookup_to<int64_t, bf16>(*e, ids_dev, table_dev, out_dev, queue)
+                              : lookup_to<int64_t, float>(*e, ids_dev, table_dev, out_dev, queue);
+  return launched(queue);
 }
 
 int32_t accordion_embedding_workspace_bytes(const acc_embedding* e, size_t* out_bytes) {
@@ -555,6 +579,7 @@ int32_t accordion_embedding_workspace_bytes(const acc_embedding* e, size_t* out_
 
 int32_t accordion_embedding_backward(const acc_embedding* e, const void* ids_dev, const void* grad_out_dev, float* grad_table_dev,
                                      void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  Queue queue(hip_stream);
   if (const int32_t rc = check_embedding(e)) return rc;
   REQUIRE(grad_table_dev, "grad_table_dev is NULL");
   REQUIRE(!off_type(grad_table_dev, 4), "a pointer is not aligned to its element type");
@@ -573,15 +598,16 @@ int32_t accordion_embedding_backward(const acc_embedding* e, const void* ids_dev
   REQUIRE(!any_overlap(s, 2, 4), "grad_table_dev or workspace_dev overlaps another buffer");
   if (e->index_bits == 32)
     embedding_gradient(*e, p, static_cast<const int32_t*>(ids_dev), grad_out_dev, grad_table_dev, static_cast<char*>(workspace_dev),
-                       hip_stream);
+                       queue);
   else
     embedding_gradient(*e, p, static_cast<const int64_t*>(ids_dev), grad_out_dev, grad_table_dev, static_cast<char*>(workspace_dev),
-                       hip_stream);
-  return launched();
+                       queue);
+  return launched(queue);
 }
 
 int32_t accordion_layernorm_forward(const acc_layernorm* c, const void* x_dev, const float* weight_dev, const float* bias_dev,
                                     void* y_dev, float* mean_dev, float* rstd_dev, void* hip_stream) {
+  Queue queue(hip_stream);
   if (const int32_t rc = check_layernorm(c, false)) return rc;
   REQUIRE((mean_dev == nullptr) == (rstd_dev == nullptr), "mean_dev and rstd_dev go together");
   if (c->rows == 0) return ACC_OK;
@@ -594,9 +620,9 @@ int32_t accordion_layernorm_forward(const acc_layernorm* c, const void* x_dev, c
                      rows_span(rstd_dev, c->rows, 1, 1, 4), rows_span(x_dev, c->rows, c->dim, c->x_stride, e),
                      rows_span(weight_dev, 1, c->dim, 0, 4), rows_span(bias_dev, 1, c->dim, 0, 4)};
   REQUIRE(!any_overlap(s, 3, 6), "a buffer that is written overlaps another one");
-  if (c->type == ACC_BF16) norm_forward_rows<bf16>(*c, x_dev, weight_dev, bias_dev, y_dev, mean_dev, rstd_dev, hip_stream);
-  else norm_forward_rows<float>(*c, x_dev, weight_dev, bias_dev, y_dev, mean_dev, rstd_dev, hip_stream);
-  return launched();
+  if (c->type == ACC_BF16) norm_forward_rows<bf16>(*c, x_dev, weight_dev, bias_dev, y_dev, mean_dev, rstd_dev, queue);
+  else norm_forward_rows<float>(*c, x_dev, weight_dev, bias_dev, y_dev, mean_dev, rstd_dev, queue);
+  return launched(queue);
 }
 
 int32_t accordion_layernorm_workspace_bytes(const acc_layernorm* c, size_t* out_bytes) {
@@ -609,6 +635,7 @@ int32_t accordion_layernorm_workspace_bytes(const acc_layernorm* c, size_t* out_
 int32_t accordion_layernorm_backward(const acc_layernorm* c, const void* grad_y_dev, const void* x_dev, const float* weight_dev,
                                      const float* mean_dev, const float* rstd_dev, void* grad_x_dev, float* grad_weight_dev,
                                      float* grad_bias_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  Queue queue(hip_stream);
   if (const int32_t rc = check_layernorm(c, true)) return rc;
   REQUIRE(weight_dev && grad_weight_dev, "a pointer is NULL");
   REQUIRE(c->rows == 0 || (grad_y_dev && x_dev && mean_dev && rstd_dev && grad_x_dev), "a pointer is NULL");
@@ -626,11 +653,11 @@ int32_t accordion_layernorm_backward(const acc_layernorm* c, const void* grad_y_
   float* parts = static_cast<float*>(workspace_dev);
   if (c->type == ACC_BF16)
     norm_backward<bf16>(*c, grad_y_dev, x_dev, weight_dev, mean_dev, rstd_dev, grad_x_dev, grad_weight_dev, grad_bias_dev, parts,
-                        hip_stream);
+                        queue);
   else
     norm_backward<float>(*c, grad_y_dev, x_dev, weight_dev, mean_dev, rstd_dev, grad_x_dev, grad_weight_dev, grad_bias_dev, parts,
-                         hip_stream);
-  return launched();
+                         queue);
+  return launched(queue);
 }
 
 int32_t accordion_recurrence_workspace_bytes(const acc_recurrence* c, size_t* out_bytes) {
@@ -645,6 +672,7 @@ int32_t accordion_recurrence_workspace_bytes(const acc_recurrence* c, size_t* ou
 int32_t accordion_recurrence_forward(const acc_recurrence* c, const void* gate_dev, const void* input_dev, const float* h0_dev,
                                      const int32_t* lengths_dev, void* out_dev, float* h_last_dev, void* workspace_dev,
                                      size_t workspace_bytes, void* hip_stream) {
+  Queue queue(hip_stream);
   if (const int32_t rc = check_recurrence(c, false)) return rc;
   if (c->batch == 0) return ACC_OK;
   REQUIRE(c->steps == 0 || (gate_dev && input_dev && out_dev), "a pointer is NULL");
@@ -666,14 +694,15 @@ int32_t accordion_recurrence_forward(const acc_recurrence* c, const void* gate_d
                    : c->channels % 2  ? run_forward<bf16, 2, 16, true, false>
                    : whole            ? run_forward<bf16, 2, 16, false, true>
                                       : run_forward<bf16, 2, 16, false, false>;
-  run(*c, p, gate_dev, input_dev, h0_dev, lengths_dev, out_dev, h_last_dev, workspace_dev, hip_stream);
-  return launched();
+  run(*c, p, gate_dev, input_dev, h0_dev, lengths_dev, out_dev, h_last_dev, workspace_dev, queue);
+  return launched(queue);
 }
 
 int32_t accordion_recurrence_backward(const acc_recurrence* c, const void* gate_dev, const void* input_dev, const void* out_dev,
                                       const float* h0_dev, const int32_t* lengths_dev, const void* grad_out_dev,
                                       const float* grad_last_dev, void* grad_gate_dev, void* grad_input_dev, float* grad_h0_dev,
                                       void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  Queue queue(hip_stream);
   if (const int32_t rc = check_recurrence(c, true)) return rc;
   if (c->batch == 0) return ACC_OK;
   REQUIRE(c->steps == 0 || (gate_dev && input_dev && out_dev && grad_out_dev && grad_gate_dev && grad_input_dev), "a pointer is NULL");
@@ -704,8 +733,8 @@ int32_t accordion_recurrence_backward(const acc_recurrence* c, const void* gate_
                    : whole            ? run_backward<bf16, 2, 8, false, true>
                                       : run_backward<bf16, 2, 8, false, false>;
   run(*c, p, gate_dev, input_dev, out_dev, h0_dev, lengths_dev, grad_out_dev, grad_last_dev, grad_gate_dev, grad_input_dev,
-                              grad_h0_dev, workspace_dev, hip_stream);
-  return launched();
+                              grad_h0_dev, workspace_dev, queue);
+  return launched(queue);
 }
 
 int32_t accordion_adamw_state_elements(const acc_adamw* c, int64_t* out_elements) {
@@ -720,6 +749,7 @@ int32_t accordion_adamw_state_elements(const acc_adamw* c, int64_t* out_elements
 int32_t accordion_adamw_step(const acc_adamw* c, void* const* weights_host_array, const void* const* grads_host_array,
                              void* const* copies_host_array, void* m_dev, void* v_dev, float* m_scale_dev, float* v_scale_dev,
                              const float* grad_scale_dev, void* hip_stream) {
+  Queue queue(hip_stream);
   if (const int32_t rc = check_adamw(c)) return rc;
   REQUIRE(std::isfinite(c->lr) && c->lr >= 0 && std::isfinite(c->eps) && c->eps >= 0, "lr and eps must be finite and not negative");
   REQUIRE(c->beta1 >= 0 && c->beta1 < 1 && c->beta2 >= 0 && c->beta2 < 1, "betas must lie in [0, 1)");
@@ -784,8 +814,8 @@ int32_t accordion_adamw_step(const acc_adamw* c, void* const* weights_host_array
   auto flush = [&]() {
     if (a.count == 0) return;
     const bool wb = c->weight_type == ACC_BF16, gb = c->grad_type == ACC_BF16;
-    if (wb) gb ? adamw<bf16, bf16>(a, c->state_bits, (unsigned)tiles, hip_stream) : adamw<bf16, float>(a, c->state_bits, (unsigned)tiles, hip_stream);
-    else gb ? adamw<float, bf16>(a, c->state_bits, (unsigned)tiles, hip_stream) : adamw<float, float>(a, c->state_bits, (unsigned)tiles, hip_stream);
+    if (wb) gb ? adamw<bf16, bf16>(a, c->state_bits, (unsigned)tiles, queue) : adamw<bf16, float>(a, c->state_bits, (unsigned)tiles, queue);
+    else gb ? adamw<float, bf16>(a, c->state_bits, (unsigned)tiles, queue) : adamw<float, float>(a, c->state_bits, (unsigned)tiles, queue);
     a.count = 0;
     tiles = 0;
   };
@@ -807,7 +837,7 @@ int32_t accordion_adamw_step(const acc_adamw* c, void* const* weights_host_array
     at += state_elements(*c, c->sizes_host[i]);
   }
   flush();
-  return launched();
+  return launched(queue);
 }
 
 }  // extern "C"
