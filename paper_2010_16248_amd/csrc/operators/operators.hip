@@ -44,19 +44,23 @@ inline bool is_type(int32_t t) { return t == ACC_FLOAT || t == ACC_BF16; }
 inline bool off_type(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)bytes != 0; }
 
 // A buffer's first byte and the bytes it spans; where its rows lie apart, the bytes of a row and a distance of which all
-// distances between rows are multiples (0: none).
+// distances between rows are multiples (0: none); where rows lie in blocks, the bytes of a block and the distance between blocks (0: none).
 struct Span {
   const char* p;
-  int64_t bytes, row = 0, every = 0;
+  int64_t bytes, row = 0, every = 0, block = 0, far = 0;
 };
 inline Span rows_span(const void* p, int64_t rows, int64_t dim, int64_t stride, int elem) {
   return {static_cast<const char*>(p), p && rows > 0 ? ((rows - 1) * stride + dim) * elem : 0, dim * elem, rows > 1 ? stride * elem : 0};
 }
+// Whether pieces of a bytes from one place on and of b bytes from `to_b` behind it, both repeated every so many bytes, are apart.
+inline bool pieces_apart(int64_t to_b, int64_t a, int64_t b, int64_t every) {
+  const int64_t at = (to_b % every + every) % every;
+  return at >= a && at <= every - b;
+}
 inline bool overlap(const Span& a, const Span& b) {
   if (!(a.bytes > 0 && b.bytes > 0 && a.p < b.p + b.bytes && b.p < a.p + a.bytes)) return false;
-  if (a.every <= 0 || a.every != b.every) return true;
-  const int64_t to_b = ((b.p - a.p) % a.every + a.every) % a.every;   // columns of one larger buffer are apart
-  return to_b < a.row || to_b > a.every - b.row;
+  if (a.every > 0 && a.every == b.every && pieces_apart(b.p - a.p, a.row, b.row, a.every)) return false;   // columns of one larger buffer
+  return !(a.far > 0 && a.far == b.far && pieces_apart(b.p - a.p, a.block, b.block, a.far));               // steps of one
 }
 // Whether one of the first `written` buffers shares memory with any other.
 bool any_overlap(const Span* s, int written, int all) {
@@ -408,10 +412,12 @@ Span steps_span(const void* p, const acc_recurrence& c, int64_t batch, int64_t s
   if (!p || c.batch == 0 || c.steps == 0) return {static_cast<const char*>(p), 0};
   if (c.batch == 1) batch = 0;
   if (c.steps == 1) step = 0;
-  const int64_t near = batch == 0 || step == 0 ? std::max(batch, step) : std::min(batch, step), far = std::max(batch, step);
+  const bool two = batch > 0 && step > 0;
+  const int64_t near = two ? std::min(batch, step) : std::max(batch, step), far = std::max(batch, step);
+  const int64_t block = ((near == step ? c.steps : c.batch) - 1) * near + c.channels;
   const int e = type_bytes(c.type);
   return {static_cast<const char*>(p), ((c.batch - 1) * batch + (c.steps - 1) * step + c.channels) * e, c.channels * e,
-          near > 0 && far % near == 0 ? near * e : 0};
+          near > 0 && far % near == 0 ? near * e : 0, block * e, two ? far * e : 0};
 }
 
 int32_t check_recurrence(const acc_recurrence* c, bool backward) {
