@@ -8,6 +8,8 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <memory>
+#include <new>
 #include <tuple>
 
 #include "op_common.h"
@@ -534,6 +536,51 @@ int32_t check_adamw(const acc_adamw* c) {
   return ACC_OK;
 }
 
+// Whether a tensor's weights or copy share memory with any tensor's weights, copy or gradients; -1: no host memory to find out.
+// Layers of flat buffers, in order, are seen to be apart in one look at each; other tensors are sorted by their place.
+int tensors_overlap(const acc_adamw& c, void* const* weights, const void* const* grads, void* const* copies) {
+  struct Piece {
+    uintptr_t from, to;
+    bool written;
+  };
+  const int64_t bytes[3] = {type_bytes(c.weight_type), 2, type_bytes(c.grad_type)};
+  auto piece = [&](int kind, int32_t i) -> Piece {
+    const void* p = kind == 0 ? weights[i] : kind == 1 ? (copies ? copies[i] : nullptr) : grads[i];
+    const uintptr_t from = reinterpret_cast<uintptr_t>(p);
+    return {from, p ? from + (uintptr_t)(c.sizes_host[i] * bytes[kind]) : from, kind < 2};
+  };
+  Piece all[3];
+  bool in_order = true;
+  for (int kind = 0; kind < 3; ++kind) {
+    all[kind] = {~(uintptr_t)0, 0, kind < 2};
+    for (int32_t i = 0; i < c.n_tensors; ++i) {
+      const Piece p = piece(kind, i);
+      if (p.from == p.to) continue;
+      in_order = in_order && (kind == 2 || p.from >= all[kind].to);
+      all[kind].from = std::min(all[kind].from, p.from);
+      all[kind].to = std::max(all[kind].to, p.to);
+    }
+  }
+  auto apart = [](const Piece& a, const Piece& b) { return a.to <= b.from || b.to <= a.from; };
+  if (in_order && apart(all[0], all[1]) && apart(all[0], all[2]) && apart(all[1], all[2])) return 0;
+  std::unique_ptr<Piece[]> pieces(new (std::nothrow) Piece[3 * (size_t)c.n_tensors]);
+  if (!pieces) return -1;
+  Piece* end = pieces.get();
+  for (int kind = 0; kind < 3; ++kind)
+    for (int32_t i = 0; i < c.n_tensors; ++i) {
+      const Piece p = piece(kind, i);
+      if (p.from != p.to) *end++ = p;
+    }
+  std::sort(pieces.get(), end, [](const Piece& a, const Piece& b) { return a.from < b.from; });
+  uintptr_t written = 0, any = 0;           // how far the pieces so far reach
+  for (const Piece* p = pieces.get(); p != end; ++p) {
+    if (p->from < (p->written ? any : written)) return 1;
+    any = std::max(any, p->to);
+    if (p->written) written = std::max(written, p->to);
+  }
+  return 0;
+}
+
 // Elements per launch at most (see kRowsPerLaunch); larger tensors go in pieces.
 constexpr int64_t kAdamPiece = int64_t(1) << 33;
 
@@ -797,6 +844,10 @@ int32_t accordion_adamw_step(const acc_adamw* c, void* const* weights_host_array
                        st[0], st[1], st[2], st[3], st[4]};
     REQUIRE(!any_overlap(t, 2, 8), "a tensor's weights or copy overlap another of its buffers or the state");
     for (int k = 0; k < 4; ++k) REQUIRE(!overlap(st[k], t[2]), "a gradient overlaps the state");
+  }
+  if (const int shared = tensors_overlap(*c, weights_host_array, grads_host_array, copies_host_array)) {
+    REQUIRE(shared < 0, "weights or copies of a tensor overlap buffers of another tensor");
+    return fail(ACC_ENOSPACE, "no host memory for the check of the tensors");
   }
   AdamArgs a;
   a.m = m_dev;

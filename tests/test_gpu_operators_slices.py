@@ -45,3 +45,28 @@ def test_steps_that_are_shared_are_refused():
     with pytest.raises(B.AccordionError) as err:
         B.recurrence_forward(gate[:2], whole[:2, :5], whole[:2, 7:11].as_strided((2, 5, 70), (770, 70, 1), 7 * 70))
     assert err.value.status == B.ACC_EINVAL
+
+
+def test_adamw_tensors_between_one_another():
+    """Weights, gradients and copies that take turns in one buffer, in any order, gradients that share memory, tensors without elements."""
+    sizes = [100, 0, 7, 256, 1, 1000]
+    gen = torch.Generator().manual_seed(1)
+    apart = [torch.randn(n, generator=gen).to(DEV) for n in sizes]
+    shared = torch.randn(1200, generator=gen).to(DEV)
+    grads = [shared[3 * i:3 * i + n] for i, n in enumerate(sizes)]
+    whole = torch.full((sum(sizes) * 3 + 64,), 4.0, device=DEV)
+    weights, own, copies, at = [None] * 6, [None] * 6, [None] * 6, 0
+    for i in (3, 0, 5, 1, 4, 2):
+        n = sizes[i]
+        copies[i] = whole[at:at + (n + 1) // 2].view(torch.bfloat16)[:n]
+        at += (n + 1) // 2
+        own[i], at = whole[at:at + n], at + n
+        weights[i], at = whole[at:at + n], at + n
+        own[i].copy_(grads[i]), weights[i].copy_(apart[i])
+    B.adamw_step(apart, grads, B.adamw_state(sizes, 32, DEV), 0.1, 1, weight_decay=0.1)
+    B.adamw_step(weights, own, B.adamw_state(sizes, 32, DEV), 0.1, 1, weight_decay=0.1, copies=copies)
+    for i in range(6):
+        assert torch.equal(weights[i], apart[i]) and torch.equal(copies[i], apart[i].bfloat16()) and torch.equal(own[i], grads[i])
+    with pytest.raises(B.AccordionError) as err:
+        B.adamw_step([apart[5], apart[5]], [grads[5], grads[5]], B.adamw_state([1000, 1000], 32, DEV), 0.1, 1)
+    assert err.value.status == B.ACC_EINVAL

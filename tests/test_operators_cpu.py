@@ -286,3 +286,21 @@ def test_sizes_beyond_a_launch_are_refused(lib):
 @pytest.mark.parametrize("dither", [-1, 2])
 def test_adamw_thresholds_are_on_or_off(lib, dither):
     refused(lib, step(lib, adamw(state_bits=8, dither=dither)), "dither")
+
+
+@pytest.mark.parametrize("case", ["a weight twice", "a weight in another's gradient", "a copy in another's weight", "a copy twice", "partly"])
+def test_adamw_tensors_must_be_apart_from_one_another(lib, case):
+    w, g, c = [at(0), at(1)], [at(2), at(3)], None
+    if case == "a weight twice":
+        w[1] = w[0]
+    elif case == "a weight in another's gradient":
+        g[0] = C.c_void_p(at(1).value + 64)
+    elif case == "a copy in another's weight":
+        c = [at(1), None]
+    elif case == "a copy twice":
+        c = [at(9), C.c_void_p(at(9).value + 8)]
+    else:
+        w[0] = C.c_void_p(at(1).value + 2396)        # the last of the second one's 600 elements
+    arr = lambda ks: None if ks is None else (C.c_void_p * 2)(*[None if k is None else k.value for k in ks])
+    cfg = adamw()
+    refused(lib, lib.accordion_adamw_step(C.byref(cfg), arr(w), arr(g), arr(c), at(4), at(5), None, None, None, None), "another tensor")
