@@ -121,3 +121,45 @@ def test_infinities_and_nan_stay_in_their_rows():
     table = torch.empty(5, 6, device=DEV)
     B.embedding_backward(ids, g, table)
     assert table[3].eq(2).all() and table[0].eq(1).all() and table[1].isinf().all() and table[2].eq(0).all() and table[4].eq(0).all()
+
+
+@pytest.mark.parametrize("tokens,dim", [(4096, 672), (5000, 333), (5000, 16), (4100, 2501), (4096, 9001)])
+@pytest.mark.parametrize("table,out", [(F32, F32), (BF, BF), (BF, F32)])
+def test_lookup_of_many_tokens(tokens, dim, table, out):
+    print(f"case lookup many {tokens} {dim} {table} {out}", flush=True)
+    gen = torch.Generator().manual_seed(tokens + dim)
+    ids = _ids(gen, tokens, 700, "outside", torch.int64)
+    tab = torch.randn(700, dim, generator=gen).to(table).to(DEV)
+    got = torch.full((tokens, dim), 7.0, dtype=out, device=DEV)
+    B.embedding_forward(ids, tab, got, 2.5)
+    known = (ids >= 0) & (ids < 700)
+    ref = (tab[ids.clamp(0, 699)].float() * 2.5 * known[:, None]).to(out)
+    assert torch.equal(got, ref)
+
+
+# gradients of more than 128 MiB, which are streamed; runs from one token to a fifth of them all
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("tokens,vocab,dim,grad", [(40001, 5000, 1024, F32), (70000, 3001, 1028, BF), (40000, 40000, 900, F32)])
+def test_gradient_of_more_than_the_caches_hold(tokens, vocab, dim, grad, accumulate):
+    print(f"case gradient streamed {tokens} {vocab} {dim} {grad} {accumulate}", flush=True)
+    gen = torch.Generator().manual_seed(tokens + dim)
+    ids = _ids(gen, tokens, vocab, "zipf", torch.int64)
+    ids[::97] = vocab + 3
+    g = (torch.randn(tokens, dim, generator=gen) * torch.exp(torch.randn(tokens, 1, generator=gen))).to(grad).to(DEV)
+    assert g.numel() * g.element_size() > 128 << 20
+    start = torch.randn(vocab, dim, generator=gen).to(DEV)
+    table = start.clone()
+    B.embedding_backward(ids, g, table, 1.7, accumulate=accumulate)
+    again = start.clone()
+    B.embedding_backward(ids, g, again, 1.7, accumulate=accumulate)
+    assert torch.equal(again, table), "the same call gave other bits"
+    # the statement of operators_plain.embedding_gradient, on the GPU
+    ok, scale = ids < vocab, float(np.float32(1.7))
+    zeros = lambda *s: torch.zeros(*s, dtype=torch.float64, device=DEV)
+    count = zeros(vocab).index_add_(0, ids[ok], torch.ones_like(ids[ok], dtype=torch.float64))
+    ref = zeros(vocab, dim).index_add_(0, ids[ok], g[ok].double()) * scale
+    bound = zeros(vocab, dim).index_add_(0, ids[ok], g[ok].double().abs()) * (count[:, None] + 2) * P.U * scale
+    if accumulate:
+        ref += start.double()
+        bound += P.U * ref.abs()
+    P.assert_within(table, P.f64(ref), P.f64(bound), "gradient")

@@ -118,3 +118,30 @@ def test_special_rows():
     dw, db = torch.full((100,), 3.0, device=DEV), torch.full((100,), 3.0, device=DEV)
     B.layernorm_backward(empty, empty, w, none, none, torch.empty_like(empty), dw, db)
     assert dw.eq(0).all() and db.eq(0).all()
+
+
+# Rows beyond what all workgroups of the backward pass have under way at once, with dense gradients, in every form of it: 16 lanes per
+# row with one and two requests each, a wave with one, two and four, a workgroup of 256, 512 and 1024, and rows beyond the registers
+TURNS = [(9000, 53), (9000, 67), (9000, 100), (4500, 201), (4500, 300), (5000, 1001), (4500, 1501), (600, 1801), (600, 2049), (600, 4100),
+         (530, 8193), (530, 16385)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("rows,dim", TURNS)
+def test_backward_where_workgroups_take_several_rows(rows, dim, dtype):
+    print(f"case layernorm turns {rows} {dim} {dtype}", flush=True)
+    gen, x, w, b = _inputs(rows, dim, dtype, 9)
+    dy = torch.randn(rows, dim, generator=gen).to(dtype).to(DEV)
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    B.layernorm_forward(x, w, b, y, mean, rstd)
+    ref_y, ref_m, ref_r, _ = P.layernorm(x, w, b, float(np.float32(1e-5)))
+    y_off, m_off, r_off = P.layernorm_bounds(x, w, b, float(np.float32(1e-5)))
+    P.assert_within(y, ref_y, y_off, "y")
+    P.assert_within(mean, ref_m, m_off, "mean")
+    P.assert_within(rstd, ref_r, r_off, "rstd")
+    dx, dw, db = torch.empty_like(x), torch.empty(dim, device=DEV), torch.empty(dim, device=DEV)
+    B.layernorm_backward(dy, x, w, mean, rstd, dx, dw, db)
+    ref, off = P.layernorm_gradients(dy, x, w, mean, rstd)
+    P.assert_within(dx, ref[0], off[0], "dx")
+    P.assert_within(dw, ref[1], off[1], "dw")
+    P.assert_within(db, ref[2], off[2], "db")

@@ -194,3 +194,38 @@ def test_gradients_against_differences():
             slope = (loss(*up) - loss(*down)) / (2 * h)
             size = float((grad.double().abs() * d.abs()).sum())
             assert abs(float((grad.double() * d).sum()) - slope) <= 1e-5 * size + 1e-7
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("batch,steps,channels", [(3, 17, 65), (4, 200, 129), (5, 1100, 33), (3, 3000, 131), (1, 1024, 64)])
+def test_the_state_in_place_over_many_steps(batch, steps, channels, dtype):
+    print(f"case in place {batch} {steps} {channels} {dtype}", flush=True)
+    gate, x, h0, _, _ = _inputs(batch, steps, channels, dtype, 4)
+    for kind in (None, "empty", "whole"):
+        lengths = _lengths(batch, steps, kind)
+        out, last = torch.empty_like(gate), torch.empty_like(h0)
+        B.recurrence_forward(gate, x, out, h0=h0, h_last=last, lengths=lengths)
+        for _ in range(3):
+            state, again = h0.clone(), torch.empty_like(gate)
+            B.recurrence_forward(gate, x, again, h0=state, h_last=state, lengths=lengths)
+            assert torch.equal(again, out) and torch.equal(state, last)
+
+
+@pytest.mark.parametrize("batch,steps,channels", [(2, 40, 129), (1, 300, 257), (2, 130, 385), (3, 9, 129)])
+def test_a_last_channel_alone_in_its_block(batch, steps, channels):
+    """bf16, two channels per lane, 128 per block: the last block has one channel."""
+    print(f"case alone {batch} {steps} {channels}", flush=True)
+    gate, x, h0, dout, dlast = _inputs(batch, steps, channels, BF, 7)
+    whole = [torch.full((batch, steps, channels + 2), 9.0, dtype=BF, device=DEV) for _ in range(3)]
+    out, dgate, dinput = (w[:, :, :channels] for w in whole)
+    last, dh0 = torch.empty_like(h0), torch.empty_like(h0)
+    B.recurrence_forward(gate, x, out, h0=h0, h_last=last)
+    ref, ref_last, off, last_off = P.recurrence(gate, x, h0)
+    P.assert_within(out, ref, off, "out")
+    P.assert_within(last, ref_last, last_off, "last")
+    B.recurrence_backward(gate, x, out, dout, dgate, dinput, h0=h0, grad_last=dlast, grad_h0=dh0)
+    ref, off = P.recurrence_gradients(gate, x, out, h0, dout, dlast)
+    for got, r, o, what in zip((dgate, dinput, dh0), ref, off, ("dgate", "dinput", "dh0")):
+        P.assert_within(got, r, o, what)
+    for w in whole:
+        assert w[:, :, channels:].eq(9).all()
