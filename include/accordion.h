@@ -361,7 +361,8 @@ const char* accordion_operator_error(void);
 
 /* Embedding lookup with scaling.
  *   forward:   out[t, :] = scale * table[id_t, :]
- *   backward:  grad_table[v, :] = scale * sum over { t : id_t = v } of grad_out[t, :]   (ascending t)
+ *   backward:  grad_table[v, :] = scale * sum over { t : id_t = v } of grad_out[t, :]
+ * The sums go by ascending t, in pieces that are then added in their order.
  * An id outside [0, vocab) gives a row of zeros and takes no part in the gradient (padding).
  * grad_table is dense fp32, as the compressors take it: rows without a token become zeros, or, with
  * accumulate, stay as they are and the sums are added (a table shared with the decoder). */
@@ -422,7 +423,7 @@ int32_t accordion_layernorm_backward(const acc_layernorm* cfg, const void* grad_
  * gradients are zeros; what their inputs hold plays no role.  A length below 0 counts as 0, one above
  * steps as steps.  steps = 1 is the serving form: one token, the state in h0 and h_last (which may be
  * the same buffer then, and for any number of steps).
- * Sequences x blocks of 64 channels (bf16: 128) x blocks of 64 steps: at most 2^22. */
+ * Sequences x blocks of 64 channels (bf16: 128) x blocks of 128 steps (bf16 backward: 64): at most 2^22. */
 typedef struct acc_recurrence {
   int64_t batch;                 /* [0, 65535] */
   int64_t steps;                 /* [0, 2^31) */

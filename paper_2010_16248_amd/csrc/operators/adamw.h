@@ -103,8 +103,9 @@ __device__ __forceinline__ uint32_t encode_block(const f4& x, float* scale, bool
   return encode4(y);
 }
 
-// One pass over weights, gradients and moments, bound by memory: 51 M parameters 32 bits 266 us (5.4 TB/s), 8 bits with bf16 gradients and
-// copy 142 (5.8), 11 M in 62 tensors 8 bits 34 (5.3).  A wave holds a block of 256 elements, four per lane, so that the largest value of
+// One pass over weights, gradients and moments, bound by memory: 51 M parameters 32 bits 264 us (5.4 TB/s), 8 bits with bf16 gradients and
+// copy 141 (5.8), 11 M in 62 tensors 8 bits 34 (5.3); weights and gradients in bf16 32 bits 201 (5.6), 8 bits 103 (5.0).  Thresholds for codes of
+// sqrt(v) 143 -> 146, of both 150 (fp32 gradients).  A wave holds a block of 256 elements, four per lane, so that the largest value of
 // an 8-bit block is a reduction inside the wave; the root and the quotient are rounded correctly, which the memory hides.
 // DITHER: some codes are dithered (a.dither_m, a.dither_v).
 template <typename W, typename G, bool BITS8, bool DITHER>

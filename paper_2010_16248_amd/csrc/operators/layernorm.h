@@ -57,7 +57,8 @@ __device__ __forceinline__ float sum_of(const F32<N>& v) {
 // ---- forward ----------------------------------------------------------------------------------------------
 // THREADS lanes hold a row in registers (K requests of N elements each): one read, one write, bound by memory; the deviations are
 // summed from the registers, after the mean.  65536 x 2048 bf16 103 us (5.2 TB/s), 4096 x 8192 bf16 24, 131072 x 64 fp32 13 (a wave per
-// row 33), 700 x 672 fp32 4.4; plain stores 107, 35.
+// row 33), 700 x 672 fp32 4.4; plain stores 107, 35.  Rows of odd length end in accesses of single elements, which the whole wave goes
+// through: 20000 x 1021 bf16 18.5 and x 1024 15.3, fp32 29.6 and 26.9.
 template <typename T, int N, int THREADS, int K, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void layernorm_forward_kernel(const T* __restrict__ x, const float* __restrict__ weight,
                                                                 const float* __restrict__ bias, T* __restrict__ y,
@@ -100,7 +101,8 @@ __global__ __launch_bounds__(BLOCK) void layernorm_forward_kernel(const T* __res
   }
 }
 
-// Rows too long for the registers of a workgroup: read three times (the second and third time from a cache).
+// Rows too long for the registers of a workgroup (beyond 16384 fp32 or 32768 bf16 columns): read three times (the second and third time
+// from a cache, as far as it holds them).  2000 x 20000 fp32 97 us for 58 at the rate of a copy, 4000 x 40000 bf16 237 for 115.
 template <typename T, int N>
 __global__ __launch_bounds__(256) void layernorm_forward_long_kernel(const T* __restrict__ x, const float* __restrict__ weight,
                                                                      const float* __restrict__ bias, T* __restrict__ y,
@@ -134,7 +136,9 @@ __global__ __launch_bounds__(256) void layernorm_forward_long_kernel(const T* __
 // A group of THREADS lanes takes every gridDim.x * groups-th row, holds it in registers (one read of x and grad_y)
 // and keeps its columns' sums of grad_y xh and grad_y over its rows in registers as well.  A workgroup adds its
 // groups' sums and leaves them in parts (two rows of dim per workgroup); layernorm_join_kernel adds the workgroups'.
-// Bound by memory: 65536 x 2048 bf16 148 us (5.4 TB/s); by the rows' latency where a wave has few: 5003 x 1001 fp32 14.3 (4.2).
+// Bound by memory: 65536 x 2048 bf16 148 us (5.4 TB/s); by the rows' latency where a wave has few: 5003 x 1001 fp32 14.2 (4.2);
+// by instructions where rows are narrow (100000 x 56 bf16 22 us for 6 at the rate of a copy) and, as forward, by the ends of odd rows (x 53 28 us;
+// 20000 x 1021 bf16 33, x 1024 27.5).  fp32 rows of 8193 to 16384 columns spill 4 registers of a lane: 2000 x 16384 78 us for 71.
 template <typename T, int N, int THREADS, int K, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void layernorm_backward_kernel(const T* __restrict__ dy, const T* __restrict__ x,
                                                                    const float* __restrict__ weight, const float* __restrict__ mean_in,
@@ -199,8 +203,9 @@ __global__ __launch_bounds__(BLOCK) void layernorm_backward_kernel(const T* __re
   }
 }
 
-// Rows too long for registers: x and grad_y are read twice (the second time from a cache), and the columns' sums
-// are formed by layernorm_columns_kernel in a pass of its own.
+// Rows too long for registers (beyond 16384 columns): x and grad_y are read twice (the second time from a cache), and the columns' sums
+// are formed by layernorm_columns_kernel in a pass of its own.  2000 x 20000 fp32 214 us for 87 at the rate of a copy, 4000 x 40000 bf16 452
+// for 173.
 template <typename T, int N>
 __global__ __launch_bounds__(256) void layernorm_backward_long_kernel(const T* __restrict__ dy, const T* __restrict__ x,
                                                                       const float* __restrict__ weight, const float* __restrict__ mean_in,

@@ -158,7 +158,8 @@ EmbeddingPlan plan_embedding(const acc_embedding& e) {
   }
   // A wave goes through a chunk's tokens one after the other, and a few through the parts of a run, of which there may be one per
   // chunk: chunks of about sqrt(n) / 12 to sqrt(n) / 6, twice that where waves abound or runs are long (us at the shorter and the longer:
-  // 86738 tokens of 62 columns 59 and 77, 20000 of 672 45 and 46, 131072 of 2048 264 and 249, 128345 of 348 in 425 rows 79 and 68).
+  // 86738 tokens of 62 columns 59 and 77, 20000 of 672 45 and 46, 131072 of 2048 264 and 249, 128345 of 348 in 425 rows 79 and 68; added to 65537 rows
+  // in fp32, 131072 tokens of 672 columns 135 and 136, 1024 174 and 175, 1280 210 and 198, 1536 245 and 229, 2048 320 and 297).
   const int64_t scale = up(e.dim, kWave * 4) >= 8 || n > 32 * e.vocab ? 64 : 128;
   p.chunk = 8;
   while (p.chunk < 128 && scale * p.chunk * p.chunk < n) p.chunk *= 2;
@@ -175,6 +176,8 @@ EmbeddingPlan plan_embedding(const acc_embedding& e) {
   return p;
 }
 
+// Lanes of a row with two requests each from here on, with one below.  us, one and two: 672 columns fp32 1024 tokens 3.0 and 3.2, 4096 4.4
+// and 3.9, 65536 40 and 37; bf16 2048 3.3 and 3.3, 4096 3.9 and 3.7, 65536 25 and 20; rows of whole waves' requests the same either way.
 constexpr int64_t kLookupMany = 4096;
 
 template <typename I, typename T, typename O>
@@ -451,7 +454,10 @@ RecurrenceShape shape_of(const acc_recurrence& c) {
           c.grad_gate_batch, c.grad_gate_step, c.grad_input_batch, c.grad_input_step, c.grad_out_batch, c.grad_out_step};
 }
 
-// Up to kWalkSteps steps a lane walks them.  More: chunks, whose number of waves follows the steps.
+// Up to kWalkSteps steps a lane walks them.  More: chunks, whose number of waves follows the steps.  us of the walk and of chunks, forward
+// and backward: fp32 20 x 672 2 steps 3.3 and 4.7, 3.5 and 6.5; 16 steps 6.3 and 3.9, 6.6 and 8.1; 24 steps 8.0 and 4.8, 8.8 and 8.2;
+// 512 x 1024 8 steps 10 and 18, 18 and 30; 16 steps 18 and 19, 34 and 40; 24 steps 25 and 27, 58 and 55; bf16 16 steps 13 and 17, 20 and 28,
+// 32 steps 23 and 23, 39 and 38; 64 x 672 bf16 16 steps 7.0 and 5.1, 9.9 and 7.8.
 constexpr int64_t kWalkSteps = 16;
 constexpr int64_t kMostChunks = int64_t(1) << 22;   // work items per launch: see kRowsPerLaunch
 

@@ -43,7 +43,8 @@ __device__ __forceinline__ int64_t steps_of(const int32_t* lengths, int64_t batc
 }
 
 // ---- a lane per N channels, step after step ---------------------------------------------------------------
-// For sequences of up to 16 steps: bound by the launch (64 x 1 x 672 fp32 3.2 us).
+// For sequences of up to 16 steps: bound by the launch (64 x 1 x 672 fp32 3.2 us) and the steps' latency (64 x 16 x 672 fp32 forward 6.4,
+// backward 7.2).
 constexpr int kWalkAhead = 8;   // steps under way
 
 template <typename T, int N>
@@ -152,9 +153,10 @@ __global__ __launch_bounds__(256) void recurrence_backward_walk_kernel(Recurrenc
 // A word of the workspace holds a value and the news that it is there at once (all ones: not yet); its accesses are
 // atomic and go past the caches that compute units do not share.
 //
-// Bound by memory with 30 (forward) and 50 (backward) vector instructions per element beside it.  us: 1 x 65536 x 672 fp32 forward 110
-// (4.8 TB/s), backward 213 (5.0); 8 x 4096 x 2048 bf16 forward 108 (3.7), backward 168 (4.8).  With sixteen waves 124, 215, 153, 198, with
-// four 370, 331, 224, 296 (before the groups); steps per wave: as many as the registers hold.
+// Bound by memory with some 35 (forward) and 55 (backward) vector instructions per element beside it.  us: 1 x 65536 x 672 fp32 forward 111
+// (4.7 TB/s), backward 217 (4.9); 8 x 4096 x 2048 bf16 forward 93 (4.3), backward 172 (4.7).  With sixteen waves 124, 215, 153, 198, with
+// four 370, 331, 224, 296 (before the groups); steps per wave: as many as the registers hold.  Of these, keeping products of open gates above
+// zero costs 1 %, gates below the normal numbers another 1 to 2.
 constexpr int kChunkWaves = 8;        // most waves of a workgroup; all of them where there are several chunks
 constexpr int kChunkGroup = 8;        // a wave for every chunk in front of the group's last one
 constexpr int kLookBack = 4;          // groups looked at in one go
