@@ -36,12 +36,13 @@ struct AdamArgs {
 // Codes to nearest follow an average only while a step moves it by about half of what lies between two codes (3 to 6 %), or while the
 // block's largest moves about by as much: sqrt(v) of random gradients, a tenth of what they were from step 2000 on, is held 1.03
 // times too large after 5000 more steps at beta2 = 0.95, but 10 times at 0.98 and 7 times at 0.999, for good; m of gradients of
-// 1 and a tenth of noise that fall to a tenth is held 1.01 times too large at beta1 = 0.9, 3.5 times at 0.95 and 9 times at 0.99.  Above these betas a code is therefore rounded up where
-// the part cut off reaches a threshold that goes through (0, 1) evenly over the steps, by the golden ratio (and over the elements, by other
-// irrational numbers): on average nothing is lost (0.98 to 1.01 times in all of these cases), with less noise than random thresholds make,
-// and the same bits for the same step.
+// 1 and a tenth of noise that fall to a tenth is held 1.01 times too large at beta1 = 0.9, 3.5 times at 0.95 and 9 times at 0.99.
+// Above these betas a code is therefore rounded up where the part cut off reaches a threshold that goes through (0, 1) evenly over the
+// steps, by the golden ratio (and over the elements, by other irrational numbers): on average nothing is lost (0.98 to 1.01 times in all of
+// these cases), with less noise than random thresholds make, and the same bits for the same step.
 constexpr double kNearestBeta1 = 0.9, kNearestBeta2 = 0.95;
-constexpr uint32_t kTurn = 0x9E3779B9u, kPhaseM = 0x6A09E667u, kPhaseV = 0xBB67AE85u;   // 2^32 times (sqrt(5) - 1) / 2, sqrt(2) - 1, sqrt(3) - 1
+// 2^32 times (sqrt(5) - 1) / 2 and the fractions of sqrt(2) and sqrt(3)
+constexpr uint32_t kTurn = 0x9E3779B9u, kPhaseM = 0x6A09E667u, kPhaseV = 0xBB67AE85u;
 
 constexpr float kTop = 448.0f;                 // largest e4m3 value
 constexpr float kLeast = 0.001953125f;         // smallest positive e4m3 value, 2^-9
@@ -80,7 +81,8 @@ __device__ __forceinline__ uint32_t wave_top(const f4& v) {
 // y cut to a code's value, or the next one where y's part beyond it and u in [0, 1) make up a spacing; NaN stays.
 __device__ __forceinline__ float dithered(float y, float u) {
   const float a = fabsf(y);
-  const uint32_t spacing = max(__float_as_uint(a) & 0x7f800000u, 0x3c800000u) - (3u << 23);   // of codes at a: 2^-9 up to 2^-6, else an eighth of a's power of two
+  // of codes at a: 2^-9 up to 2^-6, else an eighth of a's power of two
+  const uint32_t spacing = max(__float_as_uint(a) & 0x7f800000u, 0x3c800000u) - (3u << 23);
   const float r = floorf(a * __uint_as_float(0x7f000000u - spacing) + u) * __uint_as_float(spacing);
   return copysignf(r > kTop ? kTop : r, y);
 }
