@@ -335,7 +335,7 @@ const char* accordion_stage_name(int32_t stage);
 int32_t accordion_probe_copy(float* dst_dev, const float* src_dev, int64_t n, void* hip_stream);
 
 /* --- operators of a language model's training step around the compression path -----------------
- * Forward and backward pass of three layers of a recurrent language model, whose gradients the
+ * Forward and backward pass of the layers of recurrent language models and of their loss, whose gradients the
  * path compresses, and the AdamW step that consumes its averaged gradient.  They need no context.
  *
  * Conventions, besides those at the top of this file:
@@ -444,6 +444,127 @@ int32_t accordion_recurrence_backward(const acc_recurrence* cfg, const void* gat
                                       const void* grad_out_dev, const float* grad_last_dev, void* grad_gate_dev,
                                       void* grad_input_dev, float* grad_h0_dev, void* workspace_dev,
                                       size_t workspace_bytes, void* hip_stream);
+
+/* Short causal convolution of every channel along a sequence.
+ *   forward:   u_t = bias + sum_j weight[j] x_{t - width + 1 + j} (j from 0 to width - 1),
+ *              out_t = u_t, or u_t / (1 + exp(-u_t)) with silu
+ *   backward:  g_t = grad_out_t du, du = 1 or the derivative of silu at u_t (u is computed again from x),
+ *              grad_x_t = sum_j weight[j] g_{t + width - 1 - j} (+ grad_last's row, where x_t is one of last's),
+ *              grad_weight[j] = sum over sequences and t of g_t x_{t - width + 1 + j}, grad_bias = sum of g_t,
+ *              grad_state: grad_x at the steps in front of the first
+ * weight_dev is channels x width and bias_dev (NULL: none) channels, contiguous fp32, and so are their gradients.
+ * state_dev (NULL: zeros), last_dev, grad_last_dev (NULL: zeros) and grad_state_dev are batch x (width - 1) x channels,
+ * contiguous fp32: state holds the inputs in front of the first step, the latest one last, and last_dev receives the last
+ * width - 1 of state and inputs, which is the state of a call that continues the sequences (the two may be the same buffer).
+ * last_dev, grad_last_dev, grad_state_dev and grad_bias_dev may be NULL.
+ * lengths_dev as for the recurrence: out and grad_x are zeros from a sequence's length on, what x and grad_out
+ * hold there plays no role, and last is taken in front of it.  steps = 1 is the serving form. */
+typedef struct acc_convolution {
+  int64_t batch;                 /* [0, 65535] */
+  int64_t steps;                 /* [0, 2^31) */
+  int64_t channels;              /* [1, 2^23] */
+  /* elements between sequences and between steps; backward: out is grad_out */
+  int64_t x_batch, x_step, out_batch, out_step;
+  int64_t grad_x_batch, grad_x_step;           /* backward */
+  int32_t width;                 /* [1, ACC_CONVOLUTION_WIDTH] */
+  int32_t type;                  /* of x, out and their gradients */
+  int32_t silu;                  /* 0 or 1 */
+  int32_t accumulate;            /* backward: 0 or 1: grad_weight and grad_bias are added to */
+} acc_convolution;
+#define ACC_CONVOLUTION_WIDTH 8
+int32_t accordion_convolution_forward(const acc_convolution* cfg, const void* x_dev, const float* weight_dev,
+                                      const float* bias_dev, const float* state_dev, const int32_t* lengths_dev,
+                                      void* out_dev, float* last_dev, void* hip_stream);
+int32_t accordion_convolution_workspace_bytes(const acc_convolution* cfg, size_t* out_bytes);   /* backward */
+int32_t accordion_convolution_backward(const acc_convolution* cfg, const void* x_dev, const float* weight_dev,
+                                       const float* bias_dev, const float* state_dev, const int32_t* lengths_dev,
+                                       const void* grad_out_dev, const float* grad_last_dev, void* grad_x_dev,
+                                       float* grad_weight_dev, float* grad_bias_dev, float* grad_state_dev,
+                                       void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* Selective state space scan: a recurrence of `states` numbers h per channel, whose decay and input come with every step.
+ *   forward:   dt_t = log(1 + exp(delta_t + delta_bias)) with softplus, delta_t + delta_bias without,
+ *              h_t[n] = exp(dt_t a[n]) h_{t-1}[n] + dt_t b_t[n] x_t,  y_t = sum_n c_t[n] h_t[n] + d x_t,
+ *              out_t = y_t, or y_t gate_t / (1 + exp(-gate_t)) with a gate,  h_last = the last h
+ *   backward:  dy_t = grad_out_t gate_t / (1 + exp(-gate_t)) (or grad_out_t),
+ *              G_t = c_t dy_t + exp(dt_{t+1} a) G_{t+1} (the last one with grad_last), e_t = exp(dt_t a),
+ *              grad_x_t = dt_t sum_n G_t b_t + d dy_t,
+ *              grad_dt_t = sum_n (G_t e_t h_{t-1} a + G_t b_t x_t), grad_delta_t = grad_dt_t (/ (1 + exp(-(delta_t + delta_bias)))),
+ *              grad_gate_t = grad_out_t y_t times the derivative of gate / (1 + exp(-gate)),
+ *              grad_b_t = sum over the group's channels of G_t dt_t x_t, grad_c_t = sum over them of dy_t h_t,
+ *              grad_a = sum over sequences and t of G_t e_t h_{t-1} dt_t, grad_d = sum of dy_t x_t,
+ *              grad_delta_bias = sum of grad_delta_t, grad_h0 = e_0 G_0
+ *              (the states are computed again from the inputs: nothing is kept from the forward pass)
+ * a_dev is channels x states, d_dev and delta_bias_dev (NULL: zeros) channels, contiguous fp32, and so are their gradients;
+ * a is finite (negative, unless states are to grow).  b and c have a row of groups x states elements per step: channels
+ * [i channels / groups, (i + 1) channels / groups) take the i-th part of it.  gate_dev may be NULL, and grad_gate_dev then is.
+ * h0_dev (NULL: zeros), h_last_dev, grad_last_dev (NULL: zeros) and grad_h0_dev are batch x channels x states, contiguous fp32.
+ * h_last_dev, grad_h0_dev, grad_d_dev and grad_delta_bias_dev may be NULL; the last two need d_dev and delta_bias_dev.
+ * lengths_dev as for the recurrence: steps from a sequence's length on write zeros and leave the state as it is; what
+ * their inputs hold plays no role.  steps = 1 is the serving form: one token, the state in h0 and h_last (which may be the same buffer
+ * then, and for any number of steps).
+ * exp(dt a) below the normal fp32 numbers counts as zero. */
+typedef struct acc_scan {
+  int64_t batch;                 /* [0, 65535] */
+  int64_t steps;                 /* [0, 2^31); backward: up to 2^21 */
+  int64_t channels;              /* [1, 2^24], a multiple of groups */
+  /* elements between sequences and between steps; backward: out is grad_out */
+  int64_t x_batch, x_step, delta_batch, delta_step, b_batch, b_step, c_batch, c_step, gate_batch, gate_step, out_batch, out_step;
+  /* the same of the gradients (backward) */
+  int64_t grad_x_batch, grad_x_step, grad_delta_batch, grad_delta_step, grad_b_batch, grad_b_step, grad_c_batch, grad_c_step,
+      grad_gate_batch, grad_gate_step;
+  int32_t states;                /* [1, ACC_SCAN_STATES] */
+  int32_t groups;                /* >= 1 */
+  int32_t type;                  /* of x, delta, b, c, gate, out and their gradients */
+  int32_t softplus;              /* 0 or 1 */
+  int32_t accumulate;            /* backward: 0 or 1: grad_a, grad_d and grad_delta_bias are added to */
+} acc_scan;
+#define ACC_SCAN_STATES 64
+int32_t accordion_scan_workspace_bytes(const acc_scan* cfg, int32_t backward, size_t* out_bytes);
+int32_t accordion_scan_forward(const acc_scan* cfg, const void* x_dev, const void* delta_dev, const float* a_dev,
+                               const void* b_dev, const void* c_dev, const float* d_dev, const void* gate_dev,
+                               const float* delta_bias_dev, const float* h0_dev, const int32_t* lengths_dev, void* out_dev,
+                               float* h_last_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+int32_t accordion_scan_backward(const acc_scan* cfg, const void* x_dev, const void* delta_dev, const float* a_dev,
+                                const void* b_dev, const void* c_dev, const float* d_dev, const void* gate_dev,
+                                const float* delta_bias_dev, const float* h0_dev, const int32_t* lengths_dev,
+                                const void* grad_out_dev, const float* grad_last_dev, void* grad_x_dev, void* grad_delta_dev,
+                                float* grad_a_dev, void* grad_b_dev, void* grad_c_dev, float* grad_d_dev, void* grad_gate_dev,
+                                float* grad_delta_bias_dev, float* grad_h0_dev, void* workspace_dev, size_t workspace_bytes,
+                                void* hip_stream);
+
+/* Log probabilities of given tokens under rows of logits, with the rows' entropy and most probable tokens.
+ *   forward:   lse = log sum_v exp(logits[v]),  logprob = logits[target] - lse,
+ *              entropy = -sum_v p log p,  p_v = exp(logits[v] - lse),
+ *              top_ids, top_logprobs: the `top` largest logits, the largest first, of equal ones the lowest index first, and
+ *              their log probabilities
+ *   backward:  grad_logits[v] = grad_logprob ([v = target] - p_v) - grad_entropy p_v (log p_v + entropy), p from lse_dev
+ * A target outside [0, vocab) gives a log probability of zero and no gradient (padding); entropy and top are those of its logits,
+ * and without grad_entropy_dev its gradient is zero whatever its logits hold.
+ * A logit of -infinity is a token that cannot occur.  In a row of them alone lse and all log probabilities are -infinity, the entropy
+ * and, with that lse, the gradients are zero.  +infinity or NaN among a row's logits make its lse, log probabilities (of a
+ * target there is) and entropy NaN; for top_ids a NaN counts as the least, below -infinity.
+ * Forward: every pointer but logits_dev may be NULL; logprob_dev needs targets_dev, top_logprobs_dev and top_ids_dev go together and are
+ * rows x top, contiguous; lse, logprob and entropy are fp32 per row, targets and top_ids integers of index_bits.
+ * Backward: grad_entropy_dev (NULL: none) needs entropy_dev; grad_logprob_dev may be NULL (none) and targets_dev then too.  grad_logits_dev
+ * may be logits_dev (with the same stride). */
+typedef struct acc_logprob {
+  int64_t rows;                  /* [0, 2^28] */
+  int64_t vocab;                 /* [1, 2^22] */
+  int64_t logits_stride;         /* rows of logits */
+  int64_t grad_stride;           /* backward: rows of grad_logits */
+  int32_t index_bits;            /* 32 or 64 */
+  int32_t type;                  /* of logits and grad_logits */
+  int32_t top;                   /* forward: [0, min(ACC_LOGPROB_TOP, vocab)] */
+} acc_logprob;
+#define ACC_LOGPROB_TOP 64
+int32_t accordion_logprob_workspace_bytes(const acc_logprob* cfg, size_t* out_bytes);   /* forward */
+int32_t accordion_logprob_forward(const acc_logprob* cfg, const void* logits_dev, const void* targets_dev, float* logprob_dev,
+                                  float* lse_dev, float* entropy_dev, float* top_logprobs_dev, void* top_ids_dev,
+                                  void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+int32_t accordion_logprob_backward(const acc_logprob* cfg, const void* logits_dev, const void* targets_dev, const float* lse_dev,
+                                   const float* grad_logprob_dev, const float* entropy_dev, const float* grad_entropy_dev,
+                                   void* grad_logits_dev, void* hip_stream);
 
 /* One AdamW step over many tensors (for example the layers of a flat buffer and their averaged
  * gradients from accordion_decompress).  For every element, in fp32, every product and sum rounded on

@@ -60,6 +60,24 @@ class acc_recurrence(C.Structure):
                 ("type", C.c_int32)]
 
 
+class acc_convolution(C.Structure):
+    _fields_ = [(k, C.c_int64) for k in ("batch", "steps", "channels", "x_batch", "x_step", "out_batch", "out_step", "grad_x_batch",
+                                         "grad_x_step")] + \
+               [(k, C.c_int32) for k in ("width", "type", "silu", "accumulate")]
+
+
+class acc_scan(C.Structure):
+    _fields_ = [(k, C.c_int64) for k in ("batch", "steps", "channels")] + \
+               [(f"{k}_{d}", C.c_int64) for k in ("x", "delta", "b", "c", "gate", "out", "grad_x", "grad_delta", "grad_b", "grad_c",
+                                                  "grad_gate") for d in ("batch", "step")] + \
+               [(k, C.c_int32) for k in ("states", "groups", "type", "softplus", "accumulate")]
+
+
+class acc_logprob(C.Structure):
+    _fields_ = [(k, C.c_int64) for k in ("rows", "vocab", "logits_stride", "grad_stride")] + \
+               [(k, C.c_int32) for k in ("index_bits", "type", "top")]
+
+
 class acc_adamw(C.Structure):
     _fields_ = [("n_tensors", C.c_int32), ("weight_type", C.c_int32), ("grad_type", C.c_int32),
                 ("state_bits", C.c_int32), ("sizes_host", C.POINTER(C.c_int64)),
@@ -87,7 +105,9 @@ EXPORTS = [
     "accordion_operator_error", "accordion_embedding_forward", "accordion_embedding_workspace_bytes",
     "accordion_embedding_backward", "accordion_layernorm_forward", "accordion_layernorm_workspace_bytes",
     "accordion_layernorm_backward", "accordion_recurrence_workspace_bytes", "accordion_recurrence_forward",
-    "accordion_recurrence_backward", "accordion_adamw_state_elements", "accordion_adamw_step",
+    "accordion_recurrence_backward", "accordion_convolution_forward", "accordion_convolution_workspace_bytes",
+    "accordion_convolution_backward", "accordion_scan_workspace_bytes", "accordion_scan_forward", "accordion_scan_backward",
+    "accordion_logprob_workspace_bytes", "accordion_logprob_forward", "accordion_logprob_backward", "accordion_adamw_state_elements", "accordion_adamw_step",
 ]
 ACC_N_STAGES = 48     # upper bound of the stage numbers; accordion_stage_name is NULL beyond the last
 
@@ -150,6 +170,15 @@ def load_library() -> C.CDLL:
         "accordion_recurrence_workspace_bytes": [C.POINTER(acc_recurrence), C.POINTER(C.c_size_t)],
         "accordion_recurrence_forward": [C.POINTER(acc_recurrence)] + [vp] * 7 + [C.c_size_t, vp],
         "accordion_recurrence_backward": [C.POINTER(acc_recurrence)] + [vp] * 11 + [C.c_size_t, vp],
+        "accordion_convolution_forward": [C.POINTER(acc_convolution)] + [vp] * 8,
+        "accordion_convolution_workspace_bytes": [C.POINTER(acc_convolution), C.POINTER(C.c_size_t)],
+        "accordion_convolution_backward": [C.POINTER(acc_convolution)] + [vp] * 12 + [C.c_size_t, vp],
+        "accordion_scan_workspace_bytes": [C.POINTER(acc_scan), i32, C.POINTER(C.c_size_t)],
+        "accordion_scan_forward": [C.POINTER(acc_scan)] + [vp] * 13 + [C.c_size_t, vp],
+        "accordion_scan_backward": [C.POINTER(acc_scan)] + [vp] * 22 + [C.c_size_t, vp],
+        "accordion_logprob_workspace_bytes": [C.POINTER(acc_logprob), C.POINTER(C.c_size_t)],
+        "accordion_logprob_forward": [C.POINTER(acc_logprob)] + [vp] * 8 + [C.c_size_t, vp],
+        "accordion_logprob_backward": [C.POINTER(acc_logprob)] + [vp] * 8,
         "accordion_adamw_state_elements": [C.POINTER(acc_adamw), C.POINTER(i64)],
         "accordion_adamw_step": [C.POINTER(acc_adamw), C.POINTER(vp), C.POINTER(vp), C.POINTER(vp)] + [vp] * 6,
     }
@@ -431,6 +460,177 @@ def recurrence_backward(gate, input, out, grad_out, grad_gate, grad_input, h0=No
     held, ws, n = _workspace(gpu, lib.accordion_recurrence_workspace_bytes, cfg, workspace)
     _launch(gpu, lib.accordion_recurrence_backward, C.byref(cfg), gate.data_ptr(), input.data_ptr(), out.data_ptr(), first, n_steps,
             grad_out.data_ptr(), last, grad_gate.data_ptr(), grad_input.data_ptr(), dh0, ws, n)
+
+
+def _parts_of(t, name: str, shape: Tuple[int, ...], dtype) -> Tuple[int, int]:
+    """(elements between sequences, between steps) of a batch x steps x ... tensor whose steps' elements are contiguous."""
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, of shape {tuple(shape)}")
+    stride, expect = t.stride(), 1
+    for size, step in zip(reversed(shape[2:]), reversed(stride[2:])):
+        if size > 1 and step != expect:
+            raise ValueError(f"{name}: the elements of a step must be contiguous")
+        expect *= size
+    return stride[0], stride[1]
+
+
+def _convolution(x, weight, out, name: str, silu: bool, accumulate: bool, grad_x=None):
+    _need(x.dim() == 3, "x must be batch x steps x channels")
+    _need(weight.dim() == 2, "weight must be channels x width")
+    batch, steps, channels = x.shape
+    shape, width = tuple(x.shape), weight.shape[1]
+    last = (0, 0) if grad_x is None else _parts_of(grad_x, "grad_x", shape, x.dtype)
+    cfg = acc_convolution(batch, steps, channels, *_parts_of(x, "x", shape, x.dtype), *_parts_of(out, name, shape, x.dtype), *last,
+                          width, _type_of(x, "x"), silu, accumulate)
+    return cfg, (channels, width), (channels,), (batch, width - 1, channels)
+
+
+def convolution_forward(x, weight, out, bias=None, state=None, last=None, lengths=None, silu: bool = False) -> None:
+    """out_t = act(bias + sum_j weight[:, j] x_{t - width + 1 + j}) along dimension 1 of batch x steps x channels tensors, act the
+    identity or SiLU; state (batch x (width - 1) x channels, float32): the inputs in front (None: zeros); last gets those of a call that
+    continues.  steps = 1 with state and last: one token."""
+    import torch
+    lib = load_library()
+    cfg, wide, flat, ends = _convolution(x, weight, out, "out", silu, False)
+    f = torch.float32
+    w, b = _plain(weight, "weight", wide, f), _plain(bias, "bias", flat, f)
+    first, end, n_steps = _plain(state, "state", ends, f), _plain(last, "last", ends, f), _plain(lengths, "lengths", ends[:1], torch.int32)
+    _launch(_gpu_of(x, weight, out, bias, state, last, lengths), lib.accordion_convolution_forward, C.byref(cfg), x.data_ptr(), w, b, first,
+            n_steps, out.data_ptr(), end)
+
+
+def convolution_backward(x, weight, grad_out, grad_x, grad_weight, bias=None, grad_bias=None, state=None, grad_last=None, grad_state=None,
+                         lengths=None, silu: bool = False, accumulate: bool = False, workspace=None) -> None:
+    """Gradients of convolution_forward; grad_last is the gradient of last (None: zeros); accumulate adds to grad_weight and grad_bias."""
+    import torch
+    lib = load_library()
+    cfg, wide, flat, ends = _convolution(x, weight, grad_out, "grad_out", silu, accumulate, grad_x)
+    f = torch.float32
+    w, b, first = _plain(weight, "weight", wide, f), _plain(bias, "bias", flat, f), _plain(state, "state", ends, f)
+    dw, db = _plain(grad_weight, "grad_weight", wide, f), _plain(grad_bias, "grad_bias", flat, f)
+    dl, ds = _plain(grad_last, "grad_last", ends, f), _plain(grad_state, "grad_state", ends, f)
+    n_steps = _plain(lengths, "lengths", ends[:1], torch.int32)
+    gpu = _gpu_of(x, weight, grad_out, grad_x, grad_weight, bias, grad_bias, state, grad_last, grad_state, lengths)
+    held, ws, n = _workspace(gpu, lib.accordion_convolution_workspace_bytes, cfg, workspace)
+    _launch(gpu, lib.accordion_convolution_backward, C.byref(cfg), x.data_ptr(), w, b, first, n_steps, grad_out.data_ptr(), dl,
+            grad_x.data_ptr(), dw, db, ds, ws, n)
+
+
+def _scan(x, delta, a, b, c, out, name: str, gate, softplus: bool, accumulate: bool, grads=None):
+    """(config, shapes of a, of a channels' vector, of a state); grads: of x, delta, b, c and gate."""
+    _need(x.dim() == 3, "x must be batch x steps x channels")
+    _need(a.dim() == 2, "a must be channels x states")
+    _need(b.dim() in (3, 4), "b must be batch x steps x groups x states")
+    batch, steps, channels = x.shape
+    states, groups = a.shape[1], b.shape[2] if b.dim() == 4 else 1
+    shape, kind = tuple(x.shape), x.dtype
+    shared = (batch, steps, groups, states) if b.dim() == 4 else (batch, steps, states)
+    near = [*_parts_of(x, "x", shape, kind), *_parts_of(delta, "delta", shape, kind), *_parts_of(b, "b", shared, kind),
+            *_parts_of(c, "c", shared, kind), *((0, 0) if gate is None else _parts_of(gate, "gate", shape, kind)),
+            *_parts_of(out, name, shape, kind)]
+    far = [0] * 10
+    if grads is not None:
+        gx, gdelta, gb, gc, ggate = grads
+        _need((gate is None) == (ggate is None), "gate and grad_gate go together")
+        far = [*_parts_of(gx, "grad_x", shape, kind), *_parts_of(gdelta, "grad_delta", shape, kind), *_parts_of(gb, "grad_b", shared, kind),
+               *_parts_of(gc, "grad_c", shared, kind), *((0, 0) if ggate is None else _parts_of(ggate, "grad_gate", shape, kind))]
+    cfg = acc_scan(batch, steps, channels, *near, *far, states, groups, _type_of(x, "x"), softplus, accumulate)
+    return cfg, (channels, states), (channels,), (batch, channels, states)
+
+
+def _pointer(t) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def scan_forward(x, delta, a, b, c, out, d=None, gate=None, delta_bias=None, softplus: bool = False, h0=None, h_last=None, lengths=None,
+                 workspace=None) -> None:
+    """h_t = exp(dt_t a) h_{t-1} + dt_t b_t x_t, out_t = (c_t . h_t + d x_t) silu(gate_t) along dimension 1 of batch x steps x channels
+    tensors x, delta, gate and out; dt = delta + delta_bias, or its softplus; a: channels x states, b and c: batch x steps x groups x
+    states (without the third dimension: one group); h0, h_last: batch x channels x states, float32.  steps = 1 with h0 and h_last: one
+    token."""
+    import torch
+    lib = load_library()
+    cfg, wide, flat, ends = _scan(x, delta, a, b, c, out, "out", gate, softplus, False)
+    f = torch.float32
+    decay, skip, shift = _plain(a, "a", wide, f), _plain(d, "d", flat, f), _plain(delta_bias, "delta_bias", flat, f)
+    first, last, n_steps = _plain(h0, "h0", ends, f), _plain(h_last, "h_last", ends, f), _plain(lengths, "lengths", ends[:1], torch.int32)
+    gpu = _gpu_of(x, delta, a, b, c, out, d, gate, delta_bias, h0, h_last, lengths)
+    held, ws, n = _workspace(gpu, lambda cfg, n: lib.accordion_scan_workspace_bytes(cfg, 0, n), cfg, workspace)
+    _launch(gpu, lib.accordion_scan_forward, C.byref(cfg), x.data_ptr(), delta.data_ptr(), decay, b.data_ptr(), c.data_ptr(), skip,
+            _pointer(gate), shift, first, n_steps, out.data_ptr(), last, ws, n)
+
+
+def scan_backward(x, delta, a, b, c, grad_out, grad_x, grad_delta, grad_a, grad_b, grad_c, d=None, grad_d=None, gate=None, grad_gate=None,
+                  delta_bias=None, grad_delta_bias=None, softplus: bool = False, h0=None, grad_last=None, grad_h0=None, lengths=None,
+                  accumulate: bool = False, workspace=None) -> None:
+    """Gradients of scan_forward, from its inputs alone; grad_last is the gradient of h_last (None: zeros); accumulate adds to grad_a,
+    grad_d and grad_delta_bias."""
+    import torch
+    lib = load_library()
+    cfg, wide, flat, ends = _scan(x, delta, a, b, c, grad_out, "grad_out", gate, softplus, accumulate,
+                                  (grad_x, grad_delta, grad_b, grad_c, grad_gate))
+    f = torch.float32
+    decay, skip, shift = _plain(a, "a", wide, f), _plain(d, "d", flat, f), _plain(delta_bias, "delta_bias", flat, f)
+    da, dd = _plain(grad_a, "grad_a", wide, f), _plain(grad_d, "grad_d", flat, f)
+    dbias = _plain(grad_delta_bias, "grad_delta_bias", flat, f)
+    first, dl, dh = _plain(h0, "h0", ends, f), _plain(grad_last, "grad_last", ends, f), _plain(grad_h0, "grad_h0", ends, f)
+    n_steps = _plain(lengths, "lengths", ends[:1], torch.int32)
+    gpu = _gpu_of(x, delta, a, b, c, grad_out, grad_x, grad_delta, grad_a, grad_b, grad_c, d, grad_d, gate, grad_gate, delta_bias,
+                  grad_delta_bias, h0, grad_last, grad_h0, lengths)
+    held, ws, n = _workspace(gpu, lambda cfg, n: lib.accordion_scan_workspace_bytes(cfg, 1, n), cfg, workspace)
+    _launch(gpu, lib.accordion_scan_backward, C.byref(cfg), x.data_ptr(), delta.data_ptr(), decay, b.data_ptr(), c.data_ptr(), skip,
+            _pointer(gate), shift, first, n_steps, grad_out.data_ptr(), dl, grad_x.data_ptr(), grad_delta.data_ptr(), da, grad_b.data_ptr(),
+            grad_c.data_ptr(), dd, _pointer(grad_gate), dbias, dh, ws, n)
+
+
+def _logprob(logits, targets, other, rows_like):
+    """(config, index type) of rows of logits; other: a second tensor of indices, or None."""
+    import torch
+    rows, vocab, stride = _rows_of(logits, "logits")
+    index = next((t.dtype for t in (targets, other) if t is not None), torch.int64)
+    bits = _INDEX_BITS.get(index)
+    _need(bits is not None, "targets and top_ids must be int32 or int64")
+    grad_stride = 0
+    if rows_like is not None:
+        g_rows, g_vocab, grad_stride = _rows_of(rows_like, "grad_logits")
+        _need(g_rows == rows and g_vocab == vocab and rows_like.dtype == logits.dtype, "logits and grad_logits do not fit together")
+    if targets is not None:
+        _need(targets.numel() == rows and targets.is_contiguous(), "targets must be contiguous, one per row of logits")
+    return acc_logprob(rows, vocab, stride, grad_stride, bits, _type_of(logits, "logits"), 0), index
+
+
+def logprob_forward(logits, targets=None, logprob=None, lse=None, entropy=None, top_logprobs=None, top_ids=None, workspace=None) -> None:
+    """Per row of logits: logprob of the row's target (zero where that is outside the vocabulary), lse the logarithm of the sum of
+    exponentials, the entropy, and the most probable tokens' log probabilities and ids (rows x top), the largest first, of equal logits the
+    lowest id first.  What is None is not computed."""
+    import torch
+    lib = load_library()
+    cfg, index = _logprob(logits, targets, top_ids, None)
+    _need((top_logprobs is None) == (top_ids is None), "top_logprobs and top_ids go together")
+    _need(logprob is None or targets is not None, "logprob needs targets")
+    f, rows = torch.float32, (cfg.rows,)
+    if top_ids is not None:
+        _need(top_ids.dim() == 2, "top_ids must be rows x top")
+        cfg.top = top_ids.shape[1]
+    best = (cfg.rows, cfg.top)
+    lp, ls, en = _plain(logprob, "logprob", rows, f), _plain(lse, "lse", rows, f), _plain(entropy, "entropy", rows, f)
+    tv, ti = _plain(top_logprobs, "top_logprobs", best, f), _plain(top_ids, "top_ids", best, index)
+    gpu = _gpu_of(logits, targets, logprob, lse, entropy, top_logprobs, top_ids)
+    held, ws, n = _workspace(gpu, lib.accordion_logprob_workspace_bytes, cfg, workspace)
+    _launch(gpu, lib.accordion_logprob_forward, C.byref(cfg), logits.data_ptr(), _pointer(targets), lp, ls, en, tv, ti, ws, n)
+
+
+def logprob_backward(logits, targets, lse, grad_logprob, grad_logits, entropy=None, grad_entropy=None) -> None:
+    """The logits' gradient from those of logprob (may be None) and, with grad_entropy, of the entropy; lse and entropy are what the
+    forward pass wrote.  grad_logits may be logits."""
+    import torch
+    lib = load_library()
+    cfg, _ = _logprob(logits, targets, None, grad_logits)
+    f, rows = torch.float32, (cfg.rows,)
+    ls, dl = _plain(lse, "lse", rows, f), _plain(grad_logprob, "grad_logprob", rows, f)
+    en, de = _plain(entropy, "entropy", rows, f), _plain(grad_entropy, "grad_entropy", rows, f)
+    _launch(_gpu_of(logits, targets, lse, grad_logprob, grad_logits, entropy, grad_entropy), lib.accordion_logprob_backward, C.byref(cfg),
+            logits.data_ptr(), _pointer(targets), ls, dl, en, de, grad_logits.data_ptr())
 
 
 def adamw_state_elements(sizes: Sequence[int], state_bits: int = 32) -> int:

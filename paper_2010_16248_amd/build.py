@@ -5,13 +5,16 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRC = [os.path.join(HERE, "csrc", "accordion.hip"), os.path.join(HERE, "csrc", "operators", "operators.hip")]
+SRC = [os.path.join(HERE, "csrc", "accordion.hip")] + [
+    os.path.join(HERE, "csrc", "operators", f"{name}.hip") for name in ("operators", "convolution", "scan", "logprob")]
 LIB = os.path.join(HERE, "libaccordion.so")
 
 FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-ffp-contract=off", "-fhip-fp32-correctly-rounded-divide-sqrt",
     # no packed fp32 instructions: some of their forms have given wrong results on this hardware
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -27,10 +30,16 @@ def hipcc() -> str:
 
 
 def build(verbose: bool = True) -> str:
-    cmd = [hipcc()] + FLAGS + ["-o", LIB] + SRC
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    """Every source becomes an object, side by side; then they are linked."""
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True)
+
+    with tempfile.TemporaryDirectory() as where, ThreadPoolExecutor(min(len(SRC), os.cpu_count() or 1)) as pool:
+        objects = [os.path.join(where, os.path.splitext(os.path.basename(s))[0] + ".o") for s in SRC]
+        list(pool.map(run, [[hipcc()] + FLAGS + ["-c", "-o", o, s] for o, s in zip(objects, SRC)]))
+        run([hipcc()] + FLAGS + ["-shared", "-o", LIB] + objects)
     return LIB
 
 

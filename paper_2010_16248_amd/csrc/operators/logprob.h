@@ -1,0 +1,359 @@
+// Log probabilities of given tokens, entropies and most probable tokens of rows of logits; the gradient of the first two.
+#pragma once
+#include "op_common.h"
+
+namespace accop {
+
+// Running sums over some of a row's logits: the largest (at least -FLT_MAX, so that differences to it are numbers), the sum s of e^(l - top)
+// and the sum of e^(l - top) (l - top).
+struct RowSums {
+  float top, s, t;
+};
+constexpr float kLowest = -3.402823466e38f;
+constexpr float kLog2eRow = 1.44269504f;
+constexpr float kFar = -200.f;           // e^kFar is zero in fp32; keeps (l - top) e^(l - top) from being infinity times zero
+
+__device__ __forceinline__ RowSums no_sums() { return {kLowest, 0.f, 0.f}; }
+
+// The same sums with a larger top.
+__device__ __forceinline__ void raise(RowSums& r, float top) {
+  const float d = fmaxf(r.top - top, kFar), f = __builtin_amdgcn_exp2f(d * kLog2eRow);
+  r.t = f * fmaf(d, r.s, r.t);
+  r.s *= f;
+  r.top = top;
+}
+__device__ __forceinline__ RowSums joined(RowSums a, RowSums b) {
+  const float top = fmaxf(a.top, b.top);
+  raise(a, top);
+  raise(b, top);
+  return {top, a.s + b.s, a.t + b.t};
+}
+template <int N, bool ENTROPY>
+__device__ __forceinline__ void add_pack(RowSums& r, const F32<N>& l) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float d = l[i] - r.top, e = __builtin_amdgcn_exp2f(d * kLog2eRow);
+    r.s += e;
+    if (ENTROPY) r.t = fmaf(e, fmaxf(d, kFar), r.t);
+  }
+}
+template <int N>
+__device__ __forceinline__ float top_of(const F32<N>& l) {
+  float m = l[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) m = fmaxf(m, l[i]);
+  return m;
+}
+
+// Over the threads of a workgroup, the same in all of them.
+template <int THREADS>
+__device__ __forceinline__ RowSums group_sums(RowSums r, RowSums* red) {
+#pragma unroll
+  for (int k = 1; k < kWave; k *= 2) {
+    RowSums o;
+    o.top = __shfl_xor(r.top, k);
+    o.s = __shfl_xor(r.s, k);
+    o.t = __shfl_xor(r.t, k);
+    r = threadIdx.x & k ? joined(o, r) : joined(r, o);
+  }
+  constexpr int waves = THREADS / kWave;
+  if (waves == 1) return r;
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = r;
+  __syncthreads();
+  r = red[0];
+#pragma unroll
+  for (int i = 1; i < waves; ++i) r = joined(r, red[i]);
+  return r;
+}
+
+// A logit's place in the order of logits: larger logits have larger keys, a NaN the least.
+__device__ __forceinline__ unsigned key_of(float l) {
+  const unsigned u = __float_as_uint(l);
+  if (l != l) return 0;
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float logit_of(unsigned key) {
+  if (key == 0) return __uint_as_float(0x7fc00000u);
+  return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
+}
+// -0 and 0 are equal logits.
+template <typename T>
+__device__ __forceinline__ unsigned key_at(T l) { return key_of((float)l + 0.f); }
+
+struct LogprobOut {
+  const void* targets;
+  float *logprob, *lse, *entropy, *top_logprobs;
+  void* top_ids;
+  int64_t vocab, stride;
+  int top;
+  bool wide;              // ids of 64 bits
+};
+__device__ __forceinline__ int64_t id_at(const void* ids, bool wide, int64_t row) {
+  return wide ? static_cast<const int64_t*>(ids)[row] : static_cast<const int32_t*>(ids)[row];
+}
+
+// A row's results.
+__device__ __forceinline__ void write_row(const LogprobOut& o, int64_t row, RowSums r, float target_logit, bool named) {
+  const float log_s = logf(r.s);
+  if (o.lse) o.lse[row] = r.top + log_s;
+  if (o.entropy) o.entropy[row] = r.s == 0.f ? 0.f : log_s - r.t / r.s;
+  if (o.logprob) o.logprob[row] = !named ? 0.f : (r.s == 0.f ? -INFINITY : (target_logit - r.top) - log_s);
+}
+__device__ __forceinline__ void write_top(const LogprobOut& o, int64_t row, int place, RowSums r, float logit, unsigned id) {
+  o.top_logprobs[row * o.top + place] = r.s == 0.f ? -INFINITY : (logit - r.top) - logf(r.s);
+  if (o.wide) static_cast<int64_t*>(o.top_ids)[row * o.top + place] = id;
+  else static_cast<int32_t*>(o.top_ids)[row * o.top + place] = (int32_t)id;
+}
+template <typename T>
+__device__ __forceinline__ float target_of(const LogprobOut& o, const T* logits, int64_t row, bool* named) {
+  *named = false;
+  if (!o.logprob) return 0.f;
+  const int64_t id = id_at(o.targets, o.wide, row);
+  *named = id >= 0 && id < o.vocab;
+  return *named ? (float)logits[row * o.stride + id] : 0.f;
+}
+
+// ---- forward without the most probable tokens ----------------------------------------------------------------
+// A workgroup streams a part of a row; parts of a row that has several go to sums.
+template <typename T, int N, bool ENTROPY, bool PARTS>
+__global__ __launch_bounds__(256) void logprob_stream_kernel(LogprobOut o, const T* __restrict__ logits, int64_t part, int parts,
+                                                             RowSums* __restrict__ sums) {
+  constexpr int K = 4;       // requests under way
+  __shared__ RowSums red[4];
+  const int64_t row = blockIdx.x;
+  const int64_t from = blockIdx.y * part, to = min(from + part, o.vocab);
+  const T* l = logits + row * o.stride;
+  RowSums r = no_sums();
+  for (int64_t at = from + threadIdx.x * N; at < to; at += 256 * N * K) {
+    F32<N> v[K];
+    float top = r.top;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t place = at + k * 256 * N, left = to - place;
+      if (left >= N) {
+        v[k] = widen<T, N>(load<N>(l + place));
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[k][i] = i < left ? (float)l[place + i] : -INFINITY;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) top = fmaxf(top, top_of<N>(v[k]));
+    if (top > r.top) raise(r, top);
+#pragma unroll
+    for (int k = 0; k < K; ++k) add_pack<N, ENTROPY>(r, v[k]);
+  }
+  r = group_sums<256>(r, red);
+  if (threadIdx.x != 0) return;
+  if (PARTS) {
+    sums[row * parts + blockIdx.y] = r;
+  } else {
+    bool named;
+    const float t = target_of<T>(o, logits, row, &named);
+    write_row(o, row, r, t, named);
+  }
+}
+
+// ---- forward with them ------------------------------------------------------------------------------------------
+// A workgroup holds a part of a row in registers.  The part's tokens lie with 64 groups of lanes; the `top` groups with the largest maxima have a
+// least maximum, below which none of the `top` most probable tokens can be.  What is not below it, few in general, is listed in LDS
+// and ordered by counting; where it is more than the list holds, one token after the other is found among all.
+constexpr int kTopGroups = 64;
+constexpr int kTopList = 1024;
+
+__device__ __forceinline__ bool before(unsigned key, unsigned id, unsigned other_key, unsigned other_id) {
+  return key > other_key || (key == other_key && id < other_id);
+}
+
+template <typename T, int N, int K, int THREADS, bool PARTS>
+__global__ __launch_bounds__(THREADS) void logprob_top_kernel(LogprobOut o, const T* __restrict__ logits, int64_t part, int parts,
+                                                              RowSums* __restrict__ sums, uint2* __restrict__ best) {
+  __shared__ RowSums red[THREADS / kWave];
+  __shared__ unsigned group_top[kTopGroups];
+  __shared__ uint2 list[kTopList];
+  __shared__ unsigned listed;
+  __shared__ uint2 found[THREADS / kWave];
+  constexpr int each = THREADS / kTopGroups;       // lanes of a group
+  static_assert(each >= 4 && each <= 16, "groups lie within 16 lanes");
+  const int64_t row = blockIdx.x;
+  const int64_t from = blockIdx.y * part, to = min(from + part, o.vocab);
+  const T* l = logits + row * o.stride;
+  Pack<T, N> v[K];
+  float top = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int64_t place = from + (threadIdx.x + k * THREADS) * N, left = to - place;
+    if (left >= N) {
+      v[k] = load<N>(l + place);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[k][i] = i < left ? l[place + i] : (T)-INFINITY;
+    }
+  }
+  if (threadIdx.x == 0) listed = 0;
+#pragma unroll
+  for (int k = 0; k < K; ++k) top = fmaxf(top, top_of<N>(widen<T, N>(v[k])));
+  RowSums r = no_sums();
+  r.top = fmaxf(r.top, top);
+#pragma unroll
+  for (int k = 0; k < K; ++k) add_pack<N, true>(r, widen<T, N>(v[k]));
+  // the groups' maxima (of NaN and -infinity alone: the order's lowest)
+  unsigned key = top == -INFINITY ? 0u : key_of(top + 0.f);
+#pragma unroll
+  for (int m = 1; m < each; m *= 2) key = max(key, (unsigned)__shfl_xor((int)key, m));
+  if (threadIdx.x % each == 0) group_top[threadIdx.x / each] = key;
+  r = group_sums<THREADS>(r, red);                 // (its barriers are behind what is written above)
+  if (THREADS == kWave) __syncthreads();
+  const int place_of = (int)min((int64_t)o.top, to - from);     // tokens this part can give
+  // the least key that counts: the group whose place in the order is the last of `top`
+  const unsigned own = group_top[threadIdx.x & 63];
+  int rank = 0;
+  for (int i = 0; i < kTopGroups; ++i) {
+    const unsigned other = __builtin_amdgcn_readlane(own, i);
+    rank += other > own || (other == own && i < (int)(threadIdx.x & 63));
+  }
+  const unsigned long long last = __ballot(rank == o.top - 1);
+  const unsigned least = __builtin_amdgcn_readlane(own, __ffsll(last) - 1);
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int64_t place = from + (threadIdx.x + k * THREADS) * N + i;
+      const unsigned mine = key_at(v[k][i]);
+      if (mine >= least && place < to) {
+        const unsigned at = atomicAdd(&listed, 1u);
+        if (at < kTopList) list[at] = make_uint2(mine, (unsigned)place);
+      }
+    }
+  }
+  __syncthreads();
+  const unsigned count = listed;
+  auto put = [&](int place, uint2 token) {
+    if (PARTS) best[(row * parts + blockIdx.y) * o.top + place] = token;
+    else write_top(o, row, place, r, logit_of(token.x), token.y);
+  };
+  if (count <= kTopList) {
+    for (unsigned i = threadIdx.x; i < count; i += THREADS) {
+      const uint2 token = list[i];
+      int place = 0;
+      for (unsigned j = 0; j < count; ++j) place += before(list[j].x, list[j].y, token.x, token.y);
+      if (place < place_of) put(place, token);
+    }
+  } else {
+    uint2 after = make_uint2(~0u, 0u);             // in front of every token
+    bool any = false;
+    for (int place = 0; place < place_of; ++place) {
+      uint2 mine = make_uint2(0u, ~0u);            // behind every token
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int64_t id = from + (threadIdx.x + k * THREADS) * N + i;
+          const unsigned other = key_at(v[k][i]);
+          if (id < to && (!any || before(after.x, after.y, other, (unsigned)id)) && before(other, (unsigned)id, mine.x, mine.y))
+            mine = make_uint2(other, (unsigned)id);
+        }
+      }
+#pragma unroll
+      for (int m = 1; m < kWave; m *= 2) {
+        const unsigned x = __shfl_xor((int)mine.x, m), y = __shfl_xor((int)mine.y, m);
+        if (before(x, y, mine.x, mine.y)) mine = make_uint2(x, y);
+      }
+      __syncthreads();
+      if ((threadIdx.x & 63) == 0) found[threadIdx.x >> 6] = mine;
+      __syncthreads();
+      for (int w = 0; w < THREADS / kWave; ++w)
+        if (before(found[w].x, found[w].y, mine.x, mine.y)) mine = found[w];
+      if (threadIdx.x == 0) put(place, mine);
+      after = mine;
+      any = true;
+    }
+  }
+  // what a short part does not have comes behind every token
+  if (PARTS)
+    for (int place = place_of + threadIdx.x; place < o.top; place += THREADS) put(place, make_uint2(0u, ~0u));
+  if (threadIdx.x != 0) return;
+  if (PARTS) {
+    sums[row * parts + blockIdx.y] = r;
+  } else {
+    bool named;
+    const float t = target_of<T>(o, logits, row, &named);
+    write_row(o, row, r, t, named);
+  }
+}
+
+// Joins a row's parts: their sums in order, and the most probable of their most probable tokens, by counting.
+template <typename T>
+__global__ __launch_bounds__(256) void logprob_join_kernel(LogprobOut o, const T* __restrict__ logits, int parts,
+                                                           const RowSums* __restrict__ sums, const uint2* __restrict__ best) {
+  extern __shared__ uint2 tokens[];
+  __shared__ RowSums red[4];
+  const int64_t row = blockIdx.x;
+  RowSums r = no_sums();
+  for (int i = threadIdx.x; i < parts; i += 256) r = joined(r, sums[row * parts + i]);
+  const int count = parts * o.top;
+  for (int i = threadIdx.x; i < count; i += 256) tokens[i] = best[row * count + i];
+  r = group_sums<256>(r, red);
+  for (int i = threadIdx.x; i < count; i += 256) {
+    const uint2 token = tokens[i];
+    if (token.y == ~0u) continue;
+    int place = 0;
+    for (int j = 0; j < count; ++j) place += before(tokens[j].x, tokens[j].y, token.x, token.y);
+    if (place < o.top) write_top(o, row, place, r, logit_of(token.x), token.y);
+  }
+  if (threadIdx.x != 0) return;
+  bool named;
+  const float t = target_of<T>(o, logits, row, &named);
+  write_row(o, row, r, t, named);
+}
+
+// ---- backward ---------------------------------------------------------------------------------------------
+// grad may be logits: a lane writes what it has read.
+template <typename T, int N, bool ENTROPY>
+__global__ __launch_bounds__(256) void logprob_backward_kernel(const T* logits, const void* __restrict__ targets, bool wide,
+                                                               const float* __restrict__ lse_in, const float* __restrict__ dlogprob,
+                                                               const float* __restrict__ entropy_in, const float* __restrict__ dentropy,
+                                                               T* grad, int64_t vocab, int64_t stride, int64_t grad_stride, int64_t part) {
+  constexpr int K = 4;
+  const int64_t row = blockIdx.x;
+  const int64_t from = blockIdx.y * part, to = min(from + part, vocab);
+  int64_t id = -1;
+  if (dlogprob) id = id_at(targets, wide, row);
+  const bool named = id >= 0 && id < vocab;
+  const float lse = lse_in[row], g = named ? dlogprob[row] : 0.f;
+  const float entropy = ENTROPY ? entropy_in[row] : 0.f, ge = ENTROPY ? dentropy[row] : 0.f;
+  const T* l = logits + row * stride;
+  T* out = grad + row * grad_stride;
+  const bool nothing = (!ENTROPY && !named) || lse == -INFINITY;
+  for (int64_t at = from + threadIdx.x * N; at < to; at += 256 * N * K) {
+    F32<N> v[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t place = at + k * 256 * N;
+      v[k] = F32<N>{};
+      if (!nothing) v[k] = widen<T, N>(load_some<N>(l + place, to - place));
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t place = at + k * 256 * N;
+      if (place >= to) break;
+      F32<N> r = {};
+      if (!nothing) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float lp = v[k][i] - lse;
+          bool far;
+          float p = exp_neg(-lp, &far);
+          p = far ? p * 0x1p-32f : p;
+          r[i] = -g * p;
+          if (ENTROPY) r[i] -= ge * p * (fmaxf(lp, kFar) + entropy);
+          if (place + i == id) r[i] += g;
+        }
+      }
+      store_some<T, N>(out + place, r, to - place);
+    }
+  }
+}
+
+}  // namespace accop

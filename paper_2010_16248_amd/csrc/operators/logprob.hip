@@ -1,0 +1,201 @@
+// Host side of the tokens' log probabilities: argument checks, workspace layout, choice of kernels and the launches.
+#include "op_common.h"
+#include "op_host.h"
+#include "logprob.h"
+
+using namespace accop;
+
+namespace {
+
+int32_t check_logprob(const acc_logprob* c) {
+  REQUIRE(c, "config is NULL");
+  REQUIRE(c->rows >= 0 && c->rows <= (int64_t(1) << 28), "rows out of range");
+  REQUIRE(c->vocab >= 1 && c->vocab <= (int64_t(1) << 22), "vocab out of range");
+  REQUIRE(c->index_bits == 32 || c->index_bits == 64, "index_bits must be 32 or 64");
+  REQUIRE(is_type(c->type), "unknown type");
+  REQUIRE(c->top >= 0 && c->top <= ACC_LOGPROB_TOP && c->top <= c->vocab, "top out of range");
+  REQUIRE(c->rows <= 1 || (c->logits_stride >= c->vocab && c->logits_stride <= kMaxStride), "logits_stride out of range");
+  return ACC_OK;
+}
+
+struct LogprobPlan {
+  int packs = 0, threads = 256;         // with the most probable tokens: packs of a lane
+  int64_t part = 0, parts = 1;
+  int64_t sums = 0, best = 0, bytes = 0;
+};
+
+constexpr int64_t kLogprobGroups = 1024;      // workgroups that fill the chip
+constexpr int64_t kStreamPart = 8192;         // elements of a part at least
+
+LogprobPlan plan_logprob(const acc_logprob& c) {
+  LogprobPlan p;
+  const int64_t n = c.type == ACC_BF16 ? 8 : 4;
+  if (c.top > 0) {
+    // parts that 256 lanes or, where there are rows enough, 1024 hold
+    const int64_t small = 256 * 32;
+    if (c.vocab <= 256 * n) p.packs = 1;
+    else if (c.vocab <= 256 * 8) p.packs = (int)(8 / n);
+    else p.packs = (int)(32 / n);
+    p.part = 256 * n * p.packs;
+    if (c.vocab > small && c.rows * up(c.vocab, small) > kLogprobGroups) {
+      p.threads = 1024;
+      p.part = 1024 * n * p.packs;
+    }
+    if (up(c.vocab, p.part) > 32 && p.threads == 256) {
+      p.threads = 1024;
+      p.part = 1024 * n * p.packs;
+    }
+  } else {
+    p.part = c.vocab;
+    if (c.rows < kLogprobGroups) p.part = std::max(kStreamPart, up(c.vocab, up(kLogprobGroups, std::max<int64_t>(1, c.rows))));
+    p.part = up(p.part, 64) * 64;
+  }
+  p.parts = up(c.vocab, p.part);
+  if (p.parts == 1) return p;
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) { const int64_t o = at; at += round256(bytes); return o; };
+  p.sums = take(sizeof(RowSums) * c.rows * p.parts);
+  p.best = take(8 * c.rows * p.parts * c.top);
+  p.bytes = at;
+  return p;
+}
+
+template <typename T, int N, int K, int THREADS>
+void top_rows(const LogprobPlan& p, const LogprobOut& o, const T* logits, int64_t rows, RowSums* sums, uint2* best, Queue& queue) {
+  const dim3 grid((unsigned)rows, (unsigned)p.parts);
+  if (p.parts > 1) LAUNCH((logprob_top_kernel<T, N, K, THREADS, true>), grid, dim3(THREADS), queue, o, logits, p.part, (int)p.parts, sums, best);
+  else LAUNCH((logprob_top_kernel<T, N, K, THREADS, false>), grid, dim3(THREADS), queue, o, logits, p.part, 1, sums, best);
+}
+
+template <typename T>
+void forward(const acc_logprob& c, const LogprobPlan& p, const LogprobOut& all, const T* logits, char* ws, Queue& queue) {
+  constexpr int N = sizeof(T) == 2 ? 8 : 4;
+  for (int64_t r = 0; r < c.rows; r += kRowsPerLaunch) {
+    const int64_t rows = std::min(kRowsPerLaunch, c.rows - r);
+    LogprobOut o = all;
+    if (o.targets) o.targets = static_cast<const char*>(o.targets) + r * (c.index_bits / 8);
+    if (o.logprob) o.logprob += r;
+    if (o.lse) o.lse += r;
+    if (o.entropy) o.entropy += r;
+    if (o.top_logprobs) o.top_logprobs += r * c.top;
+    if (o.top_ids) o.top_ids = static_cast<char*>(o.top_ids) + r * c.top * (c.index_bits / 8);
+    RowSums* const sums = reinterpret_cast<RowSums*>(ws + p.sums) + (p.parts > 1 ? r * p.parts : 0);
+    uint2* const best = reinterpret_cast<uint2*>(ws + p.best) + (p.parts > 1 ? r * p.parts * c.top : 0);
+    const T* const from = logits + r * c.logits_stride;
+    if (c.top > 0) {
+      if (p.threads == 1024) top_rows<T, N, 32 / N, 1024>(p, o, from, rows, sums, best, queue);
+      else if (p.packs == 1) top_rows<T, N, 1, 256>(p, o, from, rows, sums, best, queue);
+      else if (p.packs == 8 / N) top_rows<T, N, 8 / N, 256>(p, o, from, rows, sums, best, queue);
+      else top_rows<T, N, 32 / N, 256>(p, o, from, rows, sums, best, queue);
+    } else {
+      const dim3 grid((unsigned)rows, (unsigned)p.parts);
+#define STREAM(ENTROPY, PARTS) \
+  LAUNCH((logprob_stream_kernel<T, N, ENTROPY, PARTS>), grid, dim3(256), queue, o, from, p.part, (int)p.parts, sums)
+      if (o.entropy) {
+        if (p.parts > 1) STREAM(true, true);
+        else STREAM(true, false);
+      } else {
+        if (p.parts > 1) STREAM(false, true);
+        else STREAM(false, false);
+      }
+#undef STREAM
+    }
+    if (p.parts > 1)
+      enqueue(queue, logprob_join_kernel<T>, dim3((unsigned)rows), dim3(256), (unsigned)(8 * p.parts * c.top), o, from, (int)p.parts, sums, best);
+  }
+}
+
+template <typename T>
+void backward(const acc_logprob& c, const T* logits, const void* targets, const float* lse, const float* dlogprob, const float* entropy,
+              const float* dentropy, T* grad, Queue& queue) {
+  constexpr int N = sizeof(T) == 2 ? 8 : 4;
+  constexpr int64_t turn = 256 * N * 4;
+  int64_t part = up(c.vocab, turn) * turn;
+  while (part > turn && c.rows * up(c.vocab, part) < 2048) part = up(part / 2, turn) * turn;
+  for (int64_t r = 0; r < c.rows; r += kRowsPerLaunch) {
+    const dim3 grid((unsigned)std::min(kRowsPerLaunch, c.rows - r), (unsigned)up(c.vocab, part));
+    const T* const from = logits + r * c.logits_stride;
+    const void* const ids = dlogprob ? static_cast<const char*>(targets) + r * (c.index_bits / 8) : nullptr;
+    T* const to = grad + r * c.grad_stride;
+    if (dentropy)
+      LAUNCH((logprob_backward_kernel<T, N, true>), grid, dim3(256), queue, from, ids, c.index_bits == 64, lse + r, dlogprob ? dlogprob + r : nullptr,
+             entropy + r, dentropy + r, to, c.vocab, c.logits_stride, c.grad_stride, part);
+    else
+      LAUNCH((logprob_backward_kernel<T, N, false>), grid, dim3(256), queue, from, ids, c.index_bits == 64, lse + r, dlogprob ? dlogprob + r : nullptr,
+             nullptr, nullptr, to, c.vocab, c.logits_stride, c.grad_stride, part);
+  }
+}
+
+Span bytes_span(const void* p, int64_t bytes) { return {static_cast<const char*>(p), p ? bytes : 0}; }
+
+}  // namespace
+
+extern "C" {
+
+int32_t accordion_logprob_workspace_bytes(const acc_logprob* c, size_t* out_bytes) {
+  REQUIRE(out_bytes, "out_bytes is NULL");
+  if (const int32_t rc = check_logprob(c)) return rc;
+  *out_bytes = (size_t)plan_logprob(*c).bytes;
+  return ACC_OK;
+}
+
+int32_t accordion_logprob_forward(const acc_logprob* c, const void* logits_dev, const void* targets_dev, float* logprob_dev,
+                                  float* lse_dev, float* entropy_dev, float* top_logprobs_dev, void* top_ids_dev, void* workspace_dev,
+                                  size_t workspace_bytes, void* hip_stream) {
+  Queue queue(hip_stream);
+  if (const int32_t rc = check_logprob(c)) return rc;
+  if (c->rows == 0) return ACC_OK;
+  REQUIRE(logits_dev, "logits_dev is NULL");
+  REQUIRE(!logprob_dev || targets_dev, "logprob_dev needs targets_dev");
+  REQUIRE(c->top == 0 || (top_logprobs_dev && top_ids_dev), "top_logprobs_dev or top_ids_dev is NULL");
+  const int e = type_bytes(c->type), i = c->index_bits / 8;
+  REQUIRE(!off_type(logits_dev, e) && !off_type(targets_dev, i) && !off_type(logprob_dev, 4) && !off_type(lse_dev, 4) &&
+              !off_type(entropy_dev, 4) && !off_type(top_logprobs_dev, 4) && !off_type(top_ids_dev, i),
+          "a pointer is not aligned to its element type");
+  const LogprobPlan p = plan_logprob(*c);
+  if (const int32_t rc = check_workspace(workspace_dev, workspace_bytes, p.bytes)) return rc;
+  const Span s[8] = {bytes_span(workspace_dev, p.bytes), bytes_span(logprob_dev, 4 * c->rows), bytes_span(lse_dev, 4 * c->rows),
+                     bytes_span(entropy_dev, 4 * c->rows), bytes_span(top_logprobs_dev, 4 * c->rows * c->top),
+                     bytes_span(top_ids_dev, i * c->rows * c->top), rows_span(logits_dev, c->rows, c->vocab, c->logits_stride, e),
+                     bytes_span(targets_dev, i * c->rows)};
+  REQUIRE(!any_overlap(s, 6, 8), "a buffer that is written overlaps another one");
+  const LogprobOut o = {targets_dev, logprob_dev, lse_dev, entropy_dev, top_logprobs_dev, top_ids_dev, c->vocab, c->logits_stride, c->top, c->index_bits == 64};
+  char* const ws = static_cast<char*>(workspace_dev);
+  if (c->type == ACC_BF16) forward(*c, p, o, static_cast<const bf16*>(logits_dev), ws, queue);
+  else forward(*c, p, o, static_cast<const float*>(logits_dev), ws, queue);
+  return launched(queue);
+}
+
+int32_t accordion_logprob_backward(const acc_logprob* c, const void* logits_dev, const void* targets_dev, const float* lse_dev,
+                                   const float* grad_logprob_dev, const float* entropy_dev, const float* grad_entropy_dev,
+                                   void* grad_logits_dev, void* hip_stream) {
+  Queue queue(hip_stream);
+  if (const int32_t rc = check_logprob(c)) return rc;
+  REQUIRE(c->rows <= 1 || (c->grad_stride >= c->vocab && c->grad_stride <= kMaxStride), "grad_stride out of range");
+  if (c->rows == 0) return ACC_OK;
+  REQUIRE(logits_dev && lse_dev && grad_logits_dev, "a pointer is NULL");
+  REQUIRE(!grad_logprob_dev || targets_dev, "grad_logprob_dev needs targets_dev");
+  REQUIRE(!grad_entropy_dev || entropy_dev, "grad_entropy_dev needs entropy_dev");
+  const int e = type_bytes(c->type), i = c->index_bits / 8;
+  REQUIRE(!off_type(logits_dev, e) && !off_type(targets_dev, i) && !off_type(lse_dev, 4) && !off_type(grad_logprob_dev, 4) &&
+              !off_type(entropy_dev, 4) && !off_type(grad_entropy_dev, 4) && !off_type(grad_logits_dev, e),
+          "a pointer is not aligned to its element type");
+  const bool in_place = grad_logits_dev == logits_dev && (c->rows <= 1 || c->grad_stride == c->logits_stride);
+  const Span s[7] = {rows_span(grad_logits_dev, c->rows, c->vocab, c->grad_stride, e),
+                     rows_span(in_place ? nullptr : logits_dev, c->rows, c->vocab, c->logits_stride, e),
+                     bytes_span(targets_dev, i * c->rows),
+                     bytes_span(lse_dev, 4 * c->rows),
+                     bytes_span(grad_logprob_dev, 4 * c->rows),
+                     bytes_span(entropy_dev, 4 * c->rows),
+                     bytes_span(grad_entropy_dev, 4 * c->rows)};
+  REQUIRE(!any_overlap(s, 1, 7), "grad_logits_dev overlaps another buffer");
+  if (c->type == ACC_BF16)
+    backward(*c, static_cast<const bf16*>(logits_dev), targets_dev, lse_dev, grad_logprob_dev, entropy_dev, grad_entropy_dev,
+             static_cast<bf16*>(grad_logits_dev), queue);
+  else
+    backward(*c, static_cast<const float*>(logits_dev), targets_dev, lse_dev, grad_logprob_dev, entropy_dev, grad_entropy_dev,
+             static_cast<float*>(grad_logits_dev), queue);
+  return launched(queue);
+}
+
+}  // extern "C"

@@ -10,38 +10,6 @@ struct RecurrenceShape {
   int64_t dgate_b, dgate_t, dinput_b, dinput_t, dout_b, dout_t;
 };
 
-// e^-x for x >= 0 (NaN for NaN), times 2^32 where `far`: 2^t of the rounded t = -x log2(e), times e^d with d = -x - t ln 2, what the
-// rounding lost (d is below 2^-16, so e^d = 1 + d; ln 2 rounded to fp32 is off by 1.9e-9, times t): within 4 units of 2^-24 up to
-// x = 20, 7 beyond.  The power's instruction gives zero below 2^-126, so the last ones are taken 2^32 times as large.
-__device__ __forceinline__ float exp_neg(float x, bool* far) {
-  x = x > 104.f ? 104.f : x;              // below half the smallest fp32 number from there on
-  const float t = -1.44269502f * x;
-  *far = t < -125.f;
-  const float d = fmaf(t, -0.693147182f, -x);
-  const float e = __builtin_amdgcn_exp2f(*far ? t + 32.f : t);
-  return fmaf(e, d, e);
-}
-
-// sigmoid(f) and sigmoid(-f).  Neither is a difference from one: a gate near one keeps all digits of 1 - a.
-struct Gates {
-  float a, z;
-};
-__device__ __forceinline__ Gates gates(float f) {
-  bool far;
-  const float e = exp_neg(fabsf(f), &far);
-  const float d = 1.f + e;                // 1 where far, and so is big
-  float big = __builtin_amdgcn_rcpf(d);
-  big = fmaf(fmaf(-d, big, 1.f), big, big);
-  const float small = e * (far ? 0x1p-32f : big);
-  return f >= 0.f ? Gates{big, small} : Gates{small, big};
-}
-
-__device__ __forceinline__ int64_t steps_of(const int32_t* lengths, int64_t batch, int64_t steps) {
-  if (!lengths) return steps;
-  const int64_t n = lengths[batch];
-  return n < 0 ? 0 : (n < steps ? n : steps);
-}
-
 // ---- a lane per N channels, step after step ---------------------------------------------------------------
 // For sequences of up to 16 steps: bound by the launch (64 x 1 x 672 fp32 3.2 us) and the steps' latency (64 x 16 x 672 fp32 forward 6.4,
 // backward 7.2).

@@ -1,0 +1,712 @@
+// Selective state space scan h_t = exp(dt_t a) h_{t-1} + dt_t b_t x_t, y_t = c_t . h_t + d x_t: forward and backward pass.
+#pragma once
+#include "op_common.h"
+
+namespace accop {
+
+struct ScanShape {
+  int64_t steps, channels;
+  int64_t x_b, x_t, delta_b, delta_t, gate_b, gate_t, out_b, out_t;                  // backward: out is grad_out
+  int64_t dx_b, dx_t, ddelta_b, ddelta_t, dgate_b, dgate_t;
+  int64_t chunk, rows;      // steps of a chunk; rows of a sequence's b and c
+  int chunks;
+  int states, padded;       // states of a channel, and as many as are held of them
+  int groups, group, blocks;// groups, channels of one, blocks of 64 channels of one
+  int softplus;
+};
+
+// Constant memory: loads at an address that a wave has in common go to its scalar registers.
+typedef const float __attribute__((address_space(4))) * Shared;
+__device__ __forceinline__ Shared shared_at(const float* p) { return (Shared)(uintptr_t)p; }
+
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+
+// log(1 + e^r) = max(r, 0) + log(1 + e), e = e^-|r|; log(1 + e) = 2 atanh(s), s = e / (2 + e) <= 1/3, by its series up to s^15 (the next
+// term is below 2^-29 of the sum).
+__device__ __forceinline__ float softplus(float r) {
+  bool far;
+  float e = exp_neg(fabsf(r), &far);
+  e = far ? e * 0x1p-32f : e;
+  const float d = 2.f + e;
+  float q = __builtin_amdgcn_rcpf(d);
+  q = fmaf(fmaf(-d, q, 1.f), q, q);
+  const float s = e * q, z = s * s;
+  float p = 2.f / 15.f;
+  p = fmaf(p, z, 2.f / 13.f);
+  p = fmaf(p, z, 2.f / 11.f);
+  p = fmaf(p, z, 2.f / 9.f);
+  p = fmaf(p, z, 2.f / 7.f);
+  p = fmaf(p, z, 2.f / 5.f);
+  p = fmaf(p, z, 2.f / 3.f);
+  return fmaxf(r, 0.f) + fmaf(p * z, s, 2.f * s);
+}
+
+// ---- b and c as the scan reads them -----------------------------------------------------------------------
+// [batch, group, step]: the states' b, then their c, in fp32, both filled up with zeros; zeros from the sequence's length on, up to whole turns
+// of kScanAhead steps.
+constexpr int kScanAhead = 8;    // steps of a turn: under way together
+
+template <typename T>
+__global__ __launch_bounds__(256) void scan_pack_kernel(const T* __restrict__ b, const T* __restrict__ c, int64_t b_b, int64_t b_t,
+                                                        int64_t c_b, int64_t c_t, int64_t all, int64_t steps, int64_t rows, int groups,
+                                                        int states, int padded, const int32_t* __restrict__ lengths,
+                                                        float* __restrict__ to) {
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / (2 * padded);
+  if (row >= all) return;
+  const int k = (int)(at - row * 2 * padded), n = k < padded ? k : k - padded;
+  const int64_t t = row % rows, g = row / rows % groups, batch = row / rows / groups;
+  float v = 0.f;
+  if (n < states && t < steps_of(lengths, batch, steps))
+    v = k < padded ? (float)b[batch * b_b + t * b_t + g * states + n] : (float)c[batch * c_b + t * c_t + g * states + n];
+  to[at] = v;
+}
+
+// ---- what the passes share --------------------------------------------------------------------------------
+// A lane has one channel and NP of its states; a wave 64 channels of a group.  The WAVES waves of a workgroup have NP states each, and add what
+// these contribute in LDS.  Steps of a turn that lie beyond the sequence have dt = 0: they change nothing.
+
+struct ScanPlace {
+  int lane, part, group;
+  unsigned block, channel;
+  bool valid;
+  int64_t batch, chunk;
+  int64_t len, from, to, end;    // steps of the sequence, of the chunk, and where both end
+};
+
+__device__ __forceinline__ ScanPlace scan_place(const ScanShape& s, const int32_t* lengths) {
+  ScanPlace p;
+  p.lane = threadIdx.x & 63;
+  p.part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  p.block = blockIdx.x;
+  p.group = (int)(blockIdx.x / (unsigned)s.blocks);
+  const int within = (int)(blockIdx.x - (unsigned)p.group * s.blocks) * kWave + p.lane;
+  p.valid = within < s.group;
+  p.channel = (unsigned)p.group * s.group + (p.valid ? within : s.group - 1);
+  p.chunk = blockIdx.y;
+  p.batch = blockIdx.z;
+  p.len = steps_of(lengths, p.batch, s.steps);
+  p.from = p.chunk * s.chunk;
+  p.to = min(p.from + s.chunk, s.steps);
+  p.end = min(p.to, p.len);
+  return p;
+}
+
+// An element of a row that the wave has in common, at a lane's place.
+template <typename T>
+__device__ __forceinline__ T& in_row(T* row, unsigned place) {
+  return *reinterpret_cast<T*>((char*)row + place * (unsigned)sizeof(T));
+}
+
+// a log2(e) of a lane's states (zero beyond the last).
+template <int NP>
+__device__ __forceinline__ void load_decay(const ScanShape& s, const ScanPlace& p, const float* a, float (&decay)[NP]) {
+#pragma unroll
+  for (int n = 0; n < NP; ++n) {
+    const int at = p.part * NP + n;
+    decay[n] = at < s.states ? a[(int64_t)p.channel * s.states + at] * kLog2e : 0.f;
+  }
+}
+
+// States as callers hold them: batch x channels x states.
+template <int NP>
+__device__ __forceinline__ void load_states(const ScanShape& s, const ScanPlace& p, const float* from, float (&h)[NP]) {
+#pragma unroll
+  for (int n = 0; n < NP; ++n) {
+    const int at = p.part * NP + n;
+    h[n] = from && at < s.states ? from[(p.batch * s.channels + p.channel) * s.states + at] : 0.f;
+  }
+}
+template <int NP>
+__device__ __forceinline__ void store_states(const ScanShape& s, const ScanPlace& p, float* to, const float (&h)[NP]) {
+  if (!p.valid) return;
+#pragma unroll
+  for (int n = 0; n < NP; ++n) {
+    const int at = p.part * NP + n;
+    if (at < s.states) to[(p.batch * s.channels + p.channel) * s.states + at] = h[n];
+  }
+}
+// The workspace's: batch x chunks x states, filled up, x channels.
+template <int NP, int WAVES>
+__device__ __forceinline__ int64_t slot_of(const ScanShape& s, const ScanPlace& p) {
+  return ((p.batch * s.chunks + p.chunk) * (NP * WAVES) + p.part * NP) * s.channels;
+}
+template <int NP, int WAVES>
+__device__ __forceinline__ void load_slots(const ScanShape& s, const ScanPlace& p, const float* from, float (&h)[NP]) {
+  const float* at = from + slot_of<NP, WAVES>(s, p);
+#pragma unroll
+  for (int n = 0; n < NP; ++n) h[n] = in_row(at + n * s.channels, p.channel);
+}
+template <int NP, int WAVES>
+__device__ __forceinline__ void store_slots(const ScanShape& s, const ScanPlace& p, float* to, const float (&h)[NP]) {
+  if (!p.valid) return;
+  float* at = to + slot_of<NP, WAVES>(s, p);
+#pragma unroll
+  for (int n = 0; n < NP; ++n) in_row(at + n * s.channels, p.channel) = h[n];
+}
+
+// The values of one step that a wave reads: b, and c where the pass needs it.
+template <int NP, int WAVES, bool C>
+struct SharedRow {
+  float b[NP], c[C ? NP : 1];
+  __device__ __forceinline__ void load(Shared at) {
+#pragma unroll
+    for (int n = 0; n < NP; ++n) b[n] = at[n];
+    if (C) {
+#pragma unroll
+      for (int n = 0; n < NP; ++n) c[n] = at[NP * WAVES + n];
+    }
+  }
+};
+template <int NP, int WAVES>
+__device__ __forceinline__ Shared shared_rows(const ScanShape& s, const ScanPlace& p, const float* bc) {
+  return shared_at(bc) + (p.batch * s.groups + p.group) * s.rows * (2 * NP * WAVES) + p.part * NP;
+}
+// Rows are requested a step ahead: without a stop the scheduler gathers those of all steps, more than the scalar registers hold.
+__device__ __forceinline__ void stop() { __builtin_amdgcn_sched_barrier(0); }
+
+// A channel's elements of a turn's steps (of the last one there is, beyond).
+template <typename T>
+__device__ __forceinline__ void load_turn(const T* row, int64_t stride, unsigned channel, int last, T (&v)[kScanAhead]) {
+#pragma unroll
+  for (int j = 0; j < kScanAhead; ++j) v[j] = in_row(row + min(j, last) * stride, channel);
+}
+__device__ __forceinline__ int last_of(const ScanPlace& p, int64_t t) { return (int)min(p.end - 1 - t, (int64_t)kScanAhead - 1); }
+
+// dt and dt x of a turn.
+template <typename T>
+__device__ __forceinline__ void steps_and_inputs(const T (&xv)[kScanAhead], const T (&dv)[kScanAhead], float shift, int soft, int last,
+                                                 float (&dt)[kScanAhead], float (&u)[kScanAhead]) {
+#pragma unroll
+  for (int j = 0; j < kScanAhead; ++j) {
+    const float raw = (float)dv[j] + shift;
+    const float v = soft ? softplus(raw) : raw;
+    dt[j] = j <= last ? v : 0.f;
+    u[j] = j <= last ? v * (float)xv[j] : 0.f;
+  }
+}
+
+// ---- chunks: what each does to a state --------------------------------------------------------------------
+// The state behind a chunk that starts from zero, the sum of its dt (the state in front decays by exp(a sum)) and, for the backward pass,
+// the gradient of the state in front of it if nothing came from behind.
+template <typename T, int NP, int WAVES, bool BACKWARD>
+__global__ __launch_bounds__(WAVES * kWave) void scan_ends_kernel(ScanShape s, const T* __restrict__ x, const T* __restrict__ delta,
+                                                                  const float* __restrict__ a, const float* __restrict__ bc,
+                                                                  const T* __restrict__ gate, const float* __restrict__ delta_bias,
+                                                                  const int32_t* __restrict__ lengths, const T* __restrict__ dout,
+                                                                  float* __restrict__ ends, float* __restrict__ starts,
+                                                                  float* __restrict__ sums) {
+  constexpr int U = kScanAhead;
+  const ScanPlace p = scan_place(s, lengths);
+  float decay[NP], h[NP], g[NP], reach[NP];
+  load_decay<NP>(s, p, a, decay);
+#pragma unroll
+  for (int n = 0; n < NP; ++n) {
+    h[n] = g[n] = 0.f;
+    reach[n] = 1.f;
+  }
+  const float shift = delta_bias ? delta_bias[p.channel] : 0.f;
+  const T* xs = x + p.batch * s.x_b + p.from * s.x_t;
+  const T* ds = delta + p.batch * s.delta_b + p.from * s.delta_t;
+  const T* gs = BACKWARD && gate ? gate + p.batch * s.gate_b + p.from * s.gate_t : nullptr;
+  const T* os = BACKWARD ? dout + p.batch * s.out_b + p.from * s.out_t : nullptr;
+  Shared rows = shared_rows<NP, WAVES>(s, p, bc) + p.from * (2 * NP * WAVES);
+  float sum = 0.f;
+  for (int64_t t = p.from; t < p.end; t += U) {
+    const int last = last_of(p, t);
+    SharedRow<NP, WAVES, BACKWARD> next;
+    next.load(rows);
+    T xv[U], dv[U], gv[U], ov[U];
+    load_turn(xs, s.x_t, p.channel, last, xv);
+    load_turn(ds, s.delta_t, p.channel, last, dv);
+    if (BACKWARD) {
+      load_turn(os, s.out_t, p.channel, last, ov);
+      if (gs) load_turn(gs, s.gate_t, p.channel, last, gv);
+    }
+    float dt[U], u[U], dy[U];
+    steps_and_inputs(xv, dv, shift, s.softplus, last, dt, u);
+    if (BACKWARD) {
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        dy[j] = (float)ov[j];
+        if (gs) {
+          const float gt = (float)gv[j];
+          dy[j] *= gt * gates(gt).a;
+        }
+        if (j > last) dy[j] = 0.f;
+      }
+    }
+    stop();
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const SharedRow<NP, WAVES, BACKWARD> row = next;
+      if (j + 1 < U) next.load(rows + (j + 1) * (2 * NP * WAVES));
+      sum += dt[j];
+#pragma unroll
+      for (int n = 0; n < NP; ++n) {
+        const float e = __builtin_amdgcn_exp2f(dt[j] * decay[n]);
+        h[n] = fmaf(e, h[n], u[j] * row.b[n]);
+        if (BACKWARD) {
+          reach[n] *= e;
+          g[n] = fmaf(reach[n], row.c[n] * dy[j], g[n]);
+        }
+      }
+      stop();
+    }
+    xs += U * s.x_t;
+    ds += U * s.delta_t;
+    if (BACKWARD) os += U * s.out_t;
+    if (gs) gs += U * s.gate_t;
+    rows += U * (2 * NP * WAVES);
+  }
+  store_slots<NP, WAVES>(s, p, ends, h);
+  if (BACKWARD) store_slots<NP, WAVES>(s, p, starts, g);
+  if (p.valid && p.part == 0) sums[(p.batch * s.chunks + p.chunk) * s.channels + p.channel] = sum;
+}
+
+// The state in front of every chunk, in place of the one behind it, and the gradient of the state behind every chunk, in place of that in front.
+// A lane has one state of one channel.
+constexpr int kCarryAhead = 8;
+template <bool BACKWARD>
+__global__ __launch_bounds__(256) void scan_carry_kernel(ScanShape s, const float* __restrict__ a, const float* __restrict__ h0,
+                                                         const float* __restrict__ dlast, float* __restrict__ ends,
+                                                         float* __restrict__ starts, const float* __restrict__ sums) {
+  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x, b = blockIdx.z;
+  const int n = blockIdx.y;
+  if (c >= s.channels) return;
+  const bool held = n < s.states;
+  const float decay = held ? a[c * s.states + n] * kLog2e : 0.f;
+  const int64_t own = (b * s.channels + c) * s.states + n;
+  float h = held && h0 ? h0[own] : 0.f;
+  float* at = ends + (b * s.chunks * s.padded + n) * s.channels + c;
+  const int64_t step = (int64_t)s.padded * s.channels;
+  const float* total = sums + b * s.chunks * s.channels + c;
+  for (int k = 0; k < s.chunks; k += kCarryAhead) {
+    float v[kCarryAhead], d[kCarryAhead];
+#pragma unroll
+    for (int j = 0; j < kCarryAhead; ++j) {
+      const int64_t i = min(k + j, s.chunks - 1);
+      v[j] = at[i * step];
+      d[j] = total[i * s.channels];
+    }
+#pragma unroll
+    for (int j = 0; j < kCarryAhead; ++j)
+      if (k + j < s.chunks) {
+        at[(k + j) * step] = h;
+        h = fmaf(__builtin_amdgcn_exp2f(d[j] * decay), h, v[j]);
+      }
+  }
+  if (!BACKWARD) return;
+  float g = held && dlast ? dlast[own] : 0.f;
+  at = starts + (b * s.chunks * s.padded + n) * s.channels + c;
+  for (int k = s.chunks - 1; k >= 0; k -= kCarryAhead) {
+    float v[kCarryAhead], d[kCarryAhead];
+#pragma unroll
+    for (int j = 0; j < kCarryAhead; ++j) {
+      const int64_t i = max(k - j, 0);
+      v[j] = at[i * step];
+      d[j] = total[i * s.channels];
+    }
+#pragma unroll
+    for (int j = 0; j < kCarryAhead; ++j)
+      if (k - j >= 0) {
+        at[(k - j) * step] = g;
+        g = fmaf(__builtin_amdgcn_exp2f(d[j] * decay), g, v[j]);
+      }
+  }
+}
+
+// ---- forward ----------------------------------------------------------------------------------------------
+template <typename T, int NP, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave) void scan_forward_kernel(ScanShape s, const T* __restrict__ x, const T* __restrict__ delta,
+                                                                     const float* __restrict__ a, const float* __restrict__ bc,
+                                                                     const float* __restrict__ d, const T* __restrict__ gate,
+                                                                     const float* __restrict__ delta_bias,
+                                                                     const int32_t* __restrict__ lengths, const float* h0,
+                                                                     const float* __restrict__ ends, T* __restrict__ out, float* h_last) {
+  constexpr int U = kScanAhead;
+  __shared__ float add[WAVES > 1 ? WAVES * U * kWave : 1];
+  const ScanPlace p = scan_place(s, lengths);
+  float decay[NP], h[NP];
+  load_decay<NP>(s, p, a, decay);
+  if (s.chunks > 1) load_slots<NP, WAVES>(s, p, ends, h);
+  else load_states<NP>(s, p, h0, h);
+  const float shift = delta_bias ? delta_bias[p.channel] : 0.f, skip = d ? d[p.channel] : 0.f;
+  const T* xs = x + p.batch * s.x_b + p.from * s.x_t;
+  const T* ds = delta + p.batch * s.delta_b + p.from * s.delta_t;
+  const T* gs = gate ? gate + p.batch * s.gate_b + p.from * s.gate_t : nullptr;
+  T* os = out + p.batch * s.out_b;
+  Shared rows = shared_rows<NP, WAVES>(s, p, bc) + p.from * (2 * NP * WAVES);
+  for (int64_t t = p.from; t < p.end; t += U) {
+    const int last = last_of(p, t);
+    SharedRow<NP, WAVES, true> next;
+    next.load(rows);
+    T xv[U], dv[U], gv[U];
+    load_turn(xs, s.x_t, p.channel, last, xv);
+    load_turn(ds, s.delta_t, p.channel, last, dv);
+    if (gs) load_turn(gs, s.gate_t, p.channel, last, gv);
+    float y[U], dt[U], u[U];
+    steps_and_inputs(xv, dv, shift, s.softplus, last, dt, u);
+    stop();
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const SharedRow<NP, WAVES, true> row = next;
+      if (j + 1 < U) next.load(rows + (j + 1) * (2 * NP * WAVES));
+      y[j] = 0.f;
+#pragma unroll
+      for (int n = 0; n < NP; ++n) {
+        h[n] = fmaf(__builtin_amdgcn_exp2f(dt[j] * decay[n]), h[n], u[j] * row.b[n]);
+        y[j] = fmaf(row.c[n], h[n], y[j]);
+      }
+      stop();
+    }
+    if (WAVES > 1) {
+#pragma unroll
+      for (int j = 0; j < U; ++j) add[(p.part * U + j) * kWave + p.lane] = y[j];
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        y[j] = 0.f;
+#pragma unroll
+        for (int o = 0; o < WAVES; ++o) y[j] += add[(o * U + j) * kWave + p.lane];
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      float r = fmaf(skip, (float)xv[j], y[j]);
+      if (gs) {
+        const float gt = (float)gv[j];
+        r *= gt * gates(gt).a;
+      }
+      y[j] = r;
+    }
+    if (p.valid) {
+#pragma unroll
+      for (int j = 0; j < U; ++j)
+        if (j <= last && (WAVES == 1 || j % WAVES == p.part)) in_row(os + (t + j) * s.out_t, p.channel) = (T)y[j];
+    }
+    xs += U * s.x_t;
+    ds += U * s.delta_t;
+    if (gs) gs += U * s.gate_t;
+    rows += U * (2 * NP * WAVES);
+  }
+  if (p.valid && p.part == 0)
+    for (int64_t t = max(p.from, p.len); t < p.to; ++t) in_row(os + t * s.out_t, p.channel) = (T)0.f;
+  if (h_last && p.chunk == (p.len > 0 ? (p.len - 1) / s.chunk : 0)) store_states<NP>(s, p, h_last, h);
+}
+
+// ---- a few steps: lanes share a channel ----------------------------------------------------------------------
+// L lanes have 4 states each of a channel: states come and go in whole pieces of memory.
+template <typename T, int L>
+__global__ __launch_bounds__(256) void scan_walk_kernel(ScanShape s, const T* __restrict__ x, const T* __restrict__ delta,
+                                                        const float* __restrict__ a, const T* __restrict__ b, const T* __restrict__ c,
+                                                        int64_t b_b, int64_t b_t, int64_t c_b, int64_t c_t, const float* __restrict__ d,
+                                                        const T* __restrict__ gate, const float* __restrict__ delta_bias,
+                                                        const int32_t* __restrict__ lengths, const float* h0, T* __restrict__ out,
+                                                        float* h_last) {
+  const int64_t channel = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L, batch = blockIdx.y;
+  const int first = (threadIdx.x % L) * 4;
+  if (channel >= s.channels) return;             // all lanes of a channel together
+  const int64_t len = steps_of(lengths, batch, s.steps), left = s.states - first, group = channel / s.group;
+  const F32<4> decay = widen<float, 4>(load_some<4>(a + channel * s.states + first, left)) * kLog2e;
+  const int64_t own = (batch * s.channels + channel) * s.states + first;
+  F32<4> h = {};
+  if (h0) h = widen<float, 4>(load_some<4>(h0 + own, left));
+  const float shift = delta_bias ? delta_bias[channel] : 0.f, skip = d ? d[channel] : 0.f;
+  for (int64_t t = 0; t < len; ++t) {
+    const float xv = (float)x[batch * s.x_b + t * s.x_t + channel];
+    const float raw = (float)delta[batch * s.delta_b + t * s.delta_t + channel] + shift;
+    const F32<4> bv = widen<T, 4>(load_some<4>(b + batch * b_b + t * b_t + group * s.states + first, left));
+    const F32<4> cv = widen<T, 4>(load_some<4>(c + batch * c_b + t * c_t + group * s.states + first, left));
+    const float gt = gate ? (float)gate[batch * s.gate_b + t * s.gate_t + channel] : 0.f;
+    const float dt = s.softplus ? softplus(raw) : raw;
+    const float u = dt * xv;
+    float y = 0.f;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      h[n] = fmaf(__builtin_amdgcn_exp2f(dt * decay[n]), h[n], u * bv[n]);
+      y = fmaf(cv[n], h[n], y);
+    }
+    if (L > 1) y += dpp<0xB1>(y);
+    if (L > 2) y += dpp<0x4E>(y);
+    if (L > 4) y += dpp<0x141>(y);
+    if (L > 8) y += dpp<0x140>(y);
+    if (first == 0) {
+      float r = fmaf(skip, xv, y);
+      if (gate) r *= gt * gates(gt).a;
+      out[batch * s.out_b + t * s.out_t + channel] = (T)r;
+    }
+  }
+  if (first == 0)
+    for (int64_t t = len; t < s.steps; ++t) out[batch * s.out_b + t * s.out_t + channel] = (T)0.f;
+  if (h_last) store_some<float, 4>(h_last + own, h, left);
+}
+
+// ---- backward ---------------------------------------------------------------------------------------------
+
+// Sums over the 64 lanes of V values a lane (V a power of two up to 32): value i ends in the lanes l with l / (64 / V) = i.  Every stage
+// halves the values a lane has: it keeps one of two, and takes the same one from the lane that keeps the other.
+template <int V>
+__device__ __forceinline__ float lanes_sum(float (&v)[V], int l) {
+  constexpr int kWide = V;
+  int left = kWide;
+  // 32 lanes apart
+  if (left > 1) {
+    left /= 2;
+#pragma unroll
+    for (int i = 0; i < kWide / 2; ++i) {
+      const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + kWide / 2]), false, false);
+      v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+  }
+  if (kWide >= 4) {
+#pragma unroll
+    for (int i = 0; i < kWide / 4; ++i) {
+      const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + kWide / 4]), false, false);
+      v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+  }
+  if (kWide >= 8) {
+#pragma unroll
+    for (int i = 0; i < kWide / 8; ++i) {
+      const float mine = l & 8 ? v[i + kWide / 8] : v[i], other = l & 8 ? v[i] : v[i + kWide / 8];
+      v[i] = mine + dpp<0x128>(other);           // 8 lanes on, within 16
+    }
+  }
+  if (kWide >= 16) {
+#pragma unroll
+    for (int i = 0; i < kWide / 16; ++i) {
+      const float mine = l & 4 ? v[i + kWide / 16] : v[i], other = l & 4 ? v[i] : v[i + kWide / 16];
+      v[i] = mine + dpp<0x141>(other);           // mirrored within 8
+    }
+  } else {
+    v[0] += dpp<0x141>(v[0]);
+  }
+  if (kWide >= 32) {
+    const float mine = l & 2 ? v[1] : v[0], other = l & 2 ? v[0] : v[1];
+    v[0] = mine + dpp<0x4E>(other);
+  } else {
+    v[0] += dpp<0x4E>(v[0]);
+  }
+  return v[0] + dpp<0xB1>(v[0]);
+}
+
+// A chunk: its states at every kScanAhead-th step go to LDS first; then, from its end, kScanAhead steps at a time are computed once more, kept in
+// registers, and walked back.  The waves of a workgroup share what the states of a channel have in common: each works it out for some of the
+// steps, and finishes the gradients of those.
+// parts: of a chunk, states + 2 rows of channels (grad_a, grad_d, grad_delta_bias); shared_parts: of a block of channels and a step, the
+// sums of grad_b and grad_c over the block.
+template <typename T, int NP, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave, 2) void scan_backward_kernel(
+    ScanShape s, const T* __restrict__ x, const T* __restrict__ delta, const float* __restrict__ a, const float* __restrict__ bc,
+    const float* __restrict__ d, const T* __restrict__ gate, const float* __restrict__ delta_bias, const int32_t* __restrict__ lengths,
+    const T* __restrict__ dout, const float* __restrict__ h0, const float* __restrict__ dlast, const float* __restrict__ ends,
+    const float* __restrict__ starts, T* __restrict__ dx, T* __restrict__ ddelta, T* __restrict__ dgate, float* __restrict__ dh0,
+    float* __restrict__ parts, float* __restrict__ shared_parts) {
+  extern __shared__ float held[];
+  constexpr int U = kScanAhead, SHARE = U / WAVES;    // steps of a turn that a wave finishes
+  constexpr int row_size = 2 * NP * WAVES;
+  const ScanPlace p = scan_place(s, lengths);
+  const int most = (int)s.chunk / U;                                          // turns
+  float* const own = held + p.part * most * NP * kWave + p.lane;              // states in front of every turn
+  float* const common = held + WAVES * most * NP * kWave + p.lane;            // dt, u, dy of a turn's steps
+  float* const add = common + 3 * U * kWave;                                  // what the waves' states contribute to a turn's steps
+  float decay[NP], h[NP], g[NP], da[NP];
+  load_decay<NP>(s, p, a, decay);
+  if (s.chunks > 1) load_slots<NP, WAVES>(s, p, ends, h);
+  else load_states<NP>(s, p, h0, h);
+  const float shift = delta_bias ? delta_bias[p.channel] : 0.f, skip = d ? d[p.channel] : 0.f;
+  const T* const xs = x + p.batch * s.x_b;
+  const T* const ds = delta + p.batch * s.delta_b;
+  const Shared rows = shared_rows<NP, WAVES>(s, p, bc);
+  const int turns = p.end > p.from ? (int)((p.end - p.from + U - 1) / U) : 0;
+  for (int i = 0; i < turns; ++i) {
+#pragma unroll
+    for (int n = 0; n < NP; ++n) own[(i * NP + n) * kWave] = h[n];
+    if (i + 1 == turns) break;
+    const int64_t t = p.from + i * U;
+    const Shared at = rows + t * row_size;
+    SharedRow<NP, WAVES, false> next;
+    next.load(at);
+    T xv[U], dv[U];
+    load_turn(xs + t * s.x_t, s.x_t, p.channel, U - 1, xv);
+    load_turn(ds + t * s.delta_t, s.delta_t, p.channel, U - 1, dv);
+    float dt[U], u[U];
+    steps_and_inputs(xv, dv, shift, s.softplus, U - 1, dt, u);
+    stop();
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const SharedRow<NP, WAVES, false> row = next;
+      if (j + 1 < U) next.load(at + (j + 1) * row_size);
+#pragma unroll
+      for (int n = 0; n < NP; ++n) h[n] = fmaf(__builtin_amdgcn_exp2f(dt[j] * decay[n]), h[n], u[j] * row.b[n]);
+      stop();
+    }
+  }
+  if (s.chunks > 1) load_slots<NP, WAVES>(s, p, starts, g);
+  else load_states<NP>(s, p, dlast, g);
+  const T* const gs = gate ? gate + p.batch * s.gate_b : nullptr;
+  const T* const os = dout + p.batch * s.out_b;
+  float dskip = 0.f, dshift = 0.f;
+#pragma unroll
+  for (int n = 0; n < NP; ++n) da[n] = 0.f;
+  float* const shared_to = shared_parts + (p.batch * s.groups * s.blocks + p.block) * s.steps * row_size;
+  for (int i = turns - 1; i >= 0; --i) {
+    const int64_t t = p.from + i * U;
+    const int last = last_of(p, t);
+    const Shared at = rows + t * row_size;
+    // this wave's steps
+    T xv[SHARE], dv[SHARE], gv[SHARE], ov[SHARE];
+#pragma unroll
+    for (int k = 0; k < SHARE; ++k) {
+      const int64_t step = t + min(p.part * SHARE + k, last);
+      xv[k] = in_row(xs + step * s.x_t, p.channel);
+      dv[k] = in_row(ds + step * s.delta_t, p.channel);
+      ov[k] = in_row(os + step * s.out_t, p.channel);
+      if (gs) gv[k] = in_row(gs + step * s.gate_t, p.channel);
+    }
+#pragma unroll
+    for (int k = 0; k < SHARE; ++k) {
+      const bool in = p.part * SHARE + k <= last, on = in && p.valid;
+      const float raw = (float)dv[k] + shift;
+      const float step = s.softplus ? softplus(raw) : raw;
+      float r = (float)ov[k];
+      if (gs) {
+        const float gt = (float)gv[k];
+        r *= gt * gates(gt).a;
+      }
+      float* const to = common + (p.part * SHARE + k) * 3 * kWave;
+      to[0] = in ? step : 0.f;
+      to[kWave] = on ? step * (float)xv[k] : 0.f;
+      to[2 * kWave] = on ? r : 0.f;
+    }
+    SharedRow<NP, WAVES, false> ahead;
+    ahead.load(at);
+    if (WAVES > 1) __syncthreads();
+    float hs[U + 1][NP], e[U][NP];
+#pragma unroll
+    for (int n = 0; n < NP; ++n) hs[0][n] = own[(i * NP + n) * kWave];
+    SharedRow<NP, WAVES, true> next;
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const SharedRow<NP, WAVES, false> row = ahead;
+      if (j + 1 < U) ahead.load(at + (j + 1) * row_size);
+      else next.load(at + j * row_size);
+      const float dt = common[j * 3 * kWave], u = common[(j * 3 + 1) * kWave];
+#pragma unroll
+      for (int n = 0; n < NP; ++n) {
+        e[j][n] = __builtin_amdgcn_exp2f(dt * decay[n]);
+        hs[j + 1][n] = fmaf(e[j][n], hs[j][n], u * row.b[n]);
+      }
+      stop();
+    }
+#pragma unroll
+    for (int j = U - 1; j >= 0; --j) {
+      const SharedRow<NP, WAVES, true> row = next;
+      if (j > 0) next.load(at + (j - 1) * row_size);
+      const float dt = common[j * 3 * kWave], u = common[(j * 3 + 1) * kWave], dy = common[(j * 3 + 2) * kWave];
+      float v[2 * NP], y = 0.f, along = 0.f, step = 0.f;
+#pragma unroll
+      for (int n = 0; n < NP; ++n) {
+        const float total = fmaf(row.c[n], dy, g[n]);
+        y = fmaf(row.c[n], hs[j + 1][n], y);
+        v[n] = total * u;
+        v[NP + n] = dy * hs[j + 1][n];
+        along = fmaf(total, row.b[n], along);
+        g[n] = total * e[j][n];
+        const float back = g[n] * hs[j][n];
+        step = fmaf(back, decay[n], step);
+        da[n] = fmaf(back, dt, da[n]);
+      }
+      const float sum = lanes_sum<2 * NP>(v, p.lane);
+      constexpr int each = kWave / (2 * NP);
+      if (j <= last && p.lane % each == 0) {
+        const int k = p.lane / each;
+        shared_to[(t + j) * row_size + p.part * NP + (k < NP ? k : NP * WAVES + k - NP)] = sum;
+      }
+      float* const to = add + (p.part * U + j) * 3 * kWave;
+      to[0] = y;
+      to[kWave] = along;
+      to[2 * kWave] = step;
+      stop();
+    }
+    if (WAVES > 1) __syncthreads();
+#pragma unroll
+    for (int k = 0; k < SHARE; ++k) {
+      const int j = p.part * SHARE + k;
+      float y = 0.f, along = 0.f, step = 0.f;
+#pragma unroll
+      for (int o = 0; o < WAVES; ++o) {
+        const float* const from = add + (o * U + j) * 3 * kWave;
+        y += from[0];
+        along += from[kWave];
+        step += from[2 * kWave];
+      }
+      if (j > last || !p.valid) continue;
+      const float dt = common[j * 3 * kWave], dy = common[(j * 3 + 2) * kWave], xt = (float)xv[k];
+      float r = fmaf(along, xt, step * kLn2);
+      if (s.softplus) r *= gates((float)dv[k] + shift).a;
+      in_row(dx + p.batch * s.dx_b + (t + j) * s.dx_t, p.channel) = (T)fmaf(dt, along, skip * dy);
+      in_row(ddelta + p.batch * s.ddelta_b + (t + j) * s.ddelta_t, p.channel) = (T)r;
+      dshift += r;
+      dskip = fmaf(dy, xt, dskip);
+      if (gs) {
+        const float gt = (float)gv[k];
+        const Gates z = gates(gt);
+        in_row(dgate + p.batch * s.dgate_b + (t + j) * s.dgate_t, p.channel) =
+            (T)((float)ov[k] * fmaf(skip, xt, y) * (z.a * fmaf(gt, z.z, 1.f)));
+      }
+    }
+    if (WAVES > 1) __syncthreads();      // common and add are written again
+  }
+  float* const to = parts + (p.batch * s.chunks + p.chunk) * (s.states + 2) * s.channels;
+  if (p.valid) {
+#pragma unroll
+    for (int n = 0; n < NP; ++n) {
+      const int at = p.part * NP + n;
+      if (at < s.states) in_row(to + at * s.channels, p.channel) = da[n];
+    }
+    if (dh0 && p.chunk == 0) store_states<NP>(s, p, dh0, g);
+  }
+  if (WAVES > 1) {
+    add[p.part * 2 * kWave] = dskip;
+    add[(p.part * 2 + 1) * kWave] = dshift;
+    __syncthreads();
+    dskip = dshift = 0.f;
+#pragma unroll
+    for (int o = 0; o < WAVES; ++o) {
+      dskip += add[o * 2 * kWave];
+      dshift += add[(o * 2 + 1) * kWave];
+    }
+  }
+  if (!p.valid || p.part != 0) return;
+  in_row(to + s.states * s.channels, p.channel) = dskip;
+  in_row(to + (s.states + 1) * s.channels, p.channel) = dshift;
+  for (int64_t t = max(p.from, p.len); t < p.to; ++t) {
+    in_row(dx + p.batch * s.dx_b + t * s.dx_t, p.channel) = (T)0.f;
+    in_row(ddelta + p.batch * s.ddelta_b + t * s.ddelta_t, p.channel) = (T)0.f;
+    if (gs) in_row(dgate + p.batch * s.dgate_b + t * s.dgate_t, p.channel) = (T)0.f;
+  }
+}
+
+// grad_b and grad_c: the sums of a group's blocks of channels, in their order.
+template <typename T>
+__global__ __launch_bounds__(256) void scan_join_kernel(const float* __restrict__ shared_parts, int64_t rows, int64_t steps, int groups,
+                                                        int blocks, int states, int padded, const int32_t* __restrict__ lengths,
+                                                        T* __restrict__ db, T* __restrict__ dc, int64_t db_b, int64_t db_t, int64_t dc_b,
+                                                        int64_t dc_t) {
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / (2 * padded);
+  if (row >= rows) return;
+  const int k = (int)(at - row * 2 * padded), n = k < padded ? k : k - padded;
+  if (n >= states) return;
+  const int64_t t = row % steps, g = row / steps % groups, batch = row / steps / groups;
+  float s = 0.f;
+  if (t < steps_of(lengths, batch, steps)) {
+    const float* from = shared_parts + ((batch * groups + g) * blocks * steps + t) * 2 * padded + k;
+    for (int i = 0; i < blocks; ++i) s += from[(int64_t)i * steps * 2 * padded];
+  }
+  if (k < padded) db[batch * db_b + t * db_t + g * states + n] = (T)s;
+  else dc[batch * dc_b + t * dc_t + g * states + n] = (T)s;
+}
+
+}  // namespace accop

@@ -1,0 +1,340 @@
+// Host side of the selective state space scan: argument checks, workspace layout, choice of kernels and the launches.
+#include "op_common.h"
+#include "op_host.h"
+#include "scan.h"
+#include "parts.h"
+
+using namespace accop;
+
+namespace {
+
+constexpr int64_t kMostBackwardSteps = int64_t(1) << 21;   // chunks of a launch: below 2^16
+
+Rows shared_rows(const acc_scan& c) { return {c.batch, c.steps, (int64_t)c.groups * c.states, c.type}; }
+
+int32_t check_scan(const acc_scan* c, bool backward) {
+  REQUIRE(c, "config is NULL");
+  REQUIRE(c->batch >= 0 && c->batch <= 65535, "batch out of range");
+  REQUIRE(c->steps >= 0 && c->steps < (int64_t(1) << 31), "steps out of range");
+  REQUIRE(c->channels >= 1 && c->channels <= (int64_t(1) << 24), "channels out of range");
+  REQUIRE(c->states >= 1 && c->states <= ACC_SCAN_STATES, "states out of range");
+  REQUIRE(c->groups >= 1 && c->channels % c->groups == 0, "channels must be a multiple of groups");
+  REQUIRE(is_type(c->type), "unknown type");
+  REQUIRE(c->softplus == 0 || c->softplus == 1, "softplus must be 0 or 1");
+  REQUIRE(c->accumulate == 0 || c->accumulate == 1, "accumulate must be 0 or 1");
+  const Rows shared = shared_rows(*c);
+  REQUIRE(strides_fit(*c, c->x_batch, c->x_step) && strides_fit(*c, c->delta_batch, c->delta_step) &&
+              strides_fit(shared, c->b_batch, c->b_step) && strides_fit(shared, c->c_batch, c->c_step) &&
+              strides_fit(*c, c->gate_batch, c->gate_step) && strides_fit(*c, c->out_batch, c->out_step),
+          "stride out of range");
+  if (!backward) return ACC_OK;
+  REQUIRE(c->steps <= kMostBackwardSteps, "steps out of range");
+  REQUIRE(strides_fit(*c, c->grad_x_batch, c->grad_x_step) && strides_fit(*c, c->grad_delta_batch, c->grad_delta_step) &&
+              strides_fit(shared, c->grad_b_batch, c->grad_b_step) && strides_fit(shared, c->grad_c_batch, c->grad_c_step) &&
+              strides_fit(*c, c->grad_gate_batch, c->grad_gate_step),
+          "stride out of range");
+  return ACC_OK;
+}
+
+constexpr int64_t kScanWalkSteps = 8;       // up to here lanes share a channel and walk the steps
+constexpr int64_t kScanWaves = 4096;        // waves that fill the chip
+constexpr int64_t kScanLone = 1024;         // from here on no chunks
+constexpr int64_t kScanShortest = 32;       // steps of a chunk at least
+
+struct ScanPlan {
+  bool walk = false;
+  int each = 16, waves = 1, padded = 16;    // states of a lane, waves of a workgroup, states in all
+  int64_t group = 0, blocks = 0;            // channels of a group, blocks of 64 of them
+  int64_t chunk = 0, chunks = 1, rows = 0;  // steps of a chunk, chunks, rows of a sequence's b and c
+  int64_t packed = 0, ends = 0, starts = 0, sums = 0, parts = 0, shared_parts = 0, bytes = 0;   // offsets in the workspace
+};
+
+ScanPlan plan_scan(const acc_scan& c, bool backward) {
+  ScanPlan p;
+  p.walk = !backward && c.steps <= kScanWalkSteps;
+  if (p.walk || c.batch == 0) return p;
+  p.each = c.states <= 4 ? 4 : c.states <= 8 ? 8 : 16;
+  p.waves = c.states <= 16 ? 1 : c.states <= 32 ? 2 : 4;
+  p.padded = p.each * p.waves;
+  p.group = c.channels / c.groups;
+  p.blocks = up(p.group, kWave);
+  const int64_t lone = c.batch * c.groups * p.blocks * p.waves;      // waves of one chunk
+  if (backward) {
+    p.chunk = p.waves > 2 ? 32 : 64;
+    while (p.chunk > 16 && lone * up(c.steps, p.chunk) < kScanWaves / 2) p.chunk /= 2;
+  } else {
+    p.chunk = c.steps;
+    if (lone < kScanLone) p.chunk = std::max(kScanShortest, up(c.steps, up(kScanWaves, lone)));
+    while (up(c.steps, p.chunk) > 65535) p.chunk *= 2;
+  }
+  p.chunk = up(p.chunk, kScanAhead) * kScanAhead;
+  p.chunks = std::max<int64_t>(1, up(c.steps, p.chunk));
+  int64_t at = 0;
+  auto take = [&](int64_t floats) { const int64_t o = at; at += round256(4 * floats); return o; };
+  p.rows = up(c.steps, kScanAhead) * kScanAhead;
+  const int64_t slots = p.chunks > 1 ? c.batch * p.chunks * c.channels : 0;
+  p.packed = take(c.batch * c.groups * p.rows * 2 * p.padded);
+  p.ends = take(slots * p.padded);
+  p.sums = take(slots);
+  if (backward) {
+    p.starts = take(slots * p.padded);
+    p.parts = take(c.batch * p.chunks * (c.states + 2) * c.channels);
+    p.shared_parts = take(c.batch * c.groups * p.blocks * c.steps * 2 * p.padded);
+  }
+  p.bytes = at;
+  return p;
+}
+
+ScanShape shape_of(const acc_scan& c, const ScanPlan& p) {
+  return {c.steps, c.channels, c.x_batch, c.x_step, c.delta_batch, c.delta_step, c.gate_batch, c.gate_step, c.out_batch, c.out_step,
+          c.grad_x_batch, c.grad_x_step, c.grad_delta_batch, c.grad_delta_step, c.grad_gate_batch, c.grad_gate_step,
+          p.chunk, p.rows, (int)p.chunks, c.states, p.padded, c.groups, (int)(c.channels / c.groups), (int)p.blocks, c.softplus};
+}
+
+struct ScanIn {
+  const void *x, *delta;
+  const float* a;
+  const void *b, *c;
+  const float* d;
+  const void* gate;
+  const float *delta_bias, *h0;
+  const int32_t* lengths;
+};
+
+template <typename T>
+const T* as(const void* p) { return static_cast<const T*>(p); }
+
+template <typename T>
+void pack(const acc_scan& c, const ScanPlan& p, const ScanIn& in, float* to, Queue& queue) {
+  const int64_t all = c.batch * c.groups * p.rows;
+  if (all == 0) return;
+  LAUNCH(scan_pack_kernel<T>, dim3((unsigned)up(all * 2 * p.padded, 256)), dim3(256), queue, as<T>(in.b), as<T>(in.c), c.b_batch, c.b_step,
+         c.c_batch, c.c_step, all, c.steps, p.rows, c.groups, c.states, p.padded, in.lengths, to);
+}
+
+template <typename T, int L>
+void walk(const acc_scan& c, const ScanPlan& p, const ScanIn& in, void* out, float* h_last, Queue& queue) {
+  LAUNCH((scan_walk_kernel<T, L>), dim3((unsigned)up(c.channels * L, 256), (unsigned)c.batch), dim3(256), queue, shape_of(c, p), as<T>(in.x),
+         as<T>(in.delta), in.a, as<T>(in.b), as<T>(in.c), c.b_batch, c.b_step, c.c_batch, c.c_step, in.d, as<T>(in.gate), in.delta_bias,
+         in.lengths, in.h0, static_cast<T*>(out), h_last);
+}
+
+template <typename T, int NP, int WAVES>
+void forward_chunks(const acc_scan& c, const ScanPlan& p, const ScanIn& in, void* out, float* h_last, char* ws, Queue& queue) {
+  const ScanShape s = shape_of(c, p);
+  float* const packed = reinterpret_cast<float*>(ws + p.packed);
+  float* const ends = reinterpret_cast<float*>(ws + p.ends);
+  float* const sums = reinterpret_cast<float*>(ws + p.sums);
+  const unsigned across = (unsigned)(c.groups * p.blocks), batch = (unsigned)c.batch, threads = kWave * WAVES;
+  pack<T>(c, p, in, packed, queue);
+  if (p.chunks > 1) {
+    LAUNCH((scan_ends_kernel<T, NP, WAVES, false>), dim3(across, (unsigned)(p.chunks - 1), batch), dim3(threads), queue, s, as<T>(in.x),
+           as<T>(in.delta), in.a, packed, nullptr, in.delta_bias, in.lengths, nullptr, ends, nullptr, sums);
+    LAUNCH(scan_carry_kernel<false>, dim3((unsigned)up(c.channels, 256), (unsigned)p.padded, batch), dim3(256), queue, s, in.a, in.h0, nullptr,
+           ends, nullptr, sums);
+  }
+  LAUNCH((scan_forward_kernel<T, NP, WAVES>), dim3(across, (unsigned)p.chunks, batch), dim3(threads), queue, s, as<T>(in.x), as<T>(in.delta),
+         in.a, packed, in.d, as<T>(in.gate), in.delta_bias, in.lengths, in.h0, ends, static_cast<T*>(out), h_last);
+}
+
+template <typename T>
+void forward(const acc_scan& c, const ScanPlan& p, const ScanIn& in, void* out, float* h_last, char* ws, Queue& queue) {
+  if (p.walk) {
+    if (c.states <= 4) walk<T, 1>(c, p, in, out, h_last, queue);
+    else if (c.states <= 8) walk<T, 2>(c, p, in, out, h_last, queue);
+    else if (c.states <= 16) walk<T, 4>(c, p, in, out, h_last, queue);
+    else if (c.states <= 32) walk<T, 8>(c, p, in, out, h_last, queue);
+    else walk<T, 16>(c, p, in, out, h_last, queue);
+    return;
+  }
+  if (p.padded == 4) forward_chunks<T, 4, 1>(c, p, in, out, h_last, ws, queue);
+  else if (p.padded == 8) forward_chunks<T, 8, 1>(c, p, in, out, h_last, ws, queue);
+  else if (p.padded == 16) forward_chunks<T, 16, 1>(c, p, in, out, h_last, ws, queue);
+  else if (p.padded == 32) forward_chunks<T, 16, 2>(c, p, in, out, h_last, ws, queue);
+  else forward_chunks<T, 16, 4>(c, p, in, out, h_last, ws, queue);
+}
+
+struct ScanGradients {
+  const void* out;
+  const float* last;
+  void *x, *delta;
+  float* a;
+  void *b, *c;
+  float* d;
+  void* gate;
+  float *delta_bias, *h0;
+};
+
+template <typename T, int NP, int WAVES>
+void backward_ends(const acc_scan& c, const ScanPlan& p, const ScanIn& in, const ScanGradients& g, char* ws, Queue& queue) {
+  auto at = [&](int64_t offset) { return reinterpret_cast<float*>(ws + offset); };
+  LAUNCH((scan_ends_kernel<T, NP, WAVES, true>), dim3((unsigned)(c.groups * p.blocks), (unsigned)p.chunks, (unsigned)c.batch),
+         dim3(kWave * WAVES), queue, shape_of(c, p), as<T>(in.x), as<T>(in.delta), in.a, at(p.packed), as<T>(in.gate),
+         in.delta_bias, in.lengths, as<T>(g.out), at(p.ends), at(p.starts), at(p.sums));
+}
+
+template <typename T, int NP, int WAVES>
+void backward_chunks(const acc_scan& c, const ScanPlan& p, const ScanIn& in, const ScanGradients& g, char* ws, Queue& queue) {
+  auto at = [&](int64_t offset) { return reinterpret_cast<float*>(ws + offset); };
+  const int64_t lds = 4 * kWave * (p.chunk / kScanAhead * p.padded + 3 * kScanAhead * (1 + WAVES));
+  enqueue(queue, scan_backward_kernel<T, NP, WAVES>, dim3((unsigned)(c.groups * p.blocks), (unsigned)p.chunks, (unsigned)c.batch),
+          dim3(kWave * WAVES), (unsigned)lds, shape_of(c, p), as<T>(in.x), as<T>(in.delta), in.a, at(p.packed), in.d, as<T>(in.gate),
+          in.delta_bias, in.lengths, as<T>(g.out), in.h0, g.last, at(p.ends), at(p.starts), static_cast<T*>(g.x), static_cast<T*>(g.delta),
+          static_cast<T*>(g.gate), g.h0, at(p.parts), at(p.shared_parts));
+}
+
+template <typename T>
+void backward(const acc_scan& c, const ScanPlan& p, const ScanIn& in, const ScanGradients& g, char* ws, Queue& queue) {
+  auto at = [&](int64_t offset) { return reinterpret_cast<float*>(ws + offset); };
+  if (c.batch > 0) {
+    pack<T>(c, p, in, at(p.packed), queue);
+    if (p.chunks > 1) {
+      if (p.padded == 4) backward_ends<T, 4, 1>(c, p, in, g, ws, queue);
+      else if (p.padded == 8) backward_ends<T, 8, 1>(c, p, in, g, ws, queue);
+      else if (p.padded == 16) backward_ends<T, 16, 1>(c, p, in, g, ws, queue);
+      else if (p.padded == 32) backward_ends<T, 16, 2>(c, p, in, g, ws, queue);
+      else backward_ends<T, 16, 4>(c, p, in, g, ws, queue);
+      LAUNCH(scan_carry_kernel<true>, dim3((unsigned)up(c.channels, 256), (unsigned)p.padded, (unsigned)c.batch), dim3(256), queue,
+             shape_of(c, p), in.a, in.h0, g.last, at(p.ends), at(p.starts), at(p.sums));
+    }
+    if (p.padded == 4) backward_chunks<T, 4, 1>(c, p, in, g, ws, queue);
+    else if (p.padded == 8) backward_chunks<T, 8, 1>(c, p, in, g, ws, queue);
+    else if (p.padded == 16) backward_chunks<T, 8, 2>(c, p, in, g, ws, queue);
+    else if (p.padded == 32) backward_chunks<T, 8, 4>(c, p, in, g, ws, queue);
+    else backward_chunks<T, 8, 8>(c, p, in, g, ws, queue);
+    const int64_t rows = c.batch * c.groups * c.steps;
+    if (rows > 0)
+      LAUNCH(scan_join_kernel<T>, dim3((unsigned)up(rows * 2 * p.padded, 256)), dim3(256), queue, at(p.shared_parts), rows, c.steps, c.groups,
+             (int)p.blocks, c.states, p.padded, in.lengths, static_cast<T*>(g.b), static_cast<T*>(g.c), c.grad_b_batch, c.grad_b_step,
+             c.grad_c_batch, c.grad_c_step);
+  }
+  LAUNCH(parts_join_kernel, dim3((unsigned)up(c.channels, kWave), (unsigned)(c.states + 2)), dim3(1024), queue,
+         reinterpret_cast<const float*>(ws + p.parts), c.batch * p.chunks, c.states + 2, c.channels, PartsTo{g.a, c.states, g.d, g.delta_bias},
+         c.accumulate);
+}
+
+// A launch has fewer than 2^32 work items per axis.
+bool too_large(const acc_scan& c, const ScanPlan& p) {
+  return !p.walk && ((double)c.batch * c.groups * c.steps * 2 * p.padded >= 4e9 || (int64_t)c.groups * p.blocks * kWave * p.waves >= (int64_t(1) << 31));
+}
+
+Span floats(const void* p, int64_t n) { return {static_cast<const char*>(p), p ? 4 * n : 0}; }
+
+}  // namespace
+
+extern "C" {
+
+int32_t accordion_scan_workspace_bytes(const acc_scan* c, int32_t backward_pass, size_t* out_bytes) {
+  REQUIRE(out_bytes, "out_bytes is NULL");
+  REQUIRE(backward_pass == 0 || backward_pass == 1, "backward must be 0 or 1");
+  if (const int32_t rc = check_scan(c, backward_pass)) return rc;
+  const ScanPlan p = plan_scan(*c, backward_pass);
+  REQUIRE(!too_large(*c, p), "batch x steps x groups out of range");
+  *out_bytes = (size_t)p.bytes;
+  return ACC_OK;
+}
+
+int32_t accordion_scan_forward(const acc_scan* c, const void* x_dev, const void* delta_dev, const float* a_dev, const void* b_dev,
+                               const void* c_dev, const float* d_dev, const void* gate_dev, const float* delta_bias_dev,
+                               const float* h0_dev, const int32_t* lengths_dev, void* out_dev, float* h_last_dev, void* workspace_dev,
+                               size_t workspace_bytes, void* hip_stream) {
+  Queue queue(hip_stream);
+  if (const int32_t rc = check_scan(c, false)) return rc;
+  REQUIRE(rows_apart(*c, c->out_batch, c->out_step), "rows of out overlap");
+  if (c->batch == 0) return ACC_OK;
+  REQUIRE(a_dev && (c->steps == 0 || (x_dev && delta_dev && b_dev && c_dev && out_dev)), "a pointer is NULL");
+  const int e = type_bytes(c->type);
+  REQUIRE(!off_type(x_dev, e) && !off_type(delta_dev, e) && !off_type(b_dev, e) && !off_type(c_dev, e) && !off_type(gate_dev, e) &&
+              !off_type(out_dev, e) && !off_type(a_dev, 4) && !off_type(d_dev, 4) && !off_type(delta_bias_dev, 4) && !off_type(h0_dev, 4) &&
+              !off_type(lengths_dev, 4) && !off_type(h_last_dev, 4),
+          "a pointer is not aligned to its element type");
+  const ScanPlan p = plan_scan(*c, false);
+  REQUIRE(!too_large(*c, p), "batch x steps x groups out of range");
+  if (const int32_t rc = check_workspace(workspace_dev, workspace_bytes, p.bytes)) return rc;
+  const Rows shared = shared_rows(*c);
+  const int64_t ends = c->batch * c->channels * c->states;
+  const Span s[13] = {{static_cast<const char*>(workspace_dev), p.bytes},
+                      steps_span(out_dev, *c, c->out_batch, c->out_step),
+                      floats(h_last_dev, ends),
+                      steps_span(x_dev, *c, c->x_batch, c->x_step),
+                      steps_span(delta_dev, *c, c->delta_batch, c->delta_step),
+                      steps_span(b_dev, shared, c->b_batch, c->b_step),
+                      steps_span(c_dev, shared, c->c_batch, c->c_step),
+                      steps_span(gate_dev, *c, c->gate_batch, c->gate_step),
+                      floats(a_dev, c->channels * c->states),
+                      floats(d_dev, c->channels),
+                      floats(delta_bias_dev, c->channels),
+                      floats(h0_dev == h_last_dev ? nullptr : h0_dev, ends),
+                      floats(lengths_dev, c->batch)};
+  REQUIRE(!any_overlap(s, 3, 13), "a buffer that is written overlaps another one");
+  const ScanIn in = {x_dev, delta_dev, a_dev, b_dev, c_dev, d_dev, gate_dev, delta_bias_dev, h0_dev, lengths_dev};
+  char* const ws = static_cast<char*>(workspace_dev);
+  if (c->type == ACC_BF16) forward<bf16>(*c, p, in, out_dev, h_last_dev, ws, queue);
+  else forward<float>(*c, p, in, out_dev, h_last_dev, ws, queue);
+  return launched(queue);
+}
+
+int32_t accordion_scan_backward(const acc_scan* c, const void* x_dev, const void* delta_dev, const float* a_dev, const void* b_dev,
+                                const void* c_dev, const float* d_dev, const void* gate_dev, const float* delta_bias_dev,
+                                const float* h0_dev, const int32_t* lengths_dev, const void* grad_out_dev, const float* grad_last_dev,
+                                void* grad_x_dev, void* grad_delta_dev, float* grad_a_dev, void* grad_b_dev, void* grad_c_dev,
+                                float* grad_d_dev, void* grad_gate_dev, float* grad_delta_bias_dev, float* grad_h0_dev,
+                                void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  Queue queue(hip_stream);
+  if (const int32_t rc = check_scan(c, true)) return rc;
+  const Rows shared = shared_rows(*c);
+  REQUIRE(rows_apart(*c, c->grad_x_batch, c->grad_x_step) && rows_apart(*c, c->grad_delta_batch, c->grad_delta_step) &&
+              rows_apart(shared, c->grad_b_batch, c->grad_b_step) && rows_apart(shared, c->grad_c_batch, c->grad_c_step) &&
+              (!gate_dev || rows_apart(*c, c->grad_gate_batch, c->grad_gate_step)),
+          "rows of a gradient overlap");
+  const bool any = c->batch > 0 && c->steps > 0;
+  REQUIRE(a_dev && grad_a_dev, "a pointer is NULL");
+  REQUIRE(!any || (x_dev && delta_dev && b_dev && c_dev && grad_out_dev && grad_x_dev && grad_delta_dev && grad_b_dev && grad_c_dev),
+          "a pointer is NULL");
+  REQUIRE(!any || (gate_dev == nullptr) == (grad_gate_dev == nullptr), "gate_dev and grad_gate_dev go together");
+  REQUIRE(d_dev || !grad_d_dev, "grad_d_dev needs d_dev");
+  REQUIRE(delta_bias_dev || !grad_delta_bias_dev, "grad_delta_bias_dev needs delta_bias_dev");
+  const int e = type_bytes(c->type);
+  REQUIRE(!off_type(x_dev, e) && !off_type(delta_dev, e) && !off_type(b_dev, e) && !off_type(c_dev, e) && !off_type(gate_dev, e) &&
+              !off_type(grad_out_dev, e) && !off_type(grad_x_dev, e) && !off_type(grad_delta_dev, e) && !off_type(grad_b_dev, e) &&
+              !off_type(grad_c_dev, e) && !off_type(grad_gate_dev, e) && !off_type(a_dev, 4) && !off_type(d_dev, 4) &&
+              !off_type(delta_bias_dev, 4) && !off_type(h0_dev, 4) && !off_type(lengths_dev, 4) && !off_type(grad_last_dev, 4) &&
+              !off_type(grad_a_dev, 4) && !off_type(grad_d_dev, 4) && !off_type(grad_delta_bias_dev, 4) && !off_type(grad_h0_dev, 4),
+          "a pointer is not aligned to its element type");
+  const ScanPlan p = plan_scan(*c, true);
+  REQUIRE(!too_large(*c, p), "batch x steps x groups out of range");
+  if (const int32_t rc = check_workspace(workspace_dev, workspace_bytes, p.bytes)) return rc;
+  const int64_t ends = c->batch * c->channels * c->states;
+  const Span s[22] = {{static_cast<const char*>(workspace_dev), p.bytes},
+                      steps_span(grad_x_dev, *c, c->grad_x_batch, c->grad_x_step),
+                      steps_span(grad_delta_dev, *c, c->grad_delta_batch, c->grad_delta_step),
+                      steps_span(grad_b_dev, shared, c->grad_b_batch, c->grad_b_step),
+                      steps_span(grad_c_dev, shared, c->grad_c_batch, c->grad_c_step),
+                      steps_span(grad_gate_dev, *c, c->grad_gate_batch, c->grad_gate_step),
+                      floats(grad_a_dev, c->channels * c->states),
+                      floats(grad_d_dev, c->channels),
+                      floats(grad_delta_bias_dev, c->channels),
+                      floats(grad_h0_dev, ends),
+                      steps_span(x_dev, *c, c->x_batch, c->x_step),
+                      steps_span(delta_dev, *c, c->delta_batch, c->delta_step),
+                      steps_span(b_dev, shared, c->b_batch, c->b_step),
+                      steps_span(c_dev, shared, c->c_batch, c->c_step),
+                      steps_span(gate_dev, *c, c->gate_batch, c->gate_step),
+                      steps_span(grad_out_dev, *c, c->out_batch, c->out_step),
+                      floats(a_dev, c->channels * c->states),
+                      floats(d_dev, c->channels),
+                      floats(delta_bias_dev, c->channels),
+                      floats(h0_dev, ends),
+                      floats(grad_last_dev, ends),
+                      floats(lengths_dev, c->batch)};
+  REQUIRE(!any_overlap(s, 10, 22), "a buffer that is written overlaps another one");
+  const ScanIn in = {x_dev, delta_dev, a_dev, b_dev, c_dev, d_dev, gate_dev, delta_bias_dev, h0_dev, lengths_dev};
+  const ScanGradients g = {grad_out_dev, grad_last_dev, grad_x_dev, grad_delta_dev, grad_a_dev, grad_b_dev, grad_c_dev,
+                           grad_d_dev, grad_gate_dev, grad_delta_bias_dev, grad_h0_dev};
+  char* const ws = static_cast<char*>(workspace_dev);
+  if (c->type == ACC_BF16) backward<bf16>(*c, p, in, g, ws, queue);
+  else backward<float>(*c, p, in, g, ws, queue);
+  return launched(queue);
+}
+
+}  // extern "C"

@@ -1,0 +1,233 @@
+"""Log probabilities, entropies and most probable tokens, and their gradient, against their definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2010_16248_amd import binding as B
+from tests import more_operators_plain as M
+from tests.operators_plain import assert_within, f64
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16 = torch.float32, torch.bfloat16
+INF, NAN = float("inf"), float("nan")
+
+
+def make(rows, vocab, kind=F32, seed=0, index=torch.int64, scale=3.0):
+    gen = torch.Generator().manual_seed(seed)
+    logits = (torch.randn(rows, vocab, generator=gen) * scale + torch.randn(rows, 1, generator=gen) * 5).to(kind).to(DEV)
+    ids = torch.randint(0, vocab, (rows,), generator=gen)
+    if rows > 2:
+        ids[rows // 2] = -100
+        ids[rows - 1] = vocab
+    return logits, ids.to(index).to(DEV)
+
+
+def forward(logits, ids, top=0, index=torch.int64, **kw):
+    rows = logits.numel() // logits.shape[-1]
+    e = lambda *s: torch.full(s, 7.0, device=DEV)
+    r = dict(logprob=e(rows), lse=e(rows), entropy=e(rows), top_logprobs=e(rows, top) if top else None,
+             top_ids=torch.full((rows, top), 7, dtype=index, device=DEV) if top else None)
+    B.logprob_forward(logits, ids, **r, **kw)
+    return r
+
+
+def check_forward(logits, ids, top=0, index=torch.int64):
+    r = forward(logits, ids, top, index)
+    lse, lp, entropy, lse_off, lp_off, ent_off = M.logprob(logits)
+    vocab, where = logits.shape[1], ids.cpu().numpy().astype(np.int64)
+    named = (where >= 0) & (where < vocab)
+    pick = np.where(named, where, 0)[:, None]
+    assert_within(r["lse"], lse, lse_off, "lse")
+    assert_within(r["logprob"], np.where(named, np.take_along_axis(lp, pick, 1)[:, 0], 0), np.where(named, np.take_along_axis(lp_off, pick, 1)[:, 0], 0), "logprob")
+    assert_within(r["entropy"], entropy, ent_off, "entropy")
+    if top:
+        best = M.best(logits, top)
+        assert np.array_equal(r["top_ids"].cpu().numpy(), best), "top_ids"
+        off = np.take_along_axis(lp_off, best, 1)
+        off[np.isinf(off) | np.isnan(off)] = 0
+        assert_within(r["top_logprobs"], np.take_along_axis(lp, best, 1), off, "top_logprobs")
+    return r
+
+
+def backward(logits, ids, lse, g, out=None, **kw):
+    out = torch.full_like(logits, 7.0) if out is None else out
+    B.logprob_backward(logits, ids, lse, g, out, **kw)
+    return out
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("rows,vocab,top", [(1, 1, 1), (3, 2, 2), (5, 64, 64), (2, 65, 3), (7, 1000, 5), (3, 1025, 20), (4, 2049, 1), (3, 8192, 64),
+                                            (2, 8193, 7), (2, 32768, 20), (1, 131072, 32), (1, 300001, 64), (300, 9001, 4), (1100, 700, 2), (3, 5000, 0),
+                                            (1, 20000, 0), (1300, 100, 0), (2, 131071, 0)])
+def test_rows_and_vocabularies(rows, vocab, top, kind):
+    print(f"case {rows} {vocab} {top} {kind}", flush=True)
+    logits, ids = make(rows, vocab, kind)
+    check_forward(logits, ids, top)
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("vocab", [30, 5000, 40000])
+def test_ties_go_to_the_lowest_index(vocab, kind):
+    """Few different values, and one alone: more equal logits than any list holds."""
+    print(f"case ties {vocab} {kind}", flush=True)
+    gen = torch.Generator().manual_seed(1)
+    logits = torch.randint(0, 3, (4, vocab), generator=gen).to(kind).to(DEV)
+    logits[1] = 2.5
+    logits[2] = -0.0
+    logits[2, ::2] = 0.0
+    check_forward(logits, torch.zeros(4, dtype=torch.int64, device=DEV), 20)
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("vocab", [100, 9000, 70000])
+@pytest.mark.parametrize("top", [0, 12])
+def test_masks(top, vocab, kind):
+    """Tokens at -infinity or the type's lowest value, up to whole rows of them."""
+    print(f"case masks {top} {vocab} {kind}", flush=True)
+    logits, _ = make(7, vocab, kind)
+    low = torch.finfo(kind).min
+    logits[0, 10:] = -INF                 # ten tokens left
+    logits[1] = -INF
+    logits[1, vocab - 1] = 3.0            # one
+    logits[2] = low
+    logits[3, : vocab - 3] = low
+    logits[4] = low
+    logits[4, 5] = -INF
+    logits[5, ::2] = -INF
+    ids = torch.tensor([0, vocab - 1, 3, vocab - 1, 5, 0, 1], device=DEV)
+    r = check_forward(logits, ids, top)
+    assert r["entropy"][1] == 0 and r["logprob"][1] == 0 and r["logprob"][4] == -INF and r["logprob"][5] == -INF
+    logits[6] = -INF                      # a row without a token
+    r = forward(logits, ids, top)
+    assert r["lse"][6] == -INF and r["logprob"][6] == -INF and r["entropy"][6] == 0
+    if top:
+        assert (r["top_logprobs"][6] == -INF).all() and r["top_ids"][6].tolist() == list(range(top))
+    g = torch.randn(7, device=DEV)
+    for kw in (dict(), dict(entropy=r["entropy"], grad_entropy=g)):
+        got = backward(logits, ids, r["lse"], g, **kw)
+        ref, off = M.logprob_gradient(logits, ids, r["lse"], g, kw.get("entropy"), kw.get("grad_entropy"))
+        assert_within(got, ref, off, "gradient")
+        assert not got[6].any() and not got[1].any()
+
+
+@pytest.mark.parametrize("vocab", [50, 20000])
+@pytest.mark.parametrize("top", [0, 6])
+def test_infinities_and_nan(top, vocab):
+    logits, ids = make(3, vocab)
+    ids = torch.tensor([1, 2, 3], device=DEV)
+    logits[0, 7] = INF
+    logits[1, 9] = NAN
+    logits[2, 11] = NAN
+    logits[2, 12] = INF
+    r = forward(logits, ids, top)
+    for k in ("logprob", "lse", "entropy"):
+        assert torch.isnan(r[k]).all(), k
+    if top:
+        assert np.array_equal(r["top_ids"].cpu().numpy(), M.best(logits, top))
+        assert torch.isnan(r["top_logprobs"]).all()
+    assert torch.isnan(backward(logits, ids, r["lse"], torch.ones(3, device=DEV))).all()
+    few = torch.full((1, 8), NAN, device=DEV)
+    few[0, 3], few[0, 5] = -INF, 2.0
+    assert forward(few, ids[:1], 5)["top_ids"][0].tolist() == [5, 3, 0, 1, 2]
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("rows,vocab", [(1, 1), (3, 5), (9, 1000), (2, 4097), (2, 33333), (1, 131072), (2100, 9)])
+@pytest.mark.parametrize("entropy", [False, True])
+def test_gradients(entropy, rows, vocab, kind):
+    print(f"case gradient {rows} {vocab} {kind} {entropy}", flush=True)
+    logits, ids = make(rows, vocab, kind, index=torch.int32)
+    r = forward(logits, ids, index=torch.int32)
+    g, ge = torch.randn(rows, device=DEV), torch.randn(rows, device=DEV)
+    kw = dict(entropy=r["entropy"], grad_entropy=ge) if entropy else {}
+    ref, off = M.logprob_gradient(logits, ids, r["lse"], g, kw.get("entropy"), kw.get("grad_entropy"))
+    got = backward(logits, ids, r["lse"], g, **kw)
+    assert_within(got, ref, off, "gradient")
+    if entropy:
+        ref, off = M.logprob_gradient(logits, None, r["lse"], None, r["entropy"], ge)
+        assert_within(backward(logits, None, r["lse"], None, **kw), ref, off, "gradient of the entropy")
+    # in place
+    assert torch.equal(backward(logits, ids, r["lse"], g, out=logits, **kw), got)
+
+
+def test_rows_without_a_token_have_no_gradient_whatever_they_hold():
+    logits, ids = make(4, 3000)
+    ids[1] = -1
+    logits[1, 5] = NAN
+    r = forward(logits, ids)
+    got = backward(logits, ids, r["lse"], torch.ones(4, device=DEV))
+    assert not got[1].any() and not torch.isnan(got).any() and r["logprob"][1] == 0
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("top", [0, 9])
+def test_rows_apart(top, kind):
+    wide, ids = make(6, 5000, kind)
+    logits = wide[:, 3:4004]
+    plain = forward(logits.contiguous(), ids, top)
+    r = forward(logits, ids, top)
+    for k, v in plain.items():
+        assert v is None or torch.equal(v, r[k]), k
+    g = torch.randn(6, device=DEV)
+    outs = torch.full((6, 4100), 9.0, dtype=kind, device=DEV)
+    got = backward(logits, ids, r["lse"], g, out=outs[:, 50:4051])
+    assert torch.equal(got, backward(logits.contiguous(), ids, r["lse"], g))
+    assert (outs[:, :50] == 9.0).all() and (outs[:, 4051:] == 9.0).all()
+
+
+def test_what_may_be_left_out():
+    logits, ids = make(5, 9000, index=torch.int32)
+    whole = forward(logits, ids, 8, torch.int32)
+    e = lambda *s: torch.empty(*s, device=DEV)
+    lse = e(5)
+    B.logprob_forward(logits, lse=lse)
+    assert_within(lse, f64(whole["lse"]), 1e-5, "lse")
+    values, at = e(5, 8), torch.empty(5, 8, dtype=torch.int64, device=DEV)
+    B.logprob_forward(logits, top_logprobs=values, top_ids=at)
+    assert torch.equal(values, whole["top_logprobs"]) and torch.equal(at, whole["top_ids"].long())
+    lp = e(5)
+    B.logprob_forward(logits, ids, lp)
+    assert_within(lp, f64(whole["logprob"]), 1e-4, "logprob")
+
+
+def test_nothing_to_do():
+    logits, ids = make(0, 100)
+    forward(logits, ids, 5)
+    backward(logits, ids, torch.empty(0, device=DEV), torch.empty(0, device=DEV))
+
+
+def test_batches_of_sequences_are_rows():
+    logits, ids = make(12, 300)
+    flat = forward(logits, ids, 3)
+    r = forward(logits.view(3, 4, 300), ids.view(3, 4), 3)
+    assert all(torch.equal(flat[k], r[k]) for k in flat)
+
+
+def test_the_same_bits_every_time():
+    logits, ids = make(40, 50000, BF16)
+    first = forward(logits, ids, 30)
+    for _ in range(3):
+        again = forward(logits, ids, 30)
+        assert all(torch.equal(first[k], again[k]) for k in first)
+
+
+def test_the_largest_vocabulary():
+    print("case largest vocabulary", flush=True)
+    logits, ids = make(1, 1 << 22, scale=1.0)
+    logits[0, -1] = 50.0
+    check_forward(logits, ids, 64)
+
+
+def test_places_beyond_2_to_the_31():
+    print("case large", flush=True)
+    stride = (1 << 31) + 16
+    wide = torch.zeros(stride + 5000, dtype=BF16, device=DEV)
+    logits, ids = make(2, 4000, BF16)
+    far = wide.as_strided((2, 4000), (stride, 1))
+    far.copy_(logits)
+    plain, r = forward(logits, ids, 5), forward(far, ids, 5)
+    assert all(torch.equal(plain[k], r[k]) for k in plain)
+    g = torch.randn(2, device=DEV)
+    ref = backward(logits, ids, r["lse"], g)
+    assert torch.equal(backward(far, ids, r["lse"], g, out=far), ref)

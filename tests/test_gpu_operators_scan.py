@@ -1,0 +1,258 @@
+"""The selective scan against its definition in 64 bits."""
+import pytest
+import torch
+
+from paper_2010_16248_amd import binding as B
+from tests import more_operators_plain as M
+from tests.operators_plain import assert_within
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def make(batch, steps, channels, states, kind=F32, groups=1, seed=0, gate=True, softplus=True, d=True, bias=True, h0=True, lengths=None):
+    gen = torch.Generator().manual_seed(seed)
+    r = lambda *s, k=F32: torch.randn(*s, generator=gen).to(k).to(DEV)
+    s = dict(x=r(batch, steps, channels, k=kind), b=r(batch, steps, groups, states, k=kind), c=r(batch, steps, groups, states, k=kind),
+             a=-torch.exp(r(channels, states)), d=r(channels) if d else None, gate=r(batch, steps, channels, k=kind) if gate else None,
+             softplus=softplus, h0=r(batch, channels, states) if h0 else None,
+             lengths=None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device=DEV))
+    if softplus:
+        s.update(delta=r(batch, steps, channels, k=kind), delta_bias=r(channels) - 2 if bias else None)
+    else:
+        s.update(delta=(torch.rand(batch, steps, channels, generator=gen) * 0.3).to(kind).to(DEV),
+                 delta_bias=torch.rand(channels, generator=gen).to(DEV) * 0.1 if bias else None)
+    s["dout"], s["dlast"] = r(batch, steps, channels, k=kind), r(batch, channels, states)
+    return s
+
+
+ARGS = ("x", "delta", "a", "b", "c")
+OPTIONS = ("d", "gate", "delta_bias", "softplus", "h0", "lengths")
+
+
+def forward(s, **kw):
+    out = torch.full_like(s["x"], 7.0)
+    last = torch.full_like(s["dlast"], 7.0)
+    B.scan_forward(*(s[k] for k in ARGS), out, h_last=last, **{k: s[k] for k in OPTIONS}, **kw)
+    return out, last
+
+
+def backward(s, dlast=True, start=None, **kw):
+    """{name: gradient}; start: what parameters' gradients hold before."""
+    like = lambda t: None if t is None else torch.full_like(t, 7.0)
+    g = {k: like(s[k]) for k in ("x", "delta", "a", "b", "c", "d", "gate", "delta_bias")}
+    if start is not None:
+        g.update({k: v.clone() for k, v in start.items()})
+    g["h0"] = torch.full_like(s["dlast"], 7.0)
+    B.scan_backward(*(s[k] for k in ARGS), s["dout"], *(g[k] for k in ARGS), grad_d=g["d"], grad_gate=g["gate"],
+                    grad_delta_bias=g["delta_bias"], grad_last=s["dlast"] if dlast else None, grad_h0=g["h0"],
+                    **{k: s[k] for k in OPTIONS}, **kw)
+    return g
+
+
+def check(s, dlast=True, back=True):
+    ref = M.Scan(*(s[k] for k in ARGS), **{k: s[k] for k in OPTIONS})
+    out, last = forward(s)
+    assert_within(out, ref.out, ref.out_off, "out")
+    assert_within(last, ref.last, ref.last_off, "h_last")
+    if not back:
+        return
+    refs, offs = ref.gradients(s["dout"], s["dlast"] if dlast else None)
+    for name, got in backward(s, dlast).items():
+        if got is not None:
+            assert_within(got, refs[name].reshape(got.shape), offs[name].reshape(got.shape), f"gradient of {name}")
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("states", [1, 3, 4, 5, 8, 9, 16, 17, 32, 33, 64])
+@pytest.mark.parametrize("shape", [(1, 1, 1), (2, 9, 5), (2, 70, 67)])
+def test_states_and_shapes(shape, states, kind):
+    print(f"case {shape} {states} {kind}", flush=True)
+    check(make(*shape, states, kind, gate=states % 2 == 0, softplus=states % 3 != 0, seed=states))
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("shape,states,groups", [((1, 700, 64), 16, 1), ((3, 33, 130), 16, 2), ((2, 200, 99), 7, 3), ((1, 1200, 3), 2, 3),
+                                                 ((9, 40, 320), 16, 4), ((2, 50, 96), 40, 2), ((70, 11, 20), 4, 1)])
+def test_chunks_blocks_and_groups(shape, states, groups, kind):
+    print(f"case {shape} {states} {groups} {kind}", flush=True)
+    check(make(*shape, states, kind, groups=groups))
+
+
+@pytest.mark.parametrize("steps", [1, 2, 7, 8, 9, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129])
+def test_lengths_around_turns_and_chunks(steps):
+    print(f"case steps {steps}", flush=True)
+    check(make(2, steps, 10, 16, seed=steps))
+
+
+def test_one_chunk_of_many_waves():
+    """Sequences enough to fill the chip: no chunks in the forward pass."""
+    print("case wide", flush=True)
+    check(make(1100, 20, 2, 2, BF16), back=False)
+    check(make(130, 30, 520, 3), back=False)
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("states", [4, 16, 20])
+@pytest.mark.parametrize("steps", [5, 77])
+def test_lengths_leave_what_lies_behind_alone(steps, states, kind):
+    """Lengths of zero, below zero and beyond the steps; what padded places hold plays no role."""
+    lengths = [0, -3, 1, 2, 5, 40, 77, 99]
+    s = make(8, steps, 19, states, kind, lengths=lengths)
+    for i, n in enumerate(lengths):
+        for k in ("x", "delta", "b", "c", "gate", "dout"):
+            s[k][i, max(n, 0):] = float("nan") if i % 2 else float("inf")
+    print(f"case lengths {steps} {states} {kind}", flush=True)
+    check(s)
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("steps", [3, 100])
+def test_what_may_be_left_out(steps, kind):
+    s = make(2, steps, 70, 16, kind, gate=False, softplus=False, d=False, bias=False, h0=False)
+    check(s, dlast=False)
+    s = make(2, steps, 70, 16, kind, bias=False, h0=False)
+    check(s, dlast=False)
+    out = torch.empty_like(s["x"])
+    B.scan_forward(*(s[k] for k in ARGS), out, d=s["d"], gate=s["gate"], softplus=True)
+    assert torch.equal(out, forward(s)[0])
+    g = backward(s, dlast=False)
+    less = {k: torch.empty_like(s[k]) for k in (*ARGS, "gate")}
+    B.scan_backward(*(s[k] for k in ARGS), s["dout"], *(less[k] for k in ARGS), d=s["d"], gate=s["gate"], grad_gate=less["gate"], softplus=True)
+    for k, v in less.items():
+        assert torch.equal(v, g[k]), k
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("steps", [4, 90])
+def test_rows_apart(steps, kind):
+    """Every tensor as columns of a wider one, sequences interleaved; b and c without a dimension of groups."""
+    print(f"case strides {steps} {kind}", flush=True)
+    s = make(3, steps, 21, 5, kind)
+    plain = (*forward(s), *backward(s).values())
+    put = dict(s)
+    wide = torch.zeros(steps, 3, 200, dtype=kind, device=DEV).transpose(0, 1)
+    at = 1
+    for k in ("x", "delta", "gate", "dout", "b", "c"):
+        n = s[k].shape[-1]
+        put[k] = wide[..., at:at + n]
+        put[k].copy_(s[k].reshape(put[k].shape))
+        at += n + 2
+    outs = torch.full((steps, 3, 200), 9.0, dtype=kind, device=DEV).transpose(0, 1)
+    used, at, o = torch.zeros(200, dtype=torch.bool), 3, {}
+    for k in ("out", "x", "delta", "gate", "b", "c"):
+        n = 5 if k in "bc" else 21
+        o[k] = outs[..., at:at + n]
+        used[at:at + n] = True
+        at += n + 3
+    last, g = torch.empty_like(s["dlast"]), {k: torch.empty_like(s[k]) for k in ("a", "d", "delta_bias", "h0")}
+    B.scan_forward(*(put[k] for k in ARGS), o["out"], h_last=last, **{k: put[k] for k in OPTIONS})
+    B.scan_backward(*(put[k] for k in ARGS), put["dout"], o["x"], o["delta"], g["a"], o["b"], o["c"], grad_d=g["d"], grad_gate=o["gate"],
+                    grad_delta_bias=g["delta_bias"], grad_last=s["dlast"], grad_h0=g["h0"], **{k: put[k] for k in OPTIONS})
+    got = (o["out"], last, o["x"], o["delta"], g["a"], o["b"], o["c"], g["d"], o["gate"], g["delta_bias"], g["h0"])
+    for i, (a, b) in enumerate(zip(plain, got)):
+        assert torch.equal(a.reshape(b.shape), b), i
+    assert (outs[..., ~used.to(DEV)] == 9.0).all()
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("states", [1, 6, 16, 24, 50])
+def test_token_by_token_is_the_whole(states, kind):
+    """The serving form, the state in one buffer; and prompts in pieces."""
+    s = make(3, 40, 37, states, kind)
+    ref = M.Scan(*(s[k] for k in ARGS), **{k: s[k] for k in OPTIONS})
+    for pieces in ([1] * 40, [5, 30, 4, 1], [33, 7]):
+        state, at = s["h0"].clone(), 0
+        for n in pieces:
+            out = torch.empty_like(s["x"][:, at:at + n]).contiguous()
+            of = lambda k: None if s[k] is None else s[k][:, at:at + n]
+            B.scan_forward(of("x"), of("delta"), s["a"], of("b"), of("c"), out, d=s["d"], gate=of("gate"), delta_bias=s["delta_bias"],
+                           softplus=s["softplus"], h0=state, h_last=state)
+            assert_within(out, ref.out[:, at:at + n], ref.out_off[:, at:at + n], f"out {pieces} at {at}")
+            at += n
+        assert_within(state, ref.last, ref.last_off, "state")
+
+
+@pytest.mark.parametrize("steps", [3, 300])
+def test_states_in_place_of_sequences_of_any_length(steps):
+    s = make(5, steps, 70, 16, lengths=[0, 1, steps, steps // 2, 2])
+    out, last = forward(s)
+    state, again = s["h0"].clone(), torch.empty_like(out)
+    B.scan_forward(*(s[k] for k in ARGS), again, h_last=state, **{**{k: s[k] for k in OPTIONS}, "h0": state})
+    assert torch.equal(state, last) and torch.equal(out, again)
+
+
+def test_gradients_are_added():
+    s = make(2, 50, 70, 16)
+    g = backward(s)
+    start = {k: torch.randn_like(g[k]) for k in ("a", "d", "delta_bias")}
+    more = backward(s, start=start, accumulate=True)
+    for k in g:
+        assert torch.equal(more[k], start[k] + g[k] if k in start else g[k]), k
+
+
+@pytest.mark.parametrize("shape", [(0, 5, 3), (2, 0, 3), (0, 0, 3)])
+def test_nothing_to_do(shape):
+    s = make(*shape, 4)
+    _, last = forward(s)
+    assert torch.equal(last, s["h0"])
+    g = backward(s)
+    assert not g["a"].any() and not g["d"].any() and not g["delta_bias"].any() and torch.equal(g["h0"], s["dlast"])
+    start = {k: torch.full_like(g[k], 3.0) for k in ("a", "d", "delta_bias")}
+    more = backward(s, start=start, accumulate=True)
+    assert all((more[k] == 3.0).all() for k in start)
+
+
+def test_the_same_bits_every_time():
+    s = make(3, 500, 200, 16, BF16)
+    first = (*forward(s), *backward(s).values())
+    for _ in range(3):
+        for a, b in zip(first, (*forward(s), *backward(s).values())):
+            assert torch.equal(a, b)
+
+
+def test_open_and_shut_decays():
+    """dt of zero keeps the state, a large one forgets it; softplus far on both sides."""
+    s = make(2, 90, 20, 16)
+    s["delta"][:, ::3] = -150.0
+    s["delta"][:, 1::3] = 60.0
+    s["delta"][:, 2::9] = -20.0
+    check(s)
+    s = make(2, 90, 20, 16, softplus=False, bias=False)
+    s["delta"][:, ::2] = 0.0
+    check(s)
+
+
+def test_growing_states():
+    s = make(2, 40, 20, 5)
+    s["a"] = -0.1 * s["a"]
+    check(s)
+
+
+def test_places_beyond_2_to_the_31():
+    step = (1 << 30) + 8
+    s = make(1, 3, 40, 16, BF16)
+    t = make(1, 20, 40, 16, BF16)
+    plain = (*forward(s), *backward(s).values())
+    big = torch.zeros(2 * step + 64, dtype=BF16, device=DEV)
+    print("case large", flush=True)
+    x = big.as_strided((1, 3, 40), (0, step, 1))
+    x.copy_(s["x"])
+    s["x"] = x
+    g = {k: torch.empty_like(s[k]).contiguous() for k in (*ARGS, "d", "gate", "delta_bias", "h0")}
+    out, last = torch.empty(1, 3, 40, dtype=BF16, device=DEV), torch.empty_like(s["dlast"])
+    B.scan_forward(*(s[k] for k in ARGS), out, h_last=last, **{k: s[k] for k in OPTIONS})
+    g["x"] = torch.empty(1, 3, 40, dtype=BF16, device=DEV)
+    B.scan_backward(*(s[k] for k in ARGS), s["dout"], *(g[k] for k in ARGS), grad_d=g["d"], grad_gate=g["gate"],
+                    grad_delta_bias=g["delta_bias"], grad_last=s["dlast"], grad_h0=g["h0"], **{k: s[k] for k in OPTIONS})
+    got = (out, last, *(g[k] for k in ("x", "delta", "a", "b", "c", "d", "gate", "delta_bias", "h0")))
+    for i, (a, b) in enumerate(zip(plain, got)):
+        assert torch.equal(a, b), i
+    plain = forward(t)
+    far = big.as_strided((1, 20, 40), (0, step // 10, 1))
+    far.copy_(t["x"])
+    t["x"] = far
+    out = torch.empty(1, 20, 40, dtype=BF16, device=DEV)
+    B.scan_forward(*(t[k] for k in ARGS), out, h_last=last, **{k: t[k] for k in OPTIONS})
+    assert torch.equal(out, plain[0]) and torch.equal(last, plain[1])
