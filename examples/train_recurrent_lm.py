@@ -6,7 +6,11 @@ feedback (accordion_step_all), and the averaged gradient it returns, clipped by 
 At the end of a window Accordion decides each layer's compression level, and after training the model continues a text token by
 token from the recurrent state.  Products with weight matrices and the loss are torch's; everything else above is the library's.
 
+--mixer scan: in the recurrence's place a short convolution and a selective state space scan, gated, and the loss is the library's too (the tokens'
+log probabilities).
+
     python examples/train_recurrent_lm.py --steps 200
+    python examples/train_recurrent_lm.py --mixer scan
 """
 from __future__ import annotations
 
@@ -75,14 +79,81 @@ class Recurrence(torch.autograd.Function):
         return grads, None
 
 
+class Convolution(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, state):
+        out, last = torch.empty_like(x, memory_format=torch.contiguous_format), torch.empty_like(state)
+        B.convolution_forward(x, weight, out, bias=bias, state=state, last=last, silu=True)
+        ctx.save_for_backward(x, weight, bias, state)
+        ctx.mark_non_differentiable(last)
+        return out, last
+
+    @staticmethod
+    def backward(ctx, grad, _):
+        x, weight, bias, state = ctx.saved_tensors
+        dx, dw, db = torch.empty_like(grad), torch.empty_like(weight), torch.empty_like(bias)
+        B.convolution_backward(x, weight, grad.contiguous(), dx, dw, bias=bias, grad_bias=db, state=state, silu=True)
+        return dx, dw, db, None
+
+
+class Scan(torch.autograd.Function):
+    """shared: b and c side by side."""
+
+    @staticmethod
+    def forward(ctx, x, delta, log_a, shared, d, gate, delta_bias, h0):
+        a, n = -torch.exp(log_a), log_a.shape[1]
+        out, last = torch.empty_like(x), torch.empty_like(h0)
+        B.scan_forward(x, delta, a, shared[..., :n], shared[..., n:], out, d=d, gate=gate, delta_bias=delta_bias, softplus=True, h0=h0, h_last=last)
+        ctx.save_for_backward(x, delta, a, shared, d, gate, delta_bias, h0)
+        ctx.mark_non_differentiable(last)
+        return out, last
+
+    @staticmethod
+    def backward(ctx, grad, _):
+        x, delta, a, shared, d, gate, delta_bias, h0 = ctx.saved_tensors
+        n, grads = a.shape[1], [torch.empty_like(t) for t in (x, delta, a, shared, d, x, delta_bias)]
+        dx, ddelta, da, dshared, dd, dgate, dbias = grads
+        B.scan_backward(x, delta, a, shared[..., :n], shared[..., n:], grad.contiguous(), dx, ddelta, da, dshared[..., :n], dshared[..., n:], d=d,
+                        grad_d=dd, gate=gate, grad_gate=dgate, delta_bias=delta_bias, grad_delta_bias=dbias, softplus=True, h0=h0)
+        return dx, ddelta, da * a, dshared, dd, dgate, dbias, None
+
+
+class LogProb(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, targets):
+        logprob, lse = (torch.empty(len(targets), device=logits.device) for _ in range(2))
+        B.logprob_forward(logits, targets, logprob, lse=lse)
+        ctx.save_for_backward(logits, targets, lse)
+        return logprob
+
+    @staticmethod
+    def backward(ctx, grad):
+        logits, targets, lse = ctx.saved_tensors
+        out = torch.empty_like(logits)
+        B.logprob_backward(logits, targets, lse, grad.contiguous(), out)
+        return out, None
+
+
+WIDTH, STATES = 4, 16       # of the convolution, of a channel
+
+
+def loss_of(model, logits, targets):
+    if model.mixer == "scan":
+        return -LogProb.apply(logits, targets).mean()
+    return torch.nn.functional.cross_entropy(logits, targets)
+
+
 class Model:
     """Parameters as views of one flat buffer; gradients of a worker as views of another one."""
 
-    def __init__(self, vocab: int, dim: int, device: str, seed: int):
+    def __init__(self, vocab: int, dim: int, device: str, seed: int, mixer: str = "recurrence"):
         gen = torch.Generator(device=device).manual_seed(seed)
-        self.vocab, self.dim = vocab, dim
+        self.vocab, self.dim, self.mixer = vocab, dim, mixer
         self.shapes = {"table": (vocab, dim), "norm1.weight": (dim,), "norm1.bias": (dim,), "project": (2 * dim, dim),
                        "project.bias": (2 * dim,), "norm2.weight": (dim,), "norm2.bias": (dim,), "decoder": (vocab, dim)}
+        if mixer == "scan":
+            self.shapes.update({"conv": (dim, WIDTH), "conv.bias": (dim,), "steps": (dim, dim), "steps.bias": (dim,), "shared": (2 * STATES, dim),
+                                "log_a": (dim, STATES), "skip": (dim,)})
         self.sizes = [math.prod(s) for s in self.shapes.values()]
         self.flat = torch.empty(sum(self.sizes), device=device)
         self.p = dict(zip(self.shapes, (v.view(s) for v, s in zip(self.flat.split(self.sizes), self.shapes.values()))))
@@ -91,7 +162,13 @@ class Model:
                 p.normal_(0.0, dim ** -0.5, generator=gen)
             else:
                 p.fill_(1.0 if name.endswith("weight") else 0.0)
-        self.p["project.bias"][:dim] = torch.linspace(-1.0, 4.0, dim, device=device)     # memories of different lengths
+        if mixer == "scan":
+            # states that remember for 1 / n steps of dt, dt from 0.001 to 0.1 by channel
+            self.p["log_a"][:] = torch.arange(1, STATES + 1, device=device).float().log()
+            self.p["steps.bias"][:] = torch.expm1(torch.linspace(math.log(1e-3), math.log(1e-1), dim, device=device).exp()).log()
+            self.p["skip"].fill_(1.0)
+        else:
+            self.p["project.bias"][:dim] = torch.linspace(-1.0, 4.0, dim, device=device)     # memories of different lengths
         for p in self.p.values():
             p.requires_grad_(True)
 
@@ -108,11 +185,27 @@ class Model:
         for p, g in zip(self.p.values(), flat.split(self.sizes)):
             p.grad = g.view(p.shape)
 
+    def first_state(self, batch: int, device: str):
+        if self.mixer == "scan":
+            return torch.zeros(batch, WIDTH - 1, self.dim, device=device), torch.zeros(batch, self.dim, STATES, device=device)
+        return torch.zeros(batch, self.dim, device=device)
+
+    def mix(self, both, state):
+        """What the mixing layer makes of its projection, and the state behind it."""
+        p, c = self.p, self.dim
+        if self.mixer != "scan":
+            return Recurrence.apply(both, state)
+        front, h0 = state
+        u, front = Convolution.apply(both[..., :c], p["conv"], p["conv.bias"], front)
+        delta, shared = u @ p["steps"].t(), u @ p["shared"].t()
+        y, last = Scan.apply(u, delta, p["log_a"], shared, p["skip"], both[..., c:], p["steps.bias"], h0)
+        return y, (front, last)
+
     def __call__(self, ids, h0):
         p = self.p
         x = LayerNorm.apply(Embedding.apply(p["table"], ids, math.sqrt(self.dim)), p["norm1.weight"], p["norm1.bias"])
         both = torch.addmm(p["project.bias"], x.view(-1, self.dim), p["project"].t()).view(*ids.shape, -1)
-        h, last = Recurrence.apply(both, h0)
+        h, last = self.mix(both, h0)
         y = LayerNorm.apply(h, p["norm2.weight"], p["norm2.bias"])
         return y.view(-1, self.dim) @ p["decoder"].t(), last
 
@@ -129,22 +222,22 @@ def text(gen, batch: int, steps: int, vocab: int, device: str):
 
 
 def train(steps: int = 200, workers: int = 2, batch: int = 8, length: int = 64, vocab: int = 257, dim: int = 96, lr: float = 4e-3,
-          window: int = 20, device: str = "cuda:0", say=print):
+          window: int = 20, device: str = "cuda:0", say=print, mixer: str = "recurrence"):
     """Losses of the steps, and how much of a continued text follows the rule."""
-    model, gen = Model(vocab, dim, device, 1), torch.Generator(device=device).manual_seed(2)
+    model, gen = Model(vocab, dim, device, 1, mixer), torch.Generator(device=device).manual_seed(2)
     n = model.flat.numel()
     accordion = B.Accordion(B.ACC_TOPK, model.layers(), workers, 20, 5, device=device)
     state = B.adamw_state(model.sizes, 8, device)
     grads, mean = [torch.zeros(n, device=device) for _ in range(workers)], torch.empty(n, device=device)
     decay = [0.01 if len(s) == 2 else 0.0 for s in model.shapes.values()]
-    h0, losses = torch.zeros(batch, dim, device=device), []
+    h0, losses = model.first_state(batch, device), []
     for step in range(1, steps + 1):
         total = 0.0
         for w in range(workers):
             ids = text(gen, batch, length, vocab, device)
             model.gradients_into(grads[w])
             logits, _ = model(ids[:, :-1].contiguous(), h0)
-            loss = torch.nn.functional.cross_entropy(logits, ids[:, 1:].reshape(-1))
+            loss = loss_of(model, logits, ids[:, 1:].reshape(-1))
             loss.backward()
             total += loss.item() / workers
         losses.append(total)
@@ -158,7 +251,7 @@ def train(steps: int = 200, workers: int = 2, batch: int = 8, length: int = 64, 
             say(f"step {step}: loss {total:.3f}, layers at the accurate level: {int(accordion.get_levels().sum())} of {len(model.sizes)}")
     # continue a text, one token at a time
     with torch.no_grad():
-        token, h = torch.randint(0, vocab, (batch, 1), generator=gen, device=device), h0.clone()
+        token, h = torch.randint(0, vocab, (batch, 1), generator=gen, device=device), h0
         right = 0
         for _ in range(length):
             logits, h = model(token, h)
@@ -173,8 +266,9 @@ def main():
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--steps", type=int, default=200)
     ap.add_argument("--workers", type=int, default=2)
+    ap.add_argument("--mixer", choices=("recurrence", "scan"), default="recurrence")
     a = ap.parse_args()
-    losses, right = train(a.steps, a.workers)
+    losses, right = train(a.steps, a.workers, mixer=a.mixer)
     print(f"loss {losses[0]:.3f} -> {losses[-1]:.3f}; {100 * right:.0f} % of the continued text follows the rule")
 
 
