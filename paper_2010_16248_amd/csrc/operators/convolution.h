@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256) void convolution_forward_kernel(ConvolutionSha
         for (int i = 0; i < N; ++i) u[i] = fmaf(w[k][i], v[j + k][i], u[i]);
       if (SILU)
 #pragma unroll
-        for (int i = 0; i < N; ++i) u[i] *= gates(u[i]).a;
+        for (int i = 0; i < N; ++i) u[i] *= sigmoid(u[i]).a;
       if (t + j < end) store_some<T, N>(to + (t + j) * s.out_t, u, left);
     }
 #pragma unroll
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(256) void convolution_backward_kernel(ConvolutionSh
             for (int i = 0; i < N; ++i) u[i] = fmaf(w[k][i], v[j + k][i], u[i]);
 #pragma unroll
           for (int i = 0; i < N; ++i) {
-            const Gates z = gates(u[i]);
+            const Gates z = sigmoid(u[i]);
             d[i] *= z.a * fmaf(u[i], z.z, 1.f);
           }
           if (t + j >= seen) d = F32<N>{};

@@ -162,28 +162,48 @@ __global__ __launch_bounds__(256) void logprob_stream_kernel(LogprobOut o, const
 constexpr int kTopGroups = 64;
 constexpr int kTopList = 1024;
 
-__device__ __forceinline__ bool before(unsigned key, unsigned id, unsigned other_key, unsigned other_id) {
-  return key > other_key || (key == other_key && id < other_id);
+__device__ __forceinline__ bool before(uint2 a, uint2 b) { return a.x > b.x || (a.x == b.x && a.y < b.y); }
+
+__device__ __forceinline__ float wave_top(float v) {
+  v = fmaxf(v, dpp<0xB1>(v));
+  v = fmaxf(v, dpp<0x4E>(v));
+  v = fmaxf(v, dpp<0x141>(v));
+  v = fmaxf(v, dpp<0x140>(v));
+  return fmaxf(fmaxf(lane(v, 0), lane(v, 16)), fmaxf(lane(v, 32), lane(v, 48)));
+}
+
+// Tokens in front of one of the list's.
+__device__ __forceinline__ int place_in(const uint2* list, int count, uint2 token) {
+  int place = 0;
+  int j = 0;
+  for (; j + 8 <= count; j += 8) {
+    uint2 o[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) o[k] = list[j + k];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) place += before(o[k], token);
+  }
+  for (; j < count; ++j) place += before(list[j], token);
+  return place;
 }
 
 template <typename T, int N, int K, int THREADS, bool PARTS>
 __global__ __launch_bounds__(THREADS) void logprob_top_kernel(LogprobOut o, const T* __restrict__ logits, int64_t part, int parts,
                                                               RowSums* __restrict__ sums, uint2* __restrict__ best) {
-  __shared__ RowSums red[THREADS / kWave];
-  __shared__ unsigned group_top[kTopGroups];
-  __shared__ uint2 list[kTopList];
+  constexpr int waves = THREADS / kWave, each = THREADS / kTopGroups;       // lanes of a group
+  static_assert(each == 4 || each == 16, "groups are whole rows or quarters of rows of 16 lanes");
+  __shared__ float group_top[kTopGroups], sum[waves], weighted[waves], least_of;
   __shared__ unsigned listed;
-  __shared__ uint2 found[THREADS / kWave];
-  constexpr int each = THREADS / kTopGroups;       // lanes of a group
-  static_assert(each >= 4 && each <= 16, "groups lie within 16 lanes");
+  __shared__ uint2 list[kTopList], found[waves];
   const int64_t row = blockIdx.x;
-  const int64_t from = blockIdx.y * part, to = min(from + part, o.vocab);
-  const T* l = logits + row * o.stride;
+  const int64_t from = blockIdx.y * part;
+  const int size = (int)min(part, o.vocab - from);
+  const T* const l = logits + row * o.stride + from;
   Pack<T, N> v[K];
   float top = -INFINITY;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    const int64_t place = from + (threadIdx.x + k * THREADS) * N, left = to - place;
+    const int place = ((int)threadIdx.x + k * THREADS) * N, left = size - place;
     if (left >= N) {
       v[k] = load<N>(l + place);
     } else {
@@ -194,85 +214,92 @@ __global__ __launch_bounds__(THREADS) void logprob_top_kernel(LogprobOut o, cons
   if (threadIdx.x == 0) listed = 0;
 #pragma unroll
   for (int k = 0; k < K; ++k) top = fmaxf(top, top_of<N>(widen<T, N>(v[k])));
+  top = fmaxf(top, dpp<0xB1>(top));
+  top = fmaxf(top, dpp<0x4E>(top));
+  if (each == 16) {
+    top = fmaxf(top, dpp<0x141>(top));
+    top = fmaxf(top, dpp<0x140>(top));
+  }
+  if (threadIdx.x % each == 0) group_top[threadIdx.x / each] = top;
+  __syncthreads();
+  const float own = group_top[threadIdx.x & 63];
   RowSums r = no_sums();
-  r.top = fmaxf(r.top, top);
+  r.top = fmaxf(kLowest, wave_top(own));
+  if (threadIdx.x < kWave) {
+    // the least of the maxima that have fewer than `top` larger ones
+    int larger = 0;
+#pragma unroll 16
+    for (int i = 0; i < kTopGroups; ++i) larger += lane(own, i) > own;
+    const float least = -wave_top(larger < o.top ? -own : -INFINITY);
+    if (threadIdx.x == 0) least_of = least;
+  }
 #pragma unroll
   for (int k = 0; k < K; ++k) add_pack<N, true>(r, widen<T, N>(v[k]));
-  // the groups' maxima (of NaN and -infinity alone: the order's lowest)
-  unsigned key = top == -INFINITY ? 0u : key_of(top + 0.f);
-#pragma unroll
-  for (int m = 1; m < each; m *= 2) key = max(key, (unsigned)__shfl_xor((int)key, m));
-  if (threadIdx.x % each == 0) group_top[threadIdx.x / each] = key;
-  r = group_sums<THREADS>(r, red);                 // (its barriers are behind what is written above)
-  if (THREADS == kWave) __syncthreads();
-  const int place_of = (int)min((int64_t)o.top, to - from);     // tokens this part can give
-  // the least key that counts: the group whose place in the order is the last of `top`
-  const unsigned own = group_top[threadIdx.x & 63];
-  int rank = 0;
-  for (int i = 0; i < kTopGroups; ++i) {
-    const unsigned other = __builtin_amdgcn_readlane(own, i);
-    rank += other > own || (other == own && i < (int)(threadIdx.x & 63));
+  r.s = wave_sum(r.s);
+  r.t = wave_sum(r.t);
+  if ((threadIdx.x & 63) == 0) {
+    sum[threadIdx.x >> 6] = r.s;
+    weighted[threadIdx.x >> 6] = r.t;
   }
-  const unsigned long long last = __ballot(rank == o.top - 1);
-  const unsigned least = __builtin_amdgcn_readlane(own, __ffsll(last) - 1);
+  __syncthreads();
+  r.s = r.t = 0.f;
+#pragma unroll
+  for (int w = 0; w < waves; ++w) {
+    r.s += sum[w];
+    r.t += weighted[w];
+  }
+  const float least = least_of;
+  // (what is not a number is below no maximum)
 #pragma unroll
   for (int k = 0; k < K; ++k) {
+    const F32<N> wide = widen<T, N>(v[k]);
+    if (top_of<N>(wide) < least) continue;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int64_t place = from + (threadIdx.x + k * THREADS) * N + i;
-      const unsigned mine = key_at(v[k][i]);
-      if (mine >= least && place < to) {
+      const int place = ((int)threadIdx.x + k * THREADS) * N + i;
+      if (!(wide[i] < least) && place < size) {
         const unsigned at = atomicAdd(&listed, 1u);
-        if (at < kTopList) list[at] = make_uint2(mine, (unsigned)place);
+        if (at < kTopList) list[at] = make_uint2(key_at(wide[i]), (unsigned)(from + place));
       }
     }
   }
   __syncthreads();
-  const unsigned count = listed;
+  const int count = (int)listed, wanted = min(o.top, size);     // tokens this part can give
   auto put = [&](int place, uint2 token) {
     if (PARTS) best[(row * parts + blockIdx.y) * o.top + place] = token;
     else write_top(o, row, place, r, logit_of(token.x), token.y);
   };
   if (count <= kTopList) {
-    for (unsigned i = threadIdx.x; i < count; i += THREADS) {
+    for (int i = threadIdx.x; i < count; i += THREADS) {
       const uint2 token = list[i];
-      int place = 0;
-      for (unsigned j = 0; j < count; ++j) place += before(list[j].x, list[j].y, token.x, token.y);
-      if (place < place_of) put(place, token);
+      const int place = place_in(list, count, token);
+      if (place < wanted) put(place, token);
     }
   } else {
-    uint2 after = make_uint2(~0u, 0u);             // in front of every token
-    bool any = false;
-    for (int place = 0; place < place_of; ++place) {
+    uint2 after = make_uint2(~0u, 0u);             // in front of every token: no key is as large
+    for (int place = 0; place < wanted; ++place) {
       uint2 mine = make_uint2(0u, ~0u);            // behind every token
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int64_t id = from + (threadIdx.x + k * THREADS) * N + i;
-          const unsigned other = key_at(v[k][i]);
-          if (id < to && (!any || before(after.x, after.y, other, (unsigned)id)) && before(other, (unsigned)id, mine.x, mine.y))
-            mine = make_uint2(other, (unsigned)id);
-        }
+      for (int at = threadIdx.x; at < size; at += THREADS) {
+        const uint2 other = make_uint2(key_at(l[at]), (unsigned)(from + at));
+        if (before(after, other) && before(other, mine)) mine = other;
       }
 #pragma unroll
       for (int m = 1; m < kWave; m *= 2) {
-        const unsigned x = __shfl_xor((int)mine.x, m), y = __shfl_xor((int)mine.y, m);
-        if (before(x, y, mine.x, mine.y)) mine = make_uint2(x, y);
+        const uint2 other = make_uint2(__shfl_xor((int)mine.x, m), __shfl_xor((int)mine.y, m));
+        if (before(other, mine)) mine = other;
       }
       __syncthreads();
       if ((threadIdx.x & 63) == 0) found[threadIdx.x >> 6] = mine;
       __syncthreads();
-      for (int w = 0; w < THREADS / kWave; ++w)
-        if (before(found[w].x, found[w].y, mine.x, mine.y)) mine = found[w];
+      for (int w = 0; w < waves; ++w)
+        if (before(found[w], mine)) mine = found[w];
       if (threadIdx.x == 0) put(place, mine);
       after = mine;
-      any = true;
     }
   }
   // what a short part does not have comes behind every token
   if (PARTS)
-    for (int place = place_of + threadIdx.x; place < o.top; place += THREADS) put(place, make_uint2(0u, ~0u));
+    for (int place = wanted + threadIdx.x; place < o.top; place += THREADS) put(place, make_uint2(0u, ~0u));
   if (threadIdx.x != 0) return;
   if (PARTS) {
     sums[row * parts + blockIdx.y] = r;
@@ -298,8 +325,7 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobOut o, const T
   for (int i = threadIdx.x; i < count; i += 256) {
     const uint2 token = tokens[i];
     if (token.y == ~0u) continue;
-    int place = 0;
-    for (int j = 0; j < count; ++j) place += before(tokens[j].x, tokens[j].y, token.x, token.y);
+    const int place = place_in(tokens, count, token);
     if (place < o.top) write_top(o, row, place, r, logit_of(token.x), token.y);
   }
   if (threadIdx.x != 0) return;

@@ -114,6 +114,18 @@ __device__ __forceinline__ Gates gates(float f) {
   return f >= 0.f ? Gates{big, small} : Gates{small, big};
 }
 
+// The same for products with f, as SiLU and its derivative take them: half as many instructions.  Below f = -88.5 both are zero (a is below
+// 2^-127 there); their NaN is left to f.
+__device__ __forceinline__ Gates sigmoid(float f) {
+  const float x = __builtin_amdgcn_fmed3f(f, -88.5f, 100.f);
+  const float t = -1.44269502f * x;
+  const float d = fmaf(t, -0.693147182f, -x);
+  float e = __builtin_amdgcn_exp2f(t);
+  e = fmaf(e, d, e);
+  const float a = f < -88.5f ? 0.f : __builtin_amdgcn_rcpf(1.f + e);
+  return {a, e * a};
+}
+
 __device__ __forceinline__ int64_t steps_of(const int32_t* lengths, int64_t batch, int64_t steps) {
   if (!lengths) return steps;
   const int64_t n = lengths[batch];

@@ -21,24 +21,23 @@ __device__ __forceinline__ Shared shared_at(const float* p) { return (Shared)(ui
 
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
-// log(1 + e^r) = max(r, 0) + log(1 + e), e = e^-|r|; log(1 + e) = 2 atanh(s), s = e / (2 + e) <= 1/3, by its series up to s^15 (the next
-// term is below 2^-29 of the sum).
-__device__ __forceinline__ float softplus(float r) {
-  bool far;
-  float e = exp_neg(fabsf(r), &far);
-  e = far ? e * 0x1p-32f : e;
-  const float d = 2.f + e;
-  float q = __builtin_amdgcn_rcpf(d);
-  q = fmaf(fmaf(-d, q, 1.f), q, q);
-  const float s = e * q, z = s * s;
-  float p = 2.f / 15.f;
-  p = fmaf(p, z, 2.f / 13.f);
-  p = fmaf(p, z, 2.f / 11.f);
-  p = fmaf(p, z, 2.f / 9.f);
-  p = fmaf(p, z, 2.f / 7.f);
-  p = fmaf(p, z, 2.f / 5.f);
-  p = fmaf(p, z, 2.f / 3.f);
-  return fmaxf(r, 0.f) + fmaf(p * z, s, 2.f * s);
+// log(1 + e^r) = max(r, 0) + log(1 + e), e = e^-|r|, and its derivative, the sigmoid of r.  log(1 + e) = 2 atanh(s), s = e / (2 + e) <= 1/3;
+// atanh(s) / s = 1 + z q(z), z = s^2, q of degree 3 with the least largest error (fitted: below 2^-27 of the whole).
+struct Softplus {
+  float value, slope;
+};
+__device__ __forceinline__ Softplus softplus(float r) {
+  const float x = fminf(fabsf(r), 100.f);
+  const float t = -1.44269502f * x;
+  const float d = fmaf(t, -0.693147182f, -x);
+  float e = __builtin_amdgcn_exp2f(t);
+  e = fmaf(e, d, e);
+  const float s = e * __builtin_amdgcn_rcpf(2.f + e), z = s * s;
+  float q = fmaf(0.140060782f, z, 0.140008867f);
+  q = fmaf(q, z, 0.200107649f);
+  q = fmaf(q, z, 0.333332092f);
+  const float half = fmaf(q * z, s, s), big = __builtin_amdgcn_rcpf(1.f + e);
+  return {fmaf(2.f, half, r < 0.f ? 0.f : r), r < 0.f ? e * big : big};
 }
 
 // ---- b and c as the scan reads them -----------------------------------------------------------------------
@@ -68,6 +67,7 @@ __global__ __launch_bounds__(256) void scan_pack_kernel(const T* __restrict__ b,
 struct ScanPlace {
   int lane, part, group;
   unsigned block, channel;
+  unsigned byte2, byte4;         // of the channel's element in a row of 2 and of 4 bytes each
   bool valid;
   int64_t batch, chunk;
   int64_t len, from, to, end;    // steps of the sequence, of the chunk, and where both end
@@ -82,6 +82,9 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanShape& s, const int32_
   const int within = (int)(blockIdx.x - (unsigned)p.group * s.blocks) * kWave + p.lane;
   p.valid = within < s.group;
   p.channel = (unsigned)p.group * s.group + (p.valid ? within : s.group - 1);
+  p.byte2 = 2 * p.channel;
+  p.byte4 = 4 * p.channel;
+  asm("" : "+v"(p.byte2), "+v"(p.byte4));      // (a sum of a base in scalar registers and 32 bits, as the loads take it, not one in 64 bits)
   p.chunk = blockIdx.y;
   p.batch = blockIdx.z;
   p.len = steps_of(lengths, p.batch, s.steps);
@@ -93,8 +96,8 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanShape& s, const int32_
 
 // An element of a row that the wave has in common, at a lane's place.
 template <typename T>
-__device__ __forceinline__ T& in_row(T* row, unsigned place) {
-  return *reinterpret_cast<T*>((char*)row + place * (unsigned)sizeof(T));
+__device__ __forceinline__ T& in_row(T* row, const ScanPlace& p) {
+  return *reinterpret_cast<T*>((char*)row + (sizeof(T) == 2 ? p.byte2 : p.byte4));
 }
 
 // a log2(e) of a lane's states (zero beyond the last).
@@ -134,14 +137,20 @@ template <int NP, int WAVES>
 __device__ __forceinline__ void load_slots(const ScanShape& s, const ScanPlace& p, const float* from, float (&h)[NP]) {
   const float* at = from + slot_of<NP, WAVES>(s, p);
 #pragma unroll
-  for (int n = 0; n < NP; ++n) h[n] = in_row(at + n * s.channels, p.channel);
+  for (int n = 0; n < NP; ++n) h[n] = in_row(at + n * s.channels, p);
 }
 template <int NP, int WAVES>
 __device__ __forceinline__ void store_slots(const ScanShape& s, const ScanPlace& p, float* to, const float (&h)[NP]) {
   if (!p.valid) return;
   float* at = to + slot_of<NP, WAVES>(s, p);
 #pragma unroll
-  for (int n = 0; n < NP; ++n) in_row(at + n * s.channels, p.channel) = h[n];
+  for (int n = 0; n < NP; ++n) in_row(at + n * s.channels, p) = h[n];
+}
+
+// What scan_ends_kernel leaves in front of the turn at step t.
+template <int NP, int WAVES, typename F>
+__device__ __forceinline__ F* marks_of(const ScanShape& s, const ScanPlace& p, F* marks, int64_t t) {
+  return marks + ((p.batch * (s.rows / kScanAhead) + t / kScanAhead) * (NP * WAVES + 1) + p.part * NP) * s.channels;
 }
 
 // The values of one step that a wave reads: b, and c where the pass needs it.
@@ -161,14 +170,42 @@ template <int NP, int WAVES>
 __device__ __forceinline__ Shared shared_rows(const ScanShape& s, const ScanPlace& p, const float* bc) {
   return shared_at(bc) + (p.batch * s.groups + p.group) * s.rows * (2 * NP * WAVES) + p.part * NP;
 }
-// Rows are requested a step ahead: without a stop the scheduler gathers those of all steps, more than the scalar registers hold.
+// Rows are requested in groups of as many as 16 scalar registers hold (at least one), a group ahead.  Scalar loads return in any order, so a wait for one is a
+// wait for all: a group is awaited before the next one is requested, which the compiler's own waits, at first use, would not do.  The stops keep the
+// scheduler from gathering more rows than the scalar registers hold.
 __device__ __forceinline__ void stop() { __builtin_amdgcn_sched_barrier(0); }
+__device__ __forceinline__ void await_shared() {
+  stop();
+  __builtin_amdgcn_s_waitcnt(0xc07f);        // lgkmcnt(0), the others as they are
+  stop();
+}
+// Values are worked out here, not where they are used: a step that the compiler has moved behind a later branch finds its row gone from the
+// scalar registers.
+template <int N>
+__device__ __forceinline__ void pin(float (&v)[N]) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) asm volatile("" : "+v"(v[n]));
+}
+__device__ __forceinline__ void pin(float& v) { asm volatile("" : "+v"(v)); }
+template <int NP, int WAVES, bool C>
+struct SharedGroup {
+  static constexpr int kRow = 2 * NP * WAVES;
+  static constexpr int kCount = NP * (C ? 2 : 1) >= 16 ? 1 : NP * (C ? 2 : 1) >= 8 ? 2 : 4;
+  SharedRow<NP, WAVES, C> row[kCount];
+  __device__ __forceinline__ void load(Shared at) {
+#pragma unroll
+    for (int k = 0; k < kCount; ++k) row[k].load(at + k * kRow);
+  }
+};
 
 // A channel's elements of a turn's steps (of the last one there is, beyond).
 template <typename T>
-__device__ __forceinline__ void load_turn(const T* row, int64_t stride, unsigned channel, int last, T (&v)[kScanAhead]) {
+__device__ __forceinline__ void load_turn(const T* row, int64_t stride, const ScanPlace& p, int last, T (&v)[kScanAhead]) {
 #pragma unroll
-  for (int j = 0; j < kScanAhead; ++j) v[j] = in_row(row + min(j, last) * stride, channel);
+  for (int j = 0; j < kScanAhead; ++j) {
+    v[j] = in_row(row, p);
+    row += j < last ? stride : 0;
+  }
 }
 __device__ __forceinline__ int last_of(const ScanPlace& p, int64_t t) { return (int)min(p.end - 1 - t, (int64_t)kScanAhead - 1); }
 
@@ -179,7 +216,7 @@ __device__ __forceinline__ void steps_and_inputs(const T (&xv)[kScanAhead], cons
 #pragma unroll
   for (int j = 0; j < kScanAhead; ++j) {
     const float raw = (float)dv[j] + shift;
-    const float v = soft ? softplus(raw) : raw;
+    const float v = soft ? softplus(raw).value : raw;
     dt[j] = j <= last ? v : 0.f;
     u[j] = j <= last ? v * (float)xv[j] : 0.f;
   }
@@ -187,14 +224,15 @@ __device__ __forceinline__ void steps_and_inputs(const T (&xv)[kScanAhead], cons
 
 // ---- chunks: what each does to a state --------------------------------------------------------------------
 // The state behind a chunk that starts from zero, the sum of its dt (the state in front decays by exp(a sum)) and, for the backward pass,
-// the gradient of the state in front of it if nothing came from behind.
+// the gradient of the state in front of it if nothing came from behind, and in marks the state and the sum in front of each of its turns
+// (batch x turns x (states, filled up, + 1) x channels).
 template <typename T, int NP, int WAVES, bool BACKWARD>
 __global__ __launch_bounds__(WAVES * kWave) void scan_ends_kernel(ScanShape s, const T* __restrict__ x, const T* __restrict__ delta,
                                                                   const float* __restrict__ a, const float* __restrict__ bc,
                                                                   const T* __restrict__ gate, const float* __restrict__ delta_bias,
                                                                   const int32_t* __restrict__ lengths, const T* __restrict__ dout,
                                                                   float* __restrict__ ends, float* __restrict__ starts,
-                                                                  float* __restrict__ sums) {
+                                                                  float* __restrict__ sums, float* __restrict__ marks) {
   constexpr int U = kScanAhead;
   const ScanPlace p = scan_place(s, lengths);
   float decay[NP], h[NP], g[NP], reach[NP];
@@ -211,16 +249,26 @@ __global__ __launch_bounds__(WAVES * kWave) void scan_ends_kernel(ScanShape s, c
   const T* os = BACKWARD ? dout + p.batch * s.out_b + p.from * s.out_t : nullptr;
   Shared rows = shared_rows<NP, WAVES>(s, p, bc) + p.from * (2 * NP * WAVES);
   float sum = 0.f;
+  using Group = SharedGroup<NP, WAVES, BACKWARD>;
+  Group next;
+  next.load(rows);
   for (int64_t t = p.from; t < p.end; t += U) {
     const int last = last_of(p, t);
-    SharedRow<NP, WAVES, BACKWARD> next;
-    next.load(rows);
     T xv[U], dv[U], gv[U], ov[U];
-    load_turn(xs, s.x_t, p.channel, last, xv);
-    load_turn(ds, s.delta_t, p.channel, last, dv);
+    load_turn(xs, s.x_t, p, last, xv);
+    load_turn(ds, s.delta_t, p, last, dv);
     if (BACKWARD) {
-      load_turn(os, s.out_t, p.channel, last, ov);
-      if (gs) load_turn(gs, s.gate_t, p.channel, last, gv);
+      if (p.valid && t > p.from) {
+        float* to = marks_of<NP, WAVES>(s, p, marks, t);
+#pragma unroll
+        for (int n = 0; n < NP; ++n) {
+          in_row(to, p) = h[n];
+          to += s.channels;
+        }
+        if (p.part == WAVES - 1) in_row(to, p) = sum;
+      }
+      load_turn(os, s.out_t, p, last, ov);
+      if (gs) load_turn(gs, s.gate_t, p, last, gv);
     }
     float dt[U], u[U], dy[U];
     steps_and_inputs(xv, dv, shift, s.softplus, last, dt, u);
@@ -230,27 +278,36 @@ __global__ __launch_bounds__(WAVES * kWave) void scan_ends_kernel(ScanShape s, c
         dy[j] = (float)ov[j];
         if (gs) {
           const float gt = (float)gv[j];
-          dy[j] *= gt * gates(gt).a;
+          dy[j] *= gt * sigmoid(gt).a;
         }
         if (j > last) dy[j] = 0.f;
       }
     }
-    stop();
 #pragma unroll
-    for (int j = 0; j < U; ++j) {
-      const SharedRow<NP, WAVES, BACKWARD> row = next;
-      if (j + 1 < U) next.load(rows + (j + 1) * (2 * NP * WAVES));
-      sum += dt[j];
+    for (int first = 0; first < U; first += Group::kCount) {
+      await_shared();
+      const Group group = next;
+      next.load(rows + (first + Group::kCount) * Group::kRow);
+      stop();
 #pragma unroll
-      for (int n = 0; n < NP; ++n) {
-        const float e = __builtin_amdgcn_exp2f(dt[j] * decay[n]);
-        h[n] = fmaf(e, h[n], u[j] * row.b[n]);
-        if (BACKWARD) {
-          reach[n] *= e;
-          g[n] = fmaf(reach[n], row.c[n] * dy[j], g[n]);
+      for (int k = 0; k < Group::kCount; ++k) {
+        const int j = first + k;
+        sum += dt[j];
+#pragma unroll
+        for (int n = 0; n < NP; ++n) {
+          const float e = __builtin_amdgcn_exp2f(dt[j] * decay[n]);
+          h[n] = fmaf(e, h[n], u[j] * group.row[k].b[n]);
+          if (BACKWARD) {
+            reach[n] *= e;
+            g[n] = fmaf(reach[n], group.row[k].c[n] * dy[j], g[n]);
+          }
         }
       }
-      stop();
+      pin(h);
+      if (BACKWARD) {
+        pin(g);
+        pin(reach);
+      }
     }
     xs += U * s.x_t;
     ds += U * s.delta_t;
@@ -264,55 +321,72 @@ __global__ __launch_bounds__(WAVES * kWave) void scan_ends_kernel(ScanShape s, c
 }
 
 // The state in front of every chunk, in place of the one behind it, and the gradient of the state behind every chunk, in place of that in front.
-// A lane has one state of one channel.
+// A lane has one state of one channel; the waves of a workgroup have runs of consecutive chunks.  Each folds its run, takes what comes out
+// of those in front, and walks its run once more.
 constexpr int kCarryAhead = 8;
-template <bool BACKWARD>
-__global__ __launch_bounds__(256) void scan_carry_kernel(ScanShape s, const float* __restrict__ a, const float* __restrict__ h0,
-                                                         const float* __restrict__ dlast, float* __restrict__ ends,
-                                                         float* __restrict__ starts, const float* __restrict__ sums) {
-  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x, b = blockIdx.z;
-  const int n = blockIdx.y;
-  if (c >= s.channels) return;
-  const bool held = n < s.states;
-  const float decay = held ? a[c * s.states + n] * kLog2e : 0.f;
-  const int64_t own = (b * s.channels + c) * s.states + n;
-  float h = held && h0 ? h0[own] : 0.f;
-  float* at = ends + (b * s.chunks * s.padded + n) * s.channels + c;
-  const int64_t step = (int64_t)s.padded * s.channels;
-  const float* total = sums + b * s.chunks * s.channels + c;
-  for (int k = 0; k < s.chunks; k += kCarryAhead) {
+constexpr int kCarryWaves = 16;
+
+// values: of a run, in its order of walking, `step` apart, and so the sums `sum_step`.  Leaves the state in front of each in its place.
+__device__ __forceinline__ void carry_runs(float* values, int64_t step, const float* total, int64_t sum_step, int count, float decay, float h,
+                                           bool valid, float (*fold)[2][kWave]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int share = (count + waves - 1) / waves, lo = min(wave * share, count), hi = min(lo + share, count);
+  if (waves > 1) {
+    float end = 0.f, sum = 0.f;
+    for (int k = lo; k < hi; k += kCarryAhead) {
+      float v[kCarryAhead], d[kCarryAhead];
+#pragma unroll
+      for (int j = 0; j < kCarryAhead; ++j) {
+        const int64_t i = min(k + j, hi - 1);
+        v[j] = values[i * step];
+        d[j] = total[i * sum_step];
+      }
+#pragma unroll
+      for (int j = 0; j < kCarryAhead; ++j)
+        if (k + j < hi) {
+          end = fmaf(__builtin_amdgcn_exp2f(d[j] * decay), end, v[j]);
+          sum += d[j];
+        }
+    }
+    __syncthreads();
+    fold[wave][0][lane] = end;
+    fold[wave][1][lane] = sum;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) h = fmaf(__builtin_amdgcn_exp2f(fold[w][1][lane] * decay), h, fold[w][0][lane]);
+  }
+  for (int k = lo; k < hi; k += kCarryAhead) {
     float v[kCarryAhead], d[kCarryAhead];
 #pragma unroll
     for (int j = 0; j < kCarryAhead; ++j) {
-      const int64_t i = min(k + j, s.chunks - 1);
-      v[j] = at[i * step];
-      d[j] = total[i * s.channels];
+      const int64_t i = min(k + j, hi - 1);
+      v[j] = values[i * step];
+      d[j] = total[i * sum_step];
     }
 #pragma unroll
     for (int j = 0; j < kCarryAhead; ++j)
-      if (k + j < s.chunks) {
-        at[(k + j) * step] = h;
+      if (k + j < hi) {
+        if (valid) values[(k + j) * step] = h;
         h = fmaf(__builtin_amdgcn_exp2f(d[j] * decay), h, v[j]);
       }
   }
-  if (!BACKWARD) return;
-  float g = held && dlast ? dlast[own] : 0.f;
-  at = starts + (b * s.chunks * s.padded + n) * s.channels + c;
-  for (int k = s.chunks - 1; k >= 0; k -= kCarryAhead) {
-    float v[kCarryAhead], d[kCarryAhead];
-#pragma unroll
-    for (int j = 0; j < kCarryAhead; ++j) {
-      const int64_t i = max(k - j, 0);
-      v[j] = at[i * step];
-      d[j] = total[i * s.channels];
-    }
-#pragma unroll
-    for (int j = 0; j < kCarryAhead; ++j)
-      if (k - j >= 0) {
-        at[(k - j) * step] = g;
-        g = fmaf(__builtin_amdgcn_exp2f(d[j] * decay), g, v[j]);
-      }
-  }
+}
+
+template <bool BACKWARD>
+__global__ __launch_bounds__(kWave * kCarryWaves) void scan_carry_kernel(ScanShape s, const float* __restrict__ a, const float* __restrict__ h0,
+                                                                         const float* __restrict__ dlast, float* ends, float* starts,
+                                                                         const float* __restrict__ sums) {
+  __shared__ float fold[kCarryWaves][2][kWave];
+  const int64_t b = blockIdx.z, at = (int64_t)blockIdx.x * kWave + (threadIdx.x & 63), c = min(at, s.channels - 1);
+  const int n = blockIdx.y;
+  const bool held = n < s.states, valid = at < s.channels;
+  const float decay = held ? a[c * s.states + n] * kLog2e : 0.f;
+  const int64_t own = (b * s.channels + c) * s.states + n, step = (int64_t)s.padded * s.channels;
+  const int64_t first = (b * s.chunks * s.padded + n) * s.channels + c, last = first + (s.chunks - 1) * step;
+  const float* const total = sums + b * s.chunks * s.channels + c;
+  carry_runs(ends + first, step, total, s.channels, s.chunks, decay, held && h0 ? h0[own] : 0.f, valid, fold);
+  if (BACKWARD)
+    carry_runs(starts + last, -step, total + (s.chunks - 1) * s.channels, -s.channels, s.chunks, decay, held && dlast ? dlast[own] : 0.f, valid,
+               fold);
 }
 
 // ---- forward ----------------------------------------------------------------------------------------------
@@ -336,28 +410,35 @@ __global__ __launch_bounds__(WAVES * kWave) void scan_forward_kernel(ScanShape s
   const T* gs = gate ? gate + p.batch * s.gate_b + p.from * s.gate_t : nullptr;
   T* os = out + p.batch * s.out_b;
   Shared rows = shared_rows<NP, WAVES>(s, p, bc) + p.from * (2 * NP * WAVES);
+  using Group = SharedGroup<NP, WAVES, true>;
+  Group next;
+  next.load(rows);
   for (int64_t t = p.from; t < p.end; t += U) {
     const int last = last_of(p, t);
-    SharedRow<NP, WAVES, true> next;
-    next.load(rows);
     T xv[U], dv[U], gv[U];
-    load_turn(xs, s.x_t, p.channel, last, xv);
-    load_turn(ds, s.delta_t, p.channel, last, dv);
-    if (gs) load_turn(gs, s.gate_t, p.channel, last, gv);
+    load_turn(xs, s.x_t, p, last, xv);
+    load_turn(ds, s.delta_t, p, last, dv);
+    if (gs) load_turn(gs, s.gate_t, p, last, gv);
     float y[U], dt[U], u[U];
     steps_and_inputs(xv, dv, shift, s.softplus, last, dt, u);
-    stop();
 #pragma unroll
-    for (int j = 0; j < U; ++j) {
-      const SharedRow<NP, WAVES, true> row = next;
-      if (j + 1 < U) next.load(rows + (j + 1) * (2 * NP * WAVES));
-      y[j] = 0.f;
-#pragma unroll
-      for (int n = 0; n < NP; ++n) {
-        h[n] = fmaf(__builtin_amdgcn_exp2f(dt[j] * decay[n]), h[n], u[j] * row.b[n]);
-        y[j] = fmaf(row.c[n], h[n], y[j]);
-      }
+    for (int first = 0; first < U; first += Group::kCount) {
+      await_shared();
+      const Group group = next;
+      next.load(rows + (first + Group::kCount) * Group::kRow);
       stop();
+#pragma unroll
+      for (int k = 0; k < Group::kCount; ++k) {
+        const int j = first + k;
+        y[j] = 0.f;
+#pragma unroll
+        for (int n = 0; n < NP; ++n) {
+          h[n] = fmaf(__builtin_amdgcn_exp2f(dt[j] * decay[n]), h[n], u[j] * group.row[k].b[n]);
+          y[j] = fmaf(group.row[k].c[n], h[n], y[j]);
+        }
+        pin(y[j]);
+      }
+      pin(h);
     }
     if (WAVES > 1) {
 #pragma unroll
@@ -376,14 +457,14 @@ __global__ __launch_bounds__(WAVES * kWave) void scan_forward_kernel(ScanShape s
       float r = fmaf(skip, (float)xv[j], y[j]);
       if (gs) {
         const float gt = (float)gv[j];
-        r *= gt * gates(gt).a;
+        r *= gt * sigmoid(gt).a;
       }
       y[j] = r;
     }
     if (p.valid) {
 #pragma unroll
       for (int j = 0; j < U; ++j)
-        if (j <= last && (WAVES == 1 || j % WAVES == p.part)) in_row(os + (t + j) * s.out_t, p.channel) = (T)y[j];
+        if (j <= last && (WAVES == 1 || j % WAVES == p.part)) in_row(os + (t + j) * s.out_t, p) = (T)y[j];
     }
     xs += U * s.x_t;
     ds += U * s.delta_t;
@@ -391,7 +472,7 @@ __global__ __launch_bounds__(WAVES * kWave) void scan_forward_kernel(ScanShape s
     rows += U * (2 * NP * WAVES);
   }
   if (p.valid && p.part == 0)
-    for (int64_t t = max(p.from, p.len); t < p.to; ++t) in_row(os + t * s.out_t, p.channel) = (T)0.f;
+    for (int64_t t = max(p.from, p.len); t < p.to; ++t) in_row(os + t * s.out_t, p) = (T)0.f;
   if (h_last && p.chunk == (p.len > 0 ? (p.len - 1) / s.chunk : 0)) store_states<NP>(s, p, h_last, h);
 }
 
@@ -419,7 +500,7 @@ __global__ __launch_bounds__(256) void scan_walk_kernel(ScanShape s, const T* __
     const F32<4> bv = widen<T, 4>(load_some<4>(b + batch * b_b + t * b_t + group * s.states + first, left));
     const F32<4> cv = widen<T, 4>(load_some<4>(c + batch * c_b + t * c_t + group * s.states + first, left));
     const float gt = gate ? (float)gate[batch * s.gate_b + t * s.gate_t + channel] : 0.f;
-    const float dt = s.softplus ? softplus(raw) : raw;
+    const float dt = s.softplus ? softplus(raw).value : raw;
     const float u = dt * xv;
     float y = 0.f;
 #pragma unroll
@@ -433,7 +514,7 @@ __global__ __launch_bounds__(256) void scan_walk_kernel(ScanShape s, const T* __
     if (L > 8) y += dpp<0x140>(y);
     if (first == 0) {
       float r = fmaf(skip, xv, y);
-      if (gate) r *= gt * gates(gt).a;
+      if (gate) r *= gt * sigmoid(gt).a;
       out[batch * s.out_b + t * s.out_t + channel] = (T)r;
     }
   }
@@ -491,58 +572,35 @@ __device__ __forceinline__ float lanes_sum(float (&v)[V], int l) {
   return v[0] + dpp<0xB1>(v[0]);
 }
 
-// A chunk: its states at every kScanAhead-th step go to LDS first; then, from its end, kScanAhead steps at a time are computed once more, kept in
-// registers, and walked back.  The waves of a workgroup share what the states of a channel have in common: each works it out for some of the
-// steps, and finishes the gradients of those.
+// A chunk, from its end: the states of kScanAhead steps at a time are computed from what scan_ends_kernel left in front of them and from the state
+// in front of the chunk, kept in registers, and walked back.  The waves of a workgroup share what the states of a channel have in common: each works
+// it out for some of the steps, and finishes the gradients of those.
 // parts: of a chunk, states + 2 rows of channels (grad_a, grad_d, grad_delta_bias); shared_parts: of a block of channels and a step, the
 // sums of grad_b and grad_c over the block.
 template <typename T, int NP, int WAVES>
-__global__ __launch_bounds__(WAVES * kWave, 2) void scan_backward_kernel(
+__global__ __launch_bounds__(WAVES * kWave, NP == 4 ? 3 : 2) void scan_backward_kernel(
     ScanShape s, const T* __restrict__ x, const T* __restrict__ delta, const float* __restrict__ a, const float* __restrict__ bc,
     const float* __restrict__ d, const T* __restrict__ gate, const float* __restrict__ delta_bias, const int32_t* __restrict__ lengths,
     const T* __restrict__ dout, const float* __restrict__ h0, const float* __restrict__ dlast, const float* __restrict__ ends,
-    const float* __restrict__ starts, T* __restrict__ dx, T* __restrict__ ddelta, T* __restrict__ dgate, float* __restrict__ dh0,
-    float* __restrict__ parts, float* __restrict__ shared_parts) {
-  extern __shared__ float held[];
+    const float* __restrict__ starts, const float* __restrict__ marks, T* __restrict__ dx, T* __restrict__ ddelta, T* __restrict__ dgate,
+    float* __restrict__ dh0, float* __restrict__ parts, float* __restrict__ shared_parts) {
   constexpr int U = kScanAhead, SHARE = U / WAVES;    // steps of a turn that a wave finishes
   constexpr int row_size = 2 * NP * WAVES;
   const ScanPlace p = scan_place(s, lengths);
-  const int most = (int)s.chunk / U;                                          // turns
-  float* const own = held + p.part * most * NP * kWave + p.lane;              // states in front of every turn
-  float* const common = held + WAVES * most * NP * kWave + p.lane;            // dt, u, dy of a turn's steps
-  float* const add = common + 3 * U * kWave;                                  // what the waves' states contribute to a turn's steps
-  float decay[NP], h[NP], g[NP], da[NP];
+  __shared__ float held[3 * U * kWave * (1 + WAVES)];
+  float* const common = held + p.lane;              // dt, u, dy of a turn's steps
+  float* const add = common + 3 * U * kWave;        // what the waves' states contribute to a turn's steps
+  float decay[NP], g[NP], da[NP];
   load_decay<NP>(s, p, a, decay);
-  if (s.chunks > 1) load_slots<NP, WAVES>(s, p, ends, h);
-  else load_states<NP>(s, p, h0, h);
   const float shift = delta_bias ? delta_bias[p.channel] : 0.f, skip = d ? d[p.channel] : 0.f;
   const T* const xs = x + p.batch * s.x_b;
   const T* const ds = delta + p.batch * s.delta_b;
   const Shared rows = shared_rows<NP, WAVES>(s, p, bc);
   const int turns = p.end > p.from ? (int)((p.end - p.from + U - 1) / U) : 0;
-  for (int i = 0; i < turns; ++i) {
-#pragma unroll
-    for (int n = 0; n < NP; ++n) own[(i * NP + n) * kWave] = h[n];
-    if (i + 1 == turns) break;
-    const int64_t t = p.from + i * U;
-    const Shared at = rows + t * row_size;
-    SharedRow<NP, WAVES, false> next;
-    next.load(at);
-    T xv[U], dv[U];
-    load_turn(xs + t * s.x_t, s.x_t, p.channel, U - 1, xv);
-    load_turn(ds + t * s.delta_t, s.delta_t, p.channel, U - 1, dv);
-    float dt[U], u[U];
-    steps_and_inputs(xv, dv, shift, s.softplus, U - 1, dt, u);
-    stop();
-#pragma unroll
-    for (int j = 0; j < U; ++j) {
-      const SharedRow<NP, WAVES, false> row = next;
-      if (j + 1 < U) next.load(at + (j + 1) * row_size);
-#pragma unroll
-      for (int n = 0; n < NP; ++n) h[n] = fmaf(__builtin_amdgcn_exp2f(dt[j] * decay[n]), h[n], u[j] * row.b[n]);
-      stop();
-    }
-  }
+  using Inputs = SharedGroup<NP, WAVES, false>;
+  using Both = SharedGroup<NP, WAVES, true>;
+  Inputs inputs;
+  inputs.load(rows + (p.from + max(turns - 1, 0) * U) * row_size);
   if (s.chunks > 1) load_slots<NP, WAVES>(s, p, starts, g);
   else load_states<NP>(s, p, dlast, g);
   const T* const gs = gate ? gate + p.batch * s.gate_b : nullptr;
@@ -550,85 +608,114 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void scan_backward_kernel(
   float dskip = 0.f, dshift = 0.f;
 #pragma unroll
   for (int n = 0; n < NP; ++n) da[n] = 0.f;
-  float* const shared_to = shared_parts + (p.batch * s.groups * s.blocks + p.block) * s.steps * row_size;
+  // where a lane's sum of two steps goes: the later one's come first
+  const int sum_of = p.lane / (kWave / (4 * NP)), value = sum_of % (2 * NP);
+  float* const shared_to = shared_parts + (p.batch * s.groups * s.blocks + p.block) * s.rows * row_size + (sum_of < 2 * NP ? row_size : 0) +
+                           p.part * NP + (value < NP ? value : NP * WAVES + value - NP);
   for (int i = turns - 1; i >= 0; --i) {
     const int64_t t = p.from + i * U;
     const int last = last_of(p, t);
     const Shared at = rows + t * row_size;
     // this wave's steps
     T xv[SHARE], dv[SHARE], gv[SHARE], ov[SHARE];
+    float slope[SHARE], through[SHARE];
 #pragma unroll
     for (int k = 0; k < SHARE; ++k) {
       const int64_t step = t + min(p.part * SHARE + k, last);
-      xv[k] = in_row(xs + step * s.x_t, p.channel);
-      dv[k] = in_row(ds + step * s.delta_t, p.channel);
-      ov[k] = in_row(os + step * s.out_t, p.channel);
-      if (gs) gv[k] = in_row(gs + step * s.gate_t, p.channel);
+      xv[k] = in_row(xs + step * s.x_t, p);
+      dv[k] = in_row(ds + step * s.delta_t, p);
+      ov[k] = in_row(os + step * s.out_t, p);
+      if (gs) gv[k] = in_row(gs + step * s.gate_t, p);
     }
 #pragma unroll
     for (int k = 0; k < SHARE; ++k) {
       const bool in = p.part * SHARE + k <= last, on = in && p.valid;
       const float raw = (float)dv[k] + shift;
-      const float step = s.softplus ? softplus(raw) : raw;
+      const Softplus soft = softplus(raw);
+      const float step = s.softplus ? soft.value : raw;
+      slope[k] = s.softplus ? soft.slope : 1.f;
       float r = (float)ov[k];
       if (gs) {
         const float gt = (float)gv[k];
-        r *= gt * gates(gt).a;
+        const Gates z = sigmoid(gt);
+        through[k] = r * (z.a * fmaf(gt, z.z, 1.f));
+        r *= gt * z.a;
       }
       float* const to = common + (p.part * SHARE + k) * 3 * kWave;
       to[0] = in ? step : 0.f;
       to[kWave] = on ? step * (float)xv[k] : 0.f;
       to[2 * kWave] = on ? r : 0.f;
     }
-    SharedRow<NP, WAVES, false> ahead;
-    ahead.load(at);
     if (WAVES > 1) __syncthreads();
-    float hs[U + 1][NP], e[U][NP];
-#pragma unroll
-    for (int n = 0; n < NP; ++n) hs[0][n] = own[(i * NP + n) * kWave];
-    SharedRow<NP, WAVES, true> next;
-#pragma unroll
-    for (int j = 0; j < U; ++j) {
-      const SharedRow<NP, WAVES, false> row = ahead;
-      if (j + 1 < U) ahead.load(at + (j + 1) * row_size);
-      else next.load(at + j * row_size);
-      const float dt = common[j * 3 * kWave], u = common[(j * 3 + 1) * kWave];
+    float hs[U + 1][NP], e[U][NP], dt[U], u[U], dy[U];
+    if (s.chunks > 1) load_slots<NP, WAVES>(s, p, ends, hs[0]);
+    else load_states<NP>(s, p, h0, hs[0]);
+    if (i > 0) {
+      const float* from = marks_of<NP, WAVES>(s, p, marks, t);
+      const float sum = in_row(from + (WAVES - p.part) * NP * s.channels, p);
 #pragma unroll
       for (int n = 0; n < NP; ++n) {
-        e[j][n] = __builtin_amdgcn_exp2f(dt * decay[n]);
-        hs[j + 1][n] = fmaf(e[j][n], hs[j][n], u * row.b[n]);
+        hs[0][n] = fmaf(__builtin_amdgcn_exp2f(sum * decay[n]), hs[0][n], in_row(from, p));
+        from += s.channels;
       }
-      stop();
     }
 #pragma unroll
-    for (int j = U - 1; j >= 0; --j) {
-      const SharedRow<NP, WAVES, true> row = next;
-      if (j > 0) next.load(at + (j - 1) * row_size);
-      const float dt = common[j * 3 * kWave], u = common[(j * 3 + 1) * kWave], dy = common[(j * 3 + 2) * kWave];
-      float v[2 * NP], y = 0.f, along = 0.f, step = 0.f;
+    for (int j = 0; j < U; ++j) {
+      dt[j] = common[j * 3 * kWave];
+      u[j] = common[(j * 3 + 1) * kWave];
+      dy[j] = common[(j * 3 + 2) * kWave];
+    }
+    Both both;
 #pragma unroll
-      for (int n = 0; n < NP; ++n) {
-        const float total = fmaf(row.c[n], dy, g[n]);
-        y = fmaf(row.c[n], hs[j + 1][n], y);
-        v[n] = total * u;
-        v[NP + n] = dy * hs[j + 1][n];
-        along = fmaf(total, row.b[n], along);
-        g[n] = total * e[j][n];
-        const float back = g[n] * hs[j][n];
-        step = fmaf(back, decay[n], step);
-        da[n] = fmaf(back, dt, da[n]);
-      }
-      const float sum = lanes_sum<2 * NP>(v, p.lane);
-      constexpr int each = kWave / (2 * NP);
-      if (j <= last && p.lane % each == 0) {
-        const int k = p.lane / each;
-        shared_to[(t + j) * row_size + p.part * NP + (k < NP ? k : NP * WAVES + k - NP)] = sum;
-      }
-      float* const to = add + (p.part * U + j) * 3 * kWave;
-      to[0] = y;
-      to[kWave] = along;
-      to[2 * kWave] = step;
+    for (int first = 0; first < U; first += Inputs::kCount) {
+      await_shared();
+      const Inputs group = inputs;
+      if (first + Inputs::kCount < U) inputs.load(at + (first + Inputs::kCount) * row_size);
+      else both.load(at + (U - Both::kCount) * row_size);
       stop();
+#pragma unroll
+      for (int k = 0; k < Inputs::kCount; ++k) {
+        const int j = first + k;
+#pragma unroll
+        for (int n = 0; n < NP; ++n) {
+          e[j][n] = __builtin_amdgcn_exp2f(dt[j] * decay[n]);
+          hs[j + 1][n] = fmaf(e[j][n], hs[j][n], u[j] * group.row[k].b[n]);
+        }
+        pin(hs[j + 1]);
+      }
+    }
+    float v[4 * NP];       // what two steps give to grad_b and grad_c
+#pragma unroll
+    for (int first = U - Both::kCount; first >= 0; first -= Both::kCount) {
+      await_shared();
+      const Both group = both;
+      if (first > 0) both.load(at + (first - Both::kCount) * row_size);
+      else inputs.load(rows + max(t - U, p.from) * row_size);
+      stop();
+#pragma unroll
+      for (int k = Both::kCount - 1; k >= 0; --k) {
+        const int j = first + k;
+        float* const pair = v + (j & 1 ? 0 : 2 * NP);
+        float y = 0.f, along = 0.f, step = 0.f;
+#pragma unroll
+        for (int n = 0; n < NP; ++n) {
+          const float total = fmaf(group.row[k].c[n], dy[j], g[n]);
+          y = fmaf(group.row[k].c[n], hs[j + 1][n], y);
+          pair[n] = total * u[j];
+          pair[NP + n] = dy[j] * hs[j + 1][n];
+          along = fmaf(total, group.row[k].b[n], along);
+          g[n] = total * e[j][n];
+          const float back = g[n] * hs[j][n];
+          step = fmaf(back, decay[n], step);
+          da[n] = fmaf(back, dt[j], da[n]);
+        }
+        float* const to = add + (p.part * U + j) * 3 * kWave;
+        to[0] = y;
+        to[kWave] = along;
+        to[2 * kWave] = step;
+        if (j % 2 == 0) shared_to[(t + j) * row_size] = lanes_sum<4 * NP>(v, p.lane);
+        stop();
+      }
     }
     if (WAVES > 1) __syncthreads();
 #pragma unroll
@@ -643,19 +730,13 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void scan_backward_kernel(
         step += from[2 * kWave];
       }
       if (j > last || !p.valid) continue;
-      const float dt = common[j * 3 * kWave], dy = common[(j * 3 + 2) * kWave], xt = (float)xv[k];
-      float r = fmaf(along, xt, step * kLn2);
-      if (s.softplus) r *= gates((float)dv[k] + shift).a;
-      in_row(dx + p.batch * s.dx_b + (t + j) * s.dx_t, p.channel) = (T)fmaf(dt, along, skip * dy);
-      in_row(ddelta + p.batch * s.ddelta_b + (t + j) * s.ddelta_t, p.channel) = (T)r;
+      const float own_dt = common[j * 3 * kWave], own_dy = common[(j * 3 + 2) * kWave], xt = (float)xv[k];
+      const float r = fmaf(along, xt, step * kLn2) * slope[k];
+      in_row(dx + p.batch * s.dx_b + (t + j) * s.dx_t, p) = (T)fmaf(own_dt, along, skip * own_dy);
+      in_row(ddelta + p.batch * s.ddelta_b + (t + j) * s.ddelta_t, p) = (T)r;
       dshift += r;
-      dskip = fmaf(dy, xt, dskip);
-      if (gs) {
-        const float gt = (float)gv[k];
-        const Gates z = gates(gt);
-        in_row(dgate + p.batch * s.dgate_b + (t + j) * s.dgate_t, p.channel) =
-            (T)((float)ov[k] * fmaf(skip, xt, y) * (z.a * fmaf(gt, z.z, 1.f)));
-      }
+      dskip = fmaf(own_dy, xt, dskip);
+      if (gs) in_row(dgate + p.batch * s.dgate_b + (t + j) * s.dgate_t, p) = (T)(fmaf(skip, xt, y) * through[k]);
     }
     if (WAVES > 1) __syncthreads();      // common and add are written again
   }
@@ -664,7 +745,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void scan_backward_kernel(
 #pragma unroll
     for (int n = 0; n < NP; ++n) {
       const int at = p.part * NP + n;
-      if (at < s.states) in_row(to + at * s.channels, p.channel) = da[n];
+      if (at < s.states) in_row(to + at * s.channels, p) = da[n];
     }
     if (dh0 && p.chunk == 0) store_states<NP>(s, p, dh0, g);
   }
@@ -680,18 +761,18 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void scan_backward_kernel(
     }
   }
   if (!p.valid || p.part != 0) return;
-  in_row(to + s.states * s.channels, p.channel) = dskip;
-  in_row(to + (s.states + 1) * s.channels, p.channel) = dshift;
+  in_row(to + s.states * s.channels, p) = dskip;
+  in_row(to + (s.states + 1) * s.channels, p) = dshift;
   for (int64_t t = max(p.from, p.len); t < p.to; ++t) {
-    in_row(dx + p.batch * s.dx_b + t * s.dx_t, p.channel) = (T)0.f;
-    in_row(ddelta + p.batch * s.ddelta_b + t * s.ddelta_t, p.channel) = (T)0.f;
-    if (gs) in_row(dgate + p.batch * s.dgate_b + t * s.dgate_t, p.channel) = (T)0.f;
+    in_row(dx + p.batch * s.dx_b + t * s.dx_t, p) = (T)0.f;
+    in_row(ddelta + p.batch * s.ddelta_b + t * s.ddelta_t, p) = (T)0.f;
+    if (gs) in_row(dgate + p.batch * s.dgate_b + t * s.dgate_t, p) = (T)0.f;
   }
 }
 
 // grad_b and grad_c: the sums of a group's blocks of channels, in their order.
 template <typename T>
-__global__ __launch_bounds__(256) void scan_join_kernel(const float* __restrict__ shared_parts, int64_t rows, int64_t steps, int groups,
+__global__ __launch_bounds__(256) void scan_join_kernel(const float* __restrict__ shared_parts, int64_t rows, int64_t steps, int64_t held, int groups,
                                                         int blocks, int states, int padded, const int32_t* __restrict__ lengths,
                                                         T* __restrict__ db, T* __restrict__ dc, int64_t db_b, int64_t db_t, int64_t dc_b,
                                                         int64_t dc_t) {
@@ -702,8 +783,8 @@ __global__ __launch_bounds__(256) void scan_join_kernel(const float* __restrict_
   const int64_t t = row % steps, g = row / steps % groups, batch = row / steps / groups;
   float s = 0.f;
   if (t < steps_of(lengths, batch, steps)) {
-    const float* from = shared_parts + ((batch * groups + g) * blocks * steps + t) * 2 * padded + k;
-    for (int i = 0; i < blocks; ++i) s += from[(int64_t)i * steps * 2 * padded];
+    const float* from = shared_parts + ((batch * groups + g) * blocks * held + t) * 2 * padded + k;
+    for (int i = 0; i < blocks; ++i) s += from[(int64_t)i * held * 2 * padded];
   }
   if (k < padded) db[batch * db_b + t * db_t + g * states + n] = (T)s;
   else dc[batch * dc_b + t * dc_t + g * states + n] = (T)s;

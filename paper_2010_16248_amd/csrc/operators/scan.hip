@@ -37,16 +37,22 @@ int32_t check_scan(const acc_scan* c, bool backward) {
 }
 
 constexpr int64_t kScanWalkSteps = 8;       // up to here lanes share a channel and walk the steps
-constexpr int64_t kScanWaves = 4096;        // waves that fill the chip
-constexpr int64_t kScanLone = 1024;         // from here on no chunks
-constexpr int64_t kScanShortest = 32;       // steps of a chunk at least
+// Chunks of the forward pass cost every step a second time (scan_ends_kernel), for waves.  Up to this many waves without chunks, chunks of 32 steps
+// and more that make so many waves.  us without chunks and with chunks of 32, 64, 128, 256 steps, 16 states, bf16: 64 x 512 x 1024 (1024 waves) 356,
+// 293, 275, 316, 371; x 2048 475, 538, 496, 478, 553; x 4096 721, 1018, 931, 871, 852; 16 x 4096 x 1024 2011, 548, 512, 519, 572;
+// 1 x 512 x 1536 236, 46, 69, 109, 199; 1 x 4096 x 1536 1866, 89, 97, 120, 216.
+constexpr int64_t kScanLone = 2048, kScanWaves = 12288, kScanShortest = 32;
+// Chunks of the backward pass: as long as leave this many workgroups, from 16 to 256 steps.  us with chunks of 16, 32, 64, 128, 256 steps:
+// 1 x 512 x 1536 (24 workgroups per chunk) 57, 66, 86, 140, 248; 2 x 2048 x 768 123, 108, 111, 162, 264; 4 x 1024 x 1536 193, 178, 175, 187,
+// 294; 64 x 128 x 512 133, 133, 149, 163, 163; 8 x 4096 x 2048 2365, 1931, 1399, 1348, 1335.
+constexpr int64_t kScanGroups = 1536, kBackwardShortest = 16, kBackwardLongest = 256;
 
 struct ScanPlan {
   bool walk = false;
   int each = 16, waves = 1, padded = 16;    // states of a lane, waves of a workgroup, states in all
   int64_t group = 0, blocks = 0;            // channels of a group, blocks of 64 of them
   int64_t chunk = 0, chunks = 1, rows = 0;  // steps of a chunk, chunks, rows of a sequence's b and c
-  int64_t packed = 0, ends = 0, starts = 0, sums = 0, parts = 0, shared_parts = 0, bytes = 0;   // offsets in the workspace
+  int64_t packed = 0, ends = 0, starts = 0, sums = 0, marks = 0, parts = 0, shared_parts = 0, bytes = 0;   // offsets in the workspace
 };
 
 ScanPlan plan_scan(const acc_scan& c, bool backward) {
@@ -60,8 +66,8 @@ ScanPlan plan_scan(const acc_scan& c, bool backward) {
   p.blocks = up(p.group, kWave);
   const int64_t lone = c.batch * c.groups * p.blocks * p.waves;      // waves of one chunk
   if (backward) {
-    p.chunk = p.waves > 2 ? 32 : 64;
-    while (p.chunk > 16 && lone * up(c.steps, p.chunk) < kScanWaves / 2) p.chunk /= 2;
+    p.chunk = kBackwardLongest;
+    while (p.chunk > kBackwardShortest && lone / p.waves * up(c.steps, p.chunk) < kScanGroups) p.chunk /= 2;
   } else {
     p.chunk = c.steps;
     if (lone < kScanLone) p.chunk = std::max(kScanShortest, up(c.steps, up(kScanWaves, lone)));
@@ -72,14 +78,16 @@ ScanPlan plan_scan(const acc_scan& c, bool backward) {
   int64_t at = 0;
   auto take = [&](int64_t floats) { const int64_t o = at; at += round256(4 * floats); return o; };
   p.rows = up(c.steps, kScanAhead) * kScanAhead;
-  const int64_t slots = p.chunks > 1 ? c.batch * p.chunks * c.channels : 0;
-  p.packed = take(c.batch * c.groups * p.rows * 2 * p.padded);
+  const int64_t slots = p.chunks > 1 || (backward && c.steps > kScanAhead) ? c.batch * p.chunks * c.channels : 0;
+  // (rows are requested ahead: up to a turn beyond the last)
+  p.packed = take((c.batch * c.groups * p.rows + kScanAhead) * 2 * p.padded);
   p.ends = take(slots * p.padded);
   p.sums = take(slots);
   if (backward) {
     p.starts = take(slots * p.padded);
+    p.marks = take(c.steps > kScanAhead ? c.batch * (p.rows / kScanAhead) * (p.padded + 1) * c.channels : 0);
     p.parts = take(c.batch * p.chunks * (c.states + 2) * c.channels);
-    p.shared_parts = take(c.batch * c.groups * p.blocks * c.steps * 2 * p.padded);
+    p.shared_parts = take(c.batch * c.groups * p.blocks * p.rows * 2 * p.padded);
   }
   p.bytes = at;
   return p;
@@ -119,6 +127,16 @@ void walk(const acc_scan& c, const ScanPlan& p, const ScanIn& in, void* out, flo
          in.lengths, in.h0, static_cast<T*>(out), h_last);
 }
 
+dim3 carry_grid(const acc_scan& c, const ScanPlan& p) {
+  return dim3((unsigned)up(c.channels, kWave), (unsigned)p.padded, (unsigned)c.batch);
+}
+constexpr int64_t kCarryFill = 4096;        // waves that fill the chip
+// More waves than one for a state's chunks where the states alone do not fill the chip.
+dim3 carry_threads(const acc_scan& c, const ScanPlan& p) {
+  const int64_t lone = c.batch * up(c.channels, kWave) * p.padded;
+  return dim3((unsigned)(kWave * std::max<int64_t>(1, std::min({(int64_t)kCarryWaves, up(kCarryFill, lone), up(p.chunks, kCarryAhead)}))));
+}
+
 template <typename T, int NP, int WAVES>
 void forward_chunks(const acc_scan& c, const ScanPlan& p, const ScanIn& in, void* out, float* h_last, char* ws, Queue& queue) {
   const ScanShape s = shape_of(c, p);
@@ -129,8 +147,8 @@ void forward_chunks(const acc_scan& c, const ScanPlan& p, const ScanIn& in, void
   pack<T>(c, p, in, packed, queue);
   if (p.chunks > 1) {
     LAUNCH((scan_ends_kernel<T, NP, WAVES, false>), dim3(across, (unsigned)(p.chunks - 1), batch), dim3(threads), queue, s, as<T>(in.x),
-           as<T>(in.delta), in.a, packed, nullptr, in.delta_bias, in.lengths, nullptr, ends, nullptr, sums);
-    LAUNCH(scan_carry_kernel<false>, dim3((unsigned)up(c.channels, 256), (unsigned)p.padded, batch), dim3(256), queue, s, in.a, in.h0, nullptr,
+           as<T>(in.delta), in.a, packed, nullptr, in.delta_bias, in.lengths, nullptr, ends, nullptr, sums, nullptr);
+    LAUNCH(scan_carry_kernel<false>, carry_grid(c, p), carry_threads(c, p), queue, s, in.a, in.h0, nullptr,
            ends, nullptr, sums);
   }
   LAUNCH((scan_forward_kernel<T, NP, WAVES>), dim3(across, (unsigned)p.chunks, batch), dim3(threads), queue, s, as<T>(in.x), as<T>(in.delta),
@@ -170,17 +188,16 @@ void backward_ends(const acc_scan& c, const ScanPlan& p, const ScanIn& in, const
   auto at = [&](int64_t offset) { return reinterpret_cast<float*>(ws + offset); };
   LAUNCH((scan_ends_kernel<T, NP, WAVES, true>), dim3((unsigned)(c.groups * p.blocks), (unsigned)p.chunks, (unsigned)c.batch),
          dim3(kWave * WAVES), queue, shape_of(c, p), as<T>(in.x), as<T>(in.delta), in.a, at(p.packed), as<T>(in.gate),
-         in.delta_bias, in.lengths, as<T>(g.out), at(p.ends), at(p.starts), at(p.sums));
+         in.delta_bias, in.lengths, as<T>(g.out), at(p.ends), at(p.starts), at(p.sums), at(p.marks));
 }
 
 template <typename T, int NP, int WAVES>
 void backward_chunks(const acc_scan& c, const ScanPlan& p, const ScanIn& in, const ScanGradients& g, char* ws, Queue& queue) {
   auto at = [&](int64_t offset) { return reinterpret_cast<float*>(ws + offset); };
-  const int64_t lds = 4 * kWave * (p.chunk / kScanAhead * p.padded + 3 * kScanAhead * (1 + WAVES));
-  enqueue(queue, scan_backward_kernel<T, NP, WAVES>, dim3((unsigned)(c.groups * p.blocks), (unsigned)p.chunks, (unsigned)c.batch),
-          dim3(kWave * WAVES), (unsigned)lds, shape_of(c, p), as<T>(in.x), as<T>(in.delta), in.a, at(p.packed), in.d, as<T>(in.gate),
-          in.delta_bias, in.lengths, as<T>(g.out), in.h0, g.last, at(p.ends), at(p.starts), static_cast<T*>(g.x), static_cast<T*>(g.delta),
-          static_cast<T*>(g.gate), g.h0, at(p.parts), at(p.shared_parts));
+  LAUNCH((scan_backward_kernel<T, NP, WAVES>), dim3((unsigned)(c.groups * p.blocks), (unsigned)p.chunks, (unsigned)c.batch), dim3(kWave * WAVES),
+         queue, shape_of(c, p), as<T>(in.x), as<T>(in.delta), in.a, at(p.packed), in.d, as<T>(in.gate), in.delta_bias, in.lengths, as<T>(g.out),
+         in.h0, g.last, at(p.ends), at(p.starts), at(p.marks), static_cast<T*>(g.x), static_cast<T*>(g.delta), static_cast<T*>(g.gate), g.h0,
+         at(p.parts), at(p.shared_parts));
 }
 
 template <typename T>
@@ -188,23 +205,24 @@ void backward(const acc_scan& c, const ScanPlan& p, const ScanIn& in, const Scan
   auto at = [&](int64_t offset) { return reinterpret_cast<float*>(ws + offset); };
   if (c.batch > 0) {
     pack<T>(c, p, in, at(p.packed), queue);
-    if (p.chunks > 1) {
+    if (c.steps > kScanAhead) {
       if (p.padded == 4) backward_ends<T, 4, 1>(c, p, in, g, ws, queue);
       else if (p.padded == 8) backward_ends<T, 8, 1>(c, p, in, g, ws, queue);
       else if (p.padded == 16) backward_ends<T, 16, 1>(c, p, in, g, ws, queue);
       else if (p.padded == 32) backward_ends<T, 16, 2>(c, p, in, g, ws, queue);
       else backward_ends<T, 16, 4>(c, p, in, g, ws, queue);
-      LAUNCH(scan_carry_kernel<true>, dim3((unsigned)up(c.channels, 256), (unsigned)p.padded, (unsigned)c.batch), dim3(256), queue,
-             shape_of(c, p), in.a, in.h0, g.last, at(p.ends), at(p.starts), at(p.sums));
     }
+    if (p.chunks > 1)
+      LAUNCH(scan_carry_kernel<true>, carry_grid(c, p), carry_threads(c, p), queue, shape_of(c, p), in.a, in.h0, g.last, at(p.ends),
+             at(p.starts), at(p.sums));
     if (p.padded == 4) backward_chunks<T, 4, 1>(c, p, in, g, ws, queue);
-    else if (p.padded == 8) backward_chunks<T, 8, 1>(c, p, in, g, ws, queue);
-    else if (p.padded == 16) backward_chunks<T, 8, 2>(c, p, in, g, ws, queue);
-    else if (p.padded == 32) backward_chunks<T, 8, 4>(c, p, in, g, ws, queue);
+    else if (p.padded == 8) backward_chunks<T, 4, 2>(c, p, in, g, ws, queue);
+    else if (p.padded == 16) backward_chunks<T, 4, 4>(c, p, in, g, ws, queue);
+    else if (p.padded == 32) backward_chunks<T, 4, 8>(c, p, in, g, ws, queue);
     else backward_chunks<T, 8, 8>(c, p, in, g, ws, queue);
     const int64_t rows = c.batch * c.groups * c.steps;
     if (rows > 0)
-      LAUNCH(scan_join_kernel<T>, dim3((unsigned)up(rows * 2 * p.padded, 256)), dim3(256), queue, at(p.shared_parts), rows, c.steps, c.groups,
+      LAUNCH(scan_join_kernel<T>, dim3((unsigned)up(rows * 2 * p.padded, 256)), dim3(256), queue, at(p.shared_parts), rows, c.steps, p.rows, c.groups,
              (int)p.blocks, c.states, p.padded, in.lengths, static_cast<T*>(g.b), static_cast<T*>(g.c), c.grad_b_batch, c.grad_b_step,
              c.grad_c_batch, c.grad_c_step);
   }

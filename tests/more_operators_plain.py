@@ -87,7 +87,7 @@ def convolution_gradients(x, weight, bias, state, lengths, silu, dout, dlast):
 
 # ---- scan -----------------------------------------------------------------------------------------------
 
-CHUNK = 64       # steps of a chunk at most, at the sizes of these tests: the roundings of a sum of its dt
+CHUNK = 256      # steps of a chunk at most, at the sizes of these tests: the roundings of a sum of its dt
 
 
 class Scan:

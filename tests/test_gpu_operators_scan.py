@@ -89,8 +89,15 @@ def test_lengths_around_turns_and_chunks(steps):
 def test_one_chunk_of_many_waves():
     """Sequences enough to fill the chip: no chunks in the forward pass."""
     print("case wide", flush=True)
-    check(make(1100, 20, 2, 2, BF16), back=False)
-    check(make(130, 30, 520, 3), back=False)
+    check(make(2100, 40, 2, 2, BF16), back=False)
+    check(make(130, 70, 1100, 3), back=False)
+
+
+def test_chunks_of_many_turns():
+    """Workgroups enough for the longest chunks of the backward pass."""
+    print("case long chunks", flush=True)
+    check(make(800, 300, 3, 2, BF16))
+    check(make(400, 520, 66, 3, lengths=[520 - i for i in range(400)]))
 
 
 @pytest.mark.parametrize("kind", [F32, BF16])
