@@ -126,6 +126,8 @@ def load_library() -> C.CDLL:
     import torch
     _TYPES.update({torch.float32: ACC_FLOAT, torch.bfloat16: ACC_BF16})
     _INDEX_BITS.update({torch.int32: 32, torch.int64: 64})
+    global _FLOAT32, _INT32
+    _FLOAT32, _INT32 = torch.float32, torch.int32
     lib = C.CDLL(LIB_PATH)
     vp, i32, i64, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
     sig = {
@@ -280,6 +282,7 @@ def _need(ok: bool, what: str) -> None:
 
 
 _TYPES, _INDEX_BITS = {}, {}      # by torch's types, filled once torch is loaded
+_FLOAT32 = _INT32 = None          # torch's types, likewise
 
 
 def _type_of(t, name: str) -> int:
@@ -334,10 +337,10 @@ def _launch(gpu: int, fn, *args) -> None:
         raise AccordionError(rc, _lib.accordion_operator_error().decode())
 
 
-def _workspace(gpu: int, fn, cfg, given):
+def _workspace(gpu: int, fn, cfg, given, *which):
     """(tensor or None, pointer, bytes) of the workspace of a call: as given, or from torch's allocator for the current stream."""
     n = C.c_size_t(0)
-    rc = fn(C.byref(cfg), C.byref(n))
+    rc = fn(C.byref(cfg), *which, C.byref(n))
     if rc != ACC_OK:
         raise AccordionError(rc, _lib.accordion_operator_error().decode())
     if given is None:
@@ -462,26 +465,30 @@ def recurrence_backward(gate, input, out, grad_out, grad_gate, grad_input, h0=No
             grad_out.data_ptr(), last, grad_gate.data_ptr(), grad_input.data_ptr(), dh0, ws, n)
 
 
-def _parts_of(t, name: str, shape: Tuple[int, ...], dtype) -> Tuple[int, int]:
+def _parts_of(t, name: str, shape, dtype) -> Tuple[int, int]:
     """(elements between sequences, between steps) of a batch x steps x ... tensor whose steps' elements are contiguous."""
-    if t.shape != shape or t.dtype != dtype:
+    if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype}, of shape {tuple(shape)}")
-    stride, expect = t.stride(), 1
-    for size, step in zip(reversed(shape[2:]), reversed(stride[2:])):
-        if size > 1 and step != expect:
-            raise ValueError(f"{name}: the elements of a step must be contiguous")
-        expect *= size
-    return stride[0], stride[1]
+    stride = t.stride()
+    if len(stride) == 3:
+        apart = stride[2] != 1 and shape[2] > 1
+    else:
+        apart = (stride[3] != 1 and shape[3] > 1) or (stride[2] != shape[3] and shape[2] > 1)
+    if apart:
+        raise ValueError(f"{name}: the elements of a step must be contiguous")
+    return stride[:2]
 
 
 def _convolution(x, weight, out, name: str, silu: bool, accumulate: bool, grad_x=None):
-    _need(x.dim() == 3, "x must be batch x steps x channels")
+    """(config, shapes of weight, of a channels' vector, of a state)."""
+    shape, kind = x.shape, x.dtype
+    _need(len(shape) == 3, "x must be batch x steps x channels")
     _need(weight.dim() == 2, "weight must be channels x width")
-    batch, steps, channels = x.shape
-    shape, width = tuple(x.shape), weight.shape[1]
-    last = (0, 0) if grad_x is None else _parts_of(grad_x, "grad_x", shape, x.dtype)
-    cfg = acc_convolution(batch, steps, channels, *_parts_of(x, "x", shape, x.dtype), *_parts_of(out, name, shape, x.dtype), *last,
-                          width, _type_of(x, "x"), silu, accumulate)
+    batch, steps, channels = shape
+    width = weight.shape[1]
+    last = (0, 0) if grad_x is None else _parts_of(grad_x, "grad_x", shape, kind)
+    cfg = acc_convolution(batch, steps, channels, *_parts_of(x, "x", shape, kind), *_parts_of(out, name, shape, kind), *last, width,
+                          _type_of(x, "x"), silu, accumulate)
     return cfg, (channels, width), (channels,), (batch, width - 1, channels)
 
 
@@ -489,12 +496,11 @@ def convolution_forward(x, weight, out, bias=None, state=None, last=None, length
     """out_t = act(bias + sum_j weight[:, j] x_{t - width + 1 + j}) along dimension 1 of batch x steps x channels tensors, act the
     identity or SiLU; state (batch x (width - 1) x channels, float32): the inputs in front (None: zeros); last gets those of a call that
     continues.  steps = 1 with state and last: one token."""
-    import torch
     lib = load_library()
     cfg, wide, flat, ends = _convolution(x, weight, out, "out", silu, False)
-    f = torch.float32
+    f = _FLOAT32
     w, b = _plain(weight, "weight", wide, f), _plain(bias, "bias", flat, f)
-    first, end, n_steps = _plain(state, "state", ends, f), _plain(last, "last", ends, f), _plain(lengths, "lengths", ends[:1], torch.int32)
+    first, end, n_steps = _plain(state, "state", ends, f), _plain(last, "last", ends, f), _plain(lengths, "lengths", ends[:1], _INT32)
     _launch(_gpu_of(x, weight, out, bias, state, last, lengths), lib.accordion_convolution_forward, C.byref(cfg), x.data_ptr(), w, b, first,
             n_steps, out.data_ptr(), end)
 
@@ -502,14 +508,13 @@ def convolution_forward(x, weight, out, bias=None, state=None, last=None, length
 def convolution_backward(x, weight, grad_out, grad_x, grad_weight, bias=None, grad_bias=None, state=None, grad_last=None, grad_state=None,
                          lengths=None, silu: bool = False, accumulate: bool = False, workspace=None) -> None:
     """Gradients of convolution_forward; grad_last is the gradient of last (None: zeros); accumulate adds to grad_weight and grad_bias."""
-    import torch
     lib = load_library()
     cfg, wide, flat, ends = _convolution(x, weight, grad_out, "grad_out", silu, accumulate, grad_x)
-    f = torch.float32
+    f = _FLOAT32
     w, b, first = _plain(weight, "weight", wide, f), _plain(bias, "bias", flat, f), _plain(state, "state", ends, f)
     dw, db = _plain(grad_weight, "grad_weight", wide, f), _plain(grad_bias, "grad_bias", flat, f)
     dl, ds = _plain(grad_last, "grad_last", ends, f), _plain(grad_state, "grad_state", ends, f)
-    n_steps = _plain(lengths, "lengths", ends[:1], torch.int32)
+    n_steps = _plain(lengths, "lengths", ends[:1], _INT32)
     gpu = _gpu_of(x, weight, grad_out, grad_x, grad_weight, bias, grad_bias, state, grad_last, grad_state, lengths)
     held, ws, n = _workspace(gpu, lib.accordion_convolution_workspace_bytes, cfg, workspace)
     _launch(gpu, lib.accordion_convolution_backward, C.byref(cfg), x.data_ptr(), w, b, first, n_steps, grad_out.data_ptr(), dl,
@@ -518,22 +523,24 @@ def convolution_backward(x, weight, grad_out, grad_x, grad_weight, bias=None, gr
 
 def _scan(x, delta, a, b, c, out, name: str, gate, softplus: bool, accumulate: bool, grads=None):
     """(config, shapes of a, of a channels' vector, of a state); grads: of x, delta, b, c and gate."""
-    _need(x.dim() == 3, "x must be batch x steps x channels")
+    shape, kind, shared = x.shape, x.dtype, b.shape
+    _need(len(shape) == 3, "x must be batch x steps x channels")
     _need(a.dim() == 2, "a must be channels x states")
-    _need(b.dim() in (3, 4), "b must be batch x steps x groups x states")
-    batch, steps, channels = x.shape
-    states, groups = a.shape[1], b.shape[2] if b.dim() == 4 else 1
-    shape, kind = tuple(x.shape), x.dtype
-    shared = (batch, steps, groups, states) if b.dim() == 4 else (batch, steps, states)
-    near = [*_parts_of(x, "x", shape, kind), *_parts_of(delta, "delta", shape, kind), *_parts_of(b, "b", shared, kind),
+    _need(len(shared) == 3 or len(shared) == 4, "b must be batch x steps x groups x states")
+    batch, steps, channels = shape
+    states, groups = a.shape[1], shared[2] if len(shared) == 4 else 1
+    if shared[0] != batch or shared[1] != steps or shared[-1] != states:
+        raise ValueError(f"b must be {batch} x {steps} x groups x {states}")
+    near = (*_parts_of(x, "x", shape, kind), *_parts_of(delta, "delta", shape, kind), *_parts_of(b, "b", shared, kind),
             *_parts_of(c, "c", shared, kind), *((0, 0) if gate is None else _parts_of(gate, "gate", shape, kind)),
-            *_parts_of(out, name, shape, kind)]
-    far = [0] * 10
-    if grads is not None:
+            *_parts_of(out, name, shape, kind))
+    if grads is None:
+        far = (0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
+    else:
         gx, gdelta, gb, gc, ggate = grads
         _need((gate is None) == (ggate is None), "gate and grad_gate go together")
-        far = [*_parts_of(gx, "grad_x", shape, kind), *_parts_of(gdelta, "grad_delta", shape, kind), *_parts_of(gb, "grad_b", shared, kind),
-               *_parts_of(gc, "grad_c", shared, kind), *((0, 0) if ggate is None else _parts_of(ggate, "grad_gate", shape, kind))]
+        far = (*_parts_of(gx, "grad_x", shape, kind), *_parts_of(gdelta, "grad_delta", shape, kind), *_parts_of(gb, "grad_b", shared, kind),
+               *_parts_of(gc, "grad_c", shared, kind), *((0, 0) if ggate is None else _parts_of(ggate, "grad_gate", shape, kind)))
     cfg = acc_scan(batch, steps, channels, *near, *far, states, groups, _type_of(x, "x"), softplus, accumulate)
     return cfg, (channels, states), (channels,), (batch, channels, states)
 
@@ -548,14 +555,13 @@ def scan_forward(x, delta, a, b, c, out, d=None, gate=None, delta_bias=None, sof
     tensors x, delta, gate and out; dt = delta + delta_bias, or its softplus; a: channels x states, b and c: batch x steps x groups x
     states (without the third dimension: one group); h0, h_last: batch x channels x states, float32.  steps = 1 with h0 and h_last: one
     token."""
-    import torch
     lib = load_library()
     cfg, wide, flat, ends = _scan(x, delta, a, b, c, out, "out", gate, softplus, False)
-    f = torch.float32
+    f = _FLOAT32
     decay, skip, shift = _plain(a, "a", wide, f), _plain(d, "d", flat, f), _plain(delta_bias, "delta_bias", flat, f)
-    first, last, n_steps = _plain(h0, "h0", ends, f), _plain(h_last, "h_last", ends, f), _plain(lengths, "lengths", ends[:1], torch.int32)
+    first, last, n_steps = _plain(h0, "h0", ends, f), _plain(h_last, "h_last", ends, f), _plain(lengths, "lengths", ends[:1], _INT32)
     gpu = _gpu_of(x, delta, a, b, c, out, d, gate, delta_bias, h0, h_last, lengths)
-    held, ws, n = _workspace(gpu, lambda cfg, n: lib.accordion_scan_workspace_bytes(cfg, 0, n), cfg, workspace)
+    held, ws, n = _workspace(gpu, lib.accordion_scan_workspace_bytes, cfg, workspace, 0)
     _launch(gpu, lib.accordion_scan_forward, C.byref(cfg), x.data_ptr(), delta.data_ptr(), decay, b.data_ptr(), c.data_ptr(), skip,
             _pointer(gate), shift, first, n_steps, out.data_ptr(), last, ws, n)
 
@@ -565,56 +571,56 @@ def scan_backward(x, delta, a, b, c, grad_out, grad_x, grad_delta, grad_a, grad_
                   accumulate: bool = False, workspace=None) -> None:
     """Gradients of scan_forward, from its inputs alone; grad_last is the gradient of h_last (None: zeros); accumulate adds to grad_a,
     grad_d and grad_delta_bias."""
-    import torch
     lib = load_library()
     cfg, wide, flat, ends = _scan(x, delta, a, b, c, grad_out, "grad_out", gate, softplus, accumulate,
                                   (grad_x, grad_delta, grad_b, grad_c, grad_gate))
-    f = torch.float32
+    f = _FLOAT32
     decay, skip, shift = _plain(a, "a", wide, f), _plain(d, "d", flat, f), _plain(delta_bias, "delta_bias", flat, f)
     da, dd = _plain(grad_a, "grad_a", wide, f), _plain(grad_d, "grad_d", flat, f)
     dbias = _plain(grad_delta_bias, "grad_delta_bias", flat, f)
     first, dl, dh = _plain(h0, "h0", ends, f), _plain(grad_last, "grad_last", ends, f), _plain(grad_h0, "grad_h0", ends, f)
-    n_steps = _plain(lengths, "lengths", ends[:1], torch.int32)
+    n_steps = _plain(lengths, "lengths", ends[:1], _INT32)
     gpu = _gpu_of(x, delta, a, b, c, grad_out, grad_x, grad_delta, grad_a, grad_b, grad_c, d, grad_d, gate, grad_gate, delta_bias,
                   grad_delta_bias, h0, grad_last, grad_h0, lengths)
-    held, ws, n = _workspace(gpu, lambda cfg, n: lib.accordion_scan_workspace_bytes(cfg, 1, n), cfg, workspace)
+    held, ws, n = _workspace(gpu, lib.accordion_scan_workspace_bytes, cfg, workspace, 1)
     _launch(gpu, lib.accordion_scan_backward, C.byref(cfg), x.data_ptr(), delta.data_ptr(), decay, b.data_ptr(), c.data_ptr(), skip,
             _pointer(gate), shift, first, n_steps, grad_out.data_ptr(), dl, grad_x.data_ptr(), grad_delta.data_ptr(), da, grad_b.data_ptr(),
             grad_c.data_ptr(), dd, _pointer(grad_gate), dbias, dh, ws, n)
 
 
-def _logprob(logits, targets, other, rows_like):
-    """(config, index type) of rows of logits; other: a second tensor of indices, or None."""
-    import torch
+def _logprob(logits, targets, top: int, bits: int, grad_logits=None) -> acc_logprob:
     rows, vocab, stride = _rows_of(logits, "logits")
-    index = next((t.dtype for t in (targets, other) if t is not None), torch.int64)
-    bits = _INDEX_BITS.get(index)
-    _need(bits is not None, "targets and top_ids must be int32 or int64")
     grad_stride = 0
-    if rows_like is not None:
-        g_rows, g_vocab, grad_stride = _rows_of(rows_like, "grad_logits")
-        _need(g_rows == rows and g_vocab == vocab and rows_like.dtype == logits.dtype, "logits and grad_logits do not fit together")
+    if grad_logits is not None:
+        g_rows, g_vocab, grad_stride = _rows_of(grad_logits, "grad_logits")
+        _need(g_rows == rows and g_vocab == vocab and grad_logits.dtype is logits.dtype, "logits and grad_logits do not fit together")
     if targets is not None:
+        bits = _INDEX_BITS.get(targets.dtype)
+        _need(bits is not None, "targets must be int32 or int64")
         _need(targets.numel() == rows and targets.is_contiguous(), "targets must be contiguous, one per row of logits")
-    return acc_logprob(rows, vocab, stride, grad_stride, bits, _type_of(logits, "logits"), 0), index
+    return acc_logprob(rows, vocab, stride, grad_stride, bits, _type_of(logits, "logits"), top)
 
 
 def logprob_forward(logits, targets=None, logprob=None, lse=None, entropy=None, top_logprobs=None, top_ids=None, workspace=None) -> None:
     """Per row of logits: logprob of the row's target (zero where that is outside the vocabulary), lse the logarithm of the sum of
     exponentials, the entropy, and the most probable tokens' log probabilities and ids (rows x top), the largest first, of equal logits the
     lowest id first.  What is None is not computed."""
-    import torch
     lib = load_library()
-    cfg, index = _logprob(logits, targets, top_ids, None)
     _need((top_logprobs is None) == (top_ids is None), "top_logprobs and top_ids go together")
     _need(logprob is None or targets is not None, "logprob needs targets")
-    f, rows = torch.float32, (cfg.rows,)
+    top, bits = 0, 64
     if top_ids is not None:
-        _need(top_ids.dim() == 2, "top_ids must be rows x top")
-        cfg.top = top_ids.shape[1]
-    best = (cfg.rows, cfg.top)
+        bits = _INDEX_BITS.get(top_ids.dtype)
+        _need(bits is not None and top_ids.dim() == 2, "top_ids must be int32 or int64, rows x top")
+        _need(targets is None or targets.dtype is top_ids.dtype, "top_ids must be of targets' type")
+        top = top_ids.shape[1]
+    cfg = _logprob(logits, targets, top, bits)
+    f, rows = _FLOAT32, (cfg.rows,)
     lp, ls, en = _plain(logprob, "logprob", rows, f), _plain(lse, "lse", rows, f), _plain(entropy, "entropy", rows, f)
-    tv, ti = _plain(top_logprobs, "top_logprobs", best, f), _plain(top_ids, "top_ids", best, index)
+    tv = ti = None
+    if top_ids is not None:
+        best = (cfg.rows, top)
+        tv, ti = _plain(top_logprobs, "top_logprobs", best, f), _plain(top_ids, "top_ids", best, top_ids.dtype)
     gpu = _gpu_of(logits, targets, logprob, lse, entropy, top_logprobs, top_ids)
     held, ws, n = _workspace(gpu, lib.accordion_logprob_workspace_bytes, cfg, workspace)
     _launch(gpu, lib.accordion_logprob_forward, C.byref(cfg), logits.data_ptr(), _pointer(targets), lp, ls, en, tv, ti, ws, n)
@@ -623,10 +629,9 @@ def logprob_forward(logits, targets=None, logprob=None, lse=None, entropy=None, 
 def logprob_backward(logits, targets, lse, grad_logprob, grad_logits, entropy=None, grad_entropy=None) -> None:
     """The logits' gradient from those of logprob (may be None) and, with grad_entropy, of the entropy; lse and entropy are what the
     forward pass wrote.  grad_logits may be logits."""
-    import torch
     lib = load_library()
-    cfg, _ = _logprob(logits, targets, None, grad_logits)
-    f, rows = torch.float32, (cfg.rows,)
+    cfg = _logprob(logits, targets, 0, 64, grad_logits)
+    f, rows = _FLOAT32, (cfg.rows,)
     ls, dl = _plain(lse, "lse", rows, f), _plain(grad_logprob, "grad_logprob", rows, f)
     en, de = _plain(entropy, "entropy", rows, f), _plain(grad_entropy, "grad_entropy", rows, f)
     _launch(_gpu_of(logits, targets, lse, grad_logprob, grad_logits, entropy, grad_entropy), lib.accordion_logprob_backward, C.byref(cfg),

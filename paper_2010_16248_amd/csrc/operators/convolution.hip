@@ -33,17 +33,20 @@ struct ConvolutionPlan {
   int64_t bytes = 0;                                   // workspace of the backward pass
 };
 
-// Runs as long as leave the chip this many waves.
-constexpr int64_t kConvolutionWaves = 4096;
+// Runs as long as leave the chip this many waves, from 8 to 128 steps.  us with runs of 8, 16, 32, 64, 128, 256 steps, width 4 with SiLU:
+// bf16 8 x 4096 x 4096 forward 147, 133, 121, 124, 106, 139, backward 376, 281, 238, 221, 179, 179; fp32 forward 251, 237, 223, 215, 210, 219,
+// backward 451, 393, 375, 334, 334, 342; bf16 1 x 2048 x 1536 forward 7.8, 10.3, 15.6, 26, 47, 89, backward 17, 17, 22, 32, 54, 97; width 3
+// fp32 7 x 1999 x 1001 forward 23, 24, 24, 29, 50, 94, backward 51, 47, 46, 61, 101, 187.
+constexpr int64_t kConvolutionWaves = 2048;
 
 ConvolutionPlan plan_convolution(const acc_convolution& c, bool backward) {
   ConvolutionPlan p;
   const int pack = backward || c.type == ACC_FLOAT ? 4 : 8;
   while (p.lanes_log2 < 6 && ((int64_t)pack << p.lanes_log2) < c.channels) ++p.lanes_log2;
   p.across = up(c.channels, (int64_t)pack << p.lanes_log2);
-  p.run = backward ? 128 : 64;
-  const int64_t least = backward ? 16 : 8, per_wave = kWave >> p.lanes_log2;
-  while (p.run > least && c.batch * up(c.steps, p.run) * p.across / per_wave < kConvolutionWaves) p.run /= 2;
+  p.run = 128;
+  const int64_t per_wave = kWave >> p.lanes_log2;
+  while (p.run > 8 && c.batch * up(c.steps, p.run) * p.across / per_wave < kConvolutionWaves) p.run /= 2;
   while (c.batch * up(c.steps, p.run) > (int64_t(1) << 25)) p.run *= 2;     // lanes of a launch: see kRowsPerLaunch
   p.runs = std::max<int64_t>(1, up(c.steps, p.run));
   p.blocks = up((c.batch * p.runs) << p.lanes_log2, 256);
@@ -54,6 +57,10 @@ ConvolutionPlan plan_convolution(const acc_convolution& c, bool backward) {
 ConvolutionShape shape_of(const acc_convolution& c, const ConvolutionPlan& p) {
   return {c.batch, c.steps, c.channels, c.x_batch, c.x_step, c.out_batch, c.out_step, c.grad_x_batch, c.grad_x_step, p.run, p.runs, p.lanes_log2};
 }
+
+// Whether every pack of N channels is whole and a wave has one run.
+template <int N>
+bool full(const acc_convolution& c, const ConvolutionPlan& p) { return c.channels % N == 0 && p.lanes_log2 == 6; }
 
 template <typename F>
 void with_width(int width, F&& run) {
@@ -75,12 +82,9 @@ void forward(const acc_convolution& c, const ConvolutionPlan& p, const void* x, 
   with_width(c.width, [&](auto width) {
     constexpr int W = decltype(width)::value;
     const dim3 grid((unsigned)p.blocks, (unsigned)p.across);
-    if (c.silu)
-      LAUNCH((convolution_forward_kernel<T, N, W, true>), grid, dim3(256), queue, shape_of(c, p), static_cast<const T*>(x), weight, bias,
-             state, lengths, static_cast<T*>(out), last);
-    else
-      LAUNCH((convolution_forward_kernel<T, N, W, false>), grid, dim3(256), queue, shape_of(c, p), static_cast<const T*>(x), weight, bias,
-             state, lengths, static_cast<T*>(out), last);
+    const auto kernel = full<N>(c, p) ? convolution_forward_kernel<T, N, W, true> : convolution_forward_kernel<T, N, W, false>;
+    LAUNCH(kernel, grid, dim3(256), queue, shape_of(c, p), static_cast<const T*>(x), weight, bias, state, lengths, static_cast<T*>(out), last,
+           c.silu);
   });
 }
 
@@ -91,12 +95,9 @@ void backward(const acc_convolution& c, const ConvolutionPlan& p, const void* x,
   with_width(c.width, [&](auto width) {
     constexpr int W = decltype(width)::value;
     const dim3 grid((unsigned)p.blocks, (unsigned)p.across);
-    if (c.silu)
-      LAUNCH((convolution_backward_kernel<T, N, W, true>), grid, dim3(256), queue, shape_of(c, p), static_cast<const T*>(x), weight, bias,
-             state, lengths, static_cast<const T*>(dout), dlast, static_cast<T*>(dx), dstate, parts);
-    else
-      LAUNCH((convolution_backward_kernel<T, N, W, false>), grid, dim3(256), queue, shape_of(c, p), static_cast<const T*>(x), weight, bias,
-             state, lengths, static_cast<const T*>(dout), dlast, static_cast<T*>(dx), dstate, parts);
+    const auto kernel = full<N>(c, p) ? convolution_backward_kernel<T, N, W, true> : convolution_backward_kernel<T, N, W, false>;
+    LAUNCH(kernel, grid, dim3(256), queue, shape_of(c, p), static_cast<const T*>(x), weight, bias, state, lengths,
+           static_cast<const T*>(dout), dlast, static_cast<T*>(dx), dstate, parts, c.silu);
   });
 }
 

@@ -162,7 +162,11 @@ __global__ __launch_bounds__(256) void logprob_stream_kernel(LogprobOut o, const
 constexpr int kTopGroups = 64;
 constexpr int kTopList = 1024;
 
-__device__ __forceinline__ bool before(uint2 a, uint2 b) { return a.x > b.x || (a.x == b.x && a.y < b.y); }
+// A token in the order of the most probable ones: its logit's key, then its id, the lowest first.  0: no token.
+typedef unsigned long long Token;
+__device__ __forceinline__ Token token_of(float l, unsigned id) { return (Token)key_at(l) << 32 | ~id; }
+__device__ __forceinline__ float logit_of(Token t) { return logit_of((unsigned)(t >> 32)); }
+__device__ __forceinline__ unsigned id_of(Token t) { return ~(unsigned)t; }
 
 __device__ __forceinline__ float wave_top(float v) {
   v = fmaxf(v, dpp<0xB1>(v));
@@ -172,29 +176,28 @@ __device__ __forceinline__ float wave_top(float v) {
   return fmaxf(fmaxf(lane(v, 0), lane(v, 16)), fmaxf(lane(v, 32), lane(v, 48)));
 }
 
-// Tokens in front of one of the list's.
-__device__ __forceinline__ int place_in(const uint2* list, int count, uint2 token) {
+// Tokens in front of one of a list's, which is filled up with "no token" to whole eights.
+__device__ __forceinline__ int place_in(const Token* list, int count, Token token) {
   int place = 0;
-  int j = 0;
-  for (; j + 8 <= count; j += 8) {
-    uint2 o[8];
+  for (int j = 0; j < count; j += 8) {
+    Token o[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) o[k] = list[j + k];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) place += before(o[k], token);
+    for (int k = 0; k < 8; ++k) place += o[k] > token;
   }
-  for (; j < count; ++j) place += before(list[j], token);
   return place;
 }
 
 template <typename T, int N, int K, int THREADS, bool PARTS>
 __global__ __launch_bounds__(THREADS) void logprob_top_kernel(LogprobOut o, const T* __restrict__ logits, int64_t part, int parts,
-                                                              RowSums* __restrict__ sums, uint2* __restrict__ best) {
+                                                              RowSums* __restrict__ sums, Token* __restrict__ best) {
   constexpr int waves = THREADS / kWave, each = THREADS / kTopGroups;       // lanes of a group
   static_assert(each == 4 || each == 16, "groups are whole rows or quarters of rows of 16 lanes");
   __shared__ float group_top[kTopGroups], sum[waves], weighted[waves], least_of;
   __shared__ unsigned listed;
-  __shared__ uint2 list[kTopList], found[waves];
+  __shared__ alignas(16) Token list[kTopList];
+  __shared__ Token found[waves];
   const int64_t row = blockIdx.x;
   const int64_t from = blockIdx.y * part;
   const int size = (int)min(part, o.vocab - from);
@@ -211,7 +214,12 @@ __global__ __launch_bounds__(THREADS) void logprob_top_kernel(LogprobOut o, cons
       for (int i = 0; i < N; ++i) v[k][i] = i < left ? l[place + i] : (T)-INFINITY;
     }
   }
+  // (requested with the logits, used at the end)
+  bool named = false;
+  const float target = PARTS ? 0.f : target_of<T>(o, logits, row, &named);
   if (threadIdx.x == 0) listed = 0;
+#pragma unroll
+  for (int i = 0; i < kTopList; i += THREADS) list[i + threadIdx.x] = 0;
 #pragma unroll
   for (int k = 0; k < K; ++k) top = fmaxf(top, top_of<N>(widen<T, N>(v[k])));
   top = fmaxf(top, dpp<0xB1>(top));
@@ -259,79 +267,80 @@ __global__ __launch_bounds__(THREADS) void logprob_top_kernel(LogprobOut o, cons
       const int place = ((int)threadIdx.x + k * THREADS) * N + i;
       if (!(wide[i] < least) && place < size) {
         const unsigned at = atomicAdd(&listed, 1u);
-        if (at < kTopList) list[at] = make_uint2(key_at(wide[i]), (unsigned)(from + place));
+        if (at < kTopList) list[at] = token_of(wide[i], (unsigned)(from + place));
       }
     }
   }
   __syncthreads();
   const int count = (int)listed, wanted = min(o.top, size);     // tokens this part can give
-  auto put = [&](int place, uint2 token) {
+  auto put = [&](int place, Token token) {
     if (PARTS) best[(row * parts + blockIdx.y) * o.top + place] = token;
-    else write_top(o, row, place, r, logit_of(token.x), token.y);
+    else write_top(o, row, place, r, logit_of(token), id_of(token));
   };
   if (count <= kTopList) {
     for (int i = threadIdx.x; i < count; i += THREADS) {
-      const uint2 token = list[i];
+      const Token token = list[i];
       const int place = place_in(list, count, token);
       if (place < wanted) put(place, token);
     }
   } else {
-    uint2 after = make_uint2(~0u, 0u);             // in front of every token: no key is as large
+    Token after = ~(Token)0;                       // in front of every token: no key is as large
     for (int place = 0; place < wanted; ++place) {
-      uint2 mine = make_uint2(0u, ~0u);            // behind every token
+      Token mine = 0;
       for (int at = threadIdx.x; at < size; at += THREADS) {
-        const uint2 other = make_uint2(key_at(l[at]), (unsigned)(from + at));
-        if (before(after, other) && before(other, mine)) mine = other;
+        const Token other = token_of((float)l[at], (unsigned)(from + at));
+        if (other < after && other > mine) mine = other;
       }
 #pragma unroll
       for (int m = 1; m < kWave; m *= 2) {
-        const uint2 other = make_uint2(__shfl_xor((int)mine.x, m), __shfl_xor((int)mine.y, m));
-        if (before(other, mine)) mine = other;
+        const Token other = __shfl_xor(mine, m);
+        if (other > mine) mine = other;
       }
       __syncthreads();
       if ((threadIdx.x & 63) == 0) found[threadIdx.x >> 6] = mine;
       __syncthreads();
       for (int w = 0; w < waves; ++w)
-        if (before(found[w], mine)) mine = found[w];
+        if (found[w] > mine) mine = found[w];
       if (threadIdx.x == 0) put(place, mine);
       after = mine;
     }
   }
-  // what a short part does not have comes behind every token
   if (PARTS)
-    for (int place = wanted + threadIdx.x; place < o.top; place += THREADS) put(place, make_uint2(0u, ~0u));
+    for (int place = wanted + threadIdx.x; place < o.top; place += THREADS) put(place, 0);
   if (threadIdx.x != 0) return;
-  if (PARTS) {
-    sums[row * parts + blockIdx.y] = r;
-  } else {
-    bool named;
-    const float t = target_of<T>(o, logits, row, &named);
-    write_row(o, row, r, t, named);
-  }
+  if (PARTS) sums[row * parts + blockIdx.y] = r;
+  else write_row(o, row, r, target, named);
 }
 
 // Joins a row's parts: their sums in order, and the most probable of their most probable tokens, by counting.
+constexpr int kJoinThreads = 512;
 template <typename T>
-__global__ __launch_bounds__(256) void logprob_join_kernel(LogprobOut o, const T* __restrict__ logits, int parts,
-                                                           const RowSums* __restrict__ sums, const uint2* __restrict__ best) {
-  extern __shared__ uint2 tokens[];
-  __shared__ RowSums red[4];
+__global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(LogprobOut o, const T* __restrict__ logits, int parts,
+                                                                    const RowSums* __restrict__ sums, const Token* __restrict__ best) {
+  extern __shared__ Token tokens[];
   const int64_t row = blockIdx.x;
-  RowSums r = no_sums();
-  for (int i = threadIdx.x; i < parts; i += 256) r = joined(r, sums[row * parts + i]);
-  const int count = parts * o.top;
-  for (int i = threadIdx.x; i < count; i += 256) tokens[i] = best[row * count + i];
-  r = group_sums<256>(r, red);
-  for (int i = threadIdx.x; i < count; i += 256) {
-    const uint2 token = tokens[i];
-    if (token.y == ~0u) continue;
-    const int place = place_in(tokens, count, token);
-    if (place < o.top) write_top(o, row, place, r, logit_of(token.x), token.y);
-  }
-  if (threadIdx.x != 0) return;
   bool named;
-  const float t = target_of<T>(o, logits, row, &named);
-  write_row(o, row, r, t, named);
+  const float target = target_of<T>(o, logits, row, &named);
+  const int count = parts * o.top;
+  for (int i = threadIdx.x; i < (count + 7) / 8 * 8; i += kJoinThreads) tokens[i] = i < count ? best[row * count + i] : 0;
+  // (every thread for itself: the parts' sums come through scalar loads)
+  RowSums r = no_sums();
+  const RowSums* const of = sums + row * parts;
+  for (int i = 0; i < parts; ++i) r.top = fmaxf(r.top, of[i].top);
+  for (int i = 0; i < parts; ++i) {
+    RowSums q = of[i];
+    raise(q, r.top);
+    r.s += q.s;
+    r.t += q.t;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < count; i += kJoinThreads) {
+    const Token token = tokens[i];
+    if (token == 0) continue;
+    const int place = place_in(tokens, count, token);
+    if (place < o.top) write_top(o, row, place, r, logit_of(token), id_of(token));
+  }
+  if (threadIdx.x == 0) write_row(o, row, r, target, named);
 }
 
 // ---- backward ---------------------------------------------------------------------------------------------

@@ -26,25 +26,20 @@ struct LogprobPlan {
 
 constexpr int64_t kLogprobGroups = 1024;      // workgroups that fill the chip
 constexpr int64_t kStreamPart = 8192;         // elements of a part at least
+// Parts of 32768 tokens where so many workgroups of 1024 lanes take all rows in two turns, of 8192 (as many as kTopMostSmall) where there are more.
+// us of parts of 8192 and of 32768, 20 tokens wanted: 1 x 32768 fp32 10.3 and 7.7, 1 x 131072 15.2 and 10.8, 128 x 131072 bf16 22.6 and 17.9,
+// 700 x 16384 fp32 18.8 and 20.1, 700 x 65536 41.9 and 50.0, 4096 x 16384 57 and 91, 4096 x 65536 225 and 258; 700 x 32768 bf16 23.6 and 21.1.
+constexpr int64_t kTopGroupsAtOnce = 512, kTopMostSmall = 64;
 
 LogprobPlan plan_logprob(const acc_logprob& c) {
   LogprobPlan p;
   const int64_t n = c.type == ACC_BF16 ? 8 : 4;
   if (c.top > 0) {
-    // parts that 256 lanes or, where there are rows enough, 1024 hold
+    // parts that 256 lanes hold, or 1024
     const int64_t small = 256 * 32;
-    if (c.vocab <= 256 * n) p.packs = 1;
-    else if (c.vocab <= 256 * 8) p.packs = (int)(8 / n);
-    else p.packs = (int)(32 / n);
-    p.part = 256 * n * p.packs;
-    if (c.vocab > small && c.rows * up(c.vocab, small) > kLogprobGroups) {
-      p.threads = 1024;
-      p.part = 1024 * n * p.packs;
-    }
-    if (up(c.vocab, p.part) > 32 && p.threads == 256) {
-      p.threads = 1024;
-      p.part = 1024 * n * p.packs;
-    }
+    p.packs = (int)(c.vocab <= 256 * n ? 1 : (c.vocab <= 256 * 8 ? 8 : 32) / n);
+    if (c.vocab > small && (c.rows * up(c.vocab, 4 * small) <= kTopGroupsAtOnce || c.vocab > kTopMostSmall * small)) p.threads = 1024;
+    p.part = p.threads * n * p.packs;
   } else {
     p.part = c.vocab;
     if (c.rows < kLogprobGroups) p.part = std::max(kStreamPart, up(c.vocab, up(kLogprobGroups, std::max<int64_t>(1, c.rows))));
@@ -61,7 +56,7 @@ LogprobPlan plan_logprob(const acc_logprob& c) {
 }
 
 template <typename T, int N, int K, int THREADS>
-void top_rows(const LogprobPlan& p, const LogprobOut& o, const T* logits, int64_t rows, RowSums* sums, uint2* best, Queue& queue) {
+void top_rows(const LogprobPlan& p, const LogprobOut& o, const T* logits, int64_t rows, RowSums* sums, Token* best, Queue& queue) {
   const dim3 grid((unsigned)rows, (unsigned)p.parts);
   if (p.parts > 1) LAUNCH((logprob_top_kernel<T, N, K, THREADS, true>), grid, dim3(THREADS), queue, o, logits, p.part, (int)p.parts, sums, best);
   else LAUNCH((logprob_top_kernel<T, N, K, THREADS, false>), grid, dim3(THREADS), queue, o, logits, p.part, 1, sums, best);
@@ -80,7 +75,7 @@ void forward(const acc_logprob& c, const LogprobPlan& p, const LogprobOut& all, 
     if (o.top_logprobs) o.top_logprobs += r * c.top;
     if (o.top_ids) o.top_ids = static_cast<char*>(o.top_ids) + r * c.top * (c.index_bits / 8);
     RowSums* const sums = reinterpret_cast<RowSums*>(ws + p.sums) + (p.parts > 1 ? r * p.parts : 0);
-    uint2* const best = reinterpret_cast<uint2*>(ws + p.best) + (p.parts > 1 ? r * p.parts * c.top : 0);
+    Token* const best = reinterpret_cast<Token*>(ws + p.best) + (p.parts > 1 ? r * p.parts * c.top : 0);
     const T* const from = logits + r * c.logits_stride;
     if (c.top > 0) {
       if (p.threads == 1024) top_rows<T, N, 32 / N, 1024>(p, o, from, rows, sums, best, queue);
@@ -101,7 +96,8 @@ void forward(const acc_logprob& c, const LogprobPlan& p, const LogprobOut& all, 
 #undef STREAM
     }
     if (p.parts > 1)
-      enqueue(queue, logprob_join_kernel<T>, dim3((unsigned)rows), dim3(256), (unsigned)(8 * p.parts * c.top), o, from, (int)p.parts, sums, best);
+      enqueue(queue, logprob_join_kernel<T>, dim3((unsigned)rows), dim3(kJoinThreads),
+              (unsigned)(8 * up(p.parts * c.top, 8) * 8), o, from, (int)p.parts, sums, best);
   }
 }
 

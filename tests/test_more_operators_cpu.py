@@ -276,7 +276,7 @@ def test_tensors_that_do_not_fit_are_refused():
         B.logprob_forward(logits, z(3), z(3))
     with pytest.raises(ValueError, match="one per row"):
         B.logprob_forward(logits, z(4, k=torch.int64), z(3))
-    with pytest.raises(ValueError, match="top_ids must be"):
+    with pytest.raises(ValueError, match="of targets' type"):
         B.logprob_forward(logits, ids, z(3), top_logprobs=z(3, 2), top_ids=z(3, 2, k=torch.int32))
     with pytest.raises(ValueError, match="lse"):
         B.logprob_forward(logits, ids, z(3), lse=z(2))
