@@ -503,11 +503,12 @@ int32_t accordion_convolution_backward(const acc_convolution* cfg, const void* x
  * lengths_dev as for the recurrence: steps from a sequence's length on write zeros and leave the state as it is; what
  * their inputs hold plays no role.  steps = 1 is the serving form: one token, the state in h0 and h_last (which may be the same buffer
  * then, and for any number of steps).
- * exp(dt a) below the normal fp32 numbers counts as zero. */
+ * exp(dt a) below the normal fp32 numbers counts as zero.
+ * More than 8 steps: batch x groups x steps x states, filled up to 4, 8, 16, 32 or 64, below 1.5e9. */
 typedef struct acc_scan {
   int64_t batch;                 /* [0, 65535] */
   int64_t steps;                 /* [0, 2^31); backward: up to 2^21 */
-  int64_t channels;              /* [1, 2^24], a multiple of groups */
+  int64_t channels;              /* [1, 2^20], a multiple of groups */
   /* elements between sequences and between steps; backward: out is grad_out */
   int64_t x_batch, x_step, delta_batch, delta_step, b_batch, b_step, c_batch, c_step, gate_batch, gate_step, out_batch, out_step;
   /* the same of the gradients (backward) */

@@ -465,10 +465,13 @@ def recurrence_backward(gate, input, out, grad_out, grad_gate, grad_input, h0=No
             grad_out.data_ptr(), last, grad_gate.data_ptr(), grad_input.data_ptr(), dh0, ws, n)
 
 
-def _parts_of(t, name: str, shape, dtype) -> Tuple[int, int]:
-    """(elements between sequences, between steps) of a batch x steps x ... tensor whose steps' elements are contiguous."""
+def _parts_of(t, name: str, shape, dtype, whole) -> Tuple[int, int]:
+    """(elements between sequences, between steps) of a batch x steps x ... tensor whose steps' elements are contiguous; whole: of one that
+    is contiguous throughout."""
     if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype}, of shape {tuple(shape)}")
+    if t.is_contiguous():
+        return whole
     stride = t.stride()
     if len(stride) == 3:
         apart = stride[2] != 1 and shape[2] > 1
@@ -485,10 +488,10 @@ def _convolution(x, weight, out, name: str, silu: bool, accumulate: bool, grad_x
     _need(len(shape) == 3, "x must be batch x steps x channels")
     _need(weight.dim() == 2, "weight must be channels x width")
     batch, steps, channels = shape
-    width = weight.shape[1]
-    last = (0, 0) if grad_x is None else _parts_of(grad_x, "grad_x", shape, kind)
-    cfg = acc_convolution(batch, steps, channels, *_parts_of(x, "x", shape, kind), *_parts_of(out, name, shape, kind), *last, width,
-                          _type_of(x, "x"), silu, accumulate)
+    width, whole = weight.shape[1], (steps * channels, channels)
+    last = (0, 0) if grad_x is None else _parts_of(grad_x, "grad_x", shape, kind, whole)
+    cfg = acc_convolution(batch, steps, channels, *_parts_of(x, "x", shape, kind, whole), *_parts_of(out, name, shape, kind, whole), *last,
+                          width, _type_of(x, "x"), silu, accumulate)
     return cfg, (channels, width), (channels,), (batch, width - 1, channels)
 
 
@@ -531,16 +534,19 @@ def _scan(x, delta, a, b, c, out, name: str, gate, softplus: bool, accumulate: b
     states, groups = a.shape[1], shared[2] if len(shared) == 4 else 1
     if shared[0] != batch or shared[1] != steps or shared[-1] != states:
         raise ValueError(f"b must be {batch} x {steps} x groups x {states}")
-    near = (*_parts_of(x, "x", shape, kind), *_parts_of(delta, "delta", shape, kind), *_parts_of(b, "b", shared, kind),
-            *_parts_of(c, "c", shared, kind), *((0, 0) if gate is None else _parts_of(gate, "gate", shape, kind)),
-            *_parts_of(out, name, shape, kind))
+    row = groups * states
+    whole, part = (steps * channels, channels), (steps * row, row)
+    near = (*_parts_of(x, "x", shape, kind, whole), *_parts_of(delta, "delta", shape, kind, whole), *_parts_of(b, "b", shared, kind, part),
+            *_parts_of(c, "c", shared, kind, part), *((0, 0) if gate is None else _parts_of(gate, "gate", shape, kind, whole)),
+            *_parts_of(out, name, shape, kind, whole))
     if grads is None:
         far = (0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
     else:
         gx, gdelta, gb, gc, ggate = grads
         _need((gate is None) == (ggate is None), "gate and grad_gate go together")
-        far = (*_parts_of(gx, "grad_x", shape, kind), *_parts_of(gdelta, "grad_delta", shape, kind), *_parts_of(gb, "grad_b", shared, kind),
-               *_parts_of(gc, "grad_c", shared, kind), *((0, 0) if ggate is None else _parts_of(ggate, "grad_gate", shape, kind)))
+        far = (*_parts_of(gx, "grad_x", shape, kind, whole), *_parts_of(gdelta, "grad_delta", shape, kind, whole),
+               *_parts_of(gb, "grad_b", shared, kind, part), *_parts_of(gc, "grad_c", shared, kind, part),
+               *((0, 0) if ggate is None else _parts_of(ggate, "grad_gate", shape, kind, whole)))
     cfg = acc_scan(batch, steps, channels, *near, *far, states, groups, _type_of(x, "x"), softplus, accumulate)
     return cfg, (channels, states), (channels,), (batch, channels, states)
 

@@ -174,7 +174,7 @@ int32_t accordion_convolution_backward(const acc_convolution* c, const void* x_d
       backward<float, 4>(*c, p, x_dev, weight_dev, bias_dev, state_dev, lengths_dev, grad_out_dev, grad_last_dev, grad_x_dev,
                          grad_state_dev, parts, queue);
   }
-  LAUNCH(parts_join_kernel, dim3((unsigned)up(c->channels, kWave), (unsigned)(c->width + 1)), dim3(1024), queue, parts, p.blocks,
+  LAUNCH(parts_join_kernel, dim3((unsigned)up(c->channels, kWave), (unsigned)(c->width + 1)), dim3(kPartsThreads), queue, parts, p.blocks,
          c->width + 1, c->channels, PartsTo{grad_weight_dev, c->width, grad_bias_dev, nullptr}, c->accumulate);
   return launched(queue);
 }

@@ -13,18 +13,18 @@ struct PartsTo {
 };
 
 // A workgroup takes 64 channels of one row, each of its 16 waves a run of consecutive parts.
-constexpr int kPartsAhead = 16;   // parts under way
-static __global__ __launch_bounds__(1024) void parts_join_kernel(const float* __restrict__ parts, int64_t count, int rows, int64_t channels,
-                                                          PartsTo to, int accumulate) {
-  __shared__ float fold[16][kWave];
-  const int l = threadIdx.x & 63, w = threadIdx.x >> 6, row = blockIdx.y;
-  const int64_t c = (int64_t)blockIdx.x * kWave + l;
+constexpr int kPartsThreads = 1024, kPartsAhead = 16;   // parts under way
+__device__ __forceinline__ void parts_join(const float* parts, int64_t count, int rows, int64_t channels, const PartsTo& to, int accumulate,
+                                           unsigned block, int row, float* fold) {
+  constexpr int waves = kPartsThreads / kWave;
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t c = (int64_t)block * kWave + l;
   float* at = row < to.columns ? to.matrix + c * to.columns + row : (row == to.columns ? to.first : to.second);
   if (row >= to.columns) {
     if (!at) return;
     at += c;
   }
-  const int64_t share = (count + 15) / 16, lo = w * share, hi = min(count, lo + share);
+  const int64_t share = (count + waves - 1) / waves, lo = w * share, hi = min(count, lo + share);
   float s = 0.f;
   if (c < channels)
     for (int64_t i = lo; i < hi; i += kPartsAhead) {
@@ -34,13 +34,19 @@ static __global__ __launch_bounds__(1024) void parts_join_kernel(const float* __
 #pragma unroll
       for (int k = 0; k < kPartsAhead; ++k) s += v[k];
     }
-  fold[w][l] = s;
+  fold[w * kWave + l] = s;
   __syncthreads();
   if (w == 0 && c < channels) {
     s = 0.f;
-    for (int i = 0; i < 16; ++i) s += fold[i][l];
+    for (int i = 0; i < waves; ++i) s += fold[i * kWave + l];
     *at = accumulate ? *at + s : s;
   }
+}
+
+static __global__ __launch_bounds__(kPartsThreads) void parts_join_kernel(const float* __restrict__ parts, int64_t count, int rows,
+                                                                          int64_t channels, PartsTo to, int accumulate) {
+  __shared__ float fold[kPartsThreads];
+  parts_join(parts, count, rows, channels, to, accumulate, blockIdx.x, (int)blockIdx.y, fold);
 }
 
 }  // namespace accop

@@ -1,6 +1,7 @@
 // Selective state space scan h_t = exp(dt_t a) h_{t-1} + dt_t b_t x_t, y_t = c_t . h_t + d x_t: forward and backward pass.
 #pragma once
 #include "op_common.h"
+#include "parts.h"
 
 namespace accop {
 
@@ -84,7 +85,6 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanShape& s, const int32_
   p.channel = (unsigned)p.group * s.group + (p.valid ? within : s.group - 1);
   p.byte2 = 2 * p.channel;
   p.byte4 = 4 * p.channel;
-  asm("" : "+v"(p.byte2), "+v"(p.byte4));      // (a sum of a base in scalar registers and 32 bits, as the loads take it, not one in 64 bits)
   p.chunk = blockIdx.y;
   p.batch = blockIdx.z;
   p.len = steps_of(lengths, p.batch, s.steps);
@@ -94,11 +94,18 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanShape& s, const int32_
   return p;
 }
 
-// An element of a row that the wave has in common, at a lane's place.
-template <typename T>
-__device__ __forceinline__ T& in_row(T* row, const ScanPlace& p) {
-  return *reinterpret_cast<T*>((char*)row + (sizeof(T) == 2 ? p.byte2 : p.byte4));
-}
+// A lane's element of rows that the wave has in common: a base in scalar registers and 32 bits of a lane's, as one access takes them.  (The 32
+// bits go through an empty statement where the accesses are, or the compiler widens them once for all and adds 64 bits for each.)
+struct LaneOf {
+  unsigned byte2, byte4;
+  __device__ __forceinline__ explicit LaneOf(const ScanPlace& p) : byte2(p.byte2), byte4(p.byte4) {
+    asm volatile("" : "+v"(byte2), "+v"(byte4));
+  }
+  template <typename T>
+  __device__ __forceinline__ T& of(T* row) const {
+    return *reinterpret_cast<T*>((char*)row + (sizeof(T) == 2 ? byte2 : byte4));
+  }
+};
 
 // a log2(e) of a lane's states (zero beyond the last).
 template <int NP>
@@ -136,15 +143,17 @@ __device__ __forceinline__ int64_t slot_of(const ScanShape& s, const ScanPlace& 
 template <int NP, int WAVES>
 __device__ __forceinline__ void load_slots(const ScanShape& s, const ScanPlace& p, const float* from, float (&h)[NP]) {
   const float* at = from + slot_of<NP, WAVES>(s, p);
+  const LaneOf lane(p);
 #pragma unroll
-  for (int n = 0; n < NP; ++n) h[n] = in_row(at + n * s.channels, p);
+  for (int n = 0; n < NP; ++n) h[n] = lane.of(at + n * s.channels);
 }
 template <int NP, int WAVES>
 __device__ __forceinline__ void store_slots(const ScanShape& s, const ScanPlace& p, float* to, const float (&h)[NP]) {
   if (!p.valid) return;
   float* at = to + slot_of<NP, WAVES>(s, p);
+  const LaneOf lane(p);
 #pragma unroll
-  for (int n = 0; n < NP; ++n) in_row(at + n * s.channels, p) = h[n];
+  for (int n = 0; n < NP; ++n) lane.of(at + n * s.channels) = h[n];
 }
 
 // What scan_ends_kernel leaves in front of the turn at step t.
@@ -201,9 +210,10 @@ struct SharedGroup {
 // A channel's elements of a turn's steps (of the last one there is, beyond).
 template <typename T>
 __device__ __forceinline__ void load_turn(const T* row, int64_t stride, const ScanPlace& p, int last, T (&v)[kScanAhead]) {
+  const LaneOf lane(p);
 #pragma unroll
   for (int j = 0; j < kScanAhead; ++j) {
-    v[j] = in_row(row, p);
+    v[j] = lane.of(row);
     row += j < last ? stride : 0;
   }
 }
@@ -214,11 +224,19 @@ template <typename T>
 __device__ __forceinline__ void steps_and_inputs(const T (&xv)[kScanAhead], const T (&dv)[kScanAhead], float shift, int soft, int last,
                                                  float (&dt)[kScanAhead], float (&u)[kScanAhead]) {
 #pragma unroll
-  for (int j = 0; j < kScanAhead; ++j) {
-    const float raw = (float)dv[j] + shift;
-    const float v = soft ? softplus(raw).value : raw;
-    dt[j] = j <= last ? v : 0.f;
-    u[j] = j <= last ? v * (float)xv[j] : 0.f;
+  for (int j = 0; j < kScanAhead; ++j) dt[j] = (float)dv[j] + shift;
+  if (soft) {            // (one branch for all steps: their chains run side by side)
+#pragma unroll
+    for (int j = 0; j < kScanAhead; ++j) dt[j] = softplus(dt[j]).value;
+  }
+#pragma unroll
+  for (int j = 0; j < kScanAhead; ++j) u[j] = dt[j] * (float)xv[j];
+  if (last < kScanAhead - 1) {
+#pragma unroll
+    for (int j = 0; j < kScanAhead; ++j) {
+      u[j] = j <= last ? u[j] : 0.f;
+      dt[j] = j <= last ? dt[j] : 0.f;
+    }
   }
 }
 
@@ -260,12 +278,13 @@ __global__ __launch_bounds__(WAVES * kWave) void scan_ends_kernel(ScanShape s, c
     if (BACKWARD) {
       if (p.valid && t > p.from) {
         float* to = marks_of<NP, WAVES>(s, p, marks, t);
+        const LaneOf lane(p);
 #pragma unroll
         for (int n = 0; n < NP; ++n) {
-          in_row(to, p) = h[n];
+          lane.of(to) = h[n];
           to += s.channels;
         }
-        if (p.part == WAVES - 1) in_row(to, p) = sum;
+        if (p.part == WAVES - 1) lane.of(to) = sum;
       }
       load_turn(os, s.out_t, p, last, ov);
       if (gs) load_turn(gs, s.gate_t, p, last, gv);
@@ -274,13 +293,14 @@ __global__ __launch_bounds__(WAVES * kWave) void scan_ends_kernel(ScanShape s, c
     steps_and_inputs(xv, dv, shift, s.softplus, last, dt, u);
     if (BACKWARD) {
 #pragma unroll
-      for (int j = 0; j < U; ++j) {
-        dy[j] = (float)ov[j];
-        if (gs) {
-          const float gt = (float)gv[j];
-          dy[j] *= gt * sigmoid(gt).a;
-        }
-        if (j > last) dy[j] = 0.f;
+      for (int j = 0; j < U; ++j) dy[j] = (float)ov[j];
+      if (gs) {
+#pragma unroll
+        for (int j = 0; j < U; ++j) dy[j] *= (float)gv[j] * sigmoid((float)gv[j]).a;
+      }
+      if (last < U - 1) {
+#pragma unroll
+        for (int j = 0; j < U; ++j) dy[j] = j <= last ? dy[j] : 0.f;
       }
     }
 #pragma unroll
@@ -377,14 +397,17 @@ __global__ __launch_bounds__(kWave * kCarryWaves) void scan_carry_kernel(ScanSha
                                                                          const float* __restrict__ sums) {
   __shared__ float fold[kCarryWaves][2][kWave];
   const int64_t b = blockIdx.z, at = (int64_t)blockIdx.x * kWave + (threadIdx.x & 63), c = min(at, s.channels - 1);
-  const int n = blockIdx.y;
+  // (the gradients' workgroups lie behind the states')
+  const bool back = BACKWARD && blockIdx.y >= (unsigned)s.padded;
+  const int n = (int)blockIdx.y - (back ? s.padded : 0);
   const bool held = n < s.states, valid = at < s.channels;
   const float decay = held ? a[c * s.states + n] * kLog2e : 0.f;
   const int64_t own = (b * s.channels + c) * s.states + n, step = (int64_t)s.padded * s.channels;
   const int64_t first = (b * s.chunks * s.padded + n) * s.channels + c, last = first + (s.chunks - 1) * step;
   const float* const total = sums + b * s.chunks * s.channels + c;
-  carry_runs(ends + first, step, total, s.channels, s.chunks, decay, held && h0 ? h0[own] : 0.f, valid, fold);
-  if (BACKWARD)
+  if (!back)
+    carry_runs(ends + first, step, total, s.channels, s.chunks, decay, held && h0 ? h0[own] : 0.f, valid, fold);
+  else
     carry_runs(starts + last, -step, total + (s.chunks - 1) * s.channels, -s.channels, s.chunks, decay, held && dlast ? dlast[own] : 0.f, valid,
                fold);
 }
@@ -408,7 +431,7 @@ __global__ __launch_bounds__(WAVES * kWave) void scan_forward_kernel(ScanShape s
   const T* xs = x + p.batch * s.x_b + p.from * s.x_t;
   const T* ds = delta + p.batch * s.delta_b + p.from * s.delta_t;
   const T* gs = gate ? gate + p.batch * s.gate_b + p.from * s.gate_t : nullptr;
-  T* os = out + p.batch * s.out_b;
+  T* os = out + p.batch * s.out_b + p.from * s.out_t;
   Shared rows = shared_rows<NP, WAVES>(s, p, bc) + p.from * (2 * NP * WAVES);
   using Group = SharedGroup<NP, WAVES, true>;
   Group next;
@@ -453,26 +476,38 @@ __global__ __launch_bounds__(WAVES * kWave) void scan_forward_kernel(ScanShape s
       __syncthreads();
     }
 #pragma unroll
-    for (int j = 0; j < U; ++j) {
-      float r = fmaf(skip, (float)xv[j], y[j]);
-      if (gs) {
-        const float gt = (float)gv[j];
-        r *= gt * sigmoid(gt).a;
-      }
-      y[j] = r;
+    for (int j = 0; j < U; ++j) y[j] = fmaf(skip, (float)xv[j], y[j]);
+    if (gs) {
+#pragma unroll
+      for (int j = 0; j < U; ++j) y[j] *= (float)gv[j] * sigmoid((float)gv[j]).a;
     }
     if (p.valid) {
+      const LaneOf lane(p);
+      T* row = os;
+      if (WAVES == 1 && last == U - 1) {
 #pragma unroll
-      for (int j = 0; j < U; ++j)
-        if (j <= last && (WAVES == 1 || j % WAVES == p.part)) in_row(os + (t + j) * s.out_t, p) = (T)y[j];
+        for (int j = 0; j < U; ++j) {
+          lane.of(row) = (T)y[j];
+          row += s.out_t;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+          if (j <= last && (WAVES == 1 || j % WAVES == p.part)) lane.of(row) = (T)y[j];
+          row += s.out_t;
+        }
+      }
     }
+    os += U * s.out_t;
     xs += U * s.x_t;
     ds += U * s.delta_t;
     if (gs) gs += U * s.gate_t;
     rows += U * (2 * NP * WAVES);
   }
-  if (p.valid && p.part == 0)
-    for (int64_t t = max(p.from, p.len); t < p.to; ++t) in_row(os + t * s.out_t, p) = (T)0.f;
+  if (p.valid && p.part == 0) {
+    const LaneOf lane(p);
+    for (int64_t t = max(p.from, p.len); t < p.to; ++t) lane.of(out + p.batch * s.out_b + t * s.out_t) = (T)0.f;
+  }
   if (h_last && p.chunk == (p.len > 0 ? (p.len - 1) / s.chunk : 0)) store_states<NP>(s, p, h_last, h);
 }
 
@@ -578,7 +613,7 @@ __device__ __forceinline__ float lanes_sum(float (&v)[V], int l) {
 // parts: of a chunk, states + 2 rows of channels (grad_a, grad_d, grad_delta_bias); shared_parts: of a block of channels and a step, the
 // sums of grad_b and grad_c over the block.
 template <typename T, int NP, int WAVES>
-__global__ __launch_bounds__(WAVES * kWave, NP == 4 ? 3 : 2) void scan_backward_kernel(
+__global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 1 ? 3 : 2) void scan_backward_kernel(
     ScanShape s, const T* __restrict__ x, const T* __restrict__ delta, const float* __restrict__ a, const float* __restrict__ bc,
     const float* __restrict__ d, const T* __restrict__ gate, const float* __restrict__ delta_bias, const int32_t* __restrict__ lengths,
     const T* __restrict__ dout, const float* __restrict__ h0, const float* __restrict__ dlast, const float* __restrict__ ends,
@@ -619,32 +654,46 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 ? 3 : 2) void scan_backward_
     // this wave's steps
     T xv[SHARE], dv[SHARE], gv[SHARE], ov[SHARE];
     float slope[SHARE], through[SHARE];
+    const LaneOf lane(p);
 #pragma unroll
     for (int k = 0; k < SHARE; ++k) {
       const int64_t step = t + min(p.part * SHARE + k, last);
-      xv[k] = in_row(xs + step * s.x_t, p);
-      dv[k] = in_row(ds + step * s.delta_t, p);
-      ov[k] = in_row(os + step * s.out_t, p);
-      if (gs) gv[k] = in_row(gs + step * s.gate_t, p);
+      xv[k] = lane.of(xs + step * s.x_t);
+      dv[k] = lane.of(ds + step * s.delta_t);
+      ov[k] = lane.of(os + step * s.out_t);
+      if (gs) gv[k] = lane.of(gs + step * s.gate_t);
+    }
+    float own_dt[SHARE], own_dy[SHARE];
+#pragma unroll
+    for (int k = 0; k < SHARE; ++k) {
+      own_dt[k] = (float)dv[k] + shift;
+      slope[k] = 1.f;
+      own_dy[k] = (float)ov[k];
+    }
+    if (s.softplus) {
+#pragma unroll
+      for (int k = 0; k < SHARE; ++k) {
+        const Softplus soft = softplus(own_dt[k]);
+        own_dt[k] = soft.value;
+        slope[k] = soft.slope;
+      }
+    }
+    if (gs) {
+#pragma unroll
+      for (int k = 0; k < SHARE; ++k) {
+        const float gt = (float)gv[k];
+        const Gates z = sigmoid(gt);
+        through[k] = own_dy[k] * (z.a * fmaf(gt, z.z, 1.f));
+        own_dy[k] *= gt * z.a;
+      }
     }
 #pragma unroll
     for (int k = 0; k < SHARE; ++k) {
       const bool in = p.part * SHARE + k <= last, on = in && p.valid;
-      const float raw = (float)dv[k] + shift;
-      const Softplus soft = softplus(raw);
-      const float step = s.softplus ? soft.value : raw;
-      slope[k] = s.softplus ? soft.slope : 1.f;
-      float r = (float)ov[k];
-      if (gs) {
-        const float gt = (float)gv[k];
-        const Gates z = sigmoid(gt);
-        through[k] = r * (z.a * fmaf(gt, z.z, 1.f));
-        r *= gt * z.a;
-      }
       float* const to = common + (p.part * SHARE + k) * 3 * kWave;
-      to[0] = in ? step : 0.f;
-      to[kWave] = on ? step * (float)xv[k] : 0.f;
-      to[2 * kWave] = on ? r : 0.f;
+      to[0] = in ? own_dt[k] : 0.f;
+      to[kWave] = on ? own_dt[k] * (float)xv[k] : 0.f;
+      to[2 * kWave] = on ? own_dy[k] : 0.f;
     }
     if (WAVES > 1) __syncthreads();
     float hs[U + 1][NP], e[U][NP], dt[U], u[U], dy[U];
@@ -652,10 +701,11 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 ? 3 : 2) void scan_backward_
     else load_states<NP>(s, p, h0, hs[0]);
     if (i > 0) {
       const float* from = marks_of<NP, WAVES>(s, p, marks, t);
-      const float sum = in_row(from + (WAVES - p.part) * NP * s.channels, p);
+      const LaneOf of_marks(p);
+      const float sum = of_marks.of(from + (WAVES - p.part) * NP * s.channels);
 #pragma unroll
       for (int n = 0; n < NP; ++n) {
-        hs[0][n] = fmaf(__builtin_amdgcn_exp2f(sum * decay[n]), hs[0][n], in_row(from, p));
+        hs[0][n] = fmaf(__builtin_amdgcn_exp2f(sum * decay[n]), hs[0][n], of_marks.of(from));
         from += s.channels;
       }
     }
@@ -718,6 +768,7 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 ? 3 : 2) void scan_backward_
       }
     }
     if (WAVES > 1) __syncthreads();
+    const LaneOf done(p);
 #pragma unroll
     for (int k = 0; k < SHARE; ++k) {
       const int j = p.part * SHARE + k;
@@ -730,22 +781,23 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 ? 3 : 2) void scan_backward_
         step += from[2 * kWave];
       }
       if (j > last || !p.valid) continue;
-      const float own_dt = common[j * 3 * kWave], own_dy = common[(j * 3 + 2) * kWave], xt = (float)xv[k];
+      const float dt_of = common[j * 3 * kWave], dy_of = common[(j * 3 + 2) * kWave], xt = (float)xv[k];
       const float r = fmaf(along, xt, step * kLn2) * slope[k];
-      in_row(dx + p.batch * s.dx_b + (t + j) * s.dx_t, p) = (T)fmaf(own_dt, along, skip * own_dy);
-      in_row(ddelta + p.batch * s.ddelta_b + (t + j) * s.ddelta_t, p) = (T)r;
+      done.of(dx + p.batch * s.dx_b + (t + j) * s.dx_t) = (T)fmaf(dt_of, along, skip * dy_of);
+      done.of(ddelta + p.batch * s.ddelta_b + (t + j) * s.ddelta_t) = (T)r;
       dshift += r;
-      dskip = fmaf(own_dy, xt, dskip);
-      if (gs) in_row(dgate + p.batch * s.dgate_b + (t + j) * s.dgate_t, p) = (T)(fmaf(skip, xt, y) * through[k]);
+      dskip = fmaf(dy_of, xt, dskip);
+      if (gs) done.of(dgate + p.batch * s.dgate_b + (t + j) * s.dgate_t) = (T)(fmaf(skip, xt, y) * through[k]);
     }
     if (WAVES > 1) __syncthreads();      // common and add are written again
   }
   float* const to = parts + (p.batch * s.chunks + p.chunk) * (s.states + 2) * s.channels;
+  const LaneOf lane(p);
   if (p.valid) {
 #pragma unroll
     for (int n = 0; n < NP; ++n) {
       const int at = p.part * NP + n;
-      if (at < s.states) in_row(to + at * s.channels, p) = da[n];
+      if (at < s.states) lane.of(to + at * s.channels) = da[n];
     }
     if (dh0 && p.chunk == 0) store_states<NP>(s, p, dh0, g);
   }
@@ -761,22 +813,31 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 ? 3 : 2) void scan_backward_
     }
   }
   if (!p.valid || p.part != 0) return;
-  in_row(to + s.states * s.channels, p) = dskip;
-  in_row(to + (s.states + 1) * s.channels, p) = dshift;
+  lane.of(to + s.states * s.channels) = dskip;
+  lane.of(to + (s.states + 1) * s.channels) = dshift;
   for (int64_t t = max(p.from, p.len); t < p.to; ++t) {
-    in_row(dx + p.batch * s.dx_b + t * s.dx_t, p) = (T)0.f;
-    in_row(ddelta + p.batch * s.ddelta_b + t * s.ddelta_t, p) = (T)0.f;
-    if (gs) in_row(dgate + p.batch * s.dgate_b + t * s.dgate_t, p) = (T)0.f;
+    lane.of(dx + p.batch * s.dx_b + t * s.dx_t) = (T)0.f;
+    lane.of(ddelta + p.batch * s.ddelta_b + t * s.ddelta_t) = (T)0.f;
+    if (gs) lane.of(dgate + p.batch * s.dgate_b + t * s.dgate_t) = (T)0.f;
   }
 }
 
-// grad_b and grad_c: the sums of a group's blocks of channels, in their order.
+// grad_b and grad_c: the sums of a group's blocks of channels, in their order; and, in the workgroups behind `shared_blocks`, the sums of the
+// chunks' parts.
 template <typename T>
-__global__ __launch_bounds__(256) void scan_join_kernel(const float* __restrict__ shared_parts, int64_t rows, int64_t steps, int64_t held, int groups,
-                                                        int blocks, int states, int padded, const int32_t* __restrict__ lengths,
-                                                        T* __restrict__ db, T* __restrict__ dc, int64_t db_b, int64_t db_t, int64_t dc_b,
-                                                        int64_t dc_t) {
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / (2 * padded);
+__global__ __launch_bounds__(kPartsThreads) void scan_join_kernel(const float* __restrict__ shared_parts, int64_t rows, int64_t steps,
+                                                                  int64_t held, int groups, int blocks, int states, int padded,
+                                                                  const int32_t* __restrict__ lengths, T* __restrict__ db, T* __restrict__ dc,
+                                                                  int64_t db_b, int64_t db_t, int64_t dc_b, int64_t dc_t,
+                                                                  unsigned shared_blocks, const float* __restrict__ parts, int64_t count,
+                                                                  int64_t channels, PartsTo to, int accumulate) {
+  __shared__ float fold[kPartsThreads];
+  if (blockIdx.x >= shared_blocks) {
+    const unsigned at = blockIdx.x - shared_blocks, across = (unsigned)((channels + kWave - 1) / kWave);
+    parts_join(parts, count, states + 2, channels, to, accumulate, at % across, (int)(at / across), fold);
+    return;
+  }
+  const int64_t at = (int64_t)blockIdx.x * kPartsThreads + threadIdx.x, row = at / (2 * padded);
   if (row >= rows) return;
   const int k = (int)(at - row * 2 * padded), n = k < padded ? k : k - padded;
   if (n >= states) return;
@@ -784,7 +845,13 @@ __global__ __launch_bounds__(256) void scan_join_kernel(const float* __restrict_
   float s = 0.f;
   if (t < steps_of(lengths, batch, steps)) {
     const float* from = shared_parts + ((batch * groups + g) * blocks * held + t) * 2 * padded + k;
-    for (int i = 0; i < blocks; ++i) s += from[(int64_t)i * held * 2 * padded];
+    for (int i = 0; i < blocks; i += kPartsAhead) {
+      float v[kPartsAhead];
+#pragma unroll
+      for (int j = 0; j < kPartsAhead; ++j) v[j] = i + j < blocks ? from[(int64_t)(i + j) * held * 2 * padded] : 0.f;
+#pragma unroll
+      for (int j = 0; j < kPartsAhead; ++j) s += v[j];
+    }
   }
   if (k < padded) db[batch * db_b + t * db_t + g * states + n] = (T)s;
   else dc[batch * dc_b + t * dc_t + g * states + n] = (T)s;

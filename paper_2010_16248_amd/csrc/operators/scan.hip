@@ -2,7 +2,6 @@
 #include "op_common.h"
 #include "op_host.h"
 #include "scan.h"
-#include "parts.h"
 
 using namespace accop;
 
@@ -16,7 +15,7 @@ int32_t check_scan(const acc_scan* c, bool backward) {
   REQUIRE(c, "config is NULL");
   REQUIRE(c->batch >= 0 && c->batch <= 65535, "batch out of range");
   REQUIRE(c->steps >= 0 && c->steps < (int64_t(1) << 31), "steps out of range");
-  REQUIRE(c->channels >= 1 && c->channels <= (int64_t(1) << 24), "channels out of range");
+  REQUIRE(c->channels >= 1 && c->channels <= (int64_t(1) << 20), "channels out of range");
   REQUIRE(c->states >= 1 && c->states <= ACC_SCAN_STATES, "states out of range");
   REQUIRE(c->groups >= 1 && c->channels % c->groups == 0, "channels must be a multiple of groups");
   REQUIRE(is_type(c->type), "unknown type");
@@ -127,8 +126,8 @@ void walk(const acc_scan& c, const ScanPlan& p, const ScanIn& in, void* out, flo
          in.lengths, in.h0, static_cast<T*>(out), h_last);
 }
 
-dim3 carry_grid(const acc_scan& c, const ScanPlan& p) {
-  return dim3((unsigned)up(c.channels, kWave), (unsigned)p.padded, (unsigned)c.batch);
+dim3 carry_grid(const acc_scan& c, const ScanPlan& p, bool backward) {
+  return dim3((unsigned)up(c.channels, kWave), (unsigned)(p.padded * (backward ? 2 : 1)), (unsigned)c.batch);
 }
 constexpr int64_t kCarryFill = 4096;        // waves that fill the chip
 // More waves than one for a state's chunks where the states alone do not fill the chip.
@@ -148,7 +147,7 @@ void forward_chunks(const acc_scan& c, const ScanPlan& p, const ScanIn& in, void
   if (p.chunks > 1) {
     LAUNCH((scan_ends_kernel<T, NP, WAVES, false>), dim3(across, (unsigned)(p.chunks - 1), batch), dim3(threads), queue, s, as<T>(in.x),
            as<T>(in.delta), in.a, packed, nullptr, in.delta_bias, in.lengths, nullptr, ends, nullptr, sums, nullptr);
-    LAUNCH(scan_carry_kernel<false>, carry_grid(c, p), carry_threads(c, p), queue, s, in.a, in.h0, nullptr,
+    LAUNCH(scan_carry_kernel<false>, carry_grid(c, p, false), carry_threads(c, p), queue, s, in.a, in.h0, nullptr,
            ends, nullptr, sums);
   }
   LAUNCH((scan_forward_kernel<T, NP, WAVES>), dim3(across, (unsigned)p.chunks, batch), dim3(threads), queue, s, as<T>(in.x), as<T>(in.delta),
@@ -213,27 +212,24 @@ void backward(const acc_scan& c, const ScanPlan& p, const ScanIn& in, const Scan
       else backward_ends<T, 16, 4>(c, p, in, g, ws, queue);
     }
     if (p.chunks > 1)
-      LAUNCH(scan_carry_kernel<true>, carry_grid(c, p), carry_threads(c, p), queue, shape_of(c, p), in.a, in.h0, g.last, at(p.ends),
+      LAUNCH(scan_carry_kernel<true>, carry_grid(c, p, true), carry_threads(c, p), queue, shape_of(c, p), in.a, in.h0, g.last, at(p.ends),
              at(p.starts), at(p.sums));
     if (p.padded == 4) backward_chunks<T, 4, 1>(c, p, in, g, ws, queue);
     else if (p.padded == 8) backward_chunks<T, 4, 2>(c, p, in, g, ws, queue);
     else if (p.padded == 16) backward_chunks<T, 4, 4>(c, p, in, g, ws, queue);
     else if (p.padded == 32) backward_chunks<T, 4, 8>(c, p, in, g, ws, queue);
     else backward_chunks<T, 8, 8>(c, p, in, g, ws, queue);
-    const int64_t rows = c.batch * c.groups * c.steps;
-    if (rows > 0)
-      LAUNCH(scan_join_kernel<T>, dim3((unsigned)up(rows * 2 * p.padded, 256)), dim3(256), queue, at(p.shared_parts), rows, c.steps, p.rows, c.groups,
-             (int)p.blocks, c.states, p.padded, in.lengths, static_cast<T*>(g.b), static_cast<T*>(g.c), c.grad_b_batch, c.grad_b_step,
-             c.grad_c_batch, c.grad_c_step);
   }
-  LAUNCH(parts_join_kernel, dim3((unsigned)up(c.channels, kWave), (unsigned)(c.states + 2)), dim3(1024), queue,
-         reinterpret_cast<const float*>(ws + p.parts), c.batch * p.chunks, c.states + 2, c.channels, PartsTo{g.a, c.states, g.d, g.delta_bias},
-         c.accumulate);
+  const int64_t rows = c.batch * c.groups * c.steps, shared_blocks = up(rows * 2 * p.padded, kPartsThreads);
+  LAUNCH(scan_join_kernel<T>, dim3((unsigned)(shared_blocks + up(c.channels, kWave) * (c.states + 2))), dim3(kPartsThreads), queue,
+         at(p.shared_parts), rows, c.steps, p.rows, c.groups, (int)p.blocks, c.states, p.padded, in.lengths, static_cast<T*>(g.b),
+         static_cast<T*>(g.c), c.grad_b_batch, c.grad_b_step, c.grad_c_batch, c.grad_c_step, (unsigned)shared_blocks, at(p.parts),
+         c.batch * p.chunks, c.channels, PartsTo{g.a, c.states, g.d, g.delta_bias}, c.accumulate);
 }
 
-// A launch has fewer than 2^32 work items per axis.
+// A launch has fewer than 2^32 work items per axis: the last one of the backward pass has these and up to 2^30 more.
 bool too_large(const acc_scan& c, const ScanPlan& p) {
-  return !p.walk && ((double)c.batch * c.groups * c.steps * 2 * p.padded >= 4e9 || (int64_t)c.groups * p.blocks * kWave * p.waves >= (int64_t(1) << 31));
+  return !p.walk && (double)c.batch * c.groups * up(c.steps, kScanAhead) * kScanAhead * 2 * p.padded >= 3e9;
 }
 
 Span floats(const void* p, int64_t n) { return {static_cast<const char*>(p), p ? 4 * n : 0}; }
