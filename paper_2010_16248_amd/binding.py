@@ -488,7 +488,7 @@ def _convolution(x, weight, out, name: str, silu: bool, accumulate: bool, grad_x
     _need(len(shape) == 3, "x must be batch x steps x channels")
     _need(weight.dim() == 2, "weight must be channels x width")
     batch, steps, channels = shape
-    width, whole = weight.shape[1], (steps * channels, channels)
+    width, whole = weight.shape[1], (max(steps, 1) * channels, channels)
     last = (0, 0) if grad_x is None else _parts_of(grad_x, "grad_x", shape, kind, whole)
     cfg = acc_convolution(batch, steps, channels, *_parts_of(x, "x", shape, kind, whole), *_parts_of(out, name, shape, kind, whole), *last,
                           width, _type_of(x, "x"), silu, accumulate)
@@ -535,7 +535,7 @@ def _scan(x, delta, a, b, c, out, name: str, gate, softplus: bool, accumulate: b
     if shared[0] != batch or shared[1] != steps or shared[-1] != states:
         raise ValueError(f"b must be {batch} x {steps} x groups x {states}")
     row = groups * states
-    whole, part = (steps * channels, channels), (steps * row, row)
+    whole, part = (max(steps, 1) * channels, channels), (max(steps, 1) * row, row)
     near = (*_parts_of(x, "x", shape, kind, whole), *_parts_of(delta, "delta", shape, kind, whole), *_parts_of(b, "b", shared, kind, part),
             *_parts_of(c, "c", shared, kind, part), *((0, 0) if gate is None else _parts_of(gate, "gate", shape, kind, whole)),
             *_parts_of(out, name, shape, kind, whole))

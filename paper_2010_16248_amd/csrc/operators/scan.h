@@ -413,37 +413,72 @@ __global__ __launch_bounds__(kWave * kCarryWaves) void scan_carry_kernel(ScanSha
 }
 
 // ---- forward ----------------------------------------------------------------------------------------------
+// The waves of a workgroup share what the states of a channel have in common: each works it out for some of a turn's steps, and finishes their
+// outputs.
 template <typename T, int NP, int WAVES>
-__global__ __launch_bounds__(WAVES * kWave) void scan_forward_kernel(ScanShape s, const T* __restrict__ x, const T* __restrict__ delta,
-                                                                     const float* __restrict__ a, const float* __restrict__ bc,
-                                                                     const float* __restrict__ d, const T* __restrict__ gate,
-                                                                     const float* __restrict__ delta_bias,
-                                                                     const int32_t* __restrict__ lengths, const float* h0,
-                                                                     const float* __restrict__ ends, T* __restrict__ out, float* h_last) {
-  constexpr int U = kScanAhead;
-  __shared__ float add[WAVES > 1 ? WAVES * U * kWave : 1];
+__global__ __launch_bounds__(WAVES * kWave) void scan_forward_kernel(
+    ScanShape s, const T* __restrict__ x, const T* __restrict__ delta, const float* __restrict__ a, const float* __restrict__ bc,
+    const float* __restrict__ d, const T* __restrict__ gate, const float* __restrict__ delta_bias, const int32_t* __restrict__ lengths,
+    const float* h0, const float* __restrict__ ends, T* __restrict__ out, float* h_last) {
+  constexpr int U = kScanAhead, SHARE = U / WAVES;
+  __shared__ float held[(2 + WAVES) * U * kWave];
   const ScanPlace p = scan_place(s, lengths);
+  float* const common = held + p.lane;                  // dt and u of a turn's steps
+  float* const add = common + 2 * U * kWave;            // what the waves' states contribute to a turn's steps
   float decay[NP], h[NP];
   load_decay<NP>(s, p, a, decay);
   if (s.chunks > 1) load_slots<NP, WAVES>(s, p, ends, h);
   else load_states<NP>(s, p, h0, h);
   const float shift = delta_bias ? delta_bias[p.channel] : 0.f, skip = d ? d[p.channel] : 0.f;
-  const T* xs = x + p.batch * s.x_b + p.from * s.x_t;
-  const T* ds = delta + p.batch * s.delta_b + p.from * s.delta_t;
-  const T* gs = gate ? gate + p.batch * s.gate_b + p.from * s.gate_t : nullptr;
-  T* os = out + p.batch * s.out_b + p.from * s.out_t;
+  const T* const xs = x + p.batch * s.x_b;
+  const T* const ds = delta + p.batch * s.delta_b;
+  const T* const gs = gate ? gate + p.batch * s.gate_b : nullptr;
+  T* const os = out + p.batch * s.out_b;
   Shared rows = shared_rows<NP, WAVES>(s, p, bc) + p.from * (2 * NP * WAVES);
   using Group = SharedGroup<NP, WAVES, true>;
   Group next;
   next.load(rows);
+  T xn[SHARE], dn[SHARE], gn[SHARE];                    // this wave's steps of the turn ahead
+  auto request = [&](int64_t t) {
+    const LaneOf lane(p);
+#pragma unroll
+    for (int k = 0; k < SHARE; ++k) {
+      const int64_t at = min(t + p.part * SHARE + k, p.end - 1);
+      xn[k] = lane.of(xs + at * s.x_t);
+      dn[k] = lane.of(ds + at * s.delta_t);
+      if (gs) gn[k] = lane.of(gs + at * s.gate_t);
+    }
+  };
+  if (p.from < p.end) request(p.from);
   for (int64_t t = p.from; t < p.end; t += U) {
     const int last = last_of(p, t);
-    T xv[U], dv[U], gv[U];
-    load_turn(xs, s.x_t, p, last, xv);
-    load_turn(ds, s.delta_t, p, last, dv);
-    if (gs) load_turn(gs, s.gate_t, p, last, gv);
-    float y[U], dt[U], u[U];
-    steps_and_inputs(xv, dv, shift, s.softplus, last, dt, u);
+    T xv[SHARE], gv[SHARE];
+    float step[SHARE];
+#pragma unroll
+    for (int k = 0; k < SHARE; ++k) {
+      xv[k] = xn[k];
+      gv[k] = gn[k];
+      step[k] = (float)dn[k] + shift;
+    }
+    if (s.softplus) {
+#pragma unroll
+      for (int k = 0; k < SHARE; ++k) step[k] = softplus(step[k]).value;
+    }
+#pragma unroll
+    for (int k = 0; k < SHARE; ++k) {
+      const bool in = p.part * SHARE + k <= last;
+      float* const to = common + (p.part * SHARE + k) * 2 * kWave;
+      to[0] = in ? step[k] : 0.f;
+      to[kWave] = in ? step[k] * (float)xv[k] : 0.f;
+    }
+    if (WAVES > 1) __syncthreads();
+    if (t + U < p.end) request(t + U);
+    float dt[U], u[U], y[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      dt[j] = common[j * 2 * kWave];
+      u[j] = common[(j * 2 + 1) * kWave];
+    }
 #pragma unroll
     for (int first = 0; first < U; first += Group::kCount) {
       await_shared();
@@ -463,50 +498,32 @@ __global__ __launch_bounds__(WAVES * kWave) void scan_forward_kernel(ScanShape s
       }
       pin(h);
     }
-    if (WAVES > 1) {
 #pragma unroll
-      for (int j = 0; j < U; ++j) add[(p.part * U + j) * kWave + p.lane] = y[j];
-      __syncthreads();
+    for (int j = 0; j < U; ++j) add[(p.part * U + j) * kWave] = y[j];
+    if (WAVES > 1) __syncthreads();
+    float r[SHARE];
 #pragma unroll
-      for (int j = 0; j < U; ++j) {
-        y[j] = 0.f;
+    for (int k = 0; k < SHARE; ++k) {
+      r[k] = 0.f;
 #pragma unroll
-        for (int o = 0; o < WAVES; ++o) y[j] += add[(o * U + j) * kWave + p.lane];
-      }
-      __syncthreads();
+      for (int o = 0; o < WAVES; ++o) r[k] += add[(o * U + p.part * SHARE + k) * kWave];
+      r[k] = fmaf(skip, (float)xv[k], r[k]);
     }
-#pragma unroll
-    for (int j = 0; j < U; ++j) y[j] = fmaf(skip, (float)xv[j], y[j]);
     if (gs) {
 #pragma unroll
-      for (int j = 0; j < U; ++j) y[j] *= (float)gv[j] * sigmoid((float)gv[j]).a;
+      for (int k = 0; k < SHARE; ++k) r[k] *= (float)gv[k] * sigmoid((float)gv[k]).a;
     }
     if (p.valid) {
       const LaneOf lane(p);
-      T* row = os;
-      if (WAVES == 1 && last == U - 1) {
 #pragma unroll
-        for (int j = 0; j < U; ++j) {
-          lane.of(row) = (T)y[j];
-          row += s.out_t;
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < U; ++j) {
-          if (j <= last && (WAVES == 1 || j % WAVES == p.part)) lane.of(row) = (T)y[j];
-          row += s.out_t;
-        }
-      }
+      for (int k = 0; k < SHARE; ++k)
+        if (p.part * SHARE + k <= last) lane.of(os + (t + p.part * SHARE + k) * s.out_t) = (T)r[k];
     }
-    os += U * s.out_t;
-    xs += U * s.x_t;
-    ds += U * s.delta_t;
-    if (gs) gs += U * s.gate_t;
     rows += U * (2 * NP * WAVES);
   }
   if (p.valid && p.part == 0) {
     const LaneOf lane(p);
-    for (int64_t t = max(p.from, p.len); t < p.to; ++t) lane.of(out + p.batch * s.out_b + t * s.out_t) = (T)0.f;
+    for (int64_t t = max(p.from, p.len); t < p.to; ++t) lane.of(os + t * s.out_t) = (T)0.f;
   }
   if (h_last && p.chunk == (p.len > 0 ? (p.len - 1) / s.chunk : 0)) store_states<NP>(s, p, h_last, h);
 }

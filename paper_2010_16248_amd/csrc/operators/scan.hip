@@ -36,11 +36,13 @@ int32_t check_scan(const acc_scan* c, bool backward) {
 }
 
 constexpr int64_t kScanWalkSteps = 8;       // up to here lanes share a channel and walk the steps
-// Chunks of the forward pass cost every step a second time (scan_ends_kernel), for waves.  Up to this many waves without chunks, chunks of 32 steps
-// and more that make so many waves.  us without chunks and with chunks of 32, 64, 128, 256 steps, 16 states, bf16: 64 x 512 x 1024 (1024 waves) 356,
-// 293, 275, 316, 371; x 2048 475, 538, 496, 478, 553; x 4096 721, 1018, 931, 871, 852; 16 x 4096 x 1024 2011, 548, 512, 519, 572;
-// 1 x 512 x 1536 236, 46, 69, 109, 199; 1 x 4096 x 1536 1866, 89, 97, 120, 216.
-constexpr int64_t kScanLone = 2048, kScanWaves = 12288, kScanShortest = 32;
+// Chunks of the forward pass cost every step a second time (scan_ends_kernel) and two more launches, for waves.  None up to 128 steps, and from this
+// many waves on without them; otherwise as long as leave this many, from 32 to 128 steps.  us without chunks and with chunks of 32, 64, 128, 256 steps,
+// bf16, 16 states: 8 x 128 x 768 (384 waves without chunks) 33, 34, 49; 1 x 512 x 1536 (96) 106, 34, 48, 74, 132; 1 x 4096 x 1536 806, 87, 81, 91, 147;
+// 20 x 512 x 1024 (1280) 125, 111, 111, 121, 172; 64 x 512 x 512 (2048) 130, 158, 151, 155, 195; 64 x 512 x 1024 (4096) 175, 287, 264, 269, 283;
+// 8 x 4096 x 2048 (1024) 834, 555, 501, 491, 523; 4 states 64 x 512 x 1024 (1024) 185, 147, 135, 142, 173; 32 states 4 x 1024 x 1536 (768) 201,
+// 127, 123, 121, 191.
+constexpr int64_t kScanFew = 128, kScanLone = 2048, kScanWaves = 6144, kScanShortest = 32, kScanLongest = 128;
 // Chunks of the backward pass: as long as leave this many workgroups, from 16 to 256 steps.  us with chunks of 16, 32, 64, 128, 256 steps:
 // 1 x 512 x 1536 (24 workgroups per chunk) 57, 66, 86, 140, 248; 2 x 2048 x 768 123, 108, 111, 162, 264; 4 x 1024 x 1536 193, 178, 175, 187,
 // 294; 64 x 128 x 512 133, 133, 149, 163, 163; 8 x 4096 x 2048 2365, 1931, 1399, 1348, 1335.
@@ -49,6 +51,7 @@ constexpr int64_t kScanGroups = 1536, kBackwardShortest = 16, kBackwardLongest =
 struct ScanPlan {
   bool walk = false;
   int each = 16, waves = 1, padded = 16;    // states of a lane, waves of a workgroup, states in all
+  int split = 1;                            // waves of a workgroup of the forward pass' last kernel
   int64_t group = 0, blocks = 0;            // channels of a group, blocks of 64 of them
   int64_t chunk = 0, chunks = 1, rows = 0;  // steps of a chunk, chunks, rows of a sequence's b and c
   int64_t packed = 0, ends = 0, starts = 0, sums = 0, marks = 0, parts = 0, shared_parts = 0, bytes = 0;   // offsets in the workspace
@@ -63,13 +66,17 @@ ScanPlan plan_scan(const acc_scan& c, bool backward) {
   p.padded = p.each * p.waves;
   p.group = c.channels / c.groups;
   p.blocks = up(p.group, kWave);
-  const int64_t lone = c.batch * c.groups * p.blocks * p.waves;      // waves of one chunk
+  const int64_t groups = c.batch * c.groups * p.blocks;              // workgroups of one chunk
   if (backward) {
     p.chunk = kBackwardLongest;
-    while (p.chunk > kBackwardShortest && lone / p.waves * up(c.steps, p.chunk) < kScanGroups) p.chunk /= 2;
+    while (p.chunk > kBackwardShortest && groups * up(c.steps, p.chunk) < kScanGroups) p.chunk /= 2;
   } else {
-    p.chunk = c.steps;
-    if (lone < kScanLone) p.chunk = std::max(kScanShortest, up(c.steps, up(kScanWaves, lone)));
+    p.split = std::min(8, p.padded / 4);
+    p.chunk = std::max<int64_t>(1, c.steps);
+    if (c.steps > kScanFew && groups * p.split < kScanLone) {
+      p.chunk = kScanLongest;
+      while (p.chunk > kScanShortest && groups * p.split * up(c.steps, p.chunk) < kScanWaves) p.chunk /= 2;
+    }
     while (up(c.steps, p.chunk) > 65535) p.chunk *= 2;
   }
   p.chunk = up(p.chunk, kScanAhead) * kScanAhead;
@@ -137,21 +144,11 @@ dim3 carry_threads(const acc_scan& c, const ScanPlan& p) {
 }
 
 template <typename T, int NP, int WAVES>
-void forward_chunks(const acc_scan& c, const ScanPlan& p, const ScanIn& in, void* out, float* h_last, char* ws, Queue& queue) {
-  const ScanShape s = shape_of(c, p);
-  float* const packed = reinterpret_cast<float*>(ws + p.packed);
-  float* const ends = reinterpret_cast<float*>(ws + p.ends);
-  float* const sums = reinterpret_cast<float*>(ws + p.sums);
-  const unsigned across = (unsigned)(c.groups * p.blocks), batch = (unsigned)c.batch, threads = kWave * WAVES;
-  pack<T>(c, p, in, packed, queue);
-  if (p.chunks > 1) {
-    LAUNCH((scan_ends_kernel<T, NP, WAVES, false>), dim3(across, (unsigned)(p.chunks - 1), batch), dim3(threads), queue, s, as<T>(in.x),
-           as<T>(in.delta), in.a, packed, nullptr, in.delta_bias, in.lengths, nullptr, ends, nullptr, sums, nullptr);
-    LAUNCH(scan_carry_kernel<false>, carry_grid(c, p, false), carry_threads(c, p), queue, s, in.a, in.h0, nullptr,
-           ends, nullptr, sums);
-  }
-  LAUNCH((scan_forward_kernel<T, NP, WAVES>), dim3(across, (unsigned)p.chunks, batch), dim3(threads), queue, s, as<T>(in.x), as<T>(in.delta),
-         in.a, packed, in.d, as<T>(in.gate), in.delta_bias, in.lengths, in.h0, ends, static_cast<T*>(out), h_last);
+void forward_ends(const acc_scan& c, const ScanPlan& p, const ScanIn& in, char* ws, Queue& queue) {
+  auto at = [&](int64_t offset) { return reinterpret_cast<float*>(ws + offset); };
+  LAUNCH((scan_ends_kernel<T, NP, WAVES, false>), dim3((unsigned)(c.groups * p.blocks), (unsigned)(p.chunks - 1), (unsigned)c.batch),
+         dim3(kWave * WAVES), queue, shape_of(c, p), as<T>(in.x), as<T>(in.delta), in.a, at(p.packed), nullptr, in.delta_bias, in.lengths,
+         nullptr, at(p.ends), nullptr, at(p.sums), nullptr);
 }
 
 template <typename T>
@@ -164,11 +161,25 @@ void forward(const acc_scan& c, const ScanPlan& p, const ScanIn& in, void* out, 
     else walk<T, 16>(c, p, in, out, h_last, queue);
     return;
   }
-  if (p.padded == 4) forward_chunks<T, 4, 1>(c, p, in, out, h_last, ws, queue);
-  else if (p.padded == 8) forward_chunks<T, 8, 1>(c, p, in, out, h_last, ws, queue);
-  else if (p.padded == 16) forward_chunks<T, 16, 1>(c, p, in, out, h_last, ws, queue);
-  else if (p.padded == 32) forward_chunks<T, 16, 2>(c, p, in, out, h_last, ws, queue);
-  else forward_chunks<T, 16, 4>(c, p, in, out, h_last, ws, queue);
+  auto at = [&](int64_t offset) { return reinterpret_cast<float*>(ws + offset); };
+  pack<T>(c, p, in, at(p.packed), queue);
+  if (p.chunks > 1) {
+    if (p.padded == 4) forward_ends<T, 4, 1>(c, p, in, ws, queue);
+    else if (p.padded == 8) forward_ends<T, 8, 1>(c, p, in, ws, queue);
+    else if (p.padded == 16) forward_ends<T, 16, 1>(c, p, in, ws, queue);
+    else if (p.padded == 32) forward_ends<T, 16, 2>(c, p, in, ws, queue);
+    else forward_ends<T, 16, 4>(c, p, in, ws, queue);
+    LAUNCH(scan_carry_kernel<false>, carry_grid(c, p, false), carry_threads(c, p), queue, shape_of(c, p), in.a, in.h0, nullptr, at(p.ends),
+           nullptr, at(p.sums));
+  }
+  const auto kernel = p.padded == 4    ? scan_forward_kernel<T, 4, 1>
+                      : p.padded == 8  ? scan_forward_kernel<T, 4, 2>
+                      : p.padded == 16 ? scan_forward_kernel<T, 4, 4>
+                      : p.padded == 32 ? scan_forward_kernel<T, 4, 8>
+                                       : scan_forward_kernel<T, 8, 8>;
+  LAUNCH(kernel, dim3((unsigned)(c.groups * p.blocks), (unsigned)p.chunks, (unsigned)c.batch), dim3((unsigned)(kWave * p.split)), queue,
+         shape_of(c, p), as<T>(in.x), as<T>(in.delta), in.a, at(p.packed), in.d, as<T>(in.gate), in.delta_bias, in.lengths, in.h0, at(p.ends),
+         static_cast<T*>(out), h_last);
 }
 
 struct ScanGradients {
