@@ -504,7 +504,7 @@ int32_t accordion_convolution_backward(const acc_convolution* cfg, const void* x
  * their inputs hold plays no role.  steps = 1 is the serving form: one token, the state in h0 and h_last (which may be the same buffer
  * then, and for any number of steps).
  * exp(dt a) below the normal fp32 numbers counts as zero.
- * More than 8 steps: batch x groups x steps x states, filled up to 4, 8, 16, 32 or 64, below 1.5e9. */
+ * More than 16 steps, and backward: batch x groups x steps x states, filled up to 4, 8, 16, 32 or 64, below 1.5e9. */
 typedef struct acc_scan {
   int64_t batch;                 /* [0, 65535] */
   int64_t steps;                 /* [0, 2^31); backward: up to 2^21 */

@@ -35,7 +35,11 @@ int32_t check_scan(const acc_scan* c, bool backward) {
   return ACC_OK;
 }
 
-constexpr int64_t kScanWalkSteps = 8;       // up to here lanes share a channel and walk the steps
+// Up to here lanes share a channel and walk the steps: one launch, but every step waits for its own loads.  us of it and of the chunks' kernels at
+// 1, 4, 8, 12, 16, 24, 32 steps, 16 states: bf16 64 x 1344 channels 5.1, 7.9, 11.9, 16.1, 20.0, 28.8, 37.0 and 17.0, 17.0, 17.6, 19.4, 19.8, 22.7, 26.2;
+// bf16 8 x 2048 3.5 (1), 6.3 (8), 8.1, 9.8, 13.2, 16.5 and 8.4, 8.7, 10.2, 10.4, 12.2, 13.8; fp32 64 x 4096 40.4 (16), 56.4 (24) and 41.5, 45.2;
+// 64 states 16 x 1024 15.5 (16), 21.5 (24) and 18.5, 21.0; 4 states 15.6 (32) and 17.6.
+constexpr int64_t kScanWalkSteps = 16;
 // Chunks of the forward pass cost every step a second time (scan_ends_kernel) and two more launches, for waves.  None up to 128 steps, and from this
 // many waves on without them; otherwise as long as leave this many, from 32 to 128 steps.  us without chunks and with chunks of 32, 64, 128, 256 steps,
 // bf16, 16 states: 8 x 128 x 768 (384 waves without chunks) 33, 34, 49; 1 x 512 x 1536 (96) 106, 34, 48, 74, 132; 1 x 4096 x 1536 806, 87, 81, 91, 147;
@@ -49,7 +53,7 @@ constexpr int64_t kScanFew = 128, kScanLone = 2048, kScanWaves = 6144, kScanShor
 constexpr int64_t kScanGroups = 1536, kBackwardShortest = 16, kBackwardLongest = 256;
 
 struct ScanPlan {
-  bool walk = false;
+  bool walk = false, large = false;
   int each = 16, waves = 1, padded = 16;    // states of a lane, waves of a workgroup, states in all
   int split = 1;                            // waves of a workgroup of the forward pass' last kernel
   int64_t group = 0, blocks = 0;            // channels of a group, blocks of 64 of them
@@ -66,6 +70,9 @@ ScanPlan plan_scan(const acc_scan& c, bool backward) {
   p.padded = p.each * p.waves;
   p.group = c.channels / c.groups;
   p.blocks = up(p.group, kWave);
+  // A launch has fewer than 2^32 work items per axis: the last one of the backward pass has these and up to 2^30 more.
+  p.large = (double)c.batch * c.groups * up(c.steps, kScanAhead) * kScanAhead * 2 * p.padded >= 3e9;
+  if (p.large) return p;
   const int64_t groups = c.batch * c.groups * p.blocks;              // workgroups of one chunk
   if (backward) {
     p.chunk = kBackwardLongest;
@@ -238,11 +245,6 @@ void backward(const acc_scan& c, const ScanPlan& p, const ScanIn& in, const Scan
          c.batch * p.chunks, c.channels, PartsTo{g.a, c.states, g.d, g.delta_bias}, c.accumulate);
 }
 
-// A launch has fewer than 2^32 work items per axis: the last one of the backward pass has these and up to 2^30 more.
-bool too_large(const acc_scan& c, const ScanPlan& p) {
-  return !p.walk && (double)c.batch * c.groups * up(c.steps, kScanAhead) * kScanAhead * 2 * p.padded >= 3e9;
-}
-
 Span floats(const void* p, int64_t n) { return {static_cast<const char*>(p), p ? 4 * n : 0}; }
 
 }  // namespace
@@ -254,7 +256,7 @@ int32_t accordion_scan_workspace_bytes(const acc_scan* c, int32_t backward_pass,
   REQUIRE(backward_pass == 0 || backward_pass == 1, "backward must be 0 or 1");
   if (const int32_t rc = check_scan(c, backward_pass)) return rc;
   const ScanPlan p = plan_scan(*c, backward_pass);
-  REQUIRE(!too_large(*c, p), "batch x steps x groups out of range");
+  REQUIRE(!p.large, "batch x steps x groups out of range");
   *out_bytes = (size_t)p.bytes;
   return ACC_OK;
 }
@@ -274,7 +276,7 @@ int32_t accordion_scan_forward(const acc_scan* c, const void* x_dev, const void*
               !off_type(lengths_dev, 4) && !off_type(h_last_dev, 4),
           "a pointer is not aligned to its element type");
   const ScanPlan p = plan_scan(*c, false);
-  REQUIRE(!too_large(*c, p), "batch x steps x groups out of range");
+  REQUIRE(!p.large, "batch x steps x groups out of range");
   if (const int32_t rc = check_workspace(workspace_dev, workspace_bytes, p.bytes)) return rc;
   const Rows shared = shared_rows(*c);
   const int64_t ends = c->batch * c->channels * c->states;
@@ -327,7 +329,7 @@ int32_t accordion_scan_backward(const acc_scan* c, const void* x_dev, const void
               !off_type(grad_a_dev, 4) && !off_type(grad_d_dev, 4) && !off_type(grad_delta_bias_dev, 4) && !off_type(grad_h0_dev, 4),
           "a pointer is not aligned to its element type");
   const ScanPlan p = plan_scan(*c, true);
-  REQUIRE(!too_large(*c, p), "batch x steps x groups out of range");
+  REQUIRE(!p.large, "batch x steps x groups out of range");
   if (const int32_t rc = check_workspace(workspace_dev, workspace_bytes, p.bytes)) return rc;
   const int64_t ends = c->batch * c->channels * c->states;
   const Span s[22] = {{static_cast<const char*>(workspace_dev), p.bytes},

@@ -135,6 +135,9 @@ def test_scan_sizes(lib):
     refused(lib, lib.accordion_scan_workspace_bytes(C.byref(long), 1, C.byref(n)), "steps")
     many = scan(steps=2 ** 21, batch=60000, x_batch=2 ** 30, delta_batch=2 ** 30, gate_batch=2 ** 30, out_batch=2 ** 30)
     refused(lib, lib.accordion_scan_workspace_bytes(C.byref(many), 0, C.byref(n)), "out of range")
+    most = scan(batch=65535, steps=2 ** 21, channels=2 ** 20, groups=2 ** 20, states=64)        # products beyond 63 bits
+    for backward in (0, 1):
+        refused(lib, lib.accordion_scan_workspace_bytes(C.byref(most), backward, C.byref(n)), "out of range")
 
 
 def test_scan_pointers(lib):
