@@ -85,8 +85,8 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanShape& s, const int32_
   p.channel = (unsigned)p.group * s.group + (p.valid ? within : s.group - 1);
   p.byte2 = 2 * p.channel;
   p.byte4 = 4 * p.channel;
-  p.chunk = blockIdx.y;
-  p.batch = blockIdx.z;
+  p.batch = blockIdx.y;
+  p.chunk = blockIdx.z;
   p.len = steps_of(lengths, p.batch, s.steps);
   p.from = p.chunk * s.chunk;
   p.to = min(p.from + s.chunk, s.steps);
@@ -162,22 +162,27 @@ __device__ __forceinline__ F* marks_of(const ScanShape& s, const ScanPlace& p, F
   return marks + ((p.batch * (s.rows / kScanAhead) + t / kScanAhead) * (NP * WAVES + 1) + p.part * NP) * s.channels;
 }
 
-// The values of one step that a wave reads: b, and c where the pass needs it.
-template <int NP, int WAVES, bool C>
+// The values of one step that a wave reads: c, and b where the pass needs it.
+template <int NP, int WAVES, bool B>
 struct SharedRow {
-  float b[NP], c[C ? NP : 1];
+  float b[B ? NP : 1], c[NP];
   __device__ __forceinline__ void load(Shared at) {
+    if (B) {
 #pragma unroll
-    for (int n = 0; n < NP; ++n) b[n] = at[n];
-    if (C) {
-#pragma unroll
-      for (int n = 0; n < NP; ++n) c[n] = at[NP * WAVES + n];
+      for (int n = 0; n < NP; ++n) b[n] = at[n];
     }
+#pragma unroll
+    for (int n = 0; n < NP; ++n) c[n] = at[NP * WAVES + n];
   }
 };
+// Where a wave's values of the sequence's first step lie.
+template <int NP, int WAVES>
+__device__ __forceinline__ int64_t rows_of(const ScanShape& s, const ScanPlace& p) {
+  return (p.batch * s.groups + p.group) * s.rows * (2 * NP * WAVES) + p.part * NP;
+}
 template <int NP, int WAVES>
 __device__ __forceinline__ Shared shared_rows(const ScanShape& s, const ScanPlace& p, const float* bc) {
-  return shared_at(bc) + (p.batch * s.groups + p.group) * s.rows * (2 * NP * WAVES) + p.part * NP;
+  return shared_at(bc) + rows_of<NP, WAVES>(s, p);
 }
 // Rows are requested in groups of as many as 16 scalar registers hold (at least one), a group ahead.  Scalar loads return in any order, so a wait for one is a
 // wait for all: a group is awaited before the next one is requested, which the compiler's own waits, at first use, would not do.  The stops keep the
@@ -196,16 +201,58 @@ __device__ __forceinline__ void pin(float (&v)[N]) {
   for (int n = 0; n < N; ++n) asm volatile("" : "+v"(v[n]));
 }
 __device__ __forceinline__ void pin(float& v) { asm volatile("" : "+v"(v)); }
-template <int NP, int WAVES, bool C>
+template <int NP, int WAVES, bool B>
 struct SharedGroup {
   static constexpr int kRow = 2 * NP * WAVES;
-  static constexpr int kCount = NP * (C ? 2 : 1) >= 16 ? 1 : NP * (C ? 2 : 1) >= 8 ? 2 : 4;
-  SharedRow<NP, WAVES, C> row[kCount];
+  static constexpr int kCount = NP * (B ? 2 : 1) >= 16 ? 1 : NP * (B ? 2 : 1) >= 8 ? 2 : 4;
+  SharedRow<NP, WAVES, B> row[kCount];
   __device__ __forceinline__ void load(Shared at) {
 #pragma unroll
     for (int k = 0; k < kCount; ++k) row[k].load(at + k * kRow);
   }
 };
+
+// Products of a step's b or c, which the channels share, with a value of each channel's: what a matrix instruction of 16 blocks of 4 states x 4
+// channels makes of 4 numbers and 64, and adds to 4 states of 64 channels, a lane's own, at the issue of one vector instruction.  The numbers of
+// a turn lie with the lanes of as few registers as hold them: lane l of the k-th has state l % NP of step k 64 / NP + l / NP.  The instruction takes those of
+// the four lanes it names for all its blocks.
+template <int NP>
+struct HeldRows {
+  static constexpr int kSteps = kWave / NP, kCount = kScanAhead > kSteps ? kScanAhead / kSteps : 1;
+  float v[kCount];
+  __device__ __forceinline__ void load(const float* rows, int row, int lane) {
+    const unsigned at = (unsigned)min(lane / NP, kScanAhead - 1) * row + lane % NP;
+#pragma unroll
+    for (int k = 0; k < kCount; ++k) v[k] = rows[k * kSteps * row + at];
+  }
+};
+template <int FROM>
+__device__ __forceinline__ F32<4> four_states(float held, float u, F32<4> add) {
+  return __builtin_amdgcn_mfma_f32_4x4x1f32(held, u, add, 4, FROM, 0);
+}
+// add + (step j's numbers of the q-th four states) u.  (j and q are known when this is compiled.)
+template <int NP>
+__device__ __forceinline__ F32<4> add_products(const HeldRows<NP>& held, int j, int q, float u, F32<4> add) {
+  const float v = held.v[j / HeldRows<NP>::kSteps];
+  switch (j % HeldRows<NP>::kSteps * (NP / 4) + q) {
+    case 0: return four_states<0>(v, u, add);
+    case 1: return four_states<1>(v, u, add);
+    case 2: return four_states<2>(v, u, add);
+    case 3: return four_states<3>(v, u, add);
+    case 4: return four_states<4>(v, u, add);
+    case 5: return four_states<5>(v, u, add);
+    case 6: return four_states<6>(v, u, add);
+    case 7: return four_states<7>(v, u, add);
+    case 8: return four_states<8>(v, u, add);
+    case 9: return four_states<9>(v, u, add);
+    case 10: return four_states<10>(v, u, add);
+    case 11: return four_states<11>(v, u, add);
+    case 12: return four_states<12>(v, u, add);
+    case 13: return four_states<13>(v, u, add);
+    case 14: return four_states<14>(v, u, add);
+    default: return four_states<15>(v, u, add);
+  }
+}
 
 // A channel's elements of a turn's steps (of the last one there is, beyond).
 template <typename T>
@@ -245,13 +292,14 @@ __device__ __forceinline__ void steps_and_inputs(const T (&xv)[kScanAhead], cons
 // the gradient of the state in front of it if nothing came from behind, and in marks the state and the sum in front of each of its turns
 // (batch x turns x (states, filled up, + 1) x channels).
 template <typename T, int NP, int WAVES, bool BACKWARD>
-__global__ __launch_bounds__(WAVES * kWave) void scan_ends_kernel(ScanShape s, const T* __restrict__ x, const T* __restrict__ delta,
-                                                                  const float* __restrict__ a, const float* __restrict__ bc,
-                                                                  const T* __restrict__ gate, const float* __restrict__ delta_bias,
-                                                                  const int32_t* __restrict__ lengths, const T* __restrict__ dout,
-                                                                  float* __restrict__ ends, float* __restrict__ starts,
-                                                                  float* __restrict__ sums, float* __restrict__ marks) {
-  constexpr int U = kScanAhead;
+__global__ __launch_bounds__(WAVES * kWave, 4) void scan_ends_kernel(ScanShape s, const T* __restrict__ x, const T* __restrict__ delta,
+                                                                     const float* __restrict__ a, const float* __restrict__ bc,
+                                                                     const T* __restrict__ gate, const float* __restrict__ delta_bias,
+                                                                     const int32_t* __restrict__ lengths, const T* __restrict__ dout,
+                                                                     float* __restrict__ ends, float* __restrict__ starts,
+                                                                     float* __restrict__ sums, float* __restrict__ marks) {
+  constexpr int U = kScanAhead, SHARE = U / WAVES, KINDS = BACKWARD ? 3 : 2;
+  __shared__ float held[2 * KINDS * U * kWave];         // dt, u and dy of a turn's steps, for two turns
   const ScanPlace p = scan_place(s, lengths);
   float decay[NP], h[NP], g[NP], reach[NP];
   load_decay<NP>(s, p, a, decay);
@@ -261,79 +309,104 @@ __global__ __launch_bounds__(WAVES * kWave) void scan_ends_kernel(ScanShape s, c
     reach[n] = 1.f;
   }
   const float shift = delta_bias ? delta_bias[p.channel] : 0.f;
-  const T* xs = x + p.batch * s.x_b + p.from * s.x_t;
-  const T* ds = delta + p.batch * s.delta_b + p.from * s.delta_t;
-  const T* gs = BACKWARD && gate ? gate + p.batch * s.gate_b + p.from * s.gate_t : nullptr;
-  const T* os = BACKWARD ? dout + p.batch * s.out_b + p.from * s.out_t : nullptr;
-  Shared rows = shared_rows<NP, WAVES>(s, p, bc) + p.from * (2 * NP * WAVES);
+  const T* const xs = x + p.batch * s.x_b;
+  const T* const ds = delta + p.batch * s.delta_b;
+  const T* const gs = BACKWARD && gate ? gate + p.batch * s.gate_b : nullptr;
+  const T* const os = BACKWARD ? dout + p.batch * s.out_b : nullptr;
+  constexpr int kRow = 2 * NP * WAVES;
+  const float* rows = bc + rows_of<NP, WAVES>(s, p) + p.from * kRow;
   float sum = 0.f;
-  using Group = SharedGroup<NP, WAVES, BACKWARD>;
-  Group next;
-  next.load(rows);
+  HeldRows<NP> next_b, next_c;
+  next_b.load(rows, kRow, p.lane);
+  if (BACKWARD) next_c.load(rows + NP * WAVES, kRow, p.lane);
+  T xn[SHARE], dn[SHARE], gn[SHARE], on[SHARE];         // this wave's steps of the turn ahead
+  auto request = [&](int64_t t) {
+    const LaneOf lane(p);
+#pragma unroll
+    for (int k = 0; k < SHARE; ++k) {
+      const int64_t at = min(t + p.part * SHARE + k, p.end - 1);
+      xn[k] = lane.of(xs + at * s.x_t);
+      dn[k] = lane.of(ds + at * s.delta_t);
+      if (BACKWARD) on[k] = lane.of(os + at * s.out_t);
+      if (gs) gn[k] = lane.of(gs + at * s.gate_t);
+    }
+  };
+  if (p.from < p.end) request(p.from);
+  int turn = 0;
   for (int64_t t = p.from; t < p.end; t += U) {
     const int last = last_of(p, t);
-    T xv[U], dv[U], gv[U], ov[U];
-    load_turn(xs, s.x_t, p, last, xv);
-    load_turn(ds, s.delta_t, p, last, dv);
-    if (BACKWARD) {
-      if (p.valid && t > p.from) {
-        float* to = marks_of<NP, WAVES>(s, p, marks, t);
-        const LaneOf lane(p);
+    float* const common = held + (turn & 1) * KINDS * U * kWave + p.lane;
+    ++turn;
+    float step[SHARE], dy_of[SHARE];
 #pragma unroll
-        for (int n = 0; n < NP; ++n) {
-          lane.of(to) = h[n];
-          to += s.channels;
-        }
-        if (p.part == WAVES - 1) lane.of(to) = sum;
-      }
-      load_turn(os, s.out_t, p, last, ov);
-      if (gs) load_turn(gs, s.gate_t, p, last, gv);
+    for (int k = 0; k < SHARE; ++k) {
+      step[k] = (float)dn[k] + shift;
+      if (BACKWARD) dy_of[k] = (float)on[k];
     }
+    if (s.softplus) {
+#pragma unroll
+      for (int k = 0; k < SHARE; ++k) step[k] = softplus(step[k]).value;
+    }
+    if (gs) {
+#pragma unroll
+      for (int k = 0; k < SHARE; ++k) dy_of[k] *= (float)gn[k] * sigmoid((float)gn[k]).a;
+    }
+#pragma unroll
+    for (int k = 0; k < SHARE; ++k) {
+      const bool in = p.part * SHARE + k <= last;
+      float* const to = common + (p.part * SHARE + k) * KINDS * kWave;
+      to[0] = in ? step[k] : 0.f;
+      to[kWave] = in ? step[k] * (float)xn[k] : 0.f;
+      if (BACKWARD) to[2 * kWave] = in ? dy_of[k] : 0.f;
+    }
+    if (BACKWARD && p.valid && t > p.from) {
+      float* to = marks_of<NP, WAVES>(s, p, marks, t);
+      const LaneOf lane(p);
+#pragma unroll
+      for (int n = 0; n < NP; ++n) {
+        lane.of(to) = h[n];
+        to += s.channels;
+      }
+      if (p.part == 0) lane.of(to + (WAVES - 1) * NP * s.channels) = sum;
+    }
+    if (t + U < p.end) request(t + U);
+    if (WAVES > 1) __syncthreads();
     float dt[U], u[U], dy[U];
-    steps_and_inputs(xv, dv, shift, s.softplus, last, dt, u);
-    if (BACKWARD) {
 #pragma unroll
-      for (int j = 0; j < U; ++j) dy[j] = (float)ov[j];
-      if (gs) {
+    for (int j = 0; j < U; ++j) {
+      dt[j] = common[j * KINDS * kWave];
+      u[j] = common[(j * KINDS + 1) * kWave];
+      if (BACKWARD) dy[j] = common[(j * KINDS + 2) * kWave];
+    }
+    const HeldRows<NP> b_of = next_b, c_of = next_c;
+    rows += U * kRow;
+    next_b.load(rows, kRow, p.lane);
+    if (BACKWARD) next_c.load(rows + NP * WAVES, kRow, p.lane);
+    if (p.part == 0) {
 #pragma unroll
-        for (int j = 0; j < U; ++j) dy[j] *= (float)gv[j] * sigmoid((float)gv[j]).a;
-      }
-      if (last < U - 1) {
-#pragma unroll
-        for (int j = 0; j < U; ++j) dy[j] = j <= last ? dy[j] : 0.f;
-      }
+      for (int j = 0; j < U; ++j) sum += dt[j];
     }
 #pragma unroll
-    for (int first = 0; first < U; first += Group::kCount) {
-      await_shared();
-      const Group group = next;
-      next.load(rows + (first + Group::kCount) * Group::kRow);
-      stop();
+    for (int j = 0; j < U; ++j) {
 #pragma unroll
-      for (int k = 0; k < Group::kCount; ++k) {
-        const int j = first + k;
-        sum += dt[j];
+      for (int q = 0; q < NP / 4; ++q) {
+        F32<4> h4, from = {};
+        if (BACKWARD) from = add_products<NP>(c_of, j, q, dy[j], from);
 #pragma unroll
-        for (int n = 0; n < NP; ++n) {
+        for (int i = 0; i < 4; ++i) {
+          const int n = 4 * q + i;
           const float e = __builtin_amdgcn_exp2f(dt[j] * decay[n]);
-          h[n] = fmaf(e, h[n], u[j] * group.row[k].b[n]);
+          h4[i] = e * h[n];
           if (BACKWARD) {
             reach[n] *= e;
-            g[n] = fmaf(reach[n], group.row[k].c[n] * dy[j], g[n]);
+            g[n] = fmaf(reach[n], from[i], g[n]);
           }
         }
-      }
-      pin(h);
-      if (BACKWARD) {
-        pin(g);
-        pin(reach);
+        h4 = add_products<NP>(b_of, j, q, u[j], h4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[4 * q + i] = h4[i];
       }
     }
-    xs += U * s.x_t;
-    ds += U * s.delta_t;
-    if (BACKWARD) os += U * s.out_t;
-    if (gs) gs += U * s.gate_t;
-    rows += U * (2 * NP * WAVES);
   }
   store_slots<NP, WAVES>(s, p, ends, h);
   if (BACKWARD) store_slots<NP, WAVES>(s, p, starts, g);
@@ -416,7 +489,7 @@ __global__ __launch_bounds__(kWave * kCarryWaves) void scan_carry_kernel(ScanSha
 // The waves of a workgroup share what the states of a channel have in common: each works it out for some of a turn's steps, and finishes their
 // outputs.
 template <typename T, int NP, int WAVES>
-__global__ __launch_bounds__(WAVES * kWave) void scan_forward_kernel(
+__global__ __launch_bounds__(WAVES * kWave, 4) void scan_forward_kernel(
     ScanShape s, const T* __restrict__ x, const T* __restrict__ delta, const float* __restrict__ a, const float* __restrict__ bc,
     const float* __restrict__ d, const T* __restrict__ gate, const float* __restrict__ delta_bias, const int32_t* __restrict__ lengths,
     const float* h0, const float* __restrict__ ends, T* __restrict__ out, float* h_last) {
@@ -434,10 +507,14 @@ __global__ __launch_bounds__(WAVES * kWave) void scan_forward_kernel(
   const T* const ds = delta + p.batch * s.delta_b;
   const T* const gs = gate ? gate + p.batch * s.gate_b : nullptr;
   T* const os = out + p.batch * s.out_b;
-  Shared rows = shared_rows<NP, WAVES>(s, p, bc) + p.from * (2 * NP * WAVES);
-  using Group = SharedGroup<NP, WAVES, true>;
+  constexpr int kRow = 2 * NP * WAVES;
+  Shared rows = shared_rows<NP, WAVES>(s, p, bc) + p.from * kRow;
+  const float* held_rows = bc + rows_of<NP, WAVES>(s, p) + p.from * kRow;
+  using Group = SharedGroup<NP, WAVES, false>;
   Group next;
   next.load(rows);
+  HeldRows<NP> next_b;
+  next_b.load(held_rows, kRow, p.lane);
   T xn[SHARE], dn[SHARE], gn[SHARE];                    // this wave's steps of the turn ahead
   auto request = [&](int64_t t) {
     const LaneOf lane(p);
@@ -479,6 +556,9 @@ __global__ __launch_bounds__(WAVES * kWave) void scan_forward_kernel(
       dt[j] = common[j * 2 * kWave];
       u[j] = common[(j * 2 + 1) * kWave];
     }
+    const HeldRows<NP> b_of = next_b;
+    held_rows += U * kRow;
+    next_b.load(held_rows, kRow, p.lane);
 #pragma unroll
     for (int first = 0; first < U; first += Group::kCount) {
       await_shared();
@@ -490,9 +570,16 @@ __global__ __launch_bounds__(WAVES * kWave) void scan_forward_kernel(
         const int j = first + k;
         y[j] = 0.f;
 #pragma unroll
-        for (int n = 0; n < NP; ++n) {
-          h[n] = fmaf(__builtin_amdgcn_exp2f(dt[j] * decay[n]), h[n], u[j] * group.row[k].b[n]);
-          y[j] = fmaf(group.row[k].c[n], h[n], y[j]);
+        for (int q = 0; q < NP / 4; ++q) {
+          F32<4> h4;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) h4[i] = __builtin_amdgcn_exp2f(dt[j] * decay[4 * q + i]) * h[4 * q + i];
+          h4 = add_products<NP>(b_of, j, q, u[j], h4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            h[4 * q + i] = h4[i];
+            y[j] = fmaf(group.row[k].c[4 * q + i], h4[i], y[j]);
+          }
         }
         pin(y[j]);
       }
@@ -649,10 +736,14 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 1 ? 3 : 2) void s
   const T* const ds = delta + p.batch * s.delta_b;
   const Shared rows = shared_rows<NP, WAVES>(s, p, bc);
   const int turns = p.end > p.from ? (int)((p.end - p.from + U - 1) / U) : 0;
-  using Inputs = SharedGroup<NP, WAVES, false>;
+  const float* const held_rows = bc + rows_of<NP, WAVES>(s, p);
   using Both = SharedGroup<NP, WAVES, true>;
-  Inputs inputs;
-  inputs.load(rows + (p.from + max(turns - 1, 0) * U) * row_size);
+  HeldRows<NP> next_b, next_c;
+  {
+    const float* const of = held_rows + (p.from + max(turns - 1, 0) * U) * row_size;
+    next_b.load(of, row_size, p.lane);
+    next_c.load(of + NP * WAVES, row_size, p.lane);
+  }
   if (s.chunks > 1) load_slots<NP, WAVES>(s, p, starts, g);
   else load_states<NP>(s, p, dlast, g);
   const T* const gs = gate ? gate + p.batch * s.gate_b : nullptr;
@@ -664,21 +755,47 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 1 ? 3 : 2) void s
   const int sum_of = p.lane / (kWave / (4 * NP)), value = sum_of % (2 * NP);
   float* const shared_to = shared_parts + (p.batch * s.groups * s.blocks + p.block) * s.rows * row_size + (sum_of < 2 * NP ? row_size : 0) +
                            p.part * NP + (value < NP ? value : NP * WAVES + value - NP);
-  for (int i = turns - 1; i >= 0; --i) {
+  float start[NP];                                  // the state in front of the chunk
+  if (s.chunks > 1) load_slots<NP, WAVES>(s, p, ends, start);
+  else load_states<NP>(s, p, h0, start);
+  // this wave's steps of the turn ahead, and the marks in front of that
+  T xn[SHARE], dn[SHARE], gn[SHARE], on[SHARE];
+  float mark[NP], mark_sum = 0.f;
+  auto request = [&](int i) {
     const int64_t t = p.from + i * U;
     const int last = last_of(p, t);
-    const Shared at = rows + t * row_size;
-    // this wave's steps
-    T xv[SHARE], dv[SHARE], gv[SHARE], ov[SHARE];
-    float slope[SHARE], through[SHARE];
     const LaneOf lane(p);
 #pragma unroll
     for (int k = 0; k < SHARE; ++k) {
       const int64_t step = t + min(p.part * SHARE + k, last);
-      xv[k] = lane.of(xs + step * s.x_t);
-      dv[k] = lane.of(ds + step * s.delta_t);
-      ov[k] = lane.of(os + step * s.out_t);
-      if (gs) gv[k] = lane.of(gs + step * s.gate_t);
+      xn[k] = lane.of(xs + step * s.x_t);
+      dn[k] = lane.of(ds + step * s.delta_t);
+      on[k] = lane.of(os + step * s.out_t);
+      if (gs) gn[k] = lane.of(gs + step * s.gate_t);
+    }
+    if (i > 0) {
+      const float* from = marks_of<NP, WAVES>(s, p, marks, t);
+      mark_sum = lane.of(from + (WAVES - p.part) * NP * s.channels);
+#pragma unroll
+      for (int n = 0; n < NP; ++n) {
+        mark[n] = lane.of(from);
+        from += s.channels;
+      }
+    }
+  };
+  if (turns > 0) request(turns - 1);
+  for (int i = turns - 1; i >= 0; --i) {
+    const int64_t t = p.from + i * U;
+    const int last = last_of(p, t);
+    const Shared at = rows + t * row_size;
+    T xv[SHARE], dv[SHARE], gv[SHARE], ov[SHARE];
+    float slope[SHARE], through[SHARE];
+#pragma unroll
+    for (int k = 0; k < SHARE; ++k) {
+      xv[k] = xn[k];
+      dv[k] = dn[k];
+      ov[k] = on[k];
+      gv[k] = gn[k];
     }
     float own_dt[SHARE], own_dy[SHARE];
 #pragma unroll
@@ -714,41 +831,37 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 1 ? 3 : 2) void s
     }
     if (WAVES > 1) __syncthreads();
     float hs[U + 1][NP], e[U][NP], dt[U], u[U], dy[U];
-    if (s.chunks > 1) load_slots<NP, WAVES>(s, p, ends, hs[0]);
-    else load_states<NP>(s, p, h0, hs[0]);
-    if (i > 0) {
-      const float* from = marks_of<NP, WAVES>(s, p, marks, t);
-      const LaneOf of_marks(p);
-      const float sum = of_marks.of(from + (WAVES - p.part) * NP * s.channels);
 #pragma unroll
-      for (int n = 0; n < NP; ++n) {
-        hs[0][n] = fmaf(__builtin_amdgcn_exp2f(sum * decay[n]), hs[0][n], of_marks.of(from));
-        from += s.channels;
-      }
-    }
+    for (int n = 0; n < NP; ++n) hs[0][n] = i > 0 ? fmaf(__builtin_amdgcn_exp2f(mark_sum * decay[n]), start[n], mark[n]) : start[n];
+    pin(hs[0]);
+    if (i > 0) request(i - 1);
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       dt[j] = common[j * 3 * kWave];
       u[j] = common[(j * 3 + 1) * kWave];
       dy[j] = common[(j * 3 + 2) * kWave];
     }
+    const HeldRows<NP> b_of = next_b, c_of = next_c;
+    {
+      const float* const of = held_rows + max(t - U, p.from) * row_size;
+      next_b.load(of, row_size, p.lane);
+      next_c.load(of + NP * WAVES, row_size, p.lane);
+    }
     Both both;
+    both.load(at + (U - Both::kCount) * row_size);
 #pragma unroll
-    for (int first = 0; first < U; first += Inputs::kCount) {
-      await_shared();
-      const Inputs group = inputs;
-      if (first + Inputs::kCount < U) inputs.load(at + (first + Inputs::kCount) * row_size);
-      else both.load(at + (U - Both::kCount) * row_size);
-      stop();
+    for (int j = 0; j < U; ++j) {
 #pragma unroll
-      for (int k = 0; k < Inputs::kCount; ++k) {
-        const int j = first + k;
+      for (int q = 0; q < NP / 4; ++q) {
+        F32<4> h4;
 #pragma unroll
-        for (int n = 0; n < NP; ++n) {
-          e[j][n] = __builtin_amdgcn_exp2f(dt[j] * decay[n]);
-          hs[j + 1][n] = fmaf(e[j][n], hs[j][n], u[j] * group.row[k].b[n]);
+        for (int i = 0; i < 4; ++i) {
+          e[j][4 * q + i] = __builtin_amdgcn_exp2f(dt[j] * decay[4 * q + i]);
+          h4[i] = e[j][4 * q + i] * hs[j][4 * q + i];
         }
-        pin(hs[j + 1]);
+        h4 = add_products<NP>(b_of, j, q, u[j], h4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) hs[j + 1][4 * q + i] = h4[i];
       }
     }
     float v[4 * NP];       // what two steps give to grad_b and grad_c
@@ -757,16 +870,25 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 1 ? 3 : 2) void s
       await_shared();
       const Both group = both;
       if (first > 0) both.load(at + (first - Both::kCount) * row_size);
-      else inputs.load(rows + max(t - U, p.from) * row_size);
       stop();
 #pragma unroll
       for (int k = Both::kCount - 1; k >= 0; --k) {
         const int j = first + k;
         float* const pair = v + (j & 1 ? 0 : 2 * NP);
         float y = 0.f, along = 0.f, step = 0.f;
+        float totals[NP];
+#pragma unroll
+        for (int q = 0; q < NP / 4; ++q) {
+          F32<4> g4;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) g4[i] = g[4 * q + i];
+          g4 = add_products<NP>(c_of, j, q, dy[j], g4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) totals[4 * q + i] = g4[i];
+        }
 #pragma unroll
         for (int n = 0; n < NP; ++n) {
-          const float total = fmaf(group.row[k].c[n], dy[j], g[n]);
+          const float total = totals[n];
           y = fmaf(group.row[k].c[n], hs[j + 1][n], y);
           pair[n] = total * u[j];
           pair[NP + n] = dy[j] * hs[j + 1][n];
