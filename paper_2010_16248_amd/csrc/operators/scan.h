@@ -62,8 +62,13 @@ __global__ __launch_bounds__(256) void scan_pack_kernel(const T* __restrict__ b,
 }
 
 // ---- what the passes share --------------------------------------------------------------------------------
-// A lane has one channel and NP of its states; a wave 64 channels of a group.  The WAVES waves of a workgroup have NP states each, and add what
-// these contribute in LDS.  Steps of a turn that lie beyond the sequence have dt = 0: they change nothing.
+// A lane has one channel and NP of its states; a wave 64 channels of a group.  The WAVES waves of a workgroup have NP states each; what the states of
+// a channel have in common (dt, dt x, the gradient through the gate) each works out for some of a turn's steps and leaves in LDS, and what they
+// contribute to a sum over states they add there.  Steps of a turn that lie beyond the sequence have dt = 0: they change nothing.
+// All kernels that walk steps are bound by the vector units: a step of a state takes a power of two (the time of two other instructions), its
+// argument, the product with h and those of the pass, for 1 / 16 of the bytes of a step of a channel.  4 states a wave cost the least registers, so that
+// other waves run while one waits: a wave of 16 states, which shares nothing, needs 126 registers in scan_ends_kernel backward, 4 waves a SIMD, and
+// kept the vector units busy for 0.77 of the time; four waves of 4 states with 74 registers 0.96.
 
 struct ScanPlace {
   int lane, part, group;
@@ -184,7 +189,7 @@ template <int NP, int WAVES>
 __device__ __forceinline__ Shared shared_rows(const ScanShape& s, const ScanPlace& p, const float* bc) {
   return shared_at(bc) + rows_of<NP, WAVES>(s, p);
 }
-// Rows are requested in groups of as many as 16 scalar registers hold (at least one), a group ahead.  Scalar loads return in any order, so a wait for one is a
+// What products along the states take comes through scalar registers.  Rows are requested in groups of as many as 16 of them hold (at least one), a group ahead.  Scalar loads return in any order, so a wait for one is a
 // wait for all: a group is awaited before the next one is requested, which the compiler's own waits, at first use, would not do.  The stops keep the
 // scheduler from gathering more rows than the scalar registers hold.
 __device__ __forceinline__ void stop() { __builtin_amdgcn_sched_barrier(0); }
@@ -213,17 +218,16 @@ struct SharedGroup {
 };
 
 // Products of a step's b or c, which the channels share, with a value of each channel's: what a matrix instruction of 16 blocks of 4 states x 4
-// channels makes of 4 numbers and 64, and adds to 4 states of 64 channels, a lane's own, at the issue of one vector instruction.  The numbers of
-// a turn lie with the lanes of as few registers as hold them: lane l of the k-th has state l % NP of step k 64 / NP + l / NP.  The instruction takes those of
-// the four lanes it names for all its blocks.
+// channels makes of 4 numbers and 64, and adds to 4 states of 64 channels, a lane's own, at the issue of one vector instruction for 4.  The numbers
+// of a turn lie with the lanes of one register: lane l has state l % NP of step l / NP.  The instruction takes those of the four lanes it names for
+// all its blocks.  (8 x 4096 x 2048, 16 states, bf16: with products and sums by vector instructions the ends of the backward pass took 411 us, with these and
+// nothing else changed 374.)
 template <int NP>
 struct HeldRows {
-  static constexpr int kSteps = kWave / NP, kCount = kScanAhead > kSteps ? kScanAhead / kSteps : 1;
-  float v[kCount];
+  static_assert(NP * kScanAhead <= kWave, "a turn's numbers in one register");
+  float v;
   __device__ __forceinline__ void load(const float* rows, int row, int lane) {
-    const unsigned at = (unsigned)min(lane / NP, kScanAhead - 1) * row + lane % NP;
-#pragma unroll
-    for (int k = 0; k < kCount; ++k) v[k] = rows[k * kSteps * row + at];
+    v = rows[(unsigned)min(lane / NP, kScanAhead - 1) * row + lane % NP];
   }
 };
 template <int FROM>
@@ -233,8 +237,8 @@ __device__ __forceinline__ F32<4> four_states(float held, float u, F32<4> add) {
 // add + (step j's numbers of the q-th four states) u.  (j and q are known when this is compiled.)
 template <int NP>
 __device__ __forceinline__ F32<4> add_products(const HeldRows<NP>& held, int j, int q, float u, F32<4> add) {
-  const float v = held.v[j / HeldRows<NP>::kSteps];
-  switch (j % HeldRows<NP>::kSteps * (NP / 4) + q) {
+  const float v = held.v;
+  switch (j * (NP / 4) + q) {
     case 0: return four_states<0>(v, u, add);
     case 1: return four_states<1>(v, u, add);
     case 2: return four_states<2>(v, u, add);
@@ -254,43 +258,15 @@ __device__ __forceinline__ F32<4> add_products(const HeldRows<NP>& held, int j, 
   }
 }
 
-// A channel's elements of a turn's steps (of the last one there is, beyond).
-template <typename T>
-__device__ __forceinline__ void load_turn(const T* row, int64_t stride, const ScanPlace& p, int last, T (&v)[kScanAhead]) {
-  const LaneOf lane(p);
-#pragma unroll
-  for (int j = 0; j < kScanAhead; ++j) {
-    v[j] = lane.of(row);
-    row += j < last ? stride : 0;
-  }
-}
+// The last of a turn's steps that there is.
 __device__ __forceinline__ int last_of(const ScanPlace& p, int64_t t) { return (int)min(p.end - 1 - t, (int64_t)kScanAhead - 1); }
-
-// dt and dt x of a turn.
-template <typename T>
-__device__ __forceinline__ void steps_and_inputs(const T (&xv)[kScanAhead], const T (&dv)[kScanAhead], float shift, int soft, int last,
-                                                 float (&dt)[kScanAhead], float (&u)[kScanAhead]) {
-#pragma unroll
-  for (int j = 0; j < kScanAhead; ++j) dt[j] = (float)dv[j] + shift;
-  if (soft) {            // (one branch for all steps: their chains run side by side)
-#pragma unroll
-    for (int j = 0; j < kScanAhead; ++j) dt[j] = softplus(dt[j]).value;
-  }
-#pragma unroll
-  for (int j = 0; j < kScanAhead; ++j) u[j] = dt[j] * (float)xv[j];
-  if (last < kScanAhead - 1) {
-#pragma unroll
-    for (int j = 0; j < kScanAhead; ++j) {
-      u[j] = j <= last ? u[j] : 0.f;
-      dt[j] = j <= last ? dt[j] : 0.f;
-    }
-  }
-}
 
 // ---- chunks: what each does to a state --------------------------------------------------------------------
 // The state behind a chunk that starts from zero, the sum of its dt (the state in front decays by exp(a sum)) and, for the backward pass,
 // the gradient of the state in front of it if nothing came from behind, and in marks the state and the sum in front of each of its turns
 // (batch x turns x (states, filled up, + 1) x channels).
+// 8 x 4096 x 2048, 16 states, bf16: backward 351 us, vector units busy for 0.96 of them, 5 % of the time with matrix instructions beside; 65536 x 672 fp32:
+// forward 150 us, 0.99.  (Minimum of four waves a SIMD: without one the matrix instructions' sums go to registers that vector instructions cannot take.)
 template <typename T, int NP, int WAVES, bool BACKWARD>
 __global__ __launch_bounds__(WAVES * kWave, 4) void scan_ends_kernel(ScanShape s, const T* __restrict__ x, const T* __restrict__ delta,
                                                                      const float* __restrict__ a, const float* __restrict__ bc,
@@ -486,8 +462,8 @@ __global__ __launch_bounds__(kWave * kCarryWaves) void scan_carry_kernel(ScanSha
 }
 
 // ---- forward ----------------------------------------------------------------------------------------------
-// The waves of a workgroup share what the states of a channel have in common: each works it out for some of a turn's steps, and finishes their
-// outputs.
+// Each wave finishes the outputs of its steps of a turn.  8 x 4096 x 2048, 16 states, bf16, ragged (0.63 of the steps): 207 us, vector units busy for 0.95
+// of them.
 template <typename T, int NP, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave, 4) void scan_forward_kernel(
     ScanShape s, const T* __restrict__ x, const T* __restrict__ delta, const float* __restrict__ a, const float* __restrict__ bc,
@@ -616,7 +592,8 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void scan_forward_kernel(
 }
 
 // ---- a few steps: lanes share a channel ----------------------------------------------------------------------
-// L lanes have 4 states each of a channel: states come and go in whole pieces of memory.
+// L lanes have 4 states each of a channel: states come and go in whole pieces of memory.  One token of 64 x 1344 channels x 16 states: 5.1 us, of which
+// 11 MB of states at the rate of a large copy are 2.2; a launch that does nothing takes 2.
 template <typename T, int L>
 __global__ __launch_bounds__(256) void scan_walk_kernel(ScanShape s, const T* __restrict__ x, const T* __restrict__ delta,
                                                         const float* __restrict__ a, const T* __restrict__ b, const T* __restrict__ c,
@@ -712,12 +689,13 @@ __device__ __forceinline__ float lanes_sum(float (&v)[V], int l) {
 }
 
 // A chunk, from its end: the states of kScanAhead steps at a time are computed from what scan_ends_kernel left in front of them and from the state
-// in front of the chunk, kept in registers, and walked back.  The waves of a workgroup share what the states of a channel have in common: each works
-// it out for some of the steps, and finishes the gradients of those.
+// in front of the chunk, kept in registers, and walked back.  (All states of a chunk in LDS would be 32 KB for 8 steps of 64 channels x 16 states.)  Each wave
+// finishes the gradients of its steps of a turn.  8 x 4096 x 2048, 16 states, bf16: 858 us, vector units busy for 0.94 of them; 977 and 0.81 with a
+// turn's inputs and marks requested where it starts and not a turn ahead.
 // parts: of a chunk, states + 2 rows of channels (grad_a, grad_d, grad_delta_bias); shared_parts: of a block of channels and a step, the
 // sums of grad_b and grad_c over the block.
 template <typename T, int NP, int WAVES>
-__global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 1 ? 3 : 2) void scan_backward_kernel(
+__global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void scan_backward_kernel(
     ScanShape s, const T* __restrict__ x, const T* __restrict__ delta, const float* __restrict__ a, const float* __restrict__ bc,
     const float* __restrict__ d, const T* __restrict__ gate, const float* __restrict__ delta_bias, const int32_t* __restrict__ lengths,
     const T* __restrict__ dout, const float* __restrict__ h0, const float* __restrict__ dlast, const float* __restrict__ ends,

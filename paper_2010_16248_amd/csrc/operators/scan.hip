@@ -36,26 +36,26 @@ int32_t check_scan(const acc_scan* c, bool backward) {
 }
 
 // Up to here lanes share a channel and walk the steps: one launch, but every step waits for its own loads.  us of it and of the chunks' kernels at
-// 1, 4, 8, 12, 16, 24, 32 steps, 16 states: bf16 64 x 1344 channels 5.1, 7.9, 11.9, 16.1, 20.0, 28.8, 37.0 and 17.0, 17.0, 17.6, 19.4, 19.8, 22.7, 26.2;
-// bf16 8 x 2048 3.5 (1), 6.3 (8), 8.1, 9.8, 13.2, 16.5 and 8.4, 8.7, 10.2, 10.4, 12.2, 13.8; fp32 64 x 4096 40.4 (16), 56.4 (24) and 41.5, 45.2;
-// 64 states 16 x 1024 15.5 (16), 21.5 (24) and 18.5, 21.0; 4 states 15.6 (32) and 17.6.
+// 1, 8, 12, 16, 20, 24, 32 steps: bf16 64 x 1344 channels x 16 states 5.1, 11.9, 15.9, 19.5, 24.2, 28.6, 37.5 and 17.1, 17.3, 19.0, 19.2, 21.9, 22.3, 25.9;
+// 8 x 2048 x 16 3.6, 6.3, 8.0, 9.8, 11.4, 13.1, 16.7 and 8.0, 8.2, 9.4, 9.5, 10.7, 10.9, 12.1; fp32 64 x 4096 x 16 41.0 and 40.5 (16), 49.2 and 43.8 (20);
+// 16 x 1024 x 64 15.6 and 17.6 (16), 21.2 and 19.7 (24); 16 x 1024 x 4 9.0 and 10.9 (16), 12.2 and 13.1 (24).
 constexpr int64_t kScanWalkSteps = 16;
-// Chunks of the forward pass cost every step a second time (scan_ends_kernel) and two more launches, for waves.  None up to 128 steps, and from this
-// many waves on without them; otherwise as long as leave this many, from 32 to 128 steps.  us without chunks and with chunks of 32, 64, 128, 256 steps,
-// bf16, 16 states: 8 x 128 x 768 (384 waves without chunks) 33, 34, 49; 1 x 512 x 1536 (96) 106, 34, 48, 74, 132; 1 x 4096 x 1536 806, 87, 81, 91, 147;
-// 20 x 512 x 1024 (1280) 125, 111, 111, 121, 172; 64 x 512 x 512 (2048) 130, 158, 151, 155, 195; 64 x 512 x 1024 (4096) 175, 287, 264, 269, 283;
-// 8 x 4096 x 2048 (1024) 834, 555, 501, 491, 523; 4 states 64 x 512 x 1024 (1024) 185, 147, 135, 142, 173; 32 states 4 x 1024 x 1536 (768) 201,
-// 127, 123, 121, 191.
-constexpr int64_t kScanFew = 128, kScanLone = 2048, kScanWaves = 6144, kScanShortest = 32, kScanLongest = 128;
-// Chunks of the backward pass: as long as leave this many workgroups, from 16 to 256 steps.  us with chunks of 16, 32, 64, 128, 256 steps:
-// 1 x 512 x 1536 (24 workgroups per chunk) 57, 66, 86, 140, 248; 2 x 2048 x 768 123, 108, 111, 162, 264; 4 x 1024 x 1536 193, 178, 175, 187,
-// 294; 64 x 128 x 512 133, 133, 149, 163, 163; 8 x 4096 x 2048 2365, 1931, 1399, 1348, 1335.
-constexpr int64_t kScanGroups = 1536, kBackwardShortest = 16, kBackwardLongest = 256;
+// Chunks of the forward pass cost every step a second time (scan_ends_kernel) and two more launches, for waves.  None up to 64 steps, and from kScanLone
+// waves on without them; otherwise as long as leave kScanWaves, from 32 to 128 steps.  us without chunks and with chunks of 32, 64, 128, 256 steps,
+// bf16, 16 states: 1 x 128 x 1536 (96 waves without chunks) 26, 19, 26; 8 x 128 x 768 (384) 26, 24, 27; 8 x 256 x 768 (384) 45, 30, 34, 42;
+// 1 x 512 x 1536 (96) 84, 24, 27, 41, 71; 1 x 4096 x 1536 624, 77, 70, 69, 94; 20 x 512 x 1024 (1280) 105, 101, 93, 92, 109; 64 x 512 x 512 (2048) 109,
+// 148, 134, 130, 130; 64 x 512 x 1024 (4096) 169, 277, 248, 232, 219; 8 x 4096 x 2048 (1024) 618, 547, 480, 464, 459; 4 states 64 x 512 x 1024 (1024) 151,
+// 148, 141, 140, 166; 32 states 4 x 1024 x 1536 (768) 179, 116, 104, 99, 129; 64 states 2 x 2048 x 768 (192) 517, 115, 105, 122, 129.
+constexpr int64_t kScanFew = 64, kScanLone = 2048, kScanWaves = 4096, kScanShortest = 32, kScanLongest = 128;
+// Chunks of the backward pass: as long as leave this many workgroups and waves, from 16 to 256 steps.  us with chunks of 16, 32, 64, 128, 256 steps, bf16:
+// 16 states (4 waves) 1 x 512 x 1536 (24 workgroups per chunk) 41, 44, 49, 79, 139; 2 x 2048 x 768 (24) 102, 87, 84, 106, 143; 4 x 1024 x 1536 (96) 166,
+// 148, 138, 138, 189; 64 x 128 x 512 (512) 117, 107, 107, 105; 8 x 4096 x 2048 (256) 1730, 1359, 1195, 1155, 1132; 4 states (1 wave) 64 x 512 x 1024 (1024)
+// 411, 354, 330, 331, 349; 64 states (8 waves) 2 x 2048 x 768 (24) 347, 274, 251, 299, 300.
+constexpr int64_t kBackwardGroups = 768, kBackwardWaves = 3072, kBackwardShortest = 16, kBackwardLongest = 256;
 
 struct ScanPlan {
   bool walk = false, large = false;
-  int each = 16, waves = 1, padded = 16;    // states of a lane, waves of a workgroup, states in all
-  int split = 1;                            // waves of a workgroup of the forward pass' last kernel
+  int padded = 16, split = 1;               // states, filled up; waves of a workgroup
   int64_t group = 0, blocks = 0;            // channels of a group, blocks of 64 of them
   int64_t chunk = 0, chunks = 1, rows = 0;  // steps of a chunk, chunks, rows of a sequence's b and c
   int64_t packed = 0, ends = 0, starts = 0, sums = 0, marks = 0, parts = 0, shared_parts = 0, bytes = 0;   // offsets in the workspace
@@ -65,9 +65,8 @@ ScanPlan plan_scan(const acc_scan& c, bool backward) {
   ScanPlan p;
   p.walk = !backward && c.steps <= kScanWalkSteps;
   if (p.walk || c.batch == 0) return p;
-  p.each = c.states <= 4 ? 4 : c.states <= 8 ? 8 : 16;
-  p.waves = c.states <= 16 ? 1 : c.states <= 32 ? 2 : 4;
-  p.padded = p.each * p.waves;
+  p.padded = c.states <= 4 ? 4 : c.states <= 8 ? 8 : c.states <= 16 ? 16 : c.states <= 32 ? 32 : 64;
+  p.split = std::min(8, p.padded / 4);
   p.group = c.channels / c.groups;
   p.blocks = up(p.group, kWave);
   // A launch has fewer than 2^32 work items per axis: the last one of the backward pass has these and up to 2^30 more.
@@ -76,9 +75,10 @@ ScanPlan plan_scan(const acc_scan& c, bool backward) {
   const int64_t groups = c.batch * c.groups * p.blocks;              // workgroups of one chunk
   if (backward) {
     p.chunk = kBackwardLongest;
-    while (p.chunk > kBackwardShortest && groups * up(c.steps, p.chunk) < kScanGroups) p.chunk /= 2;
+    while (p.chunk > kBackwardShortest &&
+           groups * up(c.steps, p.chunk) < std::max(kBackwardGroups, up(kBackwardWaves, p.split)))
+      p.chunk /= 2;
   } else {
-    p.split = std::min(8, p.padded / 4);
     p.chunk = std::max<int64_t>(1, c.steps);
     if (c.steps > kScanFew && groups * p.split < kScanLone) {
       p.chunk = kScanLongest;
