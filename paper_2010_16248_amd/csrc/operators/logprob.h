@@ -158,7 +158,8 @@ __global__ __launch_bounds__(256) void logprob_stream_kernel(LogprobOut o, const
 // ---- forward with them ------------------------------------------------------------------------------------------
 // A workgroup holds a part of a row in registers.  The part's tokens lie with 64 groups of lanes; the `top` groups with the largest maxima have a
 // least maximum, below which none of the `top` most probable tokens can be.  What is not below it, few in general, is listed in LDS
-// and ordered by counting; where it is more than the list holds, one token after the other is found among all.
+// and ordered by counting.  Where it is more than the list holds (rows masked but for a few tokens, rows of few values), list_again finds a key with
+// fewer above it.
 constexpr int kTopGroups = 64;
 constexpr int kTopList = 1024;
 
@@ -189,6 +190,106 @@ __device__ __forceinline__ int place_in(const Token* list, int count, Token toke
   return place;
 }
 
+// Lists what can be among the `wanted` most probable of a part's tokens, read again: all above a key, fewer than the list holds, and of the tokens of this
+// key the first ones.  The key is `least`, that of a logit that so many tokens reach, or, where too many lie above it, is halved up to from there; where so
+// many do not (the rest are no numbers) it is zero.  Returns their number; `counts` holds a number a wave.
+// 20 of 128 x 131072 bf16, masked but for 50: 46 us (a row as the model leaves it 19), 1024 x 50257 fp32 112 (47); 259 and 801 with one token after the
+// other sought among all.
+template <typename T, int N, int THREADS>
+__device__ __forceinline__ int list_again(const T* l, int size, unsigned from, int wanted, unsigned least, Token* list, unsigned* counts,
+                                          unsigned* listed) {
+  constexpr int waves = THREADS / kWave, turn = THREADS * N;
+  const int lane_of = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  auto pack_at = [&](int at) {
+    const int left = size - at;
+    Pack<T, N> v;
+    if (left >= N) return load<N>(l + at);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = i < left ? l[at + i] : (T)0.f;
+    return v;
+  };
+  // tokens above the key << 16 | tokens of the key
+  auto count = [&](unsigned key) {
+    unsigned n = 0;
+#pragma unroll 1
+    for (int at = threadIdx.x * N; at < size; at += turn) {
+      const Pack<T, N> v = pack_at(at);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const unsigned own = key_at(v[i]);
+        if (at + i < size) n += own > key ? 0x10000u : own == key;
+      }
+    }
+#pragma unroll
+    for (int m = 1; m < kWave; m *= 2) n += __shfl_xor(n, m);
+    __syncthreads();
+    if (lane_of == 0) counts[wave] = n;
+    __syncthreads();
+    n = 0;
+#pragma unroll 1
+    for (int w = 0; w < waves; ++w) n += counts[w];
+    return n;
+  };
+  unsigned key = least, most = 0xffffffffu, n = count(key);
+  if ((int)(n >> 16) + (int)(n & 0xffffu) < wanted) {
+    key = 0;
+    n = count(key);
+  }
+  while (n >> 16 > kTopList) {               // ends with key == most at the latest, which fewer than `wanted` are above
+    const unsigned half = key + (most - key) / 2 + 1, m = count(half);
+    if ((int)(m >> 16) + (int)(m & 0xffffu) >= wanted) {
+      key = half;
+      n = m;
+    } else {
+      most = half - 1;
+    }
+  }
+  const int above = (int)(n >> 16), need = max(wanted - above, 0);
+  for (int i = threadIdx.x; i < kTopList; i += THREADS) list[i] = 0;
+  if (threadIdx.x == 0) *listed = 0;
+  __syncthreads();
+#pragma unroll 1
+  for (int at = threadIdx.x * N; at < size; at += turn) {
+    const Pack<T, N> v = pack_at(at);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (at + i < size && key_at(v[i]) > key) list[atomicAdd(listed, 1u)] = token_of((float)v[i], from + at + i);
+  }
+  int taken = 0;
+#pragma unroll 1
+  for (int start = 0; start < size && taken < need; start += turn) {       // the same for all threads
+    const int at = start + threadIdx.x * N;
+    Pack<T, N> v{};
+    if (at < size) v = pack_at(at);
+    int own = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) own += at + i < size && key_at(v[i]) == key;
+    int up_to = own;
+#pragma unroll
+    for (int m = 1; m < kWave; m *= 2) {
+      const int other = __shfl_up(up_to, m);
+      if (lane_of >= m) up_to += other;
+    }
+    __syncthreads();
+    if (lane_of == 63) counts[wave] = up_to;
+    __syncthreads();
+    int place = taken + up_to - own;
+#pragma unroll 1
+    for (int w = 0; w < waves; ++w) {
+      if (w < wave) place += (int)counts[w];
+      taken += (int)counts[w];
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (at + i < size && key_at(v[i]) == key) {
+        if (place < need) list[above + place] = token_of((float)v[i], from + at + i);
+        ++place;
+      }
+  }
+  __syncthreads();
+  return above + min(taken, need);
+}
+
 template <typename T, int N, int K, int THREADS, bool PARTS>
 __global__ __launch_bounds__(THREADS) void logprob_top_kernel(LogprobOut o, const T* __restrict__ logits, int64_t part, int parts,
                                                               RowSums* __restrict__ sums, Token* __restrict__ best) {
@@ -197,7 +298,7 @@ __global__ __launch_bounds__(THREADS) void logprob_top_kernel(LogprobOut o, cons
   __shared__ float group_top[kTopGroups], sum[waves], weighted[waves], least_of;
   __shared__ unsigned listed;
   __shared__ alignas(16) Token list[kTopList];
-  __shared__ Token found[waves];
+  __shared__ unsigned counts[waves];
   const int64_t row = blockIdx.x;
   const int64_t from = blockIdx.y * part;
   const int size = (int)min(part, o.vocab - from);
@@ -272,38 +373,20 @@ __global__ __launch_bounds__(THREADS) void logprob_top_kernel(LogprobOut o, cons
     }
   }
   __syncthreads();
-  const int count = (int)listed, wanted = min(o.top, size);     // tokens this part can give
+  const int wanted = min(o.top, size);     // tokens this part can give
+  int count = (int)listed;
+  if (count > kTopList) {                  // (of all threads, and once more after the list is cleared)
+    __syncthreads();
+    count = list_again<T, N, THREADS>(l, size, (unsigned)from, wanted, key_of(least), list, counts, &listed);
+  }
   auto put = [&](int place, Token token) {
     if (PARTS) best[(row * parts + blockIdx.y) * o.top + place] = token;
     else write_top(o, row, place, r, logit_of(token), id_of(token));
   };
-  if (count <= kTopList) {
-    for (int i = threadIdx.x; i < count; i += THREADS) {
-      const Token token = list[i];
-      const int place = place_in(list, count, token);
-      if (place < wanted) put(place, token);
-    }
-  } else {
-    Token after = ~(Token)0;                       // in front of every token: no key is as large
-    for (int place = 0; place < wanted; ++place) {
-      Token mine = 0;
-      for (int at = threadIdx.x; at < size; at += THREADS) {
-        const Token other = token_of((float)l[at], (unsigned)(from + at));
-        if (other < after && other > mine) mine = other;
-      }
-#pragma unroll
-      for (int m = 1; m < kWave; m *= 2) {
-        const Token other = __shfl_xor(mine, m);
-        if (other > mine) mine = other;
-      }
-      __syncthreads();
-      if ((threadIdx.x & 63) == 0) found[threadIdx.x >> 6] = mine;
-      __syncthreads();
-      for (int w = 0; w < waves; ++w)
-        if (found[w] > mine) mine = found[w];
-      if (threadIdx.x == 0) put(place, mine);
-      after = mine;
-    }
+  for (int i = threadIdx.x; i < count; i += THREADS) {
+    const Token token = list[i];
+    const int place = place_in(list, count, token);
+    if (place < wanted) put(place, token);
   }
   if (PARTS)
     for (int place = wanted + threadIdx.x; place < o.top; place += THREADS) put(place, 0);

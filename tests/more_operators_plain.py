@@ -236,6 +236,9 @@ def logprob(logits):
         lse_off = base + U * np.abs(lse)
         lp_off = base + U * np.abs(d) + U * np.abs(lp)
         ent_off = base + np.abs(t) * (rel + (depth + 4) * U) + (p * far * (4 * far + 8)).sum(1, keepdims=True) * U + U * np.abs(entropy)
+    empty = top[:, 0] == -np.inf          # (without a token: by definition)
+    lse[empty], lp[empty], entropy[empty] = -np.inf, -np.inf, 0.0
+    lse_off[empty], lp_off[empty], ent_off[empty] = 0.0, np.inf, 0.0
     return lse[:, 0], lp, entropy[:, 0], lse_off[:, 0], lp_off, ent_off[:, 0]
 
 

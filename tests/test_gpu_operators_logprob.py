@@ -111,6 +111,31 @@ def test_masks(top, vocab, kind):
         assert not got[6].any() and not got[1].any()
 
 
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("vocab,top", [(4000, 20), (8192, 64), (32768, 20), (50001, 1), (70000, 64), (262145, 20)])
+def test_rows_that_fill_the_list(vocab, top, kind):
+    """Masked but for as many tokens as are wanted, one fewer, one more and a few hundred; in order; few that are numbers at all; more large logits in one
+    place than the list holds."""
+    print(f"case list {vocab} {top} {kind}", flush=True)
+    gen = torch.Generator().manual_seed(3)
+    rows = []
+    for left in (0, top - 1, top, top + 1, 300):
+        row = torch.full((vocab,), -INF)
+        at = torch.randperm(vocab, generator=gen)[:left]
+        row[at] = torch.randn(left, generator=gen) * 3
+        rows.append(row)
+    order = torch.sort(torch.randn(vocab, generator=gen) * 3).values
+    rows += [order, order.flip(0), torch.where(torch.arange(vocab) >= vocab - 2000, order + 5, -order.abs())]
+    rows.append(torch.full((vocab,), torch.finfo(kind).min))
+    rows[-1][torch.randperm(vocab, generator=gen)[:top + 2]] = 1.5
+    logits = torch.stack(rows).to(kind).to(DEV)
+    check_forward(logits, torch.arange(len(rows), device=DEV), top)
+    few = torch.full((2, vocab), NAN, device=DEV, dtype=kind)
+    few[0, vocab // 2], few[0, vocab - 1], few[1, 5] = 1.0, 2.0, -INF
+    r = forward(few, torch.zeros(2, dtype=torch.int64, device=DEV), top)
+    assert np.array_equal(r["top_ids"].cpu().numpy(), M.best(few, top))
+
+
 @pytest.mark.parametrize("vocab", [50, 20000])
 @pytest.mark.parametrize("top", [0, 6])
 def test_infinities_and_nan(top, vocab):
