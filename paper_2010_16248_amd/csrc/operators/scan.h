@@ -90,8 +90,8 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanShape& s, const int32_
   p.channel = (unsigned)p.group * s.group + (p.valid ? within : s.group - 1);
   p.byte2 = 2 * p.channel;
   p.byte4 = 4 * p.channel;
-  p.batch = blockIdx.y;
-  p.chunk = blockIdx.z;
+  p.chunk = blockIdx.y;
+  p.batch = blockIdx.z;
   p.len = steps_of(lengths, p.batch, s.steps);
   p.from = p.chunk * s.chunk;
   p.to = min(p.from + s.chunk, s.steps);

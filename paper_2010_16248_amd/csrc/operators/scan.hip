@@ -153,7 +153,7 @@ dim3 carry_threads(const acc_scan& c, const ScanPlan& p) {
 template <typename T, int NP, int WAVES>
 void forward_ends(const acc_scan& c, const ScanPlan& p, const ScanIn& in, char* ws, Queue& queue) {
   auto at = [&](int64_t offset) { return reinterpret_cast<float*>(ws + offset); };
-  LAUNCH((scan_ends_kernel<T, NP, WAVES, false>), dim3((unsigned)(c.groups * p.blocks), (unsigned)c.batch, (unsigned)(p.chunks - 1)),
+  LAUNCH((scan_ends_kernel<T, NP, WAVES, false>), dim3((unsigned)(c.groups * p.blocks), (unsigned)(p.chunks - 1), (unsigned)c.batch),
          dim3(kWave * WAVES), queue, shape_of(c, p), as<T>(in.x), as<T>(in.delta), in.a, at(p.packed), nullptr, in.delta_bias, in.lengths,
          nullptr, at(p.ends), nullptr, at(p.sums), nullptr);
 }
@@ -184,7 +184,7 @@ void forward(const acc_scan& c, const ScanPlan& p, const ScanIn& in, void* out, 
                       : p.padded == 16 ? scan_forward_kernel<T, 4, 4>
                       : p.padded == 32 ? scan_forward_kernel<T, 4, 8>
                                        : scan_forward_kernel<T, 8, 8>;
-  LAUNCH(kernel, dim3((unsigned)(c.groups * p.blocks), (unsigned)c.batch, (unsigned)p.chunks), dim3((unsigned)(kWave * p.split)), queue,
+  LAUNCH(kernel, dim3((unsigned)(c.groups * p.blocks), (unsigned)p.chunks, (unsigned)c.batch), dim3((unsigned)(kWave * p.split)), queue,
          shape_of(c, p), as<T>(in.x), as<T>(in.delta), in.a, at(p.packed), in.d, as<T>(in.gate), in.delta_bias, in.lengths, in.h0, at(p.ends),
          static_cast<T*>(out), h_last);
 }
@@ -203,7 +203,7 @@ struct ScanGradients {
 template <typename T, int NP, int WAVES>
 void backward_ends(const acc_scan& c, const ScanPlan& p, const ScanIn& in, const ScanGradients& g, char* ws, Queue& queue) {
   auto at = [&](int64_t offset) { return reinterpret_cast<float*>(ws + offset); };
-  LAUNCH((scan_ends_kernel<T, NP, WAVES, true>), dim3((unsigned)(c.groups * p.blocks), (unsigned)c.batch, (unsigned)p.chunks),
+  LAUNCH((scan_ends_kernel<T, NP, WAVES, true>), dim3((unsigned)(c.groups * p.blocks), (unsigned)p.chunks, (unsigned)c.batch),
          dim3(kWave * WAVES), queue, shape_of(c, p), as<T>(in.x), as<T>(in.delta), in.a, at(p.packed), as<T>(in.gate),
          in.delta_bias, in.lengths, as<T>(g.out), at(p.ends), at(p.starts), at(p.sums), at(p.marks));
 }
@@ -211,7 +211,7 @@ void backward_ends(const acc_scan& c, const ScanPlan& p, const ScanIn& in, const
 template <typename T, int NP, int WAVES>
 void backward_chunks(const acc_scan& c, const ScanPlan& p, const ScanIn& in, const ScanGradients& g, char* ws, Queue& queue) {
   auto at = [&](int64_t offset) { return reinterpret_cast<float*>(ws + offset); };
-  LAUNCH((scan_backward_kernel<T, NP, WAVES>), dim3((unsigned)(c.groups * p.blocks), (unsigned)c.batch, (unsigned)p.chunks), dim3(kWave * WAVES),
+  LAUNCH((scan_backward_kernel<T, NP, WAVES>), dim3((unsigned)(c.groups * p.blocks), (unsigned)p.chunks, (unsigned)c.batch), dim3(kWave * WAVES),
          queue, shape_of(c, p), as<T>(in.x), as<T>(in.delta), in.a, at(p.packed), in.d, as<T>(in.gate), in.delta_bias, in.lengths, as<T>(g.out),
          in.h0, g.last, at(p.ends), at(p.starts), at(p.marks), static_cast<T*>(g.x), static_cast<T*>(g.delta), static_cast<T*>(g.gate), g.h0,
          at(p.parts), at(p.shared_parts));
