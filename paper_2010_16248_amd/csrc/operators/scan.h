@@ -46,19 +46,23 @@ __device__ __forceinline__ Softplus softplus(float r) {
 // of kScanAhead steps.
 constexpr int kScanAhead = 8;    // steps of a turn: under way together
 
+// A lane makes four numbers of a row.  (All counts are below 2^32: divisions of 64 bits took more than half of the time.)
 template <typename T>
 __global__ __launch_bounds__(256) void scan_pack_kernel(const T* __restrict__ b, const T* __restrict__ c, int64_t b_b, int64_t b_t,
-                                                        int64_t c_b, int64_t c_t, int64_t all, int64_t steps, int64_t rows, int groups,
-                                                        int states, int padded, const int32_t* __restrict__ lengths,
+                                                        int64_t c_b, int64_t c_t, unsigned all, int64_t steps, unsigned rows, unsigned groups,
+                                                        int states, int padded, int fours_log2, const int32_t* __restrict__ lengths,
                                                         float* __restrict__ to) {
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / (2 * padded);
+  const unsigned at = blockIdx.x * 256 + threadIdx.x, row = at >> fours_log2;
   if (row >= all) return;
-  const int k = (int)(at - row * 2 * padded), n = k < padded ? k : k - padded;
-  const int64_t t = row % rows, g = row / rows % groups, batch = row / rows / groups;
-  float v = 0.f;
-  if (n < states && t < steps_of(lengths, batch, steps))
-    v = k < padded ? (float)b[batch * b_b + t * b_t + g * states + n] : (float)c[batch * c_b + t * c_t + g * states + n];
-  to[at] = v;
+  const int k = (int)(at & ((1u << fours_log2) - 1)) * 4, n = k < padded ? k : k - padded;
+  const unsigned rest = row / rows, t = row - rest * rows;
+  const int64_t batch = rest / groups, g = rest - (unsigned)batch * groups;
+  F32<4> v = {};
+  if (n < states && t < steps_of(lengths, batch, steps)) {
+    const T* const from = (k < padded ? b + batch * b_b + t * b_t : c + batch * c_b + t * c_t) + g * states + n;
+    v = widen<T, 4>(load_some<4>(from, states - n));
+  }
+  store<float, 4>(to + (int64_t)at * 4, v);
 }
 
 // ---- what the passes share --------------------------------------------------------------------------------

@@ -129,8 +129,10 @@ template <typename T>
 void pack(const acc_scan& c, const ScanPlan& p, const ScanIn& in, float* to, Queue& queue) {
   const int64_t all = c.batch * c.groups * p.rows;
   if (all == 0) return;
-  LAUNCH(scan_pack_kernel<T>, dim3((unsigned)up(all * 2 * p.padded, 256)), dim3(256), queue, as<T>(in.b), as<T>(in.c), c.b_batch, c.b_step,
-         c.c_batch, c.c_step, all, c.steps, p.rows, c.groups, c.states, p.padded, in.lengths, to);
+  int fours_log2 = 1;
+  while (4 << fours_log2 < 2 * p.padded) ++fours_log2;
+  LAUNCH(scan_pack_kernel<T>, dim3((unsigned)up(all << fours_log2, 256)), dim3(256), queue, as<T>(in.b), as<T>(in.c), c.b_batch, c.b_step,
+         c.c_batch, c.c_step, (unsigned)all, c.steps, (unsigned)p.rows, (unsigned)c.groups, c.states, p.padded, fours_log2, in.lengths, to);
 }
 
 template <typename T, int L>
