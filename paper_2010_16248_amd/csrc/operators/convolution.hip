@@ -58,9 +58,9 @@ ConvolutionShape shape_of(const acc_convolution& c, const ConvolutionPlan& p) {
   return {c.batch, c.steps, c.channels, c.x_batch, c.x_step, c.out_batch, c.out_step, c.grad_x_batch, c.grad_x_step, p.run, p.runs, p.lanes_log2};
 }
 
-// Whether every pack of N channels is whole and a wave has one run.
+// Whether a wave has one run and every pack of N channels can be made whole.  (Not where a state is replaced: packs that share channels read and write it.)
 template <int N>
-bool full(const acc_convolution& c, const ConvolutionPlan& p) { return c.channels % N == 0 && p.lanes_log2 == 6; }
+bool full(const acc_convolution& c, const ConvolutionPlan& p, bool in_place) { return p.lanes_log2 == 6 && (c.channels % N == 0 || !in_place); }
 
 template <typename F>
 void with_width(int width, F&& run) {
@@ -82,7 +82,7 @@ void forward(const acc_convolution& c, const ConvolutionPlan& p, const void* x, 
   with_width(c.width, [&](auto width) {
     constexpr int W = decltype(width)::value;
     const dim3 grid((unsigned)p.blocks, (unsigned)p.across);
-    const auto kernel = full<N>(c, p) ? convolution_forward_kernel<T, N, W, true> : convolution_forward_kernel<T, N, W, false>;
+    const auto kernel = full<N>(c, p, state && state == last) ? convolution_forward_kernel<T, N, W, true> : convolution_forward_kernel<T, N, W, false>;
     LAUNCH(kernel, grid, dim3(256), queue, shape_of(c, p), static_cast<const T*>(x), weight, bias, state, lengths, static_cast<T*>(out), last,
            c.silu);
   });
@@ -95,7 +95,7 @@ void backward(const acc_convolution& c, const ConvolutionPlan& p, const void* x,
   with_width(c.width, [&](auto width) {
     constexpr int W = decltype(width)::value;
     const dim3 grid((unsigned)p.blocks, (unsigned)p.across);
-    const auto kernel = full<N>(c, p) ? convolution_backward_kernel<T, N, W, true> : convolution_backward_kernel<T, N, W, false>;
+    const auto kernel = full<N>(c, p, false) ? convolution_backward_kernel<T, N, W, true> : convolution_backward_kernel<T, N, W, false>;
     LAUNCH(kernel, grid, dim3(256), queue, shape_of(c, p), static_cast<const T*>(x), weight, bias, state, lengths,
            static_cast<const T*>(dout), dlast, static_cast<T*>(dx), dstate, parts, c.silu);
   });

@@ -125,6 +125,27 @@ def test_states_in_place_of_sequences_shorter_than_the_window():
     assert torch.equal(state, last)
 
 
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("channels", [257, 258, 513, 515, 1001, 2049])
+def test_rows_that_end_in_a_part_of_a_pack(channels, kind):
+    """The last channels alone, in a wave of their own and beside others; a state replaced and one left as it is."""
+    print(f"case ends {channels} {kind}", flush=True)
+    for steps in (1, 2, 40):
+        s = make(3, steps, channels, 4, kind, seed=steps, lengths=[steps, 0, steps // 2])
+        last, out = torch.full_like(s["state"], 7.0), torch.full_like(s["x"], 7.0)
+        kw = dict(bias=s["bias"], lengths=s["lengths"], silu=True)
+        B.convolution_forward(s["x"], s["weight"], out, state=s["state"], last=last, **kw)
+        state, again = s["state"].clone(), torch.full_like(s["x"], 7.0)
+        B.convolution_forward(s["x"], s["weight"], again, state=state, last=state, **kw)
+        assert torch.equal(out, again) and torch.equal(last, state)
+        one = channels - 1                    # the last channel for itself
+        cut = lambda t: t[..., one:].contiguous()
+        alone, end = torch.full_like(cut(out), 7.0), torch.full_like(cut(last), 7.0)
+        B.convolution_forward(cut(s["x"]), s["weight"][one:].contiguous(), alone, state=cut(s["state"]), last=end, bias=s["bias"][one:].contiguous(),
+                              lengths=s["lengths"], silu=True)
+        assert torch.equal(alone, cut(out)) and torch.equal(end, cut(last))
+
+
 def test_what_may_be_left_out():
     s = make(2, 9, 6, 4, F32, bias=False, state=False)
     check(s, True, dlast=False)
