@@ -46,6 +46,10 @@ constexpr int64_t kScanWalkSteps = 16;
 // 1 x 512 x 1536 (96) 84, 24, 27, 41, 71; 1 x 4096 x 1536 624, 77, 70, 69, 94; 20 x 512 x 1024 (1280) 105, 101, 93, 92, 109; 64 x 512 x 512 (2048) 109,
 // 148, 134, 130, 130; 64 x 512 x 1024 (4096) 169, 277, 248, 232, 219; 8 x 4096 x 2048 (1024) 618, 547, 480, 464, 459; 4 states 64 x 512 x 1024 (1024) 151,
 // 148, 141, 140, 166; 32 states 4 x 1024 x 1536 (768) 179, 116, 104, 99, 129; 64 states 2 x 2048 x 768 (192) 517, 115, 105, 122, 129.
+// With lengths, from kScanRagged steps on, up to twice as many waves: without chunks the longest sequence's are the last ones.  32 x 4096 x 1024 (2048) without
+// chunks 691 and with chunks of 128 548, and of one length 804 and 892; fp32 29 x 4370 x 1159 (2204) 899 and 690, 1085 and 1187; 64 x 2048 x 1024 (4096) 563
+// and 562, 631 and 891; 64 x 512 x 512 (2048) 102 and 118.
+constexpr int64_t kScanRagged = 2048;
 constexpr int64_t kScanFew = 64, kScanLone = 2048, kScanWaves = 4096, kScanShortest = 32, kScanLongest = 128;
 // Chunks of the backward pass: as long as leave this many workgroups and waves, from 16 to 256 steps.  us with chunks of 16, 32, 64, 128, 256 steps, bf16:
 // 16 states (4 waves) 1 x 512 x 1536 (24 workgroups per chunk) 41, 44, 49, 79, 139; 2 x 2048 x 768 (24) 102, 87, 84, 106, 143; 4 x 1024 x 1536 (96) 166,
@@ -61,7 +65,8 @@ struct ScanPlan {
   int64_t packed = 0, ends = 0, starts = 0, sums = 0, marks = 0, parts = 0, shared_parts = 0, bytes = 0;   // offsets in the workspace
 };
 
-ScanPlan plan_scan(const acc_scan& c, bool backward) {
+// ragged: there are lengths.
+ScanPlan plan_scan(const acc_scan& c, bool backward, bool ragged) {
   ScanPlan p;
   p.walk = !backward && c.steps <= kScanWalkSteps;
   if (p.walk || c.batch == 0) return p;
@@ -80,7 +85,7 @@ ScanPlan plan_scan(const acc_scan& c, bool backward) {
       p.chunk /= 2;
   } else {
     p.chunk = std::max<int64_t>(1, c.steps);
-    if (c.steps > kScanFew && groups * p.split < kScanLone) {
+    if (c.steps > kScanFew && groups * p.split < (ragged && c.steps >= kScanRagged ? 2 : 1) * kScanLone) {
       p.chunk = kScanLongest;
       while (p.chunk > kScanShortest && groups * p.split * up(c.steps, p.chunk) < kScanWaves) p.chunk /= 2;
     }
@@ -257,7 +262,7 @@ int32_t accordion_scan_workspace_bytes(const acc_scan* c, int32_t backward_pass,
   REQUIRE(out_bytes, "out_bytes is NULL");
   REQUIRE(backward_pass == 0 || backward_pass == 1, "backward must be 0 or 1");
   if (const int32_t rc = check_scan(c, backward_pass)) return rc;
-  const ScanPlan p = plan_scan(*c, backward_pass);
+  const ScanPlan p = plan_scan(*c, backward_pass, true);      // (of one length it takes no more)
   REQUIRE(!p.large, "batch x steps x groups out of range");
   *out_bytes = (size_t)p.bytes;
   return ACC_OK;
@@ -277,7 +282,7 @@ int32_t accordion_scan_forward(const acc_scan* c, const void* x_dev, const void*
               !off_type(out_dev, e) && !off_type(a_dev, 4) && !off_type(d_dev, 4) && !off_type(delta_bias_dev, 4) && !off_type(h0_dev, 4) &&
               !off_type(lengths_dev, 4) && !off_type(h_last_dev, 4),
           "a pointer is not aligned to its element type");
-  const ScanPlan p = plan_scan(*c, false);
+  const ScanPlan p = plan_scan(*c, false, lengths_dev != nullptr);
   REQUIRE(!p.large, "batch x steps x groups out of range");
   if (const int32_t rc = check_workspace(workspace_dev, workspace_bytes, p.bytes)) return rc;
   const Rows shared = shared_rows(*c);
@@ -330,7 +335,7 @@ int32_t accordion_scan_backward(const acc_scan* c, const void* x_dev, const void
               !off_type(delta_bias_dev, 4) && !off_type(h0_dev, 4) && !off_type(lengths_dev, 4) && !off_type(grad_last_dev, 4) &&
               !off_type(grad_a_dev, 4) && !off_type(grad_d_dev, 4) && !off_type(grad_delta_bias_dev, 4) && !off_type(grad_h0_dev, 4),
           "a pointer is not aligned to its element type");
-  const ScanPlan p = plan_scan(*c, true);
+  const ScanPlan p = plan_scan(*c, true, lengths_dev != nullptr);
   REQUIRE(!p.large, "batch x steps x groups out of range");
   if (const int32_t rc = check_workspace(workspace_dev, workspace_bytes, p.bytes)) return rc;
   const int64_t ends = c->batch * c->channels * c->states;
