@@ -117,21 +117,25 @@ __device__ __forceinline__ float target_of(const LogprobOut& o, const T* logits,
 // ---- forward without the most probable tokens ----------------------------------------------------------------
 // A workgroup streams a part of a row once, with the running largest logit and sums of its lanes; parts of a row that has several go to sums.
 // 1000 x 131072 bf16: 48 us, 5.5 TB/s: the rate of a large copy.
-template <typename T, int N, bool ENTROPY, bool PARTS>
-__global__ __launch_bounds__(256) void logprob_stream_kernel(LogprobOut o, const T* __restrict__ logits, int64_t part, int parts,
+// LANES: of a row, all of the workgroup's or a wave's.
+template <typename T, int N, bool ENTROPY, bool PARTS, int LANES>
+__global__ __launch_bounds__(256) void logprob_stream_kernel(LogprobOut o, const T* __restrict__ logits, int64_t rows, int64_t part, int parts,
                                                              RowSums* __restrict__ sums) {
   constexpr int K = 4;       // requests under way
+  static_assert(LANES == 256 || (LANES == kWave && !PARTS), "a wave has a whole row");
   __shared__ RowSums red[4];
-  const int64_t row = blockIdx.x;
+  const int64_t row = LANES == 256 ? blockIdx.x : (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int own = threadIdx.x % LANES;
+  if (row >= rows) return;
   const int64_t from = blockIdx.y * part, to = min(from + part, o.vocab);
   const T* l = logits + row * o.stride;
   RowSums r = no_sums();
-  for (int64_t at = from + threadIdx.x * N; at < to; at += 256 * N * K) {
+  for (int64_t at = from + own * N; at < to; at += LANES * N * K) {
     F32<N> v[K];
     float top = r.top;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int64_t place = at + k * 256 * N, left = to - place;
+      const int64_t place = at + k * LANES * N, left = to - place;
       if (left >= N) {
         v[k] = widen<T, N>(load<N>(l + place));
       } else {
@@ -145,8 +149,8 @@ __global__ __launch_bounds__(256) void logprob_stream_kernel(LogprobOut o, const
 #pragma unroll
     for (int k = 0; k < K; ++k) add_pack<N, ENTROPY>(r, v[k]);
   }
-  r = group_sums<256>(r, red);
-  if (threadIdx.x != 0) return;
+  r = group_sums<LANES>(r, red);
+  if (own != 0) return;
   if (PARTS) {
     sums[row * parts + blockIdx.y] = r;
   } else {
@@ -157,13 +161,14 @@ __global__ __launch_bounds__(256) void logprob_stream_kernel(LogprobOut o, const
 }
 
 // ---- forward with them ------------------------------------------------------------------------------------------
-// A workgroup holds a part of a row in registers.  The part's tokens lie with 64 groups of lanes; the `top` groups with the largest maxima have a
+// A workgroup (a wave, for short rows) holds a part of a row in registers.  The part's tokens lie with 64 groups of lanes; the `top` groups with the largest maxima have a
 // least maximum, below which none of the `top` most probable tokens can be.  What is not below it, few in general, is listed in LDS
 // and ordered by counting.  Where it is more than the list holds (rows masked but for a few tokens, rows of few values), list_again finds a key with
 // fewer above it.  A row is read once: 5 of 700 x 32768 fp32 in 19.8 us, 4.6 TB/s, and 4.0 for the join; 20 of 16 x 131072 bf16 in 8.0 and 4.3, most
 // of it from one wait to the next.
 constexpr int kTopGroups = 64;
-constexpr int kTopList = 1024;
+// Tokens that a workgroup's list holds: a wave's is short, for as many workgroups as a CU takes.
+__host__ __device__ constexpr int top_list(int threads) { return threads == kWave ? 512 : 1024; }
 
 // A token in the order of the most probable ones: its logit's key, then its id, the lowest first.  0: no token.
 typedef unsigned long long Token;
@@ -200,7 +205,7 @@ __device__ __forceinline__ int place_in(const Token* list, int count, Token toke
 template <typename T, int N, int THREADS>
 __device__ __forceinline__ int list_again(const T* l, int size, unsigned from, int wanted, unsigned least, Token* list, unsigned* counts,
                                           unsigned* listed) {
-  constexpr int waves = THREADS / kWave, turn = THREADS * N;
+  constexpr int waves = THREADS / kWave, turn = THREADS * N, kTopList = top_list(THREADS);
   const int lane_of = threadIdx.x & 63, wave = threadIdx.x >> 6;
   auto pack_at = [&](int at) {
     const int left = size - at;
@@ -296,7 +301,8 @@ template <typename T, int N, int K, int THREADS, bool PARTS>
 __global__ __launch_bounds__(THREADS) void logprob_top_kernel(LogprobOut o, const T* __restrict__ logits, int64_t part, int parts,
                                                               RowSums* __restrict__ sums, Token* __restrict__ best) {
   constexpr int waves = THREADS / kWave, each = THREADS / kTopGroups;       // lanes of a group
-  static_assert(each == 4 || each == 16, "groups are whole rows or quarters of rows of 16 lanes");
+  constexpr int kTopList = top_list(THREADS);
+  static_assert(each == 1 || each == 4 || each == 16, "groups are lanes, whole rows or quarters of rows of 16 lanes");
   __shared__ float group_top[kTopGroups], sum[waves], weighted[waves], least_of;
   __shared__ unsigned listed;
   __shared__ alignas(16) Token list[kTopList];
@@ -325,8 +331,10 @@ __global__ __launch_bounds__(THREADS) void logprob_top_kernel(LogprobOut o, cons
   for (int i = 0; i < kTopList; i += THREADS) list[i + threadIdx.x] = 0;
 #pragma unroll
   for (int k = 0; k < K; ++k) top = fmaxf(top, top_of<N>(widen<T, N>(v[k])));
-  top = fmaxf(top, dpp<0xB1>(top));
-  top = fmaxf(top, dpp<0x4E>(top));
+  if (each >= 4) {
+    top = fmaxf(top, dpp<0xB1>(top));
+    top = fmaxf(top, dpp<0x4E>(top));
+  }
   if (each == 16) {
     top = fmaxf(top, dpp<0x141>(top));
     top = fmaxf(top, dpp<0x140>(top));
@@ -431,13 +439,14 @@ __global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(LogprobOut o
 // ---- backward ---------------------------------------------------------------------------------------------
 // One pass: p comes from lse.  16 bytes a lane and 4 requests under way reach the rate of a large copy: 16384 x 65536 bf16, 4.3 GB read and written, in
 // 823 us, 5.2 TB/s.  grad may be logits: a lane writes what it has read.
-template <typename T, int N, bool ENTROPY>
+template <typename T, int N, bool ENTROPY, int LANES>
 __global__ __launch_bounds__(256) void logprob_backward_kernel(const T* logits, const void* __restrict__ targets, bool wide,
                                                                const float* __restrict__ lse_in, const float* __restrict__ dlogprob,
                                                                const float* __restrict__ entropy_in, const float* __restrict__ dentropy,
-                                                               T* grad, int64_t vocab, int64_t stride, int64_t grad_stride, int64_t part) {
+                                                               T* grad, int64_t rows, int64_t vocab, int64_t stride, int64_t grad_stride, int64_t part) {
   constexpr int K = 4;
-  const int64_t row = blockIdx.x;
+  const int64_t row = LANES == 256 ? blockIdx.x : (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (row >= rows) return;
   const int64_t from = blockIdx.y * part, to = min(from + part, vocab);
   int64_t id = -1;
   if (dlogprob) id = id_at(targets, wide, row);
@@ -447,17 +456,17 @@ __global__ __launch_bounds__(256) void logprob_backward_kernel(const T* logits, 
   const T* l = logits + row * stride;
   T* out = grad + row * grad_stride;
   const bool nothing = (!ENTROPY && !named) || lse == -INFINITY;
-  for (int64_t at = from + threadIdx.x * N; at < to; at += 256 * N * K) {
+  for (int64_t at = from + threadIdx.x % LANES * N; at < to; at += LANES * N * K) {
     F32<N> v[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int64_t place = at + k * 256 * N;
+      const int64_t place = at + k * LANES * N;
       v[k] = F32<N>{};
       if (!nothing) v[k] = widen<T, N>(load_some<N>(l + place, to - place));
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int64_t place = at + k * 256 * N;
+      const int64_t place = at + k * LANES * N;
       if (place >= to) break;
       F32<N> r = {};
       if (!nothing) {

@@ -18,8 +18,14 @@ int32_t check_logprob(const acc_logprob* c) {
   return ACC_OK;
 }
 
+// Rows that a wave takes in one turn of its requests: four of them are a workgroup's.  us of a workgroup and of a wave for a row, forward and gradient: bf16
+// 1 x 1000 4.5, 3.8 and 4.3, 4.1; 700 x 2000 6.5, 4.8 and 4.8, 5.2; 3000 x 2000 13.4, 10.0 and 6.3, 8.7; 14379 x 2000 46, 31 and 19, 27; 14379 x 64 30, 14 and
+// 15, 11; fp32 700 x 1000 5.5, 4.1 and 4.2, 4.3; 14379 x 1000 36, 22 and 14, 20; 100000 x 1000 229, 165 and 77, 147.
+bool short_row(const acc_logprob& c) { return c.vocab <= kWave * 4 * (c.type == ACC_BF16 ? 8 : 4); }
+
 struct LogprobPlan {
   int packs = 0, threads = 256;         // with the most probable tokens: packs of a lane
+  bool rows_at_once = false;            // without them: a row is a wave's
   int64_t part = 0, parts = 1;
   int64_t sums = 0, best = 0, bytes = 0;
 };
@@ -36,19 +42,33 @@ constexpr int64_t kGradientGroups = 2048;
 // Parts of 32768 tokens where so many workgroups of 1024 lanes take all rows in two turns, of 8192 (as many as kTopMostSmall) where there are more.
 // us of parts of 8192 and of 32768, 20 tokens wanted: 1 x 32768 fp32 10.3 and 7.7, 1 x 131072 15.2 and 10.8, 128 x 131072 bf16 22.6 and 17.9,
 // 700 x 16384 fp32 18.8 and 20.1, 700 x 65536 41.9 and 50.0, 4096 x 16384 57 and 91, 4096 x 65536 225 and 258; 700 x 32768 bf16 23.6 and 21.1.
-constexpr int64_t kTopGroupsAtOnce = 512, kTopMostSmall = 64;
+constexpr int64_t kTopGroupsAtOnce = 512, kTopMostSmall = 64, kSmallPart = 256 * 32;
+
+// A wave for a row: of up to 512 tokens (an element a lane at a time, so that all 64 groups have some), of up to 2048 where there are many rows, or where packs
+// of n would leave some of the `top` largest groups empty.  us of a workgroup of 256 lanes and of a wave: bf16 1 x 500, 20 wanted 13.7 and 6.2;
+// 700 x 283, 16 13.3 and 6.1; 14379 x 283, 16 131 and 19.6; fp32 64 x 500, 20 5.3 and 5.7; 14379 x 283, 16 36 and 18.9; bf16 700 x 1024, 5 5.9 and 6.6; 700 x 2000,
+// 20 6.4 and 9.0, 64 71 and 37; 2000 x 2048, 20 9.7 and 9.7; 4096 x 2048, 20 15.3 and 12.9; 14379 x 1000, 20 44 and 29; fp32 14379 x 2048, 20 44 and 34,
+// 64 142 and 146.
+constexpr int64_t kTopWaveAlways = 512, kTopWaveMost = 2048, kTopWaveRows = 2048;
 
 LogprobPlan plan_logprob(const acc_logprob& c) {
   LogprobPlan p;
   const int64_t n = c.type == ACC_BF16 ? 8 : 4;
   if (c.top > 0) {
     // parts that 256 lanes hold, or 1024
-    const int64_t small = 256 * 32;
     p.packs = (int)(c.vocab <= 256 * n ? 1 : (c.vocab <= 256 * 8 ? 8 : 32) / n);
-    if (c.vocab > small && (c.rows * up(c.vocab, 4 * small) <= kTopGroupsAtOnce || c.vocab > kTopMostSmall * small)) p.threads = 1024;
+    const bool wave = c.vocab <= kTopWaveAlways || (c.vocab <= kTopWaveMost && (c.rows >= kTopWaveRows || c.top * 4 * n > c.vocab));
+    if (wave) {
+      p.threads = kWave;
+      p.part = c.vocab <= kTopWaveAlways ? kTopWaveAlways : kTopWaveMost;
+      p.parts = 1;
+      return p;
+    }
+    if (c.vocab > kSmallPart && (c.rows * up(c.vocab, 4 * kSmallPart) <= kTopGroupsAtOnce || c.vocab > kTopMostSmall * kSmallPart)) p.threads = 1024;
     p.part = p.threads * n * p.packs;
   } else {
     p.part = c.vocab;
+    p.rows_at_once = short_row(c);
     if (c.rows < kLogprobGroups) p.part = std::max(kStreamPart, up(c.vocab, up(kLogprobGroups, std::max<int64_t>(1, c.rows))));
     p.part = up(p.part, 64) * 64;
   }
@@ -65,8 +85,13 @@ LogprobPlan plan_logprob(const acc_logprob& c) {
 template <typename T, int N, int K, int THREADS>
 void top_rows(const LogprobPlan& p, const LogprobOut& o, const T* logits, int64_t rows, RowSums* sums, Token* best, Queue& queue) {
   const dim3 grid((unsigned)rows, (unsigned)p.parts);
-  if (p.parts > 1) LAUNCH((logprob_top_kernel<T, N, K, THREADS, true>), grid, dim3(THREADS), queue, o, logits, p.part, (int)p.parts, sums, best);
-  else LAUNCH((logprob_top_kernel<T, N, K, THREADS, false>), grid, dim3(THREADS), queue, o, logits, p.part, 1, sums, best);
+  if constexpr (THREADS * N * K >= kSmallPart) {         // (rows of several parts)
+    if (p.parts > 1) {
+      LAUNCH((logprob_top_kernel<T, N, K, THREADS, true>), grid, dim3(THREADS), queue, o, logits, p.part, (int)p.parts, sums, best);
+      return;
+    }
+  }
+  LAUNCH((logprob_top_kernel<T, N, K, THREADS, false>), grid, dim3(THREADS), queue, o, logits, p.part, 1, sums, best);
 }
 
 template <typename T>
@@ -85,22 +110,20 @@ void forward(const acc_logprob& c, const LogprobPlan& p, const LogprobOut& all, 
     Token* const best = reinterpret_cast<Token*>(ws + p.best) + (p.parts > 1 ? r * p.parts * c.top : 0);
     const T* const from = logits + r * c.logits_stride;
     if (c.top > 0) {
-      if (p.threads == 1024) top_rows<T, N, 32 / N, 1024>(p, o, from, rows, sums, best, queue);
+      if (p.threads == kWave && p.part == kTopWaveAlways) top_rows<T, 1, kTopWaveAlways / kWave, kWave>(p, o, from, rows, sums, best, queue);
+      else if (p.threads == kWave) top_rows<T, N, kTopWaveMost / kWave / N, kWave>(p, o, from, rows, sums, best, queue);
+      else if (p.threads == 1024) top_rows<T, N, 32 / N, 1024>(p, o, from, rows, sums, best, queue);
       else if (p.packs == 1) top_rows<T, N, 1, 256>(p, o, from, rows, sums, best, queue);
       else if (p.packs == 8 / N) top_rows<T, N, 8 / N, 256>(p, o, from, rows, sums, best, queue);
       else top_rows<T, N, 32 / N, 256>(p, o, from, rows, sums, best, queue);
     } else {
-      const dim3 grid((unsigned)rows, (unsigned)p.parts);
-#define STREAM(ENTROPY, PARTS) \
-  LAUNCH((logprob_stream_kernel<T, N, ENTROPY, PARTS>), grid, dim3(256), queue, o, from, p.part, (int)p.parts, sums)
-      if (o.entropy) {
-        if (p.parts > 1) STREAM(true, true);
-        else STREAM(true, false);
-      } else {
-        if (p.parts > 1) STREAM(false, true);
-        else STREAM(false, false);
-      }
-#undef STREAM
+      const auto kernel = o.entropy ? (p.parts > 1      ? logprob_stream_kernel<T, N, true, true, 256>
+                                       : p.rows_at_once ? logprob_stream_kernel<T, N, true, false, kWave>
+                                                        : logprob_stream_kernel<T, N, true, false, 256>)
+                                    : (p.parts > 1      ? logprob_stream_kernel<T, N, false, true, 256>
+                                       : p.rows_at_once ? logprob_stream_kernel<T, N, false, false, kWave>
+                                                        : logprob_stream_kernel<T, N, false, false, 256>);
+      LAUNCH(kernel, p.rows_at_once ? dim3((unsigned)up(rows, 4)) : dim3((unsigned)rows, (unsigned)p.parts), dim3(256), queue, o, from, rows, p.part, (int)p.parts, sums);
     }
     if (p.parts > 1)
       enqueue(queue, logprob_join_kernel<T>, dim3((unsigned)rows), dim3(kJoinThreads),
@@ -116,16 +139,16 @@ void backward(const acc_logprob& c, const T* logits, const void* targets, const 
   int64_t part = up(c.vocab, turn) * turn;
   while (part > turn && c.rows * up(c.vocab, part) < kGradientGroups) part = up(part / 2, turn) * turn;
   for (int64_t r = 0; r < c.rows; r += kRowsPerLaunch) {
-    const dim3 grid((unsigned)std::min(kRowsPerLaunch, c.rows - r), (unsigned)up(c.vocab, part));
+    const int64_t rows = std::min(kRowsPerLaunch, c.rows - r);
+    const bool four = short_row(c);
+    const dim3 grid((unsigned)(four ? up(rows, 4) : rows), (unsigned)up(c.vocab, part));
     const T* const from = logits + r * c.logits_stride;
     const void* const ids = dlogprob ? static_cast<const char*>(targets) + r * (c.index_bits / 8) : nullptr;
     T* const to = grad + r * c.grad_stride;
-    if (dentropy)
-      LAUNCH((logprob_backward_kernel<T, N, true>), grid, dim3(256), queue, from, ids, c.index_bits == 64, lse + r, dlogprob ? dlogprob + r : nullptr,
-             entropy + r, dentropy + r, to, c.vocab, c.logits_stride, c.grad_stride, part);
-    else
-      LAUNCH((logprob_backward_kernel<T, N, false>), grid, dim3(256), queue, from, ids, c.index_bits == 64, lse + r, dlogprob ? dlogprob + r : nullptr,
-             nullptr, nullptr, to, c.vocab, c.logits_stride, c.grad_stride, part);
+    const auto kernel = dentropy ? (four ? logprob_backward_kernel<T, N, true, kWave> : logprob_backward_kernel<T, N, true, 256>)
+                                 : (four ? logprob_backward_kernel<T, N, false, kWave> : logprob_backward_kernel<T, N, false, 256>);
+    LAUNCH(kernel, grid, dim3(256), queue, from, ids, c.index_bits == 64, lse + r, dlogprob ? dlogprob + r : nullptr, dentropy ? entropy + r : nullptr,
+           dentropy ? dentropy + r : nullptr, to, rows, c.vocab, c.logits_stride, c.grad_stride, part);
   }
 }
 
