@@ -9,6 +9,7 @@ struct ConvolutionShape {
   int64_t x_b, x_t, out_b, out_t, dx_b, dx_t;      // backward: out is grad_out
   int64_t run, runs;                               // steps of a run, runs of a sequence
   int lanes_log2;                                  // lanes that share a row
+  bool whole;                                      // packs at the ends of rows are made whole
 };
 
 // N elements of a row; FULL: all of them are there.  (Wide accesses need no alignment beyond the element's.)
@@ -27,9 +28,9 @@ __device__ __forceinline__ void row_store(T* p, const F32<N>& v, int64_t left) {
 }
 
 // What a lane has: N channels of a run of steps of a sequence.  FULL: a wave has one run, so that all but the channel lies in its scalar registers, and every
-// pack is whole: the last one of a row that is not a multiple of N starts among the channels of the one in front, whose results it makes once more, the
+// pack is whole, as it may be without: the last one of a row that is not a multiple of N starts among the channels of the one in front, whose results it makes once more, the
 // same ones.  (Single elements there cost every wave of the row's end a second path: 55 x 3025 x 455 bf16 forward 177 us, backward 276, with whole
-// packs 74 and 176.)
+// packs 74 and 176; 55 x 3025 x 125 44 and 92, with whole ones 28 and 52.)
 struct ConvolutionPlace {
   int64_t batch, run, channel, left;      // left: channels from its first one on
 };
@@ -42,7 +43,7 @@ __device__ __forceinline__ ConvolutionPlace convolution_place(const ConvolutionS
   p.run = unit - p.batch * s.runs;
   p.channel = (((int64_t)blockIdx.y << s.lanes_log2) + (lane & ((1 << s.lanes_log2) - 1))) * N;
   p.left = s.channels - p.channel;
-  if (FULL && p.left > 0 && p.left < N) {
+  if ((FULL || s.whole) && p.left > 0 && p.left < N) {
     p.channel = s.channels - N;
     p.left = N;
   }

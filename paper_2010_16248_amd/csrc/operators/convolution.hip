@@ -54,11 +54,13 @@ ConvolutionPlan plan_convolution(const acc_convolution& c, bool backward) {
   return p;
 }
 
-ConvolutionShape shape_of(const acc_convolution& c, const ConvolutionPlan& p) {
-  return {c.batch, c.steps, c.channels, c.x_batch, c.x_step, c.out_batch, c.out_step, c.grad_x_batch, c.grad_x_step, p.run, p.runs, p.lanes_log2};
+// in_place: a state is replaced, which packs that share channels would read and write.
+ConvolutionShape shape_of(const acc_convolution& c, const ConvolutionPlan& p, int pack, bool in_place) {
+  return {c.batch, c.steps, c.channels, c.x_batch, c.x_step, c.out_batch, c.out_step, c.grad_x_batch, c.grad_x_step, p.run, p.runs, p.lanes_log2,
+          c.channels >= pack && !in_place};
 }
 
-// Whether a wave has one run and every pack of N channels can be made whole.  (Not where a state is replaced: packs that share channels read and write it.)
+// Whether a wave has one run and every pack of N channels is or can be made whole.
 template <int N>
 bool full(const acc_convolution& c, const ConvolutionPlan& p, bool in_place) { return p.lanes_log2 == 6 && (c.channels % N == 0 || !in_place); }
 
@@ -82,8 +84,9 @@ void forward(const acc_convolution& c, const ConvolutionPlan& p, const void* x, 
   with_width(c.width, [&](auto width) {
     constexpr int W = decltype(width)::value;
     const dim3 grid((unsigned)p.blocks, (unsigned)p.across);
-    const auto kernel = full<N>(c, p, state && state == last) ? convolution_forward_kernel<T, N, W, true> : convolution_forward_kernel<T, N, W, false>;
-    LAUNCH(kernel, grid, dim3(256), queue, shape_of(c, p), static_cast<const T*>(x), weight, bias, state, lengths, static_cast<T*>(out), last,
+    const bool in_place = state && state == last;
+    const auto kernel = full<N>(c, p, in_place) ? convolution_forward_kernel<T, N, W, true> : convolution_forward_kernel<T, N, W, false>;
+    LAUNCH(kernel, grid, dim3(256), queue, shape_of(c, p, N, in_place), static_cast<const T*>(x), weight, bias, state, lengths, static_cast<T*>(out), last,
            c.silu);
   });
 }
@@ -96,7 +99,7 @@ void backward(const acc_convolution& c, const ConvolutionPlan& p, const void* x,
     constexpr int W = decltype(width)::value;
     const dim3 grid((unsigned)p.blocks, (unsigned)p.across);
     const auto kernel = full<N>(c, p, false) ? convolution_backward_kernel<T, N, W, true> : convolution_backward_kernel<T, N, W, false>;
-    LAUNCH(kernel, grid, dim3(256), queue, shape_of(c, p), static_cast<const T*>(x), weight, bias, state, lengths,
+    LAUNCH(kernel, grid, dim3(256), queue, shape_of(c, p, N, false), static_cast<const T*>(x), weight, bias, state, lengths,
            static_cast<const T*>(dout), dlast, static_cast<T*>(dx), dstate, parts, c.silu);
   });
 }

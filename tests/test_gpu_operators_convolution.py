@@ -126,7 +126,7 @@ def test_states_in_place_of_sequences_shorter_than_the_window():
 
 
 @pytest.mark.parametrize("kind", [F32, BF16])
-@pytest.mark.parametrize("channels", [257, 258, 513, 515, 1001, 2049])
+@pytest.mark.parametrize("channels", [3, 9, 35, 129, 257, 258, 513, 515, 1001, 2049])
 def test_rows_that_end_in_a_part_of_a_pack(channels, kind):
     """The last channels alone, in a wave of their own and beside others; a state replaced and one left as it is."""
     print(f"case ends {channels} {kind}", flush=True)
