@@ -93,7 +93,7 @@ __device__ __forceinline__ F32<N> weighed(const F32<N> (&w)[W], const F32<N>* v,
 // ---- forward ----------------------------------------------------------------------------------------------
 // A lane takes N channels through a run of steps: the inputs slide through its registers, each is read once (the first W - 1 of a run
 // twice).  Bound by memory where there is work: width 4, SiLU, 8 x 4096 x 4096 bf16 106 us, 5.1 TB/s, the rate of a large copy; 7 x 1999 x 1001 fp32,
-// width 3, ragged 19 us, 4.4 TB/s.  One token of 64 x 1344 channels: 6.2 us, nearly all of it one wait for weights, state and input.
+// width 3, ragged 17.5 us, 4.8 TB/s.  One token of 64 x 1344 channels: 6.2 us, nearly all of it one wait for weights, state and input.
 constexpr int kConvolutionAhead = 4;   // steps under way
 
 template <typename T, int N, int W, bool FULL>
@@ -164,8 +164,7 @@ __global__ __launch_bounds__(256) void convolution_forward_kernel(ConvolutionSha
 // A lane takes N channels through a run of steps and the W - 1 behind it, whose g it needs: inputs and g slide through its registers.
 // The gradients of its weights stay in registers over the run; a workgroup adds its runs' and leaves them in parts (W + 1 rows of
 // channels), which parts_join_kernel adds.  Packs of 4 channels: 8 would need twice the registers of w, dw, v and g.  Width 4, SiLU, 8 x 4096 x 4096 bf16:
-// 192 us, of them 179 with nothing else between calls, 4.2 to 4.5 TB/s; the vector units (two products a weight, and SiLU's derivative) are nearly as
-// long at work as memory.
+// 175 us with calls in a row, 4.6 TB/s: memory.
 template <typename T, int N, int W, bool FULL>
 __global__ __launch_bounds__(256) void convolution_backward_kernel(ConvolutionShape s, const T* __restrict__ x,
                                                                    const float* __restrict__ weight, const float* __restrict__ bias,

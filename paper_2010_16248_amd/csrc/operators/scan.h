@@ -466,7 +466,7 @@ __global__ __launch_bounds__(kWave * kCarryWaves) void scan_carry_kernel(ScanSha
 }
 
 // ---- forward ----------------------------------------------------------------------------------------------
-// Each wave finishes the outputs of its steps of a turn.  8 x 4096 x 2048, 16 states, bf16, ragged (0.63 of the steps): 207 us, vector units busy for 0.95
+// Each wave finishes the outputs of its steps of a turn.  8 x 4096 x 2048, 16 states, bf16, ragged (0.63 of the steps): 187 us, vector units busy for 0.95
 // of them.
 template <typename T, int NP, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave, 4) void scan_forward_kernel(
