@@ -496,8 +496,9 @@ int32_t accordion_convolution_backward(const acc_convolution* cfg, const void* x
  *              grad_delta_bias = sum of grad_delta_t, grad_h0 = e_0 G_0
  *              (the states are computed again from the inputs: nothing is kept from the forward pass)
  * a_dev is channels x states, d_dev and delta_bias_dev (NULL: zeros) channels, contiguous fp32, and so are their gradients;
- * a is finite (negative, unless states are to grow).  b and c have a row of groups x states elements per step: channels
- * [i channels / groups, (i + 1) channels / groups) take the i-th part of it.  gate_dev may be NULL, and grad_gate_dev then is.
+ * a is finite (negative, unless states are to grow; where they do, by more than the fp32 numbers hold within 256 steps, results
+ * may be NaN).  b and c have a row of groups x states elements per step: channels [i channels / groups, (i + 1) channels / groups)
+ * take the i-th part of it.  gate_dev may be NULL, and grad_gate_dev then is.
  * h0_dev (NULL: zeros), h_last_dev, grad_last_dev (NULL: zeros) and grad_h0_dev are batch x channels x states, contiguous fp32.
  * h_last_dev, grad_h0_dev, grad_d_dev and grad_delta_bias_dev may be NULL; the last two need d_dev and delta_bias_dev.
  * lengths_dev as for the recurrence: steps from a sequence's length on write zeros and leave the state as it is; what

@@ -20,7 +20,13 @@ struct ScanShape {
 typedef const float __attribute__((address_space(4))) * Shared;
 __device__ __forceinline__ Shared shared_at(const float* p) { return (Shared)(uintptr_t)p; }
 
-constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f, kMost = 3.40282347e38f;
+
+// a log2(e), finite where a is: a step of dt = 0 keeps the state.
+__device__ __forceinline__ float decay_of(float a) {
+  const float v = a * kLog2e;
+  return fabsf(v) > kMost ? copysignf(kMost, v) : v;
+}
 
 // log(1 + e^r) = max(r, 0) + log(1 + e), e = e^-|r|, and its derivative, the sigmoid of r.  log(1 + e) = 2 atanh(s), s = e / (2 + e) <= 1/3;
 // atanh(s) / s = 1 + z q(z), z = s^2, q of degree 3 with the least largest error (fitted: below 2^-27 of the whole).
@@ -122,7 +128,7 @@ __device__ __forceinline__ void load_decay(const ScanShape& s, const ScanPlace& 
 #pragma unroll
   for (int n = 0; n < NP; ++n) {
     const int at = p.part * NP + n;
-    decay[n] = at < s.states ? a[(int64_t)p.channel * s.states + at] * kLog2e : 0.f;
+    decay[n] = at < s.states ? decay_of(a[(int64_t)p.channel * s.states + at]) : 0.f;
   }
 }
 
@@ -454,7 +460,7 @@ __global__ __launch_bounds__(kWave * kCarryWaves) void scan_carry_kernel(ScanSha
   const bool back = BACKWARD && blockIdx.y >= (unsigned)s.padded;
   const int n = (int)blockIdx.y - (back ? s.padded : 0);
   const bool held = n < s.states, valid = at < s.channels;
-  const float decay = held ? a[c * s.states + n] * kLog2e : 0.f;
+  const float decay = held ? decay_of(a[c * s.states + n]) : 0.f;
   const int64_t own = (b * s.channels + c) * s.states + n, step = (int64_t)s.padded * s.channels;
   const int64_t first = (b * s.chunks * s.padded + n) * s.channels + c, last = first + (s.chunks - 1) * step;
   const float* const total = sums + b * s.chunks * s.channels + c;
@@ -609,7 +615,9 @@ __global__ __launch_bounds__(256) void scan_walk_kernel(ScanShape s, const T* __
   const int first = (threadIdx.x % L) * 4;
   if (channel >= s.channels) return;             // all lanes of a channel together
   const int64_t len = steps_of(lengths, batch, s.steps), left = s.states - first, group = channel / s.group;
-  const F32<4> decay = widen<float, 4>(load_some<4>(a + channel * s.states + first, left)) * kLog2e;
+  F32<4> decay = widen<float, 4>(load_some<4>(a + channel * s.states + first, left));
+#pragma unroll
+  for (int n = 0; n < 4; ++n) decay[n] = decay_of(decay[n]);
   const int64_t own = (batch * s.channels + channel) * s.states + first;
   F32<4> h = {};
   if (h0) h = widen<float, 4>(load_some<4>(h0 + own, left));

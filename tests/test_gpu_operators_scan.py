@@ -86,11 +86,31 @@ def test_lengths_around_turns_and_chunks(steps):
     check(make(2, steps, 10, 16, seed=steps))
 
 
+@pytest.mark.parametrize("steps", [9, 300])
+def test_decays_up_to_the_least_number(steps):
+    """States that are gone after a step, and kept where a sequence has ended."""
+    print(f"case decays {steps}", flush=True)
+    s = make(2, steps, 70, 16, lengths=[steps - 3, 0])
+    s["a"][:, ::3] = -3e38
+    s["a"][:, 1::3] = -1e-30
+    check(s)
+
+
 def test_one_chunk_of_many_waves():
     """Sequences enough to fill the chip: no chunks in the forward pass."""
     print("case wide", flush=True)
     check(make(2100, 40, 2, 2, BF16), back=False)
     check(make(130, 70, 1100, 3), back=False)
+
+
+def test_chunks_of_many_sequences_of_different_lengths():
+    """More waves than sequences of one length are cut into chunks for; the same sequences whole."""
+    print("case ragged", flush=True)
+    lengths = [(i * 977) % 2049 for i in range(260)]
+    s = make(260, 2048, 1, 33, lengths=lengths)
+    check(s, back=False)
+    s["lengths"] = None
+    check(s, back=False)
 
 
 def test_chunks_of_many_turns():
