@@ -55,7 +55,7 @@ constexpr int64_t kScanFew = 64, kScanLone = 2048, kScanWaves = 4096, kScanShort
 // 16 states (4 waves) 1 x 512 x 1536 (24 workgroups per chunk) 41, 44, 49, 79, 139; 2 x 2048 x 768 (24) 102, 87, 84, 106, 143; 4 x 1024 x 1536 (96) 166,
 // 148, 138, 138, 189; 64 x 128 x 512 (512) 117, 107, 107, 105; 8 x 4096 x 2048 (256) 1730, 1359, 1195, 1155, 1132; 4 states (1 wave) 64 x 512 x 1024 (1024)
 // 411, 354, 330, 331, 349; 64 states (8 waves) 2 x 2048 x 768 (24) 347, 274, 251, 299, 300.
-constexpr int64_t kBackwardGroups = 768, kBackwardWaves = 3072, kBackwardShortest = 16, kBackwardLongest = 256;
+constexpr int64_t kBackwardGroups = 768, kBackwardWaves = 3000, kBackwardShortest = 16, kBackwardLongest = 256;
 
 struct ScanPlan {
   bool walk = false, large = false;
