@@ -653,57 +653,38 @@ __global__ __launch_bounds__(256) void scan_walk_kernel(ScanShape s, const T* __
 
 // ---- backward ---------------------------------------------------------------------------------------------
 
-// Sums over the 64 lanes of V values a lane (V a power of two up to 32): value i ends in the lanes l with l / (64 / V) = i.  Every stage
-// halves the values a lane has: it keeps one of two, and takes the same one from the lane that keeps the other.
+// Sums over the 64 lanes of V values a lane (16 or 32), which the lanes have put into V rows of LDS, a wave's own: value i ends in the lanes l with
+// l / (64 / V) = i.  A lane reads V lanes' of one value and adds them by pairs, the lanes of a value add theirs.  (Rows of 68 numbers: 16 lanes read 16
+// pieces of different banks.)  Exchanges between the lanes' registers, half of the values less at every stage, take 35 vector instructions for 16 values where
+// this takes 19: 4 x 1024 x 1536 fp32 backward 140 us and 133, 2 x 2048 x 768 with 64 states bf16 244 and 238, 8 x 4096 x 2048 1125 either way.
+constexpr int kSumRow = kWave + 4;
 template <int V>
-__device__ __forceinline__ float lanes_sum(float (&v)[V], int l) {
-  constexpr int kWide = V;
-  int left = kWide;
-  // 32 lanes apart
-  if (left > 1) {
-    left /= 2;
+struct LanesSum {
+  static_assert(V == 16 || V == 32, "two or four lanes add up a value");
+  F32<4> part[V / 4];
+  __device__ __forceinline__ void request(const float* room, int l) {
+    const float* const from = room + l / (kWave / V) * kSumRow + l % (kWave / V) * V;
 #pragma unroll
-    for (int i = 0; i < kWide / 2; ++i) {
-      const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + kWide / 2]), false, false);
-      v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    }
+    for (int i = 0; i < V / 4; ++i) part[i] = *reinterpret_cast<const F32<4>*>(from + 4 * i);
   }
-  if (kWide >= 4) {
+  __device__ __forceinline__ float sum() {
 #pragma unroll
-    for (int i = 0; i < kWide / 4; ++i) {
-      const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + kWide / 4]), false, false);
-      v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    }
-  }
-  if (kWide >= 8) {
+    for (int left = V / 8; left > 0; left /= 2)
 #pragma unroll
-    for (int i = 0; i < kWide / 8; ++i) {
-      const float mine = l & 8 ? v[i + kWide / 8] : v[i], other = l & 8 ? v[i] : v[i + kWide / 8];
-      v[i] = mine + dpp<0x128>(other);           // 8 lanes on, within 16
-    }
-  }
-  if (kWide >= 16) {
+      for (int i = 0; i < left; ++i)
 #pragma unroll
-    for (int i = 0; i < kWide / 16; ++i) {
-      const float mine = l & 4 ? v[i + kWide / 16] : v[i], other = l & 4 ? v[i] : v[i + kWide / 16];
-      v[i] = mine + dpp<0x141>(other);           // mirrored within 8
-    }
-  } else {
-    v[0] += dpp<0x141>(v[0]);
+        for (int k = 0; k < 4; ++k) part[i][k] += part[i + left][k];
+    float s = (part[0][0] + part[0][1]) + (part[0][2] + part[0][3]);
+    s += dpp<0xB1>(s);
+    return V == 16 ? s + dpp<0x4E>(s) : s;
   }
-  if (kWide >= 32) {
-    const float mine = l & 2 ? v[1] : v[0], other = l & 2 ? v[0] : v[1];
-    v[0] = mine + dpp<0x4E>(other);
-  } else {
-    v[0] += dpp<0x4E>(v[0]);
-  }
-  return v[0] + dpp<0xB1>(v[0]);
-}
+};
 
 // A chunk, from its end: the states of kScanAhead steps at a time are computed from what scan_ends_kernel left in front of them and from the state
 // in front of the chunk, kept in registers, and walked back.  (All states of a chunk in LDS would be 32 KB for 8 steps of 64 channels x 16 states.)  Each wave
-// finishes the gradients of its steps of a turn.  8 x 4096 x 2048, 16 states, bf16: 858 us, vector units busy for 0.94 of them; 977 and 0.81 with a
-// turn's inputs and marks requested where it starts and not a turn ahead.
+// finishes the gradients of its steps of a turn.  8 x 4096 x 2048, 16 states, bf16: 820 us, vector units busy for 0.84 of them, at 2.1 GHz and less
+// when it runs for long (2.4 where there is less to do at once): what it draws bounds it too.  With a turn's inputs and marks requested where it starts, and not a turn
+// ahead, 977 for 858.
 // parts: of a chunk, states + 2 rows of channels (grad_a, grad_d, grad_delta_bias); shared_parts: of a block of channels and a step, the
 // sums of grad_b and grad_c over the block.
 template <typename T, int NP, int WAVES>
@@ -716,7 +697,9 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
   constexpr int U = kScanAhead, SHARE = U / WAVES;    // steps of a turn that a wave finishes
   constexpr int row_size = 2 * NP * WAVES;
   const ScanPlace p = scan_place(s, lengths);
-  __shared__ float held[3 * U * kWave * (1 + WAVES)];
+  constexpr int kRoom = 4 * NP * kSumRow;
+  __shared__ alignas(16) float held[3 * U * kWave * (1 + WAVES) + WAVES * kRoom];
+  float* const room = held + 3 * U * kWave * (1 + WAVES) + p.part * kRoom;
   float* const common = held + p.lane;              // dt, u, dy of a turn's steps
   float* const add = common + 3 * U * kWave;        // what the waves' states contribute to a turn's steps
   float decay[NP], g[NP], da[NP];
@@ -854,17 +837,24 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
         for (int i = 0; i < 4; ++i) hs[j + 1][4 * q + i] = h4[i];
       }
     }
-    float v[4 * NP];       // what two steps give to grad_b and grad_c
+    LanesSum<4 * NP> behind;       // what the two steps behind gave to grad_b and grad_c
 #pragma unroll
     for (int first = U - Both::kCount; first >= 0; first -= Both::kCount) {
       await_shared();
       const Both group = both;
-      if (first > 0) both.load(at + (first - Both::kCount) * row_size);
       stop();
+      // (LDS and scalar loads share a counter, and the latter come in any order: a wait for sums from LDS would be one for them)
+      auto ahead = [&](int k) {
+        if (k == Both::kCount - 1 && first > 0) both.load(at + (first - Both::kCount) * row_size);
+        stop();
+      };
 #pragma unroll
       for (int k = Both::kCount - 1; k >= 0; --k) {
         const int j = first + k;
-        float* const pair = v + (j & 1 ? 0 : 2 * NP);
+        float* const pair = room + (j & 1 ? 0 : 2 * NP) * kSumRow + p.lane;
+        const bool sums = j % 2 == 1 && j < U - 1;
+        if (sums) behind.request(room, p.lane);
+        else ahead(k);
         float y = 0.f, along = 0.f, step = 0.f;
         float totals[NP];
 #pragma unroll
@@ -880,8 +870,8 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
         for (int n = 0; n < NP; ++n) {
           const float total = totals[n];
           y = fmaf(group.row[k].c[n], hs[j + 1][n], y);
-          pair[n] = total * u[j];
-          pair[NP + n] = dy[j] * hs[j + 1][n];
+          pair[n * kSumRow] = total * u[j];
+          pair[(NP + n) * kSumRow] = dy[j] * hs[j + 1][n];
           along = fmaf(total, group.row[k].b[n], along);
           g[n] = total * e[j][n];
           const float back = g[n] * hs[j][n];
@@ -892,10 +882,15 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
         to[0] = y;
         to[kWave] = along;
         to[2 * kWave] = step;
-        if (j % 2 == 0) shared_to[(t + j) * row_size] = lanes_sum<4 * NP>(v, p.lane);
+        if (sums) {
+          shared_to[(t + j + 1) * row_size] = behind.sum();
+          ahead(k);
+        }
         stop();
       }
     }
+    behind.request(room, p.lane);
+    shared_to[t * row_size] = behind.sum();
     if (WAVES > 1) __syncthreads();
     const LaneOf done(p);
 #pragma unroll
