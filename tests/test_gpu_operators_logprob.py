@@ -67,6 +67,22 @@ def test_rows_and_vocabularies(rows, vocab, top, kind):
 
 
 @pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("rows,vocab,top", [(2050, 1500, 5), (2049, 2048, 20), (2051, 513, 1), (2051, 67, 64), (2050, 1024, 0), (2050, 1025, 0), (2051, 2048, 0), (3, 33, 0)])
+def test_many_short_rows(rows, vocab, top, kind):
+    """Rows that are a wave's, in whole and in started workgroups, forward and backward, also in place."""
+    print(f"case short {rows} {vocab} {top} {kind}", flush=True)
+    logits, ids = make(rows, vocab, kind)
+    r = check_forward(logits, ids, top)
+    g = torch.randn(rows, generator=torch.Generator().manual_seed(5)).to(DEV)
+    for kw in (dict(), dict(entropy=r["entropy"], grad_entropy=g.flip(0).contiguous())):
+        got = backward(logits, ids, r["lse"], g, **kw)
+        ref, off = M.logprob_gradient(logits, ids, r["lse"], g, kw.get("entropy"), kw.get("grad_entropy"))
+        assert_within(got, ref, off, "gradient")
+        over = logits.clone()
+        assert torch.equal(backward(over, ids, r["lse"], g, out=over, **kw), got)
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
 @pytest.mark.parametrize("vocab", [30, 5000, 40000])
 def test_ties_go_to_the_lowest_index(vocab, kind):
     """Few different values, and one alone: more equal logits than any list holds."""
@@ -112,7 +128,7 @@ def test_masks(top, vocab, kind):
 
 
 @pytest.mark.parametrize("kind", [F32, BF16])
-@pytest.mark.parametrize("vocab,top", [(4000, 20), (8192, 64), (32768, 20), (50001, 1), (70000, 64), (262145, 20)])
+@pytest.mark.parametrize("vocab,top", [(300, 20), (512, 64), (513, 40), (1000, 64), (2048, 64), (4000, 20), (8192, 64), (32768, 20), (50001, 1), (70000, 64), (262145, 20)])
 def test_rows_that_fill_the_list(vocab, top, kind):
     """Masked but for as many tokens as are wanted, one fewer, one more and a few hundred; in order; few that are numbers at all; more large logits in one
     place than the list holds."""
