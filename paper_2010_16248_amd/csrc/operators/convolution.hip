@@ -134,7 +134,7 @@ int32_t accordion_convolution_forward(const acc_convolution* c, const void* x_de
 
 int32_t accordion_convolution_workspace_bytes(const acc_convolution* c, size_t* out_bytes) {
   REQUIRE(out_bytes, "out_bytes is NULL");
-  if (const int32_t rc = check_convolution(c, false)) return rc;
+  if (const int32_t rc = check_convolution(c, true)) return rc;       // (grad_out is only read: its rows may share memory)
   *out_bytes = (size_t)plan_convolution(*c, true).bytes;
   return ACC_OK;
 }
