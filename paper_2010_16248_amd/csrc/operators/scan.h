@@ -659,14 +659,23 @@ __global__ __launch_bounds__(256) void scan_walk_kernel(ScanShape s, const T* __
 // pieces of different banks.)  Exchanges between the lanes' registers, half of the values less at every stage, take 35 vector instructions for 16 values where
 // this takes 19: 4 x 1024 x 1536 fp32 backward 140 us and 133, 2 x 2048 x 768 with 64 states bf16 244 and 238, 8 x 4096 x 2048 1125 either way.
 constexpr int kSumRow = kWave + 4;
+// What the wave's lanes have put into LDS is there for its other lanes, and what these have read may be overwritten.  (A wave's accesses to LDS keep their order
+// by themselves; this keeps the compiler from changing it, and is no instruction.)
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
 template <int V>
 struct LanesSum {
   static_assert(V == 16 || V == 32, "two or four lanes add up a value");
   F32<4> part[V / 4];
   __device__ __forceinline__ void request(const float* room, int l) {
     const float* const from = room + l / (kWave / V) * kSumRow + l % (kWave / V) * V;
+    wave_fence();
 #pragma unroll
     for (int i = 0; i < V / 4; ++i) part[i] = *reinterpret_cast<const F32<4>*>(from + 4 * i);
+    wave_fence();
   }
   __device__ __forceinline__ float sum() {
 #pragma unroll
