@@ -406,6 +406,13 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void scan_ends_kernel(ScanShape s
 constexpr int kCarryAhead = 8;
 constexpr int kCarryWaves = 16;
 
+// 2^z h + v.  Over many steps of a growing state the power may be beyond fp32 where its product with h is not: it is applied in two halves, and zero stays
+// zero.  (A z that is no number leaves none.)
+__device__ __forceinline__ float carried(float z, float h, float v) {
+  const float half = __builtin_amdgcn_exp2f(0.5f * z);
+  return h == 0.f && fabsf(z) < INFINITY ? v : fmaf(h * half, half, v);
+}
+
 // values: of a run, in its order of walking, `step` apart, and so the sums `sum_step`.  Leaves the state in front of each in its place.
 __device__ __forceinline__ void carry_runs(float* values, int64_t step, const float* total, int64_t sum_step, int count, float decay, float h,
                                            bool valid, float (*fold)[2][kWave]) {
@@ -424,7 +431,7 @@ __device__ __forceinline__ void carry_runs(float* values, int64_t step, const fl
 #pragma unroll
       for (int j = 0; j < kCarryAhead; ++j)
         if (k + j < hi) {
-          end = fmaf(__builtin_amdgcn_exp2f(d[j] * decay), end, v[j]);
+          end = carried(d[j] * decay, end, v[j]);
           sum += d[j];
         }
     }
@@ -432,7 +439,7 @@ __device__ __forceinline__ void carry_runs(float* values, int64_t step, const fl
     fold[wave][0][lane] = end;
     fold[wave][1][lane] = sum;
     __syncthreads();
-    for (int w = 0; w < wave; ++w) h = fmaf(__builtin_amdgcn_exp2f(fold[w][1][lane] * decay), h, fold[w][0][lane]);
+    for (int w = 0; w < wave; ++w) h = carried(fold[w][1][lane] * decay, h, fold[w][0][lane]);
   }
   for (int k = lo; k < hi; k += kCarryAhead) {
     float v[kCarryAhead], d[kCarryAhead];
@@ -446,7 +453,7 @@ __device__ __forceinline__ void carry_runs(float* values, int64_t step, const fl
     for (int j = 0; j < kCarryAhead; ++j)
       if (k + j < hi) {
         if (valid) values[(k + j) * step] = h;
-        h = fmaf(__builtin_amdgcn_exp2f(d[j] * decay), h, v[j]);
+        h = carried(d[j] * decay, h, v[j]);
       }
   }
 }
