@@ -165,6 +165,11 @@ void forward_ends(const acc_scan& c, const ScanPlan& p, const ScanIn& in, char* 
          nullptr, at(p.ends), nullptr, at(p.sums), nullptr);
 }
 
+template <typename T, int NP, int WAVES>
+auto forward_kernel(const acc_scan& c, const ScanPlan& p) {
+  return c.states == p.padded ? scan_forward_kernel<T, NP, WAVES, true> : scan_forward_kernel<T, NP, WAVES, false>;
+}
+
 template <typename T>
 void forward(const acc_scan& c, const ScanPlan& p, const ScanIn& in, void* out, float* h_last, char* ws, Queue& queue) {
   if (p.walk) {
@@ -186,11 +191,11 @@ void forward(const acc_scan& c, const ScanPlan& p, const ScanIn& in, void* out, 
     LAUNCH(scan_carry_kernel<false>, carry_grid(c, p, false), carry_threads(c, p), queue, shape_of(c, p), in.a, in.h0, nullptr, at(p.ends),
            nullptr, at(p.sums));
   }
-  const auto kernel = p.padded == 4    ? scan_forward_kernel<T, 4, 1>
-                      : p.padded == 8  ? scan_forward_kernel<T, 4, 2>
-                      : p.padded == 16 ? scan_forward_kernel<T, 4, 4>
-                      : p.padded == 32 ? scan_forward_kernel<T, 4, 8>
-                                       : scan_forward_kernel<T, 8, 8>;
+  const auto kernel = p.padded == 4    ? forward_kernel<T, 4, 1>(c, p)
+                      : p.padded == 8  ? forward_kernel<T, 4, 2>(c, p)
+                      : p.padded == 16 ? forward_kernel<T, 4, 4>(c, p)
+                      : p.padded == 32 ? forward_kernel<T, 4, 8>(c, p)
+                                       : forward_kernel<T, 8, 8>(c, p);
   LAUNCH(kernel, dim3((unsigned)(c.groups * p.blocks), (unsigned)p.chunks, (unsigned)c.batch), dim3((unsigned)(kWave * p.split)), queue,
          shape_of(c, p), as<T>(in.x), as<T>(in.delta), in.a, at(p.packed), in.d, as<T>(in.gate), in.delta_bias, in.lengths, in.h0, at(p.ends),
          static_cast<T*>(out), h_last);
@@ -218,7 +223,8 @@ void backward_ends(const acc_scan& c, const ScanPlan& p, const ScanIn& in, const
 template <typename T, int NP, int WAVES>
 void backward_chunks(const acc_scan& c, const ScanPlan& p, const ScanIn& in, const ScanGradients& g, char* ws, Queue& queue) {
   auto at = [&](int64_t offset) { return reinterpret_cast<float*>(ws + offset); };
-  LAUNCH((scan_backward_kernel<T, NP, WAVES>), dim3((unsigned)(c.groups * p.blocks), (unsigned)p.chunks, (unsigned)c.batch), dim3(kWave * WAVES),
+  const auto kernel = c.states == p.padded ? scan_backward_kernel<T, NP, WAVES, true> : scan_backward_kernel<T, NP, WAVES, false>;
+  LAUNCH(kernel, dim3((unsigned)(c.groups * p.blocks), (unsigned)p.chunks, (unsigned)c.batch), dim3(kWave * WAVES),
          queue, shape_of(c, p), as<T>(in.x), as<T>(in.delta), in.a, at(p.packed), in.d, as<T>(in.gate), in.delta_bias, in.lengths, as<T>(g.out),
          in.h0, g.last, at(p.ends), at(p.starts), at(p.marks), static_cast<T*>(g.x), static_cast<T*>(g.delta), static_cast<T*>(g.gate), g.h0,
          at(p.parts), at(p.shared_parts));
