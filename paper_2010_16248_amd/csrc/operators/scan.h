@@ -761,6 +761,13 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
   float dskip = 0.f, dshift = 0.f;
 #pragma unroll
   for (int n = 0; n < NP; ++n) da[n] = 0.f;
+  // Where a lane puts what it adds to sums over channels.  Lanes without a channel put it behind the row, and zeros into their places: beside infinity their
+  // products are not zero.
+  const int column = p.valid ? p.lane : kWave;
+  if (!p.valid) {
+#pragma unroll
+    for (int i = 0; i < 4 * NP; ++i) room[i * kSumRow + p.lane] = 0.f;
+  }
   // where a lane's sum of two steps goes: the later one's come first
   const int sum_of = p.lane / (kWave / (4 * NP)), value = sum_of % (2 * NP);
   float* const shared_to = shared_parts + (p.batch * s.groups * s.blocks + p.block) * s.rows * row_size + (sum_of < 2 * NP ? row_size : 0) +
@@ -833,11 +840,11 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
     }
 #pragma unroll
     for (int k = 0; k < SHARE; ++k) {
-      const bool in = p.part * SHARE + k <= last, on = in && p.valid;
+      const bool in = p.part * SHARE + k <= last;
       float* const to = common + (p.part * SHARE + k) * 3 * kWave;
       to[0] = in ? own_dt[k] : 0.f;
-      to[kWave] = on ? own_dt[k] * (float)xv[k] : 0.f;
-      to[2 * kWave] = on ? own_dy[k] : 0.f;
+      to[kWave] = in ? own_dt[k] * (float)xv[k] : 0.f;
+      to[2 * kWave] = in ? own_dy[k] : 0.f;
     }
     if (WAVES > 1) __syncthreads();
     float hs[U + 1][NP], e[U][NP], dt[U], u[U], dy[U];
@@ -890,7 +897,7 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
 #pragma unroll
         for (int k = Both::kCount - 1; k >= 0; --k) {
           const int j = first + k;
-          float* const pair = room + (j & 1 ? 0 : 2 * NP) * kSumRow + p.lane;
+          float* const pair = room + (j & 1 ? 0 : 2 * NP) * kSumRow + column;
           const bool sums = j % 2 == 1 && j < U - 1;
           if (sums) behind.request(room, p.lane);
           else ahead(k);
