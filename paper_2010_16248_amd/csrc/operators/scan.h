@@ -218,6 +218,14 @@ __device__ __forceinline__ void pin(float (&v)[N]) {
   for (int n = 0; n < N; ++n) asm volatile("" : "+v"(v[n]));
 }
 __device__ __forceinline__ void pin(float& v) { asm volatile("" : "+v"(v)); }
+// Whether a lane of the wave has a NaN among some values (or infinities of both signs).
+template <int N>
+__device__ __forceinline__ bool any_nan(const float (&v)[N]) {
+  float sum = v[0];
+#pragma unroll
+  for (int n = 1; n < N; ++n) sum += v[n];
+  return __any(sum != sum);
+}
 template <int NP, int WAVES, bool B>
 struct SharedGroup {
   static constexpr int kRow = 2 * NP * WAVES;
@@ -772,6 +780,7 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
   const int sum_of = p.lane / (kWave / (4 * NP)), value = sum_of % (2 * NP);
   float* const shared_to = shared_parts + (p.batch * s.groups * s.blocks + p.block) * s.rows * row_size + (sum_of < 2 * NP ? row_size : 0) +
                            p.part * NP + (value < NP ? value : NP * WAVES + value - NP);
+  float* const part_to = parts + (p.batch * s.chunks + p.chunk) * (s.states + 2) * s.channels;
   float start[NP];                                  // the state in front of the chunk
   if (s.chunks > 1) load_slots<NP, WAVES>(s, p, ends, start);
   else load_states<NP>(s, p, h0, start);
@@ -938,6 +947,14 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
       behind.request(room, p.lane);
       shared_to[t * row_size] = behind.sum();
     });
+    if (last < U - 1) {               // (the turn in which the sequence ends)
+      const LaneOf lane(p);
+#pragma unroll
+      for (int n = 0; n < NP; ++n) {
+        if (p.valid && n < own) lane.of(part_to + (p.part * NP + n) * s.channels) = da[n];
+        da[n] = 0.f;
+      }
+    }
     if (WAVES > 1) __syncthreads();
     const LaneOf done(p);
 #pragma unroll
@@ -962,8 +979,54 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
     }
     if (WAVES > 1) __syncthreads();      // common and add are written again
   }
-  float* const to = parts + (p.batch * s.chunks + p.chunk) * (s.states + 2) * s.channels;
+  float* const to = part_to;
   const LaneOf lane(p);
+  // What the turn in which the sequence ends gave to grad_a: there steps beyond the sequence have products of zero with its last state and that one's gradient.
+  // Where these are infinite it is worked out again, without them.  (A branch around every step of every turn instead: 8 x 4096 x 2048 bf16 1170 us for 1140.)
+  if ((p.end - p.from) % U != 0 && p.end > p.from) {
+    float ends_with[NP];
+#pragma unroll
+    for (int n = 0; n < NP; ++n) ends_with[n] = n < own ? lane.of(part_to + (p.part * NP + n) * s.channels) : 0.f;
+    if (any_nan(ends_with)) {
+      const int64_t t = p.from + (turns - 1) * U;
+      float back[NP];
+      if (s.chunks > 1) load_slots<NP, WAVES>(s, p, starts, back);
+      else load_states<NP>(s, p, dlast, back);
+#pragma unroll
+      for (int n = 0; n < NP; ++n) ends_with[n] = 0.f;
+      for (int64_t j = p.end - 1; j >= t; --j) {
+        float front[NP], dt_of = 0.f;
+#pragma unroll
+        for (int n = 0; n < NP; ++n) front[n] = start[n];
+        if (turns > 1) {
+          const float* const mark_at = marks_of<NP, WAVES>(s, p, marks, t);
+          const float passed = lane.of(mark_at + (WAVES - p.part) * NP * s.channels);
+#pragma unroll
+          for (int n = 0; n < NP; ++n) front[n] = fmaf(__builtin_amdgcn_exp2f(passed * decay[n]), start[n], lane.of(mark_at + n * s.channels));
+        }
+        for (int64_t k = t; k <= j; ++k) {
+          const float raw = (float)lane.of(ds + k * s.delta_t) + shift;
+          dt_of = s.softplus ? softplus(raw).value : raw;
+          const float u = dt_of * (float)lane.of(xs + k * s.x_t);
+#pragma unroll
+          for (int n = 0; n < NP; ++n)
+            if (k < j) front[n] = fmaf(__builtin_amdgcn_exp2f(dt_of * decay[n]), front[n], held_rows[k * row_size + n] * u);
+        }
+        float dy = (float)lane.of(os + j * s.out_t);
+        if (gs) {
+          const float gt = (float)lane.of(gs + j * s.gate_t);
+          dy *= gt * sigmoid(gt).a;
+        }
+#pragma unroll
+        for (int n = 0; n < NP; ++n) {
+          back[n] = fmaf(held_rows[j * row_size + NP * WAVES + n], dy, back[n]) * __builtin_amdgcn_exp2f(dt_of * decay[n]);
+          ends_with[n] = fmaf(back[n] * front[n], dt_of, ends_with[n]);
+        }
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NP; ++n) da[n] += ends_with[n];
+  }
   if (p.valid) {
 #pragma unroll
     for (int n = 0; n < NP; ++n) {

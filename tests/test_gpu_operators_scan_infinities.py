@@ -45,7 +45,7 @@ def check(s, back=True):
 
 
 STATES = [(1, F32), (3, BF16), (5, F32), (16, F32), (16, BF16), (20, BF16), (40, F32)]
-SHAPES = [(8, 64), (16, 64), (40, 64), (8, 70), (40, 70)]      # steps, channels
+SHAPES = [(1, 70), (5, 70), (8, 64), (16, 64), (40, 64), (8, 70), (40, 70), (700, 70)]      # steps, channels
 
 
 @pytest.mark.parametrize("states,kind", STATES)
