@@ -505,6 +505,8 @@ int32_t accordion_convolution_backward(const acc_convolution* cfg, const void* x
  * their inputs hold plays no role.  steps = 1 is the serving form: one token, the state in h0 and h_last (which may be the same buffer
  * then, and for any number of steps).
  * exp(dt a) below the normal fp32 numbers counts as zero, products and states below them may.
+ * What is infinite among inputs, states and gradients makes infinite what the formulas make infinite of it, however many steps lie between; only through
+ * a step whose exp(dt a) counts as zero an infinite state, or gradient of one, may be infinite or NaN.
  * More than 16 steps, and backward: batch x groups x steps x states, filled up to 4, 8, 16, 32 or 64, below 1.5e9. */
 typedef struct acc_scan {
   int64_t batch;                 /* [0, 65535] */

@@ -30,6 +30,13 @@ __device__ __forceinline__ float decay_of(float a) {
   return fabsf(v) > kMost ? copysignf(kMost, v) : v;
 }
 
+// 2^z h + v, for a power over many steps.  It may be beyond fp32 where its product with h is not: it is applied in two halves.  Zero stays zero, and infinity
+// infinite, through steps whose powers are numbers above zero, as theirs all are.  (A z that is no number leaves none.)
+__device__ __forceinline__ float carried(float z, float h, float v) {
+  const float half = __builtin_amdgcn_exp2f(0.5f * z);
+  return h + h == h && fabsf(z) < INFINITY ? h + v : fmaf(h * half, half, v);
+}
+
 // log(1 + e^r) = max(r, 0) + log(1 + e), e = e^-|r|, and its derivative, the sigmoid of r.  log(1 + e) = 2 atanh(s), s = e / (2 + e) <= 1/3;
 // atanh(s) / s = 1 + z q(z), z = s^2, q of degree 3 with the least largest error (fitted: below 2^-27 of the whole).
 struct Softplus {
@@ -417,6 +424,25 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void scan_ends_kernel(ScanShape s
       }
     }
   }
+  // (an infinite gradient may have met a power that the steps in front of it have taken below fp32: once more, power and gradient as they are carried)
+  if (BACKWARD && any_nan(g)) {
+    const float* row = bc + rows_of<NP, WAVES>(s, p) + p.from * kRow + NP * WAVES;
+    const LaneOf lane(p);
+    float passed = 0.f;
+#pragma unroll
+    for (int n = 0; n < NP; ++n) g[n] = 0.f;
+    for (int64_t t = p.from; t < p.end; ++t, row += kRow) {
+      const float raw = (float)lane.of(ds + t * s.delta_t) + shift;
+      float dy = (float)lane.of(os + t * s.out_t);
+      if (gs) {
+        const float gt = (float)lane.of(gs + t * s.gate_t);
+        dy *= gt * sigmoid(gt).a;
+      }
+      passed += s.softplus ? softplus(raw).value : raw;
+#pragma unroll
+      for (int n = 0; n < NP; ++n) g[n] = carried(passed * decay[n], row[n] * dy, g[n]);
+    }
+  }
   store_slots<NP, WAVES>(s, p, ends, h);
   if (BACKWARD) store_slots<NP, WAVES>(s, p, starts, g);
   if (p.valid && p.part == 0) sums[(p.batch * s.chunks + p.chunk) * s.channels + p.channel] = sum;
@@ -428,13 +454,6 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void scan_ends_kernel(ScanShape s
 // for 67 MB.
 constexpr int kCarryAhead = 8;
 constexpr int kCarryWaves = 16;
-
-// 2^z h + v.  Over many steps of a growing state the power may be beyond fp32 where its product with h is not: it is applied in two halves, and zero stays
-// zero.  (A z that is no number leaves none.)
-__device__ __forceinline__ float carried(float z, float h, float v) {
-  const float half = __builtin_amdgcn_exp2f(0.5f * z);
-  return h == 0.f && fabsf(z) < INFINITY ? v : fmaf(h * half, half, v);
-}
 
 // values: of a run, in its order of walking, `step` apart, and so the sums `sum_step`.  Leaves the state in front of each in its place.
 __device__ __forceinline__ void carry_runs(float* values, int64_t step, const float* total, int64_t sum_step, int count, float decay, float h,
@@ -860,6 +879,11 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
 #pragma unroll
     for (int n = 0; n < NP; ++n) hs[0][n] = i > 0 ? fmaf(__builtin_amdgcn_exp2f(mark_sum * decay[n]), start[n], mark[n]) : start[n];
     pin(hs[0]);
+    if (i > 0 && any_nan(hs[0])) {                  // (infinity and zero may have met)
+#pragma unroll
+      for (int n = 0; n < NP; ++n) hs[0][n] = carried(mark_sum * decay[n], start[n], mark[n]);
+      pin(hs[0]);
+    }
     if (i > 0) request(i - 1);
 #pragma unroll
     for (int j = 0; j < U; ++j) {
@@ -1002,7 +1026,7 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
           const float* const mark_at = marks_of<NP, WAVES>(s, p, marks, t);
           const float passed = lane.of(mark_at + (WAVES - p.part) * NP * s.channels);
 #pragma unroll
-          for (int n = 0; n < NP; ++n) front[n] = fmaf(__builtin_amdgcn_exp2f(passed * decay[n]), start[n], lane.of(mark_at + n * s.channels));
+          for (int n = 0; n < NP; ++n) front[n] = carried(passed * decay[n], start[n], lane.of(mark_at + n * s.channels));
         }
         for (int64_t k = t; k <= j; ++k) {
           const float raw = (float)lane.of(ds + k * s.delta_t) + shift;

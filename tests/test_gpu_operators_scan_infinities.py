@@ -65,6 +65,42 @@ def test_infinite_inputs(steps, channels, states, kind):
     assert np.isposinf(ref.out[1, steps // 3:, far]).all() and np.isposinf(refs["x"][1, steps // 3, far]) and np.isfinite(refs["x"]).sum() == refs["x"].size - 1
 
 
+# fall: a chunk's steps take a state below what fp32 holds, one step does not
+@pytest.mark.parametrize("states,kind", STATES)
+@pytest.mark.parametrize("steps,fall", [(1, 5.0), (16, 20.0), (40, 0.5), (40, 20.0), (100, 20.0), (700, 0.5), (700, 20.0)])
+def test_infinite_states_stay_infinite(steps, fall, states, kind):
+    print(f"case states {steps} {fall} {states} {kind}", flush=True)
+    s = positive(3, steps, 70, states, kind, fall=fall)
+    s["h0"][0, 5] = INF
+    s["h0"][1, 69, states - 1] = INF
+    ref, refs = check(s)
+    assert np.isposinf(ref.out[0, :, 5]).all() and np.isposinf(ref.out[1, :, 69]).all() and np.isposinf(refs["a"][69, states - 1])
+
+
+@pytest.mark.parametrize("states,kind", STATES)
+@pytest.mark.parametrize("steps,fall", [(1, 5.0), (8, 20.0), (16, 20.0), (40, 0.5), (40, 20.0), (700, 0.5), (700, 20.0)])
+def test_infinite_gradients_stay_infinite(steps, fall, states, kind):
+    print(f"case gradients {steps} {fall} {states} {kind}", flush=True)
+    s = positive(3, steps, 70, states, kind, fall=fall)
+    s["dlast"][0, 69] = INF
+    s["dout"][1, steps // 2, 4] = INF
+    s["dout"][2, steps - 1, 69] = INF
+    _, refs = check(s)
+    assert np.isposinf(refs["h0"][0, 69]).all() and np.isposinf(refs["x"][1, :steps // 2 + 1, 4]).all() and np.isposinf(refs["x"][2, :, 69]).all()
+
+
+def test_infinite_states_by_many_waves_and_by_lengths():
+    """Chunks of the longest kind, and beside the infinite sequences some that end before them.  (The infinite ones are whole: the definition's sums have zeros behind
+    a sequence's end, and 64 bits make NaN of these and infinity too.)"""
+    print("case many", flush=True)
+    s = positive(400, 523, 66, 3, fall=1.0, lengths=[523 - i % 2 * i for i in range(400)])
+    s["x"][4, 100, 65] = INF
+    s["h0"][6, 2] = INF
+    s["dout"][8, 300, 5] = INF
+    s["dlast"][10, 65, 1] = INF
+    check(s)
+
+
 @pytest.mark.parametrize("states", [1, 5, 16, 20])
 @pytest.mark.parametrize("steps", [16, 40])
 def test_token_by_token_is_the_whole(steps, states):
