@@ -91,8 +91,9 @@ class Convolution(torch.autograd.Function):
     @staticmethod
     def backward(ctx, grad, _):
         x, weight, bias, state = ctx.saved_tensors
+        grad = grad.contiguous()
         dx, dw, db = torch.empty_like(grad), torch.empty_like(weight), torch.empty_like(bias)
-        B.convolution_backward(x, weight, grad.contiguous(), dx, dw, bias=bias, grad_bias=db, state=state, silu=True)
+        B.convolution_backward(x, weight, grad, dx, dw, bias=bias, grad_bias=db, state=state, silu=True)
         return dx, dw, db, None
 
 
