@@ -61,7 +61,8 @@ __device__ __forceinline__ Softplus softplus(float r) {
 // of kScanAhead steps.
 constexpr int kScanAhead = 8;    // steps of a turn: under way together
 
-// A lane makes four numbers of a row.  65536 x 32 fp32: 5.4 us, of which a launch that does little takes 3.  (All counts are below 2^32: divisions of 64 bits took more than half of the time.)
+// A lane makes four numbers of a row.  65536 x 32 fp32: 5.4 us, of which a launch that does little takes 3.  (All counts are below 2^32: divisions
+// of 64 bits took more than half of the time.)
 template <typename T>
 __global__ __launch_bounds__(256) void scan_pack_kernel(const T* __restrict__ b, const T* __restrict__ c, int64_t b_b, int64_t b_t,
                                                         int64_t c_b, int64_t c_t, unsigned all, int64_t steps, unsigned rows, unsigned groups,
@@ -208,9 +209,10 @@ template <int NP, int WAVES>
 __device__ __forceinline__ Shared shared_rows(const ScanShape& s, const ScanPlace& p, const float* bc) {
   return shared_at(bc) + rows_of<NP, WAVES>(s, p);
 }
-// What products along the states take comes through scalar registers.  Rows are requested in groups of as many as 16 of them hold (at least one), a group ahead.  Scalar loads return in any order, so a wait for one is a
-// wait for all: a group is awaited before the next one is requested, which the compiler's own waits, at first use, would not do.  The stops keep the
-// scheduler from gathering more rows than the scalar registers hold.
+// What products along the states take comes through scalar registers.  Rows are requested in groups of as many as 16 of them hold (at least
+// one), a group ahead.  Scalar loads return in any order, so a wait for one is a wait for all: a group is awaited before the next one is
+// requested, which the compiler's own waits, at first use, would not do.  The stops keep the scheduler from gathering more rows than the scalar
+// registers hold.
 __device__ __forceinline__ void stop() { __builtin_amdgcn_sched_barrier(0); }
 __device__ __forceinline__ void await_shared() {
   stop();
@@ -225,13 +227,13 @@ __device__ __forceinline__ void pin(float (&v)[N]) {
   for (int n = 0; n < N; ++n) asm volatile("" : "+v"(v[n]));
 }
 __device__ __forceinline__ void pin(float& v) { asm volatile("" : "+v"(v)); }
-// Whether a lane of the wave has a NaN among some values (or infinities of both signs).
+// Whether there is a NaN among some values (or infinities of both signs).
 template <int N>
-__device__ __forceinline__ bool any_nan(const float (&v)[N]) {
+__device__ __forceinline__ bool has_nan(const float (&v)[N]) {
   float sum = v[0];
 #pragma unroll
   for (int n = 1; n < N; ++n) sum += v[n];
-  return __any(sum != sum);
+  return sum != sum;
 }
 template <int NP, int WAVES, bool B>
 struct SharedGroup {
@@ -425,7 +427,7 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void scan_ends_kernel(ScanShape s
     }
   }
   // (an infinite gradient may have met a power that the steps in front of it have taken below fp32: once more, power and gradient as they are carried)
-  if (BACKWARD && any_nan(g)) {
+  if (BACKWARD && has_nan(g)) {
     const float* row = bc + rows_of<NP, WAVES>(s, p) + p.from * kRow + NP * WAVES;
     const LaneOf lane(p);
     float passed = 0.f;
@@ -450,16 +452,44 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void scan_ends_kernel(ScanShape s
 
 // The state in front of every chunk, in place of the one behind it, and the gradient of the state behind every chunk, in place of that in front.
 // A lane has one state of one channel; the waves of a workgroup have runs of consecutive chunks.  Each folds its run, takes what comes out
-// of those in front, and walks its run once more.  512 chunks of 672 channels x 16 states: 17.5 us for 70 MB; 16 chunks of 8 x 2048 x 16, both ways: 18 us
+// of those in front, and walks its run once more.  512 chunks of 672 channels x 16 states: 18.6 us for 70 MB; 16 chunks of 8 x 2048 x 16, both ways: 18 us
 // for 67 MB.
 constexpr int kCarryAhead = 8;
 constexpr int kCarryWaves = 16;
 
-// values: of a run, in its order of walking, `step` apart, and so the sums `sum_step`.  Leaves the state in front of each in its place.
+// The state behind `count` chunks (all kCarryAhead at most), of which v are the states behind each from zero and d the sums of dt; put(j, h) takes the one in
+// front of the j-th.  First as for any numbers; once more as carried() has it where that left none, or with a power beyond fp32.  (With carried() at once: 512
+// chunks of 672 channels x 16 states 20.5 us for 18.6.)
+template <typename F>
+__device__ __forceinline__ float carry_over(const float (&v)[kCarryAhead], const float (&d)[kCarryAhead], int count, float decay, float h, F&& put) {
+  const float front = h;
+  float most = 0.f;
+#pragma unroll
+  for (int j = 0; j < kCarryAhead; ++j)
+    if (j < count) {
+      const float z = d[j] * decay;
+      most = fmaxf(most, z);
+      put(j, h);
+      h = fmaf(__builtin_amdgcn_exp2f(z), h, v[j]);
+    }
+  if (h != h || most > 127.f) {
+    h = front;
+#pragma unroll
+    for (int j = 0; j < kCarryAhead; ++j)
+      if (j < count) {
+        put(j, h);
+        h = carried(d[j] * decay, h, v[j]);
+      }
+  }
+  return h;
+}
+
+// values: of all chunks, in their order of walking, `step` apart, and so the sums `sum_step`.  Leaves the state in front of each in its place; what lies behind
+// the last one is not needed, and in the forward pass not there.
 __device__ __forceinline__ void carry_runs(float* values, int64_t step, const float* total, int64_t sum_step, int count, float decay, float h,
                                            bool valid, float (*fold)[2][kWave]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int share = (count + waves - 1) / waves, lo = min(wave * share, count), hi = min(lo + share, count);
+  const int steps = count - 1, share = (steps + waves - 1) / waves, lo = min(wave * share, steps), hi = min(lo + share, steps);
   if (waves > 1) {
     float end = 0.f, sum = 0.f;
     for (int k = lo; k < hi; k += kCarryAhead) {
@@ -472,10 +502,8 @@ __device__ __forceinline__ void carry_runs(float* values, int64_t step, const fl
       }
 #pragma unroll
       for (int j = 0; j < kCarryAhead; ++j)
-        if (k + j < hi) {
-          end = carried(d[j] * decay, end, v[j]);
-          sum += d[j];
-        }
+        if (k + j < hi) sum += d[j];
+      end = carry_over(v, d, hi - k, decay, end, [](int, float) {});
     }
     __syncthreads();
     fold[wave][0][lane] = end;
@@ -491,13 +519,11 @@ __device__ __forceinline__ void carry_runs(float* values, int64_t step, const fl
       v[j] = values[i * step];
       d[j] = total[i * sum_step];
     }
-#pragma unroll
-    for (int j = 0; j < kCarryAhead; ++j)
-      if (k + j < hi) {
-        if (valid) values[(k + j) * step] = h;
-        h = carried(d[j] * decay, h, v[j]);
-      }
+    h = carry_over(v, d, hi - k, decay, h, [&](int j, float front) {
+      if (valid) values[(k + j) * step] = front;
+    });
   }
+  if (valid && lo < hi && hi == steps) values[steps * step] = h;
 }
 
 template <bool BACKWARD>
@@ -799,10 +825,12 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
   const int sum_of = p.lane / (kWave / (4 * NP)), value = sum_of % (2 * NP);
   float* const shared_to = shared_parts + (p.batch * s.groups * s.blocks + p.block) * s.rows * row_size + (sum_of < 2 * NP ? row_size : 0) +
                            p.part * NP + (value < NP ? value : NP * WAVES + value - NP);
-  float* const part_to = parts + (p.batch * s.chunks + p.chunk) * (s.states + 2) * s.channels;
   float start[NP];                                  // the state in front of the chunk
   if (s.chunks > 1) load_slots<NP, WAVES>(s, p, ends, start);
   else load_states<NP>(s, p, h0, start);
+  bool odd = false;                                 // zero or infinite for a lane of the wave
+#pragma unroll
+  for (int n = 0; n < NP; ++n) odd |= __any(start[n] + start[n] == start[n]);
   // this wave's steps of the turn ahead, and the marks in front of that
   T xn[SHARE], dn[SHARE], gn[SHARE], on[SHARE];
   float mark[NP], mark_sum = 0.f;
@@ -828,10 +856,12 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
       }
     }
   };
-  if (turns > 0) request(turns - 1);
-  for (int i = turns - 1; i >= 0; --i) {
+  // A turn.  ENDS: the sequence ends in it, and steps beyond that leave everything as it is.  (Infinity times the zeros that stand for them would not.  It is the
+  // first one walked, outside the loop: a branch around every step of every turn took 1170 us for 1140.)
+  auto walk = [&](int i, auto ends) {
+    constexpr bool ENDS = decltype(ends)::value;
     const int64_t t = p.from + i * U;
-    const int last = last_of(p, t);
+    const int last = ENDS ? last_of(p, t) : U - 1;
     const Shared at = rows + t * row_size;
     T xv[SHARE], dv[SHARE], gv[SHARE], ov[SHARE];
     float slope[SHARE], through[SHARE];
@@ -879,7 +909,7 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
 #pragma unroll
     for (int n = 0; n < NP; ++n) hs[0][n] = i > 0 ? fmaf(__builtin_amdgcn_exp2f(mark_sum * decay[n]), start[n], mark[n]) : start[n];
     pin(hs[0]);
-    if (i > 0 && any_nan(hs[0])) {                  // (infinity and zero may have met)
+    if (odd && i > 0 && has_nan(hs[0])) {                  // (infinity and zero may have met)
 #pragma unroll
       for (int n = 0; n < NP; ++n) hs[0][n] = carried(mark_sum * decay[n], start[n], mark[n]);
       pin(hs[0]);
@@ -934,33 +964,35 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
           const bool sums = j % 2 == 1 && j < U - 1;
           if (sums) behind.request(room, p.lane);
           else ahead(k);
-          float y = 0.f, along = 0.f, step = 0.f;
-          float totals[NP];
+          if (!ENDS || j <= last) {
+            float y = 0.f, along = 0.f, step = 0.f;
+            float totals[NP];
 #pragma unroll
-          for (int q = 0; q < (N + 3) / 4; ++q) {
-            F32<4> g4 = {};
+            for (int q = 0; q < (N + 3) / 4; ++q) {
+              F32<4> g4 = {};
 #pragma unroll
-            for (int i = 0; i < 4 && 4 * q + i < N; ++i) g4[i] = g[4 * q + i];
-            g4 = add_products<NP>(c_of, j, q, dy[j], g4);
+              for (int i = 0; i < 4 && 4 * q + i < N; ++i) g4[i] = g[4 * q + i];
+              g4 = add_products<NP>(c_of, j, q, dy[j], g4);
 #pragma unroll
-            for (int i = 0; i < 4 && 4 * q + i < N; ++i) totals[4 * q + i] = g4[i];
+              for (int i = 0; i < 4 && 4 * q + i < N; ++i) totals[4 * q + i] = g4[i];
+            }
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+              const float total = totals[n];
+              y = fmaf(group.row[k].c[n], hs[j + 1][n], y);
+              pair[n * kSumRow] = total * u[j];
+              pair[(NP + n) * kSumRow] = dy[j] * hs[j + 1][n];
+              along = fmaf(total, group.row[k].b[n], along);
+              g[n] = total * e[j][n];
+              const float back = g[n] * hs[j][n];
+              step = fmaf(back, decay[n], step);
+              da[n] = fmaf(back, dt[j], da[n]);
+            }
+            float* const to = add + (p.part * U + j) * 3 * kWave;
+            to[0] = y;
+            to[kWave] = along;
+            to[2 * kWave] = step;
           }
-#pragma unroll
-          for (int n = 0; n < N; ++n) {
-            const float total = totals[n];
-            y = fmaf(group.row[k].c[n], hs[j + 1][n], y);
-            pair[n * kSumRow] = total * u[j];
-            pair[(NP + n) * kSumRow] = dy[j] * hs[j + 1][n];
-            along = fmaf(total, group.row[k].b[n], along);
-            g[n] = total * e[j][n];
-            const float back = g[n] * hs[j][n];
-            step = fmaf(back, decay[n], step);
-            da[n] = fmaf(back, dt[j], da[n]);
-          }
-          float* const to = add + (p.part * U + j) * 3 * kWave;
-          to[0] = y;
-          to[kWave] = along;
-          to[2 * kWave] = step;
           if (sums) {
             shared_to[(t + j + 1) * row_size] = behind.sum();
             ahead(k);
@@ -971,14 +1003,6 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
       behind.request(room, p.lane);
       shared_to[t * row_size] = behind.sum();
     });
-    if (last < U - 1) {               // (the turn in which the sequence ends)
-      const LaneOf lane(p);
-#pragma unroll
-      for (int n = 0; n < NP; ++n) {
-        if (p.valid && n < own) lane.of(part_to + (p.part * NP + n) * s.channels) = da[n];
-        da[n] = 0.f;
-      }
-    }
     if (WAVES > 1) __syncthreads();
     const LaneOf done(p);
 #pragma unroll
@@ -1002,55 +1026,13 @@ __global__ __launch_bounds__(WAVES * kWave, NP == 4 && WAVES > 2 ? 3 : 2) void s
       if (gs) done.of(dgate + p.batch * s.dgate_b + (t + j) * s.dgate_t) = (T)(fmaf(skip, xt, y) * through[k]);
     }
     if (WAVES > 1) __syncthreads();      // common and add are written again
-  }
-  float* const to = part_to;
+  };
+  if (turns > 0) request(turns - 1);
+  const bool whole = (p.end - p.from) % U == 0;
+  if (turns > 0 && !whole) walk(turns - 1, std::true_type());
+  for (int i = turns - (whole ? 1 : 2); i >= 0; --i) walk(i, std::false_type());
+  float* const to = parts + (p.batch * s.chunks + p.chunk) * (s.states + 2) * s.channels;
   const LaneOf lane(p);
-  // What the turn in which the sequence ends gave to grad_a: there steps beyond the sequence have products of zero with its last state and that one's gradient.
-  // Where these are infinite it is worked out again, without them.  (A branch around every step of every turn instead: 8 x 4096 x 2048 bf16 1170 us for 1140.)
-  if ((p.end - p.from) % U != 0 && p.end > p.from) {
-    float ends_with[NP];
-#pragma unroll
-    for (int n = 0; n < NP; ++n) ends_with[n] = n < own ? lane.of(part_to + (p.part * NP + n) * s.channels) : 0.f;
-    if (any_nan(ends_with)) {
-      const int64_t t = p.from + (turns - 1) * U;
-      float back[NP];
-      if (s.chunks > 1) load_slots<NP, WAVES>(s, p, starts, back);
-      else load_states<NP>(s, p, dlast, back);
-#pragma unroll
-      for (int n = 0; n < NP; ++n) ends_with[n] = 0.f;
-      for (int64_t j = p.end - 1; j >= t; --j) {
-        float front[NP], dt_of = 0.f;
-#pragma unroll
-        for (int n = 0; n < NP; ++n) front[n] = start[n];
-        if (turns > 1) {
-          const float* const mark_at = marks_of<NP, WAVES>(s, p, marks, t);
-          const float passed = lane.of(mark_at + (WAVES - p.part) * NP * s.channels);
-#pragma unroll
-          for (int n = 0; n < NP; ++n) front[n] = carried(passed * decay[n], start[n], lane.of(mark_at + n * s.channels));
-        }
-        for (int64_t k = t; k <= j; ++k) {
-          const float raw = (float)lane.of(ds + k * s.delta_t) + shift;
-          dt_of = s.softplus ? softplus(raw).value : raw;
-          const float u = dt_of * (float)lane.of(xs + k * s.x_t);
-#pragma unroll
-          for (int n = 0; n < NP; ++n)
-            if (k < j) front[n] = fmaf(__builtin_amdgcn_exp2f(dt_of * decay[n]), front[n], held_rows[k * row_size + n] * u);
-        }
-        float dy = (float)lane.of(os + j * s.out_t);
-        if (gs) {
-          const float gt = (float)lane.of(gs + j * s.gate_t);
-          dy *= gt * sigmoid(gt).a;
-        }
-#pragma unroll
-        for (int n = 0; n < NP; ++n) {
-          back[n] = fmaf(held_rows[j * row_size + NP * WAVES + n], dy, back[n]) * __builtin_amdgcn_exp2f(dt_of * decay[n]);
-          ends_with[n] = fmaf(back[n] * front[n], dt_of, ends_with[n]);
-        }
-      }
-    }
-#pragma unroll
-    for (int n = 0; n < NP; ++n) da[n] += ends_with[n];
-  }
   if (p.valid) {
 #pragma unroll
     for (int n = 0; n < NP; ++n) {

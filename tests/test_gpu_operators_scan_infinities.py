@@ -89,6 +89,21 @@ def test_infinite_gradients_stay_infinite(steps, fall, states, kind):
     assert np.isposinf(refs["h0"][0, 69]).all() and np.isposinf(refs["x"][1, :steps // 2 + 1, 4]).all() and np.isposinf(refs["x"][2, :, 69]).all()
 
 
+@pytest.mark.parametrize("states", [5, 16])
+def test_channels_beside_an_infinite_one_keep_their_bits(states):
+    s = positive(2, 700, 70, states, fall=2.0)
+    before = (*forward(s), *(v for k, v in backward(s).items() if k not in ("b", "c")))
+    s["x"][0, 100, 7], s["h0"][0, 7], s["dout"][0, 600, 7], s["dlast"][1, 7] = INF, INF, INF, INF
+    after = (*forward(s), *(v for k, v in backward(s).items() if k not in ("b", "c")))
+    for a, b in zip(before, after):
+        if a is None:
+            continue
+        axis = list(a.shape).index(70)
+        others = torch.tensor([c for c in range(70) if c != 7], device=a.device)
+        assert torch.equal(a.index_select(axis, others), b.index_select(axis, others))
+        assert not torch.isfinite(b.select(axis, 7)).all()
+
+
 def test_infinite_states_by_many_waves_and_by_lengths():
     """Chunks of the longest kind, and beside the infinite sequences some that end before them.  (The infinite ones are whole: the definition's sums have zeros behind
     a sequence's end, and 64 bits make NaN of these and infinity too.)"""
