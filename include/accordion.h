@@ -447,7 +447,7 @@ int32_t accordion_recurrence_backward(const acc_recurrence* cfg, const void* gat
 
 /* Short causal convolution of every channel along a sequence.
  *   forward:   u_t = bias + sum_j weight[j] x_{t - width + 1 + j} (j from 0 to width - 1),
- *              out_t = u_t, or u_t / (1 + exp(-u_t)) with silu
+ *              out_t = u_t, or u_t / (1 + exp(-u_t)) with silu (exp(u_t) below the normal fp32 numbers counts as zero)
  *   backward:  g_t = grad_out_t du, du = 1 or the derivative of silu at u_t (u is computed again from x),
  *              grad_x_t = sum_j weight[j] g_{t + width - 1 - j} (+ grad_last's row, where x_t is one of last's),
  *              grad_weight[j] = sum over sequences and t of g_t x_{t - width + 1 + j}, grad_bias = sum of g_t,
@@ -496,15 +496,15 @@ int32_t accordion_convolution_backward(const acc_convolution* cfg, const void* x
  *              grad_delta_bias = sum of grad_delta_t, grad_h0 = e_0 G_0
  *              (the states are computed again from the inputs: nothing is kept from the forward pass)
  * a_dev is channels x states, d_dev and delta_bias_dev (NULL: zeros) channels, contiguous fp32, and so are their gradients;
- * a is finite (negative, unless states are to grow; where they do, by more than the fp32 numbers hold within 256 steps, results
- * may be NaN).  b and c have a row of groups x states elements per step: channels [i channels / groups, (i + 1) channels / groups)
+ * a is finite (negative, unless states are to grow; where they do, by more than the fp32 numbers hold within 256 steps, gradients
+ * may be infinite or NaN).  b and c have a row of groups x states elements per step: channels [i channels / groups, (i + 1) channels / groups)
  * take the i-th part of it.  gate_dev may be NULL, and grad_gate_dev then is.
  * h0_dev (NULL: zeros), h_last_dev, grad_last_dev (NULL: zeros) and grad_h0_dev are batch x channels x states, contiguous fp32.
  * h_last_dev, grad_h0_dev, grad_d_dev and grad_delta_bias_dev may be NULL; the last two need d_dev and delta_bias_dev.
  * lengths_dev as for the recurrence: steps from a sequence's length on write zeros and leave the state as it is; what
  * their inputs hold plays no role.  steps = 1 is the serving form: one token, the state in h0 and h_last (which may be the same buffer
  * then, and for any number of steps).
- * exp(dt a) below the normal fp32 numbers counts as zero, products and states below them may.
+ * exp(dt a) below the normal fp32 numbers counts as zero, and so do exp(gate) and exp(delta + delta_bias); products and states below them may.
  * What is infinite among inputs, states and gradients makes infinite what the formulas make infinite of it, however many steps lie between; only through
  * a step whose exp(dt a) counts as zero an infinite state, or gradient of one, may be infinite or NaN.
  * More than 16 steps, and backward: batch x groups x steps x states, filled up to 4, 8, 16, 32 or 64, below 1.5e9. */

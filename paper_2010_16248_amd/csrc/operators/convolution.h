@@ -27,10 +27,10 @@ __device__ __forceinline__ void row_store(T* p, const F32<N>& v, int64_t left) {
   else store_some<T, N>(p, v, left);
 }
 
-// What a lane has: N channels of a run of steps of a sequence.  FULL: a wave has one run, so that all but the channel lies in its scalar registers, and every
-// pack is whole, as it may be without: the last one of a row that is not a multiple of N starts among the channels of the one in front, whose results it makes once more, the
-// same ones.  (Single elements there cost every wave of the row's end a second path: 55 x 3025 x 455 bf16 forward 177 us, backward 276, with whole
-// packs 74 and 176; 55 x 3025 x 125 44 and 92, with whole ones 28 and 52.)
+// What a lane has: N channels of a run of steps of a sequence.  FULL: a wave has one run, so that all but the channel lies in its scalar
+// registers, and every pack is whole, as it may be without: the last one of a row that is not a multiple of N starts among the channels of the
+// one in front, whose results it makes once more, the same ones.  (Single elements there cost every wave of the row's end a second path:
+// 55 x 3025 x 455 bf16 forward 177 us, backward 276, with whole packs 74 and 176; 55 x 3025 x 125 44 and 92, with whole ones 28 and 52.)
 struct ConvolutionPlace {
   int64_t batch, run, channel, left;      // left: channels from its first one on
 };
@@ -92,8 +92,10 @@ __device__ __forceinline__ F32<N> weighed(const F32<N> (&w)[W], const F32<N>* v,
 
 // ---- forward ----------------------------------------------------------------------------------------------
 // A lane takes N channels through a run of steps: the inputs slide through its registers, each is read once (the first W - 1 of a run
-// twice).  Bound by memory where there is work: width 4, SiLU, 8 x 4096 x 4096 bf16 106 us, 5.1 TB/s, the rate of a large copy; 7 x 1999 x 1001 fp32,
-// width 3, ragged 17.5 us, 4.8 TB/s.  One token of 64 x 1344 channels: 6.2 us, nearly all of it one wait for weights, state and input.
+// twice).  Bound by memory where there is work: width 4, SiLU, 8 x 4096 x 4096 bf16 106 us, 5.1 TB/s, the rate of a large copy; 7 x 1999 x 1001
+// fp32, width 3, ragged 17.5 us, 4.8 TB/s where the inputs are still in the Infinity Cache.  A turn's inputs are not under way during the turn
+// in front, which other waves have to cover.  One token of 64 x 1344 channels: 6.2 us, nearly all of it two waits, one for weights, state and
+// input and one for the input that last takes once more.
 constexpr int kConvolutionAhead = 4;   // steps under way
 
 template <typename T, int N, int W, bool FULL>

@@ -50,11 +50,14 @@ constexpr int64_t kScanWalkSteps = 16;
 // chunks 691 and with chunks of 128 548, and of one length 804 and 892; fp32 29 x 4370 x 1159 (2204) 899 and 690, 1085 and 1187; 64 x 2048 x 1024 (4096) 563
 // and 562, 631 and 891; 64 x 512 x 512 (2048) 102 and 118.
 constexpr int64_t kScanRagged = 2048;
+// (256 steps are no slower where they too leave kScanWaves waves: 8 x 4096 x 2048 459 us for 464.  The rule stops at 128.)
 constexpr int64_t kScanFew = 64, kScanLone = 2048, kScanWaves = 4096, kScanShortest = 32, kScanLongest = 128;
 // Chunks of the backward pass: as long as leave this many workgroups and waves, from 16 to 256 steps.  us with chunks of 16, 32, 64, 128, 256 steps, bf16:
 // 16 states (4 waves) 1 x 512 x 1536 (24 workgroups per chunk) 41, 44, 49, 79, 139; 2 x 2048 x 768 (24) 102, 87, 84, 106, 143; 4 x 1024 x 1536 (96) 166,
 // 148, 138, 138, 189; 64 x 128 x 512 (512) 117, 107, 107, 105; 8 x 4096 x 2048 (256) 1730, 1359, 1195, 1155, 1132; 4 states (1 wave) 64 x 512 x 1024 (1024)
-// 411, 354, 330, 331, 349; 64 states (8 waves) 2 x 2048 x 768 (24) 347, 274, 251, 299, 300.
+// 411, 354, 330, 331, 349; 64 states (8 waves) 2 x 2048 x 768 (24) 347, 274, 251, 299, 300.  Longer ones were not measured.  Next to the border of
+// kBackwardWaves neither side is the better one throughout: 4 states 47 x 1024 x 1024 in chunks of 256 (3008 waves) 514 and of 128 466, 188 x 200 x 1024
+// (3008) 401 and 462; 8 states (2 waves) 25 x 1024 x 960 (3000) 410 and 338.
 constexpr int64_t kBackwardGroups = 768, kBackwardWaves = 3000, kBackwardShortest = 16, kBackwardLongest = 256;
 
 struct ScanPlan {
